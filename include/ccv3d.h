@@ -400,6 +400,135 @@ ccv3d_status ccv3d_forward_ring_up(ccv3d_handle* h, const ccv3d_ring* in, int32_
                                    const ccv3d_ring* res, int32_t res_slot, const ccv3d_ring* out_ring, int32_t out_slot,
                                    int32_t rt, int32_t T, void* stream);
 
+/*
+ * ------------------------------------------------------------------------------------------------
+ * Token operators: the transformer in front of a streamed decoder
+ * ------------------------------------------------------------------------------------------------
+ * The latents that a causal video decoder turns into frames are predicted chunk by chunk by a transformer (the
+ * "transformer" stage of the paper's Section 5.2 pipelines), whose attention keeps a temporal cache of its own: the
+ * keys and values of every token so far.  The calls below are what such a transformer needs next to its matrix
+ * products: a paged cache of keys and values in 8 bits (append, attend) and the norms around its blocks.
+ *
+ * A cache is a pool of pages of page_tokens tokens.  codes[page][j][head][token][dim] holds keys (j = 0) and values
+ * (j = 1) as E4M3 (sign, 4 exponent bits, 3 mantissa bits; largest magnitude 448; 0x7F and 0xFF are NaN), and
+ * scales[page][j][head] one FP32 scale for each page and head: a key or value is code * scale.  ccv3d_kv_append only
+ * writes powers of two, so moving a page to a larger scale is exact (but for codes that fall under the smallest
+ * normal E4M3 number): a cache filled token by token and one filled in one call hold the same bits otherwise.
+ */
+typedef struct {
+    void*   codes;           /* DEVICE uint8 [pages][2][kv_heads][page_tokens][head_dim], 16-byte aligned; the caller's */
+    float*  scales;          /* DEVICE [pages][2][kv_heads]; the caller's.  Need not be initialised before the first append. */
+    int32_t pages, kv_heads;
+    int32_t page_tokens;     /* 16, 32, 64 or 128 */
+    int32_t head_dim;        /* 64 or 128 */
+} ccv3d_kv_cache;
+
+/* The sequences of one call: sequence b brings new_start[b+1] - new_start[b] new tokens, packed one sequence behind the
+ * other, as the last ones of its total[b] cached tokens (both calls take the lengths INCLUDING the new tokens), and its
+ * token at position p lies in page page_table[b][p / page_tokens].  All pointers DEVICE.  Pages must not be shared by
+ * two sequences of an append where both write them; reading shared pages is fine.
+ * These arrays are checked by the kernels: entries out of range (a page outside the pool, offsets that fall or pass
+ * `tokens`, more tokens than max_pages pages hold) are skipped or cut, never followed, and reported in the status word. */
+typedef struct {
+    const int32_t* new_start;    /* [batch + 1] */
+    const int32_t* total;        /* [batch] */
+    const int32_t* page_table;   /* [batch][max_pages] */
+    int32_t batch, max_pages;
+    int32_t tokens;              /* rows of the packed tensors, >= new_start[batch] (rows past it have no sequence: attend does not
+                                    write them) */
+    int32_t max_new;             /* most new tokens of any sequence (a bound; picks the kernel and its grid) */
+} ccv3d_token_batch;
+
+/* A packed [tokens, heads, head_dim] tensor, dim contiguous, strides in elements (a slice of a fused projection).
+ * data and both strides must be multiples of 16 bytes. */
+typedef struct {
+    void*   data;            /* DEVICE */
+    int64_t token_stride, head_stride;
+} ccv3d_heads;
+
+/* Position rotation: pair i (of `pairs` <= head_dim / 2, a multiple of 4) of a token turns by the angle whose cosine and
+ * sine stand at [positions[token][axis(i)]][i]; the first section[0] pairs go by axis 0, the next section[1] by axis 1, ...
+ * A text or frame-less stream has one axis; a video stream turns by (frame, row, column).  Pair i is elements
+ * (i, i + pairs), or (2i, 2i + 1) if interleaved; elements from 2 * pairs on stay as they are. */
+typedef struct {
+    const float*   cos_table;    /* DEVICE [rows][pairs], 16-byte aligned */
+    const float*   sin_table;    /* DEVICE [rows][pairs], 16-byte aligned */
+    const int32_t* positions;    /* DEVICE [tokens][axes]; entries outside 0 .. rows-1 are cut and reported */
+    int32_t rows, pairs;
+    int32_t axes;                /* 1 .. 3 */
+    int32_t section[3];          /* pairs of each axis; they sum to `pairs` */
+    int32_t interleaved;
+} ccv3d_rotary;
+
+/* What a kernel reported (the caller's DEVICE word, zeroed by the caller; a kernel only ever ORs bits in). */
+#define CCV3D_TOKENS_BAD_PAGE 0x1u       /* a page index outside the pool: its tokens were not written / read as absent */
+#define CCV3D_TOKENS_BAD_LENGTH 0x2u     /* new_start or total out of range: cut */
+#define CCV3D_TOKENS_BAD_POSITION 0x4u   /* a position outside the rotation table: cut */
+#define CCV3D_TOKENS_TIMEOUT 0x8u        /* a bounded wait gave up: the outputs of that call are undefined */
+
+/*
+ * Append: k and v [tokens, kv_heads, head_dim] in `dtype` go into the cache, k rotated on the way (rot != NULL), and
+ * q [tokens, q_heads, head_dim] is rotated into q_out (both NULL: no q).  Rotation is in FP32, products and sums each
+ * rounded; q_out is rounded once; k and v are rounded once, to E4M3 under their page's scale.
+ * The scale of a page and head is the smallest power of two (not under 2^-64) under which every finite value it has
+ * been given fits into +-448.  A page whose first token is among the new ones starts afresh; else it keeps at least its
+ * scale, and where the new tokens need a larger one its older codes are moved to it.  Infinities are stored as +-448,
+ * NaN as NaN; neither takes part in the scale.
+ * q_out may be q itself (same strides); any other overlap of an output with an input is CCV3D_ERR_ALIAS.
+ * Stream-ordered, one kernel, no allocation, legal in a stream capture.
+ */
+ccv3d_status ccv3d_kv_append(const ccv3d_kv_cache* cache, const ccv3d_token_batch* batch, const ccv3d_heads* k,
+                             const ccv3d_heads* v, const ccv3d_rotary* rot, const ccv3d_heads* q,
+                             const ccv3d_heads* q_out, int32_t q_heads, int32_t dtype, uint32_t* status, void* stream);
+
+/*
+ * Attend: out[token, head] = sum_t softmax_t(scale * q[token, head] . key[t, kv]) value[t, kv] over the cached tokens t
+ * that the token sees, kv = head / (q_heads / kv_heads); lse (may be NULL) receives the natural log of the sum of
+ * exponentials, [tokens, q_heads] FP32.  The token at position p of a sequence of `total` tokens sees
+ *   frame = 0:  every token;   frame = f >= 1: the tokens before the end of its frame of f tokens (1: causal; the tokens of
+ *               a latent frame: causal in frames, whole within one - the temporal rule of the cached convolutions);
+ *   window >= 0: none that lies more than `window` tokens before the start of its own frame (frame = 0: before itself).
+ * A token that sees nothing (more new tokens than cached ones) gets zeros and lse = -infinity.  What a token does not
+ * see (stale codes at a page's end, NaN included) has no part in its result.
+ * q, out: `dtype` (BF16 or F32; F32 is computed to FP32 accuracy).  Scores, softmax statistics and sums are FP32.
+ *   q_heads   a multiple of kv_heads
+ *   ws        DEVICE scratch, 256-byte aligned, ccv3d_kv_attend_workspace() bytes; holds data within the call only,
+ *             calls that may overlap on the GPU need one each
+ * out must not overlap q.  Stream-ordered, no allocation, legal in a stream capture.
+ */
+ccv3d_status ccv3d_kv_attend(const ccv3d_kv_cache* cache, const ccv3d_token_batch* batch, const ccv3d_heads* q,
+                             const ccv3d_heads* out, float* lse, int32_t q_heads, int32_t dtype, float scale,
+                             int32_t frame, int32_t window, void* ws, uint64_t ws_bytes, uint32_t* status, void* stream);
+/* Bytes of scratch that such a call needs on the current device (HOST output). */
+ccv3d_status ccv3d_kv_attend_workspace(const ccv3d_kv_cache* cache, const ccv3d_token_batch* batch, int32_t q_heads,
+                                       int32_t dtype, uint64_t* bytes_host);
+
+/*
+ * The norms on both sides of a residual sum, with the block's gate and the residual's scale between them:
+ *   r = residual_scale * x + gate * post(y)          post(y) = norm(y) * post_weight + post_bias
+ *   h = pre(r) * (1 + scale) + shift                 pre(r)  = norm(r) * pre_weight + pre_bias
+ * over rows of `channels`; norm is the division by the root mean square (RMS), the same after the mean is taken off
+ * (LAYER), or nothing (NONE), with eps added to the mean square.  gate, scale and shift stand for groups of rows (the
+ * conditioning of a sample or frame): row i reads group i / rows_per_group.  Any of y, gate, the weights and biases,
+ * scale and shift may be NULL (y: r = residual_scale * x), and either of r and h, not both.
+ * x and r are in res_dtype, y and h in act_dtype, weights and biases in weight_dtype, gate, scale and shift in mod_dtype.
+ * All arithmetic is FP32, h is formed from the unrounded r, each output is rounded once.
+ * r may be x itself and h may be y itself (same strides); any other overlap of an output is CCV3D_ERR_ALIAS.
+ */
+typedef enum { CCV3D_NORM_NONE = 0, CCV3D_NORM_RMS = 1, CCV3D_NORM_LAYER = 2 } ccv3d_norm_kind;
+typedef struct {
+    int32_t rows, channels;            /* channels <= 16384; rows = 0 is a call without work */
+    int32_t rows_per_group;            /* >= 1 */
+    int32_t post_kind, pre_kind;       /* ccv3d_norm_kind */
+    int32_t res_dtype, act_dtype, weight_dtype, mod_dtype;
+    float   residual_scale, eps;
+    int64_t x_stride, y_stride, r_stride, h_stride;   /* elements between rows, >= channels */
+    int64_t gate_stride, scale_stride, shift_stride;  /* elements between groups */
+} ccv3d_norm_desc;
+ccv3d_status ccv3d_gated_norm(const ccv3d_norm_desc* d, const void* x, const void* y, const void* post_weight,
+                              const void* post_bias, const void* gate, const void* pre_weight, const void* pre_bias,
+                              const void* scale, const void* shift, void* r, void* h, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -50,12 +50,53 @@ class Ring(ctypes.Structure):
                 ("H", ctypes.c_int32), ("W", ctypes.c_int32), ("KB", ctypes.c_int32)]
 
 
+NORM_NONE, NORM_RMS, NORM_LAYER = range(3)
+TOKENS_BAD_PAGE, TOKENS_BAD_LENGTH, TOKENS_BAD_POSITION, TOKENS_TIMEOUT = 1, 2, 4, 8
+
+
+class KvCache(ctypes.Structure):
+    """ccv3d_kv_cache: a pool of pages of E4M3 keys and values with a scale for each page and head."""
+    _fields_ = [("codes", ctypes.c_void_p), ("scales", ctypes.c_void_p), ("pages", ctypes.c_int32),
+                ("kv_heads", ctypes.c_int32), ("page_tokens", ctypes.c_int32), ("head_dim", ctypes.c_int32)]
+
+
+class TokenBatchC(ctypes.Structure):
+    """ccv3d_token_batch: the sequences of one call (device arrays)."""
+    _fields_ = [("new_start", ctypes.c_void_p), ("total", ctypes.c_void_p), ("page_table", ctypes.c_void_p),
+                ("batch", ctypes.c_int32), ("max_pages", ctypes.c_int32), ("tokens", ctypes.c_int32),
+                ("max_new", ctypes.c_int32)]
+
+
+class Heads(ctypes.Structure):
+    """ccv3d_heads: a packed [tokens, heads, dim] tensor with strides in elements."""
+    _fields_ = [("data", ctypes.c_void_p), ("token_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64)]
+
+
+class RotaryC(ctypes.Structure):
+    """ccv3d_rotary: position rotation by a table of cosines and sines over one to three axes."""
+    _fields_ = [("cos_table", ctypes.c_void_p), ("sin_table", ctypes.c_void_p), ("positions", ctypes.c_void_p),
+                ("rows", ctypes.c_int32), ("pairs", ctypes.c_int32), ("axes", ctypes.c_int32),
+                ("section", ctypes.c_int32 * 3), ("interleaved", ctypes.c_int32)]
+
+
+class NormDesc(ctypes.Structure):
+    """ccv3d_norm_desc: geometry, kinds and types of a gated-norm call."""
+    _fields_ = [("rows", ctypes.c_int32), ("channels", ctypes.c_int32), ("rows_per_group", ctypes.c_int32),
+                ("post_kind", ctypes.c_int32), ("pre_kind", ctypes.c_int32),
+                ("res_dtype", ctypes.c_int32), ("act_dtype", ctypes.c_int32), ("weight_dtype", ctypes.c_int32),
+                ("mod_dtype", ctypes.c_int32), ("residual_scale", ctypes.c_float), ("eps", ctypes.c_float),
+                ("x_stride", ctypes.c_int64), ("y_stride", ctypes.c_int64), ("r_stride", ctypes.c_int64),
+                ("h_stride", ctypes.c_int64), ("gate_stride", ctypes.c_int64), ("scale_stride", ctypes.c_int64),
+                ("shift_stride", ctypes.c_int64)]
+
+
 EXPORTS = ("ccv3d_create", "ccv3d_forward", "ccv3d_forward_host", "ccv3d_workspace_bytes", "ccv3d_destroy",
            "ccv3d_get_counters", "ccv3d_device_status", "ccv3d_status_string", "ccv3d_add_bf16",
            "ccv3d_upsample_bf16", "ccv3d_profile_enable", "ccv3d_profile_read", "ccv3d_forward_static", "ccv3d_selftest_wait_timeout", "ccv3d_forward_ex",
            "ccv3d_ring_kb", "ccv3d_ring_bytes", "ccv3d_ring_load", "ccv3d_ring_store", "ccv3d_upsample_ring",
            "ccv3d_forward_ring", "ccv3d_out_dims", "ccv3d_forward_ring_up", "ccv3d_rows_copy",
-           "ccv3d_forward_host_stream", "ccv3d_set_workspace")
+           "ccv3d_forward_host_stream", "ccv3d_set_workspace",
+           "ccv3d_kv_append", "ccv3d_kv_attend", "ccv3d_kv_attend_workspace", "ccv3d_gated_norm")
 
 
 def _load() -> ctypes.CDLL:
@@ -95,6 +136,11 @@ def _load() -> ctypes.CDLL:
     lib.ccv3d_upsample_ring.argtypes = [rp, i32, rp, i32, i32, i32, vp]
     lib.ccv3d_forward_ring.argtypes = [vp, rp, i32, i32, rp, i32, rp, i32, vp, i32, vp]
     lib.ccv3d_forward_ring_up.argtypes = [vp, rp, i32, i32, rp, i32, rp, i32, i32, i32, vp]
+    cp, tp, hp = ctypes.POINTER(KvCache), ctypes.POINTER(TokenBatchC), ctypes.POINTER(Heads)
+    lib.ccv3d_kv_append.argtypes = [cp, tp, hp, hp, ctypes.POINTER(RotaryC), hp, hp, i32, i32, vp, vp]
+    lib.ccv3d_kv_attend_workspace.argtypes = [cp, tp, i32, i32, u64p]
+    lib.ccv3d_kv_attend.argtypes = [cp, tp, hp, hp, vp, i32, i32, ctypes.c_float, i32, i32, vp, ctypes.c_uint64, vp, vp]
+    lib.ccv3d_gated_norm.argtypes = [ctypes.POINTER(NormDesc)] + [vp] * 12
     for name in EXPORTS:
         if name not in ("ccv3d_status_string", "ccv3d_ring_bytes"):
             getattr(lib, name).restype = ctypes.c_int
@@ -256,6 +302,29 @@ def ccv3d_forward_ring_up(h, rin: Ring, x_slot: int, hist_frames: int, res: Ring
     return lib.ccv3d_forward_ring_up(h, ctypes.byref(rin), x_slot, hist_frames,
                                      None if res is None else ctypes.byref(res), res_slot, ctypes.byref(out_ring),
                                      out_slot, rt, T, stream)
+
+
+def ccv3d_kv_append(cache: KvCache, batch: TokenBatchC, k: Heads, v: Heads, rot: RotaryC | None, q: Heads | None,
+                    q_out: Heads | None, q_heads: int, dtype: int, status: int | None = None, stream=0) -> int:
+    return lib.ccv3d_kv_append(cache, batch, k, v, rot, q, q_out, q_heads, dtype, status, stream)
+
+
+def ccv3d_kv_attend_workspace(cache: KvCache, batch: TokenBatchC, q_heads: int, dtype: int):
+    """(status, bytes of scratch a ccv3d_kv_attend call of this shape needs)."""
+    b = ctypes.c_uint64()
+    s = lib.ccv3d_kv_attend_workspace(cache, batch, q_heads, dtype, b)
+    return s, b.value
+
+
+def ccv3d_kv_attend(cache: KvCache, batch: TokenBatchC, q: Heads, out: Heads, lse: int | None, q_heads: int, dtype: int,
+                    scale: float, frame: int, window: int, ws: int | None, ws_bytes: int, status: int | None = None,
+                    stream=0) -> int:
+    return lib.ccv3d_kv_attend(cache, batch, q, out, lse, q_heads, dtype, scale, frame, window, ws, ws_bytes, status, stream)
+
+
+def ccv3d_gated_norm(desc: NormDesc, x, y, post_weight, post_bias, gate, pre_weight, pre_bias, scale, shift, r, h,
+                     stream=0) -> int:
+    return lib.ccv3d_gated_norm(desc, x, y, post_weight, post_bias, gate, pre_weight, pre_bias, scale, shift, r, h, stream)
 
 
 class FrameRing:

@@ -1,0 +1,293 @@
+// C entry points of the token operators: argument checks, kernel choice, launches.
+#include "../../include/ccv3d.h"
+
+#include <cuda_bf16.h>
+#include <cuda_runtime.h>
+
+#include <atomic>
+#include <cstdlib>
+
+#include "ccv3d_tokens_append.cuh"
+#include "ccv3d_tokens_attend.cuh"
+#include "ccv3d_tokens_norm.cuh"
+
+using namespace ccv3d;
+
+namespace {
+
+inline int64_t esize(int dt) { return dt == CCV3D_BF16 ? 2 : 4; }
+inline bool dtype_ok(int dt) { return dt == CCV3D_F32 || dt == CCV3D_BF16; }
+inline bool misaligned(const void* p, uintptr_t a) { return ((uintptr_t)p & (a - 1)) != 0; }
+
+ccv3d_status launched() {
+    if (cudaGetLastError() == cudaSuccess) return CCV3D_OK;
+    return CCV3D_ERR_CUDA;
+}
+
+// What the launches need to know of the current device, looked up once for each.
+struct Device { int sm_count; };
+constexpr int MAX_DEVICES = 64;
+std::atomic<int> g_sms[MAX_DEVICES];     // 0: not looked up, < 0: not compute capability 10.x
+
+ccv3d_status current_device(Device* d) {
+    int dev = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= MAX_DEVICES) { cudaGetLastError(); return CCV3D_ERR_CUDA; }
+    int sms = g_sms[dev].load(std::memory_order_relaxed);
+    if (!sms) {
+        int major = 0;
+        if (cudaDeviceGetAttribute(&major, cudaDevAttrComputeCapabilityMajor, dev) != cudaSuccess ||
+            cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) {
+            cudaGetLastError();
+            return CCV3D_ERR_CUDA;
+        }
+        if (major != 10) sms = -1;
+        g_sms[dev].store(sms, std::memory_order_relaxed);
+    }
+    if (sms < 0) return CCV3D_ERR_ARCH;
+    d->sm_count = sms;
+    return CCV3D_OK;
+}
+
+// Byte range of a strided tensor: rows (and heads) with non-negative strides.
+struct Span { uintptr_t a, b; };
+inline Span span_of(const void* p, int64_t bytes) { return {(uintptr_t)p, (uintptr_t)p + (uint64_t)bytes}; }
+inline Span span_of(const ccv3d_heads& h, int64_t tokens, int heads, int dim, int dt) {
+    return span_of(h.data, ((tokens - 1) * h.token_stride + (heads - 1) * h.head_stride + dim) * esize(dt));
+}
+inline bool meet(const Span& x, const Span& y) { return x.a < y.b && y.a < x.b; }
+
+ccv3d_status check_cache(const ccv3d_kv_cache* c) {
+    if (!c || !c->codes || !c->scales || c->pages < 1 || c->kv_heads < 1) return CCV3D_ERR_INVALID_ARG;
+    if (c->page_tokens != 16 && c->page_tokens != 32 && c->page_tokens != 64 && c->page_tokens != 128) return CCV3D_ERR_UNSUPPORTED;
+    if (c->head_dim != 64 && c->head_dim != 128) return CCV3D_ERR_UNSUPPORTED;
+    if (c->kv_heads > 65536) return CCV3D_ERR_UNSUPPORTED;
+    if (misaligned(c->codes, 16) || misaligned(c->scales, 4)) return CCV3D_ERR_ALIGNMENT;
+    return CCV3D_OK;
+}
+
+ccv3d_status check_batch(const ccv3d_token_batch* b, int page_tokens) {
+    if (!b || !b->new_start || !b->total || b->batch < 1 || b->max_pages < 0 || b->tokens < 0 || b->max_new < 0) return CCV3D_ERR_INVALID_ARG;
+    if (!b->page_table && b->max_pages > 0) return CCV3D_ERR_INVALID_ARG;
+    if ((int64_t)b->max_pages * page_tokens > 0x7FFFFFFF || b->batch > 65536) return CCV3D_ERR_UNSUPPORTED;
+    if (misaligned(b->new_start, 4) || misaligned(b->total, 4) || misaligned(b->page_table, 4)) return CCV3D_ERR_ALIGNMENT;
+    return CCV3D_OK;
+}
+
+// `tokens` > 0: an output, whose rows must not lie on one another (token by token or head by head); an input's may (a
+// broadcast head or token).
+ccv3d_status check_heads(const ccv3d_heads* h, int heads, int dim, int dt, int64_t tokens = 0) {
+    if (!h || !h->data || h->token_stride < 0 || h->head_stride < 0) return CCV3D_ERR_INVALID_ARG;
+    if (tokens) {
+        const int64_t ts = tokens > 1 ? h->token_stride : INT64_MAX, hs = heads > 1 ? h->head_stride : INT64_MAX;
+        const bool by_token = hs >= dim && ts >= (heads > 1 ? (heads - 1) * hs : 0) + dim;
+        const bool by_head = ts >= dim && hs >= (tokens > 1 ? (tokens - 1) * ts : 0) + dim;
+        if (!by_token && !by_head) return CCV3D_ERR_INVALID_ARG;
+    }
+    const int64_t unit = 16 / esize(dt);
+    if (misaligned(h->data, 16) || h->token_stride % unit || h->head_stride % unit) return CCV3D_ERR_ALIGNMENT;
+    return CCV3D_OK;
+}
+
+Span codes_span(const ccv3d_kv_cache* c) {
+    return span_of(c->codes, (int64_t)c->pages * 2 * c->kv_heads * c->page_tokens * c->head_dim);
+}
+Span scales_span(const ccv3d_kv_cache* c) { return span_of(c->scales, (int64_t)c->pages * 2 * c->kv_heads * 4); }
+
+template <typename T>
+ccv3d_status launch_append(const AppendParams& p, unsigned grid, cudaStream_t st) {
+    const int D = p.c.head_dim, P = p.c.page_tokens;
+#define CCV3D_APPEND(d, pg) \
+    if (D == d && P == pg) kv_append_kernel<T, d, pg><<<grid, APPEND_THREADS, 0, st>>>(p);
+    CCV3D_APPEND(64, 16) CCV3D_APPEND(64, 32) CCV3D_APPEND(64, 64) CCV3D_APPEND(64, 128)
+    CCV3D_APPEND(128, 16) CCV3D_APPEND(128, 32) CCV3D_APPEND(128, 64) CCV3D_APPEND(128, 128)
+#undef CCV3D_APPEND
+    return launched();
+}
+
+template <typename TX, typename TY>
+ccv3d_status launch_norm(const NormParams& p, bool vec, cudaStream_t st) {
+    const int C = p.d.channels, rows = p.d.rows;
+#define CCV3D_NORM(g, v, k) \
+    { constexpr int per = (g) < 128 ? 128 / (g) : 1; \
+      gated_norm_kernel<TX, TY, g, v, k><<<(rows + per - 1) / per, (g) < 128 ? 128 : (g), 0, st>>>(p); }
+    if (vec) {
+        if (C <= 128) CCV3D_NORM(16, 4, 2)
+        else if (C <= 512) CCV3D_NORM(32, 4, 4)
+        else if (C <= 2048) CCV3D_NORM(128, 4, 4)
+        else if (C <= 4096) CCV3D_NORM(256, 4, 4)
+        else if (C <= 8192) CCV3D_NORM(512, 4, 4)
+        else CCV3D_NORM(512, 4, 8)
+    } else {
+        if (C <= 128) CCV3D_NORM(32, 1, 4)
+        else if (C <= 1024) CCV3D_NORM(128, 1, 8)
+        else if (C <= 4096) CCV3D_NORM(512, 1, 8)
+        else CCV3D_NORM(512, 1, 32)
+    }
+#undef CCV3D_NORM
+    return launched();
+}
+
+}  // namespace
+
+extern "C" {
+
+ccv3d_status ccv3d_kv_append(const ccv3d_kv_cache* cache, const ccv3d_token_batch* batch, const ccv3d_heads* k,
+                             const ccv3d_heads* v, const ccv3d_rotary* rot, const ccv3d_heads* q,
+                             const ccv3d_heads* q_out, int32_t q_heads, int32_t dtype, uint32_t* status, void* stream) {
+    ccv3d_status s = check_cache(cache);
+    if (s != CCV3D_OK) return s;
+    if ((s = check_batch(batch, cache->page_tokens)) != CCV3D_OK) return s;
+    if (!dtype_ok(dtype) || (!q != !q_out) || (q && q_heads < 1)) return CCV3D_ERR_INVALID_ARG;
+    const int D = cache->head_dim, H = cache->kv_heads, tokens = batch->tokens;
+    if (tokens == 0) return CCV3D_OK;
+    if ((s = check_heads(k, H, D, dtype)) != CCV3D_OK || (s = check_heads(v, H, D, dtype)) != CCV3D_OK) return s;
+    if (rot) {
+        if (!rot->cos_table || !rot->sin_table || !rot->positions || rot->rows < 1 || rot->axes < 1 || rot->axes > 3) return CCV3D_ERR_INVALID_ARG;
+        if (rot->pairs < 4 || rot->pairs % 4 || rot->pairs > D / 2) return CCV3D_ERR_UNSUPPORTED;
+        int sum = 0;
+        for (int a = 0; a < 3; ++a) {
+            if (a < rot->axes && rot->section[a] < 0) return CCV3D_ERR_INVALID_ARG;
+            if (a < rot->axes) sum += rot->section[a];
+        }
+        if (sum != rot->pairs) return CCV3D_ERR_INVALID_ARG;
+        if (misaligned(rot->cos_table, 16) || misaligned(rot->sin_table, 16) || misaligned(rot->positions, 4)) return CCV3D_ERR_ALIGNMENT;
+    }
+    const Span sc = codes_span(cache), ss = scales_span(cache), sk = span_of(*k, tokens, H, D, dtype), sv = span_of(*v, tokens, H, D, dtype);
+    if (meet(sc, ss) || meet(sc, sk) || meet(sc, sv) || meet(ss, sk) || meet(ss, sv)) return CCV3D_ERR_ALIAS;
+    if (q) {
+        if ((s = check_heads(q, q_heads, D, dtype)) != CCV3D_OK || (s = check_heads(q_out, q_heads, D, dtype, tokens)) != CCV3D_OK) return s;
+        const Span a = span_of(*q, tokens, q_heads, D, dtype), b = span_of(*q_out, tokens, q_heads, D, dtype);
+        const bool self = q->data == q_out->data && q->token_stride == q_out->token_stride && q->head_stride == q_out->head_stride;
+        if (!self && meet(a, b)) return CCV3D_ERR_ALIAS;
+        if (meet(b, sc) || meet(b, ss) || meet(a, sc) || meet(a, ss)) return CCV3D_ERR_ALIAS;
+        // in place among slices of one projection the ranges of q, k and v interleave: only a dense overlap is an error
+        if (!self && (meet(b, sk) || meet(b, sv))) return CCV3D_ERR_ALIAS;
+    }
+    Device dev;
+    if ((s = current_device(&dev)) != CCV3D_OK) return s;
+    AppendParams p = {};
+    p.c = *cache;
+    p.bt = *batch;
+    p.k = *k;
+    p.v = *v;
+    if (q) { p.q = *q; p.qo = *q_out; p.q_heads = q_heads; }
+    if (rot) {
+        p.rot = *rot;
+        for (int a = rot->axes; a < 3; ++a) p.rot.section[a] = 0;
+    }
+    p.status = status;
+    const int P = cache->page_tokens;
+    // pages that n new tokens can touch: one for n = 1, else up to (n - 1) / P + 2
+    const int64_t by_tokens = (int64_t)tokens / P + 2LL * batch->batch;
+    const int64_t by_batch = (int64_t)batch->batch * (batch->max_new <= 1 ? 1 : (batch->max_new - 1) / P + 2);
+    const int64_t kv = (by_tokens < by_batch ? by_tokens : by_batch) * 2 * H;
+    const int64_t tpi = APPEND_THREADS / (D / 4);
+    const int64_t all = kv + (q ? ((int64_t)tokens * q_heads + tpi - 1) / tpi : 0);
+    if (all > 0x7FFFFFFF) return CCV3D_ERR_UNSUPPORTED;
+    p.kv_blocks = (unsigned)kv;
+    return dtype == CCV3D_BF16 ? launch_append<__nv_bfloat16>(p, (unsigned)all, (cudaStream_t)stream)
+                               : launch_append<float>(p, (unsigned)all, (cudaStream_t)stream);
+}
+
+ccv3d_status ccv3d_kv_attend_workspace(const ccv3d_kv_cache* cache, const ccv3d_token_batch* batch, int32_t q_heads,
+                                       int32_t dtype, uint64_t* bytes_host) {
+    if (!bytes_host) return CCV3D_ERR_INVALID_ARG;
+    ccv3d_status s = check_cache(cache);
+    if (s != CCV3D_OK) return s;
+    if ((s = check_batch(batch, cache->page_tokens)) != CCV3D_OK) return s;
+    if (!dtype_ok(dtype) || q_heads < 1 || q_heads % cache->kv_heads) return CCV3D_ERR_INVALID_ARG;
+    *bytes_host = 0;
+    return CCV3D_OK;
+}
+
+ccv3d_status ccv3d_kv_attend(const ccv3d_kv_cache* cache, const ccv3d_token_batch* batch, const ccv3d_heads* q,
+                             const ccv3d_heads* out, float* lse, int32_t q_heads, int32_t dtype, float scale,
+                             int32_t frame, int32_t window, void* ws, uint64_t ws_bytes, uint32_t* status, void* stream) {
+    uint64_t need = 0;
+    ccv3d_status s = ccv3d_kv_attend_workspace(cache, batch, q_heads, dtype, &need);
+    if (s != CCV3D_OK) return s;
+    if (frame < 0 || window < -1) return CCV3D_ERR_INVALID_ARG;
+    if (batch->tokens == 0 || batch->max_new == 0) return CCV3D_OK;
+    const int D = cache->head_dim, tokens = batch->tokens;
+    if ((s = check_heads(q, q_heads, D, dtype)) != CCV3D_OK || (s = check_heads(out, q_heads, D, dtype, tokens)) != CCV3D_OK) return s;
+    if (misaligned(lse, 4) || misaligned(ws, 256)) return CCV3D_ERR_ALIGNMENT;
+    const Span a = span_of(*q, tokens, q_heads, D, dtype), o = span_of(*out, tokens, q_heads, D, dtype), sc = codes_span(cache), ss = scales_span(cache);
+    if (meet(a, o) || meet(o, sc) || meet(o, ss)) return CCV3D_ERR_ALIAS;
+    if (lse) {
+        const Span l = span_of(lse, (int64_t)tokens * q_heads * 4);
+        if (meet(l, a) || meet(l, o) || meet(l, sc) || meet(l, ss)) return CCV3D_ERR_ALIAS;
+    }
+    if (need && (!ws || ws_bytes < need)) return CCV3D_ERR_NOMEM;
+    Device dev;
+    if ((s = current_device(&dev)) != CCV3D_OK) return s;
+    AttendParams p = {};
+    p.c = *cache;
+    p.bt = *batch;
+    p.q = *q;
+    p.o = *out;
+    p.lse = lse;
+    p.q_heads = q_heads;
+    p.group = q_heads / cache->kv_heads;
+    p.scale = scale;
+    p.frame = frame;
+    p.window = window;
+    p.status = status;
+    const int64_t rows = (int64_t)tokens * q_heads;
+    if (rows > 0x7FFFFFFF) return CCV3D_ERR_UNSUPPORTED;
+    cudaStream_t st = (cudaStream_t)stream;
+    if (dtype == CCV3D_BF16) {
+        if (D == 64) kv_attend_row_kernel<__nv_bfloat16, 64><<<(unsigned)rows, 128, 0, st>>>(p);
+        else kv_attend_row_kernel<__nv_bfloat16, 128><<<(unsigned)rows, 128, 0, st>>>(p);
+    } else {
+        if (D == 64) kv_attend_row_kernel<float, 64><<<(unsigned)rows, 128, 0, st>>>(p);
+        else kv_attend_row_kernel<float, 128><<<(unsigned)rows, 128, 0, st>>>(p);
+    }
+    return launched();
+}
+
+ccv3d_status ccv3d_gated_norm(const ccv3d_norm_desc* d, const void* x, const void* y, const void* post_weight,
+                              const void* post_bias, const void* gate, const void* pre_weight, const void* pre_bias,
+                              const void* scale, const void* shift, void* r, void* h, void* stream) {
+    if (!d || d->rows < 0 || d->channels < 1 || d->rows_per_group < 1) return CCV3D_ERR_INVALID_ARG;
+    if (!dtype_ok(d->res_dtype) || !dtype_ok(d->act_dtype) || !dtype_ok(d->weight_dtype) || !dtype_ok(d->mod_dtype)) return CCV3D_ERR_INVALID_ARG;
+    if (d->post_kind < 0 || d->post_kind > 2 || d->pre_kind < 0 || d->pre_kind > 2) return CCV3D_ERR_INVALID_ARG;
+    if (d->channels > 16384) return CCV3D_ERR_UNSUPPORTED;
+    if (d->rows == 0) return CCV3D_OK;
+    if (!x || (!r && !h)) return CCV3D_ERR_INVALID_ARG;
+    const int64_t C = d->channels, last = d->rows - 1, er = esize(d->res_dtype), ea = esize(d->act_dtype);
+    if (d->x_stride < 0 || (y && d->y_stride < 0) || (r && d->r_stride < C) || (h && d->h_stride < C)) return CCV3D_ERR_INVALID_ARG;
+    if ((gate && d->gate_stride < 0) || (scale && d->scale_stride < 0) || (shift && d->shift_stride < 0)) return CCV3D_ERR_INVALID_ARG;
+    const int64_t em = esize(d->mod_dtype), ew = esize(d->weight_dtype);
+    if (misaligned(x, er) || misaligned(r, er) || misaligned(y, ea) || misaligned(h, ea) || misaligned(gate, em) || misaligned(scale, em) ||
+        misaligned(shift, em) || misaligned(post_weight, ew) || misaligned(post_bias, ew) || misaligned(pre_weight, ew) || misaligned(pre_bias, ew))
+        return CCV3D_ERR_ALIGNMENT;
+    // outputs against every input (and one another); r on x and h on y are allowed row for row
+    const Span in[] = {span_of(x, (last * d->x_stride + C) * er), y ? span_of(y, (last * d->y_stride + C) * ea) : Span{0, 0},
+                       span_of(post_weight, post_weight ? C * ew : 0), span_of(post_bias, post_bias ? C * ew : 0),
+                       span_of(pre_weight, pre_weight ? C * ew : 0), span_of(pre_bias, pre_bias ? C * ew : 0),
+                       span_of(gate, gate ? (last / d->rows_per_group * d->gate_stride + C) * em : 0),
+                       span_of(scale, scale ? (last / d->rows_per_group * d->scale_stride + C) * em : 0),
+                       span_of(shift, shift ? (last / d->rows_per_group * d->shift_stride + C) * em : 0)};
+    const Span sr = span_of(r, r ? (last * d->r_stride + C) * er : 0), sh = span_of(h, h ? (last * d->h_stride + C) * ea : 0);
+    if (r && h && meet(sr, sh)) return CCV3D_ERR_ALIAS;
+    for (int i = 0; i < 9; ++i) {
+        if (in[i].a == in[i].b) continue;
+        if (r && meet(sr, in[i]) && !(i == 0 && r == x && d->r_stride == d->x_stride)) return CCV3D_ERR_ALIAS;
+        if (h && meet(sh, in[i]) && !(i == 1 && h == y && d->h_stride == d->y_stride)) return CCV3D_ERR_ALIAS;
+    }
+    Device dev;
+    const ccv3d_status s = current_device(&dev);
+    if (s != CCV3D_OK) return s;
+    NormParams p = {*d, x, y, post_weight, post_bias, gate, pre_weight, pre_bias, scale, shift, r, h};
+    // four elements per access where every row and vector starts on a multiple of four
+    const auto whole = [](const void* t, int64_t stride, int64_t e) { return !t || (!misaligned(t, 4 * e) && stride % 4 == 0); };
+    const bool vec = C % 4 == 0 && whole(x, d->x_stride, er) && whole(y, d->y_stride, ea) && whole(r, d->r_stride, er) && whole(h, d->h_stride, ea) &&
+                     whole(gate, d->gate_stride, em) && whole(scale, d->scale_stride, em) && whole(shift, d->shift_stride, em) &&
+                     whole(post_weight, 0, ew) && whole(post_bias, 0, ew) && whole(pre_weight, 0, ew) && whole(pre_bias, 0, ew);
+    cudaStream_t st = (cudaStream_t)stream;
+    if (d->res_dtype == CCV3D_BF16)
+        return d->act_dtype == CCV3D_BF16 ? launch_norm<__nv_bfloat16, __nv_bfloat16>(p, vec, st) : launch_norm<__nv_bfloat16, float>(p, vec, st);
+    return d->act_dtype == CCV3D_BF16 ? launch_norm<float, __nv_bfloat16>(p, vec, st) : launch_norm<float, float>(p, vec, st);
+}
+
+}  // extern "C"
