@@ -1,6 +1,7 @@
 // C entry points of the token operators: argument checks, kernel choice, launches.
 #include "../../include/ccv3d.h"
 
+#include <cuda.h>
 #include <cuda_bf16.h>
 #include <cuda_runtime.h>
 
@@ -8,7 +9,8 @@
 #include <cstdlib>
 
 #include "ccv3d_tokens_append.cuh"
-#include "ccv3d_tokens_attend.cuh"
+#include "ccv3d_tokens_attend_rows.cuh"
+#include "ccv3d_tokens_attend_step.cuh"
 #include "ccv3d_tokens_norm.cuh"
 
 using namespace ccv3d;
@@ -25,9 +27,22 @@ ccv3d_status launched() {
 }
 
 // What the launches need to know of the current device, looked up once for each.
-struct Device { int sm_count; };
+struct Device { int index, sm_count; long long wait_clk; };
 constexpr int MAX_DEVICES = 64;
 std::atomic<int> g_sms[MAX_DEVICES];     // 0: not looked up, < 0: not compute capability 10.x
+
+typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
+                                  const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+// CCV3D_WAIT_LIMIT_MS (1..10000) bounds the waits inside the kernels; default about a second at the highest SM clock.
+long long wait_limit_clk() {
+    static const long long clk = [] {
+        const char* e = getenv("CCV3D_WAIT_LIMIT_MS");
+        const int ms = e ? atoi(e) : 0;
+        return 2000000LL * (ms >= 1 && ms <= 10000 ? ms : 1000);
+    }();
+    return clk;
+}
 
 ccv3d_status current_device(Device* d) {
     int dev = 0;
@@ -44,7 +59,9 @@ ccv3d_status current_device(Device* d) {
         g_sms[dev].store(sms, std::memory_order_relaxed);
     }
     if (sms < 0) return CCV3D_ERR_ARCH;
+    d->index = dev;
     d->sm_count = sms;
+    d->wait_clk = wait_limit_clk();
     return CCV3D_OK;
 }
 
@@ -127,6 +144,113 @@ ccv3d_status launch_norm(const NormParams& p, bool vec, cudaStream_t st) {
     return launched();
 }
 
+ccv3d_status check_attend(const ccv3d_kv_cache* cache, const ccv3d_token_batch* batch, int q_heads, int dtype) {
+    ccv3d_status s = check_cache(cache);
+    if (s != CCV3D_OK) return s;
+    if ((s = check_batch(batch, cache->page_tokens)) != CCV3D_OK) return s;
+    if (!dtype_ok(dtype) || q_heads < 1 || q_heads % cache->kv_heads) return CCV3D_ERR_INVALID_ARG;
+    const int64_t group = q_heads / cache->kv_heads;
+    // 32-bit row numbers (TMA coordinates, query rows) and unit numbers
+    if ((int64_t)cache->pages * 2 * cache->kv_heads * cache->page_tokens > 0x7FFFFFFF) return CCV3D_ERR_UNSUPPORTED;
+    if ((int64_t)batch->tokens * q_heads > 0x7FFFFFFF) return CCV3D_ERR_UNSUPPORTED;
+    const int64_t units = (int64_t)batch->max_pages * cache->page_tokens / STEP_UNIT + 1;
+    const double all = (double)batch->batch * cache->kv_heads * (((double)batch->max_new * group) / 8 + 1) * units;
+    if (all > 2e9) return CCV3D_ERR_UNSUPPORTED;
+    return CCV3D_OK;
+}
+
+// Kernel, grid and scratch of a call.
+struct Plan {
+    Device dev;
+    int rows_per_item;       // query rows of an item: 8 or 16 (step kernel), 0: the row kernel
+    int blocks, slot_rows;
+    uint64_t ml_at, join_at, bytes;
+};
+
+ccv3d_status plan_attend(const ccv3d_kv_cache* cache, const ccv3d_token_batch* batch, int q_heads, int dtype, Plan* pl) {
+    ccv3d_status s = check_attend(cache, batch, q_heads, dtype);
+    if (s != CCV3D_OK) return s;
+    if ((s = current_device(&pl->dev)) != CCV3D_OK) return s;
+    const int64_t rows = (int64_t)batch->max_new * (q_heads / cache->kv_heads);
+    pl->rows_per_item = rows <= 8 ? 8 : rows <= 64 ? 16 : 0;
+    pl->blocks = 2 * pl->dev.sm_count;
+    pl->slot_rows = 16;
+    pl->ml_at = (uint64_t)2 * pl->blocks * pl->slot_rows * cache->head_dim * 4;
+    pl->join_at = pl->ml_at + (uint64_t)2 * pl->blocks * pl->slot_rows * sizeof(float2);
+    pl->bytes = (pl->join_at + pl->blocks * sizeof(Join) + 255) / 256 * 256;
+    return CCV3D_OK;
+}
+
+// The cache as a matrix of rows of head_dim codes, read in boxes of 32 tokens (16 where a page holds no more).
+ccv3d_status encode_cache_map(const ccv3d_kv_cache& c, CUtensorMap* tm, int box_rows) {
+    static std::atomic<EncodeTiledFn> encode{nullptr};
+    EncodeTiledFn fn = encode.load(std::memory_order_relaxed);
+    if (!fn) {
+        void* f = nullptr;
+        cudaDriverEntryPointQueryResult qres;
+        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &f, cudaEnableDefault, &qres) != cudaSuccess || !f || qres != cudaDriverEntryPointSuccess) {
+            cudaGetLastError();
+            return CCV3D_ERR_CUDA;
+        }
+        fn = (EncodeTiledFn)f;
+        encode.store(fn, std::memory_order_relaxed);
+    }
+    const cuuint64_t dims[2] = {(cuuint64_t)c.head_dim, (cuuint64_t)c.pages * 2 * c.kv_heads * c.page_tokens};
+    const cuuint64_t strides[1] = {(cuuint64_t)c.head_dim};
+    const cuuint32_t box[2] = {(cuuint32_t)c.head_dim, (cuuint32_t)box_rows}, es[2] = {1, 1};
+    const CUresult r = fn(tm, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, c.codes, dims, strides, box, es, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                          c.head_dim == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                          CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    return r == CUDA_SUCCESS ? CCV3D_OK : CCV3D_ERR_CUDA;
+}
+
+// Opts a kernel into its dynamic shared memory, once for each device.
+template <typename F>
+bool allow_smem(F* kernel, int bytes, int dev, std::atomic<uint64_t>& done) {
+    if (done.load(std::memory_order_relaxed) >> dev & 1) return true;
+    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) != cudaSuccess) return false;
+    done.fetch_or(1ull << dev, std::memory_order_relaxed);
+    return true;
+}
+
+template <typename T, int D, int NT>
+ccv3d_status launch_step(const AttendParams& p, const Plan& pl, cudaStream_t st) {
+    static std::atomic<uint64_t> done{0};
+    using S = StepShape<D>;
+    if (!allow_smem(kv_attend_step_kernel<T, D, NT>, S::BYTES, pl.dev.index, done)) { cudaGetLastError(); return CCV3D_ERR_CUDA; }
+    CUtensorMap tm;
+    const ccv3d_status s = encode_cache_map(p.c, &tm, p.c.page_tokens < STEP_TILE ? p.c.page_tokens : STEP_TILE);
+    if (s != CCV3D_OK) return s;
+    kv_attend_step_kernel<T, D, NT><<<pl.blocks, 32 * STEP_WARPS, S::BYTES, st>>>(tm, p);
+    return launched();
+}
+
+// The sum over parts, launched so that it is resident when the attention kernel ends.
+template <typename T, int D>
+ccv3d_status launch_join(const AttendParams& p, const Plan& pl, float shift, cudaStream_t st) {
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(pl.blocks, (pl.slot_rows + 3) / 4);
+    cfg.blockDim = dim3(D);
+    cfg.stream = st;
+    cfg.attrs = at;
+    cfg.numAttrs = 1;
+    if (cudaLaunchKernelEx(&cfg, attend_join_kernel<T, D>, p, shift) != cudaSuccess) { cudaGetLastError(); return CCV3D_ERR_CUDA; }
+    return CCV3D_OK;
+}
+
+template <typename T, int D>
+ccv3d_status launch_attend(const AttendParams& p, const Plan& pl, cudaStream_t st) {
+    if (pl.rows_per_item == 0) {
+        kv_attend_row_kernel<T, D><<<(unsigned)(p.bt.tokens * p.q_heads), 128, 0, st>>>(p);
+        return launched();
+    }
+    const ccv3d_status s = pl.rows_per_item == 8 ? launch_step<T, D, 1>(p, pl, st) : launch_step<T, D, 2>(p, pl, st);
+    return s == CCV3D_OK ? launch_join<T, D>(p, pl, STEP_SHIFT, st) : s;
+}
+
 }  // namespace
 
 extern "C" {
@@ -192,19 +316,17 @@ ccv3d_status ccv3d_kv_append(const ccv3d_kv_cache* cache, const ccv3d_token_batc
 ccv3d_status ccv3d_kv_attend_workspace(const ccv3d_kv_cache* cache, const ccv3d_token_batch* batch, int32_t q_heads,
                                        int32_t dtype, uint64_t* bytes_host) {
     if (!bytes_host) return CCV3D_ERR_INVALID_ARG;
-    ccv3d_status s = check_cache(cache);
-    if (s != CCV3D_OK) return s;
-    if ((s = check_batch(batch, cache->page_tokens)) != CCV3D_OK) return s;
-    if (!dtype_ok(dtype) || q_heads < 1 || q_heads % cache->kv_heads) return CCV3D_ERR_INVALID_ARG;
-    *bytes_host = 0;
-    return CCV3D_OK;
+    Plan pl;
+    const ccv3d_status s = plan_attend(cache, batch, q_heads, dtype, &pl);
+    if (s == CCV3D_OK) *bytes_host = pl.bytes;
+    return s;
 }
 
 ccv3d_status ccv3d_kv_attend(const ccv3d_kv_cache* cache, const ccv3d_token_batch* batch, const ccv3d_heads* q,
                              const ccv3d_heads* out, float* lse, int32_t q_heads, int32_t dtype, float scale,
                              int32_t frame, int32_t window, void* ws, uint64_t ws_bytes, uint32_t* status, void* stream) {
-    uint64_t need = 0;
-    ccv3d_status s = ccv3d_kv_attend_workspace(cache, batch, q_heads, dtype, &need);
+    Plan pl;
+    ccv3d_status s = check_attend(cache, batch, q_heads, dtype);
     if (s != CCV3D_OK) return s;
     if (frame < 0 || window < -1) return CCV3D_ERR_INVALID_ARG;
     if (batch->tokens == 0 || batch->max_new == 0) return CCV3D_OK;
@@ -217,9 +339,11 @@ ccv3d_status ccv3d_kv_attend(const ccv3d_kv_cache* cache, const ccv3d_token_batc
         const Span l = span_of(lse, (int64_t)tokens * q_heads * 4);
         if (meet(l, a) || meet(l, o) || meet(l, sc) || meet(l, ss)) return CCV3D_ERR_ALIAS;
     }
-    if (need && (!ws || ws_bytes < need)) return CCV3D_ERR_NOMEM;
-    Device dev;
-    if ((s = current_device(&dev)) != CCV3D_OK) return s;
+    if (!ws || ws_bytes == 0) return CCV3D_ERR_NOMEM;
+    if ((s = plan_attend(cache, batch, q_heads, dtype, &pl)) != CCV3D_OK) return s;
+    if (ws_bytes < pl.bytes) return CCV3D_ERR_NOMEM;
+    const Span w = span_of(ws, (int64_t)pl.bytes);
+    if (meet(w, a) || meet(w, o) || meet(w, sc) || meet(w, ss)) return CCV3D_ERR_ALIAS;
     AttendParams p = {};
     p.c = *cache;
     p.bt = *batch;
@@ -232,17 +356,15 @@ ccv3d_status ccv3d_kv_attend(const ccv3d_kv_cache* cache, const ccv3d_token_batc
     p.frame = frame;
     p.window = window;
     p.status = status;
-    const int64_t rows = (int64_t)tokens * q_heads;
-    if (rows > 0x7FFFFFFF) return CCV3D_ERR_UNSUPPORTED;
+    p.wait_clk = pl.dev.wait_clk;
+    p.part = (float*)ws;
+    p.part_ml = (float2*)((char*)ws + pl.ml_at);
+    p.join = (Join*)((char*)ws + pl.join_at);
+    p.slot_rows = pl.slot_rows;
     cudaStream_t st = (cudaStream_t)stream;
-    if (dtype == CCV3D_BF16) {
-        if (D == 64) kv_attend_row_kernel<__nv_bfloat16, 64><<<(unsigned)rows, 128, 0, st>>>(p);
-        else kv_attend_row_kernel<__nv_bfloat16, 128><<<(unsigned)rows, 128, 0, st>>>(p);
-    } else {
-        if (D == 64) kv_attend_row_kernel<float, 64><<<(unsigned)rows, 128, 0, st>>>(p);
-        else kv_attend_row_kernel<float, 128><<<(unsigned)rows, 128, 0, st>>>(p);
-    }
-    return launched();
+    if (dtype == CCV3D_BF16)
+        return D == 64 ? launch_attend<__nv_bfloat16, 64>(p, pl, st) : launch_attend<__nv_bfloat16, 128>(p, pl, st);
+    return D == 64 ? launch_attend<float, 64>(p, pl, st) : launch_attend<float, 128>(p, pl, st);
 }
 
 ccv3d_status ccv3d_gated_norm(const ccv3d_norm_desc* d, const void* x, const void* y, const void* post_weight,

@@ -1,8 +1,25 @@
-// Attention over the paged E4M3 cache.
+// Attention over the paged E4M3 cache: what its kernels share, and the sum over the parts of a split softmax.
+//
+// The work of a call is a list of items (a sequence, a block of its query rows, a kv head), each a run of units (a
+// stretch of cached tokens); block i of G takes units [i U / G, (i + 1) U / G) of the whole list, so every block has
+// the same to read whatever the sequences' lengths, and nothing about them has to be known on the host.  An item that
+// lies in one block is finished there; one that crosses blocks leaves a part (unnormalised sums, their running maximum
+// and weight) in each, and attend_join_kernel adds the parts in block order.
+//
+// Softmax in powers of two: with t = score * log2(e) and e_v = log2 of the value scale of the token's page, the weight
+// of a value code is 2^(t + e_v - m + shift), m the running maximum of t + e_v, so page scales of any size stay out of
+// the range of the 16-bit weights; the softmax's own sum takes that times 1 / value scale.  The shift uses the part of
+// that range above 1.
 #pragma once
+#include <cuda.h>
+
+#include "ccv3d_tc_ptx.cuh"
 #include "ccv3d_tokens_common.cuh"
 
 namespace ccv3d {
+
+// The item whose first part block i wrote in slot 2 i + 1, to be joined with the slots 2 (i + 1), 2 (i + 2), ...
+struct Join { int parts, row0, rows, head0; };   // rows row0 .. row0 + rows - 1 of the (token, head of the kv group) order
 
 struct AttendParams {
     ccv3d_kv_cache c;
@@ -13,7 +30,27 @@ struct AttendParams {
     float scale;
     int frame, window;
     uint32_t* status;
+    long long wait_clk;      // bound of every wait, in SM clocks
+    // scratch: slots 2 i (an item that began before block i) and 2 i + 1 (one that ends behind it)
+    float* part;             // [slot][slot_rows][dim] sums
+    float2* part_ml;         // [slot][slot_rows] maximum and weight
+    Join* join;              // [block]; parts = 0: nothing to join
+    int slot_rows;
 };
+
+constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
+
+__device__ __forceinline__ float exp2_fast(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+// log2 and reciprocal of a page's value scale; scales are positive (0, never written by an append, counts as tiny)
+__device__ __forceinline__ void scale_terms(float vs, float& e, float& inv) {
+    vs = fmaxf(vs, 1e-36f);
+    e = __log2f(vs);
+    inv = 1.f / vs;
+}
 
 // Tokens [lo, hi) that the token at position pos of a sequence of `total` tokens sees.
 __device__ __forceinline__ void visible(const AttendParams& p, int pos, int total, int& lo, int& hi) {
@@ -23,70 +60,42 @@ __device__ __forceinline__ void visible(const AttendParams& p, int pos, int tota
     if (pos < 0) lo = hi = 0;
 }
 
-// One block of 128 threads for each (token, head): a running softmax over the cache 128 tokens at a time.
+// Row r of a kv head's query rows: token r / group (packed), head r % group of the kv head's group.
+template <typename T>
+__device__ __forceinline__ void store_out(const AttendParams& p, int token, int head, int d, const float (&v)[4]) {
+    store4((T*)p.o.data + token * p.o.token_stride + head * p.o.head_stride + d, v);
+}
+__device__ __forceinline__ float lse_of(float m, float l, float shift) {
+    return l != 0.f ? (m - shift + log2f(l)) * LN2 : -INFINITY;     // (a row that saw NaN has l = NaN)
+}
+
+// One block for each block of the attention kernel and stretch of 4 rows: adds the parts of the item that starts there.
 template <typename T, int D>
-__global__ void __launch_bounds__(128) kv_attend_row_kernel(const AttendParams p) {
-    __shared__ float qs[D], ps[128], part[4];
-    const int64_t row = blockIdx.x;
-    const int token = (int)(row / p.q_heads), head = (int)(row % p.q_heads), tid = threadIdx.x, P = p.c.page_tokens;
-    int b = 0;
-    for (int lo = 0, hi = p.bt.batch; lo < hi;) {          // last sequence that starts at or before the token
-        const int mid = (lo + hi) / 2;
-        if (__ldg(p.bt.new_start + mid) <= token) { b = mid; lo = mid + 1; } else hi = mid;
+__global__ void __launch_bounds__(D) attend_join_kernel(const AttendParams p, float shift) {
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    const Join j = p.join[blockIdx.x];
+    const int r = blockIdx.y * 4 + (int)threadIdx.x / (D / 4), d = (int)threadIdx.x % (D / 4) * 4;
+    if (r >= j.rows || j.parts == 0) return;
+    const int64_t slot0 = 2 * (int64_t)blockIdx.x;                  // part i > 0 lies in slot0 + 2 i, part 0 in slot0 + 1
+    float m = -INFINITY;
+    for (int i = 0; i < j.parts; ++i) m = fmaxf(m, p.part_ml[(slot0 + (i ? 2 * i : 1)) * p.slot_rows + r].x);
+    float l = 0.f, acc[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+    for (int i = 0; i < j.parts; ++i) {
+        const int64_t at = (slot0 + (i ? 2 * i : 1)) * p.slot_rows + r;
+        const float2 ml = p.part_ml[at];
+        const float4 v = *reinterpret_cast<const float4*>(p.part + at * D + d);
+        const float w = ml.x == -INFINITY ? 0.f : exp2_fast(ml.x - m);
+        l = fmaf(w, ml.y, l);
+        acc[0] = fmaf(w, v.x, acc[0]); acc[1] = fmaf(w, v.y, acc[1]);
+        acc[2] = fmaf(w, v.z, acc[2]); acc[3] = fmaf(w, v.w, acc[3]);
     }
-    const Seq s = load_seq(p.bt, P, b, p.status);
-    if (token < s.first || token >= s.first + s.n) return;
-    int lo, hi;
-    visible(p, s.total - s.n + token - s.first, s.total, lo, hi);
-    if (tid < D) qs[tid] = load1((const T*)p.q.data + token * p.q.token_stride + head * p.q.head_stride + tid);
-    __syncthreads();
-    const int kvh = head / p.group, H = p.c.kv_heads;
-    float m = -INFINITY, l = 0.f, acc = 0.f;
-    for (int t0 = lo; t0 < hi; t0 += 128) {
-        const int t = t0 + tid;
-        float x = -INFINITY, vs = 0.f;
-        int page = -1;
-        if (t < hi) page = load_page(p.bt, p.c, b, t / P, p.status);
-        if (page >= 0) {
-            const uint8_t* k = (const uint8_t*)p.c.codes + (((int64_t)page * 2 * H + kvh) * P + t % P) * D;
-            float sum = 0.f;
-            for (int i = 0; i < D; i += 4) {
-                float c[4];
-                e4m3x4_to_float(*reinterpret_cast<const uint32_t*>(k + i), c);
+    const float inv = l != 0.f ? 1.f / l : 0.f;
 #pragma unroll
-                for (int j = 0; j < 4; ++j) sum = fmaf(c[j], qs[i + j], sum);
-            }
-            x = sum * p.c.scales[(int64_t)page * 2 * H + kvh] * p.scale;
-            vs = p.c.scales[((int64_t)page * 2 + 1) * H + kvh];
-        }
-        float mm = warp_max(x);
-        if ((tid & 31) == 0) part[tid >> 5] = mm;
-        __syncthreads();
-        mm = fmaxf(fmaxf(part[0], part[1]), fmaxf(part[2], part[3]));
-        const float now = fmaxf(m, mm);
-        const float f = m == -INFINITY ? 0.f : __expf(m - now), e = x == -INFINITY ? 0.f : __expf(x - now);
-        const float tot = warp_sum(e);
-        __syncthreads();
-        ps[tid] = e * vs;
-        if ((tid & 31) == 0) part[tid >> 5] = tot;
-        __syncthreads();
-        l = l * f + part[0] + part[1] + part[2] + part[3];
-        m = now;
-        acc *= f;
-        if (tid < D)
-            for (int i = 0; i < 128 && t0 + i < hi; ++i) {
-                const int pg = load_page(p.bt, p.c, b, (t0 + i) / P, nullptr);
-                if (pg < 0) continue;
-                const uint8_t* v = (const uint8_t*)p.c.codes + ((((int64_t)pg * 2 + 1) * H + kvh) * P + (t0 + i) % P) * D;
-                float c[4];
-                e4m3x4_to_float(v[tid], c);
-                acc = fmaf(ps[i], c[0], acc);
-            }
-        __syncthreads();
-    }
-    if (tid < D)
-        store1((T*)p.o.data + token * p.o.token_stride + head * p.o.head_stride + tid, l > 0.f || l != l ? acc / l : 0.f);
-    if (tid == 0 && p.lse) p.lse[(int64_t)token * p.q_heads + head] = l != 0.f ? m + logf(l) : -INFINITY;
+    for (int i = 0; i < 4; ++i) acc[i] = l != 0.f ? acc[i] * inv : 0.f;
+    const int token = (j.row0 + r) / p.group, head = j.head0 + (j.row0 + r) % p.group;
+    store_out<T>(p, token, head, d, acc);
+    if (d == 0 && p.lse) p.lse[(int64_t)token * p.q_heads + head] = lse_of(m, l, shift);
 }
 
 }  // namespace ccv3d

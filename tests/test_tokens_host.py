@@ -104,6 +104,8 @@ def test_append_refuses(bad, expected):
     (dict(lse=5 * K + 64), ccv.ERR_ALIAS),
     (dict(lse=6 * K + 2), ccv.ERR_ALIGNMENT),
     (dict(ws=32 * K + 16), ccv.ERR_ALIGNMENT),
+    (dict(ws=None), ccv.ERR_NOMEM),
+    (dict(n=0), ccv.ERR_NOMEM),
 ])
 def test_attend_refuses(bad, expected):
     assert attend(**bad) == expected
