@@ -9,8 +9,8 @@
 #include <cstdlib>
 
 #include "ccv3d_tokens_append.cuh"
-#include "ccv3d_tokens_attend_rows.cuh"
 #include "ccv3d_tokens_attend_step.cuh"
+#include "ccv3d_tokens_attend_tile.cuh"
 #include "ccv3d_tokens_norm.cuh"
 
 using namespace ccv3d;
@@ -162,7 +162,7 @@ ccv3d_status check_attend(const ccv3d_kv_cache* cache, const ccv3d_token_batch* 
 // Kernel, grid and scratch of a call.
 struct Plan {
     Device dev;
-    int rows_per_item;       // query rows of an item: 8 or 16 (step kernel), 0: the row kernel
+    int rows_per_item;       // query rows of an item: 8 or 16 (step kernel), 128 or 256 (tile kernel)
     int blocks, slot_rows;
     uint64_t ml_at, join_at, bytes;
 };
@@ -172,9 +172,10 @@ ccv3d_status plan_attend(const ccv3d_kv_cache* cache, const ccv3d_token_batch* b
     if (s != CCV3D_OK) return s;
     if ((s = current_device(&pl->dev)) != CCV3D_OK) return s;
     const int64_t rows = (int64_t)batch->max_new * (q_heads / cache->kv_heads);
-    pl->rows_per_item = rows <= 8 ? 8 : rows <= 64 ? 16 : 0;
-    pl->blocks = 2 * pl->dev.sm_count;
-    pl->slot_rows = 16;
+    pl->rows_per_item = rows <= 8 ? 8 : rows <= 64 ? 16 : dtype == CCV3D_BF16 ? 256 : 128;
+    const bool tile = pl->rows_per_item >= 128;
+    pl->blocks = tile ? pl->dev.sm_count : 2 * pl->dev.sm_count;
+    pl->slot_rows = tile ? pl->rows_per_item : 16;
     pl->ml_at = (uint64_t)2 * pl->blocks * pl->slot_rows * cache->head_dim * 4;
     pl->join_at = pl->ml_at + (uint64_t)2 * pl->blocks * pl->slot_rows * sizeof(float2);
     pl->bytes = (pl->join_at + pl->blocks * sizeof(Join) + 255) / 256 * 256;
@@ -243,9 +244,13 @@ ccv3d_status launch_join(const AttendParams& p, const Plan& pl, float shift, cud
 
 template <typename T, int D>
 ccv3d_status launch_attend(const AttendParams& p, const Plan& pl, cudaStream_t st) {
-    if (pl.rows_per_item == 0) {
-        kv_attend_row_kernel<T, D><<<(unsigned)(p.bt.tokens * p.q_heads), 128, 0, st>>>(p);
-        return launched();
+    if (pl.rows_per_item >= 128) {
+        static std::atomic<uint64_t> done{0};
+        constexpr int bytes = TileShape<T, D>::END + sizeof(TileShared) + 1024;
+        if (!allow_smem(kv_attend_tile_kernel<T, D>, bytes, pl.dev.index, done)) { cudaGetLastError(); return CCV3D_ERR_CUDA; }
+        kv_attend_tile_kernel<T, D><<<pl.blocks, TILE_THREADS, bytes, st>>>(p);
+        const ccv3d_status s = launched();
+        return s == CCV3D_OK ? launch_join<T, D>(p, pl, TILE_SHIFT, st) : s;
     }
     const ccv3d_status s = pl.rows_per_item == 8 ? launch_step<T, D, 1>(p, pl, st) : launch_step<T, D, 2>(p, pl, st);
     return s == CCV3D_OK ? launch_join<T, D>(p, pl, STEP_SHIFT, st) : s;
