@@ -246,7 +246,8 @@ template <typename T, int D>
 ccv3d_status launch_attend(const AttendParams& p, const Plan& pl, cudaStream_t st) {
     if (pl.rows_per_item >= 128) {
         static std::atomic<uint64_t> done{0};
-        constexpr int bytes = TileShape<T, D>::END + sizeof(TileShared) + 1024;
+        constexpr int bytes = TileShape<T, D>::END + sizeof(TileShared);
+        static_assert(bytes <= 232448, "shared memory of a block");
         if (!allow_smem(kv_attend_tile_kernel<T, D>, bytes, pl.dev.index, done)) { cudaGetLastError(); return CCV3D_ERR_CUDA; }
         kv_attend_tile_kernel<T, D><<<pl.blocks, TILE_THREADS, bytes, st>>>(p);
         const ccv3d_status s = launched();

@@ -1,11 +1,14 @@
 // Attention of many query rows (frames, prompts) over the paged E4M3 cache, on tcgen05.
 //
 // Bound by the tensor cores.  An item is a block of 256 query rows of one kv head (F32: 128), rows being (token, head of
-// the group) so that grouped heads share the keys they share; a unit is 128 cached tokens.  12 warps (at 168 registers), one block to an SM:
+// the group) so that grouped heads share the keys they share; a unit is 128 cached tokens.  16 warps, one block to an SM:
 //   warps 0-3, 4-7   softmax of the first and second 128 rows, a thread to a row: scores from TMEM, weights back as halves
 //                    over them, sums in registers, the output from TMEM at the end; they also stage the queries
-//   warps 8-10       fetch pages and turn codes into halves in shared memory (exact), keys and values in two slots each
-//   warp 11          issues the MMAs: S = Q K^T from shared memory, O += P V with P in TMEM
+//   warps 8-11       turn codes into halves in shared memory (exact), keys and values in two slots each
+//   warp 12          issues the MMAs: S = Q K^T from shared memory, O += P V with P in TMEM
+//   warp 13          walks the block's share ahead of the others and tells them of it: segments (an item, or the stretch of
+//                    it that falls to this block), and pages and scales of up to eight coming tiles
+//   warp 14          brings the codes in: bulk copies of 16 tokens into a ring of four half tiles
 // Two row blocks in turn keep the tensor cores busy: while one is in its softmax the other's products run.
 //
 // Keys and values are staged alike, rows of 64 channels (128 bytes, 128-byte swizzle) token by token: K-major for the
@@ -17,22 +20,44 @@
 
 namespace ccv3d {
 
-constexpr int TILE_UNIT = 128, TILE_THREADS = 384, TILE_BATCH = 1024;
+constexpr int TILE_UNIT = 128, TILE_THREADS = 512;
+constexpr int TILE_BATCH = 1024;                       // sequences whose costs are counted at a time (in the ring of codes)
+constexpr int TILE_MOVERS = 4, TILE_AHEAD = 8;                         // warps that turn codes into halves
+constexpr int TILE_REGS_SOFTMAX = 184, TILE_REGS_REST = 72;   // 256 threads each: 65536 registers, what 512 threads are launched with
 constexpr float TILE_SHIFT = 8.f, TILE_TOP = 15.f;      // weights start at 2^8 for the maximum and may reach 2^15
 
 template <typename T, int D> struct TileShape {
     static constexpr int TERMS = sizeof(T) == 4 ? 2 : 1, NQ = sizeof(T) == 4 ? 1 : 2, ROWS = 128 * NQ;
     static constexpr uint32_t HALF = 128 * 128;                       // 128 rows of 64 channels
     static constexpr uint32_t KV = HALF * (D / 64), Q = KV * TERMS;   // one staged tile; one row block's queries
-    static constexpr uint32_t Q_AT = 0, K_AT = NQ * Q, V_AT = K_AT + 2 * KV, END = V_AT + 2 * KV;
+    static constexpr uint32_t Q_AT = 0, K_AT = NQ * Q, V_AT = K_AT + 2 * KV, RAW_AT = V_AT + 2 * KV;
+    static constexpr uint32_t RAW = 64 * D, END = RAW_AT + 4 * RAW;      // codes of 64 tokens: keys, keys, values, values
     // TMEM columns: scores (and weights over them) of the row blocks, then outputs; F32 has weights of its own
     static constexpr uint32_t S_COL = 0, P_COL = NQ == 2 ? 0 : 128, O_COL = 256;
 };
 
+// A coming tile: what the movers and the softmax need to know of its pages.
+struct TileInfo {
+    float4 group[8];         // of each 16 tokens: key scale, log2 and reciprocal of the value scale
+    int rows[8];             // their rows in the pool in units of 16, -1: not to be read
+    int live, edge, t0, lo, hi;     // edge: not every row of the item sees all of it; lo, hi: tokens that any row sees
+    int absent;              // a page that should be there is not
+};
+
+// A stretch of an item that falls to this block: units unit .. unit + n - 1 of item rows row0 .. row0 + nrows - 1 (of
+// sequence b) of kv head h.
+struct TileSegment {
+    int live, n, starts, ends, parts;        // parts: blocks that an item which starts here reaches into, if it does not end here
+    int b, h, row0, nrows, first, before, total;     // before: cached tokens before the sequence's new ones; first: packed token of those
+    int t0, lo_all, hi_all;                  // first token of the stretch
+};
+
 struct TileShared {
-    float4 group[4][8];      // per staged tile and 16 tokens: key scale, log2 and reciprocal of the value scale
-    int cost[TILE_BATCH];    // units of a sequence
+    TileInfo info[TILE_AHEAD];
+    TileSegment seg[TILE_AHEAD];
     uint64_t k_full[2], k_empty[2], v_full[2], v_empty[2], q_full[2], s_full[2], p_full[2], o_full[2], o_empty[2];
+    uint64_t i_full[TILE_AHEAD], i_empty[TILE_AHEAD], g_full[TILE_AHEAD], g_empty[TILE_AHEAD];
+    uint64_t r_full[4], r_empty[4];
     uint32_t tmem;
     int abort_flag, nan_found;
 };
@@ -88,7 +113,7 @@ struct TileWalk {
 
 // Finds this block's share.  All threads of the block call it: costs of up to TILE_BATCH sequences at a time, a warp each.
 template <int ROWS>
-__device__ __forceinline__ TileWalk<ROWS> tile_share(const AttendParams& p, TileShared* sh) {
+__device__ __forceinline__ TileWalk<ROWS> tile_share(const AttendParams& p, int* cost_of) {
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = blockDim.x >> 5;
     TileWalk<ROWS> w;
     w.u = w.u1 = w.b = w.rb = w.h = w.unit = 0;
@@ -108,12 +133,12 @@ __device__ __forceinline__ TileWalk<ROWS> tile_share(const AttendParams& p, Tile
                     int units = 0;
                     for (int rb = lane; rb < blocks; rb += 32) units += tile_item<ROWS>(p, s, rb).units;
                     units = __reduce_add_sync(0xffffffffu, units);
-                    if (lane == 0) sh->cost[b] = units * p.c.kv_heads;
+                    if (lane == 0) cost_of[b] = units * p.c.kv_heads;
                 }
                 __syncthreads();
             }
             for (int b0 = 0; b0 < n && !found; b0 += 32) {
-                const int mine = b0 + lane < n ? sh->cost[b0 + lane] : 0;
+                const int mine = b0 + lane < n ? cost_of[b0 + lane] : 0;
                 const int upto = warp_scan(mine), all = __shfl_sync(0xffffffffu, upto, 31);
                 if (pass == 0) { w.total += all; continue; }
                 const unsigned hit = __ballot_sync(0xffffffffu, mine > 0 && (int64_t)w.u < before + upto);
@@ -224,17 +249,17 @@ struct TileRow {
 };
 
 // Stages the queries of one row (each thread its own) and returns what the row needs to know.
-template <typename T, int D, int ROWS>
-__device__ __forceinline__ TileRow stage_row(const AttendParams& p, const TileWalk<ROWS>& w, int r, int tid, uint8_t* q) {
+template <typename T, int D>
+__device__ __forceinline__ TileRow stage_row(const AttendParams& p, const TileSegment& w, int r, int tid, uint8_t* q) {
     using S = TileShape<T, D>;
     TileRow row = {0, 0, 0.f, -1, 0};
     float most = 0.f;
     const T* src = nullptr;
-    if (r < w.t.nrows) {
-        const int at = w.t.row0 + r;
-        row.token = w.s.first + at / p.group;
+    if (r < w.nrows) {
+        const int at = w.row0 + r;
+        row.token = w.first + at / p.group;
         row.head = w.h * p.group + at % p.group;
-        visible(p, w.s.total - w.s.n + at / p.group, w.s.total, row.lo, row.hi);
+        visible(p, w.before + at / p.group, w.total, row.lo, row.hi);
         src = (const T*)p.q.data + row.token * p.q.token_stride + row.head * p.q.head_stride;
     }
     if constexpr (sizeof(T) == 2) {
@@ -293,19 +318,18 @@ __device__ __forceinline__ TileRow stage_row(const AttendParams& p, const TileWa
     return row;
 }
 
-// One tile's scores to weights.  On return l holds the row's weight sum, mx the largest exponent met (before the shift's
-// bound is checked); pr the packed weights (BF16), or they lie in TMEM already (F32).
+// Half a tile's scores (64 tokens) to weights: packed into pr (F32: remainders into rest).  Returns the largest exponent
+// met; sum gets what the half adds to the row's weight sum.
 template <typename T, bool EDGE>
-__device__ __forceinline__ float tile_weights(uint32_t t_s, uint32_t t_p, const float4* group, const TileRow& row, float m_use, int t0,
-                                              uint32_t (&pr)[64], float& sum) {
+__device__ __forceinline__ float half_weights(uint32_t t_s, const float4* group, const TileRow& row, float m_use, int t0, uint32_t (&pr)[32],
+                                              uint32_t (&rest)[sizeof(T) == 4 ? 32 : 1], float& sum) {
     float mx = -INFINITY;
     sum = 0.f;
 #pragma unroll
-    for (int c = 0; c < 4; ++c) {
+    for (int c = 0; c < 2; ++c) {
         uint32_t v[32];
         tc_ld32(t_s + 32 * c, v);
         tc_wait_ld();
-        uint32_t lo16[16], hi16[16];
 #pragma unroll
         for (int g = 0; g < 2; ++g) {
             const float4 k = group[2 * c + g];
@@ -326,25 +350,41 @@ __device__ __forceinline__ float tile_weights(uint32_t t_s, uint32_t t_p, const 
                     part += e[j];
                 }
                 const uint32_t h = pack_half(e[0], e[1]);
-                if constexpr (sizeof(T) == 2) pr[16 * c + 8 * g + i / 2] = h;
-                else { hi16[8 * g + i / 2] = h; lo16[8 * g + i / 2] = pack_rest(e[0], e[1], h); }
+                pr[16 * c + 8 * g + i / 2] = h;
+                if constexpr (sizeof(T) == 4) rest[16 * c + 8 * g + i / 2] = pack_rest(e[0], e[1], h);
             }
             sum = fmaf(part, k.z, sum);
         }
-        if constexpr (sizeof(T) == 4) {
-            tc_st<16>(t_p + 16 * c, hi16);
-            tc_st<16>(t_p + 64 + 16 * c, lo16);
-        }
     }
     return mx;
+}
+// Scales 32 TMEM columns of this thread's lane: FP32 values or pairs of halves.
+__device__ __forceinline__ void scale_columns(uint32_t t, float f) {
+    uint32_t v[32];
+    tc_ld32(t, v);
+    tc_wait_ld();
+#pragma unroll
+    for (int k = 0; k < 32; ++k) v[k] = __float_as_uint(__uint_as_float(v[k]) * f);
+    tc_st<32>(t, v);
+}
+__device__ __forceinline__ void scale_halves(uint32_t t, float f) {
+    uint32_t v[32];
+    const __half2 h = __float2half2_rn(f);
+    tc_ld32(t, v);
+    tc_wait_ld();
+#pragma unroll
+    for (int k = 0; k < 32; ++k) {
+        const __half2 x = __hmul2(*reinterpret_cast<const __half2*>(&v[k]), h);
+        v[k] = *reinterpret_cast<const uint32_t*>(&x);
+    }
+    tc_st<32>(t, v);
 }
 
 template <typename T, int D>
 __global__ void __launch_bounds__(TILE_THREADS, 1) kv_attend_tile_kernel(const AttendParams p) {
     using S = TileShape<T, D>;
     constexpr int ROWS = S::ROWS, NQ = S::NQ, TERMS = S::TERMS;
-    extern __shared__ uint8_t smem_raw[];
-    uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+    extern __shared__ __align__(1024) uint8_t smem[];
     TileShared* sh = reinterpret_cast<TileShared*>(smem + S::END);
     const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
     const int P = p.c.page_tokens, H = p.c.kv_heads;
@@ -352,27 +392,32 @@ __global__ void __launch_bounds__(TILE_THREADS, 1) kv_attend_tile_kernel(const A
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     if (threadIdx.x == 0) {
         for (int i = 0; i < 2; ++i) {
-            mbar_init(smem_u32(&sh->k_full[i]), 3); mbar_init(smem_u32(&sh->k_empty[i]), 1);
-            mbar_init(smem_u32(&sh->v_full[i]), 3); mbar_init(smem_u32(&sh->v_empty[i]), 1);
+            mbar_init(smem_u32(&sh->k_full[i]), TILE_MOVERS); mbar_init(smem_u32(&sh->k_empty[i]), 1);
+            mbar_init(smem_u32(&sh->v_full[i]), TILE_MOVERS); mbar_init(smem_u32(&sh->v_empty[i]), 1);
             mbar_init(smem_u32(&sh->q_full[i]), 4); mbar_init(smem_u32(&sh->s_full[i]), 1);
             mbar_init(smem_u32(&sh->p_full[i]), 4); mbar_init(smem_u32(&sh->o_full[i]), 1);
             mbar_init(smem_u32(&sh->o_empty[i]), 4);
         }
+        for (int i = 0; i < TILE_AHEAD; ++i) { mbar_init(smem_u32(&sh->i_full[i]), 1); mbar_init(smem_u32(&sh->i_empty[i]), TILE_MOVERS); }
+        for (int i = 0; i < TILE_AHEAD; ++i) { mbar_init(smem_u32(&sh->g_full[i]), 1); mbar_init(smem_u32(&sh->g_empty[i]), 4 * NQ + 1); }
+        for (int i = 0; i < 4; ++i) { mbar_init(smem_u32(&sh->r_full[i]), 1); mbar_init(smem_u32(&sh->r_empty[i]), TILE_MOVERS); }
         sh->abort_flag = 0;
         sh->nan_found = 0;
         p.join[blockIdx.x] = {0, 0, 0, 0};
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
-    if (warp == 11) {
+    if (warp == 12) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&sh->tmem)), "r"(512u) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     }
     tc_fence_before();
-    TileWalk<ROWS> w = tile_share<ROWS>(p, sh);      // (synchronises the block)
+    TileWalk<ROWS> w = tile_share<ROWS>(p, reinterpret_cast<int*>(smem + S::RAW_AT));      // (synchronises the block)
     __syncthreads();
     tc_fence_after();
     const uint32_t tmem = sh->tmem;
     bool ok = true;
+    if (warp < 8) asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(TILE_REGS_SOFTMAX));
+    else asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(TILE_REGS_REST));
 
     if (warp < 4 * NQ) {
         // ------------------------------------------------------------------------------------------ softmax
@@ -382,10 +427,16 @@ __global__ void __launch_bounds__(TILE_THREADS, 1) kv_attend_tile_kernel(const A
         const uint32_t t_s = tmem + lanes + S::S_COL + qt * 128, t_p = tmem + lanes + S::P_COL + qt * 128;
         const uint32_t t_o = tmem + lanes + S::O_COL + qt * D;
         uint32_t s_ph = 0, o_ph = 0;
-        int tile = 0;                                // tiles staged so far, over all segments (for the group ring)
-        auto mine = [&](const TileWalk<ROWS>& x) { return !x.done() && x.t.nrows > 128 * qt; };
-        auto stage = [&](const TileWalk<ROWS>& x) {
-            const TileRow r = stage_row<T, D, ROWS>(p, x, 128 * qt + tid, tid, q);
+        int tile = 0;                                // tiles of the block so far, over all segments
+        auto meet = [&](int g) {                     // waits for the news of segment g
+            ok = warp_wait(&sh->g_full[g % TILE_AHEAD], (uint32_t)(g / TILE_AHEAD) & 1u, sh, p);
+        };
+        auto release = [&](int g) {
+            __syncwarp();
+            if (lane == 0) mbar_arrive(smem_u32(&sh->g_empty[g % TILE_AHEAD]));
+        };
+        auto stage = [&](const TileSegment& x) {
+            const TileRow r = stage_row<T, D>(p, x, 128 * qt + tid, tid, q);
             fence_async_smem();
             __syncwarp();
             if (lane == 0) mbar_arrive(smem_u32(&sh->q_full[qt]));
@@ -393,48 +444,54 @@ __global__ void __launch_bounds__(TILE_THREADS, 1) kv_attend_tile_kernel(const A
         };
         TileRow row = {0, 0, 0.f, -1, 0};
         bool staged = false;
-        while (ok && !w.done()) {
-            const int n = w.length();
-            if (!mine(w)) { tile += n; w.next(p); continue; }
+        meet(0);
+        for (int g = 0; ok; ++g) {
+            const TileSegment& w = sh->seg[g % TILE_AHEAD];
+            const TileSegment& nx = sh->seg[(g + 1) % TILE_AHEAD];
+            if (!w.live) break;
+            const int n = w.n;
+            if (w.nrows <= 128 * qt) {
+                tile += n;
+                staged = false;
+                release(g);
+                meet(g + 1);
+                continue;
+            }
             if (!staged) row = stage(w);
             float m = -INFINITY, l = 0.f;
             for (int i = 0; i < n; ++i, ++tile) {
                 if (!(ok = warp_wait(&sh->s_full[qt], s_ph, sh, p))) break;
                 s_ph ^= 1;
                 tc_fence_after();
-                const int t0 = w.t.base + (w.unit + i) * TILE_UNIT;
-                const float4* group = sh->group[tile & 3];
-                bool edge = t0 < w.t.lo_all || t0 + TILE_UNIT > w.t.hi_all;
-#pragma unroll
-                for (int g = 0; g < 8; ++g) edge = edge || group[g].w != 0.f;      // (a page that is not there)
-                uint32_t pr[64];
-                float sum, m_use = (m == -INFINITY ? 0.f : m) - TILE_SHIFT;
-                float mx = edge ? tile_weights<T, true>(t_s, t_p, group, row, m_use, t0, pr, sum)
-                                : tile_weights<T, false>(t_s, t_p, group, row, m_use, t0, pr, sum);
-                const bool raise = mx > TILE_TOP || (m == -INFINITY && mx > -INFINITY);
-                if (__any_sync(0xffffffffu, raise)) {
-                    if (sizeof(T) == 4) tc_wait_st();
-                    const float now = fmaxf(m, mx + m_use);                      // (mx = -inf leaves m)
-                    const float corr = m == -INFINITY ? 0.f : exp2_fast(m - now);
-                    if (i > 0)                                                   // (the scores' arrival says that the last sum is complete)
-                        for (int c = 0; c < D; c += 32) {
-                            uint32_t v[32];
-                            tc_ld32(t_o + c, v);
-                            tc_wait_ld();
-#pragma unroll
-                            for (int k = 0; k < 32; ++k) v[k] = __float_as_uint(__uint_as_float(v[k]) * corr);
-                            tc_st<32>(t_o + c, v);
+                const int t0 = w.t0 + i * TILE_UNIT;
+                const TileInfo& info = sh->info[tile % TILE_AHEAD];
+                const float4* group = info.group;
+                const bool edge = info.edge || info.absent;
+#pragma unroll 1
+                for (int half = 0; half < 2; ++half) {
+                    uint32_t pr[32], rest[TERMS == 2 ? 32 : 1];
+                    float sum, m_use = (m == -INFINITY ? 0.f : m) - TILE_SHIFT;
+                    const float mx = edge ? half_weights<T, true>(t_s + 64 * half, group + 4 * half, row, m_use, t0 + 64 * half, pr, rest, sum)
+                                          : half_weights<T, false>(t_s + 64 * half, group + 4 * half, row, m_use, t0 + 64 * half, pr, rest, sum);
+                    if (__any_sync(0xffffffffu, mx > TILE_TOP || (m == -INFINITY && mx > -INFINITY))) {
+                        // the maximum moves by whole powers of two, so what has been summed so far is scaled exactly
+                        const float now = fmaxf(m, ceilf(mx + m_use));           // (mx = -inf leaves m)
+                        const float corr = m == -INFINITY ? 0.f : exp2_fast(m - now);
+                        if (i > 0)                                               // (the scores' arrival says that the last sum is complete)
+                            for (int c = 0; c < D; c += 32) scale_columns(t_o + c, corr);
+                        if (half == 1) {
+                            tc_wait_st();
+                            for (int k = 0; k < TERMS; ++k) scale_halves(t_p + 64 * k, corr);
                         }
-                    l *= corr;
-                    m = now;
-                    m_use = (m == -INFINITY ? 0.f : m) - TILE_SHIFT;
-                    if (edge) tile_weights<T, true>(t_s, t_p, group, row, m_use, t0, pr, sum);
-                    else tile_weights<T, false>(t_s, t_p, group, row, m_use, t0, pr, sum);
-                }
-                l += sum;
-                if constexpr (sizeof(T) == 2) {
-                    tc_st<32>(t_p, pr);
-                    tc_st<32>(t_p + 32, pr + 32);
+                        l *= corr;
+                        m = now;
+                        m_use = (m == -INFINITY ? 0.f : m) - TILE_SHIFT;
+                        if (edge) half_weights<T, true>(t_s + 64 * half, group + 4 * half, row, m_use, t0 + 64 * half, pr, rest, sum);
+                        else half_weights<T, false>(t_s + 64 * half, group + 4 * half, row, m_use, t0 + 64 * half, pr, rest, sum);
+                    }
+                    l += sum;
+                    tc_st<32>(t_p + 32 * half, pr);
+                    if constexpr (TERMS == 2) tc_st<32>(t_p + 64 + 32 * half, rest);
                 }
                 tc_wait_st();
                 tc_fence_before();
@@ -443,16 +500,16 @@ __global__ void __launch_bounds__(TILE_THREADS, 1) kv_attend_tile_kernel(const A
             }
             if (!ok) break;
             // the next segment's queries go in before this one's output is complete
-            TileWalk<ROWS> nx = w;
-            nx.next(p);
-            staged = mine(nx);
+            meet(g + 1);
+            if (!ok) break;
             TileRow nrow = row;
+            staged = nx.live && nx.nrows > 128 * qt;
             if (staged) nrow = stage(nx);
             if (!(ok = warp_wait(&sh->o_full[qt], o_ph, sh, p))) break;
             o_ph ^= 1;
             tc_fence_after();
-            const bool starts = w.unit == 0, ends = w.unit + n == w.t.units, whole = starts && ends;
-            const int64_t slot = (2 * (int64_t)blockIdx.x + (starts ? 1 : 0)) * p.slot_rows + 128 * qt + tid;
+            const bool whole = w.starts && w.ends;
+            const int64_t slot = (2 * (int64_t)blockIdx.x + (w.starts ? 1 : 0)) * p.slot_rows + 128 * qt + tid;
             const float inv = l != 0.f ? 1.f / l : 0.f;
             const bool nan = *(volatile int*)&sh->nan_found != 0;
             for (int c = 0; c < D; c += 32) {
@@ -462,8 +519,8 @@ __global__ void __launch_bounds__(TILE_THREADS, 1) kv_attend_tile_kernel(const A
                 if (nan) {
                     // values that are NaN were staged as zeros where some rows do not see them: find those this row sees
                     for (int i = 0; i < n; ++i) {
-                        const int t0 = w.t.base + (w.unit + i) * TILE_UNIT;
-                        if (t0 >= w.t.lo_all && t0 + TILE_UNIT <= w.t.hi_all) continue;
+                        const int t0 = w.t0 + i * TILE_UNIT;
+                        if (t0 >= w.lo_all && t0 + TILE_UNIT <= w.hi_all) continue;
                         for (int t = max(t0, row.lo); t < min(t0 + TILE_UNIT, row.hi); ++t) {
                             const int page = load_page(p.bt, p.c, w.b, t / P, nullptr);
                             if (page < 0) continue;
@@ -497,110 +554,175 @@ __global__ void __launch_bounds__(TILE_THREADS, 1) kv_attend_tile_kernel(const A
                 if (!whole) p.part_ml[slot] = make_float2(m, l);
                 else if (p.lse) p.lse[(int64_t)row.token * p.q_heads + row.head] = lse_of(m, l, TILE_SHIFT);
             }
-            if (starts && !ends && threadIdx.x == 0) {
-                const int64_t x = (int64_t)w.u + w.t.units - 1;               // the item's last unit, and the block that takes it
-                const int z = (int)(((x + 1) * w.blocks - 1) / w.total);
-                p.join[blockIdx.x] = {z - (int)blockIdx.x + 1, w.s.first * p.group + w.t.row0, w.t.nrows, w.h * p.group};
-            }
+            if (w.starts && !w.ends && threadIdx.x == 0) p.join[blockIdx.x] = {w.parts, w.first * p.group + w.row0, w.nrows, w.h * p.group};
+            release(g);
             row = nrow;
-            w = nx;
         }
-    } else if (warp >= 8 && warp < 11) {
-        // ------------------------------------------------------------------------------------------ codes to halves
-        // a warp moves eight rows by 64 codes at a time, a thread 16 of a row, so that the eight lanes of a store phase
-        // meet eight different banks; the pieces of a tile go around the three warps
-        const int cw = warp - 8, rl = lane >> 2, piece = lane & 3;
-        constexpr int HALVES = D / 64, PIECES = 16 * HALVES, ROUNDS = (PIECES + 2) / 3;
-        uint32_t ks = 0, kp = 1, vs = 0, vp = 1;                                // slots and parities (the first use passes at once)
-        int tile = 0;
-        // pages and scales of a tile: lane g < 8 holds those of its 16 tokens [16 g, 16 g + 16)
-        auto find = [&](const TileWalk<ROWS>& x, int unit) {
-            int page = -1;
-            const int th = x.t.base + unit * TILE_UNIT + (lane & 7) * 16;
-            if (th < x.t.hi && th + 16 > x.t.lo) page = load_page(p.bt, p.c, x.b, th / P, lane < 8 && cw == 0 ? p.status : nullptr);
-            return page;
-        };
-        auto fetch = [&](const TileWalk<ROWS>& x, int unit, int page, int j, uint4 (&raw)[ROUNDS]) {
-#pragma unroll
-            for (int r = 0; r < ROUNDS; ++r) {
-                const int u = 3 * r + cw, at = u / HALVES * 8 + rl, t = x.t.base + unit * TILE_UNIT + at;
-                const int pg = __shfl_sync(0xffffffffu, page, (u / HALVES / 2) & 7);
-                raw[r] = make_uint4(0, 0, 0, 0);
-                if (u < PIECES && pg >= 0 && t >= x.t.lo && t < x.t.hi)
-                    raw[r] = __ldg(reinterpret_cast<const uint4*>((const uint8_t*)p.c.codes + ((((int64_t)pg * 2 + j) * H + x.h) * P + t % P) * D + u % HALVES * 64 + piece * 16));
+    } else if (warp == 13) {
+        // ------------------------------------------------------------------------------------------ coming tiles
+        // four tiles at a time: lane 8 k + g looks after the 16 tokens [16 g, 16 g + 16) of tile k, so that the loads of
+        // four tiles (page, then its scales) are on their way together
+        const int pshift = 31 - __clz(P), k = lane >> 3, g = lane & 7;
+        int unit = 0, left = 0, tile = 0, seg = 0;
+        auto begin = [&]() {                     // the segment w stands on: tells of it
+            unit = w.unit;
+            left = w.done() ? 0 : w.length();
+            const int slot = seg % TILE_AHEAD;
+            ok = warp_wait(&sh->g_empty[slot], ((uint32_t)(seg / TILE_AHEAD) & 1u) ^ 1u, sh, p);
+            if (ok && lane == 0) {
+                TileSegment x;
+                x.live = left > 0;
+                x.n = left;
+                x.starts = unit == 0;
+                x.ends = unit + left == w.t.units;
+                // the block that takes the item's last unit u is the largest i with floor(i U / G) <= u
+                const int64_t last = (int64_t)w.u - unit + w.t.units - 1;
+                x.parts = w.done() ? 0 : (int)(((last + 1) * w.blocks - 1) / w.total) - (int)blockIdx.x + 1;
+                x.b = w.b; x.h = w.h; x.row0 = w.t.row0; x.nrows = w.t.nrows;
+                x.first = w.s.first; x.before = w.s.total - w.s.n; x.total = w.s.total;
+                x.t0 = w.t.base + unit * TILE_UNIT;
+                x.lo_all = w.t.lo_all; x.hi_all = w.t.hi_all;
+                sh->seg[slot] = x;
+                mbar_arrive(smem_u32(&sh->g_full[slot]));
             }
-        };
-        auto put = [&](uint8_t* dst, const uint4 (&raw)[ROUNDS]) {
-#pragma unroll
-            for (int r = 0; r < ROUNDS; ++r) {
-                const int u = 3 * r + cw, at = u / HALVES * 8 + rl;
-                if (u >= PIECES) break;
-                const uint32_t c[4] = {raw[r].x, raw[r].y, raw[r].z, raw[r].w};
-                uint32_t y[8];
-#pragma unroll
-                for (int k = 0; k < 4; ++k) { y[2 * k] = e4m3x2_to_half2(c[k] & 0xFFFFu); y[2 * k + 1] = e4m3x2_to_half2(c[k] >> 16); }
-                uint8_t* line = dst + u % HALVES * S::HALF + at * 128;
-                *reinterpret_cast<uint4*>(line + ((2 * piece) ^ (at & 7)) * 16) = make_uint4(y[0], y[1], y[2], y[3]);
-                *reinterpret_cast<uint4*>(line + ((2 * piece + 1) ^ (at & 7)) * 16) = make_uint4(y[4], y[5], y[6], y[7]);
-            }
-        };
-        uint4 kraw[ROUNDS], vraw[ROUNDS];
-        int unit = w.unit, left = w.done() ? 0 : w.length(), page = -1;
-        if (left) { page = find(w, unit); fetch(w, unit, page, 0, kraw); }
-        while (ok && left) {
-            // what comes after this tile
-            TileWalk<ROWS> nx = w;
-            int nunit = unit + 1, nleft = left - 1;
-            if (!nleft) {
-                nx.next(p);
-                nunit = nx.unit;
-                nleft = nx.done() ? 0 : nx.length();
-            }
-            const int npage = nleft ? find(nx, nunit) : -1;
-            fetch(w, unit, page, 1, vraw);
-            if (cw == 0 && lane < 8) {
-                float4 g = make_float4(0.f, -INFINITY, 0.f, 1.f);                // not there: weighs nothing
-                const int th = w.t.base + unit * TILE_UNIT + lane * 16;
-                if (page >= 0) {
-                    g.x = __ldg(p.c.scales + (int64_t)page * 2 * H + w.h);
-                    scale_terms(__ldg(p.c.scales + ((int64_t)page * 2 + 1) * H + w.h), g.y, g.z);
-                    g.w = 0.f;
-                } else if (th >= w.t.hi || th + 16 <= w.t.lo) g.w = 0.f;         // masked anyway
-                sh->group[tile & 3][lane] = g;
-            }
-            if (!(ok = warp_wait(&sh->k_empty[ks], kp, sh, p))) break;
-            put(smem + S::K_AT + ks * S::KV, kraw);
-            fence_async_smem();
             __syncwarp();
-            if (lane == 0) mbar_arrive(smem_u32(&sh->k_full[ks]));
-            if (++ks == 2) { ks = 0; kp ^= 1; }
-            if (nleft) fetch(nx, nunit, npage, 0, kraw);
-            // NaN values that not every row of the item sees: staged as zeros, put in place at the end
-            const int t0 = w.t.base + unit * TILE_UNIT;
-            if (t0 < w.t.lo_all || t0 + TILE_UNIT > w.t.hi_all) {
-                bool any = false;
+            ++seg;
+        };
+        begin();
+        for (bool more = true; ok && more;) {
+            int t0 = 0, lo = 0, hi = 0, b = 0, h = 0;
+            bool live = false, edge = false;
+#pragma unroll 1
+            for (int i = 0; i < 4; ++i) {
+                if (i == k) {
+                    live = left > 0;
+                    t0 = w.t.base + unit * TILE_UNIT;
+                    lo = w.t.lo; hi = w.t.hi; b = w.b; h = w.h;
+                    edge = t0 < w.t.lo_all || t0 + TILE_UNIT > w.t.hi_all;
+                }
+                if (left > 0) {
+                    ++unit;
+                    if (--left == 0) {
+                        w.next(p);
+                        if (ok) begin();
+                    }
+                } else {
+                    more = false;                                               // the tile after the last is marked as none
+                }
+            }
+            if (!ok) break;
+            const int th = t0 + g * 16;
+            const bool wanted = live && th < hi && th + 16 > lo;
+            const int page = wanted ? load_page(p.bt, p.c, b, th >> pshift, p.status) : -1;
+            float4 c = make_float4(0.f, -INFINITY, 0.f, 0.f);                    // not there: weighs nothing
+            int rows = -1;
+            if (page >= 0) {
+                const int at = page * 2 * H + h;
+                c.x = __ldg(p.c.scales + at);
+                scale_terms(__ldg(p.c.scales + at + H), c.y, c.z);
+                rows = (at << pshift >> 4) + ((th & (P - 1)) >> 4);
+            }
+            const unsigned gone = __ballot_sync(0xffffffffu, wanted && page < 0);
+            const int n = tile + k, slot = n % TILE_AHEAD;
+            // (a wait for each of the four slots in turn: a warp's lanes do not wait for different barriers)
+            for (int i = 0; i < 4 && ok; ++i) ok = warp_wait(&sh->i_empty[(tile + i) % TILE_AHEAD], ((tile + i) / TILE_AHEAD & 1) ^ 1, sh, p);
+            if (!ok) break;
+            TileInfo& info = sh->info[slot];
+            info.group[g] = c;
+            info.rows[g] = rows;
+            if (g == 0) {
+                info.live = live; info.edge = edge; info.t0 = t0; info.lo = lo; info.hi = hi;
+                info.absent = (gone >> (8 * k) & 0xFFu) != 0;
+            }
+            __syncwarp();
+            if (g == 0) mbar_arrive(smem_u32(&sh->i_full[slot]));
+            tile += 4;
+        }
+    } else if (warp == 14) {
+        // ------------------------------------------------------------------------------------------ codes in
+        const int64_t v_codes = (int64_t)H * P * D;                             // from a key to its value
+        for (int tile = 0; ok; ++tile) {
+            if (!(ok = warp_wait(&sh->i_full[tile % TILE_AHEAD], (uint32_t)(tile / TILE_AHEAD) & 1u, sh, p))) break;
+            const TileInfo& c = sh->info[tile % TILE_AHEAD];
+            if (!c.live) break;
+            const int rows = c.rows[lane & 7];
+            for (int part = 0; part < 4; ++part) {                              // keys, keys, values, values
+                if (!(ok = warp_wait(&sh->r_empty[part], ((uint32_t)tile & 1u) ^ 1u, sh, p))) break;
+                const int mine = __shfl_sync(0xffffffffu, rows, (part & 1) * 4 + (lane & 3));
+                const int n = __popc(__ballot_sync(0xffffffffu, lane < 4 && mine >= 0));
+                const uint32_t bar = smem_u32(&sh->r_full[part]);
+                if (lane == 0) mbar_expect_tx(bar, n * 16 * D);
+                __syncwarp();
+                if (lane < 4 && mine >= 0)
+                    bulk_load(smem_u32(smem + S::RAW_AT + part * S::RAW + lane * 16 * D), (const uint8_t*)p.c.codes + (int64_t)mine * (16 * D) + (part >= 2 ? v_codes : 0), 16 * D, bar);
+            }
+        }
+    } else if (warp >= 8 && warp < 12) {
+        // ------------------------------------------------------------------------------------------ codes to halves
+        // A thread takes 16 codes of a row at a time, a warp eight rows by four such pieces: of one half of the channels in
+        // even rows and of the other in odd ones (head dimension 128), so that the eight lanes of a phase meet eight
+        // different banks both reading and writing.
+        const int cw = warp - 8, rl = lane >> 2, piece = lane & 3;
+        constexpr int ROUNDS = D == 128 ? 4 : 2, STEP = D == 128 ? 16 : 32;      // rows that the four warps take at a time
+        const int row_in = D == 128 ? (cw & 1) * 8 + rl : cw * 8 + rl, half = D == 128 ? (cw >> 1) ^ (rl & 1) : 0;
+        const uint32_t from = row_in * D + half * 64 + piece * 16;
+        const uint32_t line = half * S::HALF + row_in * 128, at0 = line + ((2 * piece) ^ rl) * 16, at1 = line + ((2 * piece + 1) ^ rl) * 16;
+        // one half tile from the ring to its place; `masked`: tokens that are not there or that no row sees become zeros, and
+        // so do NaN values that not every row sees (they are put in place at the end)
+        auto move = [&](const TileInfo& c, int part, uint8_t* dst, bool masked) {
+            const uint8_t* src = smem + S::RAW_AT + part * S::RAW + from;
+            const int base = (part & 1) * 64;
+            dst += base * 128;
 #pragma unroll
-                for (int r = 0; r < ROUNDS; ++r) {
-                    uint32_t* c = reinterpret_cast<uint32_t*>(&vraw[r]);
+            for (int r = 0; r < ROUNDS; ++r) {
+                uint4 raw = *reinterpret_cast<const uint4*>(src + r * (STEP * D));
+                if (masked) {
+                    const int at = base + r * STEP + row_in, t = c.t0 + at;
+                    if (c.rows[at >> 4] < 0 || t < c.lo || t >= c.hi) raw = make_uint4(0, 0, 0, 0);
+                    if (part >= 2 && c.edge) {
+                        uint32_t* x = reinterpret_cast<uint32_t*>(&raw);
+                        uint32_t any = 0;
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) {
-                        const uint32_t n4 = __vcmpeq4(c[k] & 0x7F7F7F7Fu, 0x7F7F7F7Fu);
-                        any = any || n4;
-                        c[k] &= ~n4;
+                        for (int k = 0; k < 4; ++k) {
+                            const uint32_t n4 = __vcmpeq4(x[k] & 0x7F7F7F7Fu, 0x7F7F7F7Fu);
+                            any |= n4;
+                            x[k] &= ~n4;
+                        }
+                        if (any) *(volatile int*)&sh->nan_found = 1;
                     }
                 }
-                if (any) *(volatile int*)&sh->nan_found = 1;
+                const uint32_t w[4] = {raw.x, raw.y, raw.z, raw.w};
+                uint32_t y[8];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) { y[2 * k] = e4m3x2_to_half2(w[k] & 0xFFFFu); y[2 * k + 1] = e4m3x2_to_half2(w[k] >> 16); }
+                *reinterpret_cast<uint4*>(dst + r * (STEP * 128) + at0) = make_uint4(y[0], y[1], y[2], y[3]);
+                *reinterpret_cast<uint4*>(dst + r * (STEP * 128) + at1) = make_uint4(y[4], y[5], y[6], y[7]);
             }
-            if (!(ok = warp_wait(&sh->v_empty[vs], vp, sh, p))) break;
-            put(smem + S::V_AT + vs * S::KV, vraw);
-            fence_async_smem();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(smem_u32(&sh->v_full[vs]));
-            if (++vs == 2) { vs = 0; vp ^= 1; }
-            ++tile;
-            w = nx; unit = nunit; left = nleft; page = npage;
+        };
+        for (int tile = 0; ok; ++tile) {
+            if (!(ok = warp_wait(&sh->i_full[tile % TILE_AHEAD], (uint32_t)(tile / TILE_AHEAD) & 1u, sh, p))) break;
+            const TileInfo& c = sh->info[tile % TILE_AHEAD];
+            if (!c.live) break;
+            const bool masked = c.edge || c.absent;
+            const int slot = tile & 1;
+            const uint32_t free_ph = ((uint32_t)(tile >> 1) & 1u) ^ 1u;          // (the first use passes at once)
+#pragma unroll 1
+            for (int part = 0; part < 4; ++part) {
+                if (part == 0 && !(ok = warp_wait(&sh->k_empty[slot], free_ph, sh, p))) break;
+                if (part == 2 && !(ok = warp_wait(&sh->v_empty[slot], free_ph, sh, p))) break;
+                if (!(ok = warp_wait(&sh->r_full[part], (uint32_t)tile & 1u, sh, p))) break;
+                move(c, part, smem + (part < 2 ? S::K_AT : S::V_AT) + slot * S::KV, masked);
+                if (part & 1) fence_async_smem();
+                __syncwarp();
+                if (lane == 0) {
+                    mbar_arrive(smem_u32(&sh->r_empty[part]));
+                    if (part & 1) mbar_arrive(smem_u32(part == 1 ? &sh->k_full[slot] : &sh->v_full[slot]));
+                    // the slot of values held the tile before last: its softmax is over, its news may go
+                    if (part == 3 && tile >= 2) mbar_arrive(smem_u32(&sh->i_empty[(tile - 2) % TILE_AHEAD]));
+                }
+            }
         }
-    } else if (warp == 11) {
+    } else if (warp == 12) {
         // ------------------------------------------------------------------------------------------ MMAs
         // D = F32, A = B = F16; scores: both K-major; outputs: A in TMEM, B MN-major (bit 16)
         constexpr uint32_t I_S = (1u << 4) | ((128u >> 3) << 17) | ((128u >> 4) << 24);
@@ -638,8 +760,13 @@ __global__ void __launch_bounds__(TILE_THREADS, 1) kv_attend_tile_kernel(const A
             if (elect_one()) tc_commit(smem_u32(bar));
             __syncwarp();
         };
-        while (ok && !w.done()) {
-            const int n = w.length(), nq = w.t.nrows > 128 ? 2 : 1;
+        for (int g = 0; ok; ++g) {
+            if (!(ok = warp_wait(&sh->g_full[g % TILE_AHEAD], (uint32_t)(g / TILE_AHEAD) & 1u, sh, p))) break;
+            const TileSegment& x = sh->seg[g % TILE_AHEAD];
+            if (!x.live) break;
+            const int n = x.n, nq = x.nrows > 128 ? 2 : 1;
+            __syncwarp();
+            if (lane == 0) mbar_arrive(smem_u32(&sh->g_empty[g % TILE_AHEAD]));
             if (!(ok = warp_wait(&sh->q_full[0], q_ph, sh, p))) break;
             q_ph ^= 1;
             if (nq == 2) {
@@ -677,7 +804,6 @@ __global__ void __launch_bounds__(TILE_THREADS, 1) kv_attend_tile_kernel(const A
                 if (i + 1 < n && ++ks == 2) { ks = 0; kp ^= 1; }
                 if (++vs == 2) { vs = 0; vp ^= 1; }
             }
-            w.next(p);
         }
     }
     if (!ok) {                                       // MMAs still reading shared memory
@@ -686,7 +812,7 @@ __global__ void __launch_bounds__(TILE_THREADS, 1) kv_attend_tile_kernel(const A
     }
     tc_fence_before();
     __syncthreads();
-    if (warp == 11) {
+    if (warp == 12) {
         tc_fence_after();
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u) : "memory");
     }
