@@ -1,14 +1,15 @@
 // Attention of many query rows (frames, prompts) over the paged E4M3 cache, on tcgen05.
 //
 // Bound by the tensor cores.  An item is a block of 256 query rows of one kv head (F32: 128), rows being (token, head of
-// the group) so that grouped heads share the keys they share; a unit is 128 cached tokens.  16 warps, one block to an SM:
+// the group) so that grouped heads share the keys they share; a unit is 128 cached tokens.  20 warps, one block to an SM:
 //   warps 0-3, 4-7   softmax of the first and second 128 rows, a thread to a row: scores from TMEM, weights back as halves
 //                    over them, sums in registers, the output from TMEM at the end; they also stage the queries
-//   warps 8-11       turn codes into halves in shared memory (exact), keys and values in two slots each
-//   warp 12          issues the MMAs: S = Q K^T from shared memory, O += P V with P in TMEM
-//   warp 13          walks the block's share ahead of the others and tells them of it: segments (an item, or the stretch of
+//   warps 8-11, 12-15  turn codes into halves in shared memory (exact): keys and values, two slots each
+//   warps 16, 19     issue the MMAs of one row block each: S = Q K^T from shared memory, O += P V with P in TMEM (an issuer is
+//                    held up while the tensor cores work on what it issued: with one for both the blocks waited in line)
+//   warp 17          walks the block's share ahead of the others and tells them of it: segments (an item, or the stretch of
 //                    it that falls to this block), and pages and scales of up to eight coming tiles
-//   warp 14          brings the codes in: bulk copies of 16 tokens into a ring of four half tiles
+//   warp 18          brings the codes in: bulk copies of 16 tokens into a ring of four half tiles
 // Two row blocks in turn keep the tensor cores busy: while one is in its softmax the other's products run.
 //
 // Keys and values are staged alike, rows of 64 channels (128 bytes, 128-byte swizzle) token by token: K-major for the
@@ -20,10 +21,10 @@
 
 namespace ccv3d {
 
-constexpr int TILE_UNIT = 128, TILE_THREADS = 512;
+constexpr int TILE_UNIT = 128, TILE_THREADS = 640;
 constexpr int TILE_BATCH = 1024;                       // sequences whose costs are counted at a time (in the ring of codes)
 constexpr int TILE_MOVERS = 4, TILE_AHEAD = 8;                         // warps that turn codes into halves
-constexpr int TILE_REGS_SOFTMAX = 184, TILE_REGS_REST = 72;   // 256 threads each: 65536 registers, what 512 threads are launched with
+constexpr int TILE_REGS_SOFTMAX = 168, TILE_REGS_REST = 48;   // of 256 and 384 threads: 61440 registers, what 640 threads are launched with at 96
 constexpr float TILE_SHIFT = 8.f, TILE_TOP = 15.f;      // weights start at 2^8 for the maximum and may reach 2^15
 
 template <typename T, int D> struct TileShape {
@@ -55,7 +56,7 @@ struct TileSegment {
 struct TileShared {
     TileInfo info[TILE_AHEAD];
     TileSegment seg[TILE_AHEAD];
-    uint64_t k_full[2], k_empty[2], v_full[2], v_empty[2], q_full[2], s_full[2], p_full[2], o_full[2], o_empty[2];
+    uint64_t k_full[2], k_empty[2], v_full[2], v_empty[2], q_full[2], s_full[2], p_full[2][2], h_done[2], o_full[2], o_empty[2], turn[2];
     uint64_t i_full[TILE_AHEAD], i_empty[TILE_AHEAD], g_full[TILE_AHEAD], g_empty[TILE_AHEAD];
     uint64_t r_full[4], r_empty[4];
     uint32_t tmem;
@@ -200,6 +201,10 @@ __device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity, TileSh
     return __all_sync(0xffffffffu, tile_wait(bar, parity, sh, p));
 }
 
+__device__ __forceinline__ void bulk_prefetch(const void* p, uint32_t bytes) {
+    asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(p), "r"(bytes) : "memory");
+}
+
 // upper word of a shared-memory operand descriptor: stride-dimension offset, version 1, 128-byte swizzle
 __device__ __forceinline__ uint32_t tile_desc_hi(uint32_t sbo) { return ((sbo >> 4) & 0x3FFFu) | (1u << 14) | (2u << 29); }
 
@@ -318,45 +323,60 @@ __device__ __forceinline__ TileRow stage_row(const AttendParams& p, const TileSe
     return row;
 }
 
-// Half a tile's scores (64 tokens) to weights: packed into pr (F32: remainders into rest).  Returns the largest exponent
-// met; sum gets what the half adds to the row's weight sum.
-template <typename T, bool EDGE>
-__device__ __forceinline__ float half_weights(uint32_t t_s, const float4* group, const TileRow& row, float m_use, int t0, uint32_t (&pr)[32],
-                                              uint32_t (&rest)[sizeof(T) == 4 ? 32 : 1], float& sum) {
-    float mx = -INFINITY;
-    sum = 0.f;
+// two floats to an instruction
+__device__ __forceinline__ uint64_t pair(float a, float b) {
+    uint64_t r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+    return r;
+}
+__device__ __forceinline__ void unpair(uint64_t v, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v)); }
+__device__ __forceinline__ uint64_t fma_pair(uint64_t a, uint64_t b, uint64_t c) {
+    uint64_t r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+__device__ __forceinline__ uint64_t add_pair(uint64_t a, uint64_t b) {
+    uint64_t r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ float max3(float a, float b, float c) {      // (NaN stays out, as with fmaxf)
+    float r;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+    return r;
+}
+
+// Scores of 32 tokens (two groups of 16) to weights: packed into pr (F32: remainders into rest).  mx gathers the largest
+// exponent met, sum what the weights add to the row's weight sum.
+template <bool REST, bool EDGE>
+__device__ __forceinline__ void chunk_weights(const uint32_t (&v)[32], const float4* group, const TileRow& row, float m_use, int t0, uint32_t* pr,
+                                              uint32_t* rest, float& mx, float& sum) {
 #pragma unroll
-    for (int c = 0; c < 2; ++c) {
-        uint32_t v[32];
-        tc_ld32(t_s + 32 * c, v);
-        tc_wait_ld();
+    for (int g = 0; g < 2; ++g) {
+        const float4 k = group[g];
+        const float f = k.x * row.factor, a = k.y - m_use;
+        const uint64_t f2 = pair(f, f), a2 = pair(a, a);
+        uint64_t part = 0;                                       // two sums: even and odd tokens
 #pragma unroll
-        for (int g = 0; g < 2; ++g) {
-            const float4 k = group[2 * c + g];
-            const float f = k.x * row.factor, a = k.y - m_use;
-            float part = 0.f;
-#pragma unroll
-            for (int i = 0; i < 16; i += 2) {
-                float t[2], e[2];
-#pragma unroll
-                for (int j = 0; j < 2; ++j) {
-                    t[j] = fmaf(__uint_as_float(v[16 * g + i + j]), f, a);
-                    if (EDGE) {
-                        const int at = t0 + 32 * c + 16 * g + i + j;
-                        if (at < row.lo || at >= row.hi || k.y == -INFINITY) t[j] = -INFINITY;
-                    }
-                    mx = fmaxf(mx, t[j]);
-                    e[j] = exp2_fast(t[j]);
-                    part += e[j];
-                }
-                const uint32_t h = pack_half(e[0], e[1]);
-                pr[16 * c + 8 * g + i / 2] = h;
-                if constexpr (sizeof(T) == 4) rest[16 * c + 8 * g + i / 2] = pack_rest(e[0], e[1], h);
+        for (int i = 0; i < 16; i += 2) {
+            float x, y;
+            unpair(fma_pair(pair(__uint_as_float(v[16 * g + i]), __uint_as_float(v[16 * g + i + 1])), f2, a2), x, y);
+            if (EDGE) {
+                const int at = t0 + 16 * g + i;
+                if (at < row.lo || at >= row.hi || k.y == -INFINITY) x = -INFINITY;
+                if (at + 1 < row.lo || at + 1 >= row.hi || k.y == -INFINITY) y = -INFINITY;
             }
-            sum = fmaf(part, k.z, sum);
+            mx = max3(mx, x, y);
+            const float e0 = exp2_fast(x), e1 = exp2_fast(y);
+            part = add_pair(part, pair(e0, e1));
+            const uint32_t h = pack_half(e0, e1);
+            pr[8 * g + i / 2] = h;
+            if (REST) rest[8 * g + i / 2] = pack_rest(e0, e1, h);
         }
+        float s0, s1;
+        unpair(part, s0, s1);
+        sum = fmaf(s0 + s1, k.z, sum);
     }
-    return mx;
 }
 // Scales 32 TMEM columns of this thread's lane: FP32 values or pairs of halves.
 __device__ __forceinline__ void scale_columns(uint32_t t, float f) {
@@ -367,17 +387,69 @@ __device__ __forceinline__ void scale_columns(uint32_t t, float f) {
     for (int k = 0; k < 32; ++k) v[k] = __float_as_uint(__uint_as_float(v[k]) * f);
     tc_st<32>(t, v);
 }
-__device__ __forceinline__ void scale_halves(uint32_t t, float f) {
-    uint32_t v[32];
-    const __half2 h = __float2half2_rn(f);
-    tc_ld32(t, v);
-    tc_wait_ld();
+
+// A softmax thread's state: TMEM addresses of its scores, weights and outputs, its running maximum (a whole number) and sum.
+struct TileSoftmax {
+    uint32_t t_s, t_p, t_o;
+    float m, l;
+};
+
+// One tile of a row: weights of 64 tokens twice; `ready(half)` tells the MMA warp that they are in TMEM.  The scores of the
+// next 32 tokens are on their way while those before are worked on.  Where a score passes the maximum by more than the
+// weights can hold, the maximum moves (by a whole power of two, so what has been summed is scaled exactly) and the half is
+// done again; `settled(half)` waits until the outputs hold all weights given before that half.
+template <typename T, int D, bool EDGE, typename Ready, typename Settled>
+__device__ __forceinline__ bool tile_softmax(TileSoftmax& x, const float4* group, const TileRow& row, int t0, bool first, const Ready& ready,
+                                             const Settled& settled) {
+    constexpr bool REST = sizeof(T) == 4;
+    uint32_t a[32], b[32], pr[32], rest[REST ? 32 : 16];
+    auto work = [&](const uint32_t (&v)[32], int c, float& mx, float& sum) {
+        chunk_weights<REST, EDGE>(v, group + 2 * c, row, (x.m == -INFINITY ? 0.f : x.m) - TILE_SHIFT, t0 + 32 * c, pr + 16 * (c & 1), rest + (REST ? 16 * (c & 1) : 0), mx, sum);
+    };
+    auto finish = [&](int half, float mx, float sum) {
+        if (__any_sync(0xffffffffu, mx > TILE_TOP || (x.m == -INFINITY && mx > -INFINITY))) {
+            const float now = fmaxf(x.m, ceilf(mx + ((x.m == -INFINITY ? 0.f : x.m) - TILE_SHIFT)));     // (mx = -inf leaves m)
+            const float corr = x.m == -INFINITY ? 0.f : exp2_fast(x.m - now);
+            if (!first || half == 1) {
+                if (!settled(half)) return false;
+                for (int c = 0; c < D; c += 32) scale_columns(x.t_o + c, corr);
+            }
+            x.l *= corr;
+            x.m = now;
+            mx = -INFINITY;
+            sum = 0.f;
 #pragma unroll
-    for (int k = 0; k < 32; ++k) {
-        const __half2 x = __hmul2(*reinterpret_cast<const __half2*>(&v[k]), h);
-        v[k] = *reinterpret_cast<const uint32_t*>(&x);
-    }
-    tc_st<32>(t, v);
+            for (int c = 0; c < 2; ++c) {
+                uint32_t v[32];
+                tc_ld32(x.t_s + 64 * half + 32 * c, v);
+                tc_wait_ld();
+                work(v, 2 * half + c, mx, sum);
+            }
+        }
+        x.l += sum;
+        tc_st<32>(x.t_p + 32 * half, pr);
+        if constexpr (REST) tc_st<32>(x.t_p + 64 + 32 * half, rest);
+        tc_wait_st();
+        ready(half);
+        return true;
+    };
+    float mx = -INFINITY, sum = 0.f;
+    tc_ld32(x.t_s, a);
+    tc_wait_ld();
+    tc_ld32(x.t_s + 32, b);
+    work(a, 0, mx, sum);
+    tc_wait_ld();
+    tc_ld32(x.t_s + 64, a);
+    work(b, 1, mx, sum);
+    if (!finish(0, mx, sum)) return false;
+    mx = -INFINITY;
+    sum = 0.f;
+    tc_wait_ld();
+    tc_ld32(x.t_s + 96, b);
+    work(a, 2, mx, sum);
+    tc_wait_ld();
+    work(b, 3, mx, sum);
+    return finish(1, mx, sum);
 }
 
 template <typename T, int D>
@@ -392,21 +464,22 @@ __global__ void __launch_bounds__(TILE_THREADS, 1) kv_attend_tile_kernel(const A
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     if (threadIdx.x == 0) {
         for (int i = 0; i < 2; ++i) {
-            mbar_init(smem_u32(&sh->k_full[i]), TILE_MOVERS); mbar_init(smem_u32(&sh->k_empty[i]), 1);
-            mbar_init(smem_u32(&sh->v_full[i]), TILE_MOVERS); mbar_init(smem_u32(&sh->v_empty[i]), 1);
+            mbar_init(smem_u32(&sh->k_full[i]), TILE_MOVERS); mbar_init(smem_u32(&sh->k_empty[i]), NQ);
+            mbar_init(smem_u32(&sh->v_full[i]), TILE_MOVERS); mbar_init(smem_u32(&sh->v_empty[i]), NQ);
             mbar_init(smem_u32(&sh->q_full[i]), 4); mbar_init(smem_u32(&sh->s_full[i]), 1);
-            mbar_init(smem_u32(&sh->p_full[i]), 4); mbar_init(smem_u32(&sh->o_full[i]), 1);
-            mbar_init(smem_u32(&sh->o_empty[i]), 4);
+            mbar_init(smem_u32(&sh->p_full[i][0]), 4); mbar_init(smem_u32(&sh->p_full[i][1]), 4);
+            mbar_init(smem_u32(&sh->h_done[i]), 1); mbar_init(smem_u32(&sh->o_full[i]), 1);
+            mbar_init(smem_u32(&sh->o_empty[i]), 4); mbar_init(smem_u32(&sh->turn[i]), 1);
         }
         for (int i = 0; i < TILE_AHEAD; ++i) { mbar_init(smem_u32(&sh->i_full[i]), 1); mbar_init(smem_u32(&sh->i_empty[i]), TILE_MOVERS); }
-        for (int i = 0; i < TILE_AHEAD; ++i) { mbar_init(smem_u32(&sh->g_full[i]), 1); mbar_init(smem_u32(&sh->g_empty[i]), 4 * NQ + 1); }
+        for (int i = 0; i < TILE_AHEAD; ++i) { mbar_init(smem_u32(&sh->g_full[i]), 1); mbar_init(smem_u32(&sh->g_empty[i]), 5 * NQ); }
         for (int i = 0; i < 4; ++i) { mbar_init(smem_u32(&sh->r_full[i]), 1); mbar_init(smem_u32(&sh->r_empty[i]), TILE_MOVERS); }
         sh->abort_flag = 0;
         sh->nan_found = 0;
         p.join[blockIdx.x] = {0, 0, 0, 0};
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
-    if (warp == 12) {
+    if (warp == 16) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&sh->tmem)), "r"(512u) : "memory");
         asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     }
@@ -458,46 +531,30 @@ __global__ void __launch_bounds__(TILE_THREADS, 1) kv_attend_tile_kernel(const A
                 continue;
             }
             if (!staged) row = stage(w);
-            float m = -INFINITY, l = 0.f;
+            TileSoftmax x = {t_s, t_p, t_o, -INFINITY, 0.f};
             for (int i = 0; i < n; ++i, ++tile) {
                 if (!(ok = warp_wait(&sh->s_full[qt], s_ph, sh, p))) break;
                 s_ph ^= 1;
                 tc_fence_after();
                 const int t0 = w.t0 + i * TILE_UNIT;
                 const TileInfo& info = sh->info[tile % TILE_AHEAD];
-                const float4* group = info.group;
-                const bool edge = info.edge || info.absent;
-#pragma unroll 1
-                for (int half = 0; half < 2; ++half) {
-                    uint32_t pr[32], rest[TERMS == 2 ? 32 : 1];
-                    float sum, m_use = (m == -INFINITY ? 0.f : m) - TILE_SHIFT;
-                    const float mx = edge ? half_weights<T, true>(t_s + 64 * half, group + 4 * half, row, m_use, t0 + 64 * half, pr, rest, sum)
-                                          : half_weights<T, false>(t_s + 64 * half, group + 4 * half, row, m_use, t0 + 64 * half, pr, rest, sum);
-                    if (__any_sync(0xffffffffu, mx > TILE_TOP || (m == -INFINITY && mx > -INFINITY))) {
-                        // the maximum moves by whole powers of two, so what has been summed so far is scaled exactly
-                        const float now = fmaxf(m, ceilf(mx + m_use));           // (mx = -inf leaves m)
-                        const float corr = m == -INFINITY ? 0.f : exp2_fast(m - now);
-                        if (i > 0)                                               // (the scores' arrival says that the last sum is complete)
-                            for (int c = 0; c < D; c += 32) scale_columns(t_o + c, corr);
-                        if (half == 1) {
-                            tc_wait_st();
-                            for (int k = 0; k < TERMS; ++k) scale_halves(t_p + 64 * k, corr);
-                        }
-                        l *= corr;
-                        m = now;
-                        m_use = (m == -INFINITY ? 0.f : m) - TILE_SHIFT;
-                        if (edge) half_weights<T, true>(t_s + 64 * half, group + 4 * half, row, m_use, t0 + 64 * half, pr, rest, sum);
-                        else half_weights<T, false>(t_s + 64 * half, group + 4 * half, row, m_use, t0 + 64 * half, pr, rest, sum);
+                auto ready = [&](int half) {
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(smem_u32(&sh->p_full[qt][half]));
+                };
+                auto settled = [&](int half) {       // (the scores' arrival says that the tile before is summed)
+                    if (half == 1) {
+                        if (!warp_wait(&sh->h_done[qt], s_ph ^ 1, sh, p)) return false;
+                        tc_fence_after();
                     }
-                    l += sum;
-                    tc_st<32>(t_p + 32 * half, pr);
-                    if constexpr (TERMS == 2) tc_st<32>(t_p + 64 + 32 * half, rest);
-                }
-                tc_wait_st();
-                tc_fence_before();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(smem_u32(&sh->p_full[qt]));
+                    return true;
+                };
+                ok = info.edge || info.absent ? tile_softmax<T, D, true>(x, info.group, row, t0, i == 0, ready, settled)
+                                              : tile_softmax<T, D, false>(x, info.group, row, t0, i == 0, ready, settled);
+                if (!ok) break;
             }
+            const float m = x.m, l = x.l;
             if (!ok) break;
             // the next segment's queries go in before this one's output is complete
             meet(g + 1);
@@ -558,7 +615,7 @@ __global__ void __launch_bounds__(TILE_THREADS, 1) kv_attend_tile_kernel(const A
             release(g);
             row = nrow;
         }
-    } else if (warp == 13) {
+    } else if (warp == 17) {
         // ------------------------------------------------------------------------------------------ coming tiles
         // four tiles at a time: lane 8 k + g looks after the 16 tokens [16 g, 16 g + 16) of tile k, so that the loads of
         // four tiles (page, then its scales) are on their way together
@@ -621,6 +678,10 @@ __global__ void __launch_bounds__(TILE_THREADS, 1) kv_attend_tile_kernel(const A
                 c.x = __ldg(p.c.scales + at);
                 scale_terms(__ldg(p.c.scales + at + H), c.y, c.z);
                 rows = (at << pshift >> 4) + ((th & (P - 1)) >> 4);
+                // into L2 already: the ring of codes is not deep enough to wait for HBM
+                const uint8_t* codes = (const uint8_t*)p.c.codes + (int64_t)rows * (16 * D);
+                bulk_prefetch(codes, 16 * D);
+                bulk_prefetch(codes + (int64_t)H * P * D, 16 * D);
             }
             const unsigned gone = __ballot_sync(0xffffffffu, wanted && page < 0);
             const int n = tile + k, slot = n % TILE_AHEAD;
@@ -638,7 +699,7 @@ __global__ void __launch_bounds__(TILE_THREADS, 1) kv_attend_tile_kernel(const A
             if (g == 0) mbar_arrive(smem_u32(&sh->i_full[slot]));
             tile += 4;
         }
-    } else if (warp == 14) {
+    } else if (warp == 18) {
         // ------------------------------------------------------------------------------------------ codes in
         const int64_t v_codes = (int64_t)H * P * D;                             // from a key to its value
         for (int tile = 0; ok; ++tile) {
@@ -657,12 +718,12 @@ __global__ void __launch_bounds__(TILE_THREADS, 1) kv_attend_tile_kernel(const A
                     bulk_load(smem_u32(smem + S::RAW_AT + part * S::RAW + lane * 16 * D), (const uint8_t*)p.c.codes + (int64_t)mine * (16 * D) + (part >= 2 ? v_codes : 0), 16 * D, bar);
             }
         }
-    } else if (warp >= 8 && warp < 12) {
+    } else if (warp >= 8 && warp < 16) {
         // ------------------------------------------------------------------------------------------ codes to halves
         // A thread takes 16 codes of a row at a time, a warp eight rows by four such pieces: of one half of the channels in
         // even rows and of the other in odd ones (head dimension 128), so that the eight lanes of a phase meet eight
         // different banks both reading and writing.
-        const int cw = warp - 8, rl = lane >> 2, piece = lane & 3;
+        const int cw = (warp - 8) & 3, values = warp >= 12, rl = lane >> 2, piece = lane & 3;
         constexpr int ROUNDS = D == 128 ? 4 : 2, STEP = D == 128 ? 16 : 32;      // rows that the four warps take at a time
         const int row_in = D == 128 ? (cw & 1) * 8 + rl : cw * 8 + rl, half = D == 128 ? (cw >> 1) ^ (rl & 1) : 0;
         const uint32_t from = row_in * D + half * 64 + piece * 16;
@@ -705,104 +766,112 @@ __global__ void __launch_bounds__(TILE_THREADS, 1) kv_attend_tile_kernel(const A
             if (!c.live) break;
             const bool masked = c.edge || c.absent;
             const int slot = tile & 1;
-            const uint32_t free_ph = ((uint32_t)(tile >> 1) & 1u) ^ 1u;          // (the first use passes at once)
+            if (!(ok = warp_wait(values ? &sh->v_empty[slot] : &sh->k_empty[slot], ((uint32_t)(tile >> 1) & 1u) ^ 1u, sh, p))) break;   // (the first use passes at once)
+            uint8_t* dst = smem + (values ? S::V_AT : S::K_AT) + slot * S::KV;
 #pragma unroll 1
-            for (int part = 0; part < 4; ++part) {
-                if (part == 0 && !(ok = warp_wait(&sh->k_empty[slot], free_ph, sh, p))) break;
-                if (part == 2 && !(ok = warp_wait(&sh->v_empty[slot], free_ph, sh, p))) break;
+            for (int part = 2 * values; part < 2 * values + 2; ++part) {
                 if (!(ok = warp_wait(&sh->r_full[part], (uint32_t)tile & 1u, sh, p))) break;
-                move(c, part, smem + (part < 2 ? S::K_AT : S::V_AT) + slot * S::KV, masked);
-                if (part & 1) fence_async_smem();
+                move(c, part, dst, masked);
                 __syncwarp();
-                if (lane == 0) {
-                    mbar_arrive(smem_u32(&sh->r_empty[part]));
-                    if (part & 1) mbar_arrive(smem_u32(part == 1 ? &sh->k_full[slot] : &sh->v_full[slot]));
-                    // the slot of values held the tile before last: its softmax is over, its news may go
-                    if (part == 3 && tile >= 2) mbar_arrive(smem_u32(&sh->i_empty[(tile - 2) % TILE_AHEAD]));
-                }
+                if (lane == 0) mbar_arrive(smem_u32(&sh->r_empty[part]));
+            }
+            fence_async_smem();
+            __syncwarp();
+            if (ok && lane == 0) {
+                mbar_arrive(smem_u32(values ? &sh->v_full[slot] : &sh->k_full[slot]));
+                // the slot of values held the tile before last: its softmax is over, its news may go
+                if (values && tile >= 2) mbar_arrive(smem_u32(&sh->i_empty[(tile - 2) % TILE_AHEAD]));
             }
         }
-    } else if (warp == 12) {
+    } else if (warp == 16 || (warp == 19 && NQ == 2)) {
         // ------------------------------------------------------------------------------------------ MMAs
+        const int qt = warp == 16 ? 0 : 1;
         // D = F32, A = B = F16; scores: both K-major; outputs: A in TMEM, B MN-major (bit 16)
         constexpr uint32_t I_S = (1u << 4) | ((128u >> 3) << 17) | ((128u >> 4) << 24);
         constexpr uint32_t I_O = (1u << 4) | (1u << 16) | (((uint32_t)D >> 3) << 17) | ((128u >> 4) << 24);
         const uint32_t hi = tile_desc_hi(1024);
-        const uint32_t q_lo = ((smem_u32(smem + S::Q_AT) & 0x3FFFFu) >> 4) | (1u << 16);
+        const uint32_t q_lo = ((smem_u32(smem + S::Q_AT + qt * S::Q) & 0x3FFFFu) >> 4) | (1u << 16);
         const uint32_t k_lo = ((smem_u32(smem + S::K_AT) & 0x3FFFFu) >> 4) | (1u << 16);
         const uint32_t v_lo = ((smem_u32(smem + S::V_AT) & 0x3FFFFu) >> 4) | ((S::HALF >> 4) << 16);
-        uint32_t ks = 0, kp = 0, vs = 0, vp = 0, q_ph = 0, p_ph[2] = {0, 0}, o_ph[2] = {1, 1}, q1_ph = 0;
-        auto scores = [&](int qt, uint32_t slot) {
+        const uint32_t d_s = tmem + S::S_COL + qt * 128, d_o = tmem + S::O_COL + qt * D, a_p = tmem + S::P_COL + qt * 128;
+        auto scores = [&](uint32_t slot) {           // and the slot's keys have been used
             if (elect_one()) {
-                const uint32_t a0 = q_lo + qt * (S::Q >> 4), b0 = k_lo + slot * (S::KV >> 4), d = tmem + S::S_COL + qt * 128;
+                const uint32_t b0 = k_lo + slot * (S::KV >> 4);
 #pragma unroll
                 for (int t = 0; t < TERMS; ++t)
 #pragma unroll
                     for (int k = 0; k < D / 16; ++k) {
                         const uint32_t off = (k / 4) * (S::HALF >> 4) + (k % 4) * 2;
-                        tc_mma_f16_ss(d, a0 + t * (S::KV >> 4) + off, b0 + off, hi, I_S, t + k > 0);
+                        tc_mma_f16_ss(d_s, q_lo + t * (S::KV >> 4) + off, b0 + off, hi, I_S, t + k > 0);
                     }
                 tc_commit(smem_u32(&sh->s_full[qt]));
+                tc_commit(smem_u32(&sh->k_empty[slot]));
             }
             __syncwarp();
         };
-        auto outputs = [&](int qt, uint32_t slot, bool first) {
+        auto outputs = [&](uint32_t slot, int half, bool first, bool last) {    // of the weights of 64 tokens
             if (elect_one()) {
-                const uint32_t b0 = v_lo + slot * (S::KV >> 4), d = tmem + S::O_COL + qt * D, a0 = tmem + S::P_COL + qt * 128;
+                const uint32_t b0 = v_lo + slot * (S::KV >> 4) + half * (8192 >> 4), a0 = a_p + 32 * half;
 #pragma unroll
                 for (int t = 0; t < TERMS; ++t)
 #pragma unroll
-                    for (int k = 0; k < 8; ++k) tc_mma_f16_ts(d, a0 + 64 * t + 8 * k, b0 + k * (2048 >> 4), hi, I_O, !first || t + k > 0);
+                    for (int k = 0; k < 4; ++k) tc_mma_f16_ts(d_o, a0 + 64 * t + 8 * k, b0 + k * (2048 >> 4), hi, I_O, !first || t + k > 0);
+                tc_commit(smem_u32(half == 0 ? &sh->h_done[qt] : &sh->v_empty[slot]));
+                if (half == 1 && last) tc_commit(smem_u32(&sh->o_full[qt]));
             }
             __syncwarp();
         };
-        auto commit = [&](uint64_t* bar) {
-            if (elect_one()) tc_commit(smem_u32(bar));
-            __syncwarp();
-        };
+        // The issuers of two row blocks take turns with a tile's second weights and the next scores: left to themselves their
+        // MMAs interleave, both blocks end together, and both softmaxes then share the exponential unit while the tensor
+        // cores wait.
+        uint32_t q_ph = 0, p_ph = 0, o_ph = 1, turn_ph = qt == 0 ? 1 : 0;        // (the first turn is block 0's)
+        int kt = 0, vt = 0;                          // tiles whose keys and values were used
+        auto keys = [&]() { return ok = warp_wait(&sh->k_full[kt & 1], (uint32_t)(kt >> 1) & 1u, sh, p); };
+        auto values = [&]() { return ok = warp_wait(&sh->v_full[vt & 1], (uint32_t)(vt >> 1) & 1u, sh, p); };
         for (int g = 0; ok; ++g) {
             if (!(ok = warp_wait(&sh->g_full[g % TILE_AHEAD], (uint32_t)(g / TILE_AHEAD) & 1u, sh, p))) break;
             const TileSegment& x = sh->seg[g % TILE_AHEAD];
             if (!x.live) break;
-            const int n = x.n, nq = x.nrows > 128 ? 2 : 1;
+            const int n = x.n, nrows = x.nrows;
             __syncwarp();
             if (lane == 0) mbar_arrive(smem_u32(&sh->g_empty[g % TILE_AHEAD]));
-            if (!(ok = warp_wait(&sh->q_full[0], q_ph, sh, p))) break;
-            q_ph ^= 1;
-            if (nq == 2) {
-                if (!(ok = warp_wait(&sh->q_full[1], q1_ph, sh, p))) break;
-                q1_ph ^= 1;
-            }
-            if (!(ok = warp_wait(&sh->k_full[ks], kp, sh, p))) break;
-            tc_fence_after();
-            for (int qt = 0; qt < nq; ++qt) scores(qt, ks);
-            commit(&sh->k_empty[ks]);
-            if (++ks == 2) { ks = 0; kp ^= 1; }
-            for (int i = 0; ok && i < n; ++i) {
-                for (int qt = 0; ok && qt < nq; ++qt) {
-                    if (i == 0) {
-                        if (!(ok = warp_wait(&sh->o_empty[qt], o_ph[qt], sh, p))) break;
-                        o_ph[qt] ^= 1;
-                    }
-                    if (qt == 0 && !(ok = warp_wait(&sh->v_full[vs], vp, sh, p))) break;
-                    if (!(ok = warp_wait(&sh->p_full[qt], p_ph[qt], sh, p))) break;
-                    p_ph[qt] ^= 1;
-                    tc_fence_after();
-                    outputs(qt, vs, i == 0);
-                    if (qt == nq - 1) commit(&sh->v_empty[vs]);
-                    if (i + 1 < n) {
-                        if (qt == 0) {
-                            if (!(ok = warp_wait(&sh->k_full[ks], kp, sh, p))) break;
-                            tc_fence_after();
-                        }
-                        scores(qt, ks);
-                        if (qt == nq - 1) commit(&sh->k_empty[ks]);
-                    } else {
-                        commit(&sh->o_full[qt]);
-                    }
+            if (nrows <= 128 * qt) {                 // no rows here: gives the slots back in step
+                for (int i = 0; ok && i < n; ++i, ++kt, ++vt) {
+                    if (!keys()) break;
+                    if (lane == 0) mbar_arrive(smem_u32(&sh->k_empty[kt & 1]));
+                    if (!values()) break;
+                    if (lane == 0) mbar_arrive(smem_u32(&sh->v_empty[vt & 1]));
                 }
-                if (i + 1 < n && ++ks == 2) { ks = 0; kp ^= 1; }
-                if (++vs == 2) { vs = 0; vp ^= 1; }
+                continue;
+            }
+            if (!(ok = warp_wait(&sh->q_full[qt], q_ph, sh, p))) break;
+            q_ph ^= 1;
+            if (!keys()) break;
+            tc_fence_after();
+            scores(kt & 1);
+            ++kt;
+            if (!(ok = warp_wait(&sh->o_empty[qt], o_ph, sh, p))) break;
+            o_ph ^= 1;
+            for (int i = 0; ok && i < n; ++i, ++vt) {
+                if (!values()) break;
+                if (i + 1 < n && !keys()) break;
+                if (!(ok = warp_wait(&sh->p_full[qt][0], p_ph, sh, p))) break;
+                tc_fence_after();
+                outputs(vt & 1, 0, i == 0, i + 1 == n);
+                if (!(ok = warp_wait(&sh->p_full[qt][1], p_ph, sh, p))) break;
+                p_ph ^= 1;
+                const bool two = nrows > 128;
+                if (two) {
+                    if (!(ok = warp_wait(&sh->turn[qt], turn_ph, sh, p))) break;
+                    turn_ph ^= 1;
+                }
+                tc_fence_after();
+                outputs(vt & 1, 1, false, i + 1 == n);
+                if (i + 1 < n) {
+                    scores(kt & 1);
+                    ++kt;
+                }
+                if (two && lane == 0) mbar_arrive(smem_u32(&sh->turn[qt ^ 1]));
             }
         }
     }
@@ -812,7 +881,7 @@ __global__ void __launch_bounds__(TILE_THREADS, 1) kv_attend_tile_kernel(const A
     }
     tc_fence_before();
     __syncthreads();
-    if (warp == 12) {
+    if (warp == 16) {
         tc_fence_after();
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u) : "memory");
     }
