@@ -429,8 +429,6 @@ __device__ __forceinline__ bool tile_softmax(TileSoftmax& x, const float4* group
         x.l += sum;
         tc_st<32>(x.t_p + 32 * half, pr);
         if constexpr (REST) tc_st<32>(x.t_p + 64 + 32 * half, rest);
-        tc_wait_st();
-        ready(half);
         return true;
     };
     float mx = -INFINITY, sum = 0.f;
@@ -447,9 +445,14 @@ __device__ __forceinline__ bool tile_softmax(TileSoftmax& x, const float4* group
     tc_wait_ld();
     tc_ld32(x.t_s + 96, b);
     work(a, 2, mx, sum);
+    tc_wait_st();
+    ready(0);                                        // (the stores had the time of 32 tokens to arrive)
     tc_wait_ld();
     work(b, 3, mx, sum);
-    return finish(1, mx, sum);
+    if (!finish(1, mx, sum)) return false;
+    tc_wait_st();
+    ready(1);
+    return true;
 }
 
 template <typename T, int D>
