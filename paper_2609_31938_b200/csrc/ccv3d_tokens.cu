@@ -110,38 +110,83 @@ Span codes_span(const ccv3d_kv_cache* c) {
 }
 Span scales_span(const ccv3d_kv_cache* c) { return span_of(c->scales, (int64_t)c->pages * 2 * c->kv_heads * 4); }
 
-template <typename T>
-ccv3d_status launch_append(const AppendParams& p, unsigned grid, cudaStream_t st) {
-    const int D = p.c.head_dim, P = p.c.page_tokens;
-#define CCV3D_APPEND(d, pg) \
-    if (D == d && P == pg) kv_append_kernel<T, d, pg><<<grid, APPEND_THREADS, 0, st>>>(p);
-    CCV3D_APPEND(64, 16) CCV3D_APPEND(64, 32) CCV3D_APPEND(64, 64) CCV3D_APPEND(64, 128)
-    CCV3D_APPEND(128, 16) CCV3D_APPEND(128, 32) CCV3D_APPEND(128, 64) CCV3D_APPEND(128, 128)
-#undef CCV3D_APPEND
+template <typename T, int D, int P, bool FEW>
+ccv3d_status launch_append_as(AppendParams& p, cudaStream_t st) {
+    using S = AppendShape<D, P, FEW>;
+    // pages that n new tokens can touch: one for n = 1, else up to (n - 1) / P + 2
+    const int64_t by_tokens = (int64_t)p.bt.tokens / P + 2LL * p.bt.batch;
+    const int64_t by_batch = (int64_t)p.bt.batch * (p.bt.max_new <= 1 ? 1 : (p.bt.max_new - 1) / P + 2);
+    const bool one = p.bt.max_new <= 1;            // (then a block's number names its sequence)
+    const int64_t kv = (one || by_batch < by_tokens ? by_batch : by_tokens) * 2 * p.c.kv_heads;
+    const int64_t items = p.q.data ? (int64_t)p.bt.tokens * ((p.q_heads + QUERY_HEADS - 1) / QUERY_HEADS) : 0;
+    const int64_t all = kv + (items + S::TPI - 1) / S::TPI;
+    if (all > 0x7FFFFFFF) return CCV3D_ERR_UNSUPPORTED;
+    p.kv_blocks = (unsigned)kv;
+    kv_append_kernel<T, D, P, FEW><<<(unsigned)all, S::THREADS, 0, st>>>(p);
     return launched();
 }
 
+template <typename T>
+ccv3d_status launch_append(AppendParams& p, cudaStream_t st) {
+    const int D = p.c.head_dim, P = p.c.page_tokens;
+    const bool few = p.bt.max_new <= 128 / (D / 4);
+#define CCV3D_APPEND(d, pg) \
+    if (D == d && P == pg) return few ? launch_append_as<T, d, pg, true>(p, st) : launch_append_as<T, d, pg, false>(p, st);
+    CCV3D_APPEND(64, 16) CCV3D_APPEND(64, 32) CCV3D_APPEND(64, 64) CCV3D_APPEND(64, 128)
+    CCV3D_APPEND(128, 16) CCV3D_APPEND(128, 32) CCV3D_APPEND(128, 64) CCV3D_APPEND(128, 128)
+#undef CCV3D_APPEND
+    return CCV3D_ERR_UNSUPPORTED;
+}
+
+// Opts a kernel into its dynamic shared memory, once for each device.
+template <typename F>
+bool allow_smem(F* kernel, int bytes, int dev, std::atomic<uint64_t>& done) {
+    if (done.load(std::memory_order_relaxed) >> dev & 1) return true;
+    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) != cudaSuccess) return false;
+    done.fetch_or(1ull << dev, std::memory_order_relaxed);
+    return true;
+}
+
+template <typename TX, typename TY, int G, int V, int K>
+ccv3d_status launch_norm_rows(const NormParams& p, const Device& dev, cudaStream_t st) {
+    constexpr int most_smem = 4 * G * V * K * 4;   // of the widest rows it takes; the blocks of an SM below have room for theirs
+    static std::atomic<uint64_t> done{0};
+    if (!allow_smem(gated_norm_rows_kernel<TX, TY, G, V, K>, most_smem, dev.index, done)) { cudaGetLastError(); return CCV3D_ERR_CUDA; }
+    const int C = p.d.channels, smem = 4 * ((C + V - 1) / V * V) * 4, teams = ROWS_THREADS / G;
+    const int most = (p.d.rows + teams - 1) / teams, wave = (K * V <= 12 ? 2 : 1) * dev.sm_count;
+    gated_norm_rows_kernel<TX, TY, G, V, K><<<most < wave ? most : wave, ROWS_THREADS, smem, st>>>(p);
+    return launched();
+}
+
+// Threads to a row (g), elements of an access (v), accesses of a thread (k).
 template <typename TX, typename TY>
-ccv3d_status launch_norm(const NormParams& p, bool vec, cudaStream_t st) {
+ccv3d_status launch_norm(const NormParams& p, bool vec, const Device& dev, cudaStream_t st) {
     const int C = p.d.channels, rows = p.d.rows;
+#define CCV3D_ROWS(g, v, k) \
+    if (C <= (g) * (v) * (k)) return launch_norm_rows<TX, TY, g, v, k>(p, dev, st);
 #define CCV3D_NORM(g, v, k) \
-    { constexpr int per = (g) < 128 ? 128 / (g) : 1; \
-      gated_norm_kernel<TX, TY, g, v, k><<<(rows + per - 1) / per, (g) < 128 ? 128 : (g), 0, st>>>(p); }
+    if (C <= (g) * (v) * (k)) { \
+        gated_norm_kernel<TX, TY, g, v, k><<<rows, g, 0, st>>>(p); \
+        return launched(); \
+    }
+    // more than two rows to an SM: rows by stretches, where a thread's share of the channels fits into its registers
+    if (rows > 2 * dev.sm_count) {
+        if (vec) {
+            CCV3D_ROWS(32, 4, 1) CCV3D_ROWS(32, 4, 2) CCV3D_ROWS(32, 4, 3) CCV3D_ROWS(64, 4, 3) CCV3D_ROWS(128, 4, 2) CCV3D_ROWS(128, 4, 3)
+            CCV3D_ROWS(256, 4, 2) CCV3D_ROWS(256, 4, 3) CCV3D_ROWS(512, 4, 2)
+        } else {
+            CCV3D_ROWS(32, 1, 4) CCV3D_ROWS(32, 1, 12) CCV3D_ROWS(128, 1, 5) CCV3D_ROWS(128, 1, 10) CCV3D_ROWS(256, 1, 8) CCV3D_ROWS(256, 1, 12)
+            CCV3D_ROWS(512, 1, 8)
+        }
+    }
     if (vec) {
-        if (C <= 128) CCV3D_NORM(16, 4, 2)
-        else if (C <= 512) CCV3D_NORM(32, 4, 4)
-        else if (C <= 2048) CCV3D_NORM(128, 4, 4)
-        else if (C <= 4096) CCV3D_NORM(256, 4, 4)
-        else if (C <= 8192) CCV3D_NORM(512, 4, 4)
-        else CCV3D_NORM(512, 4, 8)
+        CCV3D_NORM(128, 4, 1) CCV3D_NORM(512, 4, 1) CCV3D_NORM(512, 4, 2) CCV3D_NORM(512, 4, 4) CCV3D_NORM(512, 4, 8)
     } else {
-        if (C <= 128) CCV3D_NORM(32, 1, 4)
-        else if (C <= 1024) CCV3D_NORM(128, 1, 8)
-        else if (C <= 4096) CCV3D_NORM(512, 1, 8)
-        else CCV3D_NORM(512, 1, 32)
+        CCV3D_NORM(512, 1, 1) CCV3D_NORM(512, 1, 4) CCV3D_NORM(512, 1, 16) CCV3D_NORM(512, 1, 32)
     }
 #undef CCV3D_NORM
-    return launched();
+#undef CCV3D_ROWS
+    return CCV3D_ERR_UNSUPPORTED;
 }
 
 ccv3d_status check_attend(const ccv3d_kv_cache* cache, const ccv3d_token_batch* batch, int q_heads, int dtype) {
@@ -203,15 +248,6 @@ ccv3d_status encode_cache_map(const ccv3d_kv_cache& c, CUtensorMap* tm, int box_
                           c.head_dim == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                           CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
     return r == CUDA_SUCCESS ? CCV3D_OK : CCV3D_ERR_CUDA;
-}
-
-// Opts a kernel into its dynamic shared memory, once for each device.
-template <typename F>
-bool allow_smem(F* kernel, int bytes, int dev, std::atomic<uint64_t>& done) {
-    if (done.load(std::memory_order_relaxed) >> dev & 1) return true;
-    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes) != cudaSuccess) return false;
-    done.fetch_or(1ull << dev, std::memory_order_relaxed);
-    return true;
 }
 
 template <typename T, int D, int NT>
@@ -306,17 +342,7 @@ ccv3d_status ccv3d_kv_append(const ccv3d_kv_cache* cache, const ccv3d_token_batc
         for (int a = rot->axes; a < 3; ++a) p.rot.section[a] = 0;
     }
     p.status = status;
-    const int P = cache->page_tokens;
-    // pages that n new tokens can touch: one for n = 1, else up to (n - 1) / P + 2
-    const int64_t by_tokens = (int64_t)tokens / P + 2LL * batch->batch;
-    const int64_t by_batch = (int64_t)batch->batch * (batch->max_new <= 1 ? 1 : (batch->max_new - 1) / P + 2);
-    const int64_t kv = (by_tokens < by_batch ? by_tokens : by_batch) * 2 * H;
-    const int64_t tpi = APPEND_THREADS / (D / 4);
-    const int64_t all = kv + (q ? ((int64_t)tokens * q_heads + tpi - 1) / tpi : 0);
-    if (all > 0x7FFFFFFF) return CCV3D_ERR_UNSUPPORTED;
-    p.kv_blocks = (unsigned)kv;
-    return dtype == CCV3D_BF16 ? launch_append<__nv_bfloat16>(p, (unsigned)all, (cudaStream_t)stream)
-                               : launch_append<float>(p, (unsigned)all, (cudaStream_t)stream);
+    return dtype == CCV3D_BF16 ? launch_append<__nv_bfloat16>(p, (cudaStream_t)stream) : launch_append<float>(p, (cudaStream_t)stream);
 }
 
 ccv3d_status ccv3d_kv_attend_workspace(const ccv3d_kv_cache* cache, const ccv3d_token_batch* batch, int32_t q_heads,
@@ -414,8 +440,8 @@ ccv3d_status ccv3d_gated_norm(const ccv3d_norm_desc* d, const void* x, const voi
                      whole(post_weight, 0, ew) && whole(post_bias, 0, ew) && whole(pre_weight, 0, ew) && whole(pre_bias, 0, ew);
     cudaStream_t st = (cudaStream_t)stream;
     if (d->res_dtype == CCV3D_BF16)
-        return d->act_dtype == CCV3D_BF16 ? launch_norm<__nv_bfloat16, __nv_bfloat16>(p, vec, st) : launch_norm<__nv_bfloat16, float>(p, vec, st);
-    return d->act_dtype == CCV3D_BF16 ? launch_norm<float, __nv_bfloat16>(p, vec, st) : launch_norm<float, float>(p, vec, st);
+        return d->act_dtype == CCV3D_BF16 ? launch_norm<__nv_bfloat16, __nv_bfloat16>(p, vec, dev, st) : launch_norm<__nv_bfloat16, float>(p, vec, dev, st);
+    return d->act_dtype == CCV3D_BF16 ? launch_norm<float, __nv_bfloat16>(p, vec, dev, st) : launch_norm<float, float>(p, vec, dev, st);
 }
 
 }  // extern "C"

@@ -1,9 +1,11 @@
 // Append to the paged E4M3 cache, with the position rotation of keys (and queries) on the way.
 //
-// A block of 8 warps owns one (page, keys or values, head): it holds the page's new tokens in registers, takes the
-// largest magnitude over all of them, settles the page's scale (the smallest power of two under which everything fits
+// Bound by HBM where there are many tokens, by the chain of dependent loads (sequence, page, position, table) where there
+// are few.  A block owns one (page, keys or values, head): it holds the page's new tokens in registers, takes
+// the largest magnitude over all of them, settles the page's scale (the smallest power of two under which everything fits
 // into +-448, at least the old one where older tokens stay), moves older codes to it where it grew, and writes the new
-// codes.  Every input is read once.  The blocks behind those rotate the queries.
+// codes.  The blocks behind those rotate the queries, four heads of a token for each group of lanes that spans a head, so
+// that a token's cosines and sines are fetched once for them and their loads are on their way together.
 #pragma once
 #include "ccv3d_tokens_common.cuh"
 
@@ -19,91 +21,121 @@ struct AppendParams {
     uint32_t* status;
 };
 
-constexpr int APPEND_THREADS = 256;
+// Threads of a block: four rounds cover a page's new tokens, more rounds cost the registers that keep several blocks on an
+// SM (one to a block of 256 threads at 16 rounds); `few`: no sequence brings more tokens than one round of 128 threads takes.
+template <int D, int P, bool FEW> struct AppendShape {
+    static constexpr int LPT = D / 4, WHOLE = P * LPT / 4;       // lanes for one token
+    static constexpr int THREADS = FEW || WHOLE < 128 ? 128 : WHOLE;
+    static constexpr int TPI = THREADS / LPT, R = FEW ? 1 : (P + TPI - 1) / TPI;      // tokens at a time, rounds
+};
 constexpr int MIN_SCALE_EXP = -64;
+constexpr int QUERY_HEADS = 4;
 
-// Rotates the four elements 4l .. 4l+3 of a row held by lane l of a group of LPT lanes (all lanes of the warp call it).
-// Products and sums are rounded one by one, as elementwise code in FP32 would.
-template <int LPT>
-__device__ __forceinline__ void rotate4(const ccv3d_rotary& r, int token, int l, float (&v)[4], uint32_t* status) {
-    const int e = 4 * l, pairs = r.pairs;
-    const bool on = e < 2 * pairs;
-    // the pairs this lane's elements belong to: one each (split halves) or two in all (interleaved)
-    const int j = r.interleaved ? e / 2 : (e < pairs ? e : e - pairs);
-    float c[4] = {1.f, 1.f, 1.f, 1.f}, s[4] = {0.f, 0.f, 0.f, 0.f};
-    if (on) {
-        const int n = r.interleaved ? 2 : 4;
-        int row_of[3];
+// A lane's part in the rotation of the four elements 4 l .. 4 l + 3 of a head: the same for every token and head.
+struct Turn {
+    bool on, one;            // any of them turns; all by the same axis
+    int pair, axis;          // first pair they belong to (four pairs, or two if interleaved), its axis
+};
+__device__ __forceinline__ int axis_of(const ccv3d_rotary& r, int pair) {
+    return pair < r.section[0] ? 0 : (pair < r.section[0] + r.section[1] ? 1 : 2);
+}
+__device__ __forceinline__ Turn turn_of(const ccv3d_rotary& r, int l) {
+    Turn t;
+    const int e = 4 * l;
+    t.on = r.cos_table && e < 2 * r.pairs;
+    t.pair = r.interleaved ? e / 2 : (e < r.pairs ? e : e - r.pairs);
+    t.axis = t.on ? axis_of(r, t.pair) : 0;
+    t.one = t.on && t.axis == axis_of(r, t.pair + (r.interleaved ? 1 : 3));
+    return t;
+}
+// Row of the table for a token and axis; positions outside the table are cut and reported.
+__device__ __forceinline__ int table_row(const ccv3d_rotary& r, int token, int axis, uint32_t* status) {
+    const int row = __ldg(r.positions + (int64_t)token * r.axes + axis);
+    if ((unsigned)row < (unsigned)r.rows) return row;
+    report(status, CCV3D_TOKENS_BAD_POSITION);
+    return row < 0 ? 0 : r.rows - 1;
+}
+// Cosines and sines of the lane's pairs for a token; `row`: table_row of the lane's axis.
+__device__ __forceinline__ void angles(const ccv3d_rotary& r, const Turn& t, int token, int row, float (&c)[4], float (&s)[4], uint32_t* status) {
 #pragma unroll
-        for (int a = 0; a < 3; ++a) {
-            int row = a < r.axes ? __ldg(r.positions + (int64_t)token * r.axes + a) : 0;
-            if ((unsigned)row >= (unsigned)r.rows) {
-                report(status, CCV3D_TOKENS_BAD_POSITION);
-                row = row < 0 ? 0 : r.rows - 1;
-            }
-            row_of[a] = row;
-        }
-        const int s0 = r.section[0], s1 = s0 + r.section[1];
-        auto row_at = [&](int i) { return i < s0 ? row_of[0] : (i < s1 ? row_of[1] : row_of[2]); };
-        const int first = row_at(j);
-        if (!r.interleaved && first == row_at(j + 3)) {
-            load4(r.cos_table + (int64_t)first * pairs + j, c);
-            load4(r.sin_table + (int64_t)first * pairs + j, s);
+    for (int i = 0; i < 4; ++i) { c[i] = 1.f; s[i] = 0.f; }
+    if (!t.on) return;
+    if (t.one) {
+        const int64_t at = (int64_t)row * r.pairs + t.pair;
+        if (r.interleaved) {
+            const float2 x = __ldg(reinterpret_cast<const float2*>(r.cos_table + at)), y = __ldg(reinterpret_cast<const float2*>(r.sin_table + at));
+            c[0] = x.x; c[1] = x.y; s[0] = y.x; s[1] = y.y;
         } else {
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-                if (i < n) {
-                    const int64_t at = (int64_t)row_at(j + i) * pairs + j + i;
-                    c[i] = __ldg(r.cos_table + at);
-                    s[i] = __ldg(r.sin_table + at);
-                }
+            load4(r.cos_table + at, c);
+            load4(r.sin_table + at, s);
         }
+        return;
     }
+    for (int i = 0; i < (r.interleaved ? 2 : 4); ++i) {          // pairs on both sides of a section's border
+        const int64_t at = (int64_t)table_row(r, token, axis_of(r, t.pair + i), status) * r.pairs + t.pair + i;
+        c[i] = __ldg(r.cos_table + at);
+        s[i] = __ldg(r.sin_table + at);
+    }
+}
+// Turns the four elements of a head held by lane l of a group of LPT lanes (all lanes of the warp call it).  Products and
+// sums are rounded one by one, as elementwise code in FP32 would.
+template <int LPT>
+__device__ __forceinline__ void rotate4(const ccv3d_rotary& r, const Turn& t, int l, const float (&c)[4], const float (&s)[4], float (&v)[4]) {
     if (r.interleaved) {
-        if (on) {
+        if (t.on) {
             const float a0 = v[0], b0 = v[1], a1 = v[2], b1 = v[3];
             v[0] = __fsub_rn(__fmul_rn(a0, c[0]), __fmul_rn(b0, s[0]));
             v[1] = __fadd_rn(__fmul_rn(b0, c[0]), __fmul_rn(a0, s[0]));
             v[2] = __fsub_rn(__fmul_rn(a1, c[1]), __fmul_rn(b1, s[1]));
             v[3] = __fadd_rn(__fmul_rn(b1, c[1]), __fmul_rn(a1, s[1]));
         }
-    } else {
-        const bool lower = e < pairs;
-        const int other = lower ? l + pairs / 4 : l - pairs / 4;
+        return;
+    }
+    const bool lower = 4 * l < r.pairs;
+    const int other = lower ? l + r.pairs / 4 : l - r.pairs / 4;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const float w = __shfl_sync(0xffffffffu, v[i], other, LPT);
-            if (on) {
-                const float t = __fmul_rn(w, s[i]), u = __fmul_rn(v[i], c[i]);
-                v[i] = lower ? __fsub_rn(u, t) : __fadd_rn(u, t);
-            }
-        }
+    for (int i = 0; i < 4; ++i) {
+        const float w = __shfl_sync(0xffffffffu, v[i], other, LPT);
+        const float x = __fmul_rn(w, s[i]), u = __fmul_rn(v[i], c[i]);
+        if (t.on) v[i] = lower ? __fsub_rn(u, x) : __fadd_rn(u, x);
     }
 }
 
-template <typename T, int D, int P>
-__global__ void __launch_bounds__(APPEND_THREADS) kv_append_kernel(const AppendParams p) {
-    constexpr int LPT = D / 4;                       // lanes for one token
-    constexpr int TPI = APPEND_THREADS / LPT;        // tokens the block takes at a time
-    constexpr int R = (P + TPI - 1) / TPI;           // rounds for a whole page
+template <typename T, int D, int P, bool FEW>
+__global__ void __launch_bounds__(AppendShape<D, P, FEW>::THREADS, 1024 / AppendShape<D, P, FEW>::THREADS) kv_append_kernel(const AppendParams p) {
+    using S = AppendShape<D, P, FEW>;
+    constexpr int LPT = S::LPT, TPI = S::TPI, R = S::R;
     const int tid = threadIdx.x, l = tid % LPT;
-    if (blockIdx.x >= p.kv_blocks) {                 // ---- queries
-        const int64_t rows = (int64_t)p.bt.tokens * p.q_heads;
-        const int64_t row = (int64_t)(blockIdx.x - p.kv_blocks) * TPI + tid / LPT;
-        const bool live = row < rows;
-        const int token = live ? (int)(row / p.q_heads) : 0, head = live ? (int)(row % p.q_heads) : 0;
-        float v[4] = {0.f, 0.f, 0.f, 0.f};
-        if (live) load4((const T*)p.q.data + token * p.q.token_stride + head * p.q.head_stride + 4 * l, v);
-        if (p.rot.cos_table) rotate4<LPT>(p.rot, token, l, v, p.status);
-        if (live) store4((T*)p.qo.data + token * p.qo.token_stride + head * p.qo.head_stride + 4 * l, v);
+    const Turn turn = turn_of(p.rot, l);
+    if (blockIdx.x >= p.kv_blocks) {                 // ---- queries: an item is a token and QUERY_HEADS heads
+        const int per_token = (p.q_heads + QUERY_HEADS - 1) / QUERY_HEADS;
+        const int64_t item = (int64_t)(blockIdx.x - p.kv_blocks) * TPI + tid / LPT;
+        const bool live = item < (int64_t)p.bt.tokens * per_token;
+        const int token = live ? (int)(item / per_token) : 0, h0 = live ? (int)(item % per_token) * QUERY_HEADS : p.q_heads;
+        const int row = live && turn.one ? table_row(p.rot, token, turn.axis, p.status) : 0;
+        float v[QUERY_HEADS][4];
+#pragma unroll
+        for (int h = 0; h < QUERY_HEADS; ++h)
+            if (h0 + h < p.q_heads) load4((const T*)p.q.data + token * p.q.token_stride + (h0 + h) * p.q.head_stride + 4 * l, v[h]);
+        float c[4], s[4];
+        if (p.rot.cos_table) {
+            angles(p.rot, turn, token, row, c, s, p.status);
+#pragma unroll
+            for (int h = 0; h < QUERY_HEADS; ++h) rotate4<LPT>(p.rot, turn, l, c, s, v[h]);
+        }
+#pragma unroll
+        for (int h = 0; h < QUERY_HEADS; ++h)
+            if (h0 + h < p.q_heads) store4((T*)p.qo.data + token * p.qo.token_stride + (h0 + h) * p.qo.head_stride + 4 * l, v[h]);
         return;
     }
     // ---- keys and values: block -> (page of a sequence, keys or values, head)
     __shared__ int unit_seq, unit_page;
-    __shared__ float part[APPEND_THREADS / 32];
+    __shared__ float part[S::THREADS / 32];
     const int H = p.c.kv_heads;
     const int unit = blockIdx.x / (2 * H), kvh = blockIdx.x % (2 * H), is_v = kvh >= H, head = is_v ? kvh - H : kvh;
-    if (tid < 32) {
+    if (p.bt.max_new <= 1) {                         // a page to each sequence at most: no search
+        if (tid == 0) { unit_seq = unit; unit_page = 0; }
+    } else if (tid < 32) {
         if (tid == 0) unit_seq = -1;
         __syncwarp();
         int base = 0;
@@ -127,10 +159,12 @@ __global__ void __launch_bounds__(APPEND_THREADS) kv_append_kernel(const AppendP
     __syncthreads();
     const int b = unit_seq;
     if (b < 0) return;                               // the grid is a bound
-    Seq s = load_seq(p.bt, P, b, nullptr);
+    Seq s = load_seq(p.bt, P, b, p.bt.max_new <= 1 ? p.status : nullptr);
     const int lost = max(0, s.n - s.total);
+    if (p.bt.max_new <= 1 && lost) report(p.status, CCV3D_TOKENS_BAD_LENGTH);
     s.first += lost;
     s.n -= lost;
+    if (s.n == 0) return;
     const int old = s.total - s.n;
     const int j = old / P + unit_page;
     const int page = load_page(p.bt, p.c, b, j, p.status);
@@ -139,19 +173,31 @@ __global__ void __launch_bounds__(APPEND_THREADS) kv_append_kernel(const AppendP
     const int row0 = s.first + (j * P + t0) - old;
     const ccv3d_heads& src = is_v ? p.v : p.k;
     const T* in = (const T*)src.data + head * src.head_stride + 4 * l;
+    float* at = p.c.scales + ((int64_t)page * 2 + is_v) * H + head;
+    uint8_t* codes = (uint8_t*)p.c.codes + (((int64_t)page * 2 + is_v) * H + head) * (P * D);
+    const float was = t0 > 0 ? *at : 0.f;
+    const bool turns = !is_v && p.rot.cos_table;
     float v[R][4];
+    int row[R];
     float most = 0.f;
 #pragma unroll
     for (int r = 0; r < R; ++r) {
         const int t = t0 + r * TPI + tid / LPT;
         v[r][0] = v[r][1] = v[r][2] = v[r][3] = 0.f;
-        if (t < t1) load4(in + (int64_t)(row0 + t - t0) * src.token_stride, v[r]);
+        row[r] = 0;
+        if (t < t1) {
+            load4(in + (int64_t)(row0 + t - t0) * src.token_stride, v[r]);
+            if (turns && turn.one) row[r] = table_row(p.rot, row0 + t - t0, turn.axis, p.status);
+        }
     }
 #pragma unroll
     for (int r = 0; r < R; ++r) {
         const int t = t0 + r * TPI + tid / LPT;
-        if (!is_v && p.rot.cos_table && t0 + r * TPI < t1)       // (the same for the whole block)
-            rotate4<LPT>(p.rot, row0 + min(t, t1 - 1) - t0, l, v[r], p.status);
+        if (turns && t0 + r * TPI < t1) {                        // (the same for the whole block)
+            float c[4], s[4];
+            angles(p.rot, turn, row0 + min(t, t1 - 1) - t0, row[r], c, s, p.status);
+            rotate4<LPT>(p.rot, turn, l, c, s, v[r]);
+        }
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const float a = fabsf(v[r][i]);
@@ -162,20 +208,17 @@ __global__ void __launch_bounds__(APPEND_THREADS) kv_append_kernel(const AppendP
     if ((tid & 31) == 0) part[tid >> 5] = most;
     __syncthreads();
 #pragma unroll
-    for (int i = 0; i < APPEND_THREADS / 32; ++i) most = fmaxf(most, part[i]);
+    for (int i = 0; i < S::THREADS / 32; ++i) most = fmaxf(most, part[i]);
     // smallest e with most <= 448 * 2^e = 1.75 * 2^(8 + e)
     const uint32_t bits = __float_as_uint(most);
     int e = (int)(bits >> 23) - 127 - 8 + ((bits & 0x7FFFFFu) > 0x600000u ? 1 : 0);
     e = max(e, MIN_SCALE_EXP);
     float scale = __uint_as_float((uint32_t)(e + 127) << 23);
-    float* at = p.c.scales + ((int64_t)page * 2 + is_v) * H + head;
-    uint8_t* codes = (uint8_t*)p.c.codes + (((int64_t)page * 2 + is_v) * H + head) * (P * D);
     if (t0 > 0) {
-        const float was = *at;
         scale = fmaxf(was, scale);
         if (scale != was) {
             const float f = was / scale;
-            for (int i = tid; i < t0 * (D / 4); i += APPEND_THREADS) {
+            for (int i = tid; i < t0 * (D / 4); i += S::THREADS) {
                 float c[4];
                 e4m3x4_to_float(reinterpret_cast<uint32_t*>(codes)[i], c);
 #pragma unroll
@@ -183,7 +226,6 @@ __global__ void __launch_bounds__(APPEND_THREADS) kv_append_kernel(const AppendP
                 reinterpret_cast<uint32_t*>(codes)[i] = to_e4m3x4(c);
             }
         }
-        __syncthreads();                             // all have read the old scale
     }
     if (tid == 0) *at = scale;
     const float inv = 1.f / scale;                   // a power of two: exact

@@ -15,6 +15,9 @@ from . import (BF16, F32, NORM_LAYER, NORM_NONE, NORM_RMS, OK, Ccv3dError, Heads
 
 _DTYPES = {torch.bfloat16: BF16, torch.float32: F32}
 _KINDS = {"none": NORM_NONE, "rms": NORM_RMS, "layer": NORM_LAYER}
+# current device and stream as plain numbers: the calls below are short enough for the objects around them to matter
+_device = torch.cuda.current_device
+_stream = torch._C._cuda_getCurrentRawStream
 
 
 def _dtype(t: torch.Tensor, what: str) -> int:
@@ -30,21 +33,22 @@ def _on_device(t: torch.Tensor, what: str, dev: int) -> None:
 
 
 def _heads(t: torch.Tensor, what: str, tokens: int, dim: int, dev: int) -> Heads:
-    if t.dim() != 3 or t.shape[0] != tokens or t.shape[2] != dim:
-        raise ValueError(f"{what} has shape {tuple(t.shape)}: [{tokens}, heads, {dim}] is wanted")
+    shape = t.shape
+    if len(shape) != 3 or shape[0] != tokens or shape[2] != dim:
+        raise ValueError(f"{what} has shape {tuple(shape)}: [{tokens}, heads, {dim}] is wanted")
     _on_device(t, what, dev)
     ts, hs, es = t.stride()
     if es != 1:
         raise ValueError(f"{what}: the last dimension must be contiguous")
-    if t.shape[1] == 1:
+    if shape[1] == 1:
         hs = dim             # torch gives a dimension of one any stride
     if tokens == 1:
-        ts = t.shape[1] * hs
+        ts = shape[1] * hs
     return Heads(t.data_ptr(), ts, hs)
 
 
 def _int_array(t: torch.Tensor, what: str, shape, dev: int) -> None:
-    if t.dtype != torch.int32 or not t.is_contiguous() or tuple(t.shape) != tuple(shape):
+    if t.dtype is not torch.int32 or t.shape != shape or not t.is_contiguous():
         raise ValueError(f"{what} must be a contiguous int32 tensor of shape {tuple(shape)}, not {t.dtype} {tuple(t.shape)}")
     _on_device(t, what, dev)
 
@@ -56,7 +60,7 @@ class TokenBatch:
     tokens of any sequence, ``tokens`` (default: what the call's tensors hold) the rows."""
 
     def __init__(self, new_start, total, page_table, max_new: int):
-        dev = torch.cuda.current_device()
+        dev = _device()
         b = total.shape[0]
         _int_array(new_start, "new_start", (b + 1,), dev)
         _int_array(total, "total", (b,), dev)
@@ -72,7 +76,7 @@ class Rotary:
     pairs among the axes of ``positions`` (default: one axis)."""
 
     def __init__(self, cos, sin, sections=None, interleaved=False):
-        dev = torch.cuda.current_device()
+        dev = _device()
         for t, what in ((cos, "cos"), (sin, "sin")):
             if t.dtype != torch.float32 or t.dim() != 2 or not t.is_contiguous() or t.shape != cos.shape:
                 raise ValueError(f"{what} must be a contiguous float32 table [rows, pairs]")
@@ -92,7 +96,7 @@ class PagedCache:
     [pages, 2, kv_heads]; ``PagedCache.empty`` allocates them."""
 
     def __init__(self, codes, scales):
-        dev = torch.cuda.current_device()
+        dev = _device()
         if codes.dtype != torch.uint8 or codes.dim() != 5 or codes.shape[1] != 2 or not codes.is_contiguous():
             raise ValueError("codes must be a contiguous uint8 tensor [pages, 2, kv_heads, page_tokens, head_dim]")
         if scales.dtype != torch.float32 or scales.shape != codes.shape[:3] or not scales.is_contiguous():
@@ -104,6 +108,7 @@ class PagedCache:
         self.c = KvCache(codes.data_ptr(), scales.data_ptr(), self.pages, self.kv_heads, self.page_tokens, self.head_dim)
         self._status = torch.zeros(1, dtype=torch.int32, device=codes.device)
         self._status_ptr = self._status.data_ptr()
+        self._scratch = {}       # stream -> scratch of attend calls on it
 
     @classmethod
     def empty(cls, pages, kv_heads, head_dim, page_tokens=64):
@@ -120,18 +125,32 @@ class PagedCache:
     def _batch(self, batch: TokenBatch, tokens: int) -> TokenBatchC:
         if batch.device != self.device:
             raise ValueError("the batch lies on another device than the cache")
-        if torch.cuda.current_device() != self.device:
+        if _device() != self.device:
             raise ValueError(f"the cache lies on cuda:{self.device}, which is not the current device")
         batch.c.tokens = tokens
         return batch.c
 
+    def _workspace(self, c: TokenBatchC, heads: int, dt: int, stream: int):
+        """Scratch for an attend call on `stream`: kept for the next call on it, so calls on other streams never share it.
+        A captured call gets its own, which belongs to the graph."""
+        s, need = ccv3d_kv_attend_workspace(self.c, c, heads, dt)
+        if s != OK:
+            raise Ccv3dError(s, "ccv3d_kv_attend_workspace")
+        ws = self._scratch.get(stream)
+        if torch.cuda.is_current_stream_capturing():
+            return torch.empty(need, dtype=torch.uint8, device=self.codes.device), need
+        if ws is None or ws.shape[0] < need:
+            ws = self._scratch[stream] = torch.empty(need, dtype=torch.uint8, device=self.codes.device)
+        return ws, need
+
     def append(self, k, v, batch: TokenBatch, rotary: Rotary | None = None, positions=None, q=None, q_out=None):
         """Writes the new keys (rotated) and values [tokens, kv_heads, head_dim] into the cache; returns ``q`` rotated
         (a new tensor, or ``q_out``, which may be ``q`` itself), None without ``q``."""
-        tokens, dim, dev = k.shape[0], self.head_dim, self.device
+        shape = k.shape
+        tokens, dim, dev = shape[0], self.head_dim, self.device
         c = self._batch(batch, tokens)
         dt = _dtype(k, "k")
-        if k.shape != v.shape or k.shape[1] != self.kv_heads:
+        if shape != v.shape or len(shape) != 3 or shape[1] != self.kv_heads:
             raise ValueError(f"k {tuple(k.shape)} and v {tuple(v.shape)} must be [tokens, {self.kv_heads}, {dim}]")
         if v.dtype != k.dtype or (q is not None and q.dtype != k.dtype):
             raise TypeError("q, k and v must have one type")
@@ -143,22 +162,26 @@ class PagedCache:
             if positions.dim() == 1:
                 positions = positions[:, None]
             _int_array(positions, "positions", (tokens, rotary.axes), dev)
+            if rotary.cos.get_device() != dev:
+                raise ValueError("the rotation lies on another device than the cache")
             r = rotary.c
             r.positions = positions.data_ptr()
         cq = cqo = None
         heads = 0
         if q is not None:
-            heads = q.shape[1]
             cq = _heads(q, "q", tokens, dim, dev)
+            heads = q.shape[1]
             if q_out is None:
-                q_out = torch.empty((tokens, heads, dim), dtype=q.dtype, device=q.device)
+                q_out = q.new_empty(q.shape)
+                cqo = Heads(q_out.data_ptr(), heads * dim, dim)
             elif q_out.dtype != q.dtype or q_out.shape != q.shape:
                 raise ValueError("q_out must have q's shape and type")
-            cqo = _heads(q_out, "q_out", tokens, dim, dev)
+            else:
+                cqo = _heads(q_out, "q_out", tokens, dim, dev)
         elif q_out is not None:
             raise ValueError("q_out without q")
         s = lib.ccv3d_kv_append(self.c, c, ck, cv, r, cq, cqo, heads, dt, self._status_ptr,
-                                torch.cuda.current_stream().cuda_stream)
+                                _stream(dev))
         if s != OK:
             raise Ccv3dError(s, "ccv3d_kv_append")
         return q_out
@@ -167,38 +190,43 @@ class PagedCache:
                want_lse: bool = False):
         """Attention of q [tokens, q_heads, head_dim] over the cache (``frame``, ``window``: who sees what, as
         ``ccv3d_kv_attend`` says); ``scale`` defaults to head_dim ** -0.5.  Returns out, or (out, lse)."""
-        tokens, heads = q.shape[0], q.shape[1]
+        tokens, dim, dev = q.shape[0], self.head_dim, self.device
         c = self._batch(batch, tokens)
         dt = _dtype(q, "q")
-        cq = _heads(q, "q", tokens, self.head_dim, self.device)
+        cq = _heads(q, "q", tokens, dim, dev)
+        heads = q.shape[1]
         if out is None:
-            out = torch.empty((tokens, heads, self.head_dim), dtype=q.dtype, device=q.device)
+            out = q.new_empty(q.shape)
+            co = Heads(out.data_ptr(), heads * dim, dim)
         elif out.dtype != q.dtype or out.shape != q.shape:
             raise ValueError("out must have q's shape and type")
-        co = _heads(out, "out", tokens, self.head_dim, self.device)
-        lse = torch.empty((tokens, heads), dtype=torch.float32, device=q.device) if want_lse else None
-        s, need = ccv3d_kv_attend_workspace(self.c, c, heads, dt)
-        if s != OK:
-            raise Ccv3dError(s, "ccv3d_kv_attend_workspace")
-        # scratch from torch's allocator: on the current stream, so calls on other streams never share it
-        ws = torch.empty(need, dtype=torch.uint8, device=q.device) if need else None
+        else:
+            co = _heads(out, "out", tokens, dim, dev)
+        lse = q.new_empty((tokens, heads), dtype=torch.float32) if want_lse else None
+        stream = _stream(dev)
+        ws, need = self._workspace(c, heads, dt, stream)
         s = lib.ccv3d_kv_attend(self.c, c, cq, co, None if lse is None else lse.data_ptr(), heads, dt,
-                                self.head_dim ** -0.5 if scale is None else scale, frame, window,
-                                None if ws is None else ws.data_ptr(), need, self._status_ptr,
-                                torch.cuda.current_stream().cuda_stream)
+                                dim ** -0.5 if scale is None else scale, frame, window, ws.data_ptr(), need,
+                                self._status_ptr, stream)
         if s != OK:
             raise Ccv3dError(s, "ccv3d_kv_attend")
         return (out, lse) if want_lse else out
 
 
-def _rows(t, what, shape, dev):
-    if t.dim() != 2 or tuple(t.shape) != shape:
-        raise ValueError(f"{what} has shape {tuple(t.shape)}: {list(shape)} is wanted")
+def _rows(t, what, rows, ch, dev):
+    """Elements between the rows of a [rows, ch] tensor."""
+    shape = t.shape
+    if len(shape) != 2 or shape[0] != rows or shape[1] != ch:
+        raise ValueError(f"{what} has shape {tuple(shape)}: {[rows, ch]} is wanted")
     _on_device(t, what, dev)
     rs, es = t.stride()
-    if es != 1 and shape[1] > 1:
+    if es != 1 and ch > 1:
         raise ValueError(f"{what}: the last dimension must be contiguous")
-    return rs if shape[0] > 1 else shape[1]
+    return rs if rows > 1 else ch
+
+
+def _ptr(t):
+    return None if t is None else t.data_ptr()
 
 
 def gated_norm(x, y=None, *, gate=None, post_weight=None, post_bias=None, pre_weight=None, pre_bias=None, scale=None,
@@ -214,57 +242,59 @@ def gated_norm(x, y=None, *, gate=None, post_weight=None, post_bias=None, pre_we
     if x.dim() != 2:
         raise ValueError("x must be [rows, channels]")
     rows, ch = x.shape
-    shape = (rows, ch)
-    dev = torch.cuda.current_device()
-    d = NormDesc()
-    d.rows, d.channels, d.residual_scale, d.eps = rows, ch, residual_scale, eps
-    d.post_kind, d.pre_kind = _KINDS[post_kind], _KINDS[pre_kind]
-    d.res_dtype = _dtype(x, "x")
-    d.x_stride = _rows(x, "x", shape, dev)
+    dev = _device()
+    res = _dtype(x, "x")
+    xs, ys = _rows(x, "x", rows, ch, dev), 0
     if y is not None:
         if act_dtype is not None and act_dtype != y.dtype:
             raise TypeError("act_dtype differs from y's type")
         act_dtype = y.dtype
-        d.y_stride = _rows(y, "y", shape, dev)
-    act_dtype = act_dtype or x.dtype
-    if act_dtype not in _DTYPES:
-        raise TypeError(f"act_dtype {act_dtype} is neither bfloat16 nor float32")
-    d.act_dtype = _DTYPES[act_dtype]
-    groups, mod, weight = None, None, None
-    for t, what, field in ((gate, "gate", "gate_stride"), (scale, "scale", "scale_stride"), (shift, "shift", "shift_stride")):
+        ys = _rows(y, "y", rows, ch, dev)
+    elif act_dtype is None:
+        act_dtype = x.dtype
+    act = _DTYPES.get(act_dtype)
+    if act is None:
+        raise TypeError(f"{act_dtype} is neither bfloat16 nor float32")
+    groups, mod, strides = None, torch.float32, [0, 0, 0]
+    for i, t in enumerate((gate, scale, shift)):
         if t is None:
             continue
-        if t.dim() != 2 or t.shape[1] != ch or (groups is not None and t.shape[0] != groups) or (mod is not None and t.dtype != mod):
-            raise ValueError(f"{what} must be [groups, {ch}], with one type and number of groups for gate, scale and shift")
-        groups, mod = t.shape[0], t.dtype
-        setattr(d, field, _rows(t, what, (groups, ch), dev))
-    d.mod_dtype = F32 if mod is None else _DTYPES.get(mod, -1)
+        if groups is None:
+            groups, mod = t.shape[0], t.dtype
+        elif t.dtype != mod:
+            raise TypeError("gate, scale and shift must have one type")
+        strides[i] = _rows(t, ("gate", "scale", "shift")[i], groups, ch, dev)
     if rows_per_group is None:
         rows_per_group = max(1, -(-rows // groups)) if groups else max(1, rows)
     if groups is not None and rows > groups * rows_per_group:
         raise ValueError(f"{groups} groups of {rows_per_group} rows do not cover {rows} rows")
-    d.rows_per_group = rows_per_group
-    for t, what in ((post_weight, "post_weight"), (post_bias, "post_bias"), (pre_weight, "pre_weight"), (pre_bias, "pre_bias")):
+    weight = None
+    for t in (post_weight, post_bias, pre_weight, pre_bias):
         if t is None:
             continue
-        if t.shape != (ch,) or not t.is_contiguous() or (weight is not None and t.dtype != weight):
-            raise ValueError(f"{what} must be a contiguous [{ch}], with one type for all weights and biases")
-        _on_device(t, what, dev)
-        weight = t.dtype
-    d.weight_dtype = F32 if weight is None else _DTYPES.get(weight, -1)
-    if out_r is None and want_r:
-        out_r = torch.empty(shape, dtype=x.dtype, device=x.device)
-    if out_h is None and want_h:
-        out_h = torch.empty(shape, dtype=act_dtype, device=x.device)
-    for t, what, dt, field in ((out_r, "out_r", x.dtype, "r_stride"), (out_h, "out_h", act_dtype, "h_stride")):
-        if t is not None:
-            if t.dtype != dt:
-                raise TypeError(f"{what} must be {dt}")
-            setattr(d, field, _rows(t, what, shape, dev))
-    ptr = lambda t: None if t is None else t.data_ptr()  # noqa: E731
-    s = lib.ccv3d_gated_norm(d, x.data_ptr(), ptr(y), ptr(post_weight), ptr(post_bias), ptr(gate), ptr(pre_weight),
-                             ptr(pre_bias), ptr(scale), ptr(shift), ptr(out_r), ptr(out_h),
-                             torch.cuda.current_stream().cuda_stream)
+        if weight is None:
+            weight = t.dtype
+        if t.shape != (ch,) or not t.is_contiguous() or t.dtype != weight:
+            raise ValueError(f"weights and biases must be contiguous [{ch}] tensors of one type")
+        _on_device(t, "a weight or bias", dev)
+    rs = hs = ch
+    if out_r is not None:
+        if out_r.dtype != x.dtype:
+            raise TypeError(f"out_r must be {x.dtype}")
+        rs = _rows(out_r, "out_r", rows, ch, dev)
+    elif want_r:
+        out_r = x.new_empty((rows, ch))
+    if out_h is not None:
+        if out_h.dtype != act_dtype:
+            raise TypeError(f"out_h must be {act_dtype}")
+        hs = _rows(out_h, "out_h", rows, ch, dev)
+    elif want_h:
+        out_h = x.new_empty((rows, ch), dtype=act_dtype)
+    d = NormDesc(rows, ch, rows_per_group, _KINDS[post_kind], _KINDS[pre_kind], res, act,
+                 F32 if weight is None else _DTYPES.get(weight, -1), _DTYPES.get(mod, -1), residual_scale, eps, xs, ys, rs, hs,
+                 *strides)
+    s = lib.ccv3d_gated_norm(d, x.data_ptr(), _ptr(y), _ptr(post_weight), _ptr(post_bias), _ptr(gate), _ptr(pre_weight),
+                             _ptr(pre_bias), _ptr(scale), _ptr(shift), _ptr(out_r), _ptr(out_h), _stream(dev))
     if s != OK:
         raise Ccv3dError(s, "ccv3d_gated_norm")
     return out_r, out_h

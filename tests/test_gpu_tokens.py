@@ -410,6 +410,45 @@ def test_gated_norm(rows, ch, groups, res, act, wd, md, post, pre, parts):
     check_norm(args, per, 0.75, 1e-5, post, pre, r, h)
 
 
+MANY = [  # stretches of rows that cross the groups, channels that no access or team divides
+    (3001, 64, 7, BF16, BF16, F32, BF16, "rms", "layer", "ywbgs"),
+    (700, 192, 3, F32, BF16, BF16, F32, "layer", "rms", "ywbgs"),
+    (901, 390, 1, F32, F32, F32, F32, "rms", "layer", "w"),
+    (640, 1000, 64, BF16, F32, F32, F32, "rms", "layer", "ywgs"),
+    (517, 1153, 5, F32, F32, F32, BF16, "layer", "rms", "ywgs"),
+    (299, 1536, 2, F32, BF16, BF16, BF16, "rms", "layer", "ywbgs"),
+    (333, 4096, 2, BF16, BF16, F32, F32, "rms", "none", "yws"),
+    (305, 3001, 1, F32, BF16, F32, F32, "none", "rms", "yg"),
+    (300, 6001, 2, F32, F32, F32, F32, "rms", "layer", "ywgs"),
+]
+
+
+@pytest.mark.parametrize("rows,ch,groups,res,act,wd,md,post,pre,parts", MANY)
+def test_gated_norm_of_many_rows(rows, ch, groups, res, act, wd, md, post, pre, parts):
+    """As above, with r's terms counted down to what the post norm adds up: with n = (y - mean) f, f = 1 / rms, a sum
+    a x + gate (w n + b) is within 2^-20 of |a x| + |gate| (|w| (|y| + |mean|) f + |b|), which may be far over the sum itself."""
+    from paper_2609_31938_b200 import tokens as tk
+    args = norm_inputs(rows, ch, groups, res, act, wd, md, parts, seed=rows + ch)
+    x, y, gate, pw, pb, qw, qb, scale, shift = (None if t is None else t.cuda() for t in args)
+    per = -(-rows // groups)
+    r, h = tk.gated_norm(x, y, gate=gate, post_weight=pw, post_bias=pb, pre_weight=qw, pre_bias=qb, scale=scale, shift=shift,
+                         residual_scale=0.75, eps=1e-5, post_kind=post, pre_kind=pre, act_dtype=act)
+    want_r, want_h, size = ref.gated_norm(args[0], args[1], per, *args[2:], 0.75, 1e-5, post, pre)
+    if y is not None:
+        z = args[1].double()
+        mean = z.mean(-1, keepdim=True) if post == "layer" else torch.zeros(rows, 1, dtype=torch.float64)
+        f = 1.0 if post == "none" else ((z - mean).square().mean(-1, keepdim=True) + 1e-5).rsqrt()
+        z = (z.abs() + mean.abs()) * f
+        z = z * args[3].double().abs() if args[3] is not None else z
+        z = z + args[4].double().abs() if args[4] is not None else z
+        z = z * args[2].double().abs()[torch.arange(rows) // per] if args[2] is not None else z
+        size = (0.75 * args[0].double()).abs() + z
+    half = lambda t: 2.0 ** -8 if t.dtype == BF16 else U  # noqa: E731
+    assert ((r.cpu().double() - want_r).abs() <= half(r) * want_r.abs() + 2.0 ** -20 * size).all()
+    big = want_h.abs().amax(-1, keepdim=True) + 1
+    assert ((h.cpu().double() - want_h).abs() <= half(h) * want_h.abs() + 2.0 ** -18 * big).all()
+
+
 def test_gated_norm_strides_in_place_and_single_outputs():
     from paper_2609_31938_b200 import tokens as tk
     for ch, wide in ((192, 200), (193, 201)):
