@@ -18,6 +18,9 @@ _KINDS = {"none": NORM_NONE, "rms": NORM_RMS, "layer": NORM_LAYER}
 # current device and stream as plain numbers: the calls below are short enough for the objects around them to matter
 _device = torch.cuda.current_device
 _stream = torch._C._cuda_getCurrentRawStream
+_like = torch.empty_like
+_capturing = torch._C._cuda_isCurrentStreamCapturing
+_DENSE = torch.contiguous_format
 
 
 def _dtype(t: torch.Tensor, what: str) -> int:
@@ -27,16 +30,21 @@ def _dtype(t: torch.Tensor, what: str) -> int:
     return d
 
 
+def _elsewhere(t: torch.Tensor, what: str, dev: int):
+    return ValueError(f"{what} is on {t.device}, not on the current CUDA device cuda:{dev}")
+
+
 def _on_device(t: torch.Tensor, what: str, dev: int) -> None:
     if t.get_device() != dev:
-        raise ValueError(f"{what} is on {t.device}, not on the current CUDA device cuda:{dev}")
+        raise _elsewhere(t, what, dev)
 
 
 def _heads(t: torch.Tensor, what: str, tokens: int, dim: int, dev: int) -> Heads:
     shape = t.shape
     if len(shape) != 3 or shape[0] != tokens or shape[2] != dim:
         raise ValueError(f"{what} has shape {tuple(shape)}: [{tokens}, heads, {dim}] is wanted")
-    _on_device(t, what, dev)
+    if t.get_device() != dev:
+        raise _elsewhere(t, what, dev)
     ts, hs, es = t.stride()
     if es != 1:
         raise ValueError(f"{what}: the last dimension must be contiguous")
@@ -108,6 +116,7 @@ class PagedCache:
         self.c = KvCache(codes.data_ptr(), scales.data_ptr(), self.pages, self.kv_heads, self.page_tokens, self.head_dim)
         self._status = torch.zeros(1, dtype=torch.int32, device=codes.device)
         self._status_ptr = self._status.data_ptr()
+        self._needs = {}         # geometry of a call -> bytes of scratch
         self._scratch = {}       # stream -> scratch of attend calls on it
 
     @classmethod
@@ -133,12 +142,18 @@ class PagedCache:
     def _workspace(self, c: TokenBatchC, heads: int, dt: int, stream: int):
         """Scratch for an attend call on `stream`: kept for the next call on it, so calls on other streams never share it.
         A captured call gets its own, which belongs to the graph."""
-        s, need = ccv3d_kv_attend_workspace(self.c, c, heads, dt)
-        if s != OK:
-            raise Ccv3dError(s, "ccv3d_kv_attend_workspace")
-        ws = self._scratch.get(stream)
-        if torch.cuda.is_current_stream_capturing():
+        key = (c.max_new, c.batch, c.max_pages, c.tokens, heads, dt)
+        need = self._needs.get(key)
+        if need is None:
+            s, need = ccv3d_kv_attend_workspace(self.c, c, heads, dt)
+            if s != OK:
+                raise Ccv3dError(s, "ccv3d_kv_attend_workspace")
+            if len(self._needs) > 4096:
+                self._needs.clear()
+            self._needs[key] = need
+        if _capturing():
             return torch.empty(need, dtype=torch.uint8, device=self.codes.device), need
+        ws = self._scratch.get(stream)
         if ws is None or ws.shape[0] < need:
             ws = self._scratch[stream] = torch.empty(need, dtype=torch.uint8, device=self.codes.device)
         return ws, need
@@ -172,7 +187,7 @@ class PagedCache:
             cq = _heads(q, "q", tokens, dim, dev)
             heads = q.shape[1]
             if q_out is None:
-                q_out = q.new_empty(q.shape)
+                q_out = _like(q, memory_format=_DENSE)
                 cqo = Heads(q_out.data_ptr(), heads * dim, dim)
             elif q_out.dtype != q.dtype or q_out.shape != q.shape:
                 raise ValueError("q_out must have q's shape and type")
@@ -196,7 +211,7 @@ class PagedCache:
         cq = _heads(q, "q", tokens, dim, dev)
         heads = q.shape[1]
         if out is None:
-            out = q.new_empty(q.shape)
+            out = _like(q, memory_format=_DENSE)
             co = Heads(out.data_ptr(), heads * dim, dim)
         elif out.dtype != q.dtype or out.shape != q.shape:
             raise ValueError("out must have q's shape and type")
@@ -215,10 +230,10 @@ class PagedCache:
 
 def _rows(t, what, rows, ch, dev):
     """Elements between the rows of a [rows, ch] tensor."""
-    shape = t.shape
-    if len(shape) != 2 or shape[0] != rows or shape[1] != ch:
-        raise ValueError(f"{what} has shape {tuple(shape)}: {[rows, ch]} is wanted")
-    _on_device(t, what, dev)
+    if t.shape != (rows, ch):
+        raise ValueError(f"{what} has shape {tuple(t.shape)}: {[rows, ch]} is wanted")
+    if t.get_device() != dev:
+        raise _elsewhere(t, what, dev)
     rs, es = t.stride()
     if es != 1 and ch > 1:
         raise ValueError(f"{what}: the last dimension must be contiguous")
@@ -274,22 +289,23 @@ def gated_norm(x, y=None, *, gate=None, post_weight=None, post_bias=None, pre_we
             continue
         if weight is None:
             weight = t.dtype
-        if t.shape != (ch,) or not t.is_contiguous() or t.dtype != weight:
+        if t.shape != (ch,) or t.dtype != weight or not t.is_contiguous():
             raise ValueError(f"weights and biases must be contiguous [{ch}] tensors of one type")
-        _on_device(t, "a weight or bias", dev)
+        if t.get_device() != dev:
+            raise _elsewhere(t, "a weight or bias", dev)
     rs = hs = ch
     if out_r is not None:
         if out_r.dtype != x.dtype:
             raise TypeError(f"out_r must be {x.dtype}")
         rs = _rows(out_r, "out_r", rows, ch, dev)
     elif want_r:
-        out_r = x.new_empty((rows, ch))
+        out_r = _like(x, memory_format=_DENSE)
     if out_h is not None:
         if out_h.dtype != act_dtype:
             raise TypeError(f"out_h must be {act_dtype}")
         hs = _rows(out_h, "out_h", rows, ch, dev)
     elif want_h:
-        out_h = x.new_empty((rows, ch), dtype=act_dtype)
+        out_h = _like(x if y is None else y, dtype=act_dtype, memory_format=_DENSE)
     d = NormDesc(rows, ch, rows_per_group, _KINDS[post_kind], _KINDS[pre_kind], res, act,
                  F32 if weight is None else _DTYPES.get(weight, -1), _DTYPES.get(mod, -1), residual_scale, eps, xs, ys, rs, hs,
                  *strides)
