@@ -253,6 +253,38 @@ struct TileRow {
     int token, head;         // packed token, query head; token < 0: no row
 };
 
+// 32 elements of a row; zeros without one.
+template <typename T>
+__device__ __forceinline__ void load_row32(const T* src, float (&x)[32]) {
+#pragma unroll
+    for (int k = 0; k < 32; ++k) x[k] = 0.f;
+    if (!src) return;
+    if constexpr (sizeof(T) == 2) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const uint4 t = *reinterpret_cast<const uint4*>(src + 8 * j);
+            const uint32_t e[4] = {t.x, t.y, t.z, t.w};
+#pragma unroll
+            for (int k = 0; k < 4; ++k) { x[8 * j + 2 * k] = __uint_as_float(e[k] << 16); x[8 * j + 2 * k + 1] = __uint_as_float(e[k] & 0xFFFF0000u); }
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const float4 t = *reinterpret_cast<const float4*>(src + 4 * j);
+            x[4 * j] = t.x; x[4 * j + 1] = t.y; x[4 * j + 2] = t.z; x[4 * j + 3] = t.w;
+        }
+    }
+}
+template <typename T>
+__device__ __forceinline__ void store_row32(T* dst, const float (&x)[32]) {
+#pragma unroll
+    for (int j = 0; j < 32; j += sizeof(T) == 2 ? 8 : 4) {
+        if constexpr (sizeof(T) == 2)
+            *reinterpret_cast<uint4*>(dst + j) = make_uint4(pack_bf16(x[j], x[j + 1]), pack_bf16(x[j + 2], x[j + 3]), pack_bf16(x[j + 4], x[j + 5]), pack_bf16(x[j + 6], x[j + 7]));
+        else
+            *reinterpret_cast<float4*>(dst + j) = make_float4(x[j], x[j + 1], x[j + 2], x[j + 3]);
+    }
+}
 // Stages the queries of one row (each thread its own) and returns what the row needs to know.
 template <typename T, int D>
 __device__ __forceinline__ TileRow stage_row(const AttendParams& p, const TileSegment& w, int r, int tid, uint8_t* q) {
@@ -267,57 +299,34 @@ __device__ __forceinline__ TileRow stage_row(const AttendParams& p, const TileSe
         visible(p, w.before + at / p.group, w.total, row.lo, row.hi);
         src = (const T*)p.q.data + row.token * p.q.token_stride + row.head * p.q.head_stride;
     }
-    if constexpr (sizeof(T) == 2) {
-        uint4 x[D / 8];
+    // (loops, not straight-line code: what an item runs once finds the instruction cache cold, line by line)
+#pragma unroll 1
+    for (int i = 0; i < D; i += 32) {
+        float x[32];
+        load_row32(src ? src + i : nullptr, x);
 #pragma unroll
-        for (int i = 0; i < D / 8; ++i) x[i] = src ? *reinterpret_cast<const uint4*>(src + 8 * i) : make_uint4(0, 0, 0, 0);
+        for (int k = 0; k < 32; ++k) most = fmaxf(most, fabsf(x[k]));
+    }
+    float down, up;
+    row_power(most, down, up);
+    row.factor = up * (p.scale * LOG2E);
+#pragma unroll 1
+    for (int i = 0; i < D; i += 32) {
+        float x[32];
+        load_row32(src ? src + i : nullptr, x);
+        uint8_t* dst = q + (i / 64) * S::HALF + tid * 128;
 #pragma unroll
-        for (int i = 0; i < D / 8; ++i) {
-            const uint32_t e[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
-#pragma unroll
-            for (int k = 0; k < 4; ++k)
-                most = fmaxf(most, fmaxf(fabsf(__uint_as_float(e[k] << 16)), fabsf(__uint_as_float(e[k] & 0xFFFF0000u))));
-        }
-        float down, up;
-        row_power(most, down, up);
-        row.factor = up * (p.scale * LOG2E);
-#pragma unroll
-        for (int i = 0; i < D / 8; ++i) {
-            const uint32_t e[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
-            uint32_t y[4];
-#pragma unroll
-            for (int k = 0; k < 4; ++k) y[k] = pack_half(__uint_as_float(e[k] << 16) * down, __uint_as_float(e[k] & 0xFFFF0000u) * down);
-            *reinterpret_cast<uint4*>(q + (i / 8) * S::HALF + tid * 128 + ((i % 8) ^ (tid & 7)) * 16) = make_uint4(y[0], y[1], y[2], y[3]);
-        }
-    } else {
-        for (int i = 0; i < D / 4; ++i) {
-            float x[4] = {0.f, 0.f, 0.f, 0.f};
-            if (src) load4(src + 4 * i, x);
-            most = fmaxf(fmaxf(most, fmaxf(fabsf(x[0]), fabsf(x[1]))), fmaxf(fabsf(x[2]), fabsf(x[3])));
-        }
-        float down, up;
-        row_power(most, down, up);
-        row.factor = up * (p.scale * LOG2E);
-        for (int i = 0; i < D / 8; ++i) {
-            float x[8];
-#pragma unroll
-            for (int k = 0; k < 8; ++k) x[k] = 0.f;
-            if (src) {
-                float a[4];
-                load4(src + 8 * i, a);
-                x[0] = a[0]; x[1] = a[1]; x[2] = a[2]; x[3] = a[3];
-                load4(src + 8 * i + 4, a);
-                x[4] = a[0]; x[5] = a[1]; x[6] = a[2]; x[7] = a[3];
-            }
+        for (int j = 0; j < 4; ++j) {
             uint32_t y[4], z[4];
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
-                y[k] = pack_half(x[2 * k] * down, x[2 * k + 1] * down);
-                z[k] = pack_rest(x[2 * k] * down, x[2 * k + 1] * down, y[k]);
+                const float u = x[8 * j + 2 * k] * down, v = x[8 * j + 2 * k + 1] * down;
+                y[k] = pack_half(u, v);
+                z[k] = S::TERMS == 2 ? pack_rest(u, v, y[k]) : 0;
             }
-            uint8_t* dst = q + (i / 8) * S::HALF + tid * 128 + ((i % 8) ^ (tid & 7)) * 16;
-            *reinterpret_cast<uint4*>(dst) = make_uint4(y[0], y[1], y[2], y[3]);
-            *reinterpret_cast<uint4*>(dst + S::KV) = make_uint4(z[0], z[1], z[2], z[3]);
+            uint8_t* at = dst + (((i / 8 + j) & 7) ^ (tid & 7)) * 16;
+            *reinterpret_cast<uint4*>(at) = make_uint4(y[0], y[1], y[2], y[3]);
+            if (S::TERMS == 2) *reinterpret_cast<uint4*>(at + S::KV) = make_uint4(z[0], z[1], z[2], z[3]);
         }
     }
     return row;
@@ -346,6 +355,11 @@ __device__ __forceinline__ float max3(float a, float b, float c) {      // (NaN 
     return r;
 }
 
+// Bits of the tokens [first, end) of 32 that begin at 0.
+__device__ __forceinline__ uint32_t bits_between(int first, int end) {
+    const uint32_t below_end = end >= 32 ? 0xFFFFFFFFu : (1u << max(end, 0)) - 1u, below_first = first >= 32 ? 0xFFFFFFFFu : (1u << max(first, 0)) - 1u;
+    return below_end & ~below_first;
+}
 // Scores of 32 tokens (two groups of 16) to weights: packed into pr (F32: remainders into rest).  mx gathers the largest
 // exponent met, sum what the weights add to the row's weight sum.
 template <bool REST, bool EDGE>
@@ -357,14 +371,14 @@ __device__ __forceinline__ void chunk_weights(const uint32_t (&v)[32], const flo
         const float f = k.x * row.factor, a = k.y - m_use;
         const uint64_t f2 = pair(f, f), a2 = pair(a, a);
         uint64_t part = 0;                                       // two sums: even and odd tokens
+        const uint32_t seen = EDGE && k.y != -INFINITY ? bits_between(row.lo - t0 - 16 * g, row.hi - t0 - 16 * g) : 0u;
 #pragma unroll
         for (int i = 0; i < 16; i += 2) {
             float x, y;
             unpair(fma_pair(pair(__uint_as_float(v[16 * g + i]), __uint_as_float(v[16 * g + i + 1])), f2, a2), x, y);
             if (EDGE) {
-                const int at = t0 + 16 * g + i;
-                if (at < row.lo || at >= row.hi || k.y == -INFINITY) x = -INFINITY;
-                if (at + 1 < row.lo || at + 1 >= row.hi || k.y == -INFINITY) y = -INFINITY;
+                if (!(seen >> i & 1u)) x = -INFINITY;
+                if (!(seen >> (i + 1) & 1u)) y = -INFINITY;
             }
             mx = max3(mx, x, y);
             const float e0 = exp2_fast(x), e1 = exp2_fast(y);
@@ -397,61 +411,46 @@ struct TileSoftmax {
 // One tile of a row: weights of 64 tokens twice; `ready(half)` tells the MMA warp that they are in TMEM.  The scores of the
 // next 32 tokens are on their way while those before are worked on.  Where a score passes the maximum by more than the
 // weights can hold, the maximum moves (by a whole power of two, so what has been summed is scaled exactly) and the half is
-// done again; `settled(half)` waits until the outputs hold all weights given before that half.
+// done again by the same code; `settled(half)` waits until the outputs hold all weights given before that half.
 template <typename T, int D, bool EDGE, typename Ready, typename Settled>
 __device__ __forceinline__ bool tile_softmax(TileSoftmax& x, const float4* group, const TileRow& row, int t0, bool first, const Ready& ready,
                                              const Settled& settled) {
     constexpr bool REST = sizeof(T) == 4;
     uint32_t a[32], b[32], pr[32], rest[REST ? 32 : 16];
-    auto work = [&](const uint32_t (&v)[32], int c, float& mx, float& sum) {
-        chunk_weights<REST, EDGE>(v, group + 2 * c, row, (x.m == -INFINITY ? 0.f : x.m) - TILE_SHIFT, t0 + 32 * c, pr + 16 * (c & 1), rest + (REST ? 16 * (c & 1) : 0), mx, sum);
-    };
-    auto finish = [&](int half, float mx, float sum) {
-        if (__any_sync(0xffffffffu, mx > TILE_TOP || (x.m == -INFINITY && mx > -INFINITY))) {
-            const float now = fmaxf(x.m, ceilf(mx + ((x.m == -INFINITY ? 0.f : x.m) - TILE_SHIFT)));     // (mx = -inf leaves m)
+    tc_ld32(x.t_s, a);
+#pragma unroll 1
+    for (int half = 0; half < 2; ++half) {
+        const float4* k = group + 4 * half;
+        float sum;
+#pragma unroll 1
+        for (;;) {
+            float mx = -INFINITY;
+            sum = 0.f;
+            const float m_use = (x.m == -INFINITY ? 0.f : x.m) - TILE_SHIFT;
+            tc_wait_ld();
+            tc_ld32(x.t_s + 64 * half + 32, b);
+            chunk_weights<REST, EDGE>(a, k, row, m_use, t0 + 64 * half, pr, rest, mx, sum);
+            tc_wait_ld();
+            chunk_weights<REST, EDGE>(b, k + 2, row, m_use, t0 + 64 * half + 32, pr + 16, rest + (REST ? 16 : 0), mx, sum);
+            if (!__any_sync(0xffffffffu, mx > TILE_TOP || (x.m == -INFINITY && mx > -INFINITY))) break;
+            const float now = fmaxf(x.m, ceilf(mx + m_use));                     // (mx = -inf leaves m)
             const float corr = x.m == -INFINITY ? 0.f : exp2_fast(x.m - now);
             if (!first || half == 1) {
                 if (!settled(half)) return false;
+#pragma unroll 1
                 for (int c = 0; c < D; c += 32) scale_columns(x.t_o + c, corr);
             }
             x.l *= corr;
             x.m = now;
-            mx = -INFINITY;
-            sum = 0.f;
-#pragma unroll
-            for (int c = 0; c < 2; ++c) {
-                uint32_t v[32];
-                tc_ld32(x.t_s + 64 * half + 32 * c, v);
-                tc_wait_ld();
-                work(v, 2 * half + c, mx, sum);
-            }
+            tc_ld32(x.t_s + 64 * half, a);
         }
+        if (half == 0) tc_ld32(x.t_s + 64, a);
         x.l += sum;
         tc_st<32>(x.t_p + 32 * half, pr);
         if constexpr (REST) tc_st<32>(x.t_p + 64 + 32 * half, rest);
-        return true;
-    };
-    float mx = -INFINITY, sum = 0.f;
-    tc_ld32(x.t_s, a);
-    tc_wait_ld();
-    tc_ld32(x.t_s + 32, b);
-    work(a, 0, mx, sum);
-    tc_wait_ld();
-    tc_ld32(x.t_s + 64, a);
-    work(b, 1, mx, sum);
-    if (!finish(0, mx, sum)) return false;
-    mx = -INFINITY;
-    sum = 0.f;
-    tc_wait_ld();
-    tc_ld32(x.t_s + 96, b);
-    work(a, 2, mx, sum);
-    tc_wait_st();
-    ready(0);                                        // (the stores had the time of 32 tokens to arrive)
-    tc_wait_ld();
-    work(b, 3, mx, sum);
-    if (!finish(1, mx, sum)) return false;
-    tc_wait_st();
-    ready(1);
+        tc_wait_st();
+        ready(half);
+    }
     return true;
 }
 
@@ -572,6 +571,7 @@ __global__ void __launch_bounds__(TILE_THREADS, 1) kv_attend_tile_kernel(const A
             const int64_t slot = (2 * (int64_t)blockIdx.x + (w.starts ? 1 : 0)) * p.slot_rows + 128 * qt + tid;
             const float inv = l != 0.f ? 1.f / l : 0.f;
             const bool nan = *(volatile int*)&sh->nan_found != 0;
+#pragma unroll 1
             for (int c = 0; c < D; c += 32) {
                 uint32_t v[32];
                 tc_ld32(t_o + c, v);
@@ -592,19 +592,11 @@ __global__ void __launch_bounds__(TILE_THREADS, 1) kv_attend_tile_kernel(const A
                     }
                 }
                 if (row.token >= 0) {
+                    float x[32];
 #pragma unroll
-                    for (int k = 0; k < 32; k += 4) {
-                        float x[4];
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) x[e] = __uint_as_float(v[k + e]);
-                        if (whole) {
-#pragma unroll
-                            for (int e = 0; e < 4; ++e) x[e] = l != 0.f ? x[e] * inv : 0.f;
-                            store_out<T>(p, row.token, row.head, c + k, x);
-                        } else {
-                            store4(p.part + slot * D + c + k, x);
-                        }
-                    }
+                    for (int k = 0; k < 32; ++k) x[k] = whole ? (l != 0.f ? __uint_as_float(v[k]) * inv : 0.f) : __uint_as_float(v[k]);
+                    if (whole) store_row32((T*)p.o.data + row.token * p.o.token_stride + row.head * p.o.head_stride + c, x);
+                    else store_row32(p.part + slot * D + c, x);
                 }
             }
             tc_fence_before();
