@@ -114,6 +114,8 @@ struct TileWalk {
 
 // Finds this block's share.  All threads of the block call it: costs of up to TILE_BATCH sequences at a time, a warp each.
 template <int ROWS>
+__device__ __noinline__ TileItem tile_item_call(const AttendParams& p, const Seq& s, int rb) { return tile_item<ROWS>(p, s, rb); }
+template <int ROWS>
 __device__ __forceinline__ TileWalk<ROWS> tile_share(const AttendParams& p, int* cost_of) {
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = blockDim.x >> 5;
     TileWalk<ROWS> w;
@@ -132,7 +134,7 @@ __device__ __forceinline__ TileWalk<ROWS> tile_share(const AttendParams& p, int*
                     const Seq s = load_seq(p.bt, p.c.page_tokens, c0 + b, pass == 0 ? p.status : nullptr);
                     const int blocks = (s.n * p.group + ROWS - 1) / ROWS;
                     int units = 0;
-                    for (int rb = lane; rb < blocks; rb += 32) units += tile_item<ROWS>(p, s, rb).units;
+                    for (int rb = lane; rb < blocks; rb += 32) units += tile_item_call<ROWS>(p, s, rb).units;
                     units = __reduce_add_sync(0xffffffffu, units);
                     if (lane == 0) cost_of[b] = units * p.c.kv_heads;
                 }
@@ -150,14 +152,14 @@ __device__ __forceinline__ TileWalk<ROWS> tile_share(const AttendParams& p, int*
                 w.s = load_seq(p.bt, p.c.page_tokens, w.b, nullptr);
                 const int blocks = (w.s.n * p.group + ROWS - 1) / ROWS;
                 for (int r0 = 0; r0 < blocks && !found; r0 += 32) {
-                    const int cost = r0 + lane < blocks ? tile_item<ROWS>(p, w.s, r0 + lane).units * p.c.kv_heads : 0;
+                    const int cost = r0 + lane < blocks ? tile_item_call<ROWS>(p, w.s, r0 + lane).units * p.c.kv_heads : 0;
                     const int to = warp_scan(cost);
                     const unsigned in = __ballot_sync(0xffffffffu, cost > 0 && at < to);
                     if (!in) { at -= __shfl_sync(0xffffffffu, to, 31); continue; }
                     const int r = __ffs(in) - 1;
                     at -= __shfl_sync(0xffffffffu, to - cost, r);
                     w.rb = r0 + r;
-                    w.t = tile_item<ROWS>(p, w.s, w.rb);
+                    w.t = tile_item_call<ROWS>(p, w.s, w.rb);
                     w.h = at / w.t.units;
                     w.unit = at % w.t.units;
                     found = true;
@@ -181,22 +183,18 @@ __device__ __forceinline__ TileWalk<ROWS> tile_share(const AttendParams& p, int*
 __device__ __forceinline__ bool tile_wait(uint64_t* bar, uint32_t parity, TileShared* sh, const AttendParams& p) {
     const uint32_t b = smem_u32(bar);
     if (mbar_try_wait(b, parity)) return true;
-    long long since = 0;
-    for (uint32_t it = 1;; ++it) {
-        if (mbar_try_wait(b, parity)) return true;
-        if ((it & 63u) == 0u) {
-            if (*(volatile int*)&sh->abort_flag) return false;
-            const long long now = clock64();
-            if (!since) since = now;
-            else if (now - since > p.wait_clk) {
-                *(volatile int*)&sh->abort_flag = 1;
-                report(p.status, CCV3D_TOKENS_TIMEOUT);
-                return false;
-            }
+    const long long since = clock64();
+#pragma unroll 1
+    while (!mbar_try_wait(b, parity)) {
+        if (*(volatile int*)&sh->abort_flag) return false;
+        if (clock64() - since > p.wait_clk) {
+            *(volatile int*)&sh->abort_flag = 1;
+            report(p.status, CCV3D_TOKENS_TIMEOUT);
+            return false;
         }
     }
+    return true;
 }
-
 __device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity, TileShared* sh, const AttendParams& p) {
     return __all_sync(0xffffffffu, tile_wait(bar, parity, sh, p));
 }
@@ -254,25 +252,11 @@ struct TileRow {
 };
 
 // 32 elements of a row; zeros without one.
-template <typename T>
-__device__ __forceinline__ void load_row32(const T* src, float (&x)[32]) {
+__device__ __forceinline__ void load_row32(const float* src, float (&x)[32]) {
 #pragma unroll
-    for (int k = 0; k < 32; ++k) x[k] = 0.f;
-    if (!src) return;
-    if constexpr (sizeof(T) == 2) {
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const uint4 t = *reinterpret_cast<const uint4*>(src + 8 * j);
-            const uint32_t e[4] = {t.x, t.y, t.z, t.w};
-#pragma unroll
-            for (int k = 0; k < 4; ++k) { x[8 * j + 2 * k] = __uint_as_float(e[k] << 16); x[8 * j + 2 * k + 1] = __uint_as_float(e[k] & 0xFFFF0000u); }
-        }
-    } else {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const float4 t = *reinterpret_cast<const float4*>(src + 4 * j);
-            x[4 * j] = t.x; x[4 * j + 1] = t.y; x[4 * j + 2] = t.z; x[4 * j + 3] = t.w;
-        }
+    for (int j = 0; j < 8; ++j) {
+        const float4 t = src ? *reinterpret_cast<const float4*>(src + 4 * j) : make_float4(0.f, 0.f, 0.f, 0.f);
+        x[4 * j] = t.x; x[4 * j + 1] = t.y; x[4 * j + 2] = t.z; x[4 * j + 3] = t.w;
     }
 }
 template <typename T>
@@ -285,12 +269,11 @@ __device__ __forceinline__ void store_row32(T* dst, const float (&x)[32]) {
             *reinterpret_cast<float4*>(dst + j) = make_float4(x[j], x[j + 1], x[j + 2], x[j + 3]);
     }
 }
-// Stages the queries of one row (each thread its own) and returns what the row needs to know.
+// Stages the queries of 32 rows (all lanes of the warp call it) and returns what each thread needs to know of its own.
 template <typename T, int D>
 __device__ __forceinline__ TileRow stage_row(const AttendParams& p, const TileSegment& w, int r, int tid, uint8_t* q) {
     using S = TileShape<T, D>;
     TileRow row = {0, 0, 0.f, -1, 0};
-    float most = 0.f;
     const T* src = nullptr;
     if (r < w.nrows) {
         const int at = w.row0 + r;
@@ -299,36 +282,89 @@ __device__ __forceinline__ TileRow stage_row(const AttendParams& p, const TileSe
         visible(p, w.before + at / p.group, w.total, row.lo, row.hi);
         src = (const T*)p.q.data + row.token * p.q.token_stride + row.head * p.q.head_stride;
     }
-    // (loops, not straight-line code: what an item runs once finds the instruction cache cold, line by line)
-#pragma unroll 1
-    for (int i = 0; i < D; i += 32) {
-        float x[32];
-        load_row32(src ? src + i : nullptr, x);
+    float up;
+    if constexpr (sizeof(T) == 2) {
+        // A warp reads its 32 rows together, D / 8 lanes to a row: a thread's own row would take 32 lines for each access.
+        constexpr int LPR = D / 8, RPI = 32 / LPR, IT = LPR;     // lanes to a row, rows at a time, rounds
+        const int lane = tid & 31, sub = lane / LPR, l = lane % LPR, r0 = r - lane;      // first row of the warp
+        const int at = w.row0 + r0 + sub;
+        int head = at % p.group;
+        const T* from = (const T*)p.q.data + (w.first + at / p.group) * p.q.token_stride + (w.h * p.group + head) * p.q.head_stride + l * 8;
+        const int64_t step = RPI * p.q.head_stride, wrap = p.q.token_stride - p.group * p.q.head_stride;
+        uint4 x[IT];
 #pragma unroll
-        for (int k = 0; k < 32; ++k) most = fmaxf(most, fabsf(x[k]));
-    }
-    float down, up;
-    row_power(most, down, up);
-    row.factor = up * (p.scale * LOG2E);
-#pragma unroll 1
-    for (int i = 0; i < D; i += 32) {
-        float x[32];
-        load_row32(src ? src + i : nullptr, x);
-        uint8_t* dst = q + (i / 64) * S::HALF + tid * 128;
+        for (int i = 0; i < IT; ++i) {
+            x[i] = make_uint4(0, 0, 0, 0);
+            if (r0 + i * RPI + sub < w.nrows) x[i] = *reinterpret_cast<const uint4*>(from);
+            from += step;
+            head += RPI;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            uint32_t y[4], z[4];
+            for (int k = 0; k < RPI; ++k)
+                if (head >= p.group) { head -= p.group; from += wrap; }
+        }
+        // largest magnitudes from the bits, two elements to an instruction; then over a row's lanes, halving the rounds a
+        // lane answers for at each step: lane l ends with round l's
+        uint32_t big[IT];
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                const float u = x[8 * j + 2 * k] * down, v = x[8 * j + 2 * k + 1] * down;
-                y[k] = pack_half(u, v);
-                z[k] = S::TERMS == 2 ? pack_rest(u, v, y[k]) : 0;
+        for (int i = 0; i < IT; ++i)
+            big[i] = __vmaxu2(__vmaxu2(x[i].x & 0x7FFF7FFFu, x[i].y & 0x7FFF7FFFu), __vmaxu2(x[i].z & 0x7FFF7FFFu, x[i].w & 0x7FFF7FFFu));
+#pragma unroll
+        for (int o = LPR / 2; o; o >>= 1)
+#pragma unroll
+            for (int i = 0; i < o; ++i) {
+                const uint32_t give = l & o ? big[i] : big[i + o], keep = l & o ? big[i + o] : big[i];
+                big[i] = __vmaxu2(keep, __shfl_xor_sync(0xffffffffu, give, o));
             }
-            uint8_t* at = dst + (((i / 8 + j) & 7) ^ (tid & 7)) * 16;
-            *reinterpret_cast<uint4*>(at) = make_uint4(y[0], y[1], y[2], y[3]);
-            if (S::TERMS == 2) *reinterpret_cast<uint4*>(at + S::KV) = make_uint4(z[0], z[1], z[2], z[3]);
+        // BF16 s eeeeeeee mmmmmmm to a half s eeeee mmm mmmm000 with the row's largest exponent in the place of 2^14: exponents
+        // by a subtraction, both elements at once; what lies 2^-28 under the row's largest becomes zero.  The factor puts
+        // the exponent back; a row with an infinity or a NaN gets NaN for it.
+        const uint32_t most = max(big[0] & 0xFFFFu, big[0] >> 16);
+        const int field = max((int)(most >> 7) - 29, 0);
+        up = most >= 0x7F80u ? __int_as_float(0x7FFFFFFF) : __uint_as_float((uint32_t)(field + 15) << 23);
+        up = __shfl_sync(0xffffffffu, up, lane % RPI * LPR + lane / RPI);        // of this thread's own row
+        const uint32_t off = (uint32_t)(-(field << 7) & 0xFFFF) * 0x10001u;
+#pragma unroll
+        for (int i = 0; i < IT; ++i) {
+            const int rr = i * RPI + sub;                                        // row of the warp, and of the row block
+            const uint32_t o = __shfl_sync(0xffffffffu, off, sub * LPR + i);
+            const uint32_t e[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
+            uint32_t y[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) y[k] = (__viaddmax_s16x2(e[k] & 0x7FFF7FFFu, o, 0u) << 3) | (e[k] & 0x80008000u);
+            *reinterpret_cast<uint4*>(q + (l / 8) * S::HALF + (tid - lane + rr) * 128 + ((l & 7) ^ (rr & 7)) * 16) = make_uint4(y[0], y[1], y[2], y[3]);
+        }
+    } else {
+        float most = 0.f;
+#pragma unroll 1
+        for (int i = 0; i < D; i += 32) {
+            float x[32];
+            load_row32(src ? src + i : nullptr, x);
+#pragma unroll
+            for (int k = 0; k < 32; ++k) most = fmaxf(most, fabsf(x[k]));
+        }
+        float down;
+        row_power(most, down, up);
+#pragma unroll 1
+        for (int i = 0; i < D; i += 32) {
+            float x[32];
+            load_row32(src ? src + i : nullptr, x);
+            uint8_t* dst = q + (i / 64) * S::HALF + tid * 128;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                uint32_t y[4], z[4];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const float u = x[8 * j + 2 * k] * down, v = x[8 * j + 2 * k + 1] * down;
+                    y[k] = pack_half(u, v);
+                    z[k] = pack_rest(u, v, y[k]);
+                }
+                uint8_t* at = dst + (((i / 8 + j) & 7) ^ (tid & 7)) * 16;
+                *reinterpret_cast<uint4*>(at) = make_uint4(y[0], y[1], y[2], y[3]);
+                *reinterpret_cast<uint4*>(at + S::KV) = make_uint4(z[0], z[1], z[2], z[3]);
+            }
         }
     }
+    row.factor = up * (p.scale * LOG2E);
     return row;
 }
 
@@ -455,7 +491,7 @@ __device__ __forceinline__ bool tile_softmax(TileSoftmax& x, const float4* group
 }
 
 template <typename T, int D>
-__global__ void __launch_bounds__(TILE_THREADS, 1) kv_attend_tile_kernel(const AttendParams p) {
+__global__ void __launch_bounds__(TILE_THREADS, 1) kv_attend_tile_kernel(const __grid_constant__ AttendParams p) {
     using S = TileShape<T, D>;
     constexpr int ROWS = S::ROWS, NQ = S::NQ, TERMS = S::TERMS;
     extern __shared__ __align__(1024) uint8_t smem[];
@@ -503,6 +539,7 @@ __global__ void __launch_bounds__(TILE_THREADS, 1) kv_attend_tile_kernel(const A
         const uint32_t t_o = tmem + lanes + S::O_COL + qt * D;
         uint32_t s_ph = 0, o_ph = 0;
         int tile = 0;                                // tiles of the block so far, over all segments
+        const int pshift = 31 - __clz(P);
         auto meet = [&](int g) {                     // waits for the news of segment g
             ok = warp_wait(&sh->g_full[g % TILE_AHEAD], (uint32_t)(g / TILE_AHEAD) & 1u, sh, p);
         };
@@ -518,22 +555,79 @@ __global__ void __launch_bounds__(TILE_THREADS, 1) kv_attend_tile_kernel(const A
             return r;
         };
         TileRow row = {0, 0, 0.f, -1, 0};
-        bool staged = false;
-        meet(0);
+        TileSoftmax x = {t_s, t_p, t_o, 0.f, 0.f};
+        // A turn of the loop: the queries of segment g go in, then the output of the segment before comes out (it may not be
+        // complete yet when they do), then g's tiles.  (Each piece of code stands here once: it is long.)
+        bool before = false;                         // the segment before had rows here
         for (int g = 0; ok; ++g) {
+            meet(g);
+            if (!ok) break;
             const TileSegment& w = sh->seg[g % TILE_AHEAD];
-            const TileSegment& nx = sh->seg[(g + 1) % TILE_AHEAD];
-            if (!w.live) break;
+            const bool live = w.live, here = live && w.nrows > 128 * qt;
+            TileRow nrow = row;
+            if (here) nrow = stage(w);
+            if (before) {
+                const TileSegment& d = sh->seg[(g - 1) % TILE_AHEAD];
+                if (!(ok = warp_wait(&sh->o_full[qt], o_ph, sh, p))) break;
+                o_ph ^= 1;
+                tc_fence_after();
+                const bool whole = d.starts && d.ends;
+                const int64_t slot = (2 * (int64_t)blockIdx.x + (d.starts ? 1 : 0)) * p.slot_rows + 128 * qt + tid;
+                const float inv = x.l != 0.f ? 1.f / x.l : 0.f;
+                const bool nan = *(volatile int*)&sh->nan_found != 0;
+#pragma unroll 1
+                for (int c = 0; c < D; c += 32) {
+                    uint32_t v[32];
+                    tc_ld32(t_o + c, v);
+                    tc_wait_ld();
+                    if (nan) {
+                        // values that are NaN were staged as zeros where some rows do not see them: find those this row sees
+                        for (int i = 0; i < d.n; ++i) {
+                            const int t0 = d.t0 + i * TILE_UNIT;
+                            if (t0 >= d.lo_all && t0 + TILE_UNIT <= d.hi_all) continue;
+                            for (int t = max(t0, row.lo); t < min(t0 + TILE_UNIT, row.hi); ++t) {
+                                const int page = load_page(p.bt, p.c, d.b, t >> pshift, nullptr);
+                                if (page < 0) continue;
+                                const uint32_t* src = reinterpret_cast<const uint32_t*>((const uint8_t*)p.c.codes + ((((int64_t)page * 2 + 1) * H + d.h) * P + (t & (P - 1))) * D + c);
+#pragma unroll
+                                for (int k = 0; k < 8; ++k) {
+                                    const uint32_t n4 = __vcmpeq4(src[k] & 0x7F7F7F7Fu, 0x7F7F7F7Fu);
+#pragma unroll
+                                    for (int e = 0; e < 4; ++e)
+                                        if (n4 >> (8 * e) & 1u) v[4 * k + e] = 0x7FFFFFFFu;
+                                }
+                            }
+                        }
+                    }
+                    if (row.token >= 0) {
+                        float y[32];
+#pragma unroll
+                        for (int k = 0; k < 32; ++k) y[k] = whole ? (x.l != 0.f ? __uint_as_float(v[k]) * inv : 0.f) : __uint_as_float(v[k]);
+                        if (whole) store_row32((T*)p.o.data + row.token * p.o.token_stride + row.head * p.o.head_stride + c, y);
+                        else store_row32(p.part + slot * D + c, y);
+                    }
+                }
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(smem_u32(&sh->o_empty[qt]));
+                if (row.token >= 0) {
+                    if (!whole) p.part_ml[slot] = make_float2(x.m, x.l);
+                    else if (p.lse) p.lse[(int64_t)row.token * p.q_heads + row.head] = lse_of(x.m, x.l, TILE_SHIFT);
+                }
+                if (d.starts && !d.ends && threadIdx.x == 0) p.join[blockIdx.x] = {d.parts, d.first * p.group + d.row0, d.nrows, d.h * p.group};
+                release(g - 1);
+            }
+            if (!live) break;
+            before = here;
             const int n = w.n;
-            if (w.nrows <= 128 * qt) {
+            if (!here) {
                 tile += n;
-                staged = false;
                 release(g);
-                meet(g + 1);
                 continue;
             }
-            if (!staged) row = stage(w);
-            TileSoftmax x = {t_s, t_p, t_o, -INFINITY, 0.f};
+            row = nrow;
+            x.m = -INFINITY;
+            x.l = 0.f;
             for (int i = 0; i < n; ++i, ++tile) {
                 if (!(ok = warp_wait(&sh->s_full[qt], s_ph, sh, p))) break;
                 s_ph ^= 1;
@@ -556,59 +650,6 @@ __global__ void __launch_bounds__(TILE_THREADS, 1) kv_attend_tile_kernel(const A
                                               : tile_softmax<T, D, false>(x, info.group, row, t0, i == 0, ready, settled);
                 if (!ok) break;
             }
-            const float m = x.m, l = x.l;
-            if (!ok) break;
-            // the next segment's queries go in before this one's output is complete
-            meet(g + 1);
-            if (!ok) break;
-            TileRow nrow = row;
-            staged = nx.live && nx.nrows > 128 * qt;
-            if (staged) nrow = stage(nx);
-            if (!(ok = warp_wait(&sh->o_full[qt], o_ph, sh, p))) break;
-            o_ph ^= 1;
-            tc_fence_after();
-            const bool whole = w.starts && w.ends;
-            const int64_t slot = (2 * (int64_t)blockIdx.x + (w.starts ? 1 : 0)) * p.slot_rows + 128 * qt + tid;
-            const float inv = l != 0.f ? 1.f / l : 0.f;
-            const bool nan = *(volatile int*)&sh->nan_found != 0;
-#pragma unroll 1
-            for (int c = 0; c < D; c += 32) {
-                uint32_t v[32];
-                tc_ld32(t_o + c, v);
-                tc_wait_ld();
-                if (nan) {
-                    // values that are NaN were staged as zeros where some rows do not see them: find those this row sees
-                    for (int i = 0; i < n; ++i) {
-                        const int t0 = w.t0 + i * TILE_UNIT;
-                        if (t0 >= w.lo_all && t0 + TILE_UNIT <= w.hi_all) continue;
-                        for (int t = max(t0, row.lo); t < min(t0 + TILE_UNIT, row.hi); ++t) {
-                            const int page = load_page(p.bt, p.c, w.b, t / P, nullptr);
-                            if (page < 0) continue;
-                            const uint8_t* src = (const uint8_t*)p.c.codes + ((((int64_t)page * 2 + 1) * H + w.h) * P + t % P) * D + c;
-#pragma unroll
-                            for (int k = 0; k < 32; ++k)
-                                if ((src[k] & 0x7F) == 0x7F) v[k] = 0x7FFFFFFFu;
-                        }
-                    }
-                }
-                if (row.token >= 0) {
-                    float x[32];
-#pragma unroll
-                    for (int k = 0; k < 32; ++k) x[k] = whole ? (l != 0.f ? __uint_as_float(v[k]) * inv : 0.f) : __uint_as_float(v[k]);
-                    if (whole) store_row32((T*)p.o.data + row.token * p.o.token_stride + row.head * p.o.head_stride + c, x);
-                    else store_row32(p.part + slot * D + c, x);
-                }
-            }
-            tc_fence_before();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(smem_u32(&sh->o_empty[qt]));
-            if (row.token >= 0) {
-                if (!whole) p.part_ml[slot] = make_float2(m, l);
-                else if (p.lse) p.lse[(int64_t)row.token * p.q_heads + row.head] = lse_of(m, l, TILE_SHIFT);
-            }
-            if (w.starts && !w.ends && threadIdx.x == 0) p.join[blockIdx.x] = {w.parts, w.first * p.group + w.row0, w.nrows, w.h * p.group};
-            release(g);
-            row = nrow;
         }
     } else if (warp == 17) {
         // ------------------------------------------------------------------------------------------ coming tiles
@@ -640,12 +681,14 @@ __global__ void __launch_bounds__(TILE_THREADS, 1) kv_attend_tile_kernel(const A
             __syncwarp();
             ++seg;
         };
-        begin();
+        bool fresh = true;
         for (bool more = true; ok && more;) {
             int t0 = 0, lo = 0, hi = 0, b = 0, h = 0;
             bool live = false, edge = false;
 #pragma unroll 1
             for (int i = 0; i < 4; ++i) {
+                if (fresh && ok) begin();
+                fresh = false;
                 if (i == k) {
                     live = left > 0;
                     t0 = w.t.base + unit * TILE_UNIT;
@@ -656,7 +699,7 @@ __global__ void __launch_bounds__(TILE_THREADS, 1) kv_attend_tile_kernel(const A
                     ++unit;
                     if (--left == 0) {
                         w.next(p);
-                        if (ok) begin();
+                        fresh = true;
                     }
                 } else {
                     more = false;                                               // the tile after the last is marked as none
