@@ -63,7 +63,7 @@ __device__ __forceinline__ void row_power(float most, float& down, float& up) {
 struct StepWalk {
     int u, u1;               // next unit, end of the share
     int64_t total, blocks;   // units of the whole list, blocks that share it
-    int b, idx, items;       // sequence, item in it (row block fastest), items of the sequence
+    int b, h, rb, rbs;       // sequence, kv head, row block, row blocks of the sequence (an item: row blocks fastest)
     int unit, units;         // next unit of the item, its units
     int lo, hi, base;        // cached tokens that any row of the sequence sees; first token of unit 0
     Seq s;
@@ -80,7 +80,9 @@ struct StepWalk {
         items = (int)(((int64_t)s.n * p.group + rows_per_item - 1) / rows_per_item) * p.c.kv_heads;
     }
     __device__ __forceinline__ void enter(const AttendParams& p, int rows_per_item) {
+        int items;
         measure(p, rows_per_item, s, items, units, lo, hi);
+        rbs = items / p.c.kv_heads;
         base = lo / STEP_UNIT * STEP_UNIT;
     }
     __device__ __forceinline__ bool done() const { return u >= u1; }
@@ -88,13 +90,15 @@ struct StepWalk {
         if (++u >= u1) return;
         if (++unit < units) return;
         unit = 0;
-        if (++idx < items) return;
-        idx = 0;
+        if (++rb < rbs) return;
+        rb = 0;
+        if (++h < p.c.kv_heads) return;
+        h = 0;
         do {
             if (++b >= p.bt.batch) { u1 = u; return; }      // (only if the arrays changed under the kernel)
             s = load_seq(p.bt, p.c.page_tokens, b, nullptr);
             enter(p, rows_per_item);
-        } while (items == 0);
+        } while (rbs == 0);
     }
 };
 
@@ -115,7 +119,7 @@ __device__ __forceinline__ StepWalk step_share(const AttendParams& p, int rows_p
         w.u = (int)(total * blockIdx.x / w.blocks);
         w.u1 = (int)(total * (blockIdx.x + 1) / w.blocks);
     }
-    w.b = w.idx = w.items = w.unit = w.units = w.lo = w.hi = w.base = 0;
+    w.b = w.h = w.rb = w.rbs = w.unit = w.units = w.lo = w.hi = w.base = 0;
     w.s = {0, 0, 0};
     if (w.done()) return w;
     int before = 0;
@@ -130,8 +134,9 @@ __device__ __forceinline__ StepWalk step_share(const AttendParams& p, int rows_p
             const int at = w.u - __shfl_sync(0xffffffffu, upto - mine, who);
             w.s = load_seq(p.bt, p.c.page_tokens, w.b, nullptr);
             w.enter(p, rows_per_item);
-            w.idx = at / w.units;
             w.unit = at % w.units;
+            w.rb = at / w.units % w.rbs;
+            w.h = at / w.units / w.rbs;
             return w;
         }
         before = __shfl_sync(0xffffffffu, upto, 31);
@@ -152,7 +157,7 @@ __global__ void __launch_bounds__(32 * STEP_WARPS, 2) kv_attend_step_kernel(cons
     int2* pages = reinterpret_cast<int2*>(smem + S::RING + S::MERGE + STEP_WARPS * S::STAGES * 8) + warp * S::STAGES;
     float4* scales = reinterpret_cast<float4*>(smem + S::RING + S::MERGE + STEP_WARPS * S::STAGES * 16) + warp * S::STAGES;
     float2* stats = reinterpret_cast<float2*>(smem + S::RING + S::MERGE + STEP_WARPS * S::STAGES * 32);     // [warp][16]
-    const int P = p.c.page_tokens, H = p.c.kv_heads;
+    const int P = p.c.page_tokens, H = p.c.kv_heads, pshift = 31 - __clz(P);
 
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     if (lane == 0) {
@@ -166,16 +171,17 @@ __global__ void __launch_bounds__(32 * STEP_WARPS, 2) kv_attend_step_kernel(cons
 
     // ---- producer side of this warp: the same walk, ahead by up to STAGES tiles
     StepWalk f = w;
-    int f_page = -1;             // lanes 0 and 1: page of the halves of the tile f stands on (-1: not to be read)
+    int f_page = -2;             // lanes 0 and 1: page of the halves of the tile f stands on, as the table says (-2: not to be read)
     float f_scale = 0.f;         // lanes 0 .. 3: scales of the tile issued last, still to be left in its stage
     int issued = 0;
     auto seek = [&]() {          // moves f to the next unit in which this warp has tokens to read, and asks for its pages
         while (!f.done()) {
             const int t0 = f.base + f.unit * STEP_UNIT + warp * STEP_TILE;
             if (t0 < f.hi && t0 + STEP_TILE > f.lo) {
-                f_page = -1;
+                f_page = -2;
                 const int th = P < 32 ? t0 + lane * 16 : t0;
-                if (lane < 2 && (P >= 32 || (th < f.hi && th + 16 > f.lo))) f_page = load_page(p.bt, p.c, f.b, th / P, p.status);
+                if (lane < 2 && (P >= 32 || (th < f.hi && th + 16 > f.lo)))
+                    f_page = __ldg(p.bt.page_table + (size_t)f.b * p.bt.max_pages + (th >> pshift));     // (looked at when the tile is issued)
                 return;
             }
             f.next(p, ROWS);
@@ -186,8 +192,12 @@ __global__ void __launch_bounds__(32 * STEP_WARPS, 2) kv_attend_step_kernel(cons
     };
     auto issue = [&]() {
         if (f.done()) return;
+        if ((unsigned)f_page >= (unsigned)p.c.pages) {
+            if (f_page != -2) report(p.status, CCV3D_TOKENS_BAD_PAGE);
+            f_page = -1;
+        }
         const int pg0 = __shfl_sync(0xffffffffu, f_page, 0), pg1 = __shfl_sync(0xffffffffu, f_page, 1);
-        const int st = issued % S::STAGES, items_per_head = f.items / H, h = f.idx / items_per_head;
+        const int st = issued % S::STAGES, h = f.h;
         const int t0 = f.base + f.unit * STEP_UNIT + warp * STEP_TILE;
         if (lane < 4) {
             const int pg = lane < 2 ? pg0 : pg1;
@@ -201,12 +211,12 @@ __global__ void __launch_bounds__(32 * STEP_WARPS, 2) kv_attend_step_kernel(cons
             const bool second = P < 32 && pg1 >= 0;
             mbar_expect_tx(bar, ((pg0 >= 0 ? 1u : 0u) + (second ? 1u : 0u)) * 2u * box * D);
             if (pg0 >= 0) {
-                const int row = (pg0 * 2 * H + h) * P + t0 % P;
+                const int row = (pg0 * 2 * H + h) * P + (t0 & (P - 1));
                 tma_load_2d(dst, &tm, bar, 0, row);
                 tma_load_2d(dst + S::HALF, &tm, bar, 0, row + H * P);
             }
             if (second) {
-                const int row = (pg1 * 2 * H + h) * P + (t0 + 16) % P;
+                const int row = (pg1 * 2 * H + h) * P + ((t0 + 16) & (P - 1));
                 tma_load_2d(dst + 16 * D, &tm, bar, 0, row);
                 tma_load_2d(dst + S::HALF + 16 * D, &tm, bar, 0, row + H * P);
             }
@@ -228,7 +238,7 @@ __global__ void __launch_bounds__(32 * STEP_WARPS, 2) kv_attend_step_kernel(cons
     int used = 0;
     while (!w.done()) {
         // ---- an item (or this block's share of it)
-        const int per_head = w.items / H, h = w.idx / per_head, row0 = w.idx % per_head * ROWS;
+        const int h = w.h, row0 = w.rb * ROWS;
         const Seq s = w.s;
         const int nrows = min(ROWS, s.n * p.group - row0);
         const int unit0 = w.unit, units = w.units, item_u = w.u - w.unit;        // the item's first unit in the whole list
@@ -482,8 +492,8 @@ __global__ void __launch_bounds__(32 * STEP_WARPS, 2) kv_attend_step_kernel(cons
             }
             ++used;
             __syncwarp();                                                        // the stage has been read
+            leave_scales();                                                      // (of the tile before: they have had a tile's time)
             issue();
-            leave_scales();
             __syncwarp();
         }
 
