@@ -12,8 +12,9 @@
 
 namespace ccv3d {
 
+constexpr int STEP_BLOCKS = 2;
 constexpr int STEP_WARPS = 4, STEP_TILE = 32, STEP_UNIT = STEP_WARPS * STEP_TILE;
-constexpr float STEP_SHIFT = 14.f;           // weights up to 2^14
+constexpr float STEP_SHIFT = 8.f, STEP_TOP = 15.f;           // weights start at 2^8 for the maximum and may reach 2^15
 
 template <int D> struct StepShape {
     static constexpr int STAGES = D == 128 ? 3 : 6;
@@ -146,7 +147,7 @@ __device__ __forceinline__ StepWalk step_share(const AttendParams& p, int rows_p
 }
 
 template <typename T, int D, int NT>
-__global__ void __launch_bounds__(32 * STEP_WARPS, 2) kv_attend_step_kernel(const __grid_constant__ CUtensorMap tm, const AttendParams p) {
+__global__ void __launch_bounds__(32 * STEP_WARPS, NT == 1 ? STEP_BLOCKS : 2) kv_attend_step_kernel(const __grid_constant__ CUtensorMap tm, const AttendParams p) {
     using S = StepShape<D>;
     constexpr int TERMS = sizeof(T) == 4 ? 2 : 1, ROWS = 8 * NT, CH = D / 64;     // CH: 16-byte pieces of a row for a thread
     extern __shared__ __align__(1024) uint8_t smem[];
@@ -328,41 +329,55 @@ __global__ void __launch_bounds__(32 * STEP_WARPS, 2) kv_attend_step_kernel(cons
 #pragma unroll
                 for (int e = 0; e < 2; ++e) whole = whole && (8 * i + 2 * c4 + e >= nrows || (t0 >= clo[i][e] && t0 + STEP_TILE <= chi[i][e]));
             whole = __all_sync(0xffffffffu, whole);
-            float x[NT][2][4];
+            // scores of 2 x 16 tokens; even and odd steps of the contraction in sums of their own, so that four (NT = 1)
+            // products are on their way at a time
+            float x[NT][2][4], y[NT][2][4];
 #pragma unroll
-            for (int j = 0; j < 2; ++j) {                                        // 16 tokens each: scores
+            for (int i = 0; i < NT; ++i)
 #pragma unroll
-                for (int i = 0; i < NT; ++i) x[i][j][0] = x[i][j][1] = x[i][j][2] = x[i][j][3] = 0.f;
+                for (int j = 0; j < 2; ++j)
 #pragma unroll
-                for (int g = 0; g < CH; ++g) {
-                    uint4 a[2];
+                    for (int e = 0; e < 4; ++e) x[i][j][e] = y[i][j][e] = 0.f;
+#pragma unroll
+            for (int g = 0; g < CH; ++g) {
+                uint4 a[2][2];
+#pragma unroll
+                for (int j = 0; j < 2; ++j)
 #pragma unroll
                     for (int e = 0; e < 2; ++e) {
                         const int row = 16 * j + 8 * e + r8, piece = c4 * CH + g;
                         const int sw = D == 128 ? (piece ^ (row & 7)) : (piece ^ ((row >> 1) & 3));
-                        a[e] = *reinterpret_cast<const uint4*>(ks + row * D + sw * 16);
+                        a[j][e] = *reinterpret_cast<const uint4*>(ks + row * D + sw * 16);
                     }
-                    const uint32_t a0[4] = {a[0].x, a[0].y, a[0].z, a[0].w}, a1[4] = {a[1].x, a[1].y, a[1].z, a[1].w};
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) {
-                        const uint32_t af[4] = {e4m3x2_to_half2(a0[k] & 0xFFFFu), e4m3x2_to_half2(a1[k] & 0xFFFFu),
-                                                e4m3x2_to_half2(a0[k] >> 16), e4m3x2_to_half2(a1[k] >> 16)};
+                for (int k = 0; k < 4; ++k)
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) {
+                        const uint32_t a0 = k == 0 ? a[j][0].x : k == 1 ? a[j][0].y : k == 2 ? a[j][0].z : a[j][0].w;
+                        const uint32_t a1 = k == 0 ? a[j][1].x : k == 1 ? a[j][1].y : k == 2 ? a[j][1].z : a[j][1].w;
+                        const uint32_t af[4] = {e4m3x2_to_half2(a0 & 0xFFFFu), e4m3x2_to_half2(a1 & 0xFFFFu), e4m3x2_to_half2(a0 >> 16), e4m3x2_to_half2(a1 >> 16)};
 #pragma unroll
                         for (int i = 0; i < NT; ++i)
 #pragma unroll
-                            for (int t = 0; t < TERMS; ++t) mma_f16(x[i][j], af, qf[i][t][g][2 * k], qf[i][t][g][2 * k + 1]);
+                            for (int t = 0; t < TERMS; ++t) mma_f16((k + t) & 1 ? y[i][j] : x[i][j], af, qf[i][t][g][2 * k], qf[i][t][g][2 * k + 1]);
                     }
-                }
             }
+#pragma unroll
+            for (int i = 0; i < NT; ++i)
+#pragma unroll
+                for (int j = 0; j < 2; ++j)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) x[i][j][e] += y[i][j][e];
             // ---- softmax: x[i][j] holds tokens 16 j + r8 (elements 0, 1) and 16 j + 8 + r8 (2, 3) of columns 2 c4, 2 c4 + 1
             float ev[2], iv[2];
             scale_terms(sc.y, ev[0], iv[0]);
             scale_terms(sc.w, ev[1], iv[1]);
             const float kf[2] = {sc.x, sc.z};
-            uint32_t pf[NT][TERMS][2][2];                                        // weights, tokens down the contraction
+            // The maximum is that of earlier tiles until a score passes it by more than the weights can hold (2^7): then it
+            // moves, by a whole power of two, for all rows.  Most tiles so need no maximum over the lanes.
+            bool raise = false;
 #pragma unroll
-            for (int i = 0; i < NT; ++i) {
-                float mx[2] = {-INFINITY, -INFINITY};
+            for (int i = 0; i < NT; ++i)
 #pragma unroll
                 for (int j = 0; j < 2; ++j)
 #pragma unroll
@@ -373,27 +388,35 @@ __global__ void __launch_bounds__(32 * STEP_WARPS, 2) kv_attend_step_kernel(cons
                             if (t < clo[i][e & 1] || t >= chi[i][e & 1] || (j ? pg.y : pg.x) < 0) v = -INFINITY;
                         }
                         x[i][j][e] = v;
-                        mx[e & 1] = fmaxf(mx[e & 1], v);
+                        raise = raise || v > m[i][e & 1] + (STEP_TOP - STEP_SHIFT);
                     }
+            if (__any_sync(0xffffffffu, raise)) {
 #pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                    mx[e] = fmaxf(mx[e], __shfl_xor_sync(0xffffffffu, mx[e], 4));
-                    mx[e] = fmaxf(mx[e], __shfl_xor_sync(0xffffffffu, mx[e], 8));
-                    mx[e] = fmaxf(mx[e], __shfl_xor_sync(0xffffffffu, mx[e], 16));
-                    mx[e] = fmaxf(mx[e], m[i][e]);
-                    const float corr = m[i][e] == -INFINITY ? 0.f : exp2_fast(m[i][e] - mx[e]);
-                    m[i][e] = mx[e];
-                    l[i][e] *= corr;
+                for (int i = 0; i < NT; ++i)
 #pragma unroll
-                    for (int k = 0; k < D / 16; ++k) { o[i][k][e] *= corr; o[i][k][e + 2] *= corr; }
-                    mx[e] = (mx[e] == -INFINITY ? 0.f : mx[e]) - STEP_SHIFT;
-                }
+                    for (int e = 0; e < 2; ++e) {
+                        float mx = fmaxf(fmaxf(x[i][0][e], x[i][0][e + 2]), fmaxf(x[i][1][e], x[i][1][e + 2]));
+                        mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 4));
+                        mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 8));
+                        mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 16));
+                        mx = fmaxf(m[i][e], ceilf(mx));
+                        const float corr = m[i][e] == -INFINITY ? 0.f : exp2_fast(m[i][e] - mx);
+                        m[i][e] = mx;
+                        l[i][e] *= corr;
+#pragma unroll
+                        for (int k = 0; k < D / 16; ++k) { o[i][k][e] *= corr; o[i][k][e + 2] *= corr; }
+                    }
+            }
+            uint32_t pf[NT][TERMS][2][2];                                        // weights, tokens down the contraction
+#pragma unroll
+            for (int i = 0; i < NT; ++i) {
+                const float m_use[2] = {(m[i][0] == -INFINITY ? 0.f : m[i][0]) - STEP_SHIFT, (m[i][1] == -INFINITY ? 0.f : m[i][1]) - STEP_SHIFT};
 #pragma unroll
                 for (int j = 0; j < 2; ++j) {
                     float w4[4];
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
-                        w4[e] = exp2_fast(x[i][j][e] - mx[e & 1]);
+                        w4[e] = exp2_fast(x[i][j][e] - m_use[e & 1]);
                         l[i][e & 1] = fmaf(w4[e], iv[j], l[i][e & 1]);
                     }
                     const uint32_t a = pack_half(w4[0], w4[1]), b = pack_half(w4[2], w4[3]);
