@@ -219,7 +219,8 @@ ccv3d_status plan_attend(const ccv3d_kv_cache* cache, const ccv3d_token_batch* b
     const int64_t rows = (int64_t)batch->max_new * (q_heads / cache->kv_heads);
     pl->rows_per_item = rows <= 8 ? 8 : rows <= 64 ? 16 : dtype == CCV3D_BF16 ? 256 : 128;
     const bool tile = pl->rows_per_item >= 128;
-    pl->blocks = tile ? pl->dev.sm_count : 2 * pl->dev.sm_count;
+    pl->blocks = tile ? pl->dev.sm_count : (pl->rows_per_item == 8 ? STEP_BLOCKS : 2) * pl->dev.sm_count;
+    if (pl->blocks > JOIN_PARTS) pl->blocks = JOIN_PARTS;
     pl->slot_rows = tile ? pl->rows_per_item : 16;
     pl->ml_at = (uint64_t)2 * pl->blocks * pl->slot_rows * cache->head_dim * 4;
     pl->join_at = pl->ml_at + (uint64_t)2 * pl->blocks * pl->slot_rows * sizeof(float2);
@@ -269,8 +270,8 @@ ccv3d_status launch_join(const AttendParams& p, const Plan& pl, float shift, cud
     at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     at[0].val.programmaticStreamSerializationAllowed = 1;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(pl.blocks, (pl.slot_rows + 3) / 4);
-    cfg.blockDim = dim3(D);
+    cfg.gridDim = dim3(pl.blocks, pl.slot_rows <= 16 ? pl.rows_per_item : 64);
+    cfg.blockDim = dim3(JOIN_THREADS);
     cfg.stream = st;
     cfg.attrs = at;
     cfg.numAttrs = 1;

@@ -69,33 +69,93 @@ __device__ __forceinline__ float lse_of(float m, float l, float shift) {
     return l != 0.f ? (m - shift + log2f(l)) * LN2 : -INFINITY;     // (a row that saw NaN has l = NaN)
 }
 
-// One block for each block of the attention kernel and stretch of 4 rows: adds the parts of the item that starts there.
+// Adds the parts of the item that starts in block blockIdx.x of the attention kernel, rows blockIdx.y, + gridDim.y, ...
+// Few parts (a tile of rows that two blocks share): D / 4 threads to a row, part after part.  But an item can have as many
+// parts as there were blocks (one stream behind a long cache): then a row's parts are spread over all threads, their maxima
+// and weights a part to a thread, their sums D / 4 threads to a part.
+constexpr int JOIN_THREADS = 128, JOIN_PARTS = 1024, JOIN_FEW = 8;
 template <typename T, int D>
-__global__ void __launch_bounds__(D) attend_join_kernel(const AttendParams p, float shift) {
+__global__ void __launch_bounds__(JOIN_THREADS) attend_join_kernel(const AttendParams p, float shift) {
+    constexpr int L = D / 4, SLICES = JOIN_THREADS / L;
+    __shared__ float weight[JOIN_PARTS], red[2][JOIN_THREADS / 32];
+    __shared__ float4 sums[JOIN_THREADS];
     asm volatile("griddepcontrol.wait;" ::: "memory");
     const Join j = p.join[blockIdx.x];
-    const int r = blockIdx.y * 4 + (int)threadIdx.x / (D / 4), d = (int)threadIdx.x % (D / 4) * 4;
-    if (r >= j.rows || j.parts == 0) return;
+    if (j.parts == 0) return;
+    const int tid = threadIdx.x, slice = tid / L, d = tid % L * 4;
     const int64_t slot0 = 2 * (int64_t)blockIdx.x;                  // part i > 0 lies in slot0 + 2 i, part 0 in slot0 + 1
-    float m = -INFINITY;
-    for (int i = 0; i < j.parts; ++i) m = fmaxf(m, p.part_ml[(slot0 + (i ? 2 * i : 1)) * p.slot_rows + r].x);
-    float l = 0.f, acc[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 4
-    for (int i = 0; i < j.parts; ++i) {
-        const int64_t at = (slot0 + (i ? 2 * i : 1)) * p.slot_rows + r;
-        const float2 ml = p.part_ml[at];
-        const float4 v = *reinterpret_cast<const float4*>(p.part + at * D + d);
-        const float w = ml.x == -INFINITY ? 0.f : exp2_fast(ml.x - m);
-        l = fmaf(w, ml.y, l);
-        acc[0] = fmaf(w, v.x, acc[0]); acc[1] = fmaf(w, v.y, acc[1]);
-        acc[2] = fmaf(w, v.z, acc[2]); acc[3] = fmaf(w, v.w, acc[3]);
-    }
-    const float inv = l != 0.f ? 1.f / l : 0.f;
+    auto finish = [&](int r, float m, float l, float (&acc)[4]) {
+        const float inv = l != 0.f ? 1.f / l : 0.f;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) acc[i] = l != 0.f ? acc[i] * inv : 0.f;
-    const int token = (j.row0 + r) / p.group, head = j.head0 + (j.row0 + r) % p.group;
-    store_out<T>(p, token, head, d, acc);
-    if (d == 0 && p.lse) p.lse[(int64_t)token * p.q_heads + head] = lse_of(m, l, shift);
+        for (int i = 0; i < 4; ++i) acc[i] = l != 0.f ? acc[i] * inv : 0.f;
+        const int token = (j.row0 + r) / p.group, head = j.head0 + (j.row0 + r) % p.group;
+        store_out<T>(p, token, head, d, acc);
+        if (d == 0 && p.lse) p.lse[(int64_t)token * p.q_heads + head] = lse_of(m, l, shift);
+    };
+    if (j.parts <= JOIN_FEW) {
+        for (int r = blockIdx.y * SLICES + slice; r < j.rows; r += gridDim.y * SLICES) {
+            float m = -INFINITY, l = 0.f, acc[4] = {0.f, 0.f, 0.f, 0.f};
+            float2 ml[JOIN_FEW];
+#pragma unroll
+            for (int i = 0; i < JOIN_FEW; ++i)
+                if (i < j.parts) {
+                    ml[i] = p.part_ml[(slot0 + (i ? 2 * i : 1)) * p.slot_rows + r];
+                    m = fmaxf(m, ml[i].x);
+                }
+#pragma unroll
+            for (int i = 0; i < JOIN_FEW; ++i)
+                if (i < j.parts) {
+                    const float4 v = *reinterpret_cast<const float4*>(p.part + ((slot0 + (i ? 2 * i : 1)) * p.slot_rows + r) * D + d);
+                    const float w = ml[i].x == -INFINITY ? 0.f : exp2_fast(ml[i].x - m);
+                    l = fmaf(w, ml[i].y, l);
+                    acc[0] = fmaf(w, v.x, acc[0]); acc[1] = fmaf(w, v.y, acc[1]);
+                    acc[2] = fmaf(w, v.z, acc[2]); acc[3] = fmaf(w, v.w, acc[3]);
+                }
+            finish(r, m, l, acc);
+        }
+        return;
+    }
+    for (int r = blockIdx.y; r < j.rows; r += gridDim.y) {
+        auto at = [&](int i) { return (slot0 + (i ? 2 * i : 1)) * p.slot_rows + r; };
+        float m = -INFINITY;
+        for (int i = tid; i < j.parts; i += JOIN_THREADS) m = fmaxf(m, p.part_ml[at(i)].x);
+        m = warp_max(m);
+        if ((tid & 31) == 0) red[0][tid >> 5] = m;
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < JOIN_THREADS / 32; ++k) m = fmaxf(m, red[0][k]);
+        float l = 0.f;
+        for (int i = tid; i < j.parts; i += JOIN_THREADS) {
+            const float2 ml = p.part_ml[at(i)];
+            const float w = ml.x == -INFINITY ? 0.f : exp2_fast(ml.x - m);
+            weight[i] = w;
+            l = fmaf(w, ml.y, l);
+        }
+        l = warp_sum(l);
+        if ((tid & 31) == 0) red[1][tid >> 5] = l;
+        __syncthreads();
+        l = 0.f;
+#pragma unroll
+        for (int k = 0; k < JOIN_THREADS / 32; ++k) l += red[1][k];
+        float acc[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 8
+        for (int i = slice; i < j.parts; i += SLICES) {
+            const float4 v = *reinterpret_cast<const float4*>(p.part + at(i) * D + d);
+            const float w = weight[i];
+            acc[0] = fmaf(w, v.x, acc[0]); acc[1] = fmaf(w, v.y, acc[1]);
+            acc[2] = fmaf(w, v.z, acc[2]); acc[3] = fmaf(w, v.w, acc[3]);
+        }
+        sums[tid] = make_float4(acc[0], acc[1], acc[2], acc[3]);
+        __syncthreads();
+        if (slice == 0) {
+#pragma unroll
+            for (int k = 1; k < SLICES; ++k) {
+                const float4 v = sums[k * L + tid];
+                acc[0] += v.x; acc[1] += v.y; acc[2] += v.z; acc[3] += v.w;
+            }
+            finish(r, m, l, acc);
+        }
+    }
 }
 
 }  // namespace ccv3d

@@ -12,15 +12,15 @@
 
 namespace ccv3d {
 
-constexpr int STEP_BLOCKS = 2;
+constexpr int STEP_BLOCKS = 3;               // resident on an SM
 constexpr int STEP_WARPS = 4, STEP_TILE = 32, STEP_UNIT = STEP_WARPS * STEP_TILE;
 constexpr float STEP_SHIFT = 8.f, STEP_TOP = 15.f;           // weights start at 2^8 for the maximum and may reach 2^15
 
 template <int D> struct StepShape {
-    static constexpr int STAGES = D == 128 ? 3 : 6;
+    static constexpr int STAGES = D == 128 ? 2 : 4;
     static constexpr uint32_t HALF = STEP_TILE * D, STAGE = 2 * HALF;             // keys, then values
     static constexpr uint32_t RING = STEP_WARPS * STAGES * STAGE;
-    static constexpr uint32_t MERGE = (STEP_WARPS - 1) * 8 * D * 4;               // sums of 8 rows of three warps
+    static constexpr uint32_t MERGE = STEP_WARPS / 2 * 8 * D * 4;                 // sums of 8 rows of two warps
     static constexpr uint32_t BYTES = RING + MERGE + STEP_WARPS * (STAGES * (8 + 8 + 16) + 16 * 8) + 64;
 };
 
@@ -556,20 +556,25 @@ __global__ void __launch_bounds__(32 * STEP_WARPS, NT == 1 ? STEP_BLOCKS : 2) kv
             for (int k = 0; k < D / 16; ++k)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) o[i][k][e] *= f2[e & 1];
-            if (warp > 0) {
+            // warps 2 and 3 to 0 and 1, then 1 to 0
 #pragma unroll
-                for (int k = 0; k < D / 16; ++k)
-                    *reinterpret_cast<float4*>(merge + (((warp - 1) * (D / 16) + k) * 32 + lane) * 4) = make_float4(o[i][k][0], o[i][k][1], o[i][k][2], o[i][k][3]);
-            }
-            __syncthreads();
-            if (warp == 0) {
+            for (int half = STEP_WARPS / 2; half; half >>= 1) {
+                if (warp >= half && warp < 2 * half) {
 #pragma unroll
-                for (int k = 0; k < D / 16; ++k)
+                    for (int k = 0; k < D / 16; ++k)
+                        *reinterpret_cast<float4*>(merge + (((warp - half) * (D / 16) + k) * 32 + lane) * 4) = make_float4(o[i][k][0], o[i][k][1], o[i][k][2], o[i][k][3]);
+                }
+                __syncthreads();
+                if (warp < half) {
 #pragma unroll
-                    for (int j = 0; j < STEP_WARPS - 1; ++j) {
-                        const float4 t = *reinterpret_cast<const float4*>(merge + ((j * (D / 16) + k) * 32 + lane) * 4);
+                    for (int k = 0; k < D / 16; ++k) {
+                        const float4 t = *reinterpret_cast<const float4*>(merge + ((warp * (D / 16) + k) * 32 + lane) * 4);
                         o[i][k][0] += t.x; o[i][k][1] += t.y; o[i][k][2] += t.z; o[i][k][3] += t.w;
                     }
+                }
+                if (half > 1) __syncthreads();
+            }
+            if (warp == 0) {
                 // this thread: channels r8 * D / 8 + 2 k (elements 0, 1) and + 1 (2, 3) of columns 2 c4, 2 c4 + 1
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
