@@ -117,13 +117,24 @@ ccv3d_status launch_append_as(AppendParams& p, cudaStream_t st) {
     const int64_t by_tokens = (int64_t)p.bt.tokens / P + 2LL * p.bt.batch;
     const int64_t by_batch = (int64_t)p.bt.batch * (p.bt.max_new <= 1 ? 1 : (p.bt.max_new - 1) / P + 2);
     const bool one = p.bt.max_new <= 1;            // (then a block's number names its sequence)
-    const int64_t kv = (one || by_batch < by_tokens ? by_batch : by_tokens) * 2 * p.c.kv_heads;
+    const int64_t kv = (one || by_batch < by_tokens ? by_batch : by_tokens) * p.c.kv_heads;
     const int64_t items = p.q.data ? (int64_t)p.bt.tokens * ((p.q_heads + QUERY_HEADS - 1) / QUERY_HEADS) : 0;
-    const int64_t all = kv + (items + S::TPI - 1) / S::TPI;
-    if (all > 0x7FFFFFFF) return CCV3D_ERR_UNSUPPORTED;
-    p.kv_blocks = (unsigned)kv;
-    kv_append_kernel<T, D, P, FEW><<<(unsigned)all, S::THREADS, 0, st>>>(p);
-    return launched();
+    const int64_t q_blocks = ((items + S::TPI - 1) / S::TPI + S::CLUSTER - 1) / S::CLUSTER * S::CLUSTER;
+    const int64_t all = kv * S::CLUSTER + q_blocks;
+    if (all > 0x7FFFFFFF || items > 0xF0000000LL) return CCV3D_ERR_UNSUPPORTED;
+    p.kv_blocks = (unsigned)(kv * S::CLUSTER);
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeClusterDimension;
+    at[0].val.clusterDim.x = S::CLUSTER;
+    at[0].val.clusterDim.y = at[0].val.clusterDim.z = 1;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)all);
+    cfg.blockDim = dim3(S::THREADS);
+    cfg.stream = st;
+    cfg.attrs = at;
+    cfg.numAttrs = S::CLUSTER > 1 ? 1 : 0;
+    if (cudaLaunchKernelEx(&cfg, kv_append_kernel<T, D, P, FEW>, p) != cudaSuccess) { cudaGetLastError(); return CCV3D_ERR_CUDA; }
+    return CCV3D_OK;
 }
 
 template <typename T>

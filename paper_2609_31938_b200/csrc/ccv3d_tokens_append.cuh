@@ -1,12 +1,16 @@
 // Append to the paged E4M3 cache, with the position rotation of keys (and queries) on the way.
 //
 // Bound by HBM where there are many tokens, by the chain of dependent loads (sequence, page, position, table) where there
-// are few.  A block owns one (page, keys or values, head): it holds the page's new tokens in registers, takes
-// the largest magnitude over all of them, settles the page's scale (the smallest power of two under which everything fits
-// into +-448, at least the old one where older tokens stay), moves older codes to it where it grew, and writes the new
-// codes.  The blocks behind those rotate the queries, four heads of a token for each group of lanes that spans a head, so
-// that a token's cosines and sines are fetched once for them and their loads are on their way together.
+// are few.  A block owns the keys and values of one (page, head), or a cluster of 2 or 4 blocks does where the page's tokens are
+// more than four rounds of a block: it holds the page's new tokens in registers, takes the largest magnitude over all of them
+// (over the cluster through its shared memory), settles the page's scale (the smallest power of two under which
+// everything fits into +-448, at least the old one where older tokens stay), moves older codes to it where it grew, and
+// writes the new codes.  Every input is read once.  (A page of 128 tokens and 128 channels in one block: 1024 threads or 16
+// rounds, either way one block to an SM: 39 us for a frame of 3520 tokens and 12 heads; read twice, 42.)
+// The blocks behind those rotate the queries, four heads of a token for each group of lanes that spans a head, so that a
+// token's cosines and sines are fetched once for them and their loads are on their way together.
 #pragma once
+#include "ccv3d_tc_ptx.cuh"
 #include "ccv3d_tokens_common.cuh"
 
 namespace ccv3d {
@@ -21,12 +25,13 @@ struct AppendParams {
     uint32_t* status;
 };
 
-// Threads of a block: four rounds cover a page's new tokens, more rounds cost the registers that keep several blocks on an
-// SM (one to a block of 256 threads at 16 rounds); `few`: no sequence brings more tokens than one round of 128 threads takes.
+// `few`: no sequence brings more tokens than one round of 128 threads takes.
 template <int D, int P, bool FEW> struct AppendShape {
-    static constexpr int LPT = D / 4, WHOLE = P * LPT / 4;       // lanes for one token
-    static constexpr int THREADS = FEW || WHOLE < 128 ? 128 : WHOLE;
-    static constexpr int TPI = THREADS / LPT, R = FEW ? 1 : (P + TPI - 1) / TPI;      // tokens at a time, rounds
+    static constexpr int LPT = D / 4, THREADS = FEW ? 128 : 256;               // lanes for one token
+    static constexpr int TPI = THREADS / LPT;                                   // tokens at a time
+    static constexpr int CLUSTER = FEW || P <= 4 * TPI ? 1 : P / (4 * TPI);     // blocks for a page
+    static constexpr int SHARE = P / CLUSTER;                                   // a block's tokens of a page
+    static constexpr int R = FEW ? 1 : (SHARE + TPI - 1) / TPI;                 // rounds
 };
 constexpr int MIN_SCALE_EXP = -64;
 constexpr int QUERY_HEADS = 4;
@@ -102,16 +107,16 @@ __device__ __forceinline__ void rotate4(const ccv3d_rotary& r, const Turn& t, in
 }
 
 template <typename T, int D, int P, bool FEW>
-__global__ void __launch_bounds__(AppendShape<D, P, FEW>::THREADS, 1024 / AppendShape<D, P, FEW>::THREADS) kv_append_kernel(const AppendParams p) {
+__global__ void __launch_bounds__(AppendShape<D, P, FEW>::THREADS, FEW ? 8 : 3) kv_append_kernel(const AppendParams p) {
     using S = AppendShape<D, P, FEW>;
     constexpr int LPT = S::LPT, TPI = S::TPI, R = S::R;
     const int tid = threadIdx.x, l = tid % LPT;
     const Turn turn = turn_of(p.rot, l);
     if (blockIdx.x >= p.kv_blocks) {                 // ---- queries: an item is a token and QUERY_HEADS heads
         const int per_token = (p.q_heads + QUERY_HEADS - 1) / QUERY_HEADS;
-        const int64_t item = (int64_t)(blockIdx.x - p.kv_blocks) * TPI + tid / LPT;
-        const bool live = item < (int64_t)p.bt.tokens * per_token;
-        const int token = live ? (int)(item / per_token) : 0, h0 = live ? (int)(item % per_token) * QUERY_HEADS : p.q_heads;
+        const uint32_t item = (blockIdx.x - p.kv_blocks) * TPI + tid / LPT, items = (uint32_t)p.bt.tokens * per_token;     // (fewer than 2^32: checked)
+        const bool live = item < items;
+        const int token = live ? item / per_token : 0, h0 = live ? item % per_token * QUERY_HEADS : p.q_heads;
         const int row = live && turn.one ? table_row(p.rot, token, turn.axis, p.status) : 0;
         float v[QUERY_HEADS][4];
 #pragma unroll
@@ -128,11 +133,12 @@ __global__ void __launch_bounds__(AppendShape<D, P, FEW>::THREADS, 1024 / Append
             if (h0 + h < p.q_heads) store4((T*)p.qo.data + token * p.qo.token_stride + (h0 + h) * p.qo.head_stride + 4 * l, v[h]);
         return;
     }
-    // ---- keys and values: block -> (page of a sequence, keys or values, head)
+    // ---- keys and values: block -> (page of a sequence, head), rank in the cluster
     __shared__ int unit_seq, unit_page;
-    __shared__ float part[S::THREADS / 32];
+    __shared__ Seq unit_at;
+    __shared__ float part[2][S::THREADS / 32], block_most[2];
     const int H = p.c.kv_heads;
-    const int unit = blockIdx.x / (2 * H), kvh = blockIdx.x % (2 * H), is_v = kvh >= H, head = is_v ? kvh - H : kvh;
+    const int rank = blockIdx.x % S::CLUSTER, block = blockIdx.x / S::CLUSTER, unit = block / H, head = block % H;
     if (p.bt.max_new <= 1) {                         // a page to each sequence at most: no search
         if (tid == 0) { unit_seq = unit; unit_page = 0; }
     } else if (tid < 32) {
@@ -141,8 +147,9 @@ __global__ void __launch_bounds__(AppendShape<D, P, FEW>::THREADS, 1024 / Append
         int base = 0;
         for (int b0 = 0; b0 < p.bt.batch; b0 += 32) {
             int pages = 0;
+            Seq s = {0, 0, 0};
             if (b0 + tid < p.bt.batch) {
-                const Seq s = load_seq(p.bt, P, b0 + tid, p.status);
+                s = load_seq(p.bt, P, b0 + tid, p.status);
                 const int n = min(s.n, s.total);     // more new tokens than cached ones: the first have no place
                 if (n < s.n) report(p.status, CCV3D_TOKENS_BAD_LENGTH);
                 if (n > 0) pages = (s.total - 1) / P - (s.total - n) / P + 1;
@@ -151,6 +158,7 @@ __global__ void __launch_bounds__(AppendShape<D, P, FEW>::THREADS, 1024 / Append
             if (pages > 0 && unit >= upto - pages && unit < upto) {
                 unit_seq = b0 + tid;
                 unit_page = unit - (upto - pages);
+                unit_at = s;
             }
             base = __shfl_sync(0xffffffffu, upto, 31);
             if (unit < base) break;
@@ -159,7 +167,7 @@ __global__ void __launch_bounds__(AppendShape<D, P, FEW>::THREADS, 1024 / Append
     __syncthreads();
     const int b = unit_seq;
     if (b < 0) return;                               // the grid is a bound
-    Seq s = load_seq(p.bt, P, b, p.bt.max_new <= 1 ? p.status : nullptr);
+    Seq s = p.bt.max_new <= 1 ? load_seq(p.bt, P, b, p.status) : unit_at;
     const int lost = max(0, s.n - s.total);
     if (p.bt.max_new <= 1 && lost) report(p.status, CCV3D_TOKENS_BAD_LENGTH);
     s.first += lost;
@@ -167,76 +175,109 @@ __global__ void __launch_bounds__(AppendShape<D, P, FEW>::THREADS, 1024 / Append
     if (s.n == 0) return;
     const int old = s.total - s.n;
     const int j = old / P + unit_page;
-    const int page = load_page(p.bt, p.c, b, j, p.status);
-    if (page < 0) return;
+    // asked for together: the page, the tokens, their positions; looked at in that order
+    int page = __ldg(p.bt.page_table + (size_t)b * p.bt.max_pages + j);
     const int t0 = max(0, old - j * P), t1 = min(P, s.total - j * P);        // the page's new tokens
-    const int row0 = s.first + (j * P + t0) - old;
-    const ccv3d_heads& src = is_v ? p.v : p.k;
-    const T* in = (const T*)src.data + head * src.head_stride + 4 * l;
-    float* at = p.c.scales + ((int64_t)page * 2 + is_v) * H + head;
-    uint8_t* codes = (uint8_t*)p.c.codes + (((int64_t)page * 2 + is_v) * H + head) * (P * D);
-    const float was = t0 > 0 ? *at : 0.f;
-    const bool turns = !is_v && p.rot.cos_table;
-    float v[R][4];
+    const int a0 = max(t0, rank * S::SHARE), a1 = min(t1, (rank + 1) * S::SHARE);        // this block's
+    const int first = s.first + (j * P + a0) - old + tid / LPT;              // this thread's token of round 0
+    const T* k_in = (const T*)p.k.data + head * p.k.head_stride + 4 * l;
+    const T* v_in = (const T*)p.v.data + head * p.v.head_stride + 4 * l;
+    float v[2][R][4];
     int row[R];
-    float most = 0.f;
 #pragma unroll
     for (int r = 0; r < R; ++r) {
-        const int t = t0 + r * TPI + tid / LPT;
-        v[r][0] = v[r][1] = v[r][2] = v[r][3] = 0.f;
         row[r] = 0;
-        if (t < t1) {
-            load4(in + (int64_t)(row0 + t - t0) * src.token_stride, v[r]);
-            if (turns && turn.one) row[r] = table_row(p.rot, row0 + t - t0, turn.axis, p.status);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[0][r][i] = v[1][r][i] = 0.f;
+        if (a0 + r * TPI + tid / LPT < a1) {
+            load4(k_in + (int64_t)(first + r * TPI) * p.k.token_stride, v[0][r]);
+            load4(v_in + (int64_t)(first + r * TPI) * p.v.token_stride, v[1][r]);
+            if (turn.one) row[r] = table_row(p.rot, first + r * TPI, turn.axis, p.status);
         }
     }
+    const bool there = (unsigned)page < (unsigned)p.c.pages;
+    if (!there) {
+        report(p.status, CCV3D_TOKENS_BAD_PAGE);
+        page = 0;
+    }
+    float* at = p.c.scales + (int64_t)page * 2 * H + head;                   // of the keys; of the values H further
+    float was[2] = {0.f, 0.f};
+    if (t0 > 0) { was[0] = at[0]; was[1] = at[H]; }
+    float most[2] = {0.f, 0.f};
 #pragma unroll
     for (int r = 0; r < R; ++r) {
-        const int t = t0 + r * TPI + tid / LPT;
-        if (turns && t0 + r * TPI < t1) {                        // (the same for the whole block)
+        if (p.rot.cos_table && a0 + r * TPI < a1) {              // (the same for the whole block)
             float c[4], s[4];
-            angles(p.rot, turn, row0 + min(t, t1 - 1) - t0, row[r], c, s, p.status);
-            rotate4<LPT>(p.rot, turn, l, c, s, v[r]);
+            angles(p.rot, turn, first + min(r * TPI, a1 - 1 - a0 - tid / LPT), row[r], c, s, p.status);
+            rotate4<LPT>(p.rot, turn, l, c, s, v[0][r]);
         }
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const float a = fabsf(v[r][i]);
-            if (t < t1 && a <= 3.402823466e38f) most = fmaxf(most, a);   // infinities and NaN stay out
-        }
+        for (int w = 0; w < 2; ++w)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float a = fabsf(v[w][r][i]);
+                if (a0 + r * TPI + tid / LPT < a1 && a <= 3.402823466e38f) most[w] = fmaxf(most[w], a);      // infinities and NaN stay out
+            }
     }
-    most = warp_max(most);
-    if ((tid & 31) == 0) part[tid >> 5] = most;
+#pragma unroll
+    for (int w = 0; w < 2; ++w) {
+        most[w] = warp_max(most[w]);
+        if ((tid & 31) == 0) part[w][tid >> 5] = most[w];
+    }
     __syncthreads();
 #pragma unroll
-    for (int i = 0; i < S::THREADS / 32; ++i) most = fmaxf(most, part[i]);
-    // smallest e with most <= 448 * 2^e = 1.75 * 2^(8 + e)
-    const uint32_t bits = __float_as_uint(most);
-    int e = (int)(bits >> 23) - 127 - 8 + ((bits & 0x7FFFFFu) > 0x600000u ? 1 : 0);
-    e = max(e, MIN_SCALE_EXP);
-    float scale = __uint_as_float((uint32_t)(e + 127) << 23);
-    if (t0 > 0) {
-        scale = fmaxf(was, scale);
-        if (scale != was) {
-            const float f = was / scale;
-            for (int i = tid; i < t0 * (D / 4); i += S::THREADS) {
-                float c[4];
-                e4m3x4_to_float(reinterpret_cast<uint32_t*>(codes)[i], c);
+    for (int w = 0; w < 2; ++w)
 #pragma unroll
-                for (int k = 0; k < 4; ++k) c[k] *= f;
-                reinterpret_cast<uint32_t*>(codes)[i] = to_e4m3x4(c);
+        for (int i = 0; i < S::THREADS / 32; ++i) most[w] = fmaxf(most[w], part[w][i]);
+    if constexpr (S::CLUSTER > 1) {
+        if (tid == 0) { block_most[0] = most[0]; block_most[1] = most[1]; }
+        cluster_sync_all();
+#pragma unroll
+        for (int k = 0; k < S::CLUSTER; ++k)
+#pragma unroll
+            for (int w = 0; w < 2; ++w) {
+                uint32_t at_k;
+                float other;
+                asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at_k) : "r"(smem_u32(&block_most[w])), "r"(k));
+                asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(other) : "r"(at_k) : "memory");
+                most[w] = fmaxf(most[w], other);
+            }
+        cluster_sync_all();                                      // (no block leaves while another still reads its maxima)
+    }
+    if (!there) return;
+#pragma unroll
+    for (int w = 0; w < 2; ++w) {
+        // smallest e with most <= 448 * 2^e = 1.75 * 2^(8 + e)
+        const uint32_t bits = __float_as_uint(most[w]);
+        int e = (int)(bits >> 23) - 127 - 8 + ((bits & 0x7FFFFFu) > 0x600000u ? 1 : 0);
+        e = max(e, MIN_SCALE_EXP);
+        float scale = __uint_as_float((uint32_t)(e + 127) << 23);
+        uint32_t* codes = reinterpret_cast<uint32_t*>((uint8_t*)p.c.codes + (((int64_t)page * 2 + w) * H + head) * (P * D));
+        if (t0 > 0) {
+            scale = fmaxf(was[w], scale);
+            if (scale != was[w]) {
+                const float f = was[w] / scale;
+                for (int i = rank * S::THREADS + tid; i < t0 * (D / 4); i += S::CLUSTER * S::THREADS) {
+                    float c[4];
+                    e4m3x4_to_float(codes[i], c);
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) c[k] *= f;
+                    codes[i] = to_e4m3x4(c);
+                }
             }
         }
-    }
-    if (tid == 0) *at = scale;
-    const float inv = 1.f / scale;                   // a power of two: exact
+        // (every thread of the cluster read the old scale before the barriers above)
+        if (tid == 0 && rank == 0) at[w * H] = scale;
+        const float inv = 1.f / scale;               // a power of two: exact
 #pragma unroll
-    for (int r = 0; r < R; ++r) {
-        const int t = t0 + r * TPI + tid / LPT;
-        if (t < t1) {
-            float c[4];
+        for (int r = 0; r < R; ++r) {
+            const int t = a0 + r * TPI + tid / LPT;
+            if (t < a1) {
+                float c[4];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) c[i] = v[r][i] * inv;
-            reinterpret_cast<uint32_t*>(codes)[t * (D / 4) + l] = to_e4m3x4(c);
+                for (int i = 0; i < 4; ++i) c[i] = v[w][r][i] * inv;
+                codes[t * (D / 4) + l] = to_e4m3x4(c);
+            }
         }
     }
 }
