@@ -33,8 +33,9 @@ template <typename T, int D> struct TileShape {
     static constexpr uint32_t KV = HALF * (D / 64), Q = KV * TERMS;   // one staged tile; one row block's queries
     static constexpr uint32_t Q_AT = 0, K_AT = NQ * Q, V_AT = K_AT + 2 * KV, RAW_AT = V_AT + 2 * KV;
     static constexpr uint32_t RAW = 64 * D, END = RAW_AT + 4 * RAW;      // codes of 64 tokens: keys, keys, values, values
-    // TMEM columns: scores (and weights over them) of the row blocks, then outputs; F32 has weights of its own
-    static constexpr uint32_t S_COL = 0, P_COL = NQ == 2 ? 0 : 128, O_COL = 256;
+    // TMEM columns: scores of the row blocks, each half's weights over the first of its scores, then outputs; F32 has
+    // columns of its own for weights
+    static constexpr uint32_t S_COL = 0, P_COL = NQ == 2 ? 0 : 128, P_HALF = NQ == 2 ? 64 : 32, O_COL = 256;
 };
 
 // A coming tile: what the movers and the softmax need to know of its pages.
@@ -56,7 +57,7 @@ struct TileSegment {
 struct TileShared {
     TileInfo info[TILE_AHEAD];
     TileSegment seg[TILE_AHEAD];
-    uint64_t k_full[2], k_empty[2], v_full[2], v_empty[2], q_full[2], s_full[2], p_full[2][2], h_done[2], o_full[2], o_empty[2], turn[2];
+    uint64_t k_full[2], k_empty[2], v_full[2], v_empty[2], q_full[2], s_full[2][2], p_full[2][2], h_done[2], o_full[2], o_empty[2];
     uint64_t i_full[TILE_AHEAD], i_empty[TILE_AHEAD], g_full[TILE_AHEAD], g_empty[TILE_AHEAD];
     uint64_t r_full[4], r_empty[4];
     uint32_t tmem;
@@ -444,29 +445,31 @@ struct TileSoftmax {
     float m, l;
 };
 
-// One tile of a row: weights of 64 tokens twice; `ready(half)` tells the MMA warp that they are in TMEM.  The scores of the
-// next 32 tokens are on their way while those before are worked on.  Where a score passes the maximum by more than the
-// weights can hold, the maximum moves (by a whole power of two, so what has been summed is scaled exactly) and the half is
-// done again by the same code; `settled(half)` waits until the outputs hold all weights given before that half.
-template <typename T, int D, bool EDGE, typename Ready, typename Settled>
-__device__ __forceinline__ bool tile_softmax(TileSoftmax& x, const float4* group, const TileRow& row, int t0, bool first, const Ready& ready,
-                                             const Settled& settled) {
+// One tile of a row: weights of 64 tokens twice; `scores(1)` waits for the second half's scores (the first half's are there),
+// `ready(half)` tells the MMA warp that the weights are in TMEM.  Where a score passes the maximum by more than the weights
+// can hold, the maximum moves (by a whole power of two, so what has been summed is scaled exactly) and the half is done
+// again by the same code; `settled(half)` waits until the outputs hold all weights given before that half.
+template <typename T, int D, bool EDGE, typename Scores, typename Ready, typename Settled>
+__device__ __forceinline__ bool tile_softmax(TileSoftmax& x, const float4* group, const TileRow& row, int t0, bool first, const Scores& scores,
+                                             const Ready& ready, const Settled& settled) {
     constexpr bool REST = sizeof(T) == 4;
-    uint32_t a[32], b[32], pr[32], rest[REST ? 32 : 16];
-    tc_ld32(x.t_s, a);
+    uint32_t pr[32], rest[REST ? 32 : 16];
 #pragma unroll 1
     for (int half = 0; half < 2; ++half) {
         const float4* k = group + 4 * half;
         float sum;
+        if (half == 1 && !scores(1)) return false;
 #pragma unroll 1
         for (;;) {
             float mx = -INFINITY;
             sum = 0.f;
             const float m_use = (x.m == -INFINITY ? 0.f : x.m) - TILE_SHIFT;
-            tc_wait_ld();
+            // (what tcgen05.ld brings is used, and copied, behind its wait only: nothing of it is carried around a loop)
+            uint32_t a[32], b[32];
+            tc_ld32(x.t_s + 64 * half, a);
             tc_ld32(x.t_s + 64 * half + 32, b);
-            chunk_weights<REST, EDGE>(a, k, row, m_use, t0 + 64 * half, pr, rest, mx, sum);
             tc_wait_ld();
+            chunk_weights<REST, EDGE>(a, k, row, m_use, t0 + 64 * half, pr, rest, mx, sum);
             chunk_weights<REST, EDGE>(b, k + 2, row, m_use, t0 + 64 * half + 32, pr + 16, rest + (REST ? 16 : 0), mx, sum);
             if (!__any_sync(0xffffffffu, mx > TILE_TOP || (x.m == -INFINITY && mx > -INFINITY))) break;
             const float now = fmaxf(x.m, ceilf(mx + m_use));                     // (mx = -inf leaves m)
@@ -478,12 +481,10 @@ __device__ __forceinline__ bool tile_softmax(TileSoftmax& x, const float4* group
             }
             x.l *= corr;
             x.m = now;
-            tc_ld32(x.t_s + 64 * half, a);
         }
-        if (half == 0) tc_ld32(x.t_s + 64, a);
         x.l += sum;
-        tc_st<32>(x.t_p + 32 * half, pr);
-        if constexpr (REST) tc_st<32>(x.t_p + 64 + 32 * half, rest);
+        tc_st<32>(x.t_p + TileShape<T, D>::P_HALF * half, pr);
+        if constexpr (REST) tc_st<32>(x.t_p + 64 + TileShape<T, D>::P_HALF * half, rest);
         tc_wait_st();
         ready(half);
     }
@@ -504,10 +505,10 @@ __global__ void __launch_bounds__(TILE_THREADS, 1) kv_attend_tile_kernel(const _
         for (int i = 0; i < 2; ++i) {
             mbar_init(smem_u32(&sh->k_full[i]), TILE_MOVERS); mbar_init(smem_u32(&sh->k_empty[i]), NQ);
             mbar_init(smem_u32(&sh->v_full[i]), TILE_MOVERS); mbar_init(smem_u32(&sh->v_empty[i]), NQ);
-            mbar_init(smem_u32(&sh->q_full[i]), 4); mbar_init(smem_u32(&sh->s_full[i]), 1);
+            mbar_init(smem_u32(&sh->q_full[i]), 4); mbar_init(smem_u32(&sh->s_full[i][0]), 1); mbar_init(smem_u32(&sh->s_full[i][1]), 1);
             mbar_init(smem_u32(&sh->p_full[i][0]), 4); mbar_init(smem_u32(&sh->p_full[i][1]), 4);
             mbar_init(smem_u32(&sh->h_done[i]), 1); mbar_init(smem_u32(&sh->o_full[i]), 1);
-            mbar_init(smem_u32(&sh->o_empty[i]), 4); mbar_init(smem_u32(&sh->turn[i]), 1);
+            mbar_init(smem_u32(&sh->o_empty[i]), 4);
         }
         for (int i = 0; i < TILE_AHEAD; ++i) { mbar_init(smem_u32(&sh->i_full[i]), 1); mbar_init(smem_u32(&sh->i_empty[i]), TILE_MOVERS); }
         for (int i = 0; i < TILE_AHEAD; ++i) { mbar_init(smem_u32(&sh->g_full[i]), 1); mbar_init(smem_u32(&sh->g_empty[i]), 5 * NQ); }
@@ -629,25 +630,30 @@ __global__ void __launch_bounds__(TILE_THREADS, 1) kv_attend_tile_kernel(const _
             x.m = -INFINITY;
             x.l = 0.f;
             for (int i = 0; i < n; ++i, ++tile) {
-                if (!(ok = warp_wait(&sh->s_full[qt], s_ph, sh, p))) break;
-                s_ph ^= 1;
-                tc_fence_after();
                 const int t0 = w.t0 + i * TILE_UNIT;
                 const TileInfo& info = sh->info[tile % TILE_AHEAD];
+                auto scores = [&](int half) {
+                    const bool there = warp_wait(&sh->s_full[qt][half], s_ph, sh, p);
+                    tc_fence_after();
+                    return there;
+                };
                 auto ready = [&](int half) {
                     tc_fence_before();
                     __syncwarp();
                     if (lane == 0) mbar_arrive(smem_u32(&sh->p_full[qt][half]));
                 };
-                auto settled = [&](int half) {       // (the scores' arrival says that the tile before is summed)
-                    if (half == 1) {
-                        if (!warp_wait(&sh->h_done[qt], s_ph ^ 1, sh, p)) return false;
-                        tc_fence_after();
-                    }
-                    return true;
+                // all weights given before are summed: the first half's (half = 1), or the tile before's, whose second half went
+                // to the tensor cores ahead of this tile's second scores
+                auto settled = [&](int half) {
+                    const bool there = warp_wait(half ? &sh->h_done[qt] : &sh->s_full[qt][1], s_ph, sh, p);
+                    tc_fence_after();
+                    return there;
                 };
-                ok = info.edge || info.absent ? tile_softmax<T, D, true>(x, info.group, row, t0, i == 0, ready, settled)
-                                              : tile_softmax<T, D, false>(x, info.group, row, t0, i == 0, ready, settled);
+                // (the first scores' arrival says that the tile's news is there, too: it is not looked at before)
+                if (!(ok = scores(0))) break;
+                ok = info.edge || info.absent ? tile_softmax<T, D, true>(x, info.group, row, t0, i == 0, scores, ready, settled)
+                                              : tile_softmax<T, D, false>(x, info.group, row, t0, i == 0, scores, ready, settled);
+                s_ph ^= 1;
                 if (!ok) break;
             }
         }
@@ -825,31 +831,31 @@ __global__ void __launch_bounds__(TILE_THREADS, 1) kv_attend_tile_kernel(const _
         // ------------------------------------------------------------------------------------------ MMAs
         const int qt = warp == 16 ? 0 : 1;
         // D = F32, A = B = F16; scores: both K-major; outputs: A in TMEM, B MN-major (bit 16)
-        constexpr uint32_t I_S = (1u << 4) | ((128u >> 3) << 17) | ((128u >> 4) << 24);
+        constexpr uint32_t I_S = (1u << 4) | ((64u >> 3) << 17) | ((128u >> 4) << 24);        // 64 tokens
         constexpr uint32_t I_O = (1u << 4) | (1u << 16) | (((uint32_t)D >> 3) << 17) | ((128u >> 4) << 24);
         const uint32_t hi = tile_desc_hi(1024);
         const uint32_t q_lo = ((smem_u32(smem + S::Q_AT + qt * S::Q) & 0x3FFFFu) >> 4) | (1u << 16);
         const uint32_t k_lo = ((smem_u32(smem + S::K_AT) & 0x3FFFFu) >> 4) | (1u << 16);
         const uint32_t v_lo = ((smem_u32(smem + S::V_AT) & 0x3FFFFu) >> 4) | ((S::HALF >> 4) << 16);
         const uint32_t d_s = tmem + S::S_COL + qt * 128, d_o = tmem + S::O_COL + qt * D, a_p = tmem + S::P_COL + qt * 128;
-        auto scores = [&](uint32_t slot) {           // and the slot's keys have been used
+        auto scores = [&](uint32_t slot, int half) { // of 64 tokens; with the second half the slot's keys have been used
             if (elect_one()) {
-                const uint32_t b0 = k_lo + slot * (S::KV >> 4);
+                const uint32_t b0 = k_lo + slot * (S::KV >> 4) + half * (8192 >> 4);
 #pragma unroll
                 for (int t = 0; t < TERMS; ++t)
 #pragma unroll
                     for (int k = 0; k < D / 16; ++k) {
                         const uint32_t off = (k / 4) * (S::HALF >> 4) + (k % 4) * 2;
-                        tc_mma_f16_ss(d_s, q_lo + t * (S::KV >> 4) + off, b0 + off, hi, I_S, t + k > 0);
+                        tc_mma_f16_ss(d_s + 64 * half, q_lo + t * (S::KV >> 4) + off, b0 + off, hi, I_S, t + k > 0);
                     }
-                tc_commit(smem_u32(&sh->s_full[qt]));
-                tc_commit(smem_u32(&sh->k_empty[slot]));
+                tc_commit(smem_u32(&sh->s_full[qt][half]));
+                if (half) tc_commit(smem_u32(&sh->k_empty[slot]));
             }
             __syncwarp();
         };
         auto outputs = [&](uint32_t slot, int half, bool first, bool last) {    // of the weights of 64 tokens
             if (elect_one()) {
-                const uint32_t b0 = v_lo + slot * (S::KV >> 4) + half * (8192 >> 4), a0 = a_p + 32 * half;
+                const uint32_t b0 = v_lo + slot * (S::KV >> 4) + half * (8192 >> 4), a0 = a_p + S::P_HALF * half;
 #pragma unroll
                 for (int t = 0; t < TERMS; ++t)
 #pragma unroll
@@ -859,10 +865,7 @@ __global__ void __launch_bounds__(TILE_THREADS, 1) kv_attend_tile_kernel(const _
             }
             __syncwarp();
         };
-        // The issuers of two row blocks take turns with a tile's second weights and the next scores: left to themselves their
-        // MMAs interleave, both blocks end together, and both softmaxes then share the exponential unit while the tensor
-        // cores wait.
-        uint32_t q_ph = 0, p_ph = 0, o_ph = 1, turn_ph = qt == 0 ? 1 : 0;        // (the first turn is block 0's)
+        uint32_t q_ph = 0, p_ph = 0, o_ph = 1;
         int kt = 0, vt = 0;                          // tiles whose keys and values were used
         auto keys = [&]() { return ok = warp_wait(&sh->k_full[kt & 1], (uint32_t)(kt >> 1) & 1u, sh, p); };
         auto values = [&]() { return ok = warp_wait(&sh->v_full[vt & 1], (uint32_t)(vt >> 1) & 1u, sh, p); };
@@ -886,30 +889,32 @@ __global__ void __launch_bounds__(TILE_THREADS, 1) kv_attend_tile_kernel(const _
             q_ph ^= 1;
             if (!keys()) break;
             tc_fence_after();
-            scores(kt & 1);
+            scores(kt & 1, 0);
+            scores(kt & 1, 1);
             ++kt;
             if (!(ok = warp_wait(&sh->o_empty[qt], o_ph, sh, p))) break;
             o_ph ^= 1;
+            // The next tile's scores of 64 tokens go out behind the outputs of this one's, into the columns that these weights
+            // leave: the softmax finds them done when it comes to them, and no product waits for a whole tile.
             for (int i = 0; ok && i < n; ++i, ++vt) {
+                const bool more = i + 1 < n;
                 if (!values()) break;
-                if (i + 1 < n && !keys()) break;
                 if (!(ok = warp_wait(&sh->p_full[qt][0], p_ph, sh, p))) break;
                 tc_fence_after();
-                outputs(vt & 1, 0, i == 0, i + 1 == n);
+                outputs(vt & 1, 0, i == 0, !more);
+                if (more) {
+                    if (!keys()) break;
+                    tc_fence_after();
+                    scores(kt & 1, 0);
+                }
                 if (!(ok = warp_wait(&sh->p_full[qt][1], p_ph, sh, p))) break;
                 p_ph ^= 1;
-                const bool two = nrows > 128;
-                if (two) {
-                    if (!(ok = warp_wait(&sh->turn[qt], turn_ph, sh, p))) break;
-                    turn_ph ^= 1;
-                }
                 tc_fence_after();
-                outputs(vt & 1, 1, false, i + 1 == n);
-                if (i + 1 < n) {
-                    scores(kt & 1);
+                outputs(vt & 1, 1, false, !more);
+                if (more) {
+                    scores(kt & 1, 1);
                     ++kt;
                 }
-                if (two && lane == 0) mbar_arrive(smem_u32(&sh->turn[qt ^ 1]));
             }
         }
     }
