@@ -388,6 +388,7 @@ ccv3d_status ccv3d_kv_attend(const ccv3d_kv_cache* cache, const ccv3d_token_batc
     if (ws_bytes < pl.bytes) return CCV3D_ERR_NOMEM;
     const Span w = span_of(ws, (int64_t)pl.bytes);
     if (meet(w, a) || meet(w, o) || meet(w, sc) || meet(w, ss)) return CCV3D_ERR_ALIAS;
+    if (lse && meet(w, span_of(lse, (int64_t)tokens * q_heads * 4))) return CCV3D_ERR_ALIAS;
     AttendParams p = {};
     p.c = *cache;
     p.bt = *batch;

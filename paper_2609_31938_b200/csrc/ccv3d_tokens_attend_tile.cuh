@@ -23,7 +23,9 @@ namespace ccv3d {
 
 constexpr int TILE_UNIT = 128, TILE_THREADS = 640;
 constexpr int TILE_BATCH = 1024;                       // sequences whose costs are counted at a time (in the ring of codes)
-constexpr int TILE_MOVERS = 4, TILE_AHEAD = 8;                         // warps that turn codes into halves
+constexpr int TILE_MOVERS = 4;                         // warps that turn keys into halves, and as many for values
+constexpr int TILE_AHEAD = 8;                          // tiles and segments that may be known ahead
+static_assert(TILE_AHEAD >= 8, "news goes out four tiles at a time and comes back two tiles late");
 constexpr int TILE_REGS_SOFTMAX = 168, TILE_REGS_REST = 48;   // of 256 and 384 threads: 61440 registers, what 640 threads are launched with at 96
 constexpr float TILE_SHIFT = 8.f, TILE_TOP = 15.f;      // weights start at 2^8 for the maximum and may reach 2^15
 

@@ -300,6 +300,33 @@ def test_attend_many_sequences_and_shared_pages():
     check_attend(c, cache, batch)
 
 
+@pytest.mark.parametrize("new", [1, 40])
+def test_pool_beyond_32_bit_offsets(new):
+    """The same sequence at the two ends of a pool of 5.3 GB: the same bits, appended and read."""
+    from paper_2609_31938_b200 import tokens as tk
+    c = ref.Case([new], [300], 16, 8, 128, 64, BF16, seed=21)
+    need = -(-(300 + new) // 64)
+    pages = 40500
+    codes = torch.zeros(pages, 2, 8, 64, 128, dtype=torch.uint8, device="cuda")
+    assert codes.numel() > 1 << 32
+    scales = torch.ones(pages, 2, 8, device="cuda")
+    held = c.table[0, :need].long()
+    outs = []
+    for first in (0, pages - need):
+        codes[first:first + need], scales[first:first + need] = c.codes[held].cuda(), c.scales[held].cuda()
+        cache = tk.PagedCache(codes, scales)
+        batch = tk.TokenBatch(c.starts.cuda(), c.total.cuda(), torch.arange(first, first + need, dtype=torch.int32).cuda()[None], new)
+        cache.append(c.k.cuda(), c.v.cuda(), batch)
+        outs.append((cache.attend(c.q.cuda(), batch), codes[first:first + need].clone(), scales[first:first + need].clone()))
+        assert cache.status() == 0
+    assert all(torch.equal(a, b) for a, b in zip(*outs))
+    small, batch = c.on_gpu()
+    small.append(c.k.cuda(), c.v.cuda(), batch)
+    assert torch.equal(small.codes.cpu()[held], outs[0][1].cpu()) and torch.equal(small.attend(c.q.cuda(), batch), outs[0][0])
+    del codes, outs
+    torch.cuda.empty_cache()
+
+
 def test_attend_strides_and_given_output():
     c = ref.Case([9, 50], [20, 80], 6, 2, 64, 16, BF16, seed=14)
     cache, batch = c.on_gpu()
