@@ -27,6 +27,10 @@ constexpr int TILE_MOVERS = 4;                         // warps that turn keys i
 constexpr int TILE_AHEAD = 8;                          // tiles and segments that may be known ahead
 static_assert(TILE_AHEAD >= 8, "news goes out four tiles at a time and comes back two tiles late");
 constexpr int TILE_REGS_SOFTMAX = 168, TILE_REGS_REST = 48;   // of 256 and 384 threads: 61440 registers, what 640 threads are launched with at 96
+// F32: the tensor cores cut each sum they add to instead of rounding it, which over 20 000 tokens costs 5.6e-6 of the result.
+// Every so many tiles the outputs go into sums of their own in TMEM, rounded, and start again from zero: 2e-6, with 3 % more
+// time (1760 rows, 12 heads, 15840 tokens: 364 -> 378 us).  Every 4 tiles is no more exact: the rest are cuts in the scores.
+constexpr int TILE_FOLD = 16;
 constexpr float TILE_SHIFT = 8.f, TILE_TOP = 15.f;      // weights start at 2^8 for the maximum and may reach 2^15
 
 template <typename T, int D> struct TileShape {
@@ -37,7 +41,7 @@ template <typename T, int D> struct TileShape {
     static constexpr uint32_t RAW = 64 * D, END = RAW_AT + 4 * RAW;      // codes of 64 tokens: keys, keys, values, values
     // TMEM columns: scores of the row blocks, each half's weights over the first of its scores, then outputs; F32 has
     // columns of its own for weights
-    static constexpr uint32_t S_COL = 0, P_COL = NQ == 2 ? 0 : 128, P_HALF = NQ == 2 ? 64 : 32, O_COL = 256;
+    static constexpr uint32_t S_COL = 0, P_COL = NQ == 2 ? 0 : 128, P_HALF = NQ == 2 ? 64 : 32, O_COL = 256, FOLD_COL = 384;
 };
 
 // A coming tile: what the movers and the softmax need to know of its pages.
@@ -443,8 +447,9 @@ __device__ __forceinline__ void scale_columns(uint32_t t, float f) {
 
 // A softmax thread's state: TMEM addresses of its scores, weights and outputs, its running maximum (a whole number) and sum.
 struct TileSoftmax {
-    uint32_t t_s, t_p, t_o;
+    uint32_t t_s, t_p, t_o, t_fold;
     float m, l;
+    bool folded;             // (F32) there are sums at t_fold
 };
 
 // One tile of a row: weights of 64 tokens twice; `scores(1)` waits for the second half's scores (the first half's are there),
@@ -479,7 +484,10 @@ __device__ __forceinline__ bool tile_softmax(TileSoftmax& x, const float4* group
             if (!first || half == 1) {
                 if (!settled(half)) return false;
 #pragma unroll 1
-                for (int c = 0; c < D; c += 32) scale_columns(x.t_o + c, corr);
+                for (int c = 0; c < D; c += 32) {
+                    scale_columns(x.t_o + c, corr);
+                    if (REST && x.folded) scale_columns(x.t_fold + c, corr);
+                }
             }
             x.l *= corr;
             x.m = now;
@@ -558,7 +566,7 @@ __global__ void __launch_bounds__(TILE_THREADS, 1) kv_attend_tile_kernel(const _
             return r;
         };
         TileRow row = {0, 0, 0.f, -1, 0};
-        TileSoftmax x = {t_s, t_p, t_o, 0.f, 0.f};
+        TileSoftmax x = {t_s, t_p, t_o, tmem + lanes + S::FOLD_COL, 0.f, 0.f, false};
         // A turn of the loop: the queries of segment g go in, then the output of the segment before comes out (it may not be
         // complete yet when they do), then g's tiles.  (Each piece of code stands here once: it is long.)
         bool before = false;                         // the segment before had rows here
@@ -583,6 +591,13 @@ __global__ void __launch_bounds__(TILE_THREADS, 1) kv_attend_tile_kernel(const _
                     uint32_t v[32];
                     tc_ld32(t_o + c, v);
                     tc_wait_ld();
+                    if (TERMS == 2 && x.folded) {
+                        uint32_t u[32];
+                        tc_ld32(x.t_fold + c, u);
+                        tc_wait_ld();
+#pragma unroll
+                        for (int k = 0; k < 32; ++k) v[k] = __float_as_uint(__uint_as_float(v[k]) + __uint_as_float(u[k]));
+                    }
                     if (nan) {
                         // values that are NaN were staged as zeros where some rows do not see them: find those this row sees
                         for (int i = 0; i < d.n; ++i) {
@@ -631,6 +646,7 @@ __global__ void __launch_bounds__(TILE_THREADS, 1) kv_attend_tile_kernel(const _
             row = nrow;
             x.m = -INFINITY;
             x.l = 0.f;
+            x.folded = false;
             for (int i = 0; i < n; ++i, ++tile) {
                 const int t0 = w.t0 + i * TILE_UNIT;
                 const TileInfo& info = sh->info[tile % TILE_AHEAD];
@@ -653,6 +669,21 @@ __global__ void __launch_bounds__(TILE_THREADS, 1) kv_attend_tile_kernel(const _
                 };
                 // (the first scores' arrival says that the tile's news is there, too: it is not looked at before)
                 if (!(ok = scores(0))) break;
+                if (TERMS == 2 && i && i % TILE_FOLD == 0) {
+                    if (!(ok = settled(0))) break;
+#pragma unroll 1
+                    for (int c = 0; c < D; c += 32) {
+                        uint32_t u[32], v[32];
+                        tc_ld32(t_o + c, v);
+                        tc_ld32(x.t_fold + c, u);
+                        tc_wait_ld();
+#pragma unroll
+                        for (int k = 0; k < 32; ++k) v[k] = __float_as_uint(__uint_as_float(v[k]) + (x.folded ? __uint_as_float(u[k]) : 0.f));
+                        tc_st<32>(x.t_fold + c, v);
+                    }
+                    tc_wait_st();
+                    x.folded = true;
+                }
                 ok = info.edge || info.absent ? tile_softmax<T, D, true>(x, info.group, row, t0, i == 0, scores, ready, settled)
                                               : tile_softmax<T, D, false>(x, info.group, row, t0, i == 0, scores, ready, settled);
                 s_ph ^= 1;
@@ -903,7 +934,7 @@ __global__ void __launch_bounds__(TILE_THREADS, 1) kv_attend_tile_kernel(const _
                 if (!values()) break;
                 if (!(ok = warp_wait(&sh->p_full[qt][0], p_ph, sh, p))) break;
                 tc_fence_after();
-                outputs(vt & 1, 0, i == 0, !more);
+                outputs(vt & 1, 0, i == 0 || (TERMS == 2 && i % TILE_FOLD == 0), !more);
                 if (more) {
                     if (!keys()) break;
                     tc_fence_after();

@@ -300,6 +300,40 @@ def test_attend_many_sequences_and_shared_pages():
     check_attend(c, cache, batch)
 
 
+def long_items(dtype, d, rising):
+    """So many items that a block walks over more than 2000 tokens of one, also with scores that rise all along."""
+    c = ref.Case([5] * 4, [5000, 4900, 5100, 5050], 14 * 16, 16, d, 64, dtype, seed=31, stale=0x7F)
+    if rising:
+        for b in range(4):
+            for j in range(0, 75, 15):
+                c.scales[c.table[b, j:].long().clamp_min(0).unique(), 0] *= 2
+    return c
+
+
+@pytest.mark.parametrize("dtype,d,rising", [(F32, 64, False), (BF16, 64, True)])
+def test_attend_long_stretches_of_one_item(dtype, d, rising):
+    c = long_items(dtype, d, rising)
+    cache, batch = c.on_gpu()
+    check_attend(c, cache, batch)
+
+
+def test_attend_rising_scores_over_a_long_stretch():
+    """Scores up to 500 000: where the one token that counts has a value of zero, an output is made of weights under e^-90
+    of the largest (an exact output of 1.6e-51 is among them).  Weights are halves, 2^8 for the largest and 2^-24 their
+    smallest step, so each may be off by 2^-33 of the largest besides what the other tests allow."""
+    c = long_items(F32, 128, True)
+    cache, batch = c.on_gpu()
+    got = cache.attend(c.q.cuda(), batch).cpu().double()
+    want, _, mass, spread = ref.attend(c.q, cache.codes, cache.scales, c.starts, c.total, c.table, 128 ** -0.5, 1, -1)
+    kv = ref.decode(cache.codes, cache.scales)[:, 1]
+    kv[~torch.isfinite(kv)] = 0.0                                                           # (slots nobody holds)
+    magnitudes = torch.stack([kv[c.table[b, :-(-int(c.total[b]) // 64)].long()].abs().sum((0, 2)) for b in range(4)])
+    floor = 2.0 ** -33 * magnitudes.repeat_interleave(5, 0).repeat_interleave(14, 1)        # of a token's every head
+    tol = U * want.abs() + mass * (2.0 ** -20 + 2 * 128 * U * spread)[..., None] + floor
+    assert ((got - want).abs() <= tol).all()
+    assert cache.status() == 0
+
+
 @pytest.mark.parametrize("new", [1, 40])
 def test_pool_beyond_32_bit_offsets(new):
     """The same sequence at the two ends of a pool of 5.3 GB: the same bits, appended and read."""
