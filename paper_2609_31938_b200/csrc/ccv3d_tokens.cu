@@ -228,7 +228,12 @@ ccv3d_status plan_attend(const ccv3d_kv_cache* cache, const ccv3d_token_batch* b
     if (s != CCV3D_OK) return s;
     if ((s = current_device(&pl->dev)) != CCV3D_OK) return s;
     const int64_t rows = (int64_t)batch->max_new * (q_heads / cache->kv_heads);
-    pl->rows_per_item = rows <= 8 ? 8 : rows <= 64 ? 16 : dtype == CCV3D_BF16 ? 256 : 128;
+    // The step kernel reads the cache once for every 8 or 16 rows, the tile kernel once for all but always in products of 128
+    // rows.  Device time, us, BF16 (F32), 16 heads on 4, 64 streams of 2000 tokens, 8-row items / 16-row items / tiles:
+    //   8 rows 43 (47) / 51 (64) / 96 (119);  16 rows - / 55 (66) / 96 (121);  32 rows - / 90 (112) / 96 (125);
+    //   48 rows - / 125 (156) / 98 (125);  128 rows - / 293 (371) / 105 (133)
+    // (one stream of 32768: 32 rows 33 (39) / 37 (41), 48 rows 43 (53) / 37 (41); two of 500, up to 128 rows: 16 to 20 / 25)
+    pl->rows_per_item = rows <= 8 ? 8 : rows <= 32 ? 16 : dtype == CCV3D_BF16 ? 256 : 128;
     const bool tile = pl->rows_per_item >= 128;
     pl->blocks = tile ? pl->dev.sm_count : (pl->rows_per_item == 8 ? STEP_BLOCKS : 2) * pl->dev.sm_count;
     if (pl->blocks > JOIN_PARTS) pl->blocks = JOIN_PARTS;
