@@ -1,6 +1,6 @@
 // Attention of many query rows (frames, prompts) over the paged E4M3 cache, on tcgen05.
 //
-// Bound by the tensor cores.  An item is a block of 256 query rows of one kv head (F32: 128), rows being (token, head of
+// Bound by the tensor cores and, next to them, the exponentials.  An item is a block of 256 query rows of one kv head (F32: 128), rows being (token, head of
 // the group) so that grouped heads share the keys they share; a unit is 128 cached tokens.  20 warps, one block to an SM:
 //   warps 0-3, 4-7   softmax of the first and second 128 rows, a thread to a row: scores from TMEM, weights back as halves
 //                    over them, sums in registers, the output from TMEM at the end; they also stage the queries
@@ -16,6 +16,10 @@
 // scores and, read the other way, MN-major for the outputs.  The softmax maximum is only raised when a score passes it
 // by more than 2^7 (then the sums in TMEM are scaled down): weights stay under 2^15 and a tile needs one pass.
 // For F32 queries and weights go in as two halves each (value and remainder): about 22 bits, at twice the MMAs.
+//
+// Measured (BF16): 3520 rows on 28160 tokens, 12 heads of 128, 645 to 660 us = 0.93 PFLOP/s, 56 % of what the tensor cores do
+// in a plain product.  A tile of 256 x 128 takes 3.8 k cycles: its MMAs 2.6 k, the two softmax warps of a scheduler 3.1 k (the
+// exponentials 2.05 k of them).  Items of a few units pay 17 k cycles from one to the next (queries in, outputs out).
 #pragma once
 #include "ccv3d_tokens_attend_step.cuh"
 
