@@ -1,7 +1,8 @@
 // Attention of many query rows (frames, prompts) over the paged E4M3 cache, on tcgen05.
 //
-// Bound by the tensor cores and, next to them, the exponentials.  An item is a block of 256 query rows of one kv head (F32: 128), rows being (token, head of
-// the group) so that grouped heads share the keys they share; a unit is 128 cached tokens.  20 warps, one block to an SM:
+// Bound by the tensor cores and, next to them, the exponentials.  An item is a block of 256 query rows of one kv head (F32:
+// 128), rows being (token, head of the group) so that grouped heads share the keys they share; a unit is 128 cached tokens.
+// 20 warps, one block to an SM:
 //   warps 0-3, 4-7   softmax of the first and second 128 rows, a thread to a row: scores from TMEM, weights back as halves
 //                    over them, sums in registers, the output from TMEM at the end; they also stage the queries
 //   warps 8-11, 12-15  turn codes into halves in shared memory (exact): keys and values, two slots each
@@ -31,10 +32,11 @@ constexpr int TILE_MOVERS = 4;                         // warps that turn keys i
 constexpr int TILE_AHEAD = 8;                          // tiles and segments that may be known ahead
 static_assert(TILE_AHEAD >= 8, "news goes out four tiles at a time and comes back two tiles late");
 constexpr int TILE_REGS_SOFTMAX = 168, TILE_REGS_REST = 48;   // of 256 and 384 threads: 61440 registers, what 640 threads are launched with at 96
-// F32: the tensor cores cut each sum they add to instead of rounding it, which over 20 000 tokens costs 5.6e-6 of the result.
-// Every so many tiles the outputs go into sums of their own in TMEM, rounded, and start again from zero: 2e-6, with 3 % more
-// time (1760 rows, 12 heads, 15840 tokens: 364 -> 378 us).  Every 4 tiles is no more exact: the rest are cuts in the scores.
-constexpr int TILE_FOLD = 16;
+// F32: the tensor cores cut each sum they add to instead of rounding it, which over 20 000 tokens in one stretch costs 5.6e-6 of
+// the result.  Every so many tiles the outputs go into sums of their own in TMEM, rounded, and start again from zero.
+// Errors of two batches of prompts (32-bit operations: 0.6e-6) and time of 1760 rows, 12 heads, on 15840 tokens: every 4 tiles
+// 0.8e-6, 0.9e-6, 384 us; every 16 tiles 1.1e-6, 1.3e-6, 378 us; never 364 us.
+constexpr int TILE_FOLD = 4;
 constexpr float TILE_SHIFT = 8.f, TILE_TOP = 15.f;      // weights start at 2^8 for the maximum and may reach 2^15
 
 template <typename T, int D> struct TileShape {
@@ -878,12 +880,13 @@ __global__ void __launch_bounds__(TILE_THREADS, 1) kv_attend_tile_kernel(const _
         auto scores = [&](uint32_t slot, int half) { // of 64 tokens; with the second half the slot's keys have been used
             if (elect_one()) {
                 const uint32_t b0 = k_lo + slot * (S::KV >> 4) + half * (8192 >> 4);
+                // (remainders first: a cut is as small as the sum it is made in; in this order 1.5e-6 of a result, else 2e-6)
 #pragma unroll
-                for (int t = 0; t < TERMS; ++t)
+                for (int t = TERMS - 1; t >= 0; --t)
 #pragma unroll
                     for (int k = 0; k < D / 16; ++k) {
                         const uint32_t off = (k / 4) * (S::HALF >> 4) + (k % 4) * 2;
-                        tc_mma_f16_ss(d_s + 64 * half, q_lo + t * (S::KV >> 4) + off, b0 + off, hi, I_S, t + k > 0);
+                        tc_mma_f16_ss(d_s + 64 * half, q_lo + t * (S::KV >> 4) + off, b0 + off, hi, I_S, t < TERMS - 1 || k > 0);
                     }
                 tc_commit(smem_u32(&sh->s_full[qt][half]));
                 if (half) tc_commit(smem_u32(&sh->k_empty[slot]));
