@@ -11,7 +11,7 @@
 //
 // Measured (BF16): 64 streams, 612 MB of cache, 124 us = 5.0 TB/s, 76 % of the copy rate; one stream of 269 MB, 60 us =
 // 4.5 TB/s, of which some 8 us are the start and the join.  What holds it is the latency of a warp's dependent
-// instructions (0.38 of a scheduler's slots are used), not one unit.
+// instructions (0.38 of a scheduler's slots were used at two blocks), not one unit.
 #pragma once
 #include "ccv3d_tokens_attend.cuh"
 
