@@ -12,7 +12,7 @@ SOURCES = {   # source -> the files its object depends on
     "ccv3d_api.cu": ["ccv3d_simt.cuh", "ccv3d_tc.cuh", "ccv3d_tc_layout.cuh", "ccv3d_tc_ptx.cuh", "ccv3d_tc_conv.cuh",
                      "ccv3d_tc_pointwise.cuh", "ccv3d_host_common.cuh", "ccv3d_host_tc.cuh", "ccv3d_host_ring.cuh", HEADER],
     "ccv3d_tokens.cu": ["ccv3d_tokens_common.cuh", "ccv3d_tokens_norm.cuh", "ccv3d_tokens_append.cuh",
-                        "ccv3d_tokens_attend.cuh", "ccv3d_tokens_attend_step.cuh",
+                        "ccv3d_tokens_softmax.cuh", "ccv3d_tokens_attend.cuh", "ccv3d_tokens_attend_step.cuh",
                         "ccv3d_tokens_attend_tile.cuh", "ccv3d_tc_ptx.cuh", HEADER],
 }
 

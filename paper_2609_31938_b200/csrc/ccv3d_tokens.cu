@@ -281,7 +281,7 @@ ccv3d_status launch_step(const AttendParams& p, const Plan& pl, cudaStream_t st)
 
 // The sum over parts, launched so that it is resident when the attention kernel ends.
 template <typename T, int D>
-ccv3d_status launch_join(const AttendParams& p, const Plan& pl, float shift, cudaStream_t st) {
+ccv3d_status launch_join(const AttendParams& p, const Plan& pl, cudaStream_t st) {
     cudaLaunchAttribute at[1];
     at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     at[0].val.programmaticStreamSerializationAllowed = 1;
@@ -291,7 +291,7 @@ ccv3d_status launch_join(const AttendParams& p, const Plan& pl, float shift, cud
     cfg.stream = st;
     cfg.attrs = at;
     cfg.numAttrs = 1;
-    if (cudaLaunchKernelEx(&cfg, attend_join_kernel<T, D>, p, shift) != cudaSuccess) { cudaGetLastError(); return CCV3D_ERR_CUDA; }
+    if (cudaLaunchKernelEx(&cfg, attend_join_kernel<T, D>, p) != cudaSuccess) { cudaGetLastError(); return CCV3D_ERR_CUDA; }
     return CCV3D_OK;
 }
 
@@ -304,10 +304,10 @@ ccv3d_status launch_attend(const AttendParams& p, const Plan& pl, cudaStream_t s
         if (!allow_smem(kv_attend_tile_kernel<T, D>, bytes, pl.dev.index, done)) { cudaGetLastError(); return CCV3D_ERR_CUDA; }
         kv_attend_tile_kernel<T, D><<<pl.blocks, TILE_THREADS, bytes, st>>>(p);
         const ccv3d_status s = launched();
-        return s == CCV3D_OK ? launch_join<T, D>(p, pl, TILE_SHIFT, st) : s;
+        return s == CCV3D_OK ? launch_join<T, D>(p, pl, st) : s;
     }
     const ccv3d_status s = pl.rows_per_item == 8 ? launch_step<T, D, 1>(p, pl, st) : launch_step<T, D, 2>(p, pl, st);
-    return s == CCV3D_OK ? launch_join<T, D>(p, pl, STEP_SHIFT, st) : s;
+    return s == CCV3D_OK ? launch_join<T, D>(p, pl, st) : s;
 }
 
 }  // namespace

@@ -3,18 +3,18 @@
 // The work of a call is a list of items (a sequence, a block of its query rows, a kv head), each a run of units (a
 // stretch of cached tokens); block i of G takes units [i U / G, (i + 1) U / G) of the whole list, so every block has
 // the same to read whatever the sequences' lengths, and nothing about them has to be known on the host.  An item that
-// lies in one block is finished there; one that crosses blocks leaves a part (unnormalised sums, their running maximum
+// lies in one block is finished there; one that crosses blocks leaves a part (unnormalised sums, their base
 // and weight) in each, and attend_join_kernel adds the parts in block order.
 //
 // Softmax in powers of two: with t = score * log2(e) and e_v = log2 of the value scale of the token's page, the weight
-// of a value code is 2^(t + e_v - m + shift), m the running maximum of t + e_v, so page scales of any size stay out of
-// the range of the 16-bit weights; the softmax's own sum takes that times 1 / value scale.  The shift uses the part of
-// that range above 1.
+// of a value code is 2^(t + e_v - base), base the running one of t + e_v, so page scales of any size stay out of the range
+// of the 16-bit weights; the softmax's own sum takes that times 1 / value scale.
 #pragma once
 #include <cuda.h>
 
 #include "ccv3d_tc_ptx.cuh"
 #include "ccv3d_tokens_common.cuh"
+#include "ccv3d_tokens_softmax.cuh"
 
 namespace ccv3d {
 
@@ -33,7 +33,7 @@ struct AttendParams {
     long long wait_clk;      // bound of every wait, in SM clocks
     // scratch: slots 2 i (an item that began before block i) and 2 i + 1 (one that ends behind it)
     float* part;             // [slot][slot_rows][dim] sums
-    float2* part_ml;         // [slot][slot_rows] maximum and weight
+    float2* part_ml;         // [slot][slot_rows] base and weight
     Join* join;              // [block]; parts = 0: nothing to join
     int slot_rows;
 };
@@ -65,17 +65,17 @@ template <typename T>
 __device__ __forceinline__ void store_out(const AttendParams& p, int token, int head, int d, const float (&v)[4]) {
     store4((T*)p.o.data + token * p.o.token_stride + head * p.o.head_stride + d, v);
 }
-__device__ __forceinline__ float lse_of(float m, float l, float shift) {
-    return l != 0.f ? (m - shift + log2f(l)) * LN2 : -INFINITY;     // (a row that saw NaN has l = NaN)
+__device__ __forceinline__ float lse_of(float base, float l) {
+    return l != 0.f ? (base + log2f(l)) * LN2 : -INFINITY;     // (a row that saw NaN has l = NaN)
 }
 
 // Adds the parts of the item that starts in block blockIdx.x of the attention kernel, rows blockIdx.y, + gridDim.y, ...
 // Few parts (a tile of rows that two blocks share): D / 4 threads to a row, part after part.  But an item can have as many
-// parts as there were blocks (one stream behind a long cache): then a row's parts are spread over all threads, their maxima
+// parts as there were blocks (one stream behind a long cache): then a row's parts are spread over all threads, their bases
 // and weights a part to a thread, their sums D / 4 threads to a part.
 constexpr int JOIN_THREADS = 128, JOIN_PARTS = 1024, JOIN_FEW = 8;
 template <typename T, int D>
-__global__ void __launch_bounds__(JOIN_THREADS) attend_join_kernel(const AttendParams p, float shift) {
+__global__ void __launch_bounds__(JOIN_THREADS) attend_join_kernel(const AttendParams p) {
     constexpr int L = D / 4, SLICES = JOIN_THREADS / L;
     __shared__ float weight[JOIN_PARTS], red[2][JOIN_THREADS / 32];
     __shared__ float4 sums[JOIN_THREADS];
@@ -90,7 +90,7 @@ __global__ void __launch_bounds__(JOIN_THREADS) attend_join_kernel(const AttendP
         for (int i = 0; i < 4; ++i) acc[i] = l != 0.f ? acc[i] * inv : 0.f;
         const int token = (j.row0 + r) / p.group, head = j.head0 + (j.row0 + r) % p.group;
         store_out<T>(p, token, head, d, acc);
-        if (d == 0 && p.lse) p.lse[(int64_t)token * p.q_heads + head] = lse_of(m, l, shift);
+        if (d == 0 && p.lse) p.lse[(int64_t)token * p.q_heads + head] = lse_of(m, l);
     };
     if (j.parts <= JOIN_FEW) {
         for (int r = blockIdx.y * SLICES + slice; r < j.rows; r += gridDim.y * SLICES) {

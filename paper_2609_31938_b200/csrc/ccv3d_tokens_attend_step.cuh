@@ -19,7 +19,6 @@ namespace ccv3d {
 
 constexpr int STEP_BLOCKS = 3;               // resident on an SM
 constexpr int STEP_WARPS = 4, STEP_TILE = 32, STEP_UNIT = STEP_WARPS * STEP_TILE;
-constexpr float STEP_SHIFT = 8.f, STEP_TOP = 15.f;           // weights start at 2^8 for the maximum and may reach 2^15
 
 template <int D> struct StepShape {
     static constexpr int STAGES = D == 128 ? 2 : 4;
@@ -378,9 +377,14 @@ __global__ void __launch_bounds__(32 * STEP_WARPS, NT == 1 ? STEP_BLOCKS : 2) kv
             scale_terms(sc.y, ev[0], iv[0]);
             scale_terms(sc.w, ev[1], iv[1]);
             const float kf[2] = {sc.x, sc.z};
-            // The maximum is that of earlier tiles until a score passes it by more than the weights can hold (2^7): then it
-            // moves, by a whole power of two, for all rows.  Most tiles so need no maximum over the lanes.
+            // The base is that of earlier tiles until a score passes what it bears: then it moves, by a whole power of two, for
+            // all rows.  Most tiles so need no maximum over the lanes.
             bool raise = false;
+            float limit[NT][2];
+#pragma unroll
+            for (int i = 0; i < NT; ++i)
+#pragma unroll
+                for (int e = 0; e < 2; ++e) limit[i][e] = base_limit(m[i][e]);
 #pragma unroll
             for (int i = 0; i < NT; ++i)
 #pragma unroll
@@ -393,7 +397,7 @@ __global__ void __launch_bounds__(32 * STEP_WARPS, NT == 1 ? STEP_BLOCKS : 2) kv
                             if (t < clo[i][e & 1] || t >= chi[i][e & 1] || (j ? pg.y : pg.x) < 0) v = -INFINITY;
                         }
                         x[i][j][e] = v;
-                        raise = raise || v > m[i][e & 1] + (STEP_TOP - STEP_SHIFT);
+                        raise = raise || v > limit[i][e & 1];
                     }
             if (__any_sync(0xffffffffu, raise)) {
 #pragma unroll
@@ -404,7 +408,7 @@ __global__ void __launch_bounds__(32 * STEP_WARPS, NT == 1 ? STEP_BLOCKS : 2) kv
                         mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 4));
                         mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 8));
                         mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 16));
-                        mx = fmaxf(m[i][e], ceilf(mx));
+                        mx = fmaxf(m[i][e], base_for(mx));
                         const float corr = m[i][e] == -INFINITY ? 0.f : exp2_fast(m[i][e] - mx);
                         m[i][e] = mx;
                         l[i][e] *= corr;
@@ -415,7 +419,7 @@ __global__ void __launch_bounds__(32 * STEP_WARPS, NT == 1 ? STEP_BLOCKS : 2) kv
             uint32_t pf[NT][TERMS][2][2];                                        // weights, tokens down the contraction
 #pragma unroll
             for (int i = 0; i < NT; ++i) {
-                const float m_use[2] = {(m[i][0] == -INFINITY ? 0.f : m[i][0]) - STEP_SHIFT, (m[i][1] == -INFINITY ? 0.f : m[i][1]) - STEP_SHIFT};
+                const float m_use[2] = {base_or_start(m[i][0]), base_or_start(m[i][1])};
 #pragma unroll
                 for (int j = 0; j < 2; ++j) {
                     float w4[4];
@@ -594,7 +598,7 @@ __global__ void __launch_bounds__(32 * STEP_WARPS, NT == 1 ? STEP_BLOCKS : 2) kv
                             for (int t = 0; t < 4; ++t) v[t] = ll[e] != 0.f ? v[t] * inv[e] : 0.f;
                             store_out<T>(p, token, head, r8 * (D / 8) + 2 * k, v);
                         }
-                        if (r8 == 0 && p.lse) p.lse[(int64_t)token * p.q_heads + head] = lse_of(mm[e], ll[e], STEP_SHIFT);
+                        if (r8 == 0 && p.lse) p.lse[(int64_t)token * p.q_heads + head] = lse_of(mm[e], ll[e]);
                     } else {
                         float* dst = p.part + (slot * p.slot_rows + n) * D + r8 * (D / 8);
 #pragma unroll

@@ -14,8 +14,8 @@
 // Two row blocks in turn keep the tensor cores busy: while one is in its softmax the other's products run.
 //
 // Keys and values are staged alike, rows of 64 channels (128 bytes, 128-byte swizzle) token by token: K-major for the
-// scores and, read the other way, MN-major for the outputs.  The softmax maximum is only raised when a score passes it
-// by more than 2^7 (then the sums in TMEM are scaled down): weights stay under 2^15 and a tile needs one pass.
+// scores and, read the other way, MN-major for the outputs.  The softmax base is only raised when a score passes what it
+// bears (then the sums in TMEM are scaled down): weights stay under 2^15 and a tile needs one pass.
 // For F32 queries and weights go in as two halves each (value and remainder): about 22 bits, at twice the MMAs.
 //
 // Measured (BF16): 3520 rows on 28160 tokens, 12 heads of 128, 645 to 660 us = 0.93 PFLOP/s, 56 % of what the tensor cores do
@@ -37,7 +37,6 @@ constexpr int TILE_REGS_SOFTMAX = 168, TILE_REGS_REST = 48;   // of 256 and 384 
 // Errors of two batches of prompts (32-bit operations: 0.6e-6) and time of 1760 rows, 12 heads, on 15840 tokens: every 4 tiles
 // 0.8e-6, 0.9e-6, 384 us; every 16 tiles 1.1e-6, 1.3e-6, 378 us; never 364 us.
 constexpr int TILE_FOLD = 4;
-constexpr float TILE_SHIFT = 8.f, TILE_TOP = 15.f;      // weights start at 2^8 for the maximum and may reach 2^15
 
 template <typename T, int D> struct TileShape {
     static constexpr int TERMS = sizeof(T) == 4 ? 2 : 1, NQ = sizeof(T) == 4 ? 1 : 2, ROWS = 128 * NQ;
@@ -409,16 +408,18 @@ __device__ __forceinline__ uint32_t bits_between(int first, int end) {
     const uint32_t below_end = end >= 32 ? 0xFFFFFFFFu : (1u << max(end, 0)) - 1u, below_first = first >= 32 ? 0xFFFFFFFFu : (1u << max(first, 0)) - 1u;
     return below_end & ~below_first;
 }
-// Scores of 32 tokens (two groups of 16) to weights: packed into pr (F32: remainders into rest).  mx gathers the largest
-// exponent met, sum what the weights add to the row's weight sum.
+// Scores of 32 tokens (two groups of 16) to weights: packed into pr (F32: remainders into rest), sum: what the weights add to the
+// row's weight sum.  The exponent comes in one rounding from the product, and mx gathers the largest.  EDGE (tokens that this
+// row may not see, and rows with far scores) rounds the score first, and mx gathers the largest score: it then is that of some
+// token, and none lies above it, which no longer holds of the other once neighbouring floats are no small part of a unit apart.
 template <bool REST, bool EDGE>
-__device__ __forceinline__ void chunk_weights(const uint32_t (&v)[32], const float4* group, const TileRow& row, float m_use, int t0, uint32_t* pr,
+__device__ __forceinline__ void chunk_weights(const uint32_t (&v)[32], const float4* group, const TileRow& row, float base, int t0, uint32_t* pr,
                                               uint32_t* rest, float& mx, float& sum) {
 #pragma unroll
     for (int g = 0; g < 2; ++g) {
         const float4 k = group[g];
-        const float f = k.x * row.factor, a = k.y - m_use;
-        const uint64_t f2 = pair(f, f), a2 = pair(a, a);
+        const float f = k.x * row.factor, a = EDGE ? k.y : k.y - base;
+        const uint64_t f2 = pair(f, f), a2 = pair(a, a), down2 = pair(-base, -base);
         uint64_t part = 0;                                       // two sums: even and odd tokens
         const uint32_t seen = EDGE && k.y != -INFINITY ? bits_between(row.lo - t0 - 16 * g, row.hi - t0 - 16 * g) : 0u;
 #pragma unroll
@@ -430,6 +431,7 @@ __device__ __forceinline__ void chunk_weights(const uint32_t (&v)[32], const flo
                 if (!(seen >> (i + 1) & 1u)) y = -INFINITY;
             }
             mx = max3(mx, x, y);
+            if (EDGE) unpair(add_pair(pair(x, y), down2), x, y);
             const float e0 = exp2_fast(x), e1 = exp2_fast(y);
             part = add_pair(part, pair(e0, e1));
             const uint32_t h = pack_half(e0, e1);
@@ -451,44 +453,53 @@ __device__ __forceinline__ void scale_columns(uint32_t t, float f) {
     tc_st<32>(t, v);
 }
 
-// A softmax thread's state: TMEM addresses of its scores, weights and outputs, its running maximum (a whole number) and sum.
+// A softmax thread's state: TMEM addresses of its scores, weights and outputs, its running base and sum.
 struct TileSoftmax {
     uint32_t t_s, t_p, t_o, t_fold;
     float m, l;
     bool folded;             // (F32) there are sums at t_fold
+    bool far;                // (the same for the warp) scores of some row are beyond SCORE_EXACT
 };
+// Passes over a half tile: the first, and one after the base was raised.  No raise leaves an exponent that asks for another.
+constexpr int TILE_PASSES = 2;
 
-// One tile of a row: weights of 64 tokens twice; `scores(1)` waits for the second half's scores (the first half's are there),
-// `ready(half)` tells the MMA warp that the weights are in TMEM.  Where a score passes the maximum by more than the weights
-// can hold, the maximum moves (by a whole power of two, so what has been summed is scaled exactly) and the half is done
-// again by the same code; `settled(half)` waits until the outputs hold all weights given before that half.
+// One tile of a row, from `half` on: weights of 64 tokens twice; `scores(1)` waits for the second half's scores (the first half's are
+// there), `ready(half)` tells the MMA warp that the weights are in TMEM.  Where a score passes the base by more than the weights
+// can hold, the base moves (by a whole power of two, so what has been summed is scaled exactly) and the half is done
+// again by the same code; `settled(half)` waits until the outputs hold all weights given before that half.  Returns 2, or -1
+// if a wait gave up, or without EDGE the half that turned out to hold far scores (nothing of it has gone out).
 template <typename T, int D, bool EDGE, typename Scores, typename Ready, typename Settled>
-__device__ __forceinline__ bool tile_softmax(TileSoftmax& x, const float4* group, const TileRow& row, int t0, bool first, const Scores& scores,
-                                             const Ready& ready, const Settled& settled) {
+__device__ __forceinline__ int tile_softmax(TileSoftmax& x, const float4* group, const TileRow& row, int t0, bool first, int half,
+                                            const Scores& scores, const Ready& ready, const Settled& settled) {
     constexpr bool REST = sizeof(T) == 4;
     uint32_t pr[32], rest[REST ? 32 : 16];
 #pragma unroll 1
-    for (int half = 0; half < 2; ++half) {
+    for (; half < 2; ++half) {
         const float4* k = group + 4 * half;
         float sum;
-        if (half == 1 && !scores(1)) return false;
+        if (half == 1 && !scores(1)) return -1;
 #pragma unroll 1
-        for (;;) {
+        for (int pass = 1;; ++pass) {
             float mx = -INFINITY;
             sum = 0.f;
-            const float m_use = (x.m == -INFINITY ? 0.f : x.m) - TILE_SHIFT;
+            const float base = base_or_start(x.m);
             // (what tcgen05.ld brings is used, and copied, behind its wait only: nothing of it is carried around a loop)
             uint32_t a[32], b[32];
             tc_ld32(x.t_s + 64 * half, a);
             tc_ld32(x.t_s + 64 * half + 32, b);
             tc_wait_ld();
-            chunk_weights<REST, EDGE>(a, k, row, m_use, t0 + 64 * half, pr, rest, mx, sum);
-            chunk_weights<REST, EDGE>(b, k + 2, row, m_use, t0 + 64 * half + 32, pr + 16, rest + (REST ? 16 : 0), mx, sum);
-            if (!__any_sync(0xffffffffu, mx > TILE_TOP || (x.m == -INFINITY && mx > -INFINITY))) break;
-            const float now = fmaxf(x.m, ceilf(mx + m_use));                     // (mx = -inf leaves m)
+            chunk_weights<REST, EDGE>(a, k, row, base, t0 + 64 * half, pr, rest, mx, sum);
+            chunk_weights<REST, EDGE>(b, k + 2, row, base, t0 + 64 * half + 32, pr + 16, rest + (REST ? 16 : 0), mx, sum);
+            const bool raise = EDGE ? mx > base_limit(x.m) : mx > WEIGHT_TOP || (x.m == -INFINITY && mx > -INFINITY);
+            if (pass >= TILE_PASSES || !__any_sync(0xffffffffu, raise)) break;
+            const float now = fmaxf(x.m, base_for(EDGE ? mx : mx + base));       // (mx = -inf leaves the base)
+            if (__any_sync(0xffffffffu, raise && !(fabsf(now) <= SCORE_EXACT))) {
+                x.far = true;
+                if (!EDGE) return half;
+            }
             const float corr = x.m == -INFINITY ? 0.f : exp2_fast(x.m - now);
             if (!first || half == 1) {
-                if (!settled(half)) return false;
+                if (!settled(half)) return -1;
 #pragma unroll 1
                 for (int c = 0; c < D; c += 32) {
                     scale_columns(x.t_o + c, corr);
@@ -504,7 +515,7 @@ __device__ __forceinline__ bool tile_softmax(TileSoftmax& x, const float4* group
         tc_wait_st();
         ready(half);
     }
-    return true;
+    return 2;
 }
 
 template <typename T, int D>
@@ -572,7 +583,7 @@ __global__ void __launch_bounds__(TILE_THREADS, 1) kv_attend_tile_kernel(const _
             return r;
         };
         TileRow row = {0, 0, 0.f, -1, 0};
-        TileSoftmax x = {t_s, t_p, t_o, tmem + lanes + S::FOLD_COL, 0.f, 0.f, false};
+        TileSoftmax x = {t_s, t_p, t_o, tmem + lanes + S::FOLD_COL, 0.f, 0.f, false, false};
         // A turn of the loop: the queries of segment g go in, then the output of the segment before comes out (it may not be
         // complete yet when they do), then g's tiles.  (Each piece of code stands here once: it is long.)
         bool before = false;                         // the segment before had rows here
@@ -636,7 +647,7 @@ __global__ void __launch_bounds__(TILE_THREADS, 1) kv_attend_tile_kernel(const _
                 if (lane == 0) mbar_arrive(smem_u32(&sh->o_empty[qt]));
                 if (row.token >= 0) {
                     if (!whole) p.part_ml[slot] = make_float2(x.m, x.l);
-                    else if (p.lse) p.lse[(int64_t)row.token * p.q_heads + row.head] = lse_of(x.m, x.l, TILE_SHIFT);
+                    else if (p.lse) p.lse[(int64_t)row.token * p.q_heads + row.head] = lse_of(x.m, x.l);
                 }
                 if (d.starts && !d.ends && threadIdx.x == 0) p.join[blockIdx.x] = {d.parts, d.first * p.group + d.row0, d.nrows, d.h * p.group};
                 release(g - 1);
@@ -652,7 +663,7 @@ __global__ void __launch_bounds__(TILE_THREADS, 1) kv_attend_tile_kernel(const _
             row = nrow;
             x.m = -INFINITY;
             x.l = 0.f;
-            x.folded = false;
+            x.folded = x.far = false;
             for (int i = 0; i < n; ++i, ++tile) {
                 const int t0 = w.t0 + i * TILE_UNIT;
                 const TileInfo& info = sh->info[tile % TILE_AHEAD];
@@ -690,8 +701,10 @@ __global__ void __launch_bounds__(TILE_THREADS, 1) kv_attend_tile_kernel(const _
                     tc_wait_st();
                     x.folded = true;
                 }
-                ok = info.edge || info.absent ? tile_softmax<T, D, true>(x, info.group, row, t0, i == 0, scores, ready, settled)
-                                              : tile_softmax<T, D, false>(x, info.group, row, t0, i == 0, scores, ready, settled);
+                int half = 0;
+                if (!(info.edge || info.absent || x.far)) half = tile_softmax<T, D, false>(x, info.group, row, t0, i == 0, 0, scores, ready, settled);
+                if (half >= 0 && half < 2) half = tile_softmax<T, D, true>(x, info.group, row, t0, i == 0, half, scores, ready, settled);
+                ok = half == 2;
                 s_ph ^= 1;
                 if (!ok) break;
             }

@@ -1,0 +1,114 @@
+"""Attention where scores leave the range in which floats are closer than a unit.
+
+With e = head_dim * 2^-24 * sum |q||k| the error of a score (a sum of exact products in FP32), a row whose best token leads by
+more than 2 e + 100 has every other weight under e^-100 of it: its output is that token's value within the roundings of
+weights (2^-11 BF16, 2^-20 F32) and output, its lse that token's score within e and FP32.  Of any other row no more is
+known than that its output is an average of values it sees.
+"""
+import math
+
+import pytest
+
+import _tokens_ref as ref
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+
+U = 2.0 ** -24
+BF16, F32 = torch.bfloat16, torch.float32
+
+
+@pytest.fixture(autouse=True)
+def _gpu():
+    if not torch.cuda.is_available():
+        pytest.skip("no CUDA device")
+    torch.cuda.set_device(0)
+
+
+def scores_of(c, frame=1, window=-1):
+    """Per row: scores [rows, heads, tokens] in 64 bits (-inf where unseen), the sums of magnitudes, and the values."""
+    kv = ref.decode(c.codes, c.scales)
+    H, P, D = kv.shape[2], kv.shape[3], kv.shape[4]
+    G = c.q.shape[1] // H
+    out = []
+    for b, n in enumerate(c.new):
+        total = int(c.total[b])
+        pages = c.table[b, :-(-total // P)].long()
+        k, v = (kv[pages, j].transpose(0, 1).reshape(H, -1, D)[:, :total].repeat_interleave(G, 0) for j in range(2))
+        q = c.q[int(c.starts[b]):int(c.starts[b]) + n].double()
+        x = torch.einsum("nhd,htd->nht", q, k) * D ** -0.5
+        size = (torch.einsum("nhd,htd->nht", q.abs(), k.abs()) * D ** -0.5).amax(-1)
+        for i in range(n):
+            lo, hi = ref.visible(total - n + i, total, frame, window)
+            x[i, :, :lo], x[i, :, hi:] = -math.inf, -math.inf
+        out.append((x, size, v))
+    return out
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("new,dim", [(1, 128), (5, 64), (150, 128), (150, 64)])
+@pytest.mark.parametrize("size", [3e6, 3e7, 1e8, 2e8, 1e10, 1e12, 1e20, 1e30])
+def test_attend_far_scores(size, new, dim, dtype):
+    c = ref.Case([new, 2], [200, 90], 4, 2, dim, 32, dtype, seed=41, stale=0x7F)
+    c.q = (c.q.float() * size).to(dtype)
+    cache, batch = c.on_gpu()
+    got, lse = cache.attend(c.q.cuda(), batch, want_lse=True)
+    assert cache.status() == 0
+    got, lse = got.cpu().double(), lse.cpu().double()
+    led = rows = 0
+    for b, (x, mag, v) in enumerate(scores_of(c)):
+        at = slice(int(c.starts[b]), int(c.starts[b + 1]))
+        e = dim * U * mag
+        top, best = x.max(-1)
+        lead = top - x.scatter(-1, best[..., None], -math.inf).amax(-1) > 2 * e + 100
+        want = torch.stack([v[h, best[:, h]] for h in range(4)], 1)
+        tol = ((2.0 ** -8 if dtype == BF16 else U) + (2.0 ** -11 if dtype == BF16 else 2.0 ** -20)) * want.abs()
+        assert ((got[at] - want).abs() <= tol)[lead].all()
+        assert ((lse[at] - top).abs() <= e + 2.0 ** -20 * (1 + top.abs()))[lead].all()
+        most = v.abs().amax((1, 2))[None, :, None] * (1 + 2.0 ** -7)
+        assert torch.isfinite(got[at]).all() and (got[at].abs() <= most).all() and torch.isfinite(lse[at]).all()
+        led, rows = led + int(lead.sum()), rows + lead.numel()
+    assert led >= 0.8 * rows or size < 1e8               # (smaller scores lead by less)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("new", [1, 150])
+def test_attend_far_scores_of_some_rows_and_of_later_tokens(new, dtype):
+    """Rows with ordinary scores next to rows with far ones; scores that become far, and stop being so, along the cache."""
+    c = ref.Case([new], [700], 4, 2, 128, 64, dtype, seed=43, stale=0x7F)
+    c.q[:, ::2] *= 2.0 ** 20
+    for j, power in ((3, 12), (4, 20), (5, -30), (8, 24)):
+        c.scales[int(c.table[0, j]), 0, 0] *= 2.0 ** power
+    cache, batch = c.on_gpu()
+    got = cache.attend(c.q.cuda(), batch).cpu().double()
+    assert cache.status() == 0
+    (x, mag, v), = scores_of(c)
+    p = torch.softmax(x, -1)
+    want, mass = torch.einsum("nht,htd->nhd", p, v), torch.einsum("nht,htd->nhd", p, v.abs())
+    far = 128 * U * mag > 1e-2                           # rows whose scores are uncertain: hold for those that lead
+    top, best = x.max(-1)
+    lead = top - x.scatter(-1, best[..., None], -math.inf).amax(-1) > 2 * 128 * U * mag + 100
+    tol = (2.0 ** -8 if dtype == BF16 else U) * want.abs() + mass * (2.0 ** -11 if dtype == BF16 else 2.0 ** -20)
+    assert lead[far].double().mean() >= 0.5
+    assert ((got - want).abs() <= tol)[lead & far].all()
+    tol = tol + mass * (2 * 128 * U * mag)[..., None]
+    assert ((got - want).abs() <= tol)[~far].all()
+    assert torch.isfinite(got).all()
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("new", [1, 150])
+def test_attend_scores_past_the_largest_float(new, dtype):
+    """A row one of whose scores passes the largest float is NaN, as infinity minus infinity is; below the smallest it weighs nothing."""
+    c = ref.Case([new], [120], 2, 1, 64, 32, dtype, seed=44, stale=0x7F)
+    c.q = (c.q.float() * (4e31 if new == 1 else 2.5e31)).to(dtype)
+    c.scales[:, 0] *= 2.0 ** 20
+    cache, batch = c.on_gpu()
+    got, lse = cache.attend(c.q.cuda(), batch, want_lse=True)
+    (x, _, _), = scores_of(c)
+    largest = 3.402823466e38 * math.log(2.0)             # (scores are kept in units of log2)
+    over, under = (x > 1.01 * largest).any(-1), (x < 0.99 * largest).all(-1)
+    assert over.any() and under.any()
+    assert torch.isnan(got.cpu()[over]).all() and torch.isnan(lse.cpu()[over]).all()
+    assert torch.isfinite(got.cpu()[under]).all()
+    assert cache.status() == 0
