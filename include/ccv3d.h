@@ -474,7 +474,8 @@ typedef struct {
  * been given fits into +-448.  A page whose first token is among the new ones starts afresh; else it keeps at least its
  * scale, and where the new tokens need a larger one its older codes are moved to it.  Infinities are stored as +-448,
  * NaN as NaN; neither takes part in the scale.
- * q_out may be q itself (same strides); any other overlap of an output with an input is CCV3D_ERR_ALIAS.
+ * q_out may be q itself (same strides); any other overlap of an output with an input is CCV3D_ERR_ALIAS (slices of one
+ * projection, whose ranges lie in one another without sharing an element, do not overlap if their token strides agree).
  * Stream-ordered, one kernel, no allocation, legal in a stream capture.
  */
 ccv3d_status ccv3d_kv_append(const ccv3d_kv_cache* cache, const ccv3d_token_batch* batch, const ccv3d_heads* k,
@@ -494,7 +495,7 @@ ccv3d_status ccv3d_kv_append(const ccv3d_kv_cache* cache, const ccv3d_token_batc
  *   q_heads   a multiple of kv_heads
  *   ws        DEVICE scratch, 256-byte aligned, ccv3d_kv_attend_workspace() bytes; holds data within the call only,
  *             calls that may overlap on the GPU need one each
- * out must not overlap q.  Stream-ordered, no allocation, legal in a stream capture.
+ * An overlap of out, lse or ws with an input is CCV3D_ERR_ALIAS.  Stream-ordered, no allocation, legal in a stream capture.
  */
 ccv3d_status ccv3d_kv_attend(const ccv3d_kv_cache* cache, const ccv3d_token_batch* batch, const ccv3d_heads* q,
                              const ccv3d_heads* out, float* lse, int32_t q_heads, int32_t dtype, float scale,

@@ -73,6 +73,25 @@ inline Span span_of(const ccv3d_heads& h, int64_t tokens, int heads, int dim, in
 }
 inline bool meet(const Span& x, const Span& y) { return x.a < y.b && y.a < x.b; }
 
+// Whether two packed tensors of the same tokens share an element.  Slices of one projection have ranges that lie in one another
+// without sharing any: with one token stride, heads are compared within a token's stretch.  Unlike strides count as shared
+// where the ranges meet.
+bool share(const ccv3d_heads& x, int x_heads, const ccv3d_heads& y, int y_heads, int64_t tokens, int dim, int dt) {
+    if (!meet(span_of(x, tokens, x_heads, dim, dt), span_of(y, tokens, y_heads, dim, dt))) return false;
+    const int64_t e = esize(dt), len = dim * e, xs = x.head_stride * e, ys = y.head_stride * e;
+    const int64_t x_far = (x_heads - 1) * xs + len, y_far = (y_heads - 1) * ys + len;
+    const int64_t first = (int64_t)((uintptr_t)y.data - (uintptr_t)x.data), stretch = tokens > 1 ? x.token_stride * e : x_far + y_far;
+    if (tokens > 1 && (x.token_stride != y.token_stride || x_far > stretch || y_far > stretch)) return true;
+    const int64_t at = tokens > 1 ? (first % stretch + stretch) % stretch : first;     // of y in x's stretch (one token: anywhere)
+    // heads that follow one another closely are one piece
+    const int64_t x_len = xs <= len ? x_far : len, y_len = ys <= len ? y_far : len;
+    for (int i = 0; i < (xs <= len ? 1 : x_heads); ++i)
+        for (int j = 0; j < (ys <= len ? 1 : y_heads); ++j)
+            for (int64_t a = at + j * ys - i * xs - (tokens > 1 ? stretch : 0), turn = 0; turn < (tokens > 1 ? 3 : 1); ++turn, a += stretch)
+                if (a < x_len && a + y_len > 0) return true;     // (the stretch before, this one, the one behind)
+    return false;
+}
+
 ccv3d_status check_cache(const ccv3d_kv_cache* c) {
     if (!c || !c->codes || !c->scales || c->pages < 1 || c->kv_heads < 1) return CCV3D_ERR_INVALID_ARG;
     if (c->page_tokens != 16 && c->page_tokens != 32 && c->page_tokens != 64 && c->page_tokens != 128) return CCV3D_ERR_UNSUPPORTED;
@@ -109,6 +128,14 @@ Span codes_span(const ccv3d_kv_cache* c) {
     return span_of(c->codes, (int64_t)c->pages * 2 * c->kv_heads * c->page_tokens * c->head_dim);
 }
 Span scales_span(const ccv3d_kv_cache* c) { return span_of(c->scales, (int64_t)c->pages * 2 * c->kv_heads * 4); }
+bool meets_batch(const Span& x, const ccv3d_token_batch* b) {
+    return meet(x, span_of(b->new_start, (b->batch + 1LL) * 4)) || meet(x, span_of(b->total, b->batch * 4LL)) ||
+           meet(x, span_of(b->page_table, (int64_t)b->batch * b->max_pages * 4));
+}
+bool meets_rotary(const Span& x, const ccv3d_rotary* r, int64_t tokens) {
+    const int64_t table = (int64_t)r->rows * r->pairs * 4;
+    return meet(x, span_of(r->cos_table, table)) || meet(x, span_of(r->sin_table, table)) || meet(x, span_of(r->positions, tokens * r->axes * 4));
+}
 
 template <typename T, int D, int P, bool FEW>
 ccv3d_status launch_append_as(AppendParams& p, cudaStream_t st) {
@@ -337,14 +364,15 @@ ccv3d_status ccv3d_kv_append(const ccv3d_kv_cache* cache, const ccv3d_token_batc
     }
     const Span sc = codes_span(cache), ss = scales_span(cache), sk = span_of(*k, tokens, H, D, dtype), sv = span_of(*v, tokens, H, D, dtype);
     if (meet(sc, ss) || meet(sc, sk) || meet(sc, sv) || meet(ss, sk) || meet(ss, sv)) return CCV3D_ERR_ALIAS;
+    if (meets_batch(sc, batch) || meets_batch(ss, batch) || (rot && (meets_rotary(sc, rot, tokens) || meets_rotary(ss, rot, tokens)))) return CCV3D_ERR_ALIAS;
     if (q) {
         if ((s = check_heads(q, q_heads, D, dtype)) != CCV3D_OK || (s = check_heads(q_out, q_heads, D, dtype, tokens)) != CCV3D_OK) return s;
         const Span a = span_of(*q, tokens, q_heads, D, dtype), b = span_of(*q_out, tokens, q_heads, D, dtype);
         const bool self = q->data == q_out->data && q->token_stride == q_out->token_stride && q->head_stride == q_out->head_stride;
-        if (!self && meet(a, b)) return CCV3D_ERR_ALIAS;
+        if (!self && share(*q, q_heads, *q_out, q_heads, tokens, D, dtype)) return CCV3D_ERR_ALIAS;
+        if (share(*k, H, *q_out, q_heads, tokens, D, dtype) || share(*v, H, *q_out, q_heads, tokens, D, dtype)) return CCV3D_ERR_ALIAS;
         if (meet(b, sc) || meet(b, ss) || meet(a, sc) || meet(a, ss)) return CCV3D_ERR_ALIAS;
-        // in place among slices of one projection the ranges of q, k and v interleave: only a dense overlap is an error
-        if (!self && (meet(b, sk) || meet(b, sv))) return CCV3D_ERR_ALIAS;
+        if (meets_batch(b, batch) || (rot && meets_rotary(b, rot, tokens))) return CCV3D_ERR_ALIAS;
     }
     Device dev;
     if ((s = current_device(&dev)) != CCV3D_OK) return s;
@@ -383,16 +411,16 @@ ccv3d_status ccv3d_kv_attend(const ccv3d_kv_cache* cache, const ccv3d_token_batc
     if ((s = check_heads(q, q_heads, D, dtype)) != CCV3D_OK || (s = check_heads(out, q_heads, D, dtype, tokens)) != CCV3D_OK) return s;
     if (misaligned(lse, 4) || misaligned(ws, 256)) return CCV3D_ERR_ALIGNMENT;
     const Span a = span_of(*q, tokens, q_heads, D, dtype), o = span_of(*out, tokens, q_heads, D, dtype), sc = codes_span(cache), ss = scales_span(cache);
-    if (meet(a, o) || meet(o, sc) || meet(o, ss)) return CCV3D_ERR_ALIAS;
+    if (meet(a, o) || meet(o, sc) || meet(o, ss) || meets_batch(o, batch)) return CCV3D_ERR_ALIAS;
     if (lse) {
         const Span l = span_of(lse, (int64_t)tokens * q_heads * 4);
-        if (meet(l, a) || meet(l, o) || meet(l, sc) || meet(l, ss)) return CCV3D_ERR_ALIAS;
+        if (meet(l, a) || meet(l, o) || meet(l, sc) || meet(l, ss) || meets_batch(l, batch)) return CCV3D_ERR_ALIAS;
     }
     if (!ws || ws_bytes == 0) return CCV3D_ERR_NOMEM;
     if ((s = plan_attend(cache, batch, q_heads, dtype, &pl)) != CCV3D_OK) return s;
     if (ws_bytes < pl.bytes) return CCV3D_ERR_NOMEM;
     const Span w = span_of(ws, (int64_t)pl.bytes);
-    if (meet(w, a) || meet(w, o) || meet(w, sc) || meet(w, ss)) return CCV3D_ERR_ALIAS;
+    if (meet(w, a) || meet(w, o) || meet(w, sc) || meet(w, ss) || meets_batch(w, batch)) return CCV3D_ERR_ALIAS;
     if (lse && meet(w, span_of(lse, (int64_t)tokens * q_heads * 4))) return CCV3D_ERR_ALIAS;
     AttendParams p = {};
     p.c = *cache;
