@@ -491,6 +491,9 @@ ccv3d_status ccv3d_kv_append(const ccv3d_kv_cache* cache, const ccv3d_token_batc
  *   window >= 0: none that lies more than `window` tokens before the start of its own frame (frame = 0: before itself).
  * A token that sees nothing (more new tokens than cached ones) gets zeros and lse = -infinity.  What a token does not
  * see (stale codes at a page's end, NaN included) has no part in its result.
+ * CCV3D_ERR_UNSUPPORTED: head numbers, page tables or rows past 32 bits, or more than 2e9 units of work, (tokens * g / r + batch)
+ * * kv_heads * (max_pages * page_tokens / 128 + 1) for g = q_heads / kv_heads and r = 8, 16, 256 (F32: 128) where max_new * g
+ * is at most 8, at most 32, or more.
  * q, out: `dtype` (BF16 or F32; F32 is computed to FP32 accuracy).  Scores, softmax statistics and sums are FP32.
  *   q_heads   a multiple of kv_heads
  *   ws        DEVICE scratch, 256-byte aligned, ccv3d_kv_attend_workspace() bytes; holds data within the call only,

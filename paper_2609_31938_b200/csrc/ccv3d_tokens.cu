@@ -104,7 +104,7 @@ ccv3d_status check_cache(const ccv3d_kv_cache* c) {
 ccv3d_status check_batch(const ccv3d_token_batch* b, int page_tokens) {
     if (!b || !b->new_start || !b->total || b->batch < 1 || b->max_pages < 0 || b->tokens < 0 || b->max_new < 0) return CCV3D_ERR_INVALID_ARG;
     if (!b->page_table && b->max_pages > 0) return CCV3D_ERR_INVALID_ARG;
-    if ((int64_t)b->max_pages * page_tokens > 0x7FFFFFFF || b->batch > 65536) return CCV3D_ERR_UNSUPPORTED;
+    if ((int64_t)b->max_pages * page_tokens > 0x7FFFFF00 || b->batch > 65536) return CCV3D_ERR_UNSUPPORTED;    // (room for a unit more)
     if (misaligned(b->new_start, 4) || misaligned(b->total, 4) || misaligned(b->page_table, 4)) return CCV3D_ERR_ALIGNMENT;
     return CCV3D_OK;
 }
@@ -227,6 +227,14 @@ ccv3d_status launch_norm(const NormParams& p, bool vec, const Device& dev, cudaS
     return CCV3D_ERR_UNSUPPORTED;
 }
 
+// Query rows of an item (8 or 16: step kernel, 128 or 256: tile kernel) where the sequences of a call have up to `rows` of a kv head.
+// The step kernel reads the cache once for every 8 or 16 rows, the tile kernel once for all but always in products of 128
+// rows.  Device time, us, BF16 (F32), 16 heads on 4, 64 streams of 2000 tokens, 8-row items / 16-row items / tiles:
+//   8 rows 43 (47) / 51 (64) / 96 (119);  16 rows - / 55 (66) / 96 (121);  32 rows - / 90 (112) / 96 (125);
+//   48 rows - / 125 (156) / 98 (125);  128 rows - / 293 (371) / 105 (133)
+// (one stream of 32768: 32 rows 33 (39) / 37 (41), 48 rows 43 (53) / 37 (41); two of 500, up to 128 rows: 16 to 20 / 25)
+int rows_per_item(int64_t rows, int dtype) { return rows <= 8 ? 8 : rows <= 32 ? 16 : dtype == CCV3D_BF16 ? 256 : 128; }
+
 ccv3d_status check_attend(const ccv3d_kv_cache* cache, const ccv3d_token_batch* batch, int q_heads, int dtype) {
     ccv3d_status s = check_cache(cache);
     if (s != CCV3D_OK) return s;
@@ -236,9 +244,10 @@ ccv3d_status check_attend(const ccv3d_kv_cache* cache, const ccv3d_token_batch* 
     // 32-bit row numbers (TMA coordinates, query rows) and unit numbers
     if ((int64_t)cache->pages * 2 * cache->kv_heads * cache->page_tokens > 0x7FFFFFFF) return CCV3D_ERR_UNSUPPORTED;
     if ((int64_t)batch->tokens * q_heads > 0x7FFFFFFF) return CCV3D_ERR_UNSUPPORTED;
-    const int64_t units = (int64_t)batch->max_pages * cache->page_tokens / STEP_UNIT + 1;
-    const double all = (double)batch->batch * cache->kv_heads * (((double)batch->max_new * group) / 8 + 1) * units;
-    if (all > 2e9) return CCV3D_ERR_UNSUPPORTED;
+    // items of `per` rows: of a batch whose sequences all bring max_new tokens, and of all the rows there are, whichever is fewer
+    const int64_t units = (int64_t)batch->max_pages * cache->page_tokens / STEP_UNIT + 1, per = rows_per_item(batch->max_new * group, dtype);
+    const int64_t by_batch = batch->batch * ((batch->max_new * group + per - 1) / per), by_rows = batch->tokens * group / per + batch->batch;
+    if ((double)(by_batch < by_rows ? by_batch : by_rows) * cache->kv_heads * units > MAX_UNITS) return CCV3D_ERR_UNSUPPORTED;
     return CCV3D_OK;
 }
 
@@ -255,12 +264,7 @@ ccv3d_status plan_attend(const ccv3d_kv_cache* cache, const ccv3d_token_batch* b
     if (s != CCV3D_OK) return s;
     if ((s = current_device(&pl->dev)) != CCV3D_OK) return s;
     const int64_t rows = (int64_t)batch->max_new * (q_heads / cache->kv_heads);
-    // The step kernel reads the cache once for every 8 or 16 rows, the tile kernel once for all but always in products of 128
-    // rows.  Device time, us, BF16 (F32), 16 heads on 4, 64 streams of 2000 tokens, 8-row items / 16-row items / tiles:
-    //   8 rows 43 (47) / 51 (64) / 96 (119);  16 rows - / 55 (66) / 96 (121);  32 rows - / 90 (112) / 96 (125);
-    //   48 rows - / 125 (156) / 98 (125);  128 rows - / 293 (371) / 105 (133)
-    // (one stream of 32768: 32 rows 33 (39) / 37 (41), 48 rows 43 (53) / 37 (41); two of 500, up to 128 rows: 16 to 20 / 25)
-    pl->rows_per_item = rows <= 8 ? 8 : rows <= 32 ? 16 : dtype == CCV3D_BF16 ? 256 : 128;
+    pl->rows_per_item = rows_per_item(rows, dtype);
     const bool tile = pl->rows_per_item >= 128;
     pl->blocks = tile ? pl->dev.sm_count : (pl->rows_per_item == 8 ? STEP_BLOCKS : 2) * pl->dev.sm_count;
     if (pl->blocks > JOIN_PARTS) pl->blocks = JOIN_PARTS;

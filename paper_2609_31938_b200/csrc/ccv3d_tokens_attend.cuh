@@ -38,6 +38,9 @@ struct AttendParams {
     int slot_rows;
 };
 
+// Most units of a call.  The host bounds them by the rows of the packed tensors and the page tables' room; offsets that fall can
+// name rows again and again, and a list that so grows past the bound is not walked at all.
+constexpr int MAX_UNITS = 2000000000;
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 
 __device__ __forceinline__ float exp2_fast(float x) {

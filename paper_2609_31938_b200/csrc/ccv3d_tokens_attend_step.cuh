@@ -114,7 +114,11 @@ __device__ __forceinline__ StepWalk step_share(const AttendParams& p, int rows_p
     for (int b0 = 0; b0 < p.bt.batch; b0 += 32) {
         int items = 0, units = 0, lo, hi;
         if (b0 + lane < p.bt.batch) StepWalk::measure(p, rows_per_item, load_seq(p.bt, p.c.page_tokens, b0 + lane, p.status), items, units, lo, hi);
-        total += __reduce_add_sync(0xffffffffu, items * units);
+        total += warp_sum_wide(items * units);
+    }
+    if (total > MAX_UNITS) {
+        report(p.status, CCV3D_TOKENS_BAD_LENGTH);
+        total = 0;
     }
     StepWalk w;
     w.total = total;

@@ -154,8 +154,8 @@ __device__ __forceinline__ TileWalk<ROWS> tile_share(const AttendParams& p, int*
             }
             for (int b0 = 0; b0 < n && !found; b0 += 32) {
                 const int mine = b0 + lane < n ? cost_of[b0 + lane] : 0;
+                if (pass == 0) { w.total += warp_sum_wide(mine); continue; }
                 const int upto = warp_scan(mine), all = __shfl_sync(0xffffffffu, upto, 31);
-                if (pass == 0) { w.total += all; continue; }
                 const unsigned hit = __ballot_sync(0xffffffffu, mine > 0 && (int64_t)w.u < before + upto);
                 if (!hit) { before += all; continue; }
                 const int who = __ffs(hit) - 1;
@@ -179,6 +179,10 @@ __device__ __forceinline__ TileWalk<ROWS> tile_share(const AttendParams& p, int*
             }
         }
         if (pass == 0) {
+            if (w.total > MAX_UNITS) {
+                if (threadIdx.x == 0) report(p.status, CCV3D_TOKENS_BAD_LENGTH);
+                w.total = 0;
+            }
             w.blocks = min((int64_t)gridDim.x, w.total);
             if ((int64_t)blockIdx.x < w.blocks) {
                 w.u = (int)(w.total * blockIdx.x / w.blocks);

@@ -87,10 +87,14 @@ __device__ __forceinline__ Seq load_seq(const ccv3d_token_batch& bt, int page_to
     if (s < 0 || e < s || e > bt.tokens || t < 0 || t > room || e - s > bt.max_new) {
         report(status, CCV3D_TOKENS_BAD_LENGTH);
         s = min(max(s, 0), bt.tokens);
-        e = min(max(e, s), min(bt.tokens, s + bt.max_new));
+        e = min(max(e, s), s + min(bt.tokens - s, bt.max_new));
         t = (int)min((long long)max(t, 0), room);
     }
     return {s, e - s, t};
+}
+// Sum over the warp of numbers below 2^31, which itself may lie beyond.
+__device__ __forceinline__ long long warp_sum_wide(int v) {
+    return ((long long)__reduce_add_sync(0xffffffffu, (unsigned)v >> 16) << 16) + __reduce_add_sync(0xffffffffu, (unsigned)v & 0xFFFFu);
 }
 // Page of a sequence's j-th block of tokens, or -1 (reported) where the table names none of the pool's.
 __device__ __forceinline__ int load_page(const ccv3d_token_batch& bt, const ccv3d_kv_cache& c, int b, int j, uint32_t* status) {

@@ -33,3 +33,40 @@ def test_append_among_slices_that_do_not_overlap(new):
         assert cache.append(k, v, batch, rotary, pos, q=q_in, q_out=q_out) is q_out
         assert torch.equal(q_out, q) and torch.equal(cache.scales, want.scales) and torch.equal(cache.codes, want.codes)
         assert torch.equal(k.cpu(), c.k) and torch.equal(v.cpu(), c.v)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_attend_prompt_beside_single_tokens_with_wide_tables(dtype):
+    """One prompt of 8192 tokens beside 63 streams of one, tables for 131072 tokens: every stream, and rows all over the prompt."""
+    n = [1] * 40 + [8192] + [1] * 23
+    c = ref.Case(n, [(i * 37) % 150 for i in range(40)] + [0] + [5 * i for i in range(23)], 32, 8, 64, 64, dtype, seed=11, stale=0x7F)
+    c.table = torch.nn.functional.pad(c.table, (0, 2048 - c.table.shape[1]), value=-1)
+    cache, batch = c.on_gpu()
+    got = cache.attend(c.q.cuda(), batch).cpu().double()
+    assert cache.status() == 0
+    kv = ref.decode(c.codes, c.scales)
+    for b, new in enumerate(n):
+        total, first = int(c.total[b]), int(c.starts[b])
+        pages = c.table[b, :-(-total // 64)].long()
+        k, v = (kv[pages, j].transpose(0, 1).reshape(8, -1, 64) for j in range(2))
+        for i in [0] if new == 1 else [0, 1, 63, 64, 127, 128, 1000, 4097, 8190, 8191]:
+            upto = total - new + i + 1
+            q = c.q[first + i].double().view(8, 4, 64)
+            x = torch.einsum("hgd,htd->hgt", q, k[:, :upto]) / 8
+            p = torch.softmax(x, -1)
+            want, mass = (torch.einsum("hgt,htd->hgd", p, u).reshape(32, 64) for u in (v[:, :upto], v[:, :upto].abs()))
+            spread = (torch.einsum("hgd,htd->hgt", q.abs(), k[:, :upto].abs()) / 8).amax(-1).reshape(32, 1)
+            u = 2.0 ** -8 if dtype == BF16 else 2.0 ** -24
+            tol = u * want.abs() + mass * ((2.0 ** -11 if dtype == BF16 else 2.0 ** -20) + 2 * 64 * 2.0 ** -24 * spread)
+            assert ((got[first + i] - want).abs() <= tol).all(), (b, i)
+
+
+@pytest.mark.parametrize("new", [1, 60])
+def test_offsets_that_fall_are_reported(new):
+    import paper_2609_31938_b200 as ccv
+    c = ref.Case([new] * 6, [100] * 6, 4, 2, 64, 16, BF16, seed=15)
+    c.starts[2], c.starts[4] = 0, 0                      # rows named again and again
+    cache, batch = c.on_gpu()
+    cache.attend(c.q.cuda(), batch)
+    cache.append(c.k.cuda(), c.v.cuda(), batch)
+    assert cache.status() == ccv.TOKENS_BAD_LENGTH
