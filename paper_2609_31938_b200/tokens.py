@@ -65,7 +65,7 @@ class TokenBatch:
     """The sequences of a call (``ccv3d_token_batch``): packed offsets of their new tokens [batch + 1], their lengths
     with the new tokens [batch], and their page tables [batch, max_pages], int32 on the device.  The arrays may be
     changed in place between calls (a captured graph replays with what they hold then); ``max_new`` bounds the new
-    tokens of any sequence, ``tokens`` (default: what the call's tensors hold) the rows."""
+    tokens of any sequence.  A batch and a rotation may serve several calls at a time: no call writes to them."""
 
     def __init__(self, new_start, total, page_table, max_new: int):
         dev = _device()
@@ -75,8 +75,17 @@ class TokenBatch:
         _int_array(page_table, "page_table", (b, page_table.shape[1]), dev)
         self.new_start, self.total, self.page_table, self.max_new = new_start, total, page_table, int(max_new)
         self.device = dev
-        self.c = TokenBatchC(new_start.data_ptr(), total.data_ptr(), page_table.data_ptr(), b, page_table.shape[1], 0,
-                             self.max_new)
+        self._at = (new_start.data_ptr(), total.data_ptr(), page_table.data_ptr(), b, page_table.shape[1])
+        self._c = {}
+
+    def c(self, tokens: int) -> TokenBatchC:
+        """The struct of a call with so many rows (kept, and not written again)."""
+        c = self._c.get(tokens)
+        if c is None:
+            if len(self._c) >= 64:
+                self._c = {}
+            c = self._c[tokens] = TokenBatchC(*self._at, tokens, self.max_new)
+        return c
 
 
 class Rotary:
@@ -92,9 +101,15 @@ class Rotary:
         sections = tuple(int(s) for s in (sections or (cos.shape[1],)))
         if not 1 <= len(sections) <= 3 or sum(sections) != cos.shape[1]:
             raise ValueError(f"sections {sections} do not split {cos.shape[1]} pairs among one to three axes")
-        self.cos, self.sin, self.axes = cos, sin, len(sections)
+        self.cos, self.sin, self.axes = cos, sin, len(sections)      # (the struct without positions: `at` adds a call's)
         self.c = RotaryC(cos.data_ptr(), sin.data_ptr(), None, cos.shape[0], cos.shape[1], len(sections),
                          (ctypes.c_int32 * 3)(*sections, *([0] * (3 - len(sections)))), int(bool(interleaved)))
+
+    def at(self, positions: torch.Tensor) -> RotaryC:
+        """The struct of a call with these positions: its own, as several calls may be made at a time."""
+        r = RotaryC.from_buffer_copy(self.c)
+        r.positions = positions.data_ptr()
+        return r
 
 
 class PagedCache:
@@ -136,8 +151,7 @@ class PagedCache:
             raise ValueError("the batch lies on another device than the cache")
         if _device() != self.device:
             raise ValueError(f"the cache lies on cuda:{self.device}, which is not the current device")
-        batch.c.tokens = tokens
-        return batch.c
+        return batch.c(tokens)
 
     def _workspace(self, c: TokenBatchC, heads: int, dt: int, stream: int):
         """Scratch for an attend call on `stream`: kept for the next call on it, so calls on other streams never share it.
@@ -179,8 +193,7 @@ class PagedCache:
             _int_array(positions, "positions", (tokens, rotary.axes), dev)
             if rotary.cos.get_device() != dev:
                 raise ValueError("the rotation lies on another device than the cache")
-            r = rotary.c
-            r.positions = positions.data_ptr()
+            r = rotary.at(positions)
         cq = cqo = None
         heads = 0
         if q is not None:

@@ -1,0 +1,90 @@
+"""The tensor-level binding of the token operators on the CPU: tensors without a device and a library that only looks at what
+it is called with.  Calls of several threads at a time, what they may share and what not."""
+import threading
+
+import pytest
+
+torch = pytest.importorskip("torch")
+
+import paper_2609_31938_b200 as ccv  # noqa: E402
+from paper_2609_31938_b200 import tokens as tk  # noqa: E402
+
+
+class Library:
+    """Entry points whose calls meet at `gate` (all threads are inside one at that time) and note what they then find."""
+
+    def __init__(self, threads=1):
+        self.gate, self.seen, self.lock, self.inside = threading.Barrier(threads, timeout=20), [], threading.Lock(), 0
+
+    def note(self, *what):
+        self.gate.wait()
+        with self.lock:
+            self.seen.append((threading.current_thread().name, *what))
+        self.gate.wait()
+        return ccv.OK
+
+    def ccv3d_kv_append(self, cache, batch, k, v, rot, q, q_out, heads, dt, status, stream):
+        return self.note(batch, k.data, rot)
+
+    def ccv3d_kv_attend(self, cache, batch, q, out, lse, heads, dt, scale, frame, window, ws, n, status, stream):
+        return self.note(batch, q.data, ws)
+
+
+@pytest.fixture
+def binding(monkeypatch):
+    """`tokens` on tensors of the CPU (their device number is -1)."""
+    monkeypatch.setattr(tk, "_device", lambda: -1)
+    monkeypatch.setattr(tk, "_stream", lambda dev: 7)
+    monkeypatch.setattr(tk, "_capturing", lambda: False)
+    monkeypatch.setattr(tk, "ccv3d_kv_attend_workspace", lambda *a: (ccv.OK, 512))
+
+    def use(library):
+        monkeypatch.setattr(tk, "lib", library)
+        return library
+    return use
+
+
+def cache():
+    return tk.PagedCache(torch.zeros(4, 2, 2, 16, 64, dtype=torch.uint8), torch.zeros(4, 2, 2))
+
+
+def ints(*v):
+    return torch.tensor(v, dtype=torch.int32)
+
+
+def batch(n):
+    return tk.TokenBatch(ints(0, n), ints(n), ints(0, 1)[None], n)
+
+
+def together(*calls):
+    threads = [threading.Thread(target=f, name=str(i)) for i, f in enumerate(calls)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+
+
+def test_threads_share_a_rotation_and_a_batch(binding):
+    """Two caches of a model, one rotation, one batch object: each call has its own positions and number of rows."""
+    lib = binding(Library(2))
+    rotary, shared = tk.Rotary(torch.ones(8, 32), torch.zeros(8, 32)), batch(9)
+    k = [torch.zeros(n, 2, 64) for n in (5, 3)]
+    pos = [torch.zeros(n, 1, dtype=torch.int32) for n in (5, 3)]
+    caches = [cache(), cache()]
+    together(*[lambda i=i: caches[i].append(k[i], k[i], shared, rotary, pos[i]) for i in (0, 1)])
+    assert len(lib.seen) == 2
+    for name, b, at, rot in lib.seen:
+        i = int(name)
+        assert at == k[i].data_ptr()
+        assert rot.positions == pos[i].data_ptr() and rot.cos_table == rotary.cos.data_ptr()
+        assert (b.tokens, b.max_new, b.new_start) == (5 - 2 * i, 9, shared.new_start.data_ptr())
+
+
+def test_structs_of_a_batch_are_kept_but_not_without_end(binding):
+    binding(Library())
+    b = batch(9)
+    first = b.c(5)
+    assert b.c(5) is first and first.tokens == 5
+    for n in range(1000):
+        assert b.c(n).tokens == n
+    assert len(b._c) <= 64 and first.tokens == 5
