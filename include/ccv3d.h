@@ -497,7 +497,8 @@ ccv3d_status ccv3d_kv_append(const ccv3d_kv_cache* cache, const ccv3d_token_batc
  * q, out: `dtype` (BF16 or F32; F32 is computed to FP32 accuracy).  Scores, softmax statistics and sums are FP32.
  *   q_heads   a multiple of kv_heads
  *   ws        DEVICE scratch, 256-byte aligned, ccv3d_kv_attend_workspace() bytes; holds data within the call only,
- *             calls that may overlap on the GPU need one each
+ *             calls that may overlap on the GPU need one each, and so do calls that two host threads make at a time,
+ *             even on one stream (a call is two launches)
  * An overlap of out, lse or ws with an input is CCV3D_ERR_ALIAS.  Stream-ordered, no allocation, legal in a stream capture.
  */
 ccv3d_status ccv3d_kv_attend(const ccv3d_kv_cache* cache, const ccv3d_token_batch* batch, const ccv3d_heads* q,

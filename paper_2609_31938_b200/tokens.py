@@ -7,6 +7,7 @@ memory and the stream (its current one); every step runs in ``libccv3d.so`` (``c
 from __future__ import annotations
 
 import ctypes
+import threading
 
 import torch
 
@@ -133,6 +134,7 @@ class PagedCache:
         self._status_ptr = self._status.data_ptr()
         self._needs = {}         # geometry of a call -> bytes of scratch
         self._scratch = {}       # stream -> scratch of attend calls on it
+        self._lock = threading.Lock()
 
     @classmethod
     def empty(cls, pages, kv_heads, head_dim, page_tokens=64):
@@ -155,7 +157,8 @@ class PagedCache:
 
     def _workspace(self, c: TokenBatchC, heads: int, dt: int, stream: int):
         """Scratch for an attend call on `stream`: kept for the next call on it, so calls on other streams never share it.
-        A captured call gets its own, which belongs to the graph."""
+        A captured call gets its own, which belongs to the graph.  Called, and the scratch put to use, under the lock: an
+        attend call is two launches, and those of two host threads on one stream must not come in between."""
         key = (c.max_new, c.batch, c.max_pages, c.tokens, heads, dt)
         need = self._needs.get(key)
         if need is None:
@@ -232,10 +235,11 @@ class PagedCache:
             co = _heads(out, "out", tokens, dim, dev)
         lse = q.new_empty((tokens, heads), dtype=torch.float32) if want_lse else None
         stream = _stream(dev)
-        ws, need = self._workspace(c, heads, dt, stream)
-        s = lib.ccv3d_kv_attend(self.c, c, cq, co, None if lse is None else lse.data_ptr(), heads, dt,
-                                dim ** -0.5 if scale is None else scale, frame, window, ws.data_ptr(), need,
-                                self._status_ptr, stream)
+        with self._lock:
+            ws, need = self._workspace(c, heads, dt, stream)
+            s = lib.ccv3d_kv_attend(self.c, c, cq, co, None if lse is None else lse.data_ptr(), heads, dt,
+                                    dim ** -0.5 if scale is None else scale, frame, window, ws.data_ptr(), need,
+                                    self._status_ptr, stream)
         if s != OK:
             raise Ccv3dError(s, "ccv3d_kv_attend")
         return (out, lse) if want_lse else out

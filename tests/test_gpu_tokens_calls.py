@@ -70,3 +70,26 @@ def test_offsets_that_fall_are_reported(new):
     cache.attend(c.q.cuda(), batch)
     cache.append(c.k.cuda(), c.v.cuda(), batch)
     assert cache.status() == ccv.TOKENS_BAD_LENGTH
+
+
+def test_attend_from_threads_on_one_stream():
+    """Eight threads on the default stream, each with queries of its own, all items split over blocks: the bits of calls in turn."""
+    import threading
+    c = ref.Case([1, 1], [3000, 2500], 8, 2, 64, 32, BF16, seed=19)
+    cache, batch = c.on_gpu()
+    g = torch.Generator(device="cuda").manual_seed(1)
+    qs = [torch.randn(2, 8, 64, generator=g, device="cuda").to(BF16) for _ in range(8)]
+    want = [cache.attend(q, batch) for q in qs]
+    got = [[] for _ in qs]
+
+    def work(i):
+        for _ in range(50):
+            got[i].append(cache.attend(qs[i], batch))
+
+    threads = [threading.Thread(target=work, args=(i,)) for i in range(8)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert all(len(a) == 50 and all(torch.equal(o, w) for o in a) for a, w in zip(got, want))
+    assert cache.status() == 0

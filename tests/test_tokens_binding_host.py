@@ -88,3 +88,24 @@ def test_structs_of_a_batch_are_kept_but_not_without_end(binding):
     for n in range(1000):
         assert b.c(n).tokens == n
     assert len(b._c) <= 64 and first.tokens == 5
+
+
+def test_threads_on_one_stream_do_not_use_one_scratch_at_a_time(binding):
+    """An attend call is two launches that scratch connects: no other call may be given it in between."""
+    class Slow(Library):
+        busy, clashes, calls = set(), 0, 0
+
+        def ccv3d_kv_attend(self, cache, batch, q, out, lse, heads, dt, scale, frame, window, ws, n, status, stream):
+            with self.lock:
+                self.clashes += ws in self.busy
+                self.busy.add(ws)
+                self.calls += 1
+            threading.Event().wait(0.01)                 # between the launches
+            with self.lock:
+                self.busy.discard(ws)
+            return ccv.OK
+
+    lib = binding(Slow())
+    c, b = cache(), batch(2)
+    together(*[lambda: [c.attend(torch.zeros(2, 4, 64), b) for _ in range(8)] for _ in range(4)])
+    assert lib.calls == 32 and lib.clashes == 0
