@@ -21,6 +21,7 @@ _device = torch.cuda.current_device
 _stream = torch._C._cuda_getCurrentRawStream
 _like = torch.empty_like
 _capturing = torch._C._cuda_isCurrentStreamCapturing
+_synchronize = torch.cuda.synchronize
 _DENSE = torch.contiguous_format
 
 
@@ -130,7 +131,7 @@ class PagedCache:
         self.codes, self.scales, self.device = codes, scales, dev
         self.pages, _, self.kv_heads, self.page_tokens, self.head_dim = codes.shape
         self.c = KvCache(codes.data_ptr(), scales.data_ptr(), self.pages, self.kv_heads, self.page_tokens, self.head_dim)
-        self._status = torch.zeros(1, dtype=torch.int32, device=codes.device)
+        self._status = torch.zeros(1, dtype=torch.int32).to(codes.device)     # (there when this returns, for every stream)
         self._status_ptr = self._status.data_ptr()
         self._needs = {}         # geometry of a call -> bytes of scratch
         self._scratch = {}       # stream -> scratch of attend calls on it
@@ -142,10 +143,14 @@ class PagedCache:
                    torch.zeros((pages, 2, kv_heads), dtype=torch.float32, device="cuda"))
 
     def status(self) -> int:
-        """TOKENS_* bits that the calls so far have reported (waits for them), cleared by reading."""
-        bits = int(self._status.item())
-        if bits:
-            self._status.zero_()
+        """TOKENS_* bits that the calls so far have reported, cleared by reading.  Waits for the device, as the calls may have
+        gone to any of its streams, and holds back calls of other threads meanwhile (not replays of their graphs)."""
+        with self._lock:
+            _synchronize(self.device)
+            bits = int(self._status.item())
+            if bits:
+                self._status.zero_()
+                _synchronize(self.device)
         return bits
 
     def _batch(self, batch: TokenBatch, tokens: int) -> TokenBatchC:
@@ -211,8 +216,8 @@ class PagedCache:
                 cqo = _heads(q_out, "q_out", tokens, dim, dev)
         elif q_out is not None:
             raise ValueError("q_out without q")
-        s = lib.ccv3d_kv_append(self.c, c, ck, cv, r, cq, cqo, heads, dt, self._status_ptr,
-                                _stream(dev))
+        with self._lock:         # (see status)
+            s = lib.ccv3d_kv_append(self.c, c, ck, cv, r, cq, cqo, heads, dt, self._status_ptr, _stream(dev))
         if s != OK:
             raise Ccv3dError(s, "ccv3d_kv_append")
         return q_out

@@ -93,3 +93,19 @@ def test_attend_from_threads_on_one_stream():
         t.join()
     assert all(len(a) == 50 and all(torch.equal(o, w) for o in a) for a, w in zip(got, want))
     assert cache.status() == 0
+
+
+def test_status_covers_calls_on_other_streams():
+    """A bad page reported behind half a second of other work on a side stream, asked for from the default stream."""
+    import paper_2609_31938_b200 as ccv
+    c = ref.Case([1], [100], 4, 2, 64, 16, BF16, seed=15)
+    c.table[0, 2] = c.codes.shape[0] + 5
+    cache, batch = c.on_gpu()
+    q = c.q.cuda()
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(1_000_000_000)
+        cache.attend(q, batch)
+    assert cache.status() == ccv.TOKENS_BAD_PAGE
+    assert cache.status() == 0

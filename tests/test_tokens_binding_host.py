@@ -36,6 +36,7 @@ def binding(monkeypatch):
     monkeypatch.setattr(tk, "_device", lambda: -1)
     monkeypatch.setattr(tk, "_stream", lambda dev: 7)
     monkeypatch.setattr(tk, "_capturing", lambda: False)
+    monkeypatch.setattr(tk, "_synchronize", lambda dev: None, raising=False)
     monkeypatch.setattr(tk, "ccv3d_kv_attend_workspace", lambda *a: (ccv.OK, 512))
 
     def use(library):
@@ -109,3 +110,40 @@ def test_threads_on_one_stream_do_not_use_one_scratch_at_a_time(binding):
     c, b = cache(), batch(2)
     together(*[lambda: [c.attend(torch.zeros(2, 4, 64), b) for _ in range(8)] for _ in range(4)])
     assert lib.calls == 32 and lib.clashes == 0
+
+
+def test_status_waits_for_every_stream(binding, monkeypatch):
+    """Reports that arrive only once the device was waited for are read, and nothing is left for the next reading."""
+    binding(Library())
+    c, late = cache(), [4, 0]
+    monkeypatch.setattr(tk, "_synchronize", lambda dev: c._status.bitwise_or_(late.pop(0) if late else 0), raising=False)
+    c._status[0] = 1
+    assert c.status() == 5
+    assert c.status() == 0
+
+
+def test_status_does_not_come_between_a_call_and_its_report(binding):
+    """A call under way, in append or attend, is waited for: its report is neither missed nor wiped away."""
+    class Reporting(Library):
+        def ccv3d_kv_append(self, *a):
+            return self.report(1)
+
+        def ccv3d_kv_attend(self, *a):
+            return self.report(2)
+
+        def report(self, bit):
+            entered.set()
+            threading.Event().wait(0.1)
+            c._status.bitwise_or_(bit)
+            return ccv.OK
+
+    binding(Reporting())
+    c, b, x = cache(), batch(2), torch.zeros(2, 2, 64)
+    for bit, call in ((1, lambda: c.append(x, x, b)), (2, lambda: c.attend(x, b))):
+        entered = threading.Event()
+        t = threading.Thread(target=call)
+        t.start()
+        assert entered.wait(20)
+        assert c.status() == bit
+        t.join()
+        assert c.status() == 0
