@@ -12,7 +12,9 @@ are random and there is no claim about what it predicts; it shows the operators 
                 residual += gate * norm(silu(h W1) W2)                                             (with the next block's)
 
 The cache is paged: pages of frames that have left the window go back to the pool, so a stream of any length runs in a
-fixed amount of memory, as the chain does with its frame rings.
+fixed amount of memory, as the chain does with its frame rings.  Its rotation tables are of a fixed length, too: along the
+frames, pairs turn by whole numbers of turns in as many frames as a table has rows, so that a frame's row is its number
+modulo the rows and the angle between two frames is that of their distance wherever the stream stands.
 
     python -m paper_2609_31938_b200.predictor [frames]
 """
@@ -41,8 +43,12 @@ class LatentPredictor:
         self.modulation = rnd(channels, blocks * 6 * channels, a=0.3 * channels ** -0.5)
         pairs = head_dim // 2
         sections = (pairs - 2 * (pairs * 3 // 8), pairs * 3 // 8, pairs * 3 // 8)
-        rows = max(256, height, width)
-        angle = torch.arange(rows, dtype=torch.float64)[:, None] * 10000.0 ** (-torch.arange(pairs, dtype=torch.float64) / pairs)
+        rows = max(256, height, width, 8 * (window_frames + 1))
+        speed = 10000.0 ** (-torch.arange(pairs, dtype=torch.float64) / pairs)         # radians a step
+        turns = (speed[:sections[0]] * rows / (2 * math.pi)).round().clamp_min(1)      # along the frames: in `rows` of them
+        steps = torch.arange(rows, dtype=torch.float64)[:, None]
+        angle = steps * speed
+        angle[:, :sections[0]] = steps * turns % rows * (2 * math.pi / rows)
         self.rotary = tk.Rotary(angle.cos().float().cuda(), angle.sin().float().cuda(), sections)
         self.rows = rows
         # pages of window_frames + 1 frames (and one that a frame's border cuts), one table for all blocks

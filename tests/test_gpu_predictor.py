@@ -83,3 +83,36 @@ def test_stream_restarts_and_frames_that_cut_pages():
     again = [m.step(x, c) for x, c in xs]
     assert all(torch.equal(a, b) for a, b in zip(first, again)) and all(torch.isfinite(a).all() for a in first)
     assert all(c.status() == 0 for c in m.caches)
+
+
+def test_stream_past_the_end_of_the_rotation_tables():
+    """A stream that begins some frames before its tables wrap predicts what one beginning at frame 0 does: attention only
+    knows the distance of two frames."""
+    if not torch.cuda.is_available():
+        pytest.skip("no CUDA device")
+    from paper_2609_31938_b200.predictor import LatentPredictor
+    m = LatentPredictor(channels=96, heads=6, kv_heads=2, head_dim=64, blocks=2, height=8, width=16, window_frames=2, page_tokens=32)
+    m.frame = m.origin = m.rows - 3
+    g = torch.Generator(device="cuda").manual_seed(5)
+    seen = []
+    for f in range(8):
+        x, cond = torch.randn(m.n, 96, generator=g, device="cuda"), torch.randn(96, generator=g, device="cuda")
+        want = plain_step(m, x, cond, seen)                # (counts its frames from 0)
+        got = m.step(x, cond).double().cpu()
+        rel = ((got - want).square().mean() / want.square().mean()).sqrt().item()
+        assert rel <= 0.03, (f, rel)
+    assert all(c.status() == 0 for c in m.caches)
+
+
+def test_frame_axis_turns_whole_times_in_a_table():
+    """Rows 1 .. rows - 1 and 0 again: the tables' period is their length, and no pair of the frame axis stands still."""
+    if not torch.cuda.is_available():
+        pytest.skip("no CUDA device")
+    from paper_2609_31938_b200.predictor import LatentPredictor
+    m = LatentPredictor(channels=64, heads=2, kv_heads=1, head_dim=64, blocks=1, height=4, width=8, window_frames=70)
+    n = m.rotary.c.section[0]
+    assert m.rows > 2 * (m.window + 1)
+    z = torch.complex(m.rotary.cos[:, :n].double(), m.rotary.sin[:, :n].double()).cpu()
+    step = z[1:] / z[:-1]
+    assert (step - step[0]).abs().max() <= 2e-6 and (z[0] / z[-1] - step[0]).abs().max() <= 2e-6
+    assert ((step[0] - 1).abs() > 1e-3).all()
