@@ -54,6 +54,7 @@ class LatentPredictor:
         # pages of window_frames + 1 frames (and one that a frame's border cuts), one table for all blocks
         self.table_pages = -(-(window_frames + 1) * self.n // page_tokens) + 2
         self.caches = [tk.PagedCache.empty(self.table_pages, kv_heads, head_dim, page_tokens) for _ in range(blocks)]
+        self._reported = [0] * blocks                  # by caches that the pool outgrew
         self.reset()
 
     def reset(self):
@@ -77,11 +78,18 @@ class LatentPredictor:
             if not self.free:                          # a frame that is no whole number of pages keeps its neighbours longer
                 grow = self.table_pages
                 for i, c in enumerate(self.caches):
+                    self._reported[i] |= c.status()
                     self.caches[i] = tk.PagedCache(torch.cat([c.codes, torch.empty_like(c.codes[:grow])]), torch.cat([c.scales, torch.zeros_like(c.scales[:grow])]))
                 self.free = list(range(self.caches[0].pages - grow, self.caches[0].pages))
             self.held.append(self.free.pop(0))
         ints = lambda v: torch.tensor(v, dtype=torch.int32, device="cuda")  # noqa: E731
         return tk.TokenBatch(ints([0, n]), ints([total]), ints([self.held]), max_new=n)
+
+    def status(self):
+        """TOKENS_* bits that the kernels have reported for each block's cache, cleared by reading (waits for the device)."""
+        bits = [c.status() | r for c, r in zip(self.caches, self._reported)]
+        self._reported = [0] * len(bits)
+        return bits
 
     def step(self, x, condition):
         """One frame: x [H * W, channels] (noise, or what a caller has of the frame) and condition [channels] ->
@@ -133,10 +141,10 @@ def main(frames=6):
         end.record()
         end.synchronize()
         print(f"frame {f}: {tuple(z.shape)} -> {tuple(out.shape)}, {start.elapsed_time(end):.2f} ms, rms {out.float().square().mean().sqrt().item():.3f}")
-    bad = [hex(c.status()) for c in model.caches if c.status()]
+    bad = model.status()
     chain.close()
-    if bad:
-        raise SystemExit(f"reported by the cache kernels: {bad}")
+    if any(bad):
+        raise SystemExit(f"reported by the cache kernels: {[hex(b) for b in bad]}")
 
 
 if __name__ == "__main__":

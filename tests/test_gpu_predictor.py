@@ -116,3 +116,30 @@ def test_frame_axis_turns_whole_times_in_a_table():
     step = z[1:] / z[:-1]
     assert (step - step[0]).abs().max() <= 2e-6 and (z[0] / z[-1] - step[0]).abs().max() <= 2e-6
     assert ((step[0] - 1).abs() > 1e-3).all()
+
+
+def test_reports_outlive_a_pool_that_grows(monkeypatch, capsys):
+    """What a block's cache reported is told once, also after the pool grew, and main names the bits."""
+    if not torch.cuda.is_available():
+        pytest.skip("no CUDA device")
+    import paper_2609_31938_b200 as ccv
+    from paper_2609_31938_b200 import predictor
+    m = predictor.LatentPredictor(channels=64, heads=4, kv_heads=1, head_dim=64, blocks=2, height=5, width=7, window_frames=3, page_tokens=64)
+    g = torch.Generator(device="cuda").manual_seed(6)
+    m.caches[1]._status.fill_(ccv.TOKENS_BAD_POSITION)
+    small = m.caches[1].pages
+    for _ in range(12):
+        m.step(torch.randn(35, 64, generator=g, device="cuda"), torch.randn(64, generator=g, device="cuda"))
+    assert m.caches[1].pages > small
+    assert m.status() == [0, ccv.TOKENS_BAD_POSITION]
+    assert m.status() == [0, 0]
+
+    class Reporting(predictor.LatentPredictor):
+        def step(self, x, condition):
+            self.caches[0]._status.fill_(ccv.TOKENS_BAD_PAGE)
+            return super().step(x, condition)
+
+    monkeypatch.setattr(predictor, "LatentPredictor", Reporting)
+    with pytest.raises(SystemExit) as e:
+        predictor.main(1)
+    assert "0x1" in str(e.value)
