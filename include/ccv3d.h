@@ -489,7 +489,8 @@ ccv3d_status ccv3d_kv_append(const ccv3d_kv_cache* cache, const ccv3d_token_batc
  *   frame = 0:  every token;   frame = f >= 1: the tokens before the end of its frame of f tokens (1: causal; the tokens of
  *               a latent frame: causal in frames, whole within one - the temporal rule of the cached convolutions);
  *   window >= 0: none that lies more than `window` tokens before the start of its own frame (frame = 0: before itself).
- * A token that sees nothing (more new tokens than cached ones) gets zeros and lse = -infinity.  What a token does not
+ * A token that sees nothing (more new tokens than cached ones) gets zeros and lse = -infinity, and so does one whose scores are all
+ * -infinity; a score of +infinity (or past the largest FP32 number) or NaN makes its token's outputs and lse NaN.  What a token does not
  * see (stale codes at a page's end, NaN included) has no part in its result.
  * CCV3D_ERR_UNSUPPORTED: head numbers, page tables or rows past 32 bits, or more than 2e9 units of work, (tokens * g / r + batch)
  * * kv_heads * (max_pages * page_tokens / 128 + 1) for g = q_heads / kv_heads and r = 8, 16, 256 (F32: 128) where max_new * g

@@ -55,13 +55,14 @@ __device__ __forceinline__ uint32_t pack_rest(float lo, float hi, uint32_t taken
     const float a = lo - t.x, b = hi - t.y;
     return pack_half(fabsf(a) <= 65504.f ? a : 0.f, fabsf(b) <= 65504.f ? b : 0.f);
 }
-// Power of two that brings the row's largest magnitude into [1, 2), and its reciprocal; 1 for zero and non-finite rows.
+// Power of two that brings the row's largest magnitude into [1, 2), and its reciprocal.  Beside an infinity every finite number
+// stays finite as a half; a NaN is not counted.
 __device__ __forceinline__ void row_power(float most, float& down, float& up) {
     const int e = (int)(__float_as_uint(most) >> 23) - 127;
     const bool plain = e > -126 && e < 126;
     down = plain ? __uint_as_float((uint32_t)(127 - e) << 23) : (most < 1.f ? 8.5070592e37f : 1.f);      // (2^126 for tiny rows)
     up = plain ? __uint_as_float((uint32_t)(127 + e) << 23) : (most < 1.f ? 1.17549435e-38f : 1.f);
-    if (e >= 126 && most <= 3.402823466e38f) { down = 1.17549435e-38f; up = 8.5070592e37f; }
+    if (e >= 126) { down = 1.17549435e-38f; up = 8.5070592e37f; }
 }
 
 // A walk over the units of a block's share of the list.  Every member is the same for all lanes.

@@ -333,10 +333,10 @@ __device__ __forceinline__ TileRow stage_row(const AttendParams& p, const TileSe
             }
         // BF16 s eeeeeeee mmmmmmm to a half s eeeee mmm mmmm000 with the row's largest exponent in the place of 2^14: exponents
         // by a subtraction, both elements at once; what lies 2^-28 under the row's largest becomes zero.  The factor puts
-        // the exponent back; a row with an infinity or a NaN gets NaN for it.
+        // the exponent back.  Infinities and NaN go over as such if their exponent comes in the place of theirs (31).
         const uint32_t most = max(big[0] & 0xFFFFu, big[0] >> 16);
-        const int field = max((int)(most >> 7) - 29, 0);
-        up = most >= 0x7F80u ? __int_as_float(0x7FFFFFFF) : __uint_as_float((uint32_t)(field + 15) << 23);
+        const int field = max((int)(most >> 7) - (most >= 0x7F80u ? 31 : 29), 0);
+        up = __uint_as_float((uint32_t)(field + 15) << 23);
         up = __shfl_sync(0xffffffffu, up, lane % RPI * LPR + lane / RPI);        // of this thread's own row
         const uint32_t off = (uint32_t)(-(field << 7) & 0xFFFF) * 0x10001u;
 #pragma unroll

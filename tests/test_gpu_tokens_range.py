@@ -112,3 +112,50 @@ def test_attend_scores_past_the_largest_float(new, dtype):
     assert torch.isnan(got.cpu()[over]).all() and torch.isnan(lse.cpu()[over]).all()
     assert torch.isfinite(got.cpu()[under]).all()
     assert cache.status() == 0
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("new,dim", [(1, 64), (5, 128), (70, 128), (150, 64)])
+def test_attend_infinite_and_nan_queries(new, dim, dtype):
+    """A query with an infinity has infinite scores (NaN where the key is zero).  A row whose scores are all -infinity weighs nothing:
+    zeros, lse -infinity; one that has +infinity or NaN among them is NaN.  The rows beside it are right (with the bounds of
+    ordinary scores: a product per channel, weights as halves)."""
+    c = ref.Case([new], [150], 4, 2, dim, 32, dtype, seed=51, stale=0x7F)
+    total = 150 + new
+    clean = c.q.clone()
+    for j in range(c.table.shape[1]):                    # keys: channel 3 negative, 5 positive, 7 zero before token 100, channel 9 mixed
+        page = int(c.table[0, j])
+        held = max(0, min(32, total - 32 * j))
+        c.codes[page, 0, :, :held, 3] |= 0x80
+        c.codes[page, 0, :, :held, 3] = c.codes[page, 0, :, :held, 3].clamp_min(0x90)
+        c.codes[page, 0, :, :held, 5] = (c.codes[page, 0, :, :held, 5] & 0x7F).clamp_min(0x10)
+        for t in range(held):
+            if 32 * j + t < 100:
+                c.codes[page, 0, :, t, 7] = 0
+            else:
+                c.codes[page, 0, :, t, 7] = 0xA0
+    kinds = [(3, math.inf), (5, -math.inf), (3, -math.inf), (7, math.inf), (9, math.inf), (0, math.nan)]
+    rows = {}
+    for n, i in enumerate(range(0, new * 4, 3)):
+        rows[i // 4, i % 4] = kinds[n % 6]
+        c.q[i // 4, i % 4, kinds[n % 6][0]] = kinds[n % 6][1]
+        c.q[i // 4, i % 4, 20] = 3e38 * (-1) ** n        # next to an infinity, the largest finite number is one of many
+    for window in (-1, 40):
+        cache, batch = c.on_gpu()
+        got, lse = cache.attend(c.q.cuda(), batch, window=window, want_lse=True)
+        assert cache.status() == 0
+        (x, _, _), = scores_of(c, window=window)
+        got, lse = got.cpu(), lse.cpu()
+        for (i, h), _ in rows.items():
+            lo, hi = ref.visible(total - new + i, total, 1, window)
+            seen = x[i, h, lo:hi]
+            if bool((seen == -math.inf).all()):
+                assert (got[i, h] == 0).all() and lse[i, h] == -math.inf, (i, h, window)
+            else:
+                assert torch.isnan(got[i, h]).all() and torch.isnan(lse[i, h]), (i, h, window)
+        same = torch.ones(new, 4, dtype=torch.bool)
+        for i, h in rows:
+            same[i, h] = False
+        want, _, mass, spread = ref.attend(clean, c.codes, c.scales, c.starts, c.total, c.table, dim ** -0.5, 1, window)
+        tol = (2.0 ** -8 if dtype == BF16 else U) * want.abs() + mass * (2.0 ** -11 if dtype == BF16 else 2.0 ** -20)
+        assert ((got.double() - want).abs() <= tol + mass * (2 * dim * U * spread)[..., None])[same].all()
