@@ -55,14 +55,13 @@ __device__ __forceinline__ uint32_t pack_rest(float lo, float hi, uint32_t taken
     const float a = lo - t.x, b = hi - t.y;
     return pack_half(fabsf(a) <= 65504.f ? a : 0.f, fabsf(b) <= 65504.f ? b : 0.f);
 }
-// Power of two that brings the row's largest magnitude into [1, 2), and its reciprocal.  Beside an infinity every finite number
-// stays finite as a half; a NaN is not counted.
+// Power of two that brings the row's largest magnitude into [2^14, 2^15), and its reciprocal.  The halves' range lies below: an
+// element is off by 2^-40 of the row's largest at most (F32: or 2^-22 of itself), and BF16 ones are exact down to 2^-31 of it.  Rows under
+// 2^-112 come as near as powers of two go, beside an infinity every finite number stays finite; a NaN is not counted.
 __device__ __forceinline__ void row_power(float most, float& down, float& up) {
-    const int e = (int)(__float_as_uint(most) >> 23) - 127;
-    const bool plain = e > -126 && e < 126;
-    down = plain ? __uint_as_float((uint32_t)(127 - e) << 23) : (most < 1.f ? 8.5070592e37f : 1.f);      // (2^126 for tiny rows)
-    up = plain ? __uint_as_float((uint32_t)(127 + e) << 23) : (most < 1.f ? 1.17549435e-38f : 1.f);
-    if (e >= 126) { down = 1.17549435e-38f; up = 8.5070592e37f; }
+    const int d = min(14 + 127 - (int)(__float_as_uint(most) >> 23), 126);
+    down = __uint_as_float((uint32_t)(127 + d) << 23);
+    up = __uint_as_float((uint32_t)(127 - d) << 23);
 }
 
 // A walk over the units of a block's share of the list.  Every member is the same for all lanes.

@@ -159,3 +159,21 @@ def test_attend_infinite_and_nan_queries(new, dim, dtype):
         want, _, mass, spread = ref.attend(clean, c.codes, c.scales, c.starts, c.total, c.table, dim ** -0.5, 1, window)
         tol = (2.0 ** -8 if dtype == BF16 else U) * want.abs() + mass * (2.0 ** -11 if dtype == BF16 else 2.0 ** -20)
         assert ((got.double() - want).abs() <= tol + mass * (2 * dim * U * spread)[..., None])[same].all()
+
+
+@pytest.mark.parametrize("dtype,new,dim,power", [
+    (BF16, 1, 128, 22), (BF16, 5, 64, 22), (F32, 1, 64, 22), (F32, 5, 128, 22), (F32, 70, 128, 22), (F32, 70, 64, 10), (BF16, 70, 128, 16)])
+def test_attend_queries_with_one_large_channel(dtype, new, dim, power):
+    """One channel of the queries is 2^power times the others, and the keys are zero there: the scores are made of the others.
+    Bounds as for ordinary scores (spread, the sum of |q||k|, does not see the large channel)."""
+    c = ref.Case([new], [150], 4, 2, dim, 32, dtype, seed=61, stale=0x7F)
+    c.q[:, :, 11] *= 2.0 ** power
+    c.codes[:, 0, :, :, 11] = 0
+    cache, batch = c.on_gpu()
+    got, lse = cache.attend(c.q.cuda(), batch, want_lse=True)
+    assert cache.status() == 0
+    want, want_lse, mass, spread = ref.attend(c.q, c.codes, c.scales, c.starts, c.total, c.table, dim ** -0.5, 1, -1)
+    e = dim * U * spread
+    tol = (2.0 ** -8 if dtype == BF16 else U) * want.abs() + mass * ((2.0 ** -11 if dtype == BF16 else 2.0 ** -20) + 2 * e)[..., None]
+    assert ((got.cpu().double() - want).abs() <= tol).all()
+    assert ((lse.cpu().double() - want_lse).abs() <= e + 2.0 ** -20 * (1 + want_lse.abs())).all()
