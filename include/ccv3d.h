@@ -433,7 +433,7 @@ typedef struct {
     const int32_t* new_start;    /* [batch + 1] */
     const int32_t* total;        /* [batch] */
     const int32_t* page_table;   /* [batch][max_pages] */
-    int32_t batch, max_pages;
+    int32_t batch, max_pages;    /* batch = 0 (with tokens = 0; the arrays may be NULL): a call without work */
     int32_t tokens;              /* rows of the packed tensors, >= new_start[batch] (rows past it have no sequence: attend does not
                                     write them) */
     int32_t max_new;             /* most new tokens of any sequence (a bound; picks the kernel and its grid) */

@@ -102,7 +102,9 @@ ccv3d_status check_cache(const ccv3d_kv_cache* c) {
 }
 
 ccv3d_status check_batch(const ccv3d_token_batch* b, int page_tokens) {
-    if (!b || !b->new_start || !b->total || b->batch < 1 || b->max_pages < 0 || b->tokens < 0 || b->max_new < 0) return CCV3D_ERR_INVALID_ARG;
+    if (!b || b->batch < 0 || b->max_pages < 0 || b->tokens < 0 || b->max_new < 0) return CCV3D_ERR_INVALID_ARG;
+    if (b->batch == 0) return b->tokens == 0 ? CCV3D_OK : CCV3D_ERR_INVALID_ARG;      // nobody: no arrays, no rows
+    if (!b->new_start || !b->total) return CCV3D_ERR_INVALID_ARG;
     if (!b->page_table && b->max_pages > 0) return CCV3D_ERR_INVALID_ARG;
     if ((int64_t)b->max_pages * page_tokens > 0x7FFFFF00 || b->batch > 65536) return CCV3D_ERR_UNSUPPORTED;    // (room for a unit more)
     if (misaligned(b->new_start, 4) || misaligned(b->total, 4) || misaligned(b->page_table, 4)) return CCV3D_ERR_ALIGNMENT;
@@ -398,7 +400,12 @@ ccv3d_status ccv3d_kv_attend_workspace(const ccv3d_kv_cache* cache, const ccv3d_
                                        int32_t dtype, uint64_t* bytes_host) {
     if (!bytes_host) return CCV3D_ERR_INVALID_ARG;
     Plan pl;
-    const ccv3d_status s = plan_attend(cache, batch, q_heads, dtype, &pl);
+    ccv3d_status s = check_attend(cache, batch, q_heads, dtype);
+    if (s == CCV3D_OK && batch->batch == 0) {
+        *bytes_host = 0;
+        return s;
+    }
+    if (s == CCV3D_OK) s = plan_attend(cache, batch, q_heads, dtype, &pl);
     if (s == CCV3D_OK) *bytes_host = pl.bytes;
     return s;
 }
