@@ -495,7 +495,14 @@ ccv3d_status ccv3d_kv_append(const ccv3d_kv_cache* cache, const ccv3d_token_batc
  * CCV3D_ERR_UNSUPPORTED: head numbers, page tables or rows past 32 bits, or more than 2e9 units of work, (tokens * g / r + batch)
  * * kv_heads * (max_pages * page_tokens / 128 + 1) for g = q_heads / kv_heads and r = 8, 16, 256 (F32: 128) where max_new * g
  * is at most 8, at most 32, or more.
- * q, out: `dtype` (BF16 or F32; F32 is computed to FP32 accuracy).  Scores, softmax statistics and sums are FP32.
+ * q, out: `dtype` (BF16 or F32).  Scores, softmax statistics and sums are FP32; what is multiplied are halves:
+ *   - codes, exactly;
+ *   - queries times a power of two for each row.  BF16: exact down to 2^-31 of the row's largest (2^-28 where max_new * g passes 32),
+ *     elements below count as zero or half of that.  F32, as two halves: within 2^-22 of themselves or 2^-40 of the row's largest;
+ *   - weights, exp(score) times the value scale of the token's page, beside the largest such product W of the row: BF16 within 2^-11
+ *     of themselves, F32, as two halves, within 2^-22, or 2^-32 W if that is more.
+ * So a BF16 output differs by one step of BF16 in a few per cent of places from one with FP32 weights, and F32 is as exact as
+ * FP32 arithmetic unless some page's value scale is 2^10 or more above that of the pages that matter.
  *   q_heads   a multiple of kv_heads
  *   ws        DEVICE scratch, 256-byte aligned, ccv3d_kv_attend_workspace() bytes; holds data within the call only,
  *             calls that may overlap on the GPU need one each, and so do calls that two host threads make at a time,

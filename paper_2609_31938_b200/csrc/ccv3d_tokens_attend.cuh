@@ -9,6 +9,9 @@
 // Softmax in powers of two: with t = score * log2(e) and e_v = log2 of the value scale of the token's page, the weight
 // of a value code is 2^(t + e_v - base), base the running one of t + e_v, so page scales of any size stay out of the range
 // of the 16-bit weights; the softmax's own sum takes that times 1 / value scale.
+// Weights are rounded to one half for BF16 (11 bits; the sum of weights takes them unrounded): a second one for the remainder, as
+// F32 has, would double the output products for bits that outputs of 8 bits drop but where they decide a rounding, and the
+// tile kernel has no TMEM columns for it next to two row blocks.
 #pragma once
 #include <cuda.h>
 

@@ -177,3 +177,31 @@ def test_attend_queries_with_one_large_channel(dtype, new, dim, power):
     tol = (2.0 ** -8 if dtype == BF16 else U) * want.abs() + mass * ((2.0 ** -11 if dtype == BF16 else 2.0 ** -20) + 2 * e)[..., None]
     assert ((got.cpu().double() - want).abs() <= tol).all()
     assert ((lse.cpu().double() - want_lse).abs() <= e + 2.0 ** -20 * (1 + want_lse.abs())).all()
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("new", [1, 5, 100])
+@pytest.mark.parametrize("power", [10, 16, 20, 24])
+def test_attend_page_whose_scale_is_far_above_the_others(power, new, dtype):
+    """A page whose value scale is 2^power times the others' and whose own codes are small (a token that no row sees may have raised
+    it).  Weights are halves (F32: two) of exp(score) times value scale.  With W the largest of those products of a row, each is
+    within 2^-11 (2^-22) of itself and 2^-32 W: half of the halves' smallest step, 2^-25, where W is 2^7 at least.  So outputs are
+    within that of mass, and within 2^-32 W sum |code| over the softmax's sum."""
+    c = ref.Case([new], [200], 4, 2, 64, 32, dtype, seed=71, stale=0x7F)
+    big = int(c.table[0, 2])
+    c.scales[big, 1] *= 2.0 ** power
+    c.codes[big, 1] = torch.where(c.codes[big, 1] % 2 == 0, 0, 1).to(torch.uint8)         # zeros and the smallest number
+    c.codes[big, 1, :, :, :32] = 0
+    cache, batch = c.on_gpu()
+    got = cache.attend(c.q.cuda(), batch).cpu().double()
+    assert cache.status() == 0
+    want, _, mass, spread = ref.attend(c.q, c.codes, c.scales, c.starts, c.total, c.table, 64 ** -0.5, 1, -1)
+    (x, _, _), = scores_of(c)
+    p = torch.softmax(x, -1)
+    pages = c.table[0].long()
+    scale = c.scales[pages, 1].double().repeat_interleave(32, 0)[:200 + new].T.repeat_interleave(2, 0)           # [heads, tokens]
+    codes = c.codes[pages, 1].view(torch.float8_e4m3fn).double().transpose(0, 1).flatten(1, 2)[:, :200 + new].abs()
+    codes = torch.where(torch.isfinite(codes), codes, torch.zeros_like(codes)).sum(1).repeat_interleave(2, 0)    # [heads, dim]
+    most = (p * scale).amax(-1)
+    tol = (2.0 ** -8 if dtype == BF16 else U) * want.abs() + mass * ((2.0 ** -11 if dtype == BF16 else 2.0 ** -20) + 2 * 64 * U * spread)[..., None]
+    assert ((got - want).abs() <= tol + 2.0 ** -32 * most[..., None] * codes).all()
