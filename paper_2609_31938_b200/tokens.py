@@ -131,7 +131,8 @@ class PagedCache:
         self.codes, self.scales, self.device = codes, scales, dev
         self.pages, _, self.kv_heads, self.page_tokens, self.head_dim = codes.shape
         self.c = KvCache(codes.data_ptr(), scales.data_ptr(), self.pages, self.kv_heads, self.page_tokens, self.head_dim)
-        self._status = torch.zeros(1, dtype=torch.int32).to(codes.device)     # (there when this returns, for every stream)
+        # there for every stream when this returns (in a capture, whose every replay zeroes it: for what follows there)
+        self._status = torch.zeros(1, dtype=torch.int32, device=codes.device if _capturing() else None).to(codes.device)
         self._status_ptr = self._status.data_ptr()
         self._needs = {}         # geometry of a call -> bytes of scratch
         self._scratch = {}       # stream -> scratch of attend calls on it

@@ -109,3 +109,23 @@ def test_status_covers_calls_on_other_streams():
         cache.attend(q, batch)
     assert cache.status() == ccv.TOKENS_BAD_PAGE
     assert cache.status() == 0
+
+
+def test_cache_object_made_inside_a_capture():
+    """The handle of a cache whose memory is there may be made in a captured function; a replay starts with no reports."""
+    import paper_2609_31938_b200 as ccv
+    from paper_2609_31938_b200 import tokens as tk
+    c = ref.Case([1], [100], 4, 2, 64, 16, BF16, seed=15)
+    outside, batch = c.on_gpu()
+    q = c.q.cuda()
+    want = outside.attend(q, batch)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        inside = tk.PagedCache(outside.codes, outside.scales)
+        out = inside.attend(q, batch)
+    graph.replay()
+    assert inside.status() == 0 and torch.equal(out, want)
+    batch.page_table[0, 2] = c.codes.shape[0]
+    graph.replay()
+    assert inside.status() == ccv.TOKENS_BAD_PAGE
