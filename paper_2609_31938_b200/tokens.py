@@ -32,6 +32,12 @@ def _dtype(t: torch.Tensor, what: str) -> int:
     return d
 
 
+def _int32(v: int, what: str) -> int:
+    if not -0x80000000 <= v <= 0x7FFFFFFF:
+        raise ValueError(f"{what} {v} does not fit 32 bits")
+    return v
+
+
 def _elsewhere(t: torch.Tensor, what: str, dev: int):
     return ValueError(f"{what} is on {t.device}, not on the current CUDA device cuda:{dev}")
 
@@ -75,7 +81,7 @@ class TokenBatch:
         _int_array(new_start, "new_start", (b + 1,), dev)
         _int_array(total, "total", (b,), dev)
         _int_array(page_table, "page_table", (b, page_table.shape[1]), dev)
-        self.new_start, self.total, self.page_table, self.max_new = new_start, total, page_table, int(max_new)
+        self.new_start, self.total, self.page_table, self.max_new = new_start, total, page_table, _int32(int(max_new), "max_new")
         self.device = dev
         self._at = (new_start.data_ptr(), total.data_ptr(), page_table.data_ptr(), b, page_table.shape[1])
         self._c = {}
@@ -226,12 +232,15 @@ class PagedCache:
     def attend(self, q, batch: TokenBatch, scale: float | None = None, frame: int = 1, window: int = -1, out=None,
                want_lse: bool = False):
         """Attention of q [tokens, q_heads, head_dim] over the cache (``frame``, ``window``: who sees what, as
-        ``ccv3d_kv_attend`` says); ``scale`` defaults to head_dim ** -0.5.  Returns out, or (out, lse)."""
+        ``ccv3d_kv_attend`` says); ``scale`` defaults to head_dim ** -0.5.  Returns out, or (out, lse); rows behind the
+        last sequence's are not written."""
         tokens, dim, dev = q.shape[0], self.head_dim, self.device
         c = self._batch(batch, tokens)
         dt = _dtype(q, "q")
         cq = _heads(q, "q", tokens, dim, dev)
         heads = q.shape[1]
+        _int32(frame, "frame")
+        _int32(window, "window")
         if out is None:
             out = _like(q, memory_format=_DENSE)
             co = Heads(out.data_ptr(), heads * dim, dim)
@@ -280,6 +289,7 @@ def gated_norm(x, y=None, *, gate=None, post_weight=None, post_bias=None, pre_we
     if x.dim() != 2:
         raise ValueError("x must be [rows, channels]")
     rows, ch = x.shape
+    _int32(rows, "the number of rows")
     dev = _device()
     res = _dtype(x, "x")
     xs, ys = _rows(x, "x", rows, ch, dev), 0
@@ -304,6 +314,7 @@ def gated_norm(x, y=None, *, gate=None, post_weight=None, post_bias=None, pre_we
         strides[i] = _rows(t, ("gate", "scale", "shift")[i], groups, ch, dev)
     if rows_per_group is None:
         rows_per_group = max(1, -(-rows // groups)) if groups else max(1, rows)
+    _int32(rows_per_group, "rows_per_group")
     if groups is not None and rows > groups * rows_per_group:
         raise ValueError(f"{groups} groups of {rows_per_group} rows do not cover {rows} rows")
     weight = None

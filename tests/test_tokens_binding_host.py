@@ -147,3 +147,20 @@ def test_status_does_not_come_between_a_call_and_its_report(binding):
         assert c.status() == bit
         t.join()
         assert c.status() == 0
+
+
+def test_numbers_past_32_bits_are_refused(binding):
+    """They would arrive as other numbers: a window of 2^32 as 0."""
+    binding(Library())
+    c, b, x = cache(), batch(2), torch.zeros(2, 4, 64)
+    for kw in (dict(window=1 << 32), dict(window=1 << 31), dict(frame=1 << 32), dict(frame=(1 << 32) + 1), dict(window=-(1 << 32))):
+        with pytest.raises(ValueError):
+            c.attend(x, b, **kw)
+    assert c.attend(x, b, frame=(1 << 31) - 1, window=(1 << 31) - 1).shape == x.shape
+    for n in (1 << 31, (1 << 32) + 1):
+        with pytest.raises(ValueError):
+            tk.TokenBatch(ints(0, 2), ints(2), ints(0, 1)[None], n)
+    with pytest.raises(ValueError):
+        tk.gated_norm(torch.zeros(2, 4), rows_per_group=1 << 32)
+    with pytest.raises(ValueError):
+        tk.gated_norm(torch.zeros(1, 4).expand((1 << 32) + 2, 4), want_h=False, out_r=torch.zeros(1, 4).expand((1 << 32) + 2, 4))
