@@ -234,7 +234,8 @@ ccv3d_status launch_norm(const NormParams& p, bool vec, const Device& dev, cudaS
 // rows.  Device time, us, BF16 (F32), 16 heads on 4, 64 streams of 2000 tokens, 8-row items / 16-row items / tiles:
 //   8 rows 43 (47) / 51 (64) / 96 (119);  16 rows - / 55 (66) / 96 (121);  32 rows - / 90 (112) / 96 (125);
 //   48 rows - / 125 (156) / 98 (125);  128 rows - / 293 (371) / 105 (133)
-// (one stream of 32768: 32 rows 33 (39) / 37 (41), 48 rows 43 (53) / 37 (41); two of 500, up to 128 rows: 16 to 20 / 25)
+// (one stream of 32768: 32 rows 33 (39) / 37 (41), 48 rows 43 (53) / 37 (41); two of 500, up to 128 rows: 16 to 20 / 25: there the
+// rule, which goes by rows alone, gives a quarter away)
 int rows_per_item(int64_t rows, int dtype) { return rows <= 8 ? 8 : rows <= 32 ? 16 : dtype == CCV3D_BF16 ? 256 : 128; }
 
 ccv3d_status check_attend(const ccv3d_kv_cache* cache, const ccv3d_token_batch* batch, int q_heads, int dtype) {

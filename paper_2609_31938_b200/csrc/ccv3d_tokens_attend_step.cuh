@@ -9,9 +9,9 @@
 // row; the TMA swizzle keeps those reads off one another's banks.
 // For F32 the queries and the weights go in as two halves each (value and remainder): about 22 bits.
 //
-// Measured (BF16): 64 streams, 612 MB of cache, 124 us = 5.0 TB/s, 76 % of the copy rate; one stream of 269 MB, 60 us =
+// Measured (BF16): 64 streams, 612 MB of cache, 120 us = 5.1 TB/s, 78 % of the copy rate; one stream of 269 MB, 60 us =
 // 4.5 TB/s, of which some 8 us are the start and the join.  What holds it is the latency of a warp's dependent
-// instructions (0.38 of a scheduler's slots were used at two blocks), not one unit.
+// instructions (0.47 of a scheduler's slots are used, the tensor pipe 17 % of the time), not one unit.
 #pragma once
 #include "ccv3d_tokens_attend.cuh"
 

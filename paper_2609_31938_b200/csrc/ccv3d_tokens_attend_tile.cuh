@@ -18,9 +18,10 @@
 // bears (then the sums in TMEM are scaled down): weights stay under 2^15 and a tile needs one pass.
 // For F32 queries and weights go in as two halves each (value and remainder): about 22 bits, at twice the MMAs.
 //
-// Measured (BF16): 3520 rows on 28160 tokens, 12 heads of 128, 645 to 660 us = 0.93 PFLOP/s, 56 % of what the tensor cores do
-// in a plain product.  A tile of 256 x 128 takes 3.8 k cycles: its MMAs 2.6 k, the two softmax warps of a scheduler 3.1 k (the
-// exponentials 2.05 k of them).  Items of a few units pay 17 k cycles from one to the next (queries in, outputs out).
+// Measured (BF16): 3520 rows on 28160 tokens, 12 heads of 128, 665 to 690 us = 0.9 PFLOP/s, 54 % of what the tensor cores do
+// in a plain product.  A tile of 256 x 128 takes 3.8 k cycles, of which the tensor pipe is busy for 2.05 k and the exponential
+// unit for 2.07 k.  Each stretch of an item costs some 20 k cycles more (queries in, outputs out): nine tiles to an item, 260 us
+// for 100 GFLOP.
 #pragma once
 #include "ccv3d_tokens_attend_step.cuh"
 

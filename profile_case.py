@@ -2,8 +2,10 @@
 
     python profile_case.py --cin 192 --cout 192 --t 4 --h 176 --w 320 [--k 3 3 3] [--calls 3] [--ring]
                            [--stride 1 2 2] [--dilation 1 2 2]
+    python profile_case.py --operator attend-step-b64
 
-Inputs are the seeded synthetic tensors of the benchmark (normal activations, fan-in-scaled weights).
+Inputs are the seeded synthetic tensors of the benchmark (normal activations, fan-in-scaled weights).  --operator runs a
+case of perf/operators.py (a token operator) instead of a layer.
 """
 import argparse
 import os
@@ -12,6 +14,19 @@ import sys
 import numpy as np
 
 sys.path.insert(0, os.path.dirname(os.path.abspath(__file__)))
+
+
+def run_operator(name, calls):
+    import torch
+    from perf import operators
+    operators.own = True
+    case = next(c for c in operators.listed() if c["name"] == name)
+    state = operators.prepare(case, 1)
+    for _ in range(calls):
+        operators.run(state)
+    torch.cuda.synchronize()
+    assert "cache" not in state or state["cache"].status() == 0
+    print("ok", name)
 
 
 def main():
@@ -32,7 +47,10 @@ def main():
     ap.add_argument("--f32", action="store_true", help="FP32 layer (tensor cores by 3xTF32 when the call is large enough)")
     ap.add_argument("--stride", type=int, nargs=3, default=[1, 1, 1], help="(s_t, s_h, s_w)")
     ap.add_argument("--dilation", type=int, nargs=3, default=[1, 1, 1], help="(d_t, d_h, d_w); size-preserving padding")
+    ap.add_argument("--operator", help="a case of perf/operators.py by its name")
     a = ap.parse_args()
+    if a.operator:
+        return run_operator(a.operator, a.calls)
     c = si.conv_case(1, a.cin, a.cout, a.t, a.h, a.w, k=tuple(a.k), cache=None if a.no_cache else "random",
                      dtype=si.F32 if a.f32 else si.BF16)
     if a.f32:
