@@ -418,7 +418,7 @@ ccv3d_status ccv3d_forward_ring_up(ccv3d_handle* h, const ccv3d_ring* in, int32_
 typedef struct {
     void*   codes;           /* DEVICE uint8 [pages][2][kv_heads][page_tokens][head_dim], 16-byte aligned; the caller's */
     float*  scales;          /* DEVICE [pages][2][kv_heads]; the caller's.  Need not be initialised before the first append. */
-    int32_t pages, kv_heads;
+    int32_t pages, kv_heads;     /* kv_heads <= 65536; attend: pages * 2 * kv_heads * page_tokens < 2^31 */
     int32_t page_tokens;     /* 16, 32, 64 or 128 */
     int32_t head_dim;        /* 64 or 128 */
 } ccv3d_kv_cache;
@@ -433,7 +433,8 @@ typedef struct {
     const int32_t* new_start;    /* [batch + 1] */
     const int32_t* total;        /* [batch] */
     const int32_t* page_table;   /* [batch][max_pages] */
-    int32_t batch, max_pages;    /* batch = 0 (with tokens = 0; the arrays may be NULL): a call without work */
+    int32_t batch, max_pages;    /* batch <= 65536, max_pages * page_tokens <= 2^31 - 256; batch = 0 (with tokens = 0; the arrays may be
+                                    NULL): a call without work */
     int32_t tokens;              /* rows of the packed tensors, >= new_start[batch] (rows past it have no sequence: attend does not
                                     write them) */
     int32_t max_new;             /* most new tokens of any sequence (a bound; picks the kernel and its grid) */
@@ -492,7 +493,7 @@ ccv3d_status ccv3d_kv_append(const ccv3d_kv_cache* cache, const ccv3d_token_batc
  * A token that sees nothing (more new tokens than cached ones) gets zeros and lse = -infinity, and so does one whose scores are all
  * -infinity; a score of +infinity (or past the largest FP32 number) or NaN makes its token's outputs and lse NaN.  What a token does not
  * see (stale codes at a page's end, NaN included) has no part in its result.
- * CCV3D_ERR_UNSUPPORTED: head numbers, page tables or rows past 32 bits, or more than 2e9 units of work, (tokens * g / r + batch)
+ * CCV3D_ERR_UNSUPPORTED: tokens * q_heads past 32 bits, or more than 2e9 units of work, (tokens * g / r + batch)
  * * kv_heads * (max_pages * page_tokens / 128 + 1) for g = q_heads / kv_heads and r = 8, 16, 256 (F32: 128) where max_new * g
  * is at most 8, at most 32, or more.
  * q, out: `dtype` (BF16 or F32).  Scores, softmax statistics and sums are FP32; what is multiplied are halves:
