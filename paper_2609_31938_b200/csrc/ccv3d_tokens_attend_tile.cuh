@@ -18,9 +18,9 @@
 // bears (then the sums in TMEM are scaled down): weights stay under 2^15 and a tile needs one pass.
 // For F32 queries and weights go in as two halves each (value and remainder): about 22 bits, at twice the MMAs.
 //
-// Measured (BF16): 3520 rows on 28160 tokens, 12 heads of 128, 665 to 690 us = 0.9 PFLOP/s, 54 % of what the tensor cores do
-// in a plain product.  A tile of 256 x 128 takes 3.8 k cycles, of which the tensor pipe is busy for 2.05 k and the exponential
-// unit for 2.07 k.  Each stretch of an item costs some 20 k cycles more (queries in, outputs out): nine tiles to an item, 260 us
+// Measured (BF16): 3520 rows on 28160 tokens, 12 heads of 128, 645 to 665 us = 0.93 PFLOP/s, 56 % of what the tensor cores do
+// in a plain product.  A tile of 256 x 128 takes 3.6 k cycles, of which the tensor pipe is busy for 2.05 k and the exponential
+// unit for 2.07 k.  Each stretch of an item costs some 25 k cycles more (queries in, outputs out): nine tiles to an item, 260 us
 // for 100 GFLOP.
 #pragma once
 #include "ccv3d_tokens_attend_step.cuh"
@@ -495,7 +495,7 @@ __device__ __forceinline__ int tile_softmax(TileSoftmax& x, const float4* group,
             tc_wait_ld();
             chunk_weights<REST, EDGE>(a, k, row, base, t0 + 64 * half, pr, rest, mx, sum);
             chunk_weights<REST, EDGE>(b, k + 2, row, base, t0 + 64 * half + 32, pr + 16, rest + (REST ? 16 : 0), mx, sum);
-            const bool raise = EDGE ? mx > base_limit(x.m) : mx > WEIGHT_TOP || (x.m == -INFINITY && mx > -INFINITY);
+            const bool raise = mx > (EDGE ? base_limit(x.m) : x.m == -INFINITY ? -INFINITY : WEIGHT_TOP);
             if (pass >= TILE_PASSES || !__any_sync(0xffffffffu, raise)) break;
             const float now = fmaxf(x.m, base_for(EDGE ? mx : mx + base));       // (mx = -inf leaves the base)
             if (__any_sync(0xffffffffu, raise && !(fabsf(now) <= SCORE_EXACT))) {
