@@ -503,7 +503,7 @@ ccv3d_status ccv3d_kv_append(const ccv3d_kv_cache* cache, const ccv3d_token_batc
  *   - weights, exp(score) times the value scale of the token's page, beside the largest such product W of the row: BF16 within 2^-11
  *     of themselves, F32, as two halves, within 2^-22, or 2^-32 W if that is more.
  * So a BF16 output differs by one step of BF16 in a few per cent of places from one with FP32 weights, and F32 errors are of the
- * size of those of FP32 arithmetic unless some page's value scale is 2^10 or more above that of the pages that matter.
+ * size of those of FP32 arithmetic (below 1e-6 of the outputs in norm) unless some page's value scale is 2^10 or more above that of the pages that matter.
  *   q_heads   a multiple of kv_heads
  *   ws        DEVICE scratch, 256-byte aligned, ccv3d_kv_attend_workspace() bytes; holds data within the call only,
  *             calls that may overlap on the GPU need one each, and so do calls that two host threads make at a time,

@@ -232,10 +232,10 @@ ccv3d_status launch_norm(const NormParams& p, bool vec, const Device& dev, cudaS
 // Query rows of an item (8 or 16: step kernel, 128 or 256: tile kernel) where the sequences of a call have up to `rows` of a kv head.
 // The step kernel reads the cache once for every 8 or 16 rows, the tile kernel once for all but always in products of 128
 // rows.  Device time, us, BF16 (F32), 16 heads on 4, 64 streams of 2000 tokens, 8-row items / 16-row items / tiles:
-//   8 rows 43 (47) / 51 (64) / 96 (119);  16 rows - / 55 (66) / 96 (121);  32 rows - / 90 (112) / 96 (125);
-//   48 rows - / 125 (156) / 98 (125);  128 rows - / 293 (371) / 105 (133)
-// (one stream of 32768: 32 rows 33 (39) / 37 (41), 48 rows 43 (53) / 37 (41); two of 500, up to 128 rows: 16 to 20 / 25: there the
-// rule, which goes by rows alone, gives a quarter away)
+//   8 rows 43 (49) / 51 (66) / 96 (131);  16 rows - / 55 (70) / 98 (133);  32 rows - / 92 (121) / 98 (137);
+//   48 rows - / 127 (168) / 100 (139);  128 rows - / 297 (402) / 107 (145)
+// (one stream of 32768: 32 rows 33 (41) / 37 (45), 48 rows 43 (55) / 37 (45); two of 500, 48 to 128 rows: 16 to 21 (18 to 25) / 27 (29 to
+// 33): there the rule, which goes by rows alone, gives a quarter and more away)
 int rows_per_item(int64_t rows, int dtype) { return rows <= 8 ? 8 : rows <= 32 ? 16 : dtype == CCV3D_BF16 ? 256 : 128; }
 
 ccv3d_status check_attend(const ccv3d_kv_cache* cache, const ccv3d_token_batch* batch, int q_heads, int dtype) {
@@ -269,7 +269,7 @@ ccv3d_status plan_attend(const ccv3d_kv_cache* cache, const ccv3d_token_batch* b
     const int64_t rows = (int64_t)batch->max_new * (q_heads / cache->kv_heads);
     pl->rows_per_item = rows_per_item(rows, dtype);
     const bool tile = pl->rows_per_item >= 128;
-    pl->blocks = tile ? pl->dev.sm_count : (pl->rows_per_item == 8 ? STEP_BLOCKS : 2) * pl->dev.sm_count;
+    pl->blocks = (tile ? 1 : step_blocks(dtype == CCV3D_F32, cache->head_dim, pl->rows_per_item)) * pl->dev.sm_count;
     if (pl->blocks > JOIN_PARTS) pl->blocks = JOIN_PARTS;
     pl->slot_rows = tile ? pl->rows_per_item : 16;
     pl->ml_at = (uint64_t)2 * pl->blocks * pl->slot_rows * cache->head_dim * 4;

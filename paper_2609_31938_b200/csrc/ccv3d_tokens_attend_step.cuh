@@ -1,13 +1,15 @@
 // Attention of few query rows (single and drafted tokens) over the paged E4M3 cache.
 //
-// Bound by the cache's bytes.  Four warps to a block, three blocks to an SM (two with 16 query rows: registers; 64 streams,
+// Bound by the cache's bytes.  Four warps to a block, three blocks to an SM where registers allow (64 streams,
 // 8 rows, 146 us at two and 122 at three); a unit is 128 cached tokens of one kv head and
 // each warp streams its own 32 of them: keys and values arrive by TMA in a ring of stages that only this warp fills and
 // drains, so nothing but the end of an item synchronises the block.  Codes turn into halves (exactly) in registers and
 // go straight into mma.sync: scores as K Q^T with the cached tokens as M and up to 8 query rows as N, outputs as V^T P
 // with the head's channels as M.  The order of a contraction is free, so each thread takes whole 16-byte pieces of a
 // row; the TMA swizzle keeps those reads off one another's banks.
-// For F32 the queries and the weights go in as two halves each (value and remainder): about 22 bits.
+// For F32 the queries and the weights go in as two halves each (value and remainder): about 22 bits.  The tensor cores cut each
+// sum they add to instead of rounding it, which over some thousand tokens shrinks the outputs by several 1e-6: products of 16
+// tokens start from zero and are added to the rest with rounding.
 //
 // Measured (BF16): 64 streams, 612 MB of cache, 120 us = 5.1 TB/s, 78 % of the copy rate; one stream of 269 MB, 60 us =
 // 4.5 TB/s, of which some 8 us are the start and the join.  What holds it is the latency of a warp's dependent
@@ -17,7 +19,9 @@
 
 namespace ccv3d {
 
-constexpr int STEP_BLOCKS = 3;               // resident on an SM
+// Blocks on an SM.  Three where the registers allow; for F32 and heads of 128 they would spill (64 streams of 8000 tokens 234 us against
+// 229 with two blocks, one of 131000 74.5 against 69), and so they would with 16 rows.
+constexpr int step_blocks(bool f32, int dim, int rows) { return rows == 8 && !(f32 && dim == 128) ? 3 : 2; }
 constexpr int STEP_WARPS = 4, STEP_TILE = 32, STEP_UNIT = STEP_WARPS * STEP_TILE;
 
 template <int D> struct StepShape {
@@ -155,7 +159,7 @@ __device__ __forceinline__ StepWalk step_share(const AttendParams& p, int rows_p
 }
 
 template <typename T, int D, int NT>
-__global__ void __launch_bounds__(32 * STEP_WARPS, NT == 1 ? STEP_BLOCKS : 2) kv_attend_step_kernel(const __grid_constant__ CUtensorMap tm, const AttendParams p) {
+__global__ void __launch_bounds__(32 * STEP_WARPS, step_blocks(sizeof(T) == 4, D, 8 * NT)) kv_attend_step_kernel(const __grid_constant__ CUtensorMap tm, const AttendParams p) {
     using S = StepShape<D>;
     constexpr int TERMS = sizeof(T) == 4 ? 2 : 1, ROWS = 8 * NT, CH = D / 64;     // CH: 16-byte pieces of a row for a thread
     extern __shared__ __align__(1024) uint8_t smem[];
@@ -520,9 +524,17 @@ __global__ void __launch_bounds__(32 * STEP_WARPS, NT == 1 ? STEP_BLOCKS : 2) kv
                         const uint32_t af[4] = {e4m3x2_to_half2(x01 & 0xFFFFu), e4m3x2_to_half2(x01 >> 16),
                                                 e4m3x2_to_half2(x23 & 0xFFFFu), e4m3x2_to_half2(x23 >> 16)};
 #pragma unroll
-                        for (int i = 0; i < NT; ++i)
+                        for (int i = 0; i < NT; ++i) {
+                            if constexpr (TERMS == 1) {
+                                mma_f16(o[i][2 * k + half], af, pf[i][0][j][0], pf[i][0][j][1]);
+                            } else {
+                                float sum[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                            for (int t = 0; t < TERMS; ++t) mma_f16(o[i][2 * k + half], af, pf[i][t][j][0], pf[i][t][j][1]);
+                                for (int t = TERMS - 1; t >= 0; --t) mma_f16(sum, af, pf[i][t][j][0], pf[i][t][j][1]);
+#pragma unroll
+                                for (int e = 0; e < 4; ++e) o[i][2 * k + half][e] += sum[e];
+                            }
+                        }
                     }
                 }
             }

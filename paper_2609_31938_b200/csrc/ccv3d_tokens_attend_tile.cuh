@@ -35,9 +35,10 @@ static_assert(TILE_AHEAD >= 8, "news goes out four tiles at a time and comes bac
 constexpr int TILE_REGS_SOFTMAX = 168, TILE_REGS_REST = 48;   // of 256 and 384 threads: 61440 registers, what 640 threads are launched with at 96
 // F32: the tensor cores cut each sum they add to instead of rounding it, which over 20 000 tokens in one stretch costs 5.6e-6 of
 // the result.  Every so many tiles the outputs go into sums of their own in TMEM, rounded, and start again from zero.
-// Errors of two batches of prompts (32-bit operations: 0.6e-6) and time of 1760 rows, 12 heads, on 15840 tokens: every 4 tiles
-// 0.8e-6, 0.9e-6, 384 us; every 16 tiles 1.1e-6, 1.3e-6, 378 us; never 364 us.
-constexpr int TILE_FOLD = 4;
+// Errors of two batches of prompts that see 670 and 380 tokens (32-bit operations: 0.56e-6, 0.69e-6) and time of 1760 rows, 12
+// heads, on 15840 tokens: every tile 0.38e-6, 0.43e-6, 445 us; every 2 tiles 0.60e-6, 0.64e-6, 395 us; every 4 tiles 1.1e-6,
+// 1.2e-6, 371 us (without the order of the remainders below).
+constexpr int TILE_FOLD = 2;
 
 template <typename T, int D> struct TileShape {
     static constexpr int TERMS = sizeof(T) == 4 ? 2 : 1, NQ = sizeof(T) == 4 ? 1 : 2, ROWS = 128 * NQ;
@@ -914,10 +915,11 @@ __global__ void __launch_bounds__(TILE_THREADS, 1) kv_attend_tile_kernel(const _
         auto outputs = [&](uint32_t slot, int half, bool first, bool last) {    // of the weights of 64 tokens
             if (elect_one()) {
                 const uint32_t b0 = v_lo + slot * (S::KV >> 4) + half * (8192 >> 4), a0 = a_p + S::P_HALF * half;
+                // (remainders first here, too)
 #pragma unroll
-                for (int t = 0; t < TERMS; ++t)
+                for (int t = TERMS - 1; t >= 0; --t)
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) tc_mma_f16_ts(d_o, a0 + 64 * t + 8 * k, b0 + k * (2048 >> 4), hi, I_O, !first || t + k > 0);
+                    for (int k = 0; k < 4; ++k) tc_mma_f16_ts(d_o, a0 + 64 * t + 8 * k, b0 + k * (2048 >> 4), hi, I_O, !first || t < TERMS - 1 || k > 0);
                 tc_commit(smem_u32(half == 0 ? &sh->h_done[qt] : &sh->v_empty[slot]));
                 if (half == 1 && last) tc_commit(smem_u32(&sh->o_full[qt]));
             }
