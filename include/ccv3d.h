@@ -543,6 +543,114 @@ ccv3d_status ccv3d_gated_norm(const ccv3d_norm_desc* d, const void* x, const voi
                               const void* post_bias, const void* gate, const void* pre_weight, const void* pre_bias,
                               const void* scale, const void* shift, void* r, void* h, void* stream);
 
+/*
+ * ------------------------------------------------------------------------------------------------
+ * Products, decaying states and group norms: a latent predictor with a memory of fixed size, a decoder with normed blocks
+ * ------------------------------------------------------------------------------------------------
+ * What goes on in the epilogue of a product or norm.  NONE: v; SILU: v / (1 + exp(-v)); GELU: v Phi(v) (by erf); GELU_TANH: its
+ * tanh form, v / (1 + exp(-2 u)), u = sqrt(2 / pi) (v + 0.044715 v^3).
+ */
+typedef enum { CCV3D_ACT_NONE = 0, CCV3D_ACT_SILU = 1, CCV3D_ACT_GELU = 2, CCV3D_ACT_GELU_TANH = 3 } ccv3d_activation;
+
+/*
+ * A product with its epilogue, over `rows` tokens:
+ *   out[m, n] = residual[m, n] + act(x[m] . w[n] + bias[n])                                            0 <= n < n_out
+ *   gated:      residual[m, n] + act(x[m] . w[n] + bias[n]) * (x[m] . w[n_out + n] + bias[n_out + n])
+ * x [rows, k] and w [n_out, k] (gated: [2 n_out, k], the gate's rows first) in `dtype`, bias [n_out] (gated [2 n_out]) in `dtype` or NULL,
+ * residual [rows, n_out] and out in out_dtype (F32 where dtype is F32), residual may be NULL or out itself (same strides).
+ *   Rows of x and w are dense; their strides (in elements) and addresses are multiples of 16 bytes; out and residual go by elements.
+ *   k, n_out, rows: any number from 1 on (rows = 0: a call without work), each below 2^31 - 2^16; k <= 2^20.
+ * Products are exact, sums FP32 (rounded every few hundred terms; between, the tensor cores cut off bits below the last), everything
+ * behind them FP32, the output is rounded once.  F32 operands go in as three BF16 numbers each (24 bits, exact); products under 2^-24
+ * of the whole are left out.  F32: an infinity makes its outputs NaN, and numbers under 2^-110 lose bits.
+ *   ws      DEVICE scratch, 256-byte aligned, ccv3d_linear_workspace() bytes, of the call alone (NULL where that is 0)
+ *   status  DEVICE word or NULL: receives CCV3D_TOKENS_TIMEOUT
+ * Any other overlap of out or ws with another tensor is CCV3D_ERR_ALIAS.  Results do not depend on what else runs, the same call gives
+ * the same bits; how rows are grouped in calls may change last bits.  Stream-ordered, no allocation, legal in a stream capture.
+ */
+typedef struct {
+    int32_t rows, n_out, k;
+    int32_t gated;                      /* 0 or 1 */
+    int32_t activation;                 /* ccv3d_activation */
+    int32_t dtype, out_dtype;           /* ccv3d_dtype */
+    int64_t x_stride, w_stride;         /* elements between rows, >= k, multiples of 16 bytes */
+    int64_t out_stride, residual_stride;/* elements between rows, >= n_out */
+} ccv3d_linear_desc;
+ccv3d_status ccv3d_linear(const ccv3d_linear_desc* d, const void* x, const void* w, const void* bias, const void* residual,
+                          void* out, void* ws, uint64_t ws_bytes, uint32_t* status, void* stream);
+/* Bytes of scratch that such a call needs on the current device (HOST output). */
+ccv3d_status ccv3d_linear_workspace(const ccv3d_linear_desc* d, uint64_t* bytes_host);
+
+/*
+ * Attention whose memory is one state of fixed size for each sequence and head, from which old tokens fade:
+ *   S_t = exp(g_t) S_{t-1} + k_t v_t^T        out_t = scale * q_t S_t             S [key_dim, value_dim], FP32
+ * over the new tokens of each sequence in order, g the token's and head's log decay (FP32; <= 0 in ordinary use, -infinity
+ * forgets all that was before).  What kv_attend is to a cache that grows, this is to a stream of any length.
+ * states [slots][heads][key_dim][value_dim], DEVICE FP32, 16-byte aligned: sequence b reads slot[b] and leaves its state after
+ * its last token there; a sequence without new tokens leaves it as it was.  `fresh` (may be NULL): where fresh[b] is not 0, the
+ * sequence starts from zeros whatever its slot holds.
+ *   q, k   [tokens, qk_heads, key_dim], v, out [tokens, heads, value_dim] in dtype; head h goes with q and k of head
+ *          h / (heads / qk_heads).  log_decay [tokens, heads] FP32 with strides in elements (0 is allowed).
+ *   key_dim 64 or 128, value_dim a multiple of 64 up to 512, qk_heads divides heads, heads <= 4096, tokens <= 2^30
+ *   new_start [batch + 1], slot [batch], fresh [batch]: DEVICE int32, checked by the kernels: offsets out of range are cut, a slot outside the pool, or one that
+ *          an earlier sequence of the call (with new tokens) has, is not touched (its sequence starts from zeros and its state is lost), both are reported.
+ *          Rows of out that belong to no sequence are not written.
+ * All sums and states are FP32; dtype F32: products to 2^-23; BF16: scores and the state are taken to 2^-16 for the outputs and to 2^-23 for the new state.  F32: numbers beyond
+ * 3.38e38 may count as infinite, and those under 2^-110 lose bits.
+ *   ws      DEVICE scratch, 256-byte aligned, ccv3d_decay_attend_workspace() bytes, of the call alone (NULL where that is 0)
+ * An overlap of out, states or ws with another tensor is CCV3D_ERR_ALIAS.  Stream-ordered, no allocation, legal in a stream capture.
+ */
+typedef struct {
+    float*  states;
+    int32_t slots, heads, key_dim, value_dim;
+} ccv3d_decay_memory;
+typedef struct {
+    const int32_t* new_start;    /* [batch + 1] */
+    const int32_t* slot;         /* [batch] */
+    const int32_t* fresh;        /* [batch], or NULL */
+    int32_t batch;               /* <= 65536; 0 (with tokens = 0): a call without work */
+    int32_t tokens;              /* rows of the packed tensors, >= new_start[batch] */
+    int32_t max_new;             /* most new tokens of any sequence (a bound; picks the kernel and its grid) */
+} ccv3d_stream_batch;
+#define CCV3D_TOKENS_BAD_SLOT 0x10u      /* a state slot outside the pool, or of two sequences of a call */
+ccv3d_status ccv3d_decay_attend(const ccv3d_decay_memory* memory, const ccv3d_stream_batch* batch, const ccv3d_heads* q,
+                                const ccv3d_heads* k, const ccv3d_heads* v, const float* log_decay, int64_t decay_token_stride,
+                                int64_t decay_head_stride, const ccv3d_heads* out, int32_t qk_heads, int32_t dtype, float scale,
+                                void* ws, uint64_t ws_bytes, uint32_t* status, void* stream);
+ccv3d_status ccv3d_decay_attend_workspace(const ccv3d_decay_memory* memory, const ccv3d_stream_batch* batch, int32_t qk_heads,
+                                          int32_t dtype, uint64_t* bytes_host);
+
+/*
+ * Group norm with an activation on channels-last activations: for each sample and group of channels, over all pixels of the sample,
+ *   y = act(((x - mean) / sqrt(variance + eps) * weight + bias) * (1 + scale) + shift)
+ * x, y [samples, pixels, channels] in dtype with strides in elements, channels dense (any strides and alignment; fastest where rows start
+ * on 16 bytes); weight, bias [channels] FP32 or NULL; scale, shift [samples, channels] FP32 (a stride between samples) or NULL.
+ * Statistics and all arithmetic are FP32, the variance is taken around the mean; the output is rounded once.  A NaN or infinity makes
+ * its sample and group NaN.  y may be x itself (same strides).  Any other overlap is CCV3D_ERR_ALIAS.
+ *   groups divides channels; channels <= 16384; samples and pixels from 0 (samples or pixels 0: a call without work)
+ *   ws      DEVICE scratch, 256-byte aligned, ccv3d_group_norm_workspace() bytes, of the call alone (NULL where that is 0)
+ * The same sample gives the same bits whatever is normed beside it (up to samples of 1 MB).  Stream-ordered, no allocation, legal in a stream capture.
+ */
+typedef struct {
+    int32_t samples, pixels, channels, groups;
+    int32_t activation, dtype;
+    float   eps;
+    int64_t x_sample_stride, x_pixel_stride, y_sample_stride, y_pixel_stride, scale_stride, shift_stride;
+} ccv3d_group_norm_desc;
+ccv3d_status ccv3d_group_norm(const ccv3d_group_norm_desc* d, const void* x, const float* weight, const float* bias,
+                              const float* scale, const float* shift, void* y, void* ws, uint64_t ws_bytes, void* stream);
+ccv3d_status ccv3d_group_norm_workspace(const ccv3d_group_norm_desc* d, uint64_t* bytes_host);
+/*
+ * The same on resident activations: T frames of `in` from slot in_slot on, each frame of each stream a sample (so the result does
+ * not depend on how a stream is cut into chunks), into slots out_slot.. of `out` (equal N, C, H, W, KB; it may be `in` with the same slot:
+ * in place; else the rings must not overlap).  scale and shift are [N * T, C], sample n * T + t.
+ */
+ccv3d_status ccv3d_group_norm_ring(const ccv3d_ring* in, int32_t in_slot, const ccv3d_ring* out, int32_t out_slot, int32_t T,
+                                   int32_t groups, const float* weight, const float* bias, const float* scale, int64_t scale_stride,
+                                   const float* shift, int64_t shift_stride, float eps, int32_t activation, void* ws,
+                                   uint64_t ws_bytes, void* stream);
+ccv3d_status ccv3d_group_norm_ring_workspace(const ccv3d_ring* in, int32_t T, int32_t groups, uint64_t* bytes_host);
+
 #ifdef __cplusplus
 }
 #endif

@@ -51,7 +51,9 @@ class Ring(ctypes.Structure):
 
 
 NORM_NONE, NORM_RMS, NORM_LAYER = range(3)
-TOKENS_BAD_PAGE, TOKENS_BAD_LENGTH, TOKENS_BAD_POSITION, TOKENS_TIMEOUT = 1, 2, 4, 8
+TOKENS_BAD_PAGE, TOKENS_BAD_LENGTH, TOKENS_BAD_POSITION, TOKENS_TIMEOUT, TOKENS_BAD_SLOT = 1, 2, 4, 8, 16
+ACT_NONE, ACT_SILU, ACT_GELU, ACT_GELU_TANH = range(4)
+ACTIVATIONS = {"none": ACT_NONE, "silu": ACT_SILU, "gelu": ACT_GELU, "gelu_tanh": ACT_GELU_TANH}
 
 
 class KvCache(ctypes.Structure):
@@ -90,13 +92,43 @@ class NormDesc(ctypes.Structure):
                 ("shift_stride", ctypes.c_int64)]
 
 
+class LinearDesc(ctypes.Structure):
+    """ccv3d_linear_desc: sizes, epilogue and types of a product."""
+    _fields_ = [("rows", ctypes.c_int32), ("n_out", ctypes.c_int32), ("k", ctypes.c_int32), ("gated", ctypes.c_int32),
+                ("activation", ctypes.c_int32), ("dtype", ctypes.c_int32), ("out_dtype", ctypes.c_int32),
+                ("x_stride", ctypes.c_int64), ("w_stride", ctypes.c_int64), ("out_stride", ctypes.c_int64),
+                ("residual_stride", ctypes.c_int64)]
+
+
+class DecayMemoryC(ctypes.Structure):
+    """ccv3d_decay_memory: a pool of FP32 states [slots][heads][key_dim][value_dim]."""
+    _fields_ = [("states", ctypes.c_void_p), ("slots", ctypes.c_int32), ("heads", ctypes.c_int32),
+                ("key_dim", ctypes.c_int32), ("value_dim", ctypes.c_int32)]
+
+
+class StreamBatchC(ctypes.Structure):
+    """ccv3d_stream_batch: the sequences of one call on states (device arrays)."""
+    _fields_ = [("new_start", ctypes.c_void_p), ("slot", ctypes.c_void_p), ("fresh", ctypes.c_void_p),
+                ("batch", ctypes.c_int32), ("tokens", ctypes.c_int32), ("max_new", ctypes.c_int32)]
+
+
+class GroupNormDesc(ctypes.Structure):
+    """ccv3d_group_norm_desc: geometry, activation and type of a group norm on packed rows."""
+    _fields_ = [("samples", ctypes.c_int32), ("pixels", ctypes.c_int32), ("channels", ctypes.c_int32), ("groups", ctypes.c_int32),
+                ("activation", ctypes.c_int32), ("dtype", ctypes.c_int32), ("eps", ctypes.c_float),
+                ("x_sample_stride", ctypes.c_int64), ("x_pixel_stride", ctypes.c_int64), ("y_sample_stride", ctypes.c_int64),
+                ("y_pixel_stride", ctypes.c_int64), ("scale_stride", ctypes.c_int64), ("shift_stride", ctypes.c_int64)]
+
+
 EXPORTS = ("ccv3d_create", "ccv3d_forward", "ccv3d_forward_host", "ccv3d_workspace_bytes", "ccv3d_destroy",
            "ccv3d_get_counters", "ccv3d_device_status", "ccv3d_status_string", "ccv3d_add_bf16",
            "ccv3d_upsample_bf16", "ccv3d_profile_enable", "ccv3d_profile_read", "ccv3d_forward_static", "ccv3d_selftest_wait_timeout", "ccv3d_forward_ex",
            "ccv3d_ring_kb", "ccv3d_ring_bytes", "ccv3d_ring_load", "ccv3d_ring_store", "ccv3d_upsample_ring",
            "ccv3d_forward_ring", "ccv3d_out_dims", "ccv3d_forward_ring_up", "ccv3d_rows_copy",
            "ccv3d_forward_host_stream", "ccv3d_set_workspace",
-           "ccv3d_kv_append", "ccv3d_kv_attend", "ccv3d_kv_attend_workspace", "ccv3d_gated_norm")
+           "ccv3d_kv_append", "ccv3d_kv_attend", "ccv3d_kv_attend_workspace", "ccv3d_gated_norm",
+           "ccv3d_linear", "ccv3d_linear_workspace", "ccv3d_decay_attend", "ccv3d_decay_attend_workspace", "ccv3d_group_norm",
+           "ccv3d_group_norm_workspace", "ccv3d_group_norm_ring", "ccv3d_group_norm_ring_workspace")
 
 
 def _load() -> ctypes.CDLL:
@@ -141,6 +173,16 @@ def _load() -> ctypes.CDLL:
     lib.ccv3d_kv_attend_workspace.argtypes = [cp, tp, i32, i32, u64p]
     lib.ccv3d_kv_attend.argtypes = [cp, tp, hp, hp, vp, i32, i32, ctypes.c_float, i32, i32, vp, ctypes.c_uint64, vp, vp]
     lib.ccv3d_gated_norm.argtypes = [ctypes.POINTER(NormDesc)] + [vp] * 12
+    u64, i64, f32 = ctypes.c_uint64, ctypes.c_int64, ctypes.c_float
+    lp, dp, sp, gp = (ctypes.POINTER(c) for c in (LinearDesc, DecayMemoryC, StreamBatchC, GroupNormDesc))
+    lib.ccv3d_linear.argtypes = [lp, vp, vp, vp, vp, vp, vp, u64, vp, vp]
+    lib.ccv3d_linear_workspace.argtypes = [lp, u64p]
+    lib.ccv3d_decay_attend.argtypes = [dp, sp, hp, hp, hp, vp, i64, i64, hp, i32, i32, f32, vp, u64, vp, vp]
+    lib.ccv3d_decay_attend_workspace.argtypes = [dp, sp, i32, i32, u64p]
+    lib.ccv3d_group_norm.argtypes = [gp, vp, vp, vp, vp, vp, vp, vp, u64, vp]
+    lib.ccv3d_group_norm_workspace.argtypes = [gp, u64p]
+    lib.ccv3d_group_norm_ring.argtypes = [rp, i32, rp, i32, i32, i32, vp, vp, vp, i64, vp, i64, f32, i32, vp, u64, vp]
+    lib.ccv3d_group_norm_ring_workspace.argtypes = [rp, i32, i32, u64p]
     for name in EXPORTS:
         if name not in ("ccv3d_status_string", "ccv3d_ring_bytes"):
             getattr(lib, name).restype = ctypes.c_int
@@ -327,6 +369,55 @@ def ccv3d_gated_norm(desc: NormDesc, x, y, post_weight, post_bias, gate, pre_wei
     return lib.ccv3d_gated_norm(desc, x, y, post_weight, post_bias, gate, pre_weight, pre_bias, scale, shift, r, h, stream)
 
 
+def ccv3d_linear(desc: LinearDesc, x, w, bias, residual, out, ws=None, ws_bytes=0, status=None, stream=0) -> int:
+    return lib.ccv3d_linear(desc, x, w, bias, residual, out, ws, ws_bytes, status, stream)
+
+
+def ccv3d_linear_workspace(desc: LinearDesc):
+    """(status, bytes of scratch a ccv3d_linear call of this shape needs)."""
+    b = ctypes.c_uint64()
+    s = lib.ccv3d_linear_workspace(desc, b)
+    return s, b.value
+
+
+def ccv3d_decay_attend(memory: DecayMemoryC, batch: StreamBatchC, q: Heads, k: Heads, v: Heads, log_decay, decay_token_stride: int,
+                       decay_head_stride: int, out: Heads, qk_heads: int, dtype: int, scale: float, ws=None, ws_bytes=0, status=None,
+                       stream=0) -> int:
+    return lib.ccv3d_decay_attend(memory, batch, q, k, v, log_decay, decay_token_stride, decay_head_stride, out, qk_heads, dtype,
+                                  scale, ws, ws_bytes, status, stream)
+
+
+def ccv3d_decay_attend_workspace(memory: DecayMemoryC, batch: StreamBatchC, qk_heads: int, dtype: int):
+    """(status, bytes of scratch a ccv3d_decay_attend call of this shape needs)."""
+    b = ctypes.c_uint64()
+    s = lib.ccv3d_decay_attend_workspace(memory, batch, qk_heads, dtype, b)
+    return s, b.value
+
+
+def ccv3d_group_norm(desc: GroupNormDesc, x, weight, bias, scale, shift, y, ws=None, ws_bytes=0, stream=0) -> int:
+    return lib.ccv3d_group_norm(desc, x, weight, bias, scale, shift, y, ws, ws_bytes, stream)
+
+
+def ccv3d_group_norm_workspace(desc: GroupNormDesc):
+    """(status, bytes of scratch a ccv3d_group_norm call of this shape needs)."""
+    b = ctypes.c_uint64()
+    s = lib.ccv3d_group_norm_workspace(desc, b)
+    return s, b.value
+
+
+def ccv3d_group_norm_ring(rin: Ring, in_slot: int, rout: Ring, out_slot: int, T: int, groups: int, weight, bias, scale, scale_stride: int,
+                          shift, shift_stride: int, eps: float, activation: int, ws=None, ws_bytes=0, stream=0) -> int:
+    return lib.ccv3d_group_norm_ring(rin, in_slot, rout, out_slot, T, groups, weight, bias, scale, scale_stride, shift, shift_stride,
+                                     eps, activation, ws, ws_bytes, stream)
+
+
+def ccv3d_group_norm_ring_workspace(ring: Ring, T: int, groups: int):
+    """(status, bytes of scratch a ccv3d_group_norm_ring call of this shape needs)."""
+    b = ctypes.c_uint64()
+    s = lib.ccv3d_group_norm_ring_workspace(ring, T, groups, b)
+    return s, b.value
+
+
 class FrameRing:
     """A frame ring on the current CUDA device: torch owns the memory, `c` is the struct the C calls take."""
 
@@ -357,6 +448,16 @@ class FrameRing:
         if s != OK:
             raise Ccv3dError(s, "ccv3d_ring_store")
         return y
+
+
+    def group_norm(self, slot, T, groups, weight=None, bias=None, *, scale=None, shift=None, eps=1e-6, activation="none",
+                   out_ring: "FrameRing | None" = None, out_slot=0):
+        """Group norm with an activation of the T frames from slot on, each by itself (``ccv3d_group_norm_ring``), into `out_ring` from
+        out_slot on; without a ring to write to, in place.  weight, bias [C], scale, shift [N * T, C], all float32."""
+        from . import tokens
+        tokens.ring_group_norm(self, slot, T, groups, weight, bias, scale, shift, eps, activation,
+                               self if out_ring is None else out_ring, slot if out_ring is None else out_slot)
+        return self if out_ring is None else out_ring
 
 
 class CausalConv3d:

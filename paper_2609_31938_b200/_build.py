@@ -13,7 +13,12 @@ SOURCES = {   # source -> the files its object depends on
                      "ccv3d_tc_pointwise.cuh", "ccv3d_host_common.cuh", "ccv3d_host_tc.cuh", "ccv3d_host_ring.cuh", HEADER],
     "ccv3d_tokens.cu": ["ccv3d_tokens_common.cuh", "ccv3d_tokens_norm.cuh", "ccv3d_tokens_append.cuh",
                         "ccv3d_tokens_softmax.cuh", "ccv3d_tokens_attend.cuh", "ccv3d_tokens_attend_step.cuh",
-                        "ccv3d_tokens_attend_tile.cuh", "ccv3d_tc_ptx.cuh", HEADER],
+                        "ccv3d_tokens_attend_tile.cuh", "ccv3d_tokens_host.cuh", "ccv3d_tc_ptx.cuh", HEADER],
+    "ccv3d_group_norm.cu": ["ccv3d_tokens_common.cuh", "ccv3d_tokens_activation.cuh", "ccv3d_tokens_group_norm.cuh",
+                            "ccv3d_tokens_host.cuh", HEADER],
+    "ccv3d_linear.cu": ["ccv3d_tokens_common.cuh", "ccv3d_tokens_activation.cuh", "ccv3d_tokens_linear.cuh", "ccv3d_tokens_host.cuh",
+                        "ccv3d_tc_ptx.cuh", HEADER],
+    "ccv3d_decay.cu": ["ccv3d_tokens_common.cuh", "ccv3d_tokens_decay.cuh", "ccv3d_tokens_host.cuh", HEADER],
 }
 
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17", "-Xcompiler", "-fPIC"]

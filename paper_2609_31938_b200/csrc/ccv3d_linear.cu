@@ -1,0 +1,212 @@
+// C entry points of the products: argument checks, cutting into tiles, launches.
+#include <type_traits>
+
+#include "ccv3d_tokens_linear.cuh"
+#include "ccv3d_tokens_host.cuh"
+
+using namespace ccv3d;
+
+namespace {
+
+// Tokens of a tile, and how its tiles fall to the pairs of SMs.
+struct LinearPlan {
+    Device dev;
+    int BT, parts, kblocks, n_tiles, whole, tail, sharers, pairs;
+    int64_t t_tiles, pitch, x_at, w_at, part_at;      // F32: elements between rows of a split operand; bytes in the scratch
+    uint64_t bytes;
+};
+
+ccv3d_status check_linear(const ccv3d_linear_desc* d) {
+    if (!d || d->rows < 0 || d->n_out < 1 || d->k < 1 || (d->gated != 0 && d->gated != 1)) return CCV3D_ERR_INVALID_ARG;
+    if (!dtype_ok(d->dtype) || !dtype_ok(d->out_dtype) || (d->dtype == CCV3D_F32 && d->out_dtype != CCV3D_F32)) return CCV3D_ERR_INVALID_ARG;
+    if (d->activation < CCV3D_ACT_NONE || d->activation > CCV3D_ACT_GELU_TANH) return CCV3D_ERR_INVALID_ARG;
+    const int64_t most = 0x7FFF0000, parts = d->dtype == CCV3D_F32 ? 3 : 1;
+    if (d->k > (1 << 20) || parts * (d->rows + 256LL) > most || parts * (d->n_out * (1LL + d->gated) + 256) > most) return CCV3D_ERR_UNSUPPORTED;
+    return CCV3D_OK;
+}
+
+// Few rows take narrow tiles: the weights' bytes bound them, and every tile reads its weights whole.
+int tokens_of_tile(int rows, bool gated) {
+    if (rows <= 16) return 16;
+    if (rows <= 64) return 64;
+    return rows <= 128 || gated ? 128 : 256;
+}
+
+ccv3d_status plan_linear(const ccv3d_linear_desc* d, LinearPlan* q) {
+    ccv3d_status s = check_linear(d);
+    if (s != CCV3D_OK) return s;
+    if ((s = current_device(&q->dev)) != CCV3D_OK) return s;
+    const bool f32 = d->dtype == CCV3D_F32;
+    q->parts = f32 ? 3 : 1;
+    q->BT = tokens_of_tile(d->rows, d->gated);
+    const int kb = f32 ? 32 : 64;
+    q->kblocks = (d->k + kb - 1) / kb;
+    q->n_tiles = (d->n_out + 255) / 256;
+    q->t_tiles = ((int64_t)d->rows + q->BT - 1) / q->BT;
+    q->pairs = q->dev.sm_count / 2;
+    const int64_t tiles = q->n_tiles * q->t_tiles;
+    if (tiles > 0x3FFFFFFF) return CCV3D_ERR_UNSUPPORTED;
+    // The last turn: `left` tiles for all pairs.  Cutting them along K saves (1 - left / pairs) of a tile's time and costs a launch and the sums'
+    // way through memory, some 3 us.  A K block takes about 0.15 us (F32: six products of half its length).
+    const int left = (int)(tiles % q->pairs);
+    const double tile_us = q->kblocks * (f32 ? 0.45 : 0.15) * (d->gated || q->BT == 256 ? 1.0 : 0.7);
+    q->whole = (int)tiles;
+    q->tail = q->sharers = 0;
+    if (left && tile_us * (q->pairs - left) / q->pairs > 3.0) {
+        const int64_t shares = (int64_t)left * q->kblocks / 4;         // of four K blocks at least
+        q->sharers = (int)(shares < q->pairs ? shares : q->pairs);
+        if (q->sharers > left) {
+            q->whole = (int)(tiles - left);
+            q->tail = left;
+        } else {
+            q->sharers = 0;
+        }
+    }
+    const auto up = [](int64_t n) { return (n + 255) / 256 * 256; };
+    q->pitch = (d->k + 7LL) / 8 * 8;
+    q->x_at = 0;
+    q->w_at = f32 ? up(3 * q->pitch * d->rows * 2) : 0;
+    q->part_at = q->w_at + (f32 ? up(3 * q->pitch * d->n_out * (1 + d->gated) * 2) : 0);
+    q->bytes = q->part_at + 2LL * q->sharers * q->BT * (1 + d->gated) * 256 * 4;
+    return CCV3D_OK;
+}
+
+// A BF16 matrix of `rows` rows of k elements, read in boxes of a stage's row length and box_rows rows.
+ccv3d_status encode_rows(CUtensorMap* tm, const void* at, int64_t rows, int64_t k, int64_t stride, int row_bytes, int box_rows) {
+    const EncodeTiledFn fn = encode_tiled();
+    if (!fn) return CCV3D_ERR_CUDA;
+    const cuuint64_t dims[2] = {(cuuint64_t)k, (cuuint64_t)rows}, strides[1] = {(cuuint64_t)stride * 2};
+    const cuuint32_t box[2] = {(cuuint32_t)row_bytes / 2, (cuuint32_t)box_rows}, es[2] = {1, 1};
+    const CUresult r = fn(tm, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(at), dims, strides, box, es, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                          row_bytes == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                          CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    return r == CUDA_SUCCESS ? CCV3D_OK : CCV3D_ERR_CUDA;
+}
+
+template <typename S, typename TO>
+ccv3d_status launch_linear_as(LinearParams& p, const LinearPlan& q, const void* x, int64_t x_rows, int64_t x_stride, const void* w, int64_t w_rows,
+                              int64_t w_stride, int k, cudaStream_t st) {
+    static std::atomic<uint64_t> done{0};
+    if (!allow_smem(linear_tile_kernel<S, TO>, S::SMEM, q.dev.index, done)) { cudaGetLastError(); return CCV3D_ERR_CUDA; }
+    CUtensorMap tw, tx;
+    ccv3d_status s = encode_rows(&tw, w, w_rows, k, w_stride, S::ROWB, 128);
+    if (s == CCV3D_OK) s = encode_rows(&tx, x, x_rows, k, x_stride, S::ROWB, S::BT / 2);
+    if (s != CCV3D_OK) return s;
+    const int used = p.tail ? p.pairs : (p.whole < p.pairs ? p.whole : p.pairs);
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(2 * used);
+    cfg.blockDim = dim3(S::THREADS);
+    cfg.dynamicSmemBytes = S::SMEM;
+    cfg.stream = st;
+    cfg.attrs = at;
+    cfg.numAttrs = S::PARTS == 3 ? 1 : 0;            // behind the kernels that split the operands
+    if (cudaLaunchKernelEx(&cfg, linear_tile_kernel<S, TO>, tw, tx, p) != cudaSuccess) { cudaGetLastError(); return CCV3D_ERR_CUDA; }
+    if (!p.tail) return CCV3D_OK;
+    cfg.gridDim = dim3(p.tail, S::BT / LINEAR_JOIN_TOKENS);
+    cfg.blockDim = dim3(256);
+    cfg.dynamicSmemBytes = 0;
+    cfg.numAttrs = 1;
+    if (cudaLaunchKernelEx(&cfg, linear_join_kernel<TO, S::GATED>, p, S::BT) != cudaSuccess) { cudaGetLastError(); return CCV3D_ERR_CUDA; }
+    return CCV3D_OK;
+}
+
+template <int PARTS, typename TO, typename... A>
+ccv3d_status launch_linear(bool gated, int BT, A&&... a) {
+    constexpr bool F = sizeof(TO) == 4;
+    if (gated) {
+        if (BT == 16) return launch_linear_as<LinearShape<16, true, PARTS, F>, TO>(a...);
+        if (BT == 64) return launch_linear_as<LinearShape<64, true, PARTS, F>, TO>(a...);
+        return launch_linear_as<LinearShape<128, true, PARTS, F>, TO>(a...);
+    }
+    if (BT == 16) return launch_linear_as<LinearShape<16, false, PARTS, F>, TO>(a...);
+    if (BT == 64) return launch_linear_as<LinearShape<64, false, PARTS, F>, TO>(a...);
+    if (BT == 128) return launch_linear_as<LinearShape<128, false, PARTS, F>, TO>(a...);
+    return launch_linear_as<LinearShape<256, false, PARTS, F>, TO>(a...);
+}
+
+void split(const float* x, int64_t stride, int rows, int k, void* to, int64_t pitch, cudaStream_t st) {
+    const int64_t blocks = (rows * (pitch / 4) + 255) / 256;
+    linear_split_kernel<<<(unsigned)(blocks < 148 * 8 ? blocks : 148 * 8), 256, 0, st>>>(x, stride, rows, k, (__nv_bfloat16*)to, (int)pitch);
+}
+
+}  // namespace
+
+extern "C" {
+
+ccv3d_status ccv3d_linear_workspace(const ccv3d_linear_desc* d, uint64_t* bytes_host) {
+    if (!bytes_host) return CCV3D_ERR_INVALID_ARG;
+    LinearPlan q;
+    ccv3d_status s = check_linear(d);
+    if (s == CCV3D_OK && d->rows == 0) {
+        *bytes_host = 0;
+        return s;
+    }
+    if (s == CCV3D_OK) s = plan_linear(d, &q);
+    if (s == CCV3D_OK) *bytes_host = q.bytes;
+    return s;
+}
+
+ccv3d_status ccv3d_linear(const ccv3d_linear_desc* d, const void* x, const void* w, const void* bias, const void* residual,
+                          void* out, void* ws, uint64_t ws_bytes, uint32_t* status, void* stream) {
+    ccv3d_status s = check_linear(d);
+    if (s != CCV3D_OK) return s;
+    if (d->rows == 0) return CCV3D_OK;
+    if (!x || !w || !out) return CCV3D_ERR_INVALID_ARG;
+    const int64_t M = d->rows, N = d->n_out, K = d->k, NW = N * (1 + d->gated), e = esize(d->dtype), eo = esize(d->out_dtype);
+    // strides of a single row are anything
+    const int64_t xs = M > 1 ? d->x_stride : (K * e + 15) / 16 * 16 / e, wst = NW > 1 ? d->w_stride : (K * e + 15) / 16 * 16 / e;
+    if (xs < K || wst < K || (M > 1 && d->out_stride < N) || (M > 1 && residual && d->residual_stride < 0)) return CCV3D_ERR_INVALID_ARG;
+    if (misaligned(x, 16) || misaligned(w, 16) || xs * e % 16 || wst * e % 16 || misaligned(bias, e) || misaligned(residual, eo) || misaligned(out, eo) ||
+        misaligned(status, 4))
+        return CCV3D_ERR_ALIGNMENT;
+    const Span so = span_of(out, ((M - 1) * d->out_stride + N) * eo);
+    const Span in[] = {span_of(x, ((M - 1) * xs + K) * e), span_of(w, ((NW - 1) * wst + K) * e), span_of(bias, bias ? NW * e : 0),
+                       span_of(residual, residual ? ((M - 1) * d->residual_stride + N) * eo : 0)};
+    for (int i = 0; i < 4; ++i)
+        if (in[i].a != in[i].b && meet(so, in[i]) && !(i == 3 && out == residual && (M == 1 || d->out_stride == d->residual_stride))) return CCV3D_ERR_ALIAS;
+    LinearPlan q;
+    if ((s = plan_linear(d, &q)) != CCV3D_OK) return s;
+    if ((s = check_ws(ws, ws_bytes, q.bytes)) != CCV3D_OK) return s;
+    const Span sw = span_of(ws, (int64_t)q.bytes);
+    if (q.bytes) {
+        if (meet(sw, so)) return CCV3D_ERR_ALIAS;
+        for (const Span& t : in)
+            if (t.a != t.b && meet(sw, t)) return CCV3D_ERR_ALIAS;
+    }
+    cudaStream_t st = (cudaStream_t)stream;
+    LinearParams p = {};
+    p.bias = bias;
+    p.res = residual;
+    p.out = out;
+    p.out_stride = d->out_stride;
+    p.res_stride = d->residual_stride;
+    p.rows = d->rows;
+    p.n_out = d->n_out;
+    p.act = d->activation;
+    p.bias_f32 = d->dtype == CCV3D_F32;
+    p.n_tiles = q.n_tiles;
+    p.kblocks = q.kblocks;
+    p.whole = q.whole;
+    p.tail = q.tail;
+    p.sharers = q.sharers;
+    p.pairs = q.pairs;
+    p.part = (float*)((char*)ws + q.part_at);
+    p.status = status;
+    p.wait_clk = q.dev.wait_clk;
+    if (d->dtype == CCV3D_F32) {
+        void *px = (char*)ws + q.x_at, *pw = (char*)ws + q.w_at;
+        split((const float*)w, wst, (int)NW, d->k, pw, q.pitch, st);
+        split((const float*)x, xs, d->rows, d->k, px, q.pitch, st);
+        if ((s = launched()) != CCV3D_OK) return s;
+        p.x_plane = d->rows;
+        p.w_plane = (int)NW;
+        return launch_linear<3, float>(d->gated, q.BT, p, q, px, 3 * M, q.pitch, pw, 3 * NW, q.pitch, d->k, st);
+    }
+    if (d->out_dtype == CCV3D_F32) return launch_linear<1, float>(d->gated, q.BT, p, q, x, M, xs, w, NW, wst, d->k, st);
+    return launch_linear<1, __nv_bfloat16>(d->gated, q.BT, p, q, x, M, xs, w, NW, wst, d->k, st);
+}
+
+}  // extern "C"

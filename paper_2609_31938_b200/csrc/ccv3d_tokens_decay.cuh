@@ -1,0 +1,634 @@
+// Attention with decaying states: S_t = exp(g_t) S_{t-1} + k_t v_t^T, out_t = scale q_t S_t.
+//
+// Single tokens (decay_step_kernel): bound by the states' bytes.  A block holds a slice of 64 value columns of one state in registers from
+// its one load to its one store.
+// Many tokens (decay_chunk_kernel): in chunks of 64, with G the sum of the log decays from the chunk's start on,
+//   out_i = scale (exp(G_i) q_i S + sum_{j <= i} exp(G_i - G_j) (q_i . k_j) v_j)        S' = exp(G_end) S + sum_j exp(G_end - G_j) k_j v_j^T
+// as mma.sync products of BF16 with FP32 sums.  A warp owns 16 value columns of S^T, in registers as the products leave them, which is also
+// the layout that the next product wants them in as its B operand: the state never leaves the registers.  What is not BF16 already goes in
+// as several BF16 numbers, 8 bits each: scores with their decay and S as two (F32: three), v with its decay as three, F32 inputs as three.
+// G is summed in 64 bits and kept as two floats, so that differences of sums that a strong decay made large still have all their bits.
+//
+// Where sequences and heads are too few for the machine, sequences are cut into segments: their contributions to the state side by side,
+// then a scan over the segments (decay_scan_kernel), then the outputs.
+//
+// A chunk in which a key or value is not finite goes token by token (0 times infinity must not reach a token that does not see it).
+#pragma once
+#include "ccv3d_tokens_common.cuh"
+
+namespace ccv3d {
+
+constexpr int DECAY_CHUNK = 64;
+constexpr int DECAY_STEP_THREADS = 256;
+constexpr float DECAY_FORGET = -1e4f;      // a log decay below it is as good as minus infinity, and its sums stay finite
+
+struct DecayParams {
+    ccv3d_decay_memory m;
+    ccv3d_stream_batch bt;
+    ccv3d_heads q, k, v, o;
+    const float* decay;
+    int64_t d_token, d_head;
+    int group;                   // heads that share a q and k
+    float scale;
+    uint32_t* status;
+    int seg;                     // tokens of a segment (0: sequences are not cut)
+    float* part;                 // [item][head][key][value]: contributions of the segments, then the states they start from
+    float* fade;                 // [item][head]: decay over a whole segment
+    int items;                   // room in them
+};
+
+struct DecaySeq { int first, n, slot; bool zero; };     // slot < 0: the state is not kept
+
+__device__ __forceinline__ void decay_span(const ccv3d_stream_batch& bt, int b, int& first, int& n, bool& bad) {
+    int s = __ldg(bt.new_start + b), e = __ldg(bt.new_start + b + 1);
+    bad = s < 0 || e < s || e > bt.tokens || e - s > bt.max_new;
+    if (bad) {
+        s = min(max(s, 0), bt.tokens);
+        e = min(max(e, s), s + min(bt.tokens - s, bt.max_new));
+    }
+    first = s;
+    n = e - s;
+}
+// All threads of the block.
+__device__ __forceinline__ DecaySeq decay_seq(const DecayParams& p, int b, bool tell) {
+    DecaySeq s;
+    bool bad;
+    decay_span(p.bt, b, s.first, s.n, bad);
+    s.slot = __ldg(p.bt.slot + b);
+    uint32_t word = bad ? CCV3D_TOKENS_BAD_LENGTH : 0u;
+    int taken = 0;
+    if ((unsigned)s.slot >= (unsigned)p.m.slots) {
+        s.slot = -1;
+        if (s.n) word |= CCV3D_TOKENS_BAD_SLOT;
+    } else if (s.n) {
+        for (int j = threadIdx.x; j < b && !taken; j += blockDim.x)
+            if (__ldg(p.bt.slot + j) == s.slot) {
+                int f, n;
+                decay_span(p.bt, j, f, n, bad);
+                taken = n > 0;
+            }
+    }
+    if (__syncthreads_or(taken)) {
+        s.slot = -1;
+        word |= CCV3D_TOKENS_BAD_SLOT;
+    }
+    s.zero = s.slot < 0 || (p.bt.fresh && __ldg(p.bt.fresh + b) != 0);
+    if (word && tell && threadIdx.x == 0) report(p.status, word);
+    return s;
+}
+
+// exp(g) S: what is forgotten wholly is zero whatever it was
+__device__ __forceinline__ float fade(float s, float f) { return f == 0.f ? 0.f : s * f; }
+__device__ __forceinline__ float fade_add(float s, float f, float x) { return f == 0.f ? x : fmaf(s, f, x); }
+
+// ---------------------------------------------------------------------------------------------------- single tokens
+// Block (sequence, head, 64 value columns): thread t has columns 4 (t % 16) .. + 3 of rows t / 16 + 16 i.
+template <typename T, int DK>
+__global__ void __launch_bounds__(DECAY_STEP_THREADS) decay_step_kernel(const __grid_constant__ DecayParams p) {
+    constexpr int R = DK / 16;
+    __shared__ __align__(16) float kq[2][2][DK];             // [turn][k, q]
+    __shared__ __align__(16) float part[2][8][64];
+    const int slices = p.m.value_dim / 64, t = threadIdx.x, row0 = t >> 4;
+    const int slice = blockIdx.x % slices, h = blockIdx.x / slices % p.m.heads, b = blockIdx.x / slices / p.m.heads;
+    const DecaySeq s = decay_seq(p, b, slice == 0 && h == 0);
+    if (s.n == 0) return;
+    const int col = slice * 64 + (t & 15) * 4;
+    float* state = p.m.states + ((int64_t)max(s.slot, 0) * p.m.heads + h) * DK * p.m.value_dim + col;
+    float4 S[R];
+#pragma unroll
+    for (int i = 0; i < R; ++i) S[i] = s.zero ? make_float4(0.f, 0.f, 0.f, 0.f) : *reinterpret_cast<const float4*>(state + (int64_t)(row0 + 16 * i) * p.m.value_dim);
+    const T* k = (const T*)p.k.data + h / p.group * p.k.head_stride;
+    const T* q = (const T*)p.q.data + h / p.group * p.q.head_stride;
+    const T* v = (const T*)p.v.data + h * p.v.head_stride + col;
+    T* o = (T*)p.o.data + h * p.o.head_stride + slice * 64;
+    for (int i = 0; i < s.n; ++i) {
+        const int64_t tok = s.first + i;
+        float(&now)[2][DK] = kq[i & 1];
+        if (t < DK / 2) {
+            float x[4];
+            const T* at = t < DK / 4 ? k + tok * p.k.token_stride + 4 * t : q + tok * p.q.token_stride + 4 * (t - DK / 4);
+            load4(at, x);
+            store4(&now[t >= DK / 4][4 * (t & (DK / 4 - 1))], x);
+        }
+        float x[4];
+        load4(v + tok * p.v.token_stride, x);
+        const float g = __ldg(p.decay + tok * p.d_token + h * p.d_head), f = expf(g);
+        __syncthreads();
+        float y[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+            const float kk = now[0][row0 + 16 * r], qq = now[1][row0 + 16 * r];
+            S[r].x = fade_add(S[r].x, f, kk * x[0]);
+            S[r].y = fade_add(S[r].y, f, kk * x[1]);
+            S[r].z = fade_add(S[r].z, f, kk * x[2]);
+            S[r].w = fade_add(S[r].w, f, kk * x[3]);
+            y[0] = fmaf(qq, S[r].x, y[0]);
+            y[1] = fmaf(qq, S[r].y, y[1]);
+            y[2] = fmaf(qq, S[r].z, y[2]);
+            y[3] = fmaf(qq, S[r].w, y[3]);
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) y[j] += __shfl_xor_sync(0xffffffffu, y[j], 16);
+        if ((t & 31) < 16) store4(&part[i & 1][t >> 5][(t & 15) * 4], y);
+        __syncthreads();
+        if (t < 64) {
+            float sum = part[i & 1][0][t];
+#pragma unroll
+            for (int w = 1; w < 8; ++w) sum += part[i & 1][w][t];
+            store1(o + tok * p.o.token_stride + t, sum * p.scale);
+        }
+    }
+    if (s.slot >= 0) {
+#pragma unroll
+        for (int i = 0; i < R; ++i) *reinterpret_cast<float4*>(state + (int64_t)(row0 + 16 * i) * p.m.value_dim) = S[i];
+    }
+}
+
+// ------------------------------------------------------------------------------------------------------ many tokens
+__device__ __forceinline__ void mma_bf16(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+                 : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t smem_at(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
+__device__ __forceinline__ void ldsm(uint32_t at, uint32_t (&r)[4]) {
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(at) : "memory");
+}
+__device__ __forceinline__ void ldsm_t(uint32_t at, uint32_t (&r)[4]) {
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(at) : "memory");
+}
+// Two floats as N pairs of BF16 numbers, each what the ones before leave.  (Infinities leave NaN: their products are not finite anyway.)
+template <int N>
+__device__ __forceinline__ void split_pair(float x, float y, uint32_t (&out)[N]) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        out[i] = pack_bf16(x, y);
+        x -= __uint_as_float(out[i] << 16);
+        y -= __uint_as_float(out[i] & 0xFFFF0000u);
+    }
+}
+
+// Shared memory of a block: rows of BF16 with 16 bytes between them, so that eight rows of a matrix lie in different banks.
+template <typename T, int DK, int NW> struct DecayShape {
+    static constexpr bool F32 = sizeof(T) == 4;
+    static constexpr int PI = F32 ? 3 : 1, PM = F32 ? 3 : 2, PV = 3;     // BF16 parts of inputs, of scores and the state, of values with their decay
+    static constexpr int DV = 16 * NW, THREADS = 32 * NW, BUFFERS = F32 ? 1 : 2;
+    static constexpr int QS = DK + 8, VS = DV + 8, PS = DECAY_CHUNK + 8; // elements of a row
+    static constexpr int Q = DECAY_CHUNK * QS, V = DECAY_CHUNK * VS, P = DECAY_CHUNK * PS;   // elements of a plane
+    static constexpr int IN = PI * (2 * Q + V);                          // of a buffer: q, k, v
+    static constexpr int BYTES = (BUFFERS * IN + PM * P) * 2;
+};
+
+template <typename T, int DK, int NW>
+struct DecayShared {
+    float2 g[DECAY_CHUNK];       // sums of log decays, as two floats
+    float end[DECAY_CHUNK];      // exp(G_end - G_j)
+    float begin[DECAY_CHUNK];    // exp(G_i)
+    float last;                  // exp(G_end)
+};
+
+// Item (sequence, segment) of a cut call; false: there is none of this number.  All threads; word: two ints in shared memory.
+__device__ __forceinline__ bool decay_item(const DecayParams& p, int item, int& b, int& seg, int* word) {
+    __shared__ int scan[32];
+    const int t = threadIdx.x, warps = blockDim.x >> 5;
+    int before = 0;
+    if (t == 0) word[0] = -1;
+    for (int base = 0; base < p.bt.batch; base += blockDim.x) {
+        int n = 0, first;
+        bool bad;
+        if (base + t < p.bt.batch) {
+            decay_span(p.bt, base + t, first, n, bad);
+            n = n / p.seg + (n % p.seg != 0);
+        }
+        const int upto = warp_scan(n);
+        if ((t & 31) == 31) scan[t >> 5] = upto;
+        __syncthreads();
+        int mine = before + upto - n, all = before;
+        for (int i = 0; i < warps; ++i) {
+            if (i < (t >> 5)) mine += scan[i];
+            all += scan[i];
+        }
+        if (item >= mine && item < mine + n) { word[0] = base + t; word[1] = item - mine; }
+        __syncthreads();
+        before = all;
+        if (item < before) break;
+    }
+    b = word[0];
+    seg = word[1];
+    return b >= 0;
+}
+
+enum { DECAY_ALL, DECAY_STATES, DECAY_OUTPUTS };     // a whole sequence; a segment's contribution to the state; a segment's outputs
+
+template <typename T, int DK, int NW, int MODE>
+__global__ void __launch_bounds__(32 * NW, NW == 4 ? 2 : 1) decay_chunk_kernel(const __grid_constant__ DecayParams p) {
+    using S = DecayShape<T, DK, NW>;
+    constexpr int PI = S::PI, PM = S::PM, PV = S::PV, L = DECAY_CHUNK;
+    extern __shared__ __align__(16) __nv_bfloat16 decay_smem[];
+    __shared__ DecayShared<T, DK, NW> sh;
+    __shared__ int word[2];
+    const int t = threadIdx.x, warp = t >> 5, lane = t & 31, g = lane >> 2, tc = lane & 3;
+    const int slices = p.m.value_dim / S::DV, slice = blockIdx.y % slices, h = blockIdx.y / slices;
+    const int dv0 = slice * S::DV;
+    int first, n;
+    int64_t part_at = 0;                               // of the item's head in part
+    DecaySeq sq = {0, 0, -1, true};
+    if constexpr (MODE == DECAY_ALL) {
+        sq = decay_seq(p, blockIdx.x, blockIdx.y == 0);
+        first = sq.first;
+        n = sq.n;
+        if (n == 0) return;
+    } else {
+        int b, seg;
+        bool bad;
+        if (!decay_item(p, blockIdx.x, b, seg, word)) return;
+        decay_span(p.bt, b, first, n, bad);
+        first += seg * p.seg;
+        n = min(p.seg, n - seg * p.seg);
+        part_at = ((int64_t)blockIdx.x * p.m.heads + h) * DK * p.m.value_dim;
+    }
+    const T* kp = (const T*)p.k.data + h / p.group * p.k.head_stride;
+    const T* qp = (const T*)p.q.data + h / p.group * p.q.head_stride;
+    const T* vp = (const T*)p.v.data + h * p.v.head_stride + dv0;
+    T* op = (T*)p.o.data + h * p.o.head_stride + dv0;
+
+    // S^T of this warp: rows dv = 16 warp + g (+ 8), columns dk = 8 j + 2 tc (+ 1)
+    float st[DK / 8][4];
+    auto state_at = [&](float* base, int j, int i) { return base + (int64_t)(8 * j + 2 * tc + (i & 1)) * p.m.value_dim + dv0 + 16 * warp + g + (i >> 1) * 8; };
+    {
+        float* from = MODE == DECAY_ALL ? p.m.states + ((int64_t)max(sq.slot, 0) * p.m.heads + h) * DK * p.m.value_dim : p.part + part_at;
+        const bool zero = MODE == DECAY_STATES || (MODE == DECAY_ALL && sq.zero);
+#pragma unroll
+        for (int j = 0; j < DK / 8; ++j)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) st[j][i] = zero ? 0.f : *state_at(from, j, i);
+    }
+
+    uint32_t most = 0;                                 // of keys and values: whether all are finite (this thread's)
+    // rows of `dim` elements of tokens tok .. of a chunk of `live` into planes at `to`; what lies behind them is zero
+    auto bring = [&](const T* from, int64_t stride, int tok, int live, __nv_bfloat16* to, int pitch, int dim) {
+        const int per = dim / 8;
+        for (int i = t; i < L * per; i += S::THREADS) {
+            const int r = i / per, c = (i - r * per) * 8;
+            const T* at = from + (int64_t)(tok + r) * stride + c;
+            if constexpr (!S::F32) {
+                const uint32_t dst = smem_at(to + r * pitch + c), size = r < live ? 16u : 0u;
+                asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(r < live ? at : from), "r"(size) : "memory");
+            } else {
+                float x[4] = {0.f, 0.f, 0.f, 0.f}, y[4] = {0.f, 0.f, 0.f, 0.f};
+                if (r < live) { load4(at, x); load4(at + 4, y); }
+                uint32_t w[4][3];
+                split_pair<3>(x[0], x[1], w[0]);
+                split_pair<3>(x[2], x[3], w[1]);
+                split_pair<3>(y[0], y[1], w[2]);
+                split_pair<3>(y[2], y[3], w[3]);
+#pragma unroll
+                for (int z = 0; z < 3; ++z)
+                    *reinterpret_cast<uint4*>(to + z * L * pitch + r * pitch + c) = make_uint4(w[0][z], w[1][z], w[2][z], w[3][z]);
+            }
+        }
+    };
+    auto bring_chunk = [&](int chunk) {
+        __nv_bfloat16* to = decay_smem + chunk % S::BUFFERS * S::IN;
+        const int tok = first + chunk * L, live = min(L, n - chunk * L);
+        if (MODE != DECAY_STATES) bring(qp, p.q.token_stride, tok, live, to, S::QS, DK);
+        bring(kp, p.k.token_stride, tok, live, to + PI * S::Q, S::QS, DK);
+        bring(vp, p.v.token_stride, tok, live, to + 2 * PI * S::Q, S::VS, S::DV);
+        if constexpr (!S::F32) asm volatile("cp.async.commit_group;" ::: "memory");
+    };
+    // whether this thread's share of the keys and values is finite
+    auto look = [&](const __nv_bfloat16* at, int pitch, int dim) {
+        const int per = dim / 8;
+        for (int i = t; i < L * per; i += S::THREADS) {
+            const int r = i / per, c = (i - r * per) * 8;
+            const uint4 w = *reinterpret_cast<const uint4*>(at + r * pitch + c);
+            most = __vmaxu2(most, __vmaxu2(__vmaxu2(w.x & 0x7FFF7FFFu, w.y & 0x7FFF7FFFu), __vmaxu2(w.z & 0x7FFF7FFFu, w.w & 0x7FFF7FFFu)));
+        }
+    };
+
+    const int chunks = (n + L - 1) / L;
+    double total = 0.0;                                // log decay of the chunks so far (warp 0)
+    bring_chunk(0);
+    for (int chunk = 0; chunk < chunks; ++chunk) {
+        const int tok0 = first + chunk * L, live = min(L, n - chunk * L);
+        __nv_bfloat16* sq_ = decay_smem + chunk % S::BUFFERS * S::IN;
+        __nv_bfloat16 *sk = sq_ + PI * S::Q, *sv = sk + PI * S::Q, *sp = decay_smem + S::BUFFERS * S::IN;
+        if (warp == 0) {
+            // log decays of tokens 2 lane, 2 lane + 1 and their sums
+            double x[2];
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const int r = 2 * lane + i;
+                const float d = r < live ? __ldg(p.decay + (int64_t)(tok0 + r) * p.d_token + h * p.d_head) : 0.f;
+                x[i] = d < DECAY_FORGET ? (double)DECAY_FORGET : (double)d;
+            }
+            double s = x[0] + x[1];
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const double y = __shfl_up_sync(0xffffffffu, s, o);
+                if (lane >= o) s += y;
+            }
+            const double end = __shfl_sync(0xffffffffu, s, 31);
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const double at = i ? s : s - x[1];
+                const float hi = (float)at;
+                sh.g[2 * lane + i] = make_float2(hi, (float)(at - hi));
+                sh.begin[2 * lane + i] = expf((float)at);
+                sh.end[2 * lane + i] = expf((float)(end - at));
+            }
+            if (lane == 31) sh.last = expf((float)end);
+            total += end;
+        }
+        if constexpr (!S::F32) asm volatile("cp.async.wait_group 0;" ::: "memory");
+        most = 0;
+        __syncthreads();
+        look(sk, S::QS, DK);
+        look(sv, S::VS, S::DV);
+        if constexpr (S::BUFFERS == 2)
+            if (chunk + 1 < chunks) bring_chunk(chunk + 1);
+        const bool odd = __syncthreads_or((most & 0xFFFFu) >= 0x7F80u || (most >> 16) >= 0x7F80u);
+        const float last = sh.last;
+        if (odd) {
+            // token by token; a lane's part of q S is summed over the four lanes of its rows
+            auto value = [&](const __nv_bfloat16* at, int plane) {
+                float x = 0.f;
+#pragma unroll
+                for (int z = PI - 1; z >= 0; --z) {
+                    const float y = __bfloat162float(at[z * plane]);
+                    x = isnan(y) && z ? x : x + y;                   // (an infinity's remainders are NaN)
+                }
+                return x;
+            };
+#pragma unroll 1
+            for (int i = 0; i < live; ++i) {
+                const float prev = i ? sh.g[i - 1].x : 0.f, prev_lo = i ? sh.g[i - 1].y : 0.f;
+                const float f = expf((sh.g[i].x - prev) + (sh.g[i].y - prev_lo));
+                const float v0 = value(sv + i * S::VS + 16 * warp + g, S::V), v1 = value(sv + i * S::VS + 16 * warp + g + 8, S::V);
+                float y0 = 0.f, y1 = 0.f;
+#pragma unroll
+                for (int j = 0; j < DK / 8; ++j) {
+#pragma unroll
+                    for (int c = 0; c < 2; ++c) {
+                        const int d = 8 * j + 2 * tc + c;
+                        const float kk = value(sk + i * S::QS + d, S::Q);
+                        st[j][c] = fade_add(st[j][c], f, kk * v0);
+                        st[j][2 + c] = fade_add(st[j][2 + c], f, kk * v1);
+                        if (MODE != DECAY_STATES) {
+                            const float qq = value(sq_ + i * S::QS + d, S::Q);
+                            y0 = fmaf(qq, st[j][c], y0);
+                            y1 = fmaf(qq, st[j][2 + c], y1);
+                        }
+                    }
+                }
+                if (MODE != DECAY_STATES) {
+#pragma unroll
+                    for (int o = 1; o < 4; o <<= 1) {
+                        y0 += __shfl_xor_sync(0xffffffffu, y0, o);
+                        y1 += __shfl_xor_sync(0xffffffffu, y1, o);
+                    }
+                    if (tc == 0) {
+                        T* at = op + (int64_t)(tok0 + i) * p.o.token_stride + 16 * warp + g;
+                        store1(at, y0 * p.scale);
+                        store1(at + 8, y1 * p.scale);
+                    }
+                }
+            }
+        } else {
+            if constexpr (MODE != DECAY_STATES) {
+                // scores of 16 tokens i with 64 (or 32) tokens j, times their decay, as parts
+                {
+                    constexpr int JT = 256 / (NW * 8) >= 8 ? 8 : 4;          // 8-token tiles of a warp
+                    const int i0 = 16 * (warp & 3), j0 = NW == 8 ? 32 * (warp >> 2) : 0;
+                    float sc[JT][4];
+#pragma unroll
+                    for (int j = 0; j < JT; ++j)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) sc[j][i] = 0.f;
+                    if (j0 <= i0 + 15) {
+#pragma unroll
+                        for (int o = PI - 1; o >= 0; --o)
+#pragma unroll
+                            for (int a = o; a >= 0; --a)
+#pragma unroll
+                                for (int kt = 0; kt < DK / 16; ++kt) {
+                                    uint32_t af[4];
+                                    ldsm(smem_at(sq_ + a * S::Q + (i0 + (lane & 15)) * S::QS + 16 * kt + (lane >> 4) * 8), af);
+#pragma unroll
+                                    for (int j = 0; j < JT; j += 2) {
+                                        if (j0 + 8 * j > i0 + 15) continue;
+                                        uint32_t bf[4];
+                                        ldsm(smem_at(sk + (o - a) * S::Q + (j0 + 8 * j + (lane & 7) + (lane >> 4) * 8) * S::QS + 16 * kt + (lane >> 3 & 1) * 8), bf);
+                                        mma_bf16(sc[j], af, bf[0], bf[1]);
+                                        mma_bf16(sc[j + 1], af, bf[2], bf[3]);
+                                    }
+                                }
+                    }
+                    const float2 ga = sh.g[i0 + g], gb = sh.g[i0 + g + 8];
+#pragma unroll
+                    for (int j = 0; j < JT; ++j) {
+                        const int c = j0 + 8 * j + 2 * tc;
+                        const float2 g0 = sh.g[c], g1 = sh.g[c + 1];
+                        float x[4];
+                        const auto weigh = [&](float s, const float2& gi, const float2& gj, bool seen) {
+                            const float w = seen ? expf((gi.x - gj.x) + (gi.y - gj.y)) : 0.f;
+                            return w == 0.f ? 0.f : s * w;
+                        };
+                        x[0] = weigh(sc[j][0], ga, g0, c <= i0 + g);
+                        x[1] = weigh(sc[j][1], ga, g1, c + 1 <= i0 + g);
+                        x[2] = weigh(sc[j][2], gb, g0, c <= i0 + g + 8);
+                        x[3] = weigh(sc[j][3], gb, g1, c + 1 <= i0 + g + 8);
+                        uint32_t a[PM], b[PM];
+                        split_pair<PM>(x[0], x[1], a);
+                        split_pair<PM>(x[2], x[3], b);
+#pragma unroll
+                        for (int z = 0; z < PM; ++z) {
+                            *reinterpret_cast<uint32_t*>(sp + z * S::P + (i0 + g) * S::PS + c) = a[z];
+                            *reinterpret_cast<uint32_t*>(sp + z * S::P + (i0 + g + 8) * S::PS + c) = b[z];
+                        }
+                    }
+                }
+                // q S, for all 64 tokens and the warp's 16 columns
+                float out[4][2][4];
+#pragma unroll
+                for (int m = 0; m < 4; ++m)
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) out[m][i >> 2][i & 3] = 0.f;
+                // (F32: the remainders' products of all keys first, so that the whole sums are only added to, and cut, eight times)
+#pragma unroll
+                for (int pass = S::F32 ? 0 : 1; pass < 2; ++pass)
+#pragma unroll
+                    for (int kt = 0; kt < DK / 16; ++kt) {
+                        uint32_t b[2][2][PM];                // [columns g, g + 8][k halves][part]
+#pragma unroll
+                        for (int c = 0; c < 2; ++c)
+#pragma unroll
+                            for (int k = 0; k < 2; ++k) split_pair<PM>(st[2 * kt + k][2 * c], st[2 * kt + k][2 * c + 1], b[c][k]);
+#pragma unroll
+                        for (int m = 0; m < 4; ++m) {
+                            if (16 * m >= live) break;
+#pragma unroll
+                            for (int a = PI - 1; a >= 0; --a) {
+                                if (S::F32 && pass == 1 && a > 0) continue;
+                                uint32_t af[4];
+                                ldsm(smem_at(sq_ + a * S::Q + (16 * m + (lane & 15)) * S::QS + 16 * kt + (lane >> 4) * 8), af);
+#pragma unroll
+                                for (int z = PM - 1; z >= 0; --z) {
+                                    if (a + z >= PM || (S::F32 && (pass == 1) != (a + z == 0))) continue;
+                                    mma_bf16(out[m][0], af, b[0][0][z], b[0][1][z]);
+                                    mma_bf16(out[m][1], af, b[1][0][z], b[1][1][z]);
+                                }
+                            }
+                        }
+                    }
+                __syncthreads();                             // all scores are there
+#pragma unroll
+                for (int m = 0; m < 4; ++m) {
+                    if (16 * m >= live) break;
+                    float pv[2][4];
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) pv[i >> 2][i & 3] = 0.f;
+#pragma unroll
+                    for (int o = PM - 1; o >= 0; --o)        // part a of the scores, o - a of the values
+#pragma unroll
+                        for (int kt = 0; kt <= m; ++kt)
+#pragma unroll
+                            for (int a = o; a >= 0 && o - a < PI; --a) {
+                                uint32_t af[4], bf[4];
+                                ldsm(smem_at(sp + a * S::P + (16 * m + (lane & 15)) * S::PS + 16 * kt + (lane >> 4) * 8), af);
+                                ldsm_t(smem_at(sv + (o - a) * S::V + (16 * kt + (lane & 15)) * S::VS + 16 * warp + (lane >> 4) * 8), bf);
+                                mma_bf16(pv[0], af, bf[0], bf[1]);
+                                mma_bf16(pv[1], af, bf[2], bf[3]);
+                            }
+                    const float e0 = sh.begin[16 * m + g], e1 = sh.begin[16 * m + g + 8];
+#pragma unroll
+                    for (int half = 0; half < 2; ++half) {
+                        const int r = 16 * m + g + 8 * half;
+                        if (r >= live) continue;
+                        const float e = half ? e1 : e0;
+                        T* at = op + (int64_t)(tok0 + r) * p.o.token_stride + 16 * warp + 2 * tc;
+#pragma unroll
+                        for (int c = 0; c < 2; ++c) {
+                            const float x = p.scale * fade_add(out[m][c][2 * half], e, pv[c][2 * half]);
+                            const float y = p.scale * fade_add(out[m][c][2 * half + 1], e, pv[c][2 * half + 1]);
+                            if constexpr (S::F32) *reinterpret_cast<float2*>(at + 8 * c) = make_float2(x, y);
+                            else *reinterpret_cast<uint32_t*>(at + 8 * c) = pack_bf16(x, y);
+                        }
+                    }
+                }
+            }
+            if (MODE != DECAY_OUTPUTS || chunk + 1 < chunks) {
+                // the state: v with its decay to the chunk's end, as parts, times k
+                uint32_t va[L / 16][PV][4];
+#pragma unroll
+                for (int kt = 0; kt < L / 16; ++kt) {
+                    uint32_t raw[PI][4];
+#pragma unroll
+                    for (int z = 0; z < PI; ++z)
+                        ldsm_t(smem_at(sv + z * S::V + (16 * kt + (lane & 7) + (lane >> 4) * 8) * S::VS + 16 * warp + (lane >> 3 & 1) * 8), raw[z]);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        float x = 0.f, y = 0.f;
+#pragma unroll
+                        for (int z = PI - 1; z >= 0; --z) {
+                            x += __uint_as_float(raw[z][i] << 16);
+                            y += __uint_as_float(raw[z][i] & 0xFFFF0000u);
+                        }
+                        const float2 e = *reinterpret_cast<const float2*>(&sh.end[16 * kt + 2 * tc + (i >> 1) * 8]);
+                        uint32_t w[PV];
+                        split_pair<PV>(x * e.x, y * e.y, w);
+#pragma unroll
+                        for (int z = 0; z < PV; ++z) va[kt][z][i] = w[z];
+                    }
+                }
+#pragma unroll
+                for (int j = 0; j < DK / 8; j += 2) {
+                    float d[2][4];
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) d[i >> 2][i & 3] = 0.f;
+#pragma unroll
+                    for (int o = PV - 1; o >= 0; --o)
+#pragma unroll
+                        for (int kt = 0; kt < L / 16; ++kt)
+#pragma unroll
+                            for (int a = (o < PI ? o : PI - 1); a >= 0; --a) {            // part a of k, o - a of v
+                                uint32_t bf[4];
+                                ldsm_t(smem_at(sk + a * S::Q + (16 * kt + (lane & 15)) * S::QS + 8 * j + (lane >> 4) * 8), bf);
+                                mma_bf16(d[0], va[kt][o - a], bf[0], bf[1]);
+                                mma_bf16(d[1], va[kt][o - a], bf[2], bf[3]);
+                            }
+#pragma unroll
+                    for (int c = 0; c < 2; ++c)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) st[j + c][i] = fade_add(st[j + c][i], last, d[c][i]);
+                }
+            }
+        }
+        __syncthreads();                                     // this chunk's rows and scores have been used
+        if constexpr (S::BUFFERS == 1)
+            if (chunk + 1 < chunks) bring_chunk(chunk + 1);
+    }
+    if (MODE == DECAY_STATES || (MODE == DECAY_ALL && sq.slot >= 0)) {
+        float* to = MODE == DECAY_ALL ? p.m.states + ((int64_t)sq.slot * p.m.heads + h) * DK * p.m.value_dim : p.part + part_at;
+#pragma unroll
+        for (int j = 0; j < DK / 8; ++j)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) *state_at(to, j, i) = st[j][i];
+        if (MODE == DECAY_STATES && t == 0 && slice == 0) p.fade[(int64_t)blockIdx.x * p.m.heads + h] = expf((float)total);
+    }
+}
+
+// States that the segments of a sequence start from, in place of their contributions, and the sequence's last state.
+// Block (sequence, head, 1024 elements), a thread to four.
+constexpr int DECAY_SCAN_THREADS = 256, DECAY_SCAN_AHEAD = 4;
+__global__ void __launch_bounds__(DECAY_SCAN_THREADS) decay_scan_kernel(const __grid_constant__ DecayParams p) {
+    const int64_t size = (int64_t)p.m.key_dim * p.m.value_dim, per = p.m.heads * size;
+    const int b = blockIdx.x, h = blockIdx.z;
+    const DecaySeq s = decay_seq(p, b, blockIdx.y == 0 && h == 0);
+    if (s.n == 0) return;
+    // items before this sequence's
+    long long before = 0;
+    for (int j = threadIdx.x; j < b; j += DECAY_SCAN_THREADS) {
+        int f, n;
+        bool bad;
+        decay_span(p.bt, j, f, n, bad);
+        before += n / p.seg + (n % p.seg != 0);
+    }
+    __shared__ long long sums[DECAY_SCAN_THREADS / 32];
+#pragma unroll
+    for (int o = 16; o; o >>= 1) before += __shfl_xor_sync(0xffffffffu, before, o);
+    if ((threadIdx.x & 31) == 0) sums[threadIdx.x >> 5] = before;
+    __syncthreads();
+    before = 0;
+    for (int i = 0; i < DECAY_SCAN_THREADS / 32; ++i) before += sums[i];
+    const int64_t e = (int64_t)blockIdx.y * (4 * DECAY_SCAN_THREADS) + 4 * threadIdx.x;
+    if (e >= size) return;
+    // (offsets that name tokens twice can give more items than there is room for)
+    const int items = (int)min((long long)(s.n / p.seg + (s.n % p.seg != 0)), max(0ll, p.items - before));
+    float* state = p.m.states + ((int64_t)max(s.slot, 0) * p.m.heads + h) * size + e;
+    float4 x = s.zero ? make_float4(0.f, 0.f, 0.f, 0.f) : *reinterpret_cast<const float4*>(state);
+    float* at = p.part + before * per + h * size + e;
+    const float* fades = p.fade + (int64_t)before * p.m.heads + h;
+    for (int i = 0; i < items; i += DECAY_SCAN_AHEAD) {
+        float4 y[DECAY_SCAN_AHEAD];
+        float f[DECAY_SCAN_AHEAD];
+#pragma unroll
+        for (int j = 0; j < DECAY_SCAN_AHEAD; ++j)
+            if (i + j < items) {
+                y[j] = *reinterpret_cast<const float4*>(at + (i + j) * per);
+                f[j] = fades[(int64_t)(i + j) * p.m.heads];
+            }
+#pragma unroll
+        for (int j = 0; j < DECAY_SCAN_AHEAD; ++j)
+            if (i + j < items) {
+                *reinterpret_cast<float4*>(at + (i + j) * per) = x;
+                x.x = fade_add(x.x, f[j], y[j].x);
+                x.y = fade_add(x.y, f[j], y[j].y);
+                x.z = fade_add(x.z, f[j], y[j].z);
+                x.w = fade_add(x.w, f[j], y[j].w);
+            }
+    }
+    if (s.slot >= 0) *reinterpret_cast<float4*>(state) = x;
+}
+
+}  // namespace ccv3d

@@ -1,0 +1,411 @@
+// Products of token rows with weights, with bias, activation or gated pair, and residual in the epilogue, on tcgen05.
+//
+// Few rows: bound by the weights' bytes.  Many rows: bound by the tensor cores.  One kernel for both, with the weights as the rows of
+// the products (M = 256, a pair of CTAs) and BT tokens as their columns (16 for single tokens, up to 256 for frames), so that a lane of
+// tensor memory is an output feature: its bias is one register, and a warp's loads and stores of a token's features are contiguous at any
+// alignment and any number of features.  A gated pair has two accumulators, of its two rows of weights, side by side.
+//
+// 12 or 20 warps, persistent, one pair of CTAs to two SMs:
+//   warp 0     TMA of weight and token tiles (K blocks of 128 bytes, F32: 64) into a ring of stages; each CTA of a pair loads its own 128
+//              weight rows and half of the tokens
+//   warp 1     the leader's issues the MMAs of the pair
+//   warp 2     tensor memory
+//   warps 4..  epilogue of one accumulator while the next is filled: four warps to the 128 lanes, the columns in two or four parts
+// Tiles go round the pairs in turn; those of the last, unfilled turn are cut along K into equal shares of K blocks, whose sums
+// linear_join_kernel adds in order (no atomics: the same bits every run).
+//
+// F32 outputs: the tensor cores cut what they add to instead of rounding it, which shrinks long sums; so accumulators are handed over every
+// few K blocks and summed in registers with rounding.  F32 operands are split beforehand into three BF16 numbers each (8 + 8 + 8 bits,
+// exact); six of the nine products, smallest first, keep 2^-24.
+#pragma once
+#include "ccv3d_tc_ptx.cuh"
+#include "ccv3d_tokens_activation.cuh"
+#include "ccv3d_tokens_common.cuh"
+
+namespace ccv3d {
+
+constexpr int LINEAR_MAX_STAGES = 12;
+
+struct LinearParams {
+    const void *bias, *res;
+    void* out;
+    int64_t out_stride, res_stride;
+    int rows, n_out;
+    int act, bias_f32;
+    int n_tiles, kblocks;        // tiles of 256 features (of a pair of CTAs); K blocks of a tile
+    int whole;                   // tiles 0 .. whole - 1 go round the pairs
+    int tail, sharers;           // the next `tail` tiles are cut into `sharers` equal runs of K blocks
+    int x_plane, w_plane;        // F32: rows between the three parts of an operand
+    int pairs, stages;
+    float* part;                 // [2 * sharers][columns][256 features]
+    uint32_t* status;
+    long long wait_clk;
+};
+
+// A piece of work: K blocks kb0 .. kb1 - 1 of a tile; slot >= 0: an unfinished sum.
+struct LinearPiece { int tile, kb0, kb1, slot; };
+struct LinearWalk {
+    int next, pair, pairs, whole, kblocks;
+    int64_t u, u1, first;
+    __device__ __forceinline__ LinearWalk(const LinearParams& p, int pair_) : next(pair_), pair(pair_), pairs(p.pairs), whole(p.whole), kblocks(p.kblocks) {
+        const int64_t units = (int64_t)p.tail * p.kblocks;
+        u = u1 = 0;
+        if (pair_ < p.sharers) { u = units * pair_ / p.sharers; u1 = units * (pair_ + 1) / p.sharers; }
+        first = u;
+    }
+    __device__ __forceinline__ bool get(LinearPiece& w) {
+        if (next < whole) {
+            w = {next, 0, kblocks, -1};
+            next += pairs;
+            return true;
+        }
+        if (u >= u1) return false;
+        const int t = (int)(u / kblocks);
+        w.tile = whole + t;
+        w.kb0 = (int)(u - (int64_t)t * kblocks);
+        w.kb1 = (int)min((int64_t)kblocks, w.kb0 + u1 - u);
+        w.slot = w.kb0 == 0 && w.kb1 == kblocks ? -1 : 2 * pair + (u == first ? 0 : 1);
+        u += w.kb1 - w.kb0;
+        return true;
+    }
+};
+
+template <int BT_, bool GATED_, int PARTS_, bool F32_OUT> struct LinearShape {
+    static constexpr int BT = BT_, PARTS = PARTS_, SETS = GATED_ ? 2 : 1;
+    static constexpr bool GATED = GATED_, FOLD = F32_OUT;
+    static constexpr int COLS = SETS * BT;                                   // of an accumulator
+    static constexpr int ROWB = PARTS == 3 ? 64 : 128, KB = ROWB / 2;        // bytes and elements of a row of a stage
+    static constexpr uint32_t A_TILE = 128 * ROWB, B_TILE = BT / 2 * ROWB, A_BYTES = PARTS * SETS * A_TILE, STAGE = A_BYTES + PARTS * B_TILE;
+    static constexpr int STAGES = (int)(206000 / STAGE) < LINEAR_MAX_STAGES ? (int)(206000 / STAGE) : LINEAR_MAX_STAGES;
+    static constexpr int EPI_WARPS = FOLD && COLS == 256 ? 16 : 8, PARTS_OF_COLS = EPI_WARPS / 4, CW = BT / PARTS_OF_COLS;   // CW: tokens of a warp
+    static constexpr int LD = CW < 16 ? CW : 16, CH = FOLD || CW < 32 ? LD : 32;   // columns read at a time onto rounded sums; finished at a time
+    static constexpr int THREADS = 128 + 32 * EPI_WARPS;
+    static constexpr uint32_t TMEM = 2 * COLS < 32 ? 32 : 2 * COLS;
+    // K blocks between hand-overs of a sum that is kept with rounding: 256 terms of BF16, 64 of F32 (with their remainders)
+    static constexpr int HAND = FOLD ? (PARTS == 3 ? 2 : 4) : 1 << 30;
+    static constexpr uint32_t SMEM = STAGES * STAGE + 1024;
+    static_assert(STAGES >= 2 && SMEM <= 220000 && (CW == 8 || CW % 32 == 0) && (TMEM & (TMEM - 1)) == 0, "");
+};
+
+struct LinearShared {
+    uint64_t full[LINEAR_MAX_STAGES], empty[LINEAR_MAX_STAGES], acc_full[2], acc_empty[2];
+    uint32_t tmem;
+    int abort_flag;
+};
+
+// Bounded wait; false when it gave up or another role did.
+__device__ __forceinline__ bool linear_wait(uint64_t* bar, uint32_t parity, LinearShared* sh, const LinearParams& p) {
+    const uint32_t b = smem_u32(bar);
+    if (mbar_try_wait(b, parity)) return true;
+    const long long since = clock64();
+#pragma unroll 1
+    while (!mbar_try_wait(b, parity)) {
+        if (*(volatile int*)&sh->abort_flag) return false;
+        if (clock64() - since > p.wait_clk) {
+            *(volatile int*)&sh->abort_flag = 1;
+            report(p.status, CCV3D_TOKENS_TIMEOUT);
+            return false;
+        }
+    }
+    return true;
+}
+__device__ __forceinline__ bool linear_warp_wait(uint64_t* bar, uint32_t parity, LinearShared* sh, const LinearParams& p) {
+    return __all_sync(0xffffffffu, linear_wait(bar, parity, sh, p));
+}
+
+template <int N>
+__device__ __forceinline__ void tc_ld(uint32_t at, uint32_t (&v)[32]) {
+    if constexpr (N == 32) tc_ld32(at, v);
+    else if constexpr (N == 16) tc_ld16(at, v);
+    else {
+        static_assert(N == 8, "");
+        asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                     : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7])
+                     : "r"(at)
+                     : "memory");
+    }
+}
+
+__device__ __forceinline__ float bias_at(const LinearParams& p, int i) {
+    return p.bias_f32 ? __ldg((const float*)p.bias + i) : __bfloat162float(((const __nv_bfloat16*)p.bias)[i]);
+}
+
+// The epilogue of N tokens t0 .. of one feature: g (and u) hold the sums, bg and bu the biases.
+template <typename TO, bool GATED, int N>
+__device__ __forceinline__ void linear_finish(const LinearParams& p, int n, int t0, float* g, const float* u, float bg, float bu) {
+    constexpr bool EXACT = sizeof(TO) == 4;
+    const int live = n < p.n_out ? min(N, p.rows - t0) : 0;
+    if (live <= 0) return;
+    float r[N];
+    if (p.res) {
+        const TO* at = (const TO*)p.res + (int64_t)t0 * p.res_stride + n;
+#pragma unroll
+        for (int j = 0; j < N; ++j) r[j] = j < live ? load1(at + j * p.res_stride) : 0.f;
+    }
+    auto apply = [&](auto kind) {
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+            g[j] = activate<EXACT>(g[j] + bg, decltype(kind)::value);
+            if (GATED) g[j] *= u[j] + bu;
+        }
+    };
+    switch (p.act) {
+        case CCV3D_ACT_SILU: apply(std::integral_constant<int, CCV3D_ACT_SILU>()); break;
+        case CCV3D_ACT_GELU: apply(std::integral_constant<int, CCV3D_ACT_GELU>()); break;
+        case CCV3D_ACT_GELU_TANH: apply(std::integral_constant<int, CCV3D_ACT_GELU_TANH>()); break;
+        default: apply(std::integral_constant<int, CCV3D_ACT_NONE>());
+    }
+    TO* at = (TO*)p.out + (int64_t)t0 * p.out_stride + n;
+#pragma unroll
+    for (int j = 0; j < N; ++j)
+        if (j < live) store1(at + j * p.out_stride, p.res ? r[j] + g[j] : g[j]);
+}
+
+template <typename S, typename TO>
+__global__ void __launch_bounds__(S::THREADS, 1) __cluster_dims__(2, 1, 1)
+linear_tile_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ LinearParams p) {
+    extern __shared__ uint8_t linear_smem[];
+    __shared__ LinearShared shared;
+    LinearShared* sh = &shared;
+    const uint32_t base = (smem_u32(linear_smem) + 1023u) & ~1023u;
+    const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
+    const uint32_t rank = cluster_rank();
+    const int pair = blockIdx.x >> 1;
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < S::STAGES; ++i) { mbar_init(smem_u32(&sh->full[i]), 1); mbar_init(smem_u32(&sh->empty[i]), 1); }
+        for (int i = 0; i < 2; ++i) { mbar_init(smem_u32(&sh->acc_full[i]), 1); mbar_init(smem_u32(&sh->acc_empty[i]), 2 * S::EPI_WARPS); }
+        sh->abort_flag = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    cluster_sync_all();                  // both CTAs' barriers exist before anything of the peer can arrive on them
+    if (warp == 2) {
+        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(&sh->tmem)), "r"(S::TMEM) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = sh->tmem;
+    asm volatile("griddepcontrol.wait;" ::: "memory");               // (the split operands)
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    bool ok = true;
+    LinearWalk walk(p, pair);
+    LinearPiece w;
+    if (warp == 0) {
+        // ------------------------------------------------------------------------------------------ loads
+        if (lane == 0) {
+            asm volatile("prefetch.tensormap [%0];" ::"l"(&tm_w) : "memory");
+            asm volatile("prefetch.tensormap [%0];" ::"l"(&tm_x) : "memory");
+            int s = 0;
+            uint32_t ph = 1;
+            while (ok && walk.get(w)) {
+                const int nt = w.tile % p.n_tiles, f0 = nt * 256 + (int)rank * 128, t0 = w.tile / p.n_tiles * S::BT + (int)rank * (S::BT / 2);
+                for (int kb = w.kb0; kb < w.kb1; ++kb) {
+                    if (!(ok = linear_wait(&sh->empty[s], ph, sh, p))) break;
+                    const uint32_t bar = smem_u32(&sh->full[s]), at = base + s * S::STAGE;
+                    if (rank == 0) mbar_expect_tx(bar, 2 * S::STAGE);      // both CTAs' boxes are counted on the leader's barrier
+#pragma unroll
+                    for (int i = 0; i < S::PARTS; ++i) {
+#pragma unroll
+                        for (int h = 0; h < S::SETS; ++h)
+                            tma_load_2d_pair(at + (i * S::SETS + h) * S::A_TILE, &tm_w, bar, kb * S::KB, i * p.w_plane + h * p.n_out + f0);
+                        tma_load_2d_pair(at + S::A_BYTES + i * S::B_TILE, &tm_x, bar, kb * S::KB, i * p.x_plane + t0);
+                    }
+                    if (++s == S::STAGES) { s = 0; ph ^= 1; }
+                }
+            }
+        }
+    } else if (warp == 1 && rank == 0) {
+        // ------------------------------------------------------------------------------------------ MMAs
+        // D = F32, A = B = BF16, both K-major, M = 256, N = BT
+        constexpr uint32_t IDESC = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(S::BT >> 3) << 17) | ((256u >> 4) << 24);
+        constexpr uint32_t HI = ((8u * S::ROWB) >> 4) | (1u << 14) | ((S::ROWB == 128 ? 2u : 4u) << 29);
+        const uint32_t a0 = ((base & 0x3FFFFu) >> 4) | (1u << 16), b0 = a0 + (S::A_BYTES >> 4);
+        int s = 0, acc = 0;
+        uint32_t ph = 0, acc_ph = 1;
+        while (ok && walk.get(w)) {
+            for (int kb = w.kb0; ok && kb < w.kb1;) {
+                const int end = min(w.kb1 - kb, S::HAND) + kb;
+                if (!(ok = linear_warp_wait(&sh->acc_empty[acc], acc_ph, sh, p))) break;
+                tc_fence_after();
+                const uint32_t d = tmem + acc * S::COLS;
+                uint32_t add = 0;
+                for (; kb < end; ++kb) {
+                    if (!(ok = linear_warp_wait(&sh->full[s], ph, sh, p))) break;
+                    tc_fence_after();
+                    if (elect_one()) {
+                        const uint32_t a = a0 + s * (S::STAGE >> 4), b = b0 + s * (S::STAGE >> 4);
+#pragma unroll
+                        for (int o = S::PARTS - 1; o >= 0; --o)          // products of parts i and o - i: the small ones first
+#pragma unroll
+                            for (int i = o; i >= 0; --i)
+#pragma unroll
+                                for (int k = 0; k < S::KB / 16; ++k)
+#pragma unroll
+                                    for (int h = 0; h < S::SETS; ++h)
+                                        tc_mma_bf16_pair(d + h * S::BT, a + (i * S::SETS + h) * (S::A_TILE >> 4) + 2 * k, HI, b + (o - i) * (S::B_TILE >> 4) + 2 * k, HI,
+                                                         IDESC, o < S::PARTS - 1 || i < o || k > 0 ? 1u : add);
+                        tc_commit_pair(smem_u32(&sh->empty[s]));
+                        if (kb + 1 == end) tc_commit_pair(smem_u32(&sh->acc_full[acc]));
+                    }
+                    __syncwarp();
+                    add = 1;
+                    if (++s == S::STAGES) { s = 0; ph ^= 1; }
+                }
+                acc ^= 1;
+                if (acc == 0) acc_ph ^= 1;
+            }
+        }
+    } else if (warp >= 4) {
+        // ------------------------------------------------------------------------------------------ epilogue
+        const int q = warp & 3, half = (warp - 4) >> 2;                 // lanes 32 q .., part of the columns
+        const uint32_t mine = tmem + ((uint32_t)q << 21) + half * S::CW;
+        int acc = 0;
+        uint32_t ph = 0;
+        while (ok && walk.get(w)) {
+            const int nt = w.tile % p.n_tiles, f = (int)rank * 128 + q * 32 + lane, n = nt * 256 + f, t0 = w.tile / p.n_tiles * S::BT + half * S::CW;
+            float bg = 0.f, bu = 0.f;
+            if (p.bias && n < p.n_out) {
+                bg = bias_at(p, n);
+                if (S::GATED) bu = bias_at(p, p.n_out + n);
+            }
+            // sums of CH tokens from column c of the warp's on: finished, or put down for the join
+            auto leave = [&](int c, float* g, float* u) {
+                if (w.slot < 0) {
+                    linear_finish<TO, S::GATED, S::CH>(p, n, t0 + c, g, u, bg, bu);
+                    return;
+                }
+                float* at = p.part + ((int64_t)w.slot * S::COLS + half * S::CW + c) * 256 + f;
+#pragma unroll
+                for (int j = 0; j < S::CH; ++j) {
+                    at[j * 256] = g[j];
+                    if (S::GATED) at[(S::BT + j) * 256] = u[j];
+                }
+            };
+            if constexpr (S::FOLD) {
+                float sum[S::SETS][S::CW];
+#pragma unroll
+                for (int h = 0; h < S::SETS; ++h)
+#pragma unroll
+                    for (int j = 0; j < S::CW; ++j) sum[h][j] = 0.f;
+                for (int kb = w.kb0; kb < w.kb1; kb += S::HAND) {
+                    if (!(ok = linear_warp_wait(&sh->acc_full[acc], ph, sh, p))) break;
+                    tc_fence_after();
+#pragma unroll
+                    for (int h = 0; h < S::SETS; ++h)
+#pragma unroll
+                        for (int c = 0; c < S::CW; c += S::LD) {
+                            uint32_t v[32];
+                            tc_ld<S::LD>(mine + acc * S::COLS + h * S::BT + c, v);
+                            tc_wait_ld();
+#pragma unroll
+                            for (int j = 0; j < S::LD; ++j) sum[h][c + j] += __uint_as_float(v[j]);
+                        }
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive_leader(smem_u32(&sh->acc_empty[acc]));
+                    acc ^= 1;
+                    if (acc == 0) ph ^= 1;
+                }
+                if (ok) {
+#pragma unroll
+                    for (int c = 0; c < S::CW; c += S::CH) leave(c, &sum[0][c], &sum[S::SETS - 1][c]);
+                }
+            } else {
+                if (!(ok = linear_warp_wait(&sh->acc_full[acc], ph, sh, p))) break;
+                tc_fence_after();
+#pragma unroll 1
+                for (int c = 0; c < S::CW; c += S::CH) {
+                    uint32_t v[2][32];
+#pragma unroll
+                    for (int h = 0; h < S::SETS; ++h) tc_ld<S::CH>(mine + acc * S::COLS + h * S::BT + c, v[h]);
+                    tc_wait_ld();
+                    if (c + S::CH == S::CW) {
+                        tc_fence_before();
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive_leader(smem_u32(&sh->acc_empty[acc]));
+                    }
+                    float g[S::CH], u[S::CH];
+#pragma unroll
+                    for (int j = 0; j < S::CH; ++j) { g[j] = __uint_as_float(v[0][j]); u[j] = __uint_as_float(v[S::SETS - 1][j]); }
+                    leave(c, g, u);
+                }
+                acc ^= 1;
+                if (acc == 0) ph ^= 1;
+            }
+        }
+    }
+    if (!ok) {                                       // loads and MMAs still in flight
+        const long long t = clock64();
+        while (clock64() - t < 400000) __nanosleep(1000);
+    }
+    tc_fence_before();
+    __syncthreads();
+    cluster_sync_all();                              // the leader's MMAs read the peer's shared memory and write its tensor memory
+    if (warp == 2) {
+        tc_fence_after();
+        asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(S::TMEM) : "memory");
+    }
+}
+
+// The sums of the tiles that were cut along K: block (tile of the tail, group of 8 tokens), a thread to a feature.
+constexpr int LINEAR_JOIN_TOKENS = 8;
+template <typename TO, bool GATED>
+__global__ void __launch_bounds__(256) linear_join_kernel(const __grid_constant__ LinearParams p, int BT) {
+    asm volatile("griddepcontrol.wait;" ::: "memory");
+    const int t = blockIdx.x, c = blockIdx.y * LINEAR_JOIN_TOKENS, f = threadIdx.x, tile = p.whole + t, cols = GATED ? 2 * BT : BT;
+    const int n = tile % p.n_tiles * 256 + f, t0 = tile / p.n_tiles * BT + c;
+    const int64_t units = (int64_t)p.tail * p.kblocks, begin = (int64_t)t * p.kblocks, end = begin + p.kblocks;
+    const int64_t from = ((begin + 1) * p.sharers - 1) / units, to = (end * p.sharers - 1) / units;      // the sharers of the first and last K block
+    if (from == to || n >= p.n_out || t0 >= p.rows) return;
+    float g[LINEAR_JOIN_TOKENS], u[LINEAR_JOIN_TOKENS];
+#pragma unroll
+    for (int j = 0; j < LINEAR_JOIN_TOKENS; ++j) g[j] = u[j] = 0.f;
+    for (int64_t i = from; i <= to; ++i) {
+        const int64_t slot = 2 * i + (units * i / p.sharers >= begin ? 0 : 1);
+        const float* at = p.part + (slot * cols + c) * 256 + f;
+#pragma unroll
+        for (int j = 0; j < LINEAR_JOIN_TOKENS; ++j) {
+            g[j] += at[j * 256];
+            if (GATED) u[j] += at[(BT + j) * 256];
+        }
+    }
+    float bg = 0.f, bu = 0.f;
+    if (p.bias) {
+        bg = bias_at(p, n);
+        if (GATED) bu = bias_at(p, p.n_out + n);
+    }
+    linear_finish<TO, GATED, LINEAR_JOIN_TOKENS>(p, n, t0, g, u, bg, bu);
+}
+
+// F32 rows as three BF16 numbers each, in three planes [rows][pitch]: rounded to 8 bits, what is left to 8 more, and the rest (8 bits: exact).
+// A thread to four elements.
+__global__ void __launch_bounds__(256) linear_split_kernel(const float* x, int64_t stride, int rows, int k, __nv_bfloat16* to, int pitch) {
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    const int quads = pitch / 4;
+    const int64_t all = (int64_t)rows * quads;
+    for (int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; i < all; i += (int64_t)gridDim.x * blockDim.x) {
+        const int64_t r = i / quads;
+        const int c = (int)(i - r * quads) * 4;
+        float v[4] = {0.f, 0.f, 0.f, 0.f}, a[4], b[4], d[4];
+        const float* at = x + r * stride + c;
+        if (c + 4 <= k) load4(at, v);
+        else
+            for (int j = 0; c + j < k; ++j) v[j] = at[j];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const float whole = 3.38953138925e38f;                        // largest BF16 number: what lies above it must not become an infinity
+            a[j] = isinf(v[j]) ? v[j] : __bfloat162float(__float2bfloat16_rn(isnan(v[j]) ? v[j] : fminf(fmaxf(v[j], -whole), whole)));
+            const float rest = isfinite(v[j]) ? v[j] - a[j] : 0.f;
+            b[j] = __bfloat162float(__float2bfloat16_rn(rest));
+            d[j] = rest - b[j];
+        }
+        __nv_bfloat16* o = to + r * pitch + c;
+        const int64_t plane = (int64_t)rows * pitch;
+        store4(o, a);
+        store4(o + plane, b);
+        store4(o + 2 * plane, d);
+    }
+}
+
+}  // namespace ccv3d

@@ -11,8 +11,9 @@ import threading
 
 import torch
 
-from . import (BF16, F32, NORM_LAYER, NORM_NONE, NORM_RMS, OK, Ccv3dError, Heads, KvCache, NormDesc, RotaryC, TokenBatchC,
-               ccv3d_kv_attend_workspace, lib)
+from . import (ACTIVATIONS, BF16, F32, NORM_LAYER, NORM_NONE, NORM_RMS, OK, Ccv3dError, DecayMemoryC, GroupNormDesc, Heads, KvCache,
+               LinearDesc, NormDesc, RotaryC, StreamBatchC, TokenBatchC, ccv3d_decay_attend_workspace, ccv3d_group_norm_ring_workspace,
+               ccv3d_group_norm_workspace, ccv3d_kv_attend_workspace, ccv3d_linear_workspace, lib)
 
 _DTYPES = {torch.bfloat16: BF16, torch.float32: F32}
 _KINDS = {"none": NORM_NONE, "rms": NORM_RMS, "layer": NORM_LAYER}
@@ -348,3 +349,274 @@ def gated_norm(x, y=None, *, gate=None, post_weight=None, post_bias=None, pre_we
     if s != OK:
         raise Ccv3dError(s, "ccv3d_gated_norm")
     return out_r, out_h
+
+
+# ---- scratch of a call: taken from torch's allocator on the current stream and given back when the call has been made, so that what
+# ---- follows on the stream may have it next (and a captured call's belongs to its graph)
+_needs = {}
+
+
+def _scratch(key, ask, what, *args):
+    """(tensor or None, address, bytes) of scratch for a call; `key` says what the size depends on."""
+    need = _needs.get(key)
+    if need is None:
+        s, need = ask(*args)
+        if s != OK:
+            raise Ccv3dError(s, what)
+        if len(_needs) > 4096:
+            _needs.clear()
+        _needs[key] = need
+    if need == 0:
+        return None, None, 0
+    ws = torch.empty(need, dtype=torch.uint8, device="cuda")
+    return ws, ws.data_ptr(), need
+
+
+def _vector(t, what, n, dtype, dev):
+    if t is None:
+        return None
+    if t.shape != (n,) or t.dtype != dtype or not t.is_contiguous():
+        raise ValueError(f"{what} must be a contiguous [{n}] tensor of {dtype}, not {t.dtype} {tuple(t.shape)}")
+    if t.get_device() != dev:
+        raise _elsewhere(t, what, dev)
+    return t.data_ptr()
+
+
+def _per_sample(t, what, samples, ch, dev):
+    """(address, elements between rows) of a float32 [samples, channels] tensor, which may be a slice."""
+    if t is None:
+        return None, 0
+    if t.dtype != torch.float32:
+        raise TypeError(f"{what} must be float32")
+    return t.data_ptr(), _rows(t, what, samples, ch, dev)
+
+
+def _activation(name):
+    kind = ACTIVATIONS.get(name)
+    if kind is None:
+        raise ValueError(f"activation {name!r} is none of {', '.join(ACTIVATIONS)}")
+    return kind
+
+
+def group_norm(x, groups: int, weight=None, bias=None, *, scale=None, shift=None, eps: float = 1e-6, activation: str = "none", out=None):
+    """act((norm(x) * weight + bias) * (1 + scale) + shift), as ``ccv3d_group_norm`` says: x [samples, pixels, channels] (channels dense, any
+    strides), normed for each sample and group of channels over all pixels.  weight and bias are [channels], scale
+    and shift [samples, channels], all float32.  ``out`` may be x."""
+    if x.dim() != 3:
+        raise ValueError("x must be [samples, pixels, channels]")
+    samples, pixels, ch = x.shape
+    dt, dev = _dtype(x, "x"), _device()
+    for n, what in ((samples, "the number of samples"), (pixels, "the number of pixels"), (ch, "the number of channels")):
+        _int32(n, what)
+    _int32(groups, "groups")
+    if out is None:
+        out = _like(x, memory_format=_DENSE)
+    elif out.dtype != x.dtype or out.shape != x.shape:
+        raise ValueError("out must have x's shape and type")
+    for t, what in ((x, "x"), (out, "out")):
+        if t.get_device() != dev:
+            raise _elsewhere(t, what, dev)
+        if t.stride(2) != 1 and ch > 1:
+            raise ValueError(f"{what}: the last dimension must be contiguous")
+    sc, sc_stride = _per_sample(scale, "scale", samples, ch, dev)
+    sh, sh_stride = _per_sample(shift, "shift", samples, ch, dev)
+    w, b = _vector(weight, "weight", ch, torch.float32, dev), _vector(bias, "bias", ch, torch.float32, dev)
+    d = GroupNormDesc(samples, pixels, ch, groups, _activation(activation), dt, eps, x.stride(0), x.stride(1), out.stride(0), out.stride(1),
+                      sc_stride, sh_stride)
+    keep, ws, need = _scratch(("group_norm", samples, pixels, ch, groups, dt), ccv3d_group_norm_workspace, "ccv3d_group_norm_workspace", d)
+    s = lib.ccv3d_group_norm(d, x.data_ptr(), w, b, sc, sh, out.data_ptr(), ws, need, _stream(dev))
+    if s != OK:
+        raise Ccv3dError(s, "ccv3d_group_norm")
+    return out
+
+
+def ring_group_norm(ring, slot, T, groups, weight, bias, scale, shift, eps, activation, out_ring, out_slot):
+    """``FrameRing.group_norm``."""
+    dev = _device()
+    for r in (ring, out_ring):
+        if r.buf.get_device() != dev:
+            raise _elsewhere(r.buf, "the ring", dev)
+    for n, what in ((slot, "slot"), (out_slot, "out_slot"), (T, "T"), (groups, "groups")):
+        _int32(n, what)
+    samples = ring.N * T
+    sc, sc_stride = _per_sample(scale, "scale", samples, ring.C, dev)
+    sh, sh_stride = _per_sample(shift, "shift", samples, ring.C, dev)
+    w, b = _vector(weight, "weight", ring.C, torch.float32, dev), _vector(bias, "bias", ring.C, torch.float32, dev)
+    keep, ws, need = _scratch(("ring", ring.N, ring.C, ring.F, ring.H, ring.W, T, groups), ccv3d_group_norm_ring_workspace,
+                              "ccv3d_group_norm_ring_workspace", ring.c, T, groups)
+    s = lib.ccv3d_group_norm_ring(ring.c, slot, out_ring.c, out_slot, T, groups, w, b, sc, sc_stride, sh, sh_stride, eps,
+                                  _activation(activation), ws, need, _stream(dev))
+    if s != OK:
+        raise Ccv3dError(s, "ccv3d_group_norm_ring")
+
+
+_words = {}              # device -> word that products report in
+
+
+def _word(dev):
+    w = _words.get(dev)
+    if w is None:
+        # (there for every stream; a capture cannot make it, and its first call goes without)
+        if _capturing():
+            return None
+        w = _words[dev] = torch.zeros(1, dtype=torch.int32).to(f"cuda:{dev}")
+    return w.data_ptr()
+
+
+def status() -> int:
+    """TOKENS_* bits that products (``linear``) on the current device have reported, cleared by reading.  Waits for the device."""
+    dev = _device()
+    _synchronize(dev)
+    w = _words.get(dev)
+    bits = 0 if w is None else int(w.item())
+    if bits:
+        w.zero_()
+        _synchronize(dev)
+    return bits
+
+
+def linear(x, weight, bias=None, *, activation: str = "none", gated: bool = False, residual=None, out=None, out_dtype=None):
+    """residual + act(x weight^T + bias), or gated: residual + act(x w1^T + b1) * (x w2^T + b2) for weight [w1; w2] and bias [b1; b2]
+    (``ccv3d_linear``).
+
+    x [rows, k] and weight [n, k] (gated [2 n, k]) have one type, rows dense and on 16 bytes; bias has it too.  out [rows, n] has x's
+    type, or ``out_dtype`` (float32), which residual has as well; it may be residual."""
+    if x.dim() != 2 or weight.dim() != 2 or weight.shape[1] != x.shape[1]:
+        raise ValueError(f"x {tuple(x.shape)} and weight {tuple(weight.shape)} must be [rows, k] and [n, k]")
+    rows, k = x.shape
+    n, dev = weight.shape[0], _device()
+    dt = _dtype(x, "x")
+    if weight.dtype != x.dtype:
+        raise TypeError("x and weight must have one type")
+    if gated:
+        if n % 2:
+            raise ValueError("a gated pair has an even number of rows of weights")
+        n //= 2
+    for v, what in ((rows, "the number of rows"), (k, "k"), (2 * n, "the number of features")):
+        _int32(v, what)
+    if out is not None:
+        if out_dtype is not None and out_dtype != out.dtype:
+            raise TypeError("out_dtype differs from out's type")
+        out_dtype = out.dtype
+    elif out_dtype is None:
+        out_dtype = x.dtype
+    od = _DTYPES.get(out_dtype)
+    if od is None:
+        raise TypeError(f"{out_dtype} is neither bfloat16 nor float32")
+    if dt == F32 and od != F32:
+        raise TypeError("a product of float32 is float32")
+    xs, ws_ = _rows(x, "x", rows, k, dev), _rows(weight, "weight", weight.shape[0], k, dev)
+    b = _vector(bias, "bias", weight.shape[0], x.dtype, dev)
+    rs = n
+    if residual is not None:
+        if residual.dtype != out_dtype:
+            raise TypeError(f"residual must be {out_dtype}")
+        rs = _rows(residual, "residual", rows, n, dev)
+    if out is None:
+        out, os_ = x.new_empty((rows, n), dtype=out_dtype), n
+    else:
+        os_ = _rows(out, "out", rows, n, dev)
+    if rows == 0 or n == 0:
+        return out
+    d = LinearDesc(rows, n, k, bool(gated), _activation(activation), dt, od, xs, ws_, os_, rs)
+    keep, ws, need = _scratch(("linear", dev, rows, n, k, bool(gated), dt), ccv3d_linear_workspace, "ccv3d_linear_workspace", d)
+    s = lib.ccv3d_linear(d, x.data_ptr(), weight.data_ptr(), b, _ptr(residual), out.data_ptr(), ws, need, _word(dev), _stream(dev))
+    if s != OK:
+        raise Ccv3dError(s, "ccv3d_linear")
+    return out
+
+
+class StreamBatch:
+    """The sequences of a call on decaying states (``ccv3d_stream_batch``): packed offsets of their new tokens [batch + 1], the
+    slots of their states [batch], and, where given, which of them start anew (``fresh`` [batch], not 0), int32 on the device.  The arrays
+    may be changed in place between calls; ``max_new`` bounds the new tokens of any sequence.  May serve several calls at a time."""
+
+    def __init__(self, new_start, slot, max_new: int, fresh=None):
+        dev = _device()
+        b = slot.shape[0]
+        _int_array(new_start, "new_start", (b + 1,), dev)
+        _int_array(slot, "slot", (b,), dev)
+        if fresh is not None:
+            _int_array(fresh, "fresh", (b,), dev)
+        self.new_start, self.slot, self.fresh, self.max_new = new_start, slot, fresh, _int32(int(max_new), "max_new")
+        self.device = dev
+        self._at = (new_start.data_ptr(), slot.data_ptr(), _ptr(fresh), b)
+        self._c = {}
+
+    def c(self, tokens: int) -> StreamBatchC:
+        """The struct of a call with so many rows (kept, and not written again)."""
+        c = self._c.get(tokens)
+        if c is None:
+            if len(self._c) >= 64:
+                self._c = {}
+            c = self._c[tokens] = StreamBatchC(*self._at, tokens, self.max_new)
+        return c
+
+
+class DecayMemory:
+    """States of fixed size from which old tokens fade, one for each slot and head: float32 [slots, heads, key_dim, value_dim].
+
+    ``DecayMemory.empty`` allocates them (zeros)."""
+
+    def __init__(self, states):
+        dev = _device()
+        if states.dtype != torch.float32 or states.dim() != 4 or not states.is_contiguous():
+            raise ValueError("states must be a contiguous float32 tensor [slots, heads, key_dim, value_dim]")
+        _on_device(states, "states", dev)
+        self.states, self.device = states, dev
+        self.slots, self.heads, self.key_dim, self.value_dim = states.shape
+        self.c = DecayMemoryC(states.data_ptr(), *states.shape)
+        # there for every stream when this returns (in a capture, whose every replay zeroes it: for what follows there)
+        self._status = torch.zeros(1, dtype=torch.int32, device=states.device if _capturing() else None).to(states.device)
+        self._status_ptr = self._status.data_ptr()
+
+    @classmethod
+    def empty(cls, slots, heads, key_dim, value_dim):
+        return cls(torch.zeros((slots, heads, key_dim, value_dim), dtype=torch.float32, device="cuda"))
+
+    def status(self) -> int:
+        """TOKENS_* bits that the calls so far have reported, cleared by reading.  Waits for the device."""
+        _synchronize(self.device)
+        bits = int(self._status.item())
+        if bits:
+            self._status.zero_()
+            _synchronize(self.device)
+        return bits
+
+    def attend(self, q, k, v, log_decay, batch: StreamBatch, scale: float | None = None, out=None):
+        """Takes the new tokens' keys and values into the states of their sequences, each after the states have faded by
+        exp(log_decay), and reads them with the queries (``ccv3d_decay_attend``): q, k [tokens, qk_heads, key_dim], v, out [tokens, heads,
+        value_dim], log_decay [tokens, heads] float32; ``scale`` defaults to key_dim ** -0.5.  Rows behind the last sequence's are not written."""
+        tokens, dev, heads = q.shape[0], self.device, self.heads
+        if batch.device != dev:
+            raise ValueError("the batch lies on another device than the states")
+        if _device() != dev:
+            raise ValueError(f"the states lie on cuda:{dev}, which is not the current device")
+        c = batch.c(tokens)
+        dt = _dtype(q, "q")
+        if k.dtype != q.dtype or v.dtype != q.dtype:
+            raise TypeError("q, k and v must have one type")
+        if k.shape != q.shape:
+            raise ValueError(f"q {tuple(q.shape)} and k {tuple(k.shape)} must have one shape")
+        cq, ck = _heads(q, "q", tokens, self.key_dim, dev), _heads(k, "k", tokens, self.key_dim, dev)
+        cv = _heads(v, "v", tokens, self.value_dim, dev)
+        if v.shape[1] != heads:
+            raise ValueError(f"v has {v.shape[1]} heads, the states {heads}")
+        if log_decay.dtype != torch.float32 or log_decay.shape != (tokens, heads):
+            raise ValueError(f"log_decay must be float32 [{tokens}, {heads}], not {log_decay.dtype} {tuple(log_decay.shape)}")
+        _on_device(log_decay, "log_decay", dev)
+        if out is None:
+            out = _like(v, memory_format=_DENSE)
+            co = Heads(out.data_ptr(), heads * self.value_dim, self.value_dim)
+        elif out.dtype != v.dtype or out.shape != v.shape:
+            raise ValueError("out must have v's shape and type")
+        else:
+            co = _heads(out, "out", tokens, self.value_dim, dev)
+        qk_heads = q.shape[1]
+        keep, ws, need = _scratch(("decay", dev, c.batch, tokens, c.max_new, heads, self.key_dim, self.value_dim),
+                                  ccv3d_decay_attend_workspace, "ccv3d_decay_attend_workspace", self.c, c, qk_heads, dt)
+        s = lib.ccv3d_decay_attend(self.c, c, cq, ck, cv, log_decay.data_ptr(), log_decay.stride(0), log_decay.stride(1), co, qk_heads,
+                                   dt, self.key_dim ** -0.5 if scale is None else scale, ws, need, self._status_ptr, _stream(dev))
+        if s != OK:
+            raise Ccv3dError(s, "ccv3d_decay_attend")
+        return out
