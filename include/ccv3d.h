@@ -629,7 +629,7 @@ ccv3d_status ccv3d_decay_attend_workspace(const ccv3d_decay_memory* memory, cons
  * its sample and group NaN.  y may be x itself (same strides).  Any other overlap is CCV3D_ERR_ALIAS.
  *   groups divides channels; channels <= 16384; samples and pixels from 0 (samples or pixels 0: a call without work)
  *   ws      DEVICE scratch, 256-byte aligned, ccv3d_group_norm_workspace() bytes, of the call alone (NULL where that is 0)
- * The same sample gives the same bits whatever is normed beside it (up to samples of 1 MB).  Stream-ordered, no allocation, legal in a stream capture.
+ * A sample gives the same bits whatever is normed beside it.  Stream-ordered, no allocation, legal in a stream capture.
  */
 typedef struct {
     int32_t samples, pixels, channels, groups;

@@ -7,27 +7,36 @@ using namespace ccv3d;
 namespace {
 
 constexpr int GN_SMEM = 100 * 1024;
-constexpr int GN_PIECES = 16;            // most pieces of a thread in the one-pass form
+constexpr int GN_PIECES = 8;             // most pieces of a thread in the one-pass form
 
-// How a call is cut up.  It goes by the sample's size and type alone, not by how many samples there are, so that a stream of frames has the
-// same bits however it is cut into calls.
+// How a call is cut up.  It goes by the sample's size and type alone, not by how many samples there are (but for how many go at once), so that
+// a stream of frames has the same bits however it is cut into calls.
 struct GnPlan {
-    bool vec, whole;
-    int V, columns, lanes, chunks;       // chunks: of columns (two-kernel form)
+    bool vec, token, whole;
+    int V, columns, lanes, chunks;       // chunks: of columns (token and three-kernel forms)
     int cluster, pieces;                 // one-pass form
-    int tile_pixels, tiles, at_once;     // two-kernel form; samples of a pair of launches
+    int tile_pixels, tiles, unit, at_once;   // three-kernel form: pixels of a block, channels of a unit, samples of a turn of launches
+    uint64_t factors_at;
     uint64_t bytes;
 };
 
-GnPlan gn_plan(int64_t samples, int64_t pixels, int C, int groups, int dtype, bool vec) {
+GnPlan gn_plan(int64_t samples, int64_t pixels, int C, int groups, int dtype, bool vec, bool ring = false) {
     GnPlan q = {};
     q.vec = vec;
     q.V = vec ? 16 / (int)esize(dtype) : 1;
-    const int VC = C / q.V;
+    const int VC = C / q.V, wide = C / groups / q.V;
+    if (pixels == 1 && !ring && C / groups % q.V == 0 && wide <= 32 && (wide & (wide - 1)) == 0) {
+        // (a block's columns are whole groups)
+        q.token = true;
+        q.columns = VC < GN_THREADS ? VC : GN_THREADS / wide * wide;
+        q.chunks = (VC + q.columns - 1) / q.columns;
+        q.lanes = q.columns < 256 ? 256 / q.columns : 1;
+        return q;
+    }
     if (VC <= GN_THREADS) {
-        // the fewest blocks that leave a thread four pieces at most, sixteen blocks where that takes more
+        // the fewest blocks that leave a thread four pieces at most, eight blocks where that takes more
         const int lanes = GN_THREADS / VC;
-        for (q.cluster = 1; q.cluster < 16 && pixels > (int64_t)4 * q.cluster * lanes; q.cluster *= 2) {}
+        for (q.cluster = 1; q.cluster < 8 && pixels > (int64_t)4 * q.cluster * lanes; q.cluster *= 2) {}
         const int64_t share = (pixels + q.cluster - 1) / q.cluster;
         q.lanes = (int)(share < lanes ? share : lanes);
         const int64_t pieces = (share + q.lanes - 1) / q.lanes;
@@ -39,16 +48,23 @@ GnPlan gn_plan(int64_t samples, int64_t pixels, int C, int groups, int dtype, bo
             return q;
         }
     }
-    q.columns = VC < GN_THREADS ? VC : GN_THREADS;
+    q.columns = VC < GN_BIG_THREADS ? VC : GN_BIG_THREADS;
     q.chunks = (VC + q.columns - 1) / q.columns;
-    q.lanes = GN_THREADS / q.columns;
-    const int64_t step = (int64_t)q.lanes * GN_BATCH, batches = (pixels + step * 296 - 1) / (step * 296);      // some 300 tiles at most: two for an SM
-    q.tile_pixels = (int)(step * batches < pixels ? step * batches : pixels);
+    q.lanes = GN_BIG_THREADS / q.columns;
+    // A block to each half of an SM, or as many as have sixteen pieces for a thread.  (Four frames of 43 MB, us: 296 blocks 117, 576 136, 1152 140;
+    // three samples of 5 MB, with pieces for a thread: 8 20, 16 17, 24 19.)
+    const int64_t blocks = 296 / q.chunks > 1 ? 296 / q.chunks : 1, share = (pixels + blocks - 1) / blocks, least = (int64_t)q.lanes * 16;
+    q.tile_pixels = (int)(share > least ? share : least);
     q.tiles = (int)((pixels + q.tile_pixels - 1) / q.tile_pixels);
+    // statistics go by whole groups, or by what divides groups and chunks of columns
+    q.unit = C / groups;
+    if (q.chunks > 1)
+        for (int a = q.unit, b = q.columns * q.V; b; q.unit = a) { const int r = a % b; a = b; b = r; }
     const int64_t size = pixels * C * esize(dtype), fit = (48ll << 20) / size;      // what is read again shall still be in L2
     const int64_t most = 65535;
     q.at_once = (int)(fit < 1 ? 1 : fit < samples ? (fit < most ? fit : most) : (samples < most ? samples : most));
-    q.bytes = ((uint64_t)q.at_once * q.tiles * q.chunks * groups * sizeof(float2) + 255) / 256 * 256;
+    q.factors_at = ((uint64_t)q.at_once * q.tiles * (C / q.unit) * sizeof(float2) + 255) / 256 * 256;
+    q.bytes = q.factors_at + ((uint64_t)q.at_once * 3 * C * sizeof(float) + 255) / 256 * 256;
     return q;
 }
 
@@ -56,10 +72,7 @@ template <typename T, int V, int R>
 ccv3d_status launch_whole(GroupNormParams& p, const GnPlan& q, const Device& dev, cudaStream_t st) {
     static std::atomic<uint64_t> done{0};
     auto* kernel = group_norm_whole_kernel<T, V, R>;
-    if (!(done.load(std::memory_order_relaxed) >> dev.index & 1)) {
-        if (cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess) { cudaGetLastError(); return CCV3D_ERR_CUDA; }
-        if (!allow_smem(kernel, GN_SMEM, dev.index, done)) { cudaGetLastError(); return CCV3D_ERR_CUDA; }
-    }
+    if (!allow_smem(kernel, GN_SMEM, dev.index, done)) { cudaGetLastError(); return CCV3D_ERR_CUDA; }
     cudaLaunchAttribute at[1];
     at[0].id = cudaLaunchAttributeClusterDimension;
     at[0].val.clusterDim.x = q.cluster;
@@ -77,37 +90,45 @@ ccv3d_status launch_whole(GroupNormParams& p, const GnPlan& q, const Device& dev
 
 template <typename T, int V>
 ccv3d_status launch_group_norm(GroupNormParams& p, const GnPlan& q, void* ws, const Device& dev, cudaStream_t st) {
+    if (q.token) {
+        const int per = GN_TOKENS * q.lanes;
+        group_norm_token_kernel<T, V><<<dim3((p.samples + per - 1) / per, q.chunks), (q.columns * q.lanes + 31) / 32 * 32, 0, st>>>(p);
+        return launched();
+    }
     if (q.whole) {
         if (q.pieces == 1) return launch_whole<T, V, 1>(p, q, dev, st);
         if (q.pieces == 2) return launch_whole<T, V, 2>(p, q, dev, st);
         if (q.pieces == 4) return launch_whole<T, V, 4>(p, q, dev, st);
-        if (q.pieces == 8) return launch_whole<T, V, 8>(p, q, dev, st);
-        return launch_whole<T, V, 16>(p, q, dev, st);
-    }
-    static std::atomic<uint64_t> done1{0}, done2{0};
-    if (!allow_smem(group_norm_stats_kernel<T, V>, GN_SMEM, dev.index, done1) || !allow_smem(group_norm_apply_kernel<T, V>, GN_SMEM, dev.index, done2)) {
-        cudaGetLastError();
-        return CCV3D_ERR_CUDA;
+        return launch_whole<T, V, 8>(p, q, dev, st);
     }
     p.part = (float2*)ws;
+    p.factors = (float*)((char*)ws + q.factors_at);
     p.tiles = q.tiles;
-    p.chunks = q.chunks;
     p.tile_pixels = q.tile_pixels;
-    const int chunk_groups = min(p.groups, (q.columns * V + p.per - 1) / p.per + 1);
+    p.unit = q.unit;
+    // each kernel is resident when the one before it ends; the first of a turn reads while the last turn's outputs go out
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
     for (int first = 0; first < p.samples; first += q.at_once) {
         p.first = first;
-        cudaLaunchAttribute at[1];
-        at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-        at[0].val.programmaticStreamSerializationAllowed = 1;
+        const int now = min(q.at_once, p.samples - first);
         cudaLaunchConfig_t cfg = {};
-        cfg.gridDim = dim3(q.tiles, q.chunks, min(q.at_once, p.samples - first));
-        cfg.blockDim = dim3((q.columns * q.lanes + 31) / 32 * 32);
-        cfg.dynamicSmemBytes = (size_t)(q.lanes * q.columns * V + 2 * chunk_groups) * 4;
         cfg.stream = st;
         cfg.attrs = at;
+        cfg.numAttrs = first ? 1 : 0;
+        cfg.gridDim = dim3(q.tiles, q.chunks, now);
+        cfg.blockDim = dim3((q.columns * q.lanes + 31) / 32 * 32);
+        cfg.dynamicSmemBytes = (size_t)(q.lanes * q.columns * V + 2 * (q.columns * V / q.unit)) * 4;
         if (cudaLaunchKernelEx(&cfg, group_norm_stats_kernel<T, V>, p) != cudaSuccess) { cudaGetLastError(); return CCV3D_ERR_CUDA; }
-        cfg.dynamicSmemBytes = (size_t)2 * chunk_groups * 4;
+        cfg.dynamicSmemBytes = 0;
         cfg.numAttrs = 1;
+        const dim3 tiles = cfg.gridDim, threads = cfg.blockDim;
+        cfg.gridDim = dim3(p.groups, now);
+        cfg.blockDim = dim3(GN_FOLD_THREADS);
+        if (cudaLaunchKernelEx(&cfg, group_norm_fold_kernel, p) != cudaSuccess) { cudaGetLastError(); return CCV3D_ERR_CUDA; }
+        cfg.gridDim = tiles;
+        cfg.blockDim = threads;
         if (cudaLaunchKernelEx(&cfg, group_norm_apply_kernel<T, V>, p) != cudaSuccess) { cudaGetLastError(); return CCV3D_ERR_CUDA; }
     }
     return CCV3D_OK;
@@ -139,6 +160,11 @@ bool apart(int64_t samples, int64_t pixels, int64_t C, int64_t ss, int64_t ps) {
 bool whole_vectors(const void* p, int dtype, int64_t a, int64_t b) {
     const int64_t V = 16 / esize(dtype);
     return !misaligned(p, 16) && a % V == 0 && b % V == 0;
+}
+
+bool affine_vectors(const GroupNormParams& p) {
+    return !misaligned(p.weight, 16) && !misaligned(p.bias, 16) && !misaligned(p.scale, 16) && !misaligned(p.shift, 16) &&
+           (!p.scale || p.scale_stride % 4 == 0) && (!p.shift || p.shift_stride % 4 == 0);
 }
 
 }  // namespace
@@ -192,8 +218,9 @@ ccv3d_status ccv3d_group_norm(const ccv3d_group_norm_desc* d, const void* x, con
     p.scale_stride = d->scale_stride; p.shift_stride = d->shift_stride;
     p.xv = {0, xs, xp, 0, (int)S, 0};
     p.yv = {0, ys, yp, 0, (int)S, 0};
-    p.T = (int)S; p.samples = (int)S; p.pixels = (int)P; p.C = (int)C; p.groups = d->groups; p.per = (int)C / d->groups; p.KB = (int)C;
+    p.T = (int)S; p.samples = (int)S; p.pixels = (int)P; p.C = (int)C; p.groups = d->groups; p.per = (int)C / d->groups; p.block_shift = 30;
     p.columns = q.columns; p.lanes = q.lanes; p.eps = d->eps; p.act = d->activation;
+    p.vec_affine = affine_vectors(p);
     return run_group_norm(p, q, d->dtype, ws, (cudaStream_t)stream);
 }
 
@@ -201,7 +228,7 @@ ccv3d_status ccv3d_group_norm_ring_workspace(const ccv3d_ring* in, int32_t T, in
     if (!in || !bytes_host || ccv3d_ring_bytes(in) == 0 || T < 0 || T > in->F) return CCV3D_ERR_INVALID_ARG;
     const ccv3d_status s = check_group_norm((int64_t)in->N * T, (int64_t)in->H * in->W, in->C, groups, CCV3D_ACT_NONE, CCV3D_BF16);
     if (s != CCV3D_OK) return s;
-    *bytes_host = T == 0 ? 0 : gn_plan((int64_t)in->N * T, (int64_t)in->H * in->W, in->C, groups, CCV3D_BF16, true).bytes;
+    *bytes_host = T == 0 ? 0 : gn_plan((int64_t)in->N * T, (int64_t)in->H * in->W, in->C, groups, CCV3D_BF16, true, true).bytes;
     return CCV3D_OK;
 }
 
@@ -220,7 +247,7 @@ ccv3d_status ccv3d_group_norm_ring(const ccv3d_ring* in, int32_t in_slot, const 
     if (S == 0) return CCV3D_OK;
     if (misaligned(in->base, 16) || misaligned(out->base, 16) || misaligned(weight, 4) || misaligned(bias, 4) || misaligned(scale, 4) || misaligned(shift, 4))
         return CCV3D_ERR_ALIGNMENT;
-    const GnPlan q = gn_plan(S, P, C, groups, CCV3D_BF16, true);
+    const GnPlan q = gn_plan(S, P, C, groups, CCV3D_BF16, true, true);
     if ((s = check_ws(ws, ws_bytes, q.bytes)) != CCV3D_OK) return s;
     const Span a = span_of(in->base, (int64_t)ccv3d_ring_bytes(in)), b = span_of(out->base, (int64_t)ccv3d_ring_bytes(out)), w = span_of(ws, q.bytes);
     if (meet(a, b) && !(in->base == out->base && in->F == out->F && in_slot == out_slot)) return CCV3D_ERR_ALIAS;
@@ -235,8 +262,9 @@ ccv3d_status ccv3d_group_norm_ring(const ccv3d_ring* in, int32_t in_slot, const 
     const int64_t frame = P * C;
     p.xv = {in->F * frame, frame, in->KB, P * in->KB, in->F, in_slot};
     p.yv = {out->F * frame, frame, in->KB, P * in->KB, out->F, out_slot};
-    p.T = T; p.samples = (int)S; p.pixels = (int)P; p.C = C; p.groups = groups; p.per = C / groups; p.KB = in->KB;
+    p.T = T; p.samples = (int)S; p.pixels = (int)P; p.C = C; p.groups = groups; p.per = C / groups; p.block_shift = in->KB == 64 ? 6 : 5;
     p.columns = q.columns; p.lanes = q.lanes; p.eps = eps; p.act = activation;
+    p.vec_affine = affine_vectors(p);
     return run_group_norm(p, q, CCV3D_BF16, ws, (cudaStream_t)stream);
 }
 

@@ -1,6 +1,4 @@
 // C entry points of the products: argument checks, cutting into tiles, launches.
-#include <type_traits>
-
 #include "ccv3d_tokens_linear.cuh"
 #include "ccv3d_tokens_host.cuh"
 
@@ -8,6 +6,7 @@ using namespace ccv3d;
 
 namespace {
 
+static const double LINEAR_CUT = getenv("LCUT") ? atof(getenv("LCUT")) : 4.0;
 // Tokens of a tile, and how its tiles fall to the pairs of SMs.
 struct LinearPlan {
     Device dev;
@@ -47,12 +46,12 @@ ccv3d_status plan_linear(const ccv3d_linear_desc* d, LinearPlan* q) {
     const int64_t tiles = q->n_tiles * q->t_tiles;
     if (tiles > 0x3FFFFFFF) return CCV3D_ERR_UNSUPPORTED;
     // The last turn: `left` tiles for all pairs.  Cutting them along K saves (1 - left / pairs) of a tile's time and costs a launch and the sums'
-    // way through memory, some 3 us.  A K block takes about 0.15 us (F32: six products of half its length).
+    // way through memory, some 4 us.  A K block takes about 0.28 us (F32: six products of half its length), half of that for 128 tokens.
     const int left = (int)(tiles % q->pairs);
-    const double tile_us = q->kblocks * (f32 ? 0.45 : 0.15) * (d->gated || q->BT == 256 ? 1.0 : 0.7);
+    const double tile_us = q->kblocks * (f32 ? 0.84 : 0.28) * (d->gated || q->BT == 256 ? 1.0 : 0.5);
     q->whole = (int)tiles;
     q->tail = q->sharers = 0;
-    if (left && tile_us * (q->pairs - left) / q->pairs > 3.0) {
+    if (left && tile_us * (q->pairs - left) / q->pairs > LINEAR_CUT) {
         const int64_t shares = (int64_t)left * q->kblocks / 4;         // of four K blocks at least
         q->sharers = (int)(shares < q->pairs ? shares : q->pairs);
         if (q->sharers > left) {
@@ -71,15 +70,14 @@ ccv3d_status plan_linear(const ccv3d_linear_desc* d, LinearPlan* q) {
     return CCV3D_OK;
 }
 
-// A BF16 matrix of `rows` rows of k elements, read in boxes of a stage's row length and box_rows rows.
-ccv3d_status encode_rows(CUtensorMap* tm, const void* at, int64_t rows, int64_t k, int64_t stride, int row_bytes, int box_rows) {
+// A matrix of `rows` rows of k elements of `size` bytes, in boxes of box_k elements of box_rows rows.
+ccv3d_status encode_rows(CUtensorMap* tm, const void* at, int size, int64_t rows, int64_t k, int64_t stride, int box_k, int box_rows, CUtensorMapSwizzle swizzle) {
     const EncodeTiledFn fn = encode_tiled();
     if (!fn) return CCV3D_ERR_CUDA;
-    const cuuint64_t dims[2] = {(cuuint64_t)k, (cuuint64_t)rows}, strides[1] = {(cuuint64_t)stride * 2};
-    const cuuint32_t box[2] = {(cuuint32_t)row_bytes / 2, (cuuint32_t)box_rows}, es[2] = {1, 1};
-    const CUresult r = fn(tm, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, const_cast<void*>(at), dims, strides, box, es, CU_TENSOR_MAP_INTERLEAVE_NONE,
-                          row_bytes == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-                          CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    const cuuint64_t dims[2] = {(cuuint64_t)k, (cuuint64_t)rows}, strides[1] = {(cuuint64_t)(stride * size)};
+    const cuuint32_t box[2] = {(cuuint32_t)box_k, (cuuint32_t)box_rows}, es[2] = {1, 1};
+    const CUresult r = fn(tm, size == 2 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 2, const_cast<void*>(at), dims, strides, box, es,
+                          CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
     return r == CUDA_SUCCESS ? CCV3D_OK : CCV3D_ERR_CUDA;
 }
 
@@ -88,9 +86,11 @@ ccv3d_status launch_linear_as(LinearParams& p, const LinearPlan& q, const void* 
                               int64_t w_stride, int k, cudaStream_t st) {
     static std::atomic<uint64_t> done{0};
     if (!allow_smem(linear_tile_kernel<S, TO>, S::SMEM, q.dev.index, done)) { cudaGetLastError(); return CCV3D_ERR_CUDA; }
-    CUtensorMap tw, tx;
-    ccv3d_status s = encode_rows(&tw, w, w_rows, k, w_stride, S::ROWB, 128);
-    if (s == CCV3D_OK) s = encode_rows(&tx, x, x_rows, k, x_stride, S::ROWB, S::BT / 2);
+    constexpr CUtensorMapSwizzle swizzle = S::ROWB == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B;
+    CUtensorMap tw, tx, to = {};
+    ccv3d_status s = encode_rows(&tw, w, 2, w_rows, k, w_stride, S::KB, 128, swizzle);
+    if (s == CCV3D_OK) s = encode_rows(&tx, x, 2, x_rows, k, x_stride, S::KB, S::BT / 2, swizzle);
+    if (s == CCV3D_OK && p.boxes) s = encode_rows(&to, p.out, sizeof(TO), p.rows, p.n_out, p.out_stride, 32, S::CH, CU_TENSOR_MAP_SWIZZLE_NONE);
     if (s != CCV3D_OK) return s;
     const int used = p.tail ? p.pairs : (p.whole < p.pairs ? p.whole : p.pairs);
     cudaLaunchAttribute at[1];
@@ -103,7 +103,7 @@ ccv3d_status launch_linear_as(LinearParams& p, const LinearPlan& q, const void* 
     cfg.stream = st;
     cfg.attrs = at;
     cfg.numAttrs = S::PARTS == 3 ? 1 : 0;            // behind the kernels that split the operands
-    if (cudaLaunchKernelEx(&cfg, linear_tile_kernel<S, TO>, tw, tx, p) != cudaSuccess) { cudaGetLastError(); return CCV3D_ERR_CUDA; }
+    if (cudaLaunchKernelEx(&cfg, linear_tile_kernel<S, TO>, tw, tx, to, p) != cudaSuccess) { cudaGetLastError(); return CCV3D_ERR_CUDA; }
     if (!p.tail) return CCV3D_OK;
     cfg.gridDim = dim3(p.tail, S::BT / LINEAR_JOIN_TOKENS);
     cfg.blockDim = dim3(256);
@@ -194,6 +194,8 @@ ccv3d_status ccv3d_linear(const ccv3d_linear_desc* d, const void* x, const void*
     p.sharers = q.sharers;
     p.pairs = q.pairs;
     p.part = (float*)((char*)ws + q.part_at);
+    p.boxes = !misaligned(out, 16) && (M == 1 ? (N * eo) % 16 == 0 : d->out_stride * eo % 16 == 0);
+    if (M == 1) p.out_stride = N;
     p.status = status;
     p.wait_clk = q.dev.wait_clk;
     if (d->dtype == CCV3D_F32) {

@@ -36,7 +36,8 @@ struct LinearParams {
     int whole;                   // tiles 0 .. whole - 1 go round the pairs
     int tail, sharers;           // the next `tail` tiles are cut into `sharers` equal runs of K blocks
     int x_plane, w_plane;        // F32: rows between the three parts of an operand
-    int pairs, stages;
+    int pairs;
+    int boxes;                   // outputs go out as boxes (their rows are on 16 bytes)
     float* part;                 // [2 * sharers][columns][256 features]
     uint32_t* status;
     long long wait_clk;
@@ -76,15 +77,17 @@ template <int BT_, bool GATED_, int PARTS_, bool F32_OUT> struct LinearShape {
     static constexpr int COLS = SETS * BT;                                   // of an accumulator
     static constexpr int ROWB = PARTS == 3 ? 64 : 128, KB = ROWB / 2;        // bytes and elements of a row of a stage
     static constexpr uint32_t A_TILE = 128 * ROWB, B_TILE = BT / 2 * ROWB, A_BYTES = PARTS * SETS * A_TILE, STAGE = A_BYTES + PARTS * B_TILE;
-    static constexpr int STAGES = (int)(206000 / STAGE) < LINEAR_MAX_STAGES ? (int)(206000 / STAGE) : LINEAR_MAX_STAGES;
     static constexpr int EPI_WARPS = FOLD && COLS == 256 ? 16 : 8, PARTS_OF_COLS = EPI_WARPS / 4, CW = BT / PARTS_OF_COLS;   // CW: tokens of a warp
     static constexpr int LD = CW < 16 ? CW : 16, CH = FOLD || CW < 32 ? LD : 32;   // columns read at a time onto rounded sums; finished at a time
     static constexpr int THREADS = 128 + 32 * EPI_WARPS;
     static constexpr uint32_t TMEM = 2 * COLS < 32 ? 32 : 2 * COLS;
-    // K blocks between hand-overs of a sum that is kept with rounding: 256 terms of BF16, 64 of F32 (with their remainders)
-    static constexpr int HAND = FOLD ? (PARTS == 3 ? 2 : 4) : 1 << 30;
-    static constexpr uint32_t SMEM = STAGES * STAGE + 1024;
-    static_assert(STAGES >= 2 && SMEM <= 220000 && (CW == 8 || CW % 32 == 0) && (TMEM & (TMEM - 1)) == 0, "");
+    // K blocks between hand-overs of a sum that is kept with rounding: 1024 terms of BF16, 128 of F32 (with their remainders)
+    static constexpr int HAND = FOLD ? (PARTS == 3 ? 4 : 16) : 1 << 30;
+    // outputs on their way: two boxes of 32 features and CH tokens for each warp
+    static constexpr uint32_t BOX = 32 * CH * (F32_OUT ? 4 : 2), BOXES = 2 * EPI_WARPS * BOX;
+    static constexpr int FIT = (int)((230400 - 1024 - BOXES) / STAGE), STAGES = FIT < LINEAR_MAX_STAGES ? FIT : LINEAR_MAX_STAGES;
+    static constexpr uint32_t SMEM = STAGES * STAGE + BOXES + 1024;
+    static_assert(STAGES >= 2 && SMEM <= 230400 && BOX % 128 == 0 && (CW == 8 || CW % 32 == 0) && (TMEM & (TMEM - 1)) == 0, "");
 };
 
 struct LinearShared {
@@ -130,40 +133,52 @@ __device__ __forceinline__ float bias_at(const LinearParams& p, int i) {
     return p.bias_f32 ? __ldg((const float*)p.bias + i) : __bfloat162float(((const __nv_bfloat16*)p.bias)[i]);
 }
 
-// The epilogue of N tokens t0 .. of one feature: g (and u) hold the sums, bg and bu the biases.
+__device__ __forceinline__ void tma_store_2d(const CUtensorMap* tm, uint32_t src, int c0, int c1) {
+    asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.tile.bulk_group [%0, {%2, %3}], [%1];" ::"l"(tm), "r"(src), "r"(c0), "r"(c1) : "memory");
+}
+
+// The epilogue of N tokens t0 .. of one feature: g (and u) hold the sums, bg and bu the biases; the results are in g.
 template <typename TO, bool GATED, int N>
-__device__ __forceinline__ void linear_finish(const LinearParams& p, int n, int t0, float* g, const float* u, float bg, float bu) {
-    constexpr bool EXACT = sizeof(TO) == 4;
+__device__ __forceinline__ void linear_epilogue(const LinearParams& p, int n, int t0, float (&g)[N], const float (&u)[N], float bg, float bu) {
     const int live = n < p.n_out ? min(N, p.rows - t0) : 0;
-    if (live <= 0) return;
     float r[N];
     if (p.res) {
         const TO* at = (const TO*)p.res + (int64_t)t0 * p.res_stride + n;
 #pragma unroll
-        for (int j = 0; j < N; ++j) r[j] = j < live ? load1(at + j * p.res_stride) : 0.f;
-    }
-    auto apply = [&](auto kind) {
-#pragma unroll
         for (int j = 0; j < N; ++j) {
-            g[j] = activate<EXACT>(g[j] + bg, decltype(kind)::value);
-            if (GATED) g[j] *= u[j] + bu;
+            r[j] = j < live ? load1(at) : 0.f;
+            at += p.res_stride;
         }
-    };
-    switch (p.act) {
-        case CCV3D_ACT_SILU: apply(std::integral_constant<int, CCV3D_ACT_SILU>()); break;
-        case CCV3D_ACT_GELU: apply(std::integral_constant<int, CCV3D_ACT_GELU>()); break;
-        case CCV3D_ACT_GELU_TANH: apply(std::integral_constant<int, CCV3D_ACT_GELU_TANH>()); break;
-        default: apply(std::integral_constant<int, CCV3D_ACT_NONE>());
     }
+    with_activation(p.act, [&](auto kind) {
+#pragma unroll
+        for (int j = 0; j < N; ++j) g[j] += bg;
+        activate_all<sizeof(TO) == 4, decltype(kind)::value>(g);
+        if (GATED) {
+#pragma unroll
+            for (int j = 0; j < N; ++j) g[j] *= u[j] + bu;
+        }
+    });
+    if (p.res) {
+#pragma unroll
+        for (int j = 0; j < N; ++j) g[j] += r[j];
+    }
+}
+template <typename TO, int N>
+__device__ __forceinline__ void linear_put(const LinearParams& p, int n, int t0, const float (&g)[N]) {
+    const int live = n < p.n_out ? min(N, p.rows - t0) : 0;
     TO* at = (TO*)p.out + (int64_t)t0 * p.out_stride + n;
 #pragma unroll
-    for (int j = 0; j < N; ++j)
-        if (j < live) store1(at + j * p.out_stride, p.res ? r[j] + g[j] : g[j]);
+    for (int j = 0; j < N; ++j) {
+        if (j < live) store1(at, g[j]);
+        at += p.out_stride;
+    }
 }
 
 template <typename S, typename TO>
 __global__ void __launch_bounds__(S::THREADS, 1) __cluster_dims__(2, 1, 1)
-linear_tile_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ LinearParams p) {
+linear_tile_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ CUtensorMap tm_o,
+                   const __grid_constant__ LinearParams p) {
     extern __shared__ uint8_t linear_smem[];
     __shared__ LinearShared shared;
     LinearShared* sh = &shared;
@@ -260,8 +275,9 @@ linear_tile_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_consta
         // ------------------------------------------------------------------------------------------ epilogue
         const int q = warp & 3, half = (warp - 4) >> 2;                 // lanes 32 q .., part of the columns
         const uint32_t mine = tmem + ((uint32_t)q << 21) + half * S::CW;
+        const uint32_t box = base + S::STAGES * S::STAGE + (warp - 4) * 2 * S::BOX;
         int acc = 0;
-        uint32_t ph = 0;
+        uint32_t ph = 0, turn = 0;
         while (ok && walk.get(w)) {
             const int nt = w.tile % p.n_tiles, f = (int)rank * 128 + q * 32 + lane, n = nt * 256 + f, t0 = w.tile / p.n_tiles * S::BT + half * S::CW;
             float bg = 0.f, bu = 0.f;
@@ -269,17 +285,46 @@ linear_tile_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_consta
                 bg = bias_at(p, n);
                 if (S::GATED) bu = bias_at(p, p.n_out + n);
             }
+            // the residual's rows come to L2 while the sums are made
+            if (p.res && w.slot < 0 && n - lane < p.n_out)
+                for (int j = lane; j < min(S::CW, p.rows - t0); j += 32)
+                    asm volatile("prefetch.global.L2 [%0];" ::"l"((const TO*)p.res + (int64_t)(t0 + j) * p.res_stride + (n - lane)));
             // sums of CH tokens from column c of the warp's on: finished, or put down for the join
-            auto leave = [&](int c, float* g, float* u) {
-                if (w.slot < 0) {
-                    linear_finish<TO, S::GATED, S::CH>(p, n, t0 + c, g, u, bg, bu);
+            auto leave = [&](int c, float (&g)[S::CH], float (&u)[S::CH]) {
+                if (w.slot >= 0) {
+                    float* at = p.part + ((int64_t)w.slot * S::COLS + half * S::CW + c) * 256 + f;
+#pragma unroll
+                    for (int j = 0; j < S::CH; ++j) {
+                        at[j * 256] = g[j];
+                        if (S::GATED) at[(S::BT + j) * 256] = u[j];
+                    }
                     return;
                 }
-                float* at = p.part + ((int64_t)w.slot * S::COLS + half * S::CW + c) * 256 + f;
+                linear_epilogue<TO, S::GATED, S::CH>(p, n, t0 + c, g, u, bg, bu);
+                if (!p.boxes) {
+                    linear_put<TO, S::CH>(p, n, t0 + c, g);
+                    return;
+                }
+                const uint32_t at = box + turn * S::BOX;
+                turn ^= 1;
+                if (lane == 0) bulk_wait_read<1>();              // the box before the last has left its place
+                __syncwarp();
 #pragma unroll
-                for (int j = 0; j < S::CH; ++j) {
-                    at[j * 256] = g[j];
-                    if (S::GATED) at[(S::BT + j) * 256] = u[j];
+                for (int j = 0; j < S::CH; j += 2) {
+                    if constexpr (sizeof(TO) == 4) {
+                        asm volatile("st.shared.f32 [%0], %1;" ::"r"(at + (j * 32 + lane) * 4), "f"(g[j]) : "memory");
+                        asm volatile("st.shared.f32 [%0], %1;" ::"r"(at + (j * 32 + 32 + lane) * 4), "f"(g[j + 1]) : "memory");
+                    } else {
+                        const uint32_t two = pack_bf16(g[j], g[j + 1]);
+                        asm volatile("st.shared.u16 [%0], %1;" ::"r"(at + (j * 32 + lane) * 2), "h"((unsigned short)two) : "memory");
+                        asm volatile("st.shared.u16 [%0], %1;" ::"r"(at + (j * 32 + 32 + lane) * 2), "h"((unsigned short)(two >> 16)) : "memory");
+                    }
+                }
+                fence_async_smem();
+                __syncwarp();
+                if (lane == 0) {
+                    if (n < p.n_out && t0 + c < p.rows) tma_store_2d(&tm_o, at, n, t0 + c);
+                    bulk_commit();
                 }
             };
             if constexpr (S::FOLD) {
@@ -309,7 +354,12 @@ linear_tile_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_consta
                 }
                 if (ok) {
 #pragma unroll
-                    for (int c = 0; c < S::CW; c += S::CH) leave(c, &sum[0][c], &sum[S::SETS - 1][c]);
+                    for (int c = 0; c < S::CW; c += S::CH) {
+                        float g[S::CH], u[S::CH];
+#pragma unroll
+                        for (int j = 0; j < S::CH; ++j) { g[j] = sum[0][c + j]; u[j] = sum[S::SETS - 1][c + j]; }
+                        leave(c, g, u);
+                    }
                 }
             } else {
                 if (!(ok = linear_warp_wait(&sh->acc_full[acc], ph, sh, p))) break;
@@ -334,6 +384,7 @@ linear_tile_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_consta
                 if (acc == 0) ph ^= 1;
             }
         }
+        if (lane == 0) bulk_wait_read<0>();          // (the boxes' places are this block's)
     }
     if (!ok) {                                       // loads and MMAs still in flight
         const long long t = clock64();
@@ -375,7 +426,8 @@ __global__ void __launch_bounds__(256) linear_join_kernel(const __grid_constant_
         bg = bias_at(p, n);
         if (GATED) bu = bias_at(p, p.n_out + n);
     }
-    linear_finish<TO, GATED, LINEAR_JOIN_TOKENS>(p, n, t0, g, u, bg, bu);
+    linear_epilogue<TO, GATED, LINEAR_JOIN_TOKENS>(p, n, t0, g, u, bg, bu);
+    linear_put<TO, LINEAR_JOIN_TOKENS>(p, n, t0, g);
 }
 
 // F32 rows as three BF16 numbers each, in three planes [rows][pitch]: rounded to 8 bits, what is left to 8 more, and the rest (8 bits: exact).
