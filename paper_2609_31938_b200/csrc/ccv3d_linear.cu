@@ -6,7 +6,6 @@ using namespace ccv3d;
 
 namespace {
 
-static const double LINEAR_CUT = getenv("LCUT") ? atof(getenv("LCUT")) : 4.0;
 // Tokens of a tile, and how its tiles fall to the pairs of SMs.
 struct LinearPlan {
     Device dev;
@@ -24,11 +23,11 @@ ccv3d_status check_linear(const ccv3d_linear_desc* d) {
     return CCV3D_OK;
 }
 
-// Few rows take narrow tiles: the weights' bytes bound them, and every tile reads its weights whole.
-int tokens_of_tile(int rows, bool gated) {
-    if (rows <= 16) return 16;
-    if (rows <= 64) return 64;
-    return rows <= 128 || gated ? 128 : 256;
+// Microseconds of a K block of a tile with every pair of SMs at work (measured with one tile for each: the way from L2, at 12 to 14 TB/s,
+// bounds narrow tiles, so that one of 128 tokens takes as long as one of 16), and of a tile's end.
+double block_us(int BT, bool gated, bool f32) {
+    if (f32) return (gated ? 2.0 : 1.0) * (BT == 16 ? 0.60 : BT == 64 ? 0.65 : BT == 128 ? 0.75 : 1.15);
+    return gated ? (BT == 128 ? 0.55 : 0.47) : BT == 256 ? 0.35 : 0.26;
 }
 
 ccv3d_status plan_linear(const ccv3d_linear_desc* d, LinearPlan* q) {
@@ -37,30 +36,44 @@ ccv3d_status plan_linear(const ccv3d_linear_desc* d, LinearPlan* q) {
     if ((s = current_device(&q->dev)) != CCV3D_OK) return s;
     const bool f32 = d->dtype == CCV3D_F32;
     q->parts = f32 ? 3 : 1;
-    q->BT = tokens_of_tile(d->rows, d->gated);
     const int kb = f32 ? 32 : 64;
     q->kblocks = (d->k + kb - 1) / kb;
     q->n_tiles = (d->n_out + 255) / 256;
-    q->t_tiles = ((int64_t)d->rows + q->BT - 1) / q->BT;
     q->pairs = q->dev.sm_count / 2;
-    const int64_t tiles = q->n_tiles * q->t_tiles;
-    if (tiles > 0x3FFFFFFF) return CCV3D_ERR_UNSUPPORTED;
-    // The last turn: `left` tiles for all pairs.  Cutting them along K saves (1 - left / pairs) of a tile's time and costs a launch and the sums'
-    // way through memory, some 4 us.  A K block takes about 0.28 us (F32: six products of half its length), half of that for 128 tokens.
-    const int left = (int)(tiles % q->pairs);
-    const double tile_us = q->kblocks * (f32 ? 0.84 : 0.28) * (d->gated || q->BT == 256 ? 1.0 : 0.5);
-    q->whole = (int)tiles;
-    q->tail = q->sharers = 0;
-    if (left && tile_us * (q->pairs - left) / q->pairs > LINEAR_CUT) {
+    // Tokens of a tile, and whether the tiles of the last, unfilled turn are cut along K: by the time that the call would take.  It is not under
+    // that of the weights' bytes; cutting costs a launch, and the sums' way through memory.
+    const double bytes_us = (double)d->n_out * (1 + d->gated) * d->k * esize(d->dtype) / 5.6e6;
+    double best = 1e30;
+    for (const int BT : {16, 64, 128, 256}) {
+        if (BT == 256 && d->gated) continue;
+        const int64_t t_tiles = ((int64_t)d->rows + BT - 1) / BT, tiles = q->n_tiles * t_tiles, turns = tiles / q->pairs;
+        if (tiles > 0x3FFFFFFF) continue;
+        const double tile_us = q->kblocks * block_us(BT, d->gated, f32), end_us = BT * (1 + d->gated) / 85.0;
+        const int left = (int)(tiles % q->pairs);
+        const auto longer = [](double a, double b) { return a > b ? a : b; };
+        double us = longer((turns + (left > 0)) * tile_us, bytes_us) + end_us;
+        if (us < best) {
+            best = us;
+            q->BT = BT;
+            q->t_tiles = t_tiles;
+            q->whole = (int)tiles;
+            q->tail = q->sharers = 0;
+        }
         const int64_t shares = (int64_t)left * q->kblocks / 4;         // of four K blocks at least
-        q->sharers = (int)(shares < q->pairs ? shares : q->pairs);
-        if (q->sharers > left) {
+        const int sharers = (int)(shares < q->pairs ? shares : q->pairs);
+        if (left == 0 || sharers <= left) continue;
+        const double sums = 2.0 * (sharers + left) * BT * (1 + d->gated) * 1024;
+        us = longer(turns * tile_us + left * tile_us / sharers, bytes_us) + end_us + 5.0 + sums / 4e6;
+        if (us < best) {
+            best = us;
+            q->BT = BT;
+            q->t_tiles = t_tiles;
             q->whole = (int)(tiles - left);
             q->tail = left;
-        } else {
-            q->sharers = 0;
+            q->sharers = sharers;
         }
     }
+    if (best == 1e30) return CCV3D_ERR_UNSUPPORTED;
     const auto up = [](int64_t n) { return (n + 255) / 256 * 256; };
     q->pitch = (d->k + 7LL) / 8 * 8;
     q->x_at = 0;
@@ -125,11 +138,6 @@ ccv3d_status launch_linear(bool gated, int BT, A&&... a) {
     if (BT == 64) return launch_linear_as<LinearShape<64, false, PARTS, F>, TO>(a...);
     if (BT == 128) return launch_linear_as<LinearShape<128, false, PARTS, F>, TO>(a...);
     return launch_linear_as<LinearShape<256, false, PARTS, F>, TO>(a...);
-}
-
-void split(const float* x, int64_t stride, int rows, int k, void* to, int64_t pitch, cudaStream_t st) {
-    const int64_t blocks = (rows * (pitch / 4) + 255) / 256;
-    linear_split_kernel<<<(unsigned)(blocks < 148 * 8 ? blocks : 148 * 8), 256, 0, st>>>(x, stride, rows, k, (__nv_bfloat16*)to, (int)pitch);
 }
 
 }  // namespace
@@ -200,8 +208,9 @@ ccv3d_status ccv3d_linear(const ccv3d_linear_desc* d, const void* x, const void*
     p.wait_clk = q.dev.wait_clk;
     if (d->dtype == CCV3D_F32) {
         void *px = (char*)ws + q.x_at, *pw = (char*)ws + q.w_at;
-        split((const float*)w, wst, (int)NW, d->k, pw, q.pitch, st);
-        split((const float*)x, xs, d->rows, d->k, px, q.pitch, st);
+        const int64_t blocks = ((NW + M) * (q.pitch / 4) + 255) / 256;
+        linear_split_kernel<<<(unsigned)(blocks < 16 * q.dev.sm_count ? blocks : 16 * q.dev.sm_count), 256, 0, st>>>(
+            (const float*)w, wst, (int)NW, (__nv_bfloat16*)pw, (const float*)x, xs, d->rows, (__nv_bfloat16*)px, d->k, (int)q.pitch);
         if ((s = launched()) != CCV3D_OK) return s;
         p.x_plane = d->rows;
         p.w_plane = (int)NW;

@@ -430,17 +430,19 @@ __global__ void __launch_bounds__(256) linear_join_kernel(const __grid_constant_
     linear_put<TO, LINEAR_JOIN_TOKENS>(p, n, t0, g);
 }
 
-// F32 rows as three BF16 numbers each, in three planes [rows][pitch]: rounded to 8 bits, what is left to 8 more, and the rest (8 bits: exact).
-// A thread to four elements.
-__global__ void __launch_bounds__(256) linear_split_kernel(const float* x, int64_t stride, int rows, int k, __nv_bfloat16* to, int pitch) {
+// F32 rows of both operands as three BF16 numbers each, in three planes [rows][pitch]: rounded to 8 bits, what is left to 8 more, and the
+// rest (8 bits: exact).  A thread to four elements.
+__global__ void __launch_bounds__(256) linear_split_kernel(const float* w, int64_t w_stride, int w_rows, __nv_bfloat16* w_to, const float* x, int64_t x_stride,
+                                                           int x_rows, __nv_bfloat16* x_to, int k, int pitch) {
     asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
     const int quads = pitch / 4;
-    const int64_t all = (int64_t)rows * quads;
+    const int64_t w_all = (int64_t)w_rows * quads, all = w_all + (int64_t)x_rows * quads;
     for (int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; i < all; i += (int64_t)gridDim.x * blockDim.x) {
-        const int64_t r = i / quads;
-        const int c = (int)(i - r * quads) * 4;
+        const bool of_x = i >= w_all;
+        const int64_t j0 = of_x ? i - w_all : i, r = j0 / quads, plane = (int64_t)(of_x ? x_rows : w_rows) * pitch;
+        const int c = (int)(j0 - r * quads) * 4;
         float v[4] = {0.f, 0.f, 0.f, 0.f}, a[4], b[4], d[4];
-        const float* at = x + r * stride + c;
+        const float* at = of_x ? x + r * x_stride + c : w + r * w_stride + c;
         if (c + 4 <= k) load4(at, v);
         else
             for (int j = 0; c + j < k; ++j) v[j] = at[j];
@@ -452,8 +454,7 @@ __global__ void __launch_bounds__(256) linear_split_kernel(const float* x, int64
             b[j] = __bfloat162float(__float2bfloat16_rn(rest));
             d[j] = rest - b[j];
         }
-        __nv_bfloat16* o = to + r * pitch + c;
-        const int64_t plane = (int64_t)rows * pitch;
+        __nv_bfloat16* o = (of_x ? x_to : w_to) + r * pitch + c;
         store4(o, a);
         store4(o + plane, b);
         store4(o + 2 * plane, d);
