@@ -100,10 +100,11 @@ ccv3d_status launch_linear_as(LinearParams& p, const LinearPlan& q, const void* 
     static std::atomic<uint64_t> done{0};
     if (!allow_smem(linear_tile_kernel<S, TO>, S::SMEM, q.dev.index, done)) { cudaGetLastError(); return CCV3D_ERR_CUDA; }
     constexpr CUtensorMapSwizzle swizzle = S::ROWB == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B;
-    CUtensorMap tw, tx, to = {};
+    CUtensorMap tw, tx, to = {}, tr = {};
     ccv3d_status s = encode_rows(&tw, w, 2, w_rows, k, w_stride, S::KB, 128, swizzle);
     if (s == CCV3D_OK) s = encode_rows(&tx, x, 2, x_rows, k, x_stride, S::KB, S::BT / 2, swizzle);
     if (s == CCV3D_OK && p.boxes) s = encode_rows(&to, p.out, sizeof(TO), p.rows, p.n_out, p.out_stride, 32, S::CH, CU_TENSOR_MAP_SWIZZLE_NONE);
+    if (s == CCV3D_OK && p.res_boxes) s = encode_rows(&tr, p.res, sizeof(TO), p.rows, p.n_out, p.res_stride, 32, S::CH, CU_TENSOR_MAP_SWIZZLE_NONE);
     if (s != CCV3D_OK) return s;
     const int used = p.tail ? p.pairs : (p.whole < p.pairs ? p.whole : p.pairs);
     cudaLaunchAttribute at[1];
@@ -116,7 +117,7 @@ ccv3d_status launch_linear_as(LinearParams& p, const LinearPlan& q, const void* 
     cfg.stream = st;
     cfg.attrs = at;
     cfg.numAttrs = S::PARTS == 3 ? 1 : 0;            // behind the kernels that split the operands
-    if (cudaLaunchKernelEx(&cfg, linear_tile_kernel<S, TO>, tw, tx, to, p) != cudaSuccess) { cudaGetLastError(); return CCV3D_ERR_CUDA; }
+    if (cudaLaunchKernelEx(&cfg, linear_tile_kernel<S, TO>, tw, tx, to, tr, p) != cudaSuccess) { cudaGetLastError(); return CCV3D_ERR_CUDA; }
     if (!p.tail) return CCV3D_OK;
     cfg.gridDim = dim3(p.tail, S::BT / LINEAR_JOIN_TOKENS);
     cfg.blockDim = dim3(256);
@@ -203,7 +204,9 @@ ccv3d_status ccv3d_linear(const ccv3d_linear_desc* d, const void* x, const void*
     p.pairs = q.pairs;
     p.part = (float*)((char*)ws + q.part_at);
     p.boxes = !misaligned(out, 16) && (M == 1 ? (N * eo) % 16 == 0 : d->out_stride * eo % 16 == 0);
-    if (M == 1) p.out_stride = N;
+    if (M == 1) p.out_stride = p.res_stride = N;
+    // (rows on one another, a broadcast residual, have no map)
+    p.res_boxes = residual && !misaligned(residual, 16) && p.res_stride >= N && p.res_stride * eo % 16 == 0;
     p.status = status;
     p.wait_clk = q.dev.wait_clk;
     if (d->dtype == CCV3D_F32) {

@@ -37,7 +37,7 @@ struct LinearParams {
     int tail, sharers;           // the next `tail` tiles are cut into `sharers` equal runs of K blocks
     int x_plane, w_plane;        // F32: rows between the three parts of an operand
     int pairs;
-    int boxes;                   // outputs go out as boxes (their rows are on 16 bytes)
+    int boxes, res_boxes;        // outputs go out, residuals come in as boxes (their rows are on 16 bytes)
     float* part;                 // [2 * sharers][columns][256 features]
     uint32_t* status;
     long long wait_clk;
@@ -91,7 +91,7 @@ template <int BT_, bool GATED_, int PARTS_, bool F32_OUT> struct LinearShape {
 };
 
 struct LinearShared {
-    uint64_t full[LINEAR_MAX_STAGES], empty[LINEAR_MAX_STAGES], acc_full[2], acc_empty[2];
+    uint64_t full[LINEAR_MAX_STAGES], empty[LINEAR_MAX_STAGES], acc_full[2], acc_empty[2], res_full[16][2];
     uint32_t tmem;
     int abort_flag;
 };
@@ -137,12 +137,29 @@ __device__ __forceinline__ void tma_store_2d(const CUtensorMap* tm, uint32_t src
     asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.tile.bulk_group [%0, {%2, %3}], [%1];" ::"l"(tm), "r"(src), "r"(c0), "r"(c1) : "memory");
 }
 
-// The epilogue of N tokens t0 .. of one feature: g (and u) hold the sums, bg and bu the biases; the results are in g.
+__device__ __forceinline__ void tma_load_2d(uint32_t dst, const CUtensorMap* tm, uint32_t bar, int c0, int c1) {
+    asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(dst), "l"(tm), "r"(c0),
+                 "r"(c1), "r"(bar)
+                 : "memory");
+}
+
+// The epilogue of N tokens t0 .. of one feature: g (and u) hold the sums, bg and bu the biases; the results are in g.  `box`: where the
+// residual lies in shared memory, 0: where p.res says.
 template <typename TO, bool GATED, int N>
-__device__ __forceinline__ void linear_epilogue(const LinearParams& p, int n, int t0, float (&g)[N], const float (&u)[N], float bg, float bu) {
+__device__ __forceinline__ void linear_epilogue(const LinearParams& p, int n, int t0, float (&g)[N], const float (&u)[N], float bg, float bu, uint32_t box = 0) {
     const int live = n < p.n_out ? min(N, p.rows - t0) : 0;
     float r[N];
-    if (p.res) {
+    if (box) {
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+            if constexpr (sizeof(TO) == 4) asm volatile("ld.shared.f32 %0, [%1];" : "=f"(r[j]) : "r"(box + (j * 32 + (threadIdx.x & 31)) * 4) : "memory");
+            else {
+                unsigned short h;
+                asm volatile("ld.shared.u16 %0, [%1];" : "=h"(h) : "r"(box + (j * 32 + (threadIdx.x & 31)) * 2) : "memory");
+                r[j] = __uint_as_float((uint32_t)h << 16);
+            }
+        }
+    } else if (p.res) {
         const TO* at = (const TO*)p.res + (int64_t)t0 * p.res_stride + n;
 #pragma unroll
         for (int j = 0; j < N; ++j) {
@@ -178,7 +195,7 @@ __device__ __forceinline__ void linear_put(const LinearParams& p, int n, int t0,
 template <typename S, typename TO>
 __global__ void __launch_bounds__(S::THREADS, 1) __cluster_dims__(2, 1, 1)
 linear_tile_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_constant__ CUtensorMap tm_x, const __grid_constant__ CUtensorMap tm_o,
-                   const __grid_constant__ LinearParams p) {
+                   const __grid_constant__ CUtensorMap tm_r, const __grid_constant__ LinearParams p) {
     extern __shared__ uint8_t linear_smem[];
     __shared__ LinearShared shared;
     LinearShared* sh = &shared;
@@ -189,6 +206,7 @@ linear_tile_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_consta
     if (threadIdx.x == 0) {
         for (int i = 0; i < S::STAGES; ++i) { mbar_init(smem_u32(&sh->full[i]), 1); mbar_init(smem_u32(&sh->empty[i]), 1); }
         for (int i = 0; i < 2; ++i) { mbar_init(smem_u32(&sh->acc_full[i]), 1); mbar_init(smem_u32(&sh->acc_empty[i]), 2 * S::EPI_WARPS); }
+        for (int i = 0; i < S::EPI_WARPS; ++i) { mbar_init(smem_u32(&sh->res_full[i][0]), 1); mbar_init(smem_u32(&sh->res_full[i][1]), 1); }
         sh->abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
@@ -277,7 +295,7 @@ linear_tile_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_consta
         const uint32_t mine = tmem + ((uint32_t)q << 21) + half * S::CW;
         const uint32_t box = base + S::STAGES * S::STAGE + (warp - 4) * 2 * S::BOX;
         int acc = 0;
-        uint32_t ph = 0, turn = 0;
+        uint32_t ph = 0, turn = 0, res_ph = 0;
         while (ok && walk.get(w)) {
             const int nt = w.tile % p.n_tiles, f = (int)rank * 128 + q * 32 + lane, n = nt * 256 + f, t0 = w.tile / p.n_tiles * S::BT + half * S::CW;
             float bg = 0.f, bu = 0.f;
@@ -285,10 +303,24 @@ linear_tile_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_consta
                 bg = bias_at(p, n);
                 if (S::GATED) bu = bias_at(p, p.n_out + n);
             }
-            // the residual's rows come to L2 while the sums are made
-            if (p.res && w.slot < 0 && n - lane < p.n_out)
-                for (int j = lane; j < min(S::CW, p.rows - t0); j += 32)
-                    asm volatile("prefetch.global.L2 [%0];" ::"l"((const TO*)p.res + (int64_t)(t0 + j) * p.res_stride + (n - lane)));
+            // the residual's first boxes come in while the sums are made, the rest of it comes to L2
+            auto ask = [&](int c, uint32_t b) {
+                if (lane == 0) {
+                    const uint32_t bar = smem_u32(&sh->res_full[warp - 4][b]);
+                    mbar_expect_tx(bar, S::BOX);
+                    tma_load_2d(box + b * S::BOX, &tm_r, bar, n, t0 + c);
+                }
+            };
+            if (p.res && w.slot < 0) {
+                if (p.res_boxes) {
+                    if (lane == 0) bulk_wait_read<0>();
+                    ask(0, turn);
+                    if (S::CW > S::CH) ask(S::CH, turn ^ 1);
+                }
+                if (n - lane < p.n_out && (S::CW > 2 * S::CH || !p.res_boxes))
+                    for (int j = lane; j < min(S::CW, p.rows - t0); j += 32)
+                        asm volatile("prefetch.global.L2 [%0];" ::"l"((const TO*)p.res + (int64_t)(t0 + j) * p.res_stride + (n - lane)));
+            }
             // sums of CH tokens from column c of the warp's on: finished, or put down for the join
             auto leave = [&](int c, float (&g)[S::CH], float (&u)[S::CH]) {
                 if (w.slot >= 0) {
@@ -300,15 +332,27 @@ linear_tile_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_consta
                     }
                     return;
                 }
-                linear_epilogue<TO, S::GATED, S::CH>(p, n, t0 + c, g, u, bg, bu);
+                const uint32_t b = turn, at = box + b * S::BOX;
+                const bool by_box = p.res && p.res_boxes;
+                if (by_box) {
+                    ok = linear_warp_wait(&sh->res_full[warp - 4][b], res_ph >> b & 1u, sh, p) && ok;
+                    res_ph ^= 1u << b;
+                }
+                linear_epilogue<TO, S::GATED, S::CH>(p, n, t0 + c, g, u, bg, bu, by_box ? at : 0u);
+                if (p.boxes || by_box) turn ^= 1;
                 if (!p.boxes) {
                     linear_put<TO, S::CH>(p, n, t0 + c, g);
+                    if (by_box && c + 2 * S::CH < S::CW) {
+                        fence_async_smem();                      // (read before it is written again)
+                        __syncwarp();
+                        ask(c + 2 * S::CH, b);
+                    }
                     return;
                 }
-                const uint32_t at = box + turn * S::BOX;
-                turn ^= 1;
-                if (lane == 0) bulk_wait_read<1>();              // the box before the last has left its place
-                __syncwarp();
+                if (!by_box) {
+                    if (lane == 0) bulk_wait_read<1>();          // the box before the last has left its place
+                    __syncwarp();
+                }
 #pragma unroll
                 for (int j = 0; j < S::CH; j += 2) {
                     if constexpr (sizeof(TO) == 4) {
@@ -325,6 +369,10 @@ linear_tile_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_consta
                 if (lane == 0) {
                     if (n < p.n_out && t0 + c < p.rows) tma_store_2d(&tm_o, at, n, t0 + c);
                     bulk_commit();
+                }
+                if (by_box && c + 2 * S::CH < S::CW) {           // this box's place takes the residual after next
+                    if (lane == 0) bulk_wait_read<0>();
+                    ask(c + 2 * S::CH, b);
                 }
             };
             if constexpr (S::FOLD) {
