@@ -18,7 +18,8 @@ SOURCES = {   # source -> the files its object depends on
                             "ccv3d_tokens_host.cuh", HEADER],
     "ccv3d_linear.cu": ["ccv3d_tokens_common.cuh", "ccv3d_tokens_activation.cuh", "ccv3d_tokens_linear.cuh", "ccv3d_tokens_host.cuh",
                         "ccv3d_tc_ptx.cuh", HEADER],
-    "ccv3d_decay.cu": ["ccv3d_tokens_common.cuh", "ccv3d_tokens_decay.cuh", "ccv3d_tokens_host.cuh", HEADER],
+    "ccv3d_decay.cu": ["ccv3d_tokens_common.cuh", "ccv3d_tokens_decay.cuh", "ccv3d_tokens_decay_tile.cuh", "ccv3d_tokens_host.cuh",
+                       "ccv3d_tc_ptx.cuh", HEADER],
 }
 
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17", "-Xcompiler", "-fPIC"]

@@ -1,5 +1,5 @@
 // C entry points of the attention with decaying states: argument checks, kernel choice, launches.
-#include "ccv3d_tokens_decay.cuh"
+#include "ccv3d_tokens_decay_tile.cuh"
 #include "ccv3d_tokens_host.cuh"
 
 using namespace ccv3d;
@@ -9,7 +9,7 @@ namespace {
 struct DecayPlan {
     Device dev;
     bool step;
-    int warps;                   // of a chunk block: 16 value columns each
+    int columns;                 // value columns of a chunk block
     int seg;                     // tokens of a segment, 0: not cut
     int64_t items, fade_at;
     uint64_t bytes;
@@ -32,13 +32,13 @@ ccv3d_status plan_decay(const ccv3d_decay_memory* m, const ccv3d_stream_batch* b
     const ccv3d_status s = current_device(&q->dev);
     if (s != CCV3D_OK) return s;
     q->step = b->max_new <= 8;
-    q->warps = m->value_dim % 128 == 0 ? 8 : 4;
+    q->columns = dtype == CCV3D_BF16 || m->value_dim % 128 == 0 ? 128 : 64;
     q->seg = 0;
     q->items = q->fade_at = 0;
     q->bytes = 0;
     if (q->step) return CCV3D_OK;
     // blocks of a chunk kernel for each item, and how many there should be
-    const int64_t wide = (int64_t)m->heads * (m->value_dim / (16 * q->warps)), want = 2 * q->dev.sm_count;
+    const int64_t wide = (int64_t)m->heads * ((m->value_dim + q->columns - 1) / q->columns), want = (getenv("DWANT") ? atoi(getenv("DWANT")) : 2) * q->dev.sm_count;
     const int64_t longest = b->max_new < b->tokens ? b->max_new : b->tokens;
     if (wide * b->batch >= want && longest <= 8 * ((int64_t)b->tokens / b->batch + 64)) return CCV3D_OK;
     const int64_t items = (want + wide - 1) / wide, chunks = (b->tokens + DECAY_CHUNK - 1) / DECAY_CHUNK;
@@ -52,24 +52,30 @@ ccv3d_status plan_decay(const ccv3d_decay_memory* m, const ccv3d_stream_batch* b
     return CCV3D_OK;
 }
 
-template <typename T, int DK, int NW, int MODE>
+// A pass over the chunks of sequences or items: BF16 on tcgen05, F32 by mma.sync, with eight or four warps to 128 or 64 value columns.
+template <typename T, int DK, int MODE>
 ccv3d_status launch_chunks(const DecayParams& p, const DecayPlan& q, int64_t items, cudaStream_t st) {
-    static std::atomic<uint64_t> done{0};
-    using S = DecayShape<T, DK, NW>;
-    if (!allow_smem(decay_chunk_kernel<T, DK, NW, MODE>, S::BYTES, q.dev.index, done)) { cudaGetLastError(); return CCV3D_ERR_CUDA; }
-    decay_chunk_kernel<T, DK, NW, MODE><<<dim3((unsigned)items, p.m.heads * (p.m.value_dim / S::DV)), S::THREADS, S::BYTES, st>>>(p);
-    return launched();
+    const dim3 grid((unsigned)items, p.m.heads * ((p.m.value_dim + q.columns - 1) / q.columns));
+    const auto launch = [&](auto* kernel, int threads, int bytes, std::atomic<uint64_t>& done) {
+        if (!allow_smem(kernel, bytes, q.dev.index, done)) { cudaGetLastError(); return CCV3D_ERR_CUDA; }
+        kernel<<<grid, threads, bytes, st>>>(p);
+        return launched();
+    };
+    static std::atomic<uint64_t> done[2];
+    if constexpr (sizeof(T) == 2) return launch(decay_tile_kernel<DK, MODE>, DECAY_TILE_THREADS, DecayTileShape<DK>::BYTES, done[0]);
+    else if (q.columns == 128) return launch(decay_chunk_kernel<T, DK, 8, MODE>, 256, DecayShape<T, DK, 8>::BYTES, done[0]);
+    else return launch(decay_chunk_kernel<T, DK, 4, MODE>, 128, DecayShape<T, DK, 4>::BYTES, done[1]);
 }
 
-template <typename T, int DK, int NW>
+template <typename T, int DK>
 ccv3d_status launch_prompt(const DecayParams& p, const DecayPlan& q, cudaStream_t st) {
-    if (!q.seg) return launch_chunks<T, DK, NW, DECAY_ALL>(p, q, p.bt.batch, st);
-    ccv3d_status s = launch_chunks<T, DK, NW, DECAY_STATES>(p, q, q.items, st);
+    if (!q.seg) return launch_chunks<T, DK, DECAY_ALL>(p, q, p.bt.batch, st);
+    ccv3d_status s = launch_chunks<T, DK, DECAY_STATES>(p, q, q.items, st);
     if (s != CCV3D_OK) return s;
     const int64_t size = (int64_t)DK * p.m.value_dim;
     decay_scan_kernel<<<dim3(p.bt.batch, (unsigned)((size + 1023) / 1024), p.m.heads), DECAY_SCAN_THREADS, 0, st>>>(p);
     if ((s = launched()) != CCV3D_OK) return s;
-    return launch_chunks<T, DK, NW, DECAY_OUTPUTS>(p, q, q.items, st);
+    return launch_chunks<T, DK, DECAY_OUTPUTS>(p, q, q.items, st);
 }
 
 template <typename T, int DK>
@@ -80,7 +86,7 @@ ccv3d_status launch_decay(const DecayParams& p, const DecayPlan& q, cudaStream_t
         decay_step_kernel<T, DK><<<(unsigned)blocks, DECAY_STEP_THREADS, 0, st>>>(p);
         return launched();
     }
-    return q.warps == 8 ? launch_prompt<T, DK, 8>(p, q, st) : launch_prompt<T, DK, 4>(p, q, st);
+    return launch_prompt<T, DK>(p, q, st);
 }
 
 }  // namespace
@@ -137,6 +143,7 @@ ccv3d_status ccv3d_decay_attend(const ccv3d_decay_memory* memory, const ccv3d_st
     p.group = H / qk_heads;
     p.scale = scale;
     p.status = status;
+    p.wait_clk = pl.dev.wait_clk;
     p.seg = pl.seg;
     p.items = (int)pl.items;
     p.part = (float*)ws;

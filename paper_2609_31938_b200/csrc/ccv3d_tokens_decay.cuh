@@ -35,6 +35,7 @@ struct DecayParams {
     float* part;                 // [item][head][key][value]: contributions of the segments, then the states they start from
     float* fade;                 // [item][head]: decay over a whole segment
     int items;                   // room in them
+    long long wait_clk;
 };
 
 struct DecaySeq { int first, n, slot; bool zero; };     // slot < 0: the state is not kept
@@ -187,9 +188,9 @@ struct DecayShared {
     float last;                  // exp(G_end)
 };
 
-// Item (sequence, segment) of a cut call; false: there is none of this number.  All threads; word: two ints in shared memory.
+// Item (sequence, segment) of a cut call; false: there is none of this number.  All threads; word: 34 ints in shared memory.
 __device__ __forceinline__ bool decay_item(const DecayParams& p, int item, int& b, int& seg, int* word) {
-    __shared__ int scan[32];
+    int* scan = word + 2;
     const int t = threadIdx.x, warps = blockDim.x >> 5;
     int before = 0;
     if (t == 0) word[0] = -1;
@@ -215,6 +216,7 @@ __device__ __forceinline__ bool decay_item(const DecayParams& p, int item, int& 
     }
     b = word[0];
     seg = word[1];
+    __syncthreads();
     return b >= 0;
 }
 
@@ -226,7 +228,7 @@ __global__ void __launch_bounds__(32 * NW, NW == 4 ? 2 : 1) decay_chunk_kernel(c
     constexpr int PI = S::PI, PM = S::PM, PV = S::PV, L = DECAY_CHUNK;
     extern __shared__ __align__(16) __nv_bfloat16 decay_smem[];
     __shared__ DecayShared<T, DK, NW> sh;
-    __shared__ int word[2];
+    __shared__ int word[34];
     const int t = threadIdx.x, warp = t >> 5, lane = t & 31, g = lane >> 2, tc = lane & 3;
     const int slices = p.m.value_dim / S::DV, slice = blockIdx.y % slices, h = blockIdx.y / slices;
     const int dv0 = slice * S::DV;
@@ -482,40 +484,55 @@ __global__ void __launch_bounds__(32 * NW, NW == 4 ? 2 : 1) decay_chunk_kernel(c
                         }
                     }
                 __syncthreads();                             // all scores are there
+                // ... faded, and the scores' part on top (F32: summed for itself)
+                float pv[S::F32 ? 4 : 1][2][4];
 #pragma unroll
                 for (int m = 0; m < 4; ++m) {
-                    if (16 * m >= live) break;
-                    float pv[2][4];
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) pv[i >> 2][i & 3] = 0.f;
-#pragma unroll
-                    for (int o = PM - 1; o >= 0; --o)        // part a of the scores, o - a of the values
-#pragma unroll
-                        for (int kt = 0; kt <= m; ++kt)
-#pragma unroll
-                            for (int a = o; a >= 0 && o - a < PI; --a) {
-                                uint32_t af[4], bf[4];
-                                ldsm(smem_at(sp + a * S::P + (16 * m + (lane & 15)) * S::PS + 16 * kt + (lane >> 4) * 8), af);
-                                ldsm_t(smem_at(sv + (o - a) * S::V + (16 * kt + (lane & 15)) * S::VS + 16 * warp + (lane >> 4) * 8), bf);
-                                mma_bf16(pv[0], af, bf[0], bf[1]);
-                                mma_bf16(pv[1], af, bf[2], bf[3]);
-                            }
                     const float e0 = sh.begin[16 * m + g], e1 = sh.begin[16 * m + g + 8];
+#pragma unroll
+                    for (int c = 0; c < 2; ++c)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            out[m][c][i] = fade(out[m][c][i], i < 2 ? e0 : e1);
+                            if (S::F32) pv[S::F32 ? m : 0][c][i] = 0.f;
+                        }
+                }
+#pragma unroll
+                for (int o = PM - 1; o >= 0; --o)            // part a of the scores, o - a of the values
+#pragma unroll
+                    for (int kt = 0; kt < 4; ++kt)
+#pragma unroll
+                        for (int a = o; a >= 0 && o - a < PI; --a) {
+                            uint32_t bf[4];
+                            ldsm_t(smem_at(sv + (o - a) * S::V + (16 * kt + (lane & 15)) * S::VS + 16 * warp + (lane >> 4) * 8), bf);
+#pragma unroll
+                            for (int m = kt; m < 4; ++m) {
+                                if (16 * m >= live) break;
+                                uint32_t af[4];
+                                ldsm(smem_at(sp + a * S::P + (16 * m + (lane & 15)) * S::PS + 16 * kt + (lane >> 4) * 8), af);
+#pragma unroll
+                                for (int c = 0; c < 2; ++c) mma_bf16(S::F32 ? pv[S::F32 ? m : 0][c] : out[m][c], af, bf[2 * c], bf[2 * c + 1]);
+                            }
+                        }
+#pragma unroll
+                for (int m = 0; m < 4; ++m)
 #pragma unroll
                     for (int half = 0; half < 2; ++half) {
                         const int r = 16 * m + g + 8 * half;
                         if (r >= live) continue;
-                        const float e = half ? e1 : e0;
                         T* at = op + (int64_t)(tok0 + r) * p.o.token_stride + 16 * warp + 2 * tc;
 #pragma unroll
                         for (int c = 0; c < 2; ++c) {
-                            const float x = p.scale * fade_add(out[m][c][2 * half], e, pv[c][2 * half]);
-                            const float y = p.scale * fade_add(out[m][c][2 * half + 1], e, pv[c][2 * half + 1]);
-                            if constexpr (S::F32) *reinterpret_cast<float2*>(at + 8 * c) = make_float2(x, y);
-                            else *reinterpret_cast<uint32_t*>(at + 8 * c) = pack_bf16(x, y);
+                            float x = out[m][c][2 * half], y = out[m][c][2 * half + 1];
+                            if constexpr (S::F32) {
+                                x += pv[m][c][2 * half];
+                                y += pv[m][c][2 * half + 1];
+                                *reinterpret_cast<float2*>(at + 8 * c) = make_float2(p.scale * x, p.scale * y);
+                            } else {
+                                *reinterpret_cast<uint32_t*>(at + 8 * c) = pack_bf16(p.scale * x, p.scale * y);
+                            }
                         }
                     }
-                }
             }
             if (MODE != DECAY_OUTPUTS || chunk + 1 < chunks) {
                 // the state: v with its decay to the chunk's end, as parts, times k
@@ -541,24 +558,29 @@ __global__ void __launch_bounds__(32 * NW, NW == 4 ? 2 : 1) decay_chunk_kernel(c
                         for (int z = 0; z < PV; ++z) va[kt][z][i] = w[z];
                     }
                 }
+                constexpr int JN = S::F32 ? 2 : 4;           // tiles of 8 keys' channels at a time
 #pragma unroll
-                for (int j = 0; j < DK / 8; j += 2) {
-                    float d[2][4];
+                for (int j = 0; j < DK / 8; j += JN) {
+                    float d[JN][4];
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) d[i >> 2][i & 3] = 0.f;
+                    for (int i = 0; i < 4 * JN; ++i) d[i >> 2][i & 3] = 0.f;
 #pragma unroll
-                    for (int o = PV - 1; o >= 0; --o)
+                    for (int a = PI - 1; a >= 0; --a) {      // part a of k; the small products first
+                        uint32_t bf[L / 16][JN / 2][4];
 #pragma unroll
                         for (int kt = 0; kt < L / 16; ++kt)
 #pragma unroll
-                            for (int a = (o < PI ? o : PI - 1); a >= 0; --a) {            // part a of k, o - a of v
-                                uint32_t bf[4];
-                                ldsm_t(smem_at(sk + a * S::Q + (16 * kt + (lane & 15)) * S::QS + 8 * j + (lane >> 4) * 8), bf);
-                                mma_bf16(d[0], va[kt][o - a], bf[0], bf[1]);
-                                mma_bf16(d[1], va[kt][o - a], bf[2], bf[3]);
-                            }
+                            for (int c = 0; c < JN / 2; ++c)
+                                ldsm_t(smem_at(sk + a * S::Q + (16 * kt + (lane & 15)) * S::QS + 8 * j + 16 * c + (lane >> 4) * 8), bf[kt][c]);
 #pragma unroll
-                    for (int c = 0; c < 2; ++c)
+                        for (int z = PV - 1 - a; z >= 0; --z)
+#pragma unroll
+                            for (int kt = 0; kt < L / 16; ++kt)
+#pragma unroll
+                                for (int c = 0; c < JN; ++c) mma_bf16(d[c], va[kt][z], bf[kt][c >> 1][2 * (c & 1)], bf[kt][c >> 1][2 * (c & 1) + 1]);
+                    }
+#pragma unroll
+                    for (int c = 0; c < JN; ++c)
 #pragma unroll
                         for (int i = 0; i < 4; ++i) st[j + c][i] = fade_add(st[j + c][i], last, d[c][i]);
                 }
