@@ -8,9 +8,10 @@
 //   D2 [value, token] = V^T P^T    scores times decay (two parts)
 //   out = scale (exp(G) D1 + D2);  S = exp(G_end) S + D3
 // 20 warps:
-//   0-7    bring q, k, v in (cp.async, a chunk ahead), take the sums of log decays, make scores (mma.sync, 64 x 64) and P, decay the values
+//   0-7    bring q, k, v in (cp.async, a chunk ahead), decay the values, make scores (mma.sync, 64 x 64) and P
 //   8-15   the state in registers (lane: value column; half of the keys each): its update, its parts to shared memory, and the outputs
-//   16     issues the MMAs: D3 as soon as the values are there, D1 and D2 when the state is (17-19: none)
+//   16     issues the MMAs: D3 as soon as the values are there, D1 and D2 when scores and state are
+//   17     the sums of log decays, ahead of the others (18, 19: none)
 // Measured: see below.
 #pragma once
 #include "ccv3d_tc_ptx.cuh"
@@ -20,26 +21,26 @@ namespace ccv3d {
 
 // registers of 256, 256 and 128 threads: 61440, what 640 threads are launched with at 96
 constexpr int DECAY_REGS_FRONT = 88, DECAY_REGS_STATE = 128, DECAY_REGS_REST = 48;
-constexpr int DECAY_TILE_THREADS = 640, DECAY_TILE_DV = 128, DECAY_TILE_RING = 4;
+constexpr int DECAY_TILE_THREADS = 640, DECAY_TILE_DV = 128, DECAY_TILE_RING = 5;
 
 template <int DK> struct DecayTileShape {
     static constexpr uint32_t HALF = 64 * 128;                            // 64 tokens of 64 channels
     static constexpr uint32_t QK = DK / 64 * HALF, V = 2 * HALF, STAGE = 2 * QK + V;
     static constexpr uint32_t S_HALF = 128 * 128, S_PART = DK / 64 * S_HALF;   // 128 value columns of 64 keys
-    static constexpr uint32_t P_AT = 2 * STAGE, VD_AT = P_AT + 2 * HALF, S_AT = VD_AT + 3 * V, BYTES = S_AT + 2 * S_PART + 1024;
+    static constexpr uint32_t P_AT = 2 * STAGE, VD_AT = P_AT + 2 * HALF, S_AT = VD_AT + 3 * V, SHARED_AT = S_AT + 2 * S_PART;
 };
 
 struct DecayTileShared {
+    // (a ring of five: the outputs of chunk c - 2 may still be made while the sums of chunk c + 2 are taken)
     float begin[DECAY_TILE_RING][DECAY_CHUNK];      // exp(G_i)
-    float2 g[DECAY_CHUNK];
-    float end[DECAY_CHUNK];
     float last[DECAY_TILE_RING];
     int odd[DECAY_TILE_RING];
-    uint64_t ready, used, stage_empty[2], s_full, out_full[2], out_empty[2], d3_full[2], d3_empty[2], meet_full, meet_empty, odd_done;
     uint32_t tmem;
     int abort_flag;
+    float2 g[2][DECAY_CHUNK];
+    float end[2][DECAY_CHUNK];
+    uint64_t told[4], g_full[2], g_empty[2], v_ready, v_used, ready, used, s_full, out_full[2], out_empty[2], d3_full[2], d3_empty[2], meet_full, meet_empty, odd_done;
 };
-static_assert(sizeof(DecayTileShared) <= 2032, "beside 225 KB of tiles");
 
 // Bounded wait of a whole warp; false when it gave up or another did.  Warps that meet at named barriers go on to the end all the same, every
 // further wait returning at once, so that none is left waiting there.
@@ -62,6 +63,8 @@ __device__ __forceinline__ bool decay_wait(uint64_t* bar, uint32_t parity, Decay
     return __all_sync(0xffffffffu, ok);
 }
 
+static_assert(DecayTileShape<128>::SHARED_AT + sizeof(DecayTileShared) <= 232448, "shared memory of a block");
+
 // A position in a matrix of rows of 64 BF16 numbers (128 bytes, 128-byte swizzle): row r, 16-byte piece c.
 __device__ __forceinline__ uint32_t swizzled(int r, int c) { return r * 128 + ((c ^ (r & 7)) << 4); }
 
@@ -77,9 +80,8 @@ __global__ void __launch_bounds__(DECAY_TILE_THREADS, 1) decay_tile_kernel(const
     constexpr int L = DECAY_CHUNK, KH = DK / 2;               // KH: keys of a thread of the state
     constexpr bool OUT = MODE != DECAY_STATES;
     extern __shared__ uint8_t decay_tile_smem[];
-    __shared__ DecayTileShared shared;
-    DecayTileShared* sh = &shared;
-    uint8_t* base = decay_tile_smem + (1024 - (smem_u32(decay_tile_smem) & 1023u) & 1023u);
+    uint8_t* base = decay_tile_smem;                           // (all shared memory there is: on 1024 bytes)
+    DecayTileShared* sh = reinterpret_cast<DecayTileShared*>(base + S::SHARED_AT);
     const uint32_t at0 = smem_u32(base);
     const int t = threadIdx.x, warp = __shfl_sync(0xffffffffu, t >> 5, 0), lane = t & 31;
     const int slices = (p.m.value_dim + DECAY_TILE_DV - 1) / DECAY_TILE_DV, slice = blockIdx.y % slices, h = blockIdx.y / slices;
@@ -102,7 +104,14 @@ __global__ void __launch_bounds__(DECAY_TILE_THREADS, 1) decay_tile_kernel(const
         part_at = ((int64_t)blockIdx.x * p.m.heads + h) * DK * p.m.value_dim;
     }
     const int chunks = (n + L - 1) / L;
+    if (at0 & 1023u) {                                         // (not so: nothing is touched)
+        if (t == 0) report(p.status, CCV3D_TOKENS_TIMEOUT);
+        return;
+    }
     if (t == 0) {
+        for (int i = 0; i < 4; ++i) mbar_init(smem_u32(&sh->told[i]), 1);
+        mbar_init(smem_u32(&sh->v_ready), 8);
+        mbar_init(smem_u32(&sh->v_used), 1);
         mbar_init(smem_u32(&sh->ready), 8);
         mbar_init(smem_u32(&sh->used), 1);
         mbar_init(smem_u32(&sh->s_full), 8);
@@ -110,7 +119,8 @@ __global__ void __launch_bounds__(DECAY_TILE_THREADS, 1) decay_tile_kernel(const
         mbar_init(smem_u32(&sh->meet_empty), 4);
         mbar_init(smem_u32(&sh->odd_done), 8);
         for (int i = 0; i < 2; ++i) {
-            mbar_init(smem_u32(&sh->stage_empty[i]), 1);
+            mbar_init(smem_u32(&sh->g_full[i]), 1);
+            mbar_init(smem_u32(&sh->g_empty[i]), 8);
             mbar_init(smem_u32(&sh->out_full[i]), 1);
             mbar_init(smem_u32(&sh->out_empty[i]), 8);
             mbar_init(smem_u32(&sh->d3_full[i]), 1);
@@ -154,43 +164,28 @@ __global__ void __launch_bounds__(DECAY_TILE_THREADS, 1) decay_tile_kernel(const
             asm volatile("cp.async.commit_group;" ::: "memory");
         };
         auto front_sync = [] { asm volatile("bar.sync 1, 256;" ::: "memory"); };
-        bring_chunk(0);
-        if (chunks > 1) bring_chunk(1);
-        double total = 0.0;
-        for (int chunk = 0; chunk < chunks; ++chunk) {
-            const int tok0 = first + chunk * L, live = min(L, n - chunk * L), ring = chunk % DECAY_TILE_RING;
-            const uint8_t* st = base + (chunk & 1) * S::STAGE;
-            const uint32_t sq_ = smem_u32(st), sk = sq_ + S::QK, sv = sk + S::QK;
-            if (warp == 0) {
-                // log decays of tokens 2 lane, 2 lane + 1 and their sums
-                double x[2];
-#pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    const int r = 2 * lane + i;
-                    const float d = r < live ? __ldg(p.decay + (int64_t)(tok0 + r) * p.d_token + h * p.d_head) : 0.f;
-                    x[i] = d < DECAY_FORGET ? (double)DECAY_FORGET : (double)d;
-                }
-                double s = x[0] + x[1];
-#pragma unroll
-                for (int o = 1; o < 32; o <<= 1) {
-                    const double y = __shfl_up_sync(0xffffffffu, s, o);
-                    if (lane >= o) s += y;
-                }
-                const double end = __shfl_sync(0xffffffffu, s, 31);
-#pragma unroll
-                for (int i = 0; i < 2; ++i) {
-                    const double at = i ? s : s - x[1];
-                    const float hi = (float)at;
-                    sh->g[2 * lane + i] = make_float2(hi, (float)(at - hi));
-                    sh->begin[ring][2 * lane + i] = expf((float)at);
-                    sh->end[2 * lane + i] = expf((float)(end - at));
-                }
-                if (lane == 31) sh->last[ring] = expf((float)end);
-                if (t == 0) sh->odd[ring] = 0;
-                total += end;
+        // the rows of a chunk come to L2 ahead of their turn, a line of 128 bytes to a thread
+        auto prefetch = [&](const T* from, int64_t stride, int tok, int live, int have) {
+            const int per = (have + 63) / 64;
+            for (int i = t; i < live * per; i += 256) {
+                const int r = i / per, c = i - r * per;
+                asm volatile("prefetch.global.L2 [%0];" ::"l"(from + (int64_t)(tok + r) * stride + 64 * c));
             }
-            if (chunk + 1 < chunks) asm volatile("cp.async.wait_group 1;" ::: "memory");
-            else asm volatile("cp.async.wait_group 0;" ::: "memory");
+        };
+        bring_chunk(0);
+        for (int chunk = 0; chunk < chunks; ++chunk) {
+            const int ring = chunk % DECAY_TILE_RING, two = chunk & 1;
+            const uint8_t* st = base + two * S::STAGE;
+            const uint32_t sq_ = smem_u32(st), sk = sq_ + S::QK;
+            const float2* gs = sh->g[two];
+            if (chunk + 2 < chunks) {
+                const int tok = first + (chunk + 2) * L, live = min(L, n - (chunk + 2) * L);
+                if (OUT) prefetch(qp, p.q.token_stride, tok, live, DK);
+                prefetch(kp, p.k.token_stride, tok, live, DK);
+                prefetch(vp, p.v.token_stride, tok, live, dvs);
+            }
+            if (t == 0) sh->odd[ring] = 0;
+            asm volatile("cp.async.wait_group 0;" ::: "memory");
             front_sync();
             // whether all keys and values are finite
             uint32_t most = 0;
@@ -202,6 +197,26 @@ __global__ void __launch_bounds__(DECAY_TILE_THREADS, 1) decay_tile_kernel(const
             };
             look(st + S::QK, S::QK + S::V);
             if ((most & 0xFFFFu) >= 0x7F80u || (most >> 16) >= 0x7F80u) sh->odd[ring] = 1;
+            // values with their decay to the chunk's end, as parts
+            ok = decay_wait(&sh->g_full[two], chunk >> 1 & 1, sh, p) && ok;
+            if (chunk) ok = decay_wait(&sh->v_used, (chunk - 1) & 1, sh, p) && ok;
+#pragma unroll
+            for (int i = 0; i < L * 16 / 256; ++i) {
+                const int at = t + 256 * i, r = at >> 4, c = at & 15;
+                const uint32_t pos = (c >> 3) * S::HALF + swizzled(r, c & 7);
+                const uint4 w = *reinterpret_cast<const uint4*>(st + 2 * S::QK + pos);
+                const float e = sh->end[two][r];
+                const uint32_t raw[4] = {w.x, w.y, w.z, w.w};
+                uint32_t part[4][3];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) split_pair<3>(__uint_as_float(raw[j] << 16) * e, __uint_as_float(raw[j] & 0xFFFF0000u) * e, part[j]);
+#pragma unroll
+                for (int z = 0; z < 3; ++z)
+                    *reinterpret_cast<uint4*>(base + S::VD_AT + z * S::V + pos) = make_uint4(part[0][z], part[1][z], part[2][z], part[3][z]);
+            }
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            __syncwarp();
+            if (lane == 0) mbar_arrive(smem_u32(&sh->v_ready));
             if constexpr (OUT) {
                 // scores of 16 tokens i with 32 tokens j, times their decay, as parts
                 const int i0 = 16 * (warp & 3), j0 = 32 * (warp >> 2);
@@ -223,55 +238,37 @@ __global__ void __launch_bounds__(DECAY_TILE_THREADS, 1) decay_tile_kernel(const
                         }
                     }
                 }
-                if (chunk) ok = decay_wait(&sh->used, (chunk - 1) & 1, sh, p) && ok;      // (the products of the chunk before are done)
-                const float2 ga = sh->g[i0 + g], gb = sh->g[i0 + g + 8];
+                uint32_t pa[4][2], pb[4][2];
+                const float2 ga = gs[i0 + g], gb = gs[i0 + g + 8];
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
                     const int c = j0 + 8 * j + 2 * tc;
-                    const float4 gj = *reinterpret_cast<const float4*>(&sh->g[c]);
+                    const float4 gj = *reinterpret_cast<const float4*>(&gs[c]);
                     const auto weigh = [&](float s, const float2& gi, float hi, float lo, bool seen) {
                         const float w = seen ? __expf((gi.x - hi) + (gi.y - lo)) : 0.f;
                         return w == 0.f ? 0.f : s * w;
                     };
-                    uint32_t a[2], b[2];
-                    split_pair<2>(weigh(sc[j][0], ga, gj.x, gj.y, c <= i0 + g), weigh(sc[j][1], ga, gj.z, gj.w, c + 1 <= i0 + g), a);
-                    split_pair<2>(weigh(sc[j][2], gb, gj.x, gj.y, c <= i0 + g + 8), weigh(sc[j][3], gb, gj.z, gj.w, c + 1 <= i0 + g + 8), b);
+                    split_pair<2>(weigh(sc[j][0], ga, gj.x, gj.y, c <= i0 + g), weigh(sc[j][1], ga, gj.z, gj.w, c + 1 <= i0 + g), pa[j]);
+                    split_pair<2>(weigh(sc[j][2], gb, gj.x, gj.y, c <= i0 + g + 8), weigh(sc[j][3], gb, gj.z, gj.w, c + 1 <= i0 + g + 8), pb[j]);
+                }
+                if (chunk) ok = decay_wait(&sh->used, (chunk - 1) & 1, sh, p) && ok;       // (the products of the chunk before are done)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const int c = j0 + 8 * j + 2 * tc;
 #pragma unroll
                     for (int z = 0; z < 2; ++z) {
-                        *reinterpret_cast<uint32_t*>(base + S::P_AT + z * S::HALF + swizzled(i0 + g, c >> 3) + (c & 7) * 2) = a[z];
-                        *reinterpret_cast<uint32_t*>(base + S::P_AT + z * S::HALF + swizzled(i0 + g + 8, c >> 3) + (c & 7) * 2) = b[z];
+                        *reinterpret_cast<uint32_t*>(base + S::P_AT + z * S::HALF + swizzled(i0 + g, c >> 3) + (c & 7) * 2) = pa[j][z];
+                        *reinterpret_cast<uint32_t*>(base + S::P_AT + z * S::HALF + swizzled(i0 + g + 8, c >> 3) + (c & 7) * 2) = pb[j][z];
                     }
                 }
-            } else {
-                if (chunk) ok = decay_wait(&sh->used, (chunk - 1) & 1, sh, p) && ok;
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                __syncwarp();
+                if (lane == 0) mbar_arrive(smem_u32(&sh->ready));
             }
-            // values with their decay to the chunk's end, as parts
-#pragma unroll
-            for (int i = 0; i < L * 16 / 256; ++i) {
-                const int at = t + 256 * i, r = at >> 4, c = at & 15;
-                const uint32_t pos = (c >> 3) * S::HALF + swizzled(r, c & 7);
-                const uint4 w = *reinterpret_cast<const uint4*>(st + 2 * S::QK + pos);
-                const float e = sh->end[r];
-                const uint32_t raw[4] = {w.x, w.y, w.z, w.w};
-                uint32_t part[4][3];
-#pragma unroll
-                for (int j = 0; j < 4; ++j) split_pair<3>(__uint_as_float(raw[j] << 16) * e, __uint_as_float(raw[j] & 0xFFFF0000u) * e, part[j]);
-#pragma unroll
-                for (int z = 0; z < 3; ++z)
-                    *reinterpret_cast<uint4*>(base + S::VD_AT + z * S::V + pos) = make_uint4(part[0][z], part[1][z], part[2][z], part[3][z]);
-            }
-            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-            __syncwarp();
-            if (lane == 0) mbar_arrive(smem_u32(&sh->ready));
-            front_sync();                                     // (g and end have been used)
-            if (chunk + 2 < chunks) {
-                // this chunk's place takes the chunk after next
-                ok = decay_wait(&sh->stage_empty[chunk & 1], (chunk >> 1) & 1, sh, p) && ok;
-                bring_chunk(chunk + 2);
-            }
+            if (lane == 0) mbar_arrive(smem_u32(&sh->g_empty[two]));
+            if (chunk + 1 < chunks) bring_chunk(chunk + 1);      // (into the place of the chunk before, whose products are done)
         }
         asm volatile("cp.async.wait_all;" ::: "memory");
-        if (MODE == DECAY_STATES && ok && t == 0 && slice == 0) p.fade[(int64_t)blockIdx.x * p.m.heads + h] = expf((float)total);
     } else if (warp < 16) {
         // ------------------------------------------------------------------------------------------ the state, outputs
         asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(DECAY_REGS_STATE));
@@ -307,7 +304,8 @@ __global__ void __launch_bounds__(DECAY_TILE_THREADS, 1) decay_tile_kernel(const
         int turn = 0, met = 0;                                 // chunks that went through the tensor cores, tokens that did not
         for (int chunk = 0; ok && chunk < chunks; ++chunk) {
             const int tok0 = first + chunk * L, live = min(L, n - chunk * L), ring = chunk % DECAY_TILE_RING;
-            if (!(ok = decay_wait(&sh->ready, chunk & 1, sh, p))) break;
+            // (the issuer tells of a chunk; it is never four ahead, while the front may be more than a phase of its barriers ahead of this)
+            if (!(ok = decay_wait(&sh->told[chunk & 3], chunk >> 2 & 1, sh, p))) break;
             const bool last_one = chunk + 1 == chunks;
             if (sh->odd[ring]) {
                 // token by token; the two halves' parts of q S meet in shared memory (the place of P)
@@ -396,6 +394,47 @@ __global__ void __launch_bounds__(DECAY_TILE_THREADS, 1) decay_tile_kernel(const
     } else {
         // ------------------------------------------------------------------------------------------ MMAs
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(DECAY_REGS_REST));
+        if (warp == 17) {
+            // log decays of tokens 2 lane, 2 lane + 1 of a chunk and their sums, up to two chunks ahead
+            double total = 0.0;
+            float next[2];
+            auto fetch = [&](int chunk) {
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    const int r = chunk * L + 2 * lane + i;
+                    next[i] = r < n ? __ldg(p.decay + (int64_t)(first + r) * p.d_token + h * p.d_head) : 0.f;
+                }
+            };
+            fetch(0);
+            for (int chunk = 0; ok && chunk < chunks; ++chunk) {
+                const int two = chunk & 1, ring = chunk % DECAY_TILE_RING;
+                double x[2];
+#pragma unroll
+                for (int i = 0; i < 2; ++i) x[i] = next[i] < DECAY_FORGET ? (double)DECAY_FORGET : (double)next[i];
+                if (chunk + 1 < chunks) fetch(chunk + 1);
+                double s = x[0] + x[1];
+#pragma unroll
+                for (int o = 1; o < 32; o <<= 1) {
+                    const double y = __shfl_up_sync(0xffffffffu, s, o);
+                    if (lane >= o) s += y;
+                }
+                const double end = __shfl_sync(0xffffffffu, s, 31);
+                if (!(ok = decay_wait(&sh->g_empty[two], (chunk >> 1 & 1) ^ 1u, sh, p))) break;
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    const double at = i ? s : s - x[1];
+                    const float hi = (float)at;
+                    sh->g[two][2 * lane + i] = make_float2(hi, (float)(at - hi));
+                    sh->begin[ring][2 * lane + i] = expf((float)at);
+                    sh->end[two][2 * lane + i] = expf((float)(end - at));
+                }
+                if (lane == 31) sh->last[ring] = expf((float)end);
+                total += end;
+                __syncwarp();
+                if (lane == 0) mbar_arrive(smem_u32(&sh->g_full[two]));
+            }
+            if (MODE == DECAY_STATES && ok && lane == 0 && slice == 0) p.fade[(int64_t)blockIdx.x * p.m.heads + h] = expf((float)total);
+        }
         // D = F32, A = B = BF16, M = 128; bits 15, 16: A, B lie with their rows, not K, side by side (tokens are K in D3 and for the values)
         constexpr uint32_t I = (1u << 4) | (1u << 7) | (1u << 10) | ((128u >> 4) << 24);
         constexpr uint32_t I_D3 = I | (1u << 15) | (1u << 16) | ((uint32_t)(DK >> 3) << 17), I_D1 = I | ((64u >> 3) << 17), I_D2 = I | (1u << 15) | ((64u >> 3) << 17);
@@ -403,15 +442,22 @@ __global__ void __launch_bounds__(DECAY_TILE_THREADS, 1) decay_tile_kernel(const
         const auto mn_major = [&](uint32_t at) { return (((at0 + at) & 0x3FFFFu) >> 4) | ((S::HALF >> 4) << 16); };
         int turn = 0, s_turn = 0, odd_turn = 0;
         for (int chunk = 0; warp == 16 && ok && chunk < chunks; ++chunk) {
-            if (!(ok = decay_wait(&sh->ready, chunk & 1, sh, p))) break;
-            if (sh->odd[chunk % DECAY_TILE_RING]) {             // (goes token by token; the state that was made for it is not used)
-                if (OUT && !(ok = decay_wait(&sh->s_full, s_turn & 1, sh, p))) break;
+            if (!(ok = decay_wait(&sh->v_ready, chunk & 1, sh, p))) break;
+            const bool odd = sh->odd[chunk % DECAY_TILE_RING];
+            if (odd && OUT) {
+                // P and the state have been written, and go unused: before the state's warps hear of the chunk and go on
+                if (!(ok = decay_wait(&sh->ready, chunk & 1, sh, p))) break;
+                if (!(ok = decay_wait(&sh->s_full, s_turn & 1, sh, p))) break;
                 ++s_turn;
+            }
+            if (lane == 0) mbar_arrive(smem_u32(&sh->told[chunk & 3]));
+            __syncwarp();
+            if (odd) {                                          // token by token
                 if (!(ok = decay_wait(&sh->odd_done, odd_turn & 1, sh, p))) break;
                 ++odd_turn;
                 if (lane == 0) {
-                    mbar_arrive(smem_u32(&sh->used));
-                    mbar_arrive(smem_u32(&sh->stage_empty[chunk & 1]));
+                    mbar_arrive(smem_u32(&sh->v_used));
+                    if (OUT) mbar_arrive(smem_u32(&sh->used));
                 }
                 __syncwarp();
                 continue;
@@ -430,14 +476,12 @@ __global__ void __launch_bounds__(DECAY_TILE_THREADS, 1) decay_tile_kernel(const
                         for (int k = 0; k < 4; ++k)
                             decay_mma(tmem + buf * 128, a0 + z * (S::V >> 4) + k * (2048 >> 4), b0 + k * (2048 >> 4), I_D3, z < 2 || k > 0);
                     tc_commit(smem_u32(&sh->d3_full[buf]));
-                    if (!OUT) {
-                        tc_commit(smem_u32(&sh->used));
-                        tc_commit(smem_u32(&sh->stage_empty[chunk & 1]));
-                    }
+                    tc_commit(smem_u32(&sh->v_used));
                 }
                 __syncwarp();
             }
             if constexpr (OUT) {
+                if (!(ok = decay_wait(&sh->ready, chunk & 1, sh, p))) break;
                 if (!(ok = decay_wait(&sh->out_empty[buf], ph, sh, p))) break;
                 if (!(ok = decay_wait(&sh->s_full, s_turn & 1, sh, p))) break;
                 ++s_turn;
@@ -457,7 +501,6 @@ __global__ void __launch_bounds__(DECAY_TILE_THREADS, 1) decay_tile_kernel(const
                             decay_mma(tmem + 384 + buf * 64, a2 + k * (2048 >> 4), b2 + z * (S::HALF >> 4) + 2 * k, I_D2, z < 1 || k > 0);
                     tc_commit(smem_u32(&sh->out_full[buf]));
                     tc_commit(smem_u32(&sh->used));
-                    tc_commit(smem_u32(&sh->stage_empty[chunk & 1]));
                 }
                 __syncwarp();
             }

@@ -58,11 +58,13 @@ def test_against_64_bits(new, dk, dv, dtype):
 
 
 @pytest.mark.parametrize("dtype", [BF, F])
-@pytest.mark.parametrize("new,heads", [([1500], 3), ([700, 5, 0, 1201], 2), ([33] * 40, 8), ([3000], 1)])
-def test_long_and_many(new, heads, dtype):
-    c = Case(new, heads, 1, 64, 64, dtype, seed=5, rate=0.01)
+@pytest.mark.parametrize("new,heads,dk,dv", [([1500], 3, 64, 64), ([700, 5, 0, 1201], 2, 128, 128), ([33] * 40, 8, 64, 64), ([3000], 1, 64, 64), ([6000], 1, 128, 64),
+                                             ([1300] * 9, 16, 128, 128)])
+def test_long_and_many(new, heads, dk, dv, dtype):
+    c = Case(new, heads, 1, dk, dv, dtype, seed=5, rate=0.01)
     out, m = c.run()
     c.check(out, m)
+    assert m.status() == 0
     again, other = c.run()
     assert torch.equal(out, again) and torch.equal(m.states, other.states)
 
@@ -85,7 +87,7 @@ def test_strong_decays_and_forgetting(n, dtype):
 @pytest.mark.parametrize("n", [6, 200, 900])
 def test_what_is_not_finite_reaches_only_what_sees_it(n, dtype):
     c = Case([n], 2, 2, 64, 64, dtype, seed=7)
-    clean, m0 = c.run()
+    clean, _ = c.run()
     bad = n - 3
     c.v[bad, 0, 5], c.k[bad, 1, 3] = float("nan"), float("inf")
     out, m = c.run()
@@ -93,6 +95,7 @@ def test_what_is_not_finite_reaches_only_what_sees_it(n, dtype):
     torch.testing.assert_close(out[:bad], clean[:bad], **tol)             # earlier tokens
     assert torch.isnan(out[bad:, 0, 5]).all() and not torch.isnan(out[:, 0, :5]).any()
     assert not torch.isfinite(out[bad, 1]).any() and not torch.isfinite(m.states[c.slot[0], 1, 3]).any()
+    assert m.status() == 0
     # all that went wrong is forgotten at once
     c.g[bad + 1] = -float("inf")
     out, m = c.run()
