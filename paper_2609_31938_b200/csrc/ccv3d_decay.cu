@@ -31,17 +31,19 @@ ccv3d_status check_decay(const ccv3d_decay_memory* m, const ccv3d_stream_batch* 
 ccv3d_status plan_decay(const ccv3d_decay_memory* m, const ccv3d_stream_batch* b, int dtype, DecayPlan* q) {
     const ccv3d_status s = current_device(&q->dev);
     if (s != CCV3D_OK) return s;
-    q->step = b->max_new <= 8;
+    q->step = b->max_new <= (dtype == CCV3D_F32 && getenv("DSTEP") ? atoi(getenv("DSTEP")) : 8);
+    if (dtype == CCV3D_BF16 && getenv("DSTEPB")) q->step = b->max_new <= atoi(getenv("DSTEPB"));
     q->columns = dtype == CCV3D_BF16 || m->value_dim % 128 == 0 ? 128 : 64;
     q->seg = 0;
     q->items = q->fade_at = 0;
     q->bytes = 0;
     if (q->step) return CCV3D_OK;
-    // blocks of a chunk kernel for each item, and how many there should be
-    const int64_t wide = (int64_t)m->heads * ((m->value_dim + q->columns - 1) / q->columns), want = (getenv("DWANT") ? atoi(getenv("DWANT")) : 2) * q->dev.sm_count;
+    // Blocks of a chunk kernel for each item.  Where the sequences do not fill the machine, or one is far longer than the others, they are cut
+    // so that one turn of blocks does: a block's start and end cost as much as some chunks.
+    const int64_t wide = (int64_t)m->heads * ((m->value_dim + q->columns - 1) / q->columns), fit = q->dev.sm_count;
     const int64_t longest = b->max_new < b->tokens ? b->max_new : b->tokens;
-    if (wide * b->batch >= want && longest <= 8 * ((int64_t)b->tokens / b->batch + 64)) return CCV3D_OK;
-    const int64_t items = (want + wide - 1) / wide, chunks = (b->tokens + DECAY_CHUNK - 1) / DECAY_CHUNK;
+    if (wide * b->batch >= fit && longest <= 8 * ((int64_t)b->tokens / b->batch + 64)) return CCV3D_OK;
+    const int64_t items = fit / wide > b->batch ? fit / wide : b->batch, chunks = (b->tokens + DECAY_CHUNK - 1) / DECAY_CHUNK;
     int64_t per = (chunks + items - 1) / items;
     if (per < 4) per = 4;
     if (per * DECAY_CHUNK >= longest) return CCV3D_OK;

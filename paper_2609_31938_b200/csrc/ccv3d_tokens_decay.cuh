@@ -83,65 +83,87 @@ __device__ __forceinline__ float fade(float s, float f) { return f == 0.f ? 0.f 
 __device__ __forceinline__ float fade_add(float s, float f, float x) { return f == 0.f ? x : fmaf(s, f, x); }
 
 // ---------------------------------------------------------------------------------------------------- single tokens
-// Block (sequence, head, 64 value columns): thread t has columns 4 (t % 16) .. + 3 of rows t / 16 + 16 i.
+// Block (sequence, head, 64 value columns): thread t has columns 4 (t % 16) .. + 3 of rows R (t / 16) + i, whose keys and queries it reads four at
+// a time (one by one, the way to shared memory bounds prompts:   Up to eight tokens are brought in at
+// a time, and their outputs' parts summed together.
+constexpr int DECAY_STEP_TOKENS = 8;
 template <typename T, int DK>
 __global__ void __launch_bounds__(DECAY_STEP_THREADS) decay_step_kernel(const __grid_constant__ DecayParams p) {
-    constexpr int R = DK / 16;
-    __shared__ __align__(16) float kq[2][2][DK];             // [turn][k, q]
-    __shared__ __align__(16) float part[2][8][64];
-    const int slices = p.m.value_dim / 64, t = threadIdx.x, row0 = t >> 4;
+    constexpr int R = DK / 16, M = DECAY_STEP_TOKENS;
+    __shared__ __align__(16) float ks[M][DK], qs[M][DK], vs[M][64], fs[M];
+    __shared__ __align__(16) float part[M][8][64];
+    const int slices = p.m.value_dim / 64, t = threadIdx.x, team = t >> 4, row0 = team * R, c4 = (t & 15) * 4;
     const int slice = blockIdx.x % slices, h = blockIdx.x / slices % p.m.heads, b = blockIdx.x / slices / p.m.heads;
     const DecaySeq s = decay_seq(p, b, slice == 0 && h == 0);
     if (s.n == 0) return;
-    const int col = slice * 64 + (t & 15) * 4;
-    float* state = p.m.states + ((int64_t)max(s.slot, 0) * p.m.heads + h) * DK * p.m.value_dim + col;
+    float* state = p.m.states + ((int64_t)max(s.slot, 0) * p.m.heads + h) * DK * p.m.value_dim + slice * 64 + c4;
     float4 S[R];
 #pragma unroll
-    for (int i = 0; i < R; ++i) S[i] = s.zero ? make_float4(0.f, 0.f, 0.f, 0.f) : *reinterpret_cast<const float4*>(state + (int64_t)(row0 + 16 * i) * p.m.value_dim);
+    for (int i = 0; i < R; ++i) S[i] = s.zero ? make_float4(0.f, 0.f, 0.f, 0.f) : *reinterpret_cast<const float4*>(state + (int64_t)(row0 + i) * p.m.value_dim);
     const T* k = (const T*)p.k.data + h / p.group * p.k.head_stride;
     const T* q = (const T*)p.q.data + h / p.group * p.q.head_stride;
-    const T* v = (const T*)p.v.data + h * p.v.head_stride + col;
+    const T* v = (const T*)p.v.data + h * p.v.head_stride + slice * 64;
     T* o = (T*)p.o.data + h * p.o.head_stride + slice * 64;
-    for (int i = 0; i < s.n; ++i) {
-        const int64_t tok = s.first + i;
-        float(&now)[2][DK] = kq[i & 1];
-        if (t < DK / 2) {
+    for (int base = 0; base < s.n; base += M) {
+        const int m = min(M, s.n - base);
+        const int64_t tok = s.first + base;
+        for (int i = t; i < m * (DK / 4); i += DECAY_STEP_THREADS) {
+            const int r = i / (DK / 4), c = i % (DK / 4) * 4;
             float x[4];
-            const T* at = t < DK / 4 ? k + tok * p.k.token_stride + 4 * t : q + tok * p.q.token_stride + 4 * (t - DK / 4);
-            load4(at, x);
-            store4(&now[t >= DK / 4][4 * (t & (DK / 4 - 1))], x);
+            load4(k + (tok + r) * p.k.token_stride + c, x);
+            store4(&ks[r][c], x);
+            load4(q + (tok + r) * p.q.token_stride + c, x);
+            store4(&qs[r][c], x);
         }
-        float x[4];
-        load4(v + tok * p.v.token_stride, x);
-        const float g = __ldg(p.decay + tok * p.d_token + h * p.d_head), f = expf(g);
-        __syncthreads();
-        float y[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int r = 0; r < R; ++r) {
-            const float kk = now[0][row0 + 16 * r], qq = now[1][row0 + 16 * r];
-            S[r].x = fade_add(S[r].x, f, kk * x[0]);
-            S[r].y = fade_add(S[r].y, f, kk * x[1]);
-            S[r].z = fade_add(S[r].z, f, kk * x[2]);
-            S[r].w = fade_add(S[r].w, f, kk * x[3]);
-            y[0] = fmaf(qq, S[r].x, y[0]);
-            y[1] = fmaf(qq, S[r].y, y[1]);
-            y[2] = fmaf(qq, S[r].z, y[2]);
-            y[3] = fmaf(qq, S[r].w, y[3]);
+        if (team < m) {
+            float x[4];
+            load4(v + (tok + team) * p.v.token_stride + c4, x);
+            store4(&vs[team][c4], x);
         }
-#pragma unroll
-        for (int j = 0; j < 4; ++j) y[j] += __shfl_xor_sync(0xffffffffu, y[j], 16);
-        if ((t & 31) < 16) store4(&part[i & 1][t >> 5][(t & 15) * 4], y);
+        if (t < m) fs[t] = expf(__ldg(p.decay + (tok + t) * p.d_token + h * p.d_head));
         __syncthreads();
-        if (t < 64) {
-            float sum = part[i & 1][0][t];
+        for (int i = 0; i < m; ++i) {
+            const float4 x = *reinterpret_cast<const float4*>(&vs[i][c4]);
+            const float f = fs[i];
+            float y[4] = {0.f, 0.f, 0.f, 0.f};
+            if (f == 0.f) {                                      // all before is forgotten, whatever it was
 #pragma unroll
-            for (int w = 1; w < 8; ++w) sum += part[i & 1][w][t];
-            store1(o + tok * p.o.token_stride + t, sum * p.scale);
+                for (int r = 0; r < R; ++r) S[r] = make_float4(0.f, 0.f, 0.f, 0.f);
+            }
+#pragma unroll
+            for (int r4 = 0; r4 < R; r4 += 4) {
+                float kk[4], qq[4];
+                load4(&ks[i][row0 + r4], kk);
+                load4(&qs[i][row0 + r4], qq);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    float4& st = S[r4 + j];
+                    st.x = fmaf(st.x, f, kk[j] * x.x);
+                    st.y = fmaf(st.y, f, kk[j] * x.y);
+                    st.z = fmaf(st.z, f, kk[j] * x.z);
+                    st.w = fmaf(st.w, f, kk[j] * x.w);
+                    y[0] = fmaf(qq[j], st.x, y[0]);
+                    y[1] = fmaf(qq[j], st.y, y[1]);
+                    y[2] = fmaf(qq[j], st.z, y[2]);
+                    y[3] = fmaf(qq[j], st.w, y[3]);
+                }
+            }
+#pragma unroll
+            for (int j = 0; j < 4; ++j) y[j] += __shfl_xor_sync(0xffffffffu, y[j], 16);
+            if ((t & 31) < 16) store4(&part[i][t >> 5][c4], y);
+        }
+        __syncthreads();
+        for (int i = t; i < m * 64; i += DECAY_STEP_THREADS) {
+            const int r = i >> 6, c = i & 63;
+            float sum = part[r][0][c];
+#pragma unroll
+            for (int w = 1; w < 8; ++w) sum += part[r][w][c];
+            store1(o + (tok + r) * p.o.token_stride + c, sum * p.scale);
         }
     }
     if (s.slot >= 0) {
 #pragma unroll
-        for (int i = 0; i < R; ++i) *reinterpret_cast<float4*>(state + (int64_t)(row0 + 16 * i) * p.m.value_dim) = S[i];
+        for (int i = 0; i < R; ++i) *reinterpret_cast<float4*>(state + (int64_t)(row0 + i) * p.m.value_dim) = S[i];
     }
 }
 
@@ -313,6 +335,16 @@ __global__ void __launch_bounds__(32 * NW, NW == 4 ? 2 : 1) decay_chunk_kernel(c
     bring_chunk(0);
     for (int chunk = 0; chunk < chunks; ++chunk) {
         const int tok0 = first + chunk * L, live = min(L, n - chunk * L);
+        if (S::BUFFERS == 1 && chunk + 1 < chunks) {       // the next chunk's rows come to L2
+            const int ahead = min(L, n - (chunk + 1) * L), kl = DK * (int)sizeof(T) / 128, vl = S::DV * (int)sizeof(T) / 128;
+            for (int i = t; i < ahead * (2 * kl + vl); i += S::THREADS) {
+                const int r = i / (2 * kl + vl), c = i - r * (2 * kl + vl);
+                const int64_t tok = tok0 + L + r;
+                const T* at = c < kl ? kp + tok * p.k.token_stride + c * (128 / sizeof(T))
+                              : c < 2 * kl ? qp + tok * p.q.token_stride + (c - kl) * (128 / sizeof(T)) : vp + tok * p.v.token_stride + (c - 2 * kl) * (128 / sizeof(T));
+                asm volatile("prefetch.global.L2 [%0];" ::"l"(at));
+            }
+        }
         __nv_bfloat16* sq_ = decay_smem + chunk % S::BUFFERS * S::IN;
         __nv_bfloat16 *sk = sq_ + PI * S::Q, *sv = sk + PI * S::Q, *sp = decay_smem + S::BUFFERS * S::IN;
         if (warp == 0) {

@@ -355,8 +355,13 @@ __global__ void __launch_bounds__(DECAY_TILE_THREADS, 1) decay_tile_kernel(const
                     uint32_t v[32];
                     tc_ld16(lanes + buf * 128 + half * KH + j, v);
                     tc_wait_ld();
+                    if (f != 0.f) {
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) st[j + i] = fade_add(st[j + i], f, __uint_as_float(v[i]));
+                        for (int i = 0; i < 16; ++i) st[j + i] = fmaf(st[j + i], f, __uint_as_float(v[i]));
+                    } else {
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) st[j + i] = __uint_as_float(v[i]);
+                    }
                 }
                 tc_fence_before();
                 __syncwarp();
