@@ -561,8 +561,8 @@ typedef enum { CCV3D_ACT_NONE = 0, CCV3D_ACT_SILU = 1, CCV3D_ACT_GELU = 2, CCV3D
  *   Rows of x and w are dense; their strides (in elements) and addresses are multiples of 16 bytes; out and residual go by elements.
  *   k, n_out, rows: any number from 1 on (rows = 0: a call without work), each below 2^31 - 2^16; k <= 2^20.
  * Products are exact, sums FP32 (rounded every few hundred terms; between, the tensor cores cut off bits below the last), everything
- * behind them FP32, the output is rounded once.  F32 operands go in as three BF16 numbers each (24 bits, exact); products under 2^-24
- * of the whole are left out.  F32: an infinity makes its outputs NaN, and numbers under 2^-110 lose bits.
+ * behind them FP32, the output is rounded once.  F32 operands go in as three BF16 numbers each (24 bits, exact), and products under 2^-24
+ * of the whole are left out (few rows: FP32 arithmetic).  F32: an infinity may make its outputs NaN, and numbers under 2^-110 lose bits.
  *   ws      DEVICE scratch, 256-byte aligned, ccv3d_linear_workspace() bytes, of the call alone (NULL where that is 0)
  *   status  DEVICE word or NULL: receives CCV3D_TOKENS_TIMEOUT
  * Any other overlap of out or ws with another tensor is CCV3D_ERR_ALIAS.  Results do not depend on what else runs, the same call gives
@@ -595,7 +595,7 @@ ccv3d_status ccv3d_linear_workspace(const ccv3d_linear_desc* d, uint64_t* bytes_
  *   new_start [batch + 1], slot [batch], fresh [batch]: DEVICE int32, checked by the kernels: offsets out of range are cut, a slot outside the pool, or one that
  *          an earlier sequence of the call (with new tokens) has, is not touched (its sequence starts from zeros and its state is lost), both are reported.
  *          Rows of out that belong to no sequence are not written.
- * All sums and states are FP32; dtype F32: products to 2^-23; BF16: scores and the state are taken to 2^-16 for the outputs and to 2^-23 for the new state.  F32: numbers beyond
+ * All sums and states are FP32; dtype F32: products to 2^-23; BF16 (from some 20 new tokens on): scores and the state are taken to 2^-16 for the outputs and to 2^-23 for the new state.  F32: numbers beyond
  * 3.38e38 may count as infinite, and those under 2^-110 lose bits.
  *   ws      DEVICE scratch, 256-byte aligned, ccv3d_decay_attend_workspace() bytes, of the call alone (NULL where that is 0)
  * An overlap of out, states or ws with another tensor is CCV3D_ERR_ALIAS.  Stream-ordered, no allocation, legal in a stream capture.

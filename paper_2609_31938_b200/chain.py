@@ -133,3 +133,34 @@ class ResidentDecoderChain:
     def close(self):
         for l in self.layers.values():
             l.close()
+
+
+class NormedDecoderChain(ResidentDecoderChain):
+    """The resident chain with the residual blocks of a trained decoder: a group norm with SiLU in front of each of their
+    convolutions, x <- x + conv2(act(norm(conv1(act(norm(x))))).  Each frame is normed by itself, so a stream may still be cut into
+    chunks anywhere.  The first norm of a block writes a ring of its own (the block's input is its residual), the second works in
+    place; the temporal history of a convolution is the normed frames of earlier chunks."""
+
+    def __init__(self, weights: dict, biases: dict, norms: dict, groups: int = 32, eps: float = 1e-6):
+        """norms: for each 3x3x3 layer (A1, A2, B1, B2, C1, C2) the (weight, bias) of the norm in front of it, [channels] float32 each."""
+        super().__init__(weights, biases)
+        self.norms, self.groups, self.eps = norms, groups, eps
+
+    def _alloc(self, N, T, H, W):
+        super()._alloc(N, T, H, W)
+        for n in ("A1", "B1", "C1"):
+            r = self.rings[n]
+            self.rings[n + "n"] = FrameRing(r.N, r.C, r.F, r.H, r.W)
+
+    def _norm(self, name, ring, slot, T, to=None):
+        ring.group_norm(slot, T, self.groups, *self.norms[name], eps=self.eps, activation="silu", out_ring=to, out_slot=slot if to else 0)
+
+    def _block(self, first, second, nxt, slot, hist, T, out=None):
+        r, L = self.rings, self.layers
+        self._norm(first, r[first], slot, T, r[first + "n"])
+        L[first].forward_ring(r[first + "n"], slot, hist, T, out_ring=r[second], out_slot=slot)
+        self._norm(second, r[second], slot, T)
+        if out is None:
+            L[second].forward_ring(r[second], slot, hist, T, out_ring=r[nxt], out_slot=0, res=r[first], res_slot=slot)
+        else:
+            L[second].forward_ring(r[second], slot, hist, T, out=out, res=r[first], res_slot=slot)

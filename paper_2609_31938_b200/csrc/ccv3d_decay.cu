@@ -31,8 +31,10 @@ ccv3d_status check_decay(const ccv3d_decay_memory* m, const ccv3d_stream_batch* 
 ccv3d_status plan_decay(const ccv3d_decay_memory* m, const ccv3d_stream_batch* b, int dtype, DecayPlan* q) {
     const ccv3d_status s = current_device(&q->dev);
     if (s != CCV3D_OK) return s;
-    q->step = b->max_new <= (dtype == CCV3D_F32 && getenv("DSTEP") ? atoi(getenv("DSTEP")) : 8);
-    if (dtype == CCV3D_BF16 && getenv("DSTEPB")) q->step = b->max_new <= atoi(getenv("DSTEPB"));
+    // Up to which number of new tokens a state goes token by token.  us, 64 sequences of n tokens, 32 heads of 128 (16 of 64), step kernel /
+    // chunks, BF16: 9 tokens 87 / 155 (17 / 56), 16 119 / 156 (21 / 56), 32 204 / 159 (37 / 56), 64 377 / 164 (66 / 58);
+    // F32: 16 122 / 271 (21 / 58), 64 378 / 411 (72 / 84), 128 721 / 726 (136 / 170)
+    q->step = b->max_new <= (dtype == CCV3D_F32 ? 128 : 24);
     q->columns = dtype == CCV3D_BF16 || m->value_dim % 128 == 0 ? 128 : 64;
     q->seg = 0;
     q->items = q->fade_at = 0;

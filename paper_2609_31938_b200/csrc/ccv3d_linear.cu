@@ -9,7 +9,8 @@ namespace {
 // Tokens of a tile, and how its tiles fall to the pairs of SMs.
 struct LinearPlan {
     Device dev;
-    int BT, parts, kblocks, n_tiles, whole, tail, sharers, pairs;
+    bool few;                    // F32 without the tensor cores
+    int BT, kblocks, n_tiles, whole, tail, sharers, pairs;      // pairs: of SMs (few: blocks)
     int64_t t_tiles, pitch, x_at, w_at, part_at;      // F32: elements between rows of a split operand; bytes in the scratch
     uint64_t bytes;
 };
@@ -23,6 +24,10 @@ ccv3d_status check_linear(const ccv3d_linear_desc* d) {
     return CCV3D_OK;
 }
 
+// F32 rows that go without the tensor cores.  us, 4096 -> 9472, without / with them: 16 rows 59 / 146, 32 rows 96 / 145, 64 rows 175 / 149;
+// gated 16 rows 120 / 275.
+int few_rows(bool gated) { return gated ? 16 : 32; }
+
 // Microseconds of a K block of a tile with every pair of SMs at work (measured with one tile for each: the way from L2, at 12 to 14 TB/s,
 // bounds narrow tiles, so that one of 128 tokens takes as long as one of 16), and of a tile's end.
 double block_us(int BT, bool gated, bool f32) {
@@ -35,20 +40,20 @@ ccv3d_status plan_linear(const ccv3d_linear_desc* d, LinearPlan* q) {
     if (s != CCV3D_OK) return s;
     if ((s = current_device(&q->dev)) != CCV3D_OK) return s;
     const bool f32 = d->dtype == CCV3D_F32;
-    q->parts = f32 ? 3 : 1;
+    q->few = f32 && d->rows <= few_rows(d->gated);
     const int kb = f32 ? 32 : 64;
     q->kblocks = (d->k + kb - 1) / kb;
     q->n_tiles = (d->n_out + 255) / 256;
-    q->pairs = q->dev.sm_count / 2;
+    q->pairs = q->few ? (d->gated ? 1 : 2) * q->dev.sm_count : q->dev.sm_count / 2;
     // Tokens of a tile, and whether the tiles of the last, unfilled turn are cut along K: by the time that the call would take.  It is not under
     // that of the weights' bytes; cutting costs a launch, and the sums' way through memory.
     const double bytes_us = (double)d->n_out * (1 + d->gated) * d->k * esize(d->dtype) / 5.6e6;
     double best = 1e30;
-    for (const int BT : {16, 64, 128, 256}) {
-        if (BT == 256 && d->gated) continue;
+    for (const int BT : {16, 32, 64, 128, 256}) {
+        if (q->few ? BT > few_rows(d->gated) : BT == 32 || (BT == 256 && d->gated)) continue;
         const int64_t t_tiles = ((int64_t)d->rows + BT - 1) / BT, tiles = q->n_tiles * t_tiles, turns = tiles / q->pairs;
         if (tiles > 0x3FFFFFFF) continue;
-        const double tile_us = q->kblocks * block_us(BT, d->gated, f32), end_us = BT * (1 + d->gated) / 85.0;
+        const double tile_us = q->kblocks * (q->few ? (BT == 32 ? 1.5 : 1.0) : block_us(BT, d->gated, f32)), end_us = BT * (1 + d->gated) / 85.0;
         const int left = (int)(tiles % q->pairs);
         const auto longer = [](double a, double b) { return a > b ? a : b; };
         double us = longer((turns + (left > 0)) * tile_us, bytes_us) + end_us;
@@ -77,8 +82,9 @@ ccv3d_status plan_linear(const ccv3d_linear_desc* d, LinearPlan* q) {
     const auto up = [](int64_t n) { return (n + 255) / 256 * 256; };
     q->pitch = (d->k + 7LL) / 8 * 8;
     q->x_at = 0;
-    q->w_at = f32 ? up(3 * q->pitch * d->rows * 2) : 0;
-    q->part_at = q->w_at + (f32 ? up(3 * q->pitch * d->n_out * (1 + d->gated) * 2) : 0);
+    const bool split = f32 && !q->few;
+    q->w_at = split ? up(3 * q->pitch * d->rows * 2) : 0;
+    q->part_at = q->w_at + (split ? up(3 * q->pitch * d->n_out * (1 + d->gated) * 2) : 0);
     q->bytes = q->part_at + 2LL * q->sharers * q->BT * (1 + d->gated) * 256 * 4;
     return CCV3D_OK;
 }
@@ -92,6 +98,22 @@ ccv3d_status encode_rows(CUtensorMap* tm, const void* at, int size, int64_t rows
     const CUresult r = fn(tm, size == 2 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 2, const_cast<void*>(at), dims, strides, box, es,
                           CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
     return r == CUDA_SUCCESS ? CCV3D_OK : CCV3D_ERR_CUDA;
+}
+
+// The sums of tiles that were cut, launched so that it is resident when the kernel before it ends.
+template <typename TO, bool GATED>
+ccv3d_status launch_join(const LinearParams& p, int BT, cudaStream_t st) {
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[0].val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(p.tail, BT / LINEAR_JOIN_TOKENS);
+    cfg.blockDim = dim3(256);
+    cfg.stream = st;
+    cfg.attrs = at;
+    cfg.numAttrs = 1;
+    if (cudaLaunchKernelEx(&cfg, linear_join_kernel<TO, GATED>, p, BT) != cudaSuccess) { cudaGetLastError(); return CCV3D_ERR_CUDA; }
+    return CCV3D_OK;
 }
 
 template <typename S, typename TO>
@@ -118,13 +140,18 @@ ccv3d_status launch_linear_as(LinearParams& p, const LinearPlan& q, const void* 
     cfg.attrs = at;
     cfg.numAttrs = S::PARTS == 3 ? 1 : 0;            // behind the kernels that split the operands
     if (cudaLaunchKernelEx(&cfg, linear_tile_kernel<S, TO>, tw, tx, to, tr, p) != cudaSuccess) { cudaGetLastError(); return CCV3D_ERR_CUDA; }
-    if (!p.tail) return CCV3D_OK;
-    cfg.gridDim = dim3(p.tail, S::BT / LINEAR_JOIN_TOKENS);
-    cfg.blockDim = dim3(256);
-    cfg.dynamicSmemBytes = 0;
-    cfg.numAttrs = 1;
-    if (cudaLaunchKernelEx(&cfg, linear_join_kernel<TO, S::GATED>, p, S::BT) != cudaSuccess) { cudaGetLastError(); return CCV3D_ERR_CUDA; }
-    return CCV3D_OK;
+    return p.tail ? launch_join<TO, S::GATED>(p, S::BT, st) : CCV3D_OK;
+}
+
+template <bool GATED, int BT>
+ccv3d_status launch_few(LinearParams& p, const LinearPlan& q, const float* x, int64_t x_stride, const float* w, int64_t w_stride, int k, cudaStream_t st) {
+    constexpr int bytes = (LINEAR_FEW_STAGES * (GATED ? 2 : 1) * 256 + 2 * BT) * LINEAR_FEW_K * 4;
+    static std::atomic<uint64_t> done{0};
+    if (!allow_smem(linear_few_kernel<GATED, BT>, bytes, q.dev.index, done)) { cudaGetLastError(); return CCV3D_ERR_CUDA; }
+    const int used = p.tail ? p.pairs : (p.whole < p.pairs ? p.whole : p.pairs);
+    linear_few_kernel<GATED, BT><<<used, LINEAR_FEW_THREADS, bytes, st>>>(p, x, x_stride, w, w_stride, k);
+    const ccv3d_status s = launched();
+    return s == CCV3D_OK && p.tail ? launch_join<float, GATED>(p, BT, st) : s;
 }
 
 template <int PARTS, typename TO, typename... A>
@@ -209,6 +236,11 @@ ccv3d_status ccv3d_linear(const ccv3d_linear_desc* d, const void* x, const void*
     p.res_boxes = residual && !misaligned(residual, 16) && p.res_stride >= N && p.res_stride * eo % 16 == 0;
     p.status = status;
     p.wait_clk = q.dev.wait_clk;
+    if (q.few) {
+        const float *xf = (const float*)x, *wf = (const float*)w;
+        if (d->gated) return launch_few<true, 16>(p, q, xf, xs, wf, wst, d->k, st);
+        return q.BT == 16 ? launch_few<false, 16>(p, q, xf, xs, wf, wst, d->k, st) : launch_few<false, 32>(p, q, xf, xs, wf, wst, d->k, st);
+    }
     if (d->dtype == CCV3D_F32) {
         void *px = (char*)ws + q.x_at, *pw = (char*)ws + q.w_at;
         const int64_t blocks = ((NW + M) * (q.pitch / 4) + 255) / 256;

@@ -478,6 +478,126 @@ __global__ void __launch_bounds__(256) linear_join_kernel(const __grid_constant_
     linear_put<TO, LINEAR_JOIN_TOKENS>(p, n, t0, g);
 }
 
+// Few rows of F32: bound by the weights' bytes, which splitting them would double and double again; so in plain FP32 arithmetic.  A thread has
+// two features of a tile of 256 and BT tokens.  Weights come in by cp.async, K blocks of 32, in rows of 128 bytes whose 16-byte pieces are
+// swapped by row so that eight threads read eight banks' worth; tokens through registers, one block ahead.  Sums of 256 terms are added up
+// apart.
+constexpr int LINEAR_FEW_K = 32, LINEAR_FEW_FOLD = 8, LINEAR_FEW_THREADS = 128, LINEAR_FEW_STAGES = 3;
+template <bool GATED, int BT>
+__global__ void __launch_bounds__(LINEAR_FEW_THREADS) linear_few_kernel(const __grid_constant__ LinearParams p, const float* x, int64_t x_stride, const float* w,
+                                                                        int64_t w_stride, int k) {
+    constexpr int SETS = GATED ? 2 : 1, KB = LINEAR_FEW_K, COLS = SETS * BT, ROWS = SETS * 256, XQ = BT * (KB / 4) / LINEAR_FEW_THREADS, NST = LINEAR_FEW_STAGES;
+    extern __shared__ __align__(16) float few[];
+    float *ws = few, *xs = few + NST * ROWS * KB;                 // weights [stage][row][KB], tokens [2][k][BT]
+    asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+    const int t = threadIdx.x;
+    LinearWalk walk(p, blockIdx.x);
+    LinearPiece piece;
+    while (walk.get(piece)) {
+        const int n0 = piece.tile % p.n_tiles * 256, t0 = piece.tile / p.n_tiles * BT, blocks = piece.kb1 - piece.kb0;
+        float total[SETS][2][BT], sum[SETS][2][BT], xr[XQ][4];
+#pragma unroll
+        for (int h = 0; h < SETS; ++h)
+#pragma unroll
+            for (int j = 0; j < 2 * BT; ++j) total[h][j / BT][j % BT] = sum[h][j / BT][j % BT] = 0.f;
+        auto bring = [&](int i) {                                 // weights of the piece's i-th K block; what is not there is zero
+            if (i < blocks) {
+                const int k0 = (piece.kb0 + i) * KB, c = t & 7, left = max(0, min(16, (k - k0 - 4 * c) * 4));
+#pragma unroll 4
+                for (int r = t >> 3; r < ROWS; r += LINEAR_FEW_THREADS / 8) {
+                    const int f = r & 255, row = (r >> 8) * p.n_out + n0 + f;
+                    const int size = n0 + f < p.n_out ? left : 0;
+                    const uint32_t dst = smem_u32(ws + (i % NST * ROWS + r) * KB + ((c ^ (r & 7)) << 2));
+                    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(size ? w + row * w_stride + k0 + 4 * c : w), "r"(size) : "memory");
+                }
+            }
+            asm volatile("cp.async.commit_group;" ::: "memory");
+        };
+        auto tokens = [&](int i) {                                // of the i-th, into registers
+            const int k0 = (piece.kb0 + i) * KB;
+#pragma unroll
+            for (int e = 0; e < XQ; ++e) {
+                const int at = t + e * LINEAR_FEW_THREADS, r = at / (KB / 4), c = at % (KB / 4) * 4;
+                const float* from = x + (int64_t)(t0 + r) * x_stride + k0 + c;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) xr[e][j] = 0.f;
+                if (t0 + r < p.rows && i < blocks) {
+                    if (k0 + c + 4 <= k) load4(from, xr[e]);
+                    else {
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) if (k0 + c + j < k) xr[e][j] = from[j];
+                    }
+                }
+            }
+        };
+        __syncthreads();                                          // the last piece's stages have been read
+#pragma unroll
+        for (int i = 0; i < NST - 1; ++i) bring(i);
+        tokens(0);
+        for (int i = 0; i < blocks; ++i) {
+            asm volatile("cp.async.wait_group %0;" ::"n"(NST - 2) : "memory");
+            float* xb = xs + (i & 1) * KB * BT;
+#pragma unroll
+            for (int e = 0; e < XQ; ++e) {
+                const int at = t + e * LINEAR_FEW_THREADS, r = at / (KB / 4), c = at % (KB / 4) * 4;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) xb[(c + j) * BT + r] = xr[e][j];
+            }
+            __syncthreads();
+            bring(i + NST - 1);
+            tokens(i + 1);
+            const float* wb = ws + i % NST * ROWS * KB;
+#pragma unroll 2
+            for (int c = 0; c < KB; c += 4) {
+                float a[SETS][2][4];
+#pragma unroll
+                for (int h = 0; h < SETS; ++h)
+#pragma unroll
+                    for (int f = 0; f < 2; ++f) load4(wb + (h * 256 + f * 128 + t) * KB + (((c >> 2) ^ (t & 7)) << 2), a[h][f]);
+#pragma unroll
+                for (int kk = 0; kk < 4; ++kk)
+#pragma unroll
+                    for (int j = 0; j < BT; j += 4) {
+                        float v[4];
+                        load4(xb + (c + kk) * BT + j, v);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+#pragma unroll
+                            for (int h = 0; h < SETS; ++h)
+#pragma unroll
+                                for (int f = 0; f < 2; ++f) sum[h][f][j + e] = fmaf(a[h][f][kk], v[e], sum[h][f][j + e]);
+                    }
+            }
+            if (i % LINEAR_FEW_FOLD == LINEAR_FEW_FOLD - 1 || i + 1 == blocks) {
+#pragma unroll
+                for (int h = 0; h < SETS; ++h)
+#pragma unroll
+                    for (int j = 0; j < 2 * BT; ++j) { total[h][j / BT][j % BT] += sum[h][j / BT][j % BT]; sum[h][j / BT][j % BT] = 0.f; }
+            }
+        }
+#pragma unroll
+        for (int f = 0; f < 2; ++f) {
+            const int n = n0 + f * 128 + t;
+            if (piece.slot >= 0) {
+                float* at = p.part + (int64_t)piece.slot * COLS * 256 + f * 128 + t;
+#pragma unroll
+                for (int h = 0; h < SETS; ++h)
+#pragma unroll
+                    for (int j = 0; j < BT; ++j) at[(h * BT + j) * 256] = total[h][f][j];
+                continue;
+            }
+            float bg = 0.f, bu = 0.f;
+            if (p.bias && n < p.n_out) {
+                bg = bias_at(p, n);
+                if (GATED) bu = bias_at(p, p.n_out + n);
+            }
+            linear_epilogue<float, GATED, BT>(p, n, t0, total[0][f], total[SETS - 1][f], bg, bu);
+            linear_put<float, BT>(p, n, t0, total[0][f]);
+        }
+    }
+    asm volatile("cp.async.wait_all;" ::: "memory");
+}
+
 // F32 rows of both operands as three BF16 numbers each, in three planes [rows][pitch]: rounded to 8 bits, what is left to 8 more, and the
 // rest (8 bits: exact).  A thread to four elements.
 __global__ void __launch_bounds__(256) linear_split_kernel(const float* w, int64_t w_stride, int w_rows, __nv_bfloat16* w_to, const float* x, int64_t x_stride,

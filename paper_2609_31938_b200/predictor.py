@@ -16,7 +16,16 @@ fixed amount of memory, as the chain does with its frame rings.  Its rotation ta
 frames, pairs turn by whole numbers of turns in as many frames as a table has rows, so that a frame's row is its number
 modulo the rows and the angle between two frames is that of their distance wherever the stream stands.
 
-    python -m paper_2609_31938_b200.predictor [frames]
+``DecayPredictor`` is the same with a memory of fixed size, one state for each head that old frames fade from, in place of the
+cache, and with every product in the library:
+
+    per block   h = pre-norm of the residual, scaled and shifted for the frame                 gated_norm
+                q, k, v = h Wqkv, log decays from h Wg                                         linear
+                the frame's tokens into the states, read in their order                        DecayMemory.attend
+                residual += (norm of each head) Wo                                             group_norm, linear
+                h = pre-norm ...; residual += (silu(h W1) * (h W2)) W3                         gated_norm, linear (gated), linear
+
+    python -m paper_2609_31938_b200.predictor [frames] [cache | decay]
 """
 from __future__ import annotations
 
@@ -123,15 +132,71 @@ class LatentPredictor:
         return r.view(1, 1, self.h, self.w, self.c).permute(0, 4, 1, 2, 3).to(torch.bfloat16).contiguous()
 
 
-def main(frames=6):
-    from .chain import LAYERS, ResidentDecoderChain
+class DecayPredictor:
+    def __init__(self, channels=192, heads=6, key_dim=64, value_dim=64, blocks=2, height=44, width=80, seed=0, dtype=torch.bfloat16):
+        g = torch.Generator(device="cuda").manual_seed(seed)
+        rnd = lambda *s, a=1.0: torch.randn(s, generator=g, device="cuda") * a  # noqa: E731
+        self.c, self.heads, self.dk, self.dv = channels, heads, key_dim, value_dim
+        self.h, self.w, self.n, self.dtype = height, width, height * width, dtype
+        inner = 4 * channels
+        self.blocks = [dict(qkv=rnd(heads * (2 * key_dim + value_dim), channels, a=channels ** -0.5).to(dtype),
+                            decay=rnd(heads, channels, a=0.3 * channels ** -0.5).to(dtype),
+                            # heads that remember from a part of a frame to several frames
+                            rate=-torch.linspace(4.0, 11.0, heads, device="cuda").to(dtype),
+                            head=(1 + rnd(heads * value_dim, a=0.1), rnd(heads * value_dim, a=0.1)),
+                            out=rnd(channels, heads * value_dim, a=(heads * value_dim) ** -0.5).to(dtype),
+                            up=rnd(2 * inner, channels, a=channels ** -0.5).to(dtype), down=rnd(channels, inner, a=inner ** -0.5).to(dtype),
+                            w=[1 + rnd(channels, a=0.1) for _ in range(2)]) for _ in range(blocks)]
+        self.modulation = rnd(channels, blocks * 4 * channels, a=0.3 * channels ** -0.5)     # scale and shift of each half block
+        self.memories = [tk.DecayMemory.empty(1, heads, key_dim, value_dim) for _ in range(blocks)]
+        self._fresh = torch.ones(1, dtype=torch.int32, device="cuda")
+        self.batch = tk.StreamBatch(torch.tensor([0, self.n], dtype=torch.int32, device="cuda"), torch.zeros(1, dtype=torch.int32, device="cuda"),
+                                    self.n, fresh=self._fresh)
+        self.reset()
+
+    def reset(self):
+        """Forget the stream (the next frame is the first)."""
+        self._fresh.fill_(1)
+
+    def status(self):
+        """TOKENS_* bits that the kernels have reported, for each block's states and for the products, cleared by reading."""
+        return [m.status() for m in self.memories] + [tk.status()]
+
+    def step(self, x, condition):
+        """One frame: x [H * W, channels] and condition [channels] -> the predicted latent frame [H * W, channels] (float32)."""
+        n, c, hk, hv = self.n, self.c, self.heads * self.dk, self.heads * self.dv
+        mod = (condition.float() @ self.modulation).view(len(self.blocks), 2, 2, 1, c)
+        r = x.float().clone()
+        for i, (b, memory) in enumerate(zip(self.blocks, self.memories)):
+            _, h = tk.gated_norm(r, pre_weight=b["w"][0], scale=mod[i, 0, 0], shift=mod[i, 0, 1], act_dtype=self.dtype, want_r=False)
+            qkv = tk.linear(h, b["qkv"])
+            q, k, v = qkv[:, :hk].unflatten(1, (self.heads, self.dk)), qkv[:, hk:2 * hk].unflatten(1, (self.heads, self.dk)), qkv[:, 2 * hk:].unflatten(1, (self.heads, self.dv))
+            log_decay = -torch.nn.functional.softplus(tk.linear(h, b["decay"], b["rate"], out_dtype=torch.float32))
+            o = memory.attend(q, k, v, log_decay, self.batch)
+            o = tk.group_norm(o.view(n, 1, hv), self.heads, *b["head"])
+            r = tk.linear(o.view(n, hv), b["out"], residual=r, out=r)
+            _, h = tk.gated_norm(r, pre_weight=b["w"][1], scale=mod[i, 1, 0], shift=mod[i, 1, 1], act_dtype=self.dtype, want_r=False)
+            u = tk.linear(h, b["up"], activation="silu", gated=True)
+            r = tk.linear(u, b["down"], residual=r, out=r)
+        self._fresh.zero_()
+        return r
+
+    latent = LatentPredictor.latent
+
+
+def main(frames=6, memory="cache"):
+    from .chain import LAYERS, NormedDecoderChain, ResidentDecoderChain
     g = torch.Generator(device="cuda").manual_seed(1)
     ca, cb, cc = 192, 96, 96
     shapes = {"A1": (ca, ca, 3), "A2": (ca, ca, 3), "PA": (cb, ca, 1), "B1": (cb, cb, 3), "B2": (cb, cb, 3), "PB": (cc, cb, 1),
               "C1": (cc, cc, 3), "C2": (cc, cc, 3)}
     w = {k: (torch.randn((co, ci, n, n, n), generator=g, device="cuda") * (ci * n ** 3) ** -0.5).bfloat16() for k, (co, ci, n) in shapes.items()}
     b = {k: torch.zeros(w[k].shape[0], device="cuda").bfloat16() for k in LAYERS}
-    chain, model = ResidentDecoderChain(w, b), LatentPredictor(channels=ca)
+    if memory == "decay":
+        norms = {k: (torch.ones(shapes[k][1], device="cuda"), torch.zeros(shapes[k][1], device="cuda")) for k in LAYERS if k[0] != "P"}
+        chain, model = NormedDecoderChain(w, b, norms), DecayPredictor(channels=ca)
+    else:
+        chain, model = ResidentDecoderChain(w, b), LatentPredictor(channels=ca)
     start, end = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
     for f in range(frames):
         noise, condition = torch.randn(model.n, ca, generator=g, device="cuda"), torch.randn(ca, generator=g, device="cuda")
@@ -149,4 +214,4 @@ def main(frames=6):
 
 if __name__ == "__main__":
     import sys
-    main(int(sys.argv[1]) if len(sys.argv) > 1 else 6)
+    main(int(sys.argv[1]) if len(sys.argv) > 1 else 6, sys.argv[2] if len(sys.argv) > 2 else "cache")
