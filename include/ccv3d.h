@@ -559,9 +559,11 @@ typedef enum { CCV3D_ACT_NONE = 0, CCV3D_ACT_SILU = 1, CCV3D_ACT_GELU = 2, CCV3D
  * x [rows, k] and w [n_out, k] (gated: [2 n_out, k], the gate's rows first) in `dtype`, bias [n_out] (gated [2 n_out]) in `dtype` or NULL,
  * residual [rows, n_out] and out in out_dtype (F32 where dtype is F32), residual may be NULL or out itself (same strides).
  *   Rows of x and w are dense; their strides (in elements) and addresses are multiples of 16 bytes; out and residual go by elements.
- *   k, n_out, rows: any number from 1 on (rows = 0: a call without work), each below 2^31 - 2^16; k <= 2^20.
- * Products are exact, sums FP32 (rounded every few hundred terms; between, the tensor cores cut off bits below the last), everything
- * behind them FP32, the output is rounded once.  F32 operands go in as three BF16 numbers each (24 bits, exact), and products under 2^-24
+ *   k, n_out, rows: any number from 1 on (rows = 0: a call without work); k <= 65536, rows and n_out (gated: 2 n_out) below 2^31 - 2^16 - 256
+ *   (F32: a third of that).
+ * Products are exact, sums FP32: the tensor cores cut off what lies below a sum's last bit, 16 terms at a time, so that BF16 outputs lose up to
+ * k 2^-28 of their terms' magnitude; F32 outputs are summed with rounding every 1024 terms (F32 operands: 128).  All behind the sums is FP32, the
+ * output is rounded once.  F32 operands go in as three BF16 numbers each (24 bits, exact), and products under 2^-24
  * of the whole are left out (few rows: FP32 arithmetic).  F32: an infinity may make its outputs NaN, and numbers under 2^-110 lose bits.
  *   ws      DEVICE scratch, 256-byte aligned, ccv3d_linear_workspace() bytes, of the call alone (NULL where that is 0)
  *   status  DEVICE word or NULL: receives CCV3D_TOKENS_TIMEOUT

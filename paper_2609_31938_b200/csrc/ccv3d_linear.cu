@@ -20,7 +20,7 @@ ccv3d_status check_linear(const ccv3d_linear_desc* d) {
     if (!dtype_ok(d->dtype) || !dtype_ok(d->out_dtype) || (d->dtype == CCV3D_F32 && d->out_dtype != CCV3D_F32)) return CCV3D_ERR_INVALID_ARG;
     if (d->activation < CCV3D_ACT_NONE || d->activation > CCV3D_ACT_GELU_TANH) return CCV3D_ERR_INVALID_ARG;
     const int64_t most = 0x7FFF0000, parts = d->dtype == CCV3D_F32 ? 3 : 1;
-    if (d->k > (1 << 20) || parts * (d->rows + 256LL) > most || parts * (d->n_out * (1LL + d->gated) + 256) > most) return CCV3D_ERR_UNSUPPORTED;
+    if (d->k > (1 << 16) || parts * (d->rows + 256LL) > most || parts * (d->n_out * (1LL + d->gated) + 256) > most) return CCV3D_ERR_UNSUPPORTED;
     return CCV3D_OK;
 }
 

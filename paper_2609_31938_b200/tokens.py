@@ -613,7 +613,7 @@ class DecayMemory:
         else:
             co = _heads(out, "out", tokens, self.value_dim, dev)
         qk_heads = q.shape[1]
-        keep, ws, need = _scratch(("decay", dev, c.batch, tokens, c.max_new, heads, self.key_dim, self.value_dim),
+        keep, ws, need = _scratch(("decay", dev, c.batch, tokens, c.max_new, heads, self.key_dim, self.value_dim, dt),
                                   ccv3d_decay_attend_workspace, "ccv3d_decay_attend_workspace", self.c, c, qk_heads, dt)
         s = lib.ccv3d_decay_attend(self.c, c, cq, ck, cv, log_decay.data_ptr(), log_decay.stride(0), log_decay.stride(1), co, qk_heads,
                                    dt, self.key_dim ** -0.5 if scale is None else scale, ws, need, self._status_ptr, _stream(dev))

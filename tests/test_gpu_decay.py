@@ -192,6 +192,23 @@ def test_streams_and_graphs():
         assert torch.equal(out, want) and torch.equal(still.states, m.states)
 
 
+def test_types_in_turn_and_two_memories():
+    from paper_2609_31938_b200 import tokens as tk
+    cases = [Case([700, 20], 2, 2, 64, 64, t, seed=13) for t in (BF, F, BF, F)]
+    for c in cases:                                                       # (calls of one geometry and two types)
+        c.check(*c.run())
+    a, b = cases[0], cases[2]
+    streams, memories, outs = [torch.cuda.Stream() for _ in range(2)], [], []
+    for c, s in zip((a, b), streams):
+        s.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(s):
+            memories.append(tk.DecayMemory(c.states.clone()))
+            outs.append(memories[-1].attend(c.q, c.k, c.v, c.g, tk.StreamBatch(c.starts, c.slot, 700)))
+    torch.cuda.synchronize()
+    for c, m, o in zip((a, b), memories, outs):
+        c.check(o, m)
+
+
 def test_nothing_to_do():
     from paper_2609_31938_b200 import tokens as tk
     c = Case([0, 0], 2, 2, 64, 64, BF)

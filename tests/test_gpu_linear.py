@@ -72,6 +72,17 @@ def test_output_strides_and_in_place(dtype, out):
     assert torch.equal(wide[:, 3:48], want) and bool((wide[:, :3] == -3).all()) and bool((wide[:, 48:] == -3).all())
     again = r.clone()
     assert torch.equal(tk.linear(x, w, b, residual=again, out=again), want)
+    # residuals and outputs as boxes, by elements, and one of each: the same bits
+    for rows in (40, 600):
+        x, w, b, r = inputs(rows, 160, 96, dtype, False, out, seed=2)
+        want = tk.linear(x, w, b, residual=r, out_dtype=out, activation="silu")
+        close(want, x, w, b, "silu", False, r)
+        wide, off = (torch.zeros((rows, 177), device="cuda", dtype=out) for _ in range(2))
+        wide[:, 5:165] = r
+        for res in (r, wide[:, 5:165]):
+            for to in (torch.empty_like(r), off[:, 9:169]):
+                assert torch.equal(tk.linear(x, w, b, residual=res, out=to, activation="silu"), want)
+    x, w, b, r = inputs(70, 45, 96, dtype, False, out, seed=1)
     close(tk.linear(x, w, b, residual=r[:1].expand(70, -1), out_dtype=out), x, w, b, "none", False, r[:1].expand(70, -1))
     one = x[:1].expand(70, -1)
     if dtype == BF:                                              # (rows on one another: any stride)

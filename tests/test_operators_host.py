@@ -26,7 +26,7 @@ def linear(x=4 * K, w=8 * K, bias=None, res=None, out=16 * K, ws=None, n=0, stat
     (dict(rows=-1), ccv.ERR_INVALID_ARG), (dict(n_out=0), ccv.ERR_INVALID_ARG), (dict(k=0), ccv.ERR_INVALID_ARG), (dict(gated=2), ccv.ERR_INVALID_ARG),
     (dict(activation=4), ccv.ERR_INVALID_ARG), (dict(activation=-1), ccv.ERR_INVALID_ARG), (dict(dtype=2), ccv.ERR_INVALID_ARG),
     (dict(dtype=ccv.F32), ccv.ERR_INVALID_ARG),                                   # F32 into BF16
-    (dict(k=1 << 21), ccv.ERR_UNSUPPORTED), (dict(n_out=0x7FFFFFF0), ccv.ERR_UNSUPPORTED), (dict(rows=0x7FFFFFF0), ccv.ERR_UNSUPPORTED),
+    (dict(k=65544, x_stride=65544, w_stride=65544), ccv.ERR_UNSUPPORTED), (dict(n_out=0x7FFFFFF0), ccv.ERR_UNSUPPORTED), (dict(rows=0x7FFFFFF0), ccv.ERR_UNSUPPORTED),
     (dict(rows=800_000_000, dtype=ccv.F32, out_dtype=ccv.F32), ccv.ERR_UNSUPPORTED),
     (dict(x=None), ccv.ERR_INVALID_ARG), (dict(w=None), ccv.ERR_INVALID_ARG), (dict(out=None), ccv.ERR_INVALID_ARG),
     (dict(x_stride=56), ccv.ERR_INVALID_ARG), (dict(w_stride=8), ccv.ERR_INVALID_ARG), (dict(out_stride=31), ccv.ERR_INVALID_ARG),
