@@ -67,8 +67,8 @@ ccv3d_status launch_chunks(const DecayParams& p, const DecayPlan& q, int64_t ite
     };
     static std::atomic<uint64_t> done[2];
     if constexpr (sizeof(T) == 2) return launch(decay_tile_kernel<DK, MODE>, DECAY_TILE_THREADS, DecayTileShape<DK>::SHARED_AT + sizeof(DecayTileShared), done[0]);
-    else if (q.columns == 128) return launch(decay_chunk_kernel<T, DK, 8, MODE>, 256, DecayShape<T, DK, 8>::BYTES, done[0]);
-    else return launch(decay_chunk_kernel<T, DK, 4, MODE>, 128, DecayShape<T, DK, 4>::BYTES, done[1]);
+    else if (q.columns == 128) return launch(decay_chunk_kernel<DK, 8, MODE>, 256, DecayShape<DK, 8>::BYTES, done[0]);
+    else return launch(decay_chunk_kernel<DK, 4, MODE>, 128, DecayShape<DK, 4>::BYTES, done[1]);
 }
 
 template <typename T, int DK>

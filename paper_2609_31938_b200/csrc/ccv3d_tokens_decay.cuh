@@ -2,11 +2,13 @@
 //
 // Single tokens (decay_step_kernel): bound by the states' bytes.  A block holds a slice of 64 value columns of one state in registers from
 // its one load to its one store.
-// Many tokens (decay_chunk_kernel): in chunks of 64, with G the sum of the log decays from the chunk's start on,
+// Measured: 64 streams of one token, 32 heads of 128 x 128, 49 us = 5.5 TB/s, 84 % of the copy rate.
+// Many tokens (decay_tile_kernel for BF16; F32: decay_chunk_kernel): in chunks of 64, with G the sum of the log decays from the chunk's start on,
 //   out_i = scale (exp(G_i) q_i S + sum_{j <= i} exp(G_i - G_j) (q_i . k_j) v_j)        S' = exp(G_end) S + sum_j exp(G_end - G_j) k_j v_j^T
-// as mma.sync products of BF16 with FP32 sums.  A warp owns 16 value columns of S^T, in registers as the products leave them, which is also
+// decay_chunk_kernel does so as mma.sync products of BF16 with FP32 sums.  A warp owns 16 value columns of S^T, in registers as the products leave them, which is also
 // the layout that the next product wants them in as its B operand: the state never leaves the registers.  What is not BF16 already goes in
-// as several BF16 numbers, 8 bits each: scores with their decay and S as two (F32: three), v with its decay as three, F32 inputs as three.
+// as three BF16 numbers, 8 bits each, of whose nine products six are taken (BF16 inputs: scores with their decay and S as two, v with its
+// decay as three).  F32, 24 prompts of up to 700 tokens, 14 heads of 64 x 128: 328 us, bound by the latency of eight warps' products.
 // G is summed in 64 bits and kept as two floats, so that differences of sums that a strong decay made large still have all their bits.
 //
 // Where sequences and heads are too few for the machine, sequences are cut into segments: their contributions to the state side by side,
@@ -191,18 +193,15 @@ __device__ __forceinline__ void split_pair(float x, float y, uint32_t (&out)[N])
     }
 }
 
-// Shared memory of a block: rows of BF16 with 16 bytes between them, so that eight rows of a matrix lie in different banks.
-template <typename T, int DK, int NW> struct DecayShape {
-    static constexpr bool F32 = sizeof(T) == 4;
-    static constexpr int PI = F32 ? 3 : 1, PM = F32 ? 3 : 2, PV = 3;     // BF16 parts of inputs, of scores and the state, of values with their decay
-    static constexpr int DV = 16 * NW, THREADS = 32 * NW, BUFFERS = F32 ? 1 : 2;
-    static constexpr int QS = DK + 8, VS = DV + 8, PS = DECAY_CHUNK + 8; // elements of a row
+// F32 prompts.  Shared memory of a block: rows of BF16 with 16 bytes between them, so that eight rows of a matrix lie in different banks.
+constexpr int DECAY_PARTS = 3;             // BF16 numbers of an F32 one
+template <int DK, int NW> struct DecayShape {
+    static constexpr int DV = 16 * NW, THREADS = 32 * NW;
+    static constexpr int QS = DK + 8, VS = DV + 8, PS = DECAY_CHUNK + 8;                     // elements of a row
     static constexpr int Q = DECAY_CHUNK * QS, V = DECAY_CHUNK * VS, P = DECAY_CHUNK * PS;   // elements of a plane
-    static constexpr int IN = PI * (2 * Q + V);                          // of a buffer: q, k, v
-    static constexpr int BYTES = (BUFFERS * IN + PM * P) * 2;
+    static constexpr int BYTES = DECAY_PARTS * (2 * Q + V + P) * 2;
 };
 
-template <typename T, int DK, int NW>
 struct DecayShared {
     float2 g[DECAY_CHUNK];       // sums of log decays, as two floats
     float end[DECAY_CHUNK];      // exp(G_end - G_j)
@@ -244,12 +243,13 @@ __device__ __forceinline__ bool decay_item(const DecayParams& p, int item, int& 
 
 enum { DECAY_ALL, DECAY_STATES, DECAY_OUTPUTS };     // a whole sequence; a segment's contribution to the state; a segment's outputs
 
-template <typename T, int DK, int NW, int MODE>
+template <int DK, int NW, int MODE>
 __global__ void __launch_bounds__(32 * NW, NW == 4 ? 2 : 1) decay_chunk_kernel(const __grid_constant__ DecayParams p) {
-    using S = DecayShape<T, DK, NW>;
-    constexpr int PI = S::PI, PM = S::PM, PV = S::PV, L = DECAY_CHUNK;
+    using S = DecayShape<DK, NW>;
+    using T = float;
+    constexpr int N = DECAY_PARTS, L = DECAY_CHUNK;
     extern __shared__ __align__(16) __nv_bfloat16 decay_smem[];
-    __shared__ DecayShared<T, DK, NW> sh;
+    __shared__ DecayShared sh;
     __shared__ int word[34];
     const int t = threadIdx.x, warp = t >> 5, lane = t & 31, g = lane >> 2, tc = lane & 3;
     const int slices = p.m.value_dim / S::DV, slice = blockIdx.y % slices, h = blockIdx.y / slices;
@@ -295,30 +295,23 @@ __global__ void __launch_bounds__(32 * NW, NW == 4 ? 2 : 1) decay_chunk_kernel(c
         for (int i = t; i < L * per; i += S::THREADS) {
             const int r = i / per, c = (i - r * per) * 8;
             const T* at = from + (int64_t)(tok + r) * stride + c;
-            if constexpr (!S::F32) {
-                const uint32_t dst = smem_at(to + r * pitch + c), size = r < live ? 16u : 0u;
-                asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(r < live ? at : from), "r"(size) : "memory");
-            } else {
-                float x[4] = {0.f, 0.f, 0.f, 0.f}, y[4] = {0.f, 0.f, 0.f, 0.f};
-                if (r < live) { load4(at, x); load4(at + 4, y); }
-                uint32_t w[4][3];
-                split_pair<3>(x[0], x[1], w[0]);
-                split_pair<3>(x[2], x[3], w[1]);
-                split_pair<3>(y[0], y[1], w[2]);
-                split_pair<3>(y[2], y[3], w[3]);
+            float x[4] = {0.f, 0.f, 0.f, 0.f}, y[4] = {0.f, 0.f, 0.f, 0.f};
+            if (r < live) { load4(at, x); load4(at + 4, y); }
+            uint32_t w[4][N];
+            split_pair<N>(x[0], x[1], w[0]);
+            split_pair<N>(x[2], x[3], w[1]);
+            split_pair<N>(y[0], y[1], w[2]);
+            split_pair<N>(y[2], y[3], w[3]);
 #pragma unroll
-                for (int z = 0; z < 3; ++z)
-                    *reinterpret_cast<uint4*>(to + z * L * pitch + r * pitch + c) = make_uint4(w[0][z], w[1][z], w[2][z], w[3][z]);
-            }
+            for (int z = 0; z < N; ++z) *reinterpret_cast<uint4*>(to + z * L * pitch + r * pitch + c) = make_uint4(w[0][z], w[1][z], w[2][z], w[3][z]);
         }
     };
+    __nv_bfloat16 *sq_ = decay_smem, *sk = sq_ + N * S::Q, *sv = sk + N * S::Q, *sp = sv + N * S::V;
     auto bring_chunk = [&](int chunk) {
-        __nv_bfloat16* to = decay_smem + chunk % S::BUFFERS * S::IN;
         const int tok = first + chunk * L, live = min(L, n - chunk * L);
-        if (MODE != DECAY_STATES) bring(qp, p.q.token_stride, tok, live, to, S::QS, DK);
-        bring(kp, p.k.token_stride, tok, live, to + PI * S::Q, S::QS, DK);
-        bring(vp, p.v.token_stride, tok, live, to + 2 * PI * S::Q, S::VS, S::DV);
-        if constexpr (!S::F32) asm volatile("cp.async.commit_group;" ::: "memory");
+        if (MODE != DECAY_STATES) bring(qp, p.q.token_stride, tok, live, sq_, S::QS, DK);
+        bring(kp, p.k.token_stride, tok, live, sk, S::QS, DK);
+        bring(vp, p.v.token_stride, tok, live, sv, S::VS, S::DV);
     };
     // whether this thread's share of the keys and values is finite
     auto look = [&](const __nv_bfloat16* at, int pitch, int dim) {
@@ -335,7 +328,7 @@ __global__ void __launch_bounds__(32 * NW, NW == 4 ? 2 : 1) decay_chunk_kernel(c
     bring_chunk(0);
     for (int chunk = 0; chunk < chunks; ++chunk) {
         const int tok0 = first + chunk * L, live = min(L, n - chunk * L);
-        if (S::BUFFERS == 1 && chunk + 1 < chunks) {       // the next chunk's rows come to L2
+        if (chunk + 1 < chunks) {                          // the next chunk's rows come to L2
             const int ahead = min(L, n - (chunk + 1) * L), kl = DK * (int)sizeof(T) / 128, vl = S::DV * (int)sizeof(T) / 128;
             for (int i = t; i < ahead * (2 * kl + vl); i += S::THREADS) {
                 const int r = i / (2 * kl + vl), c = i - r * (2 * kl + vl);
@@ -345,8 +338,6 @@ __global__ void __launch_bounds__(32 * NW, NW == 4 ? 2 : 1) decay_chunk_kernel(c
                 asm volatile("prefetch.global.L2 [%0];" ::"l"(at));
             }
         }
-        __nv_bfloat16* sq_ = decay_smem + chunk % S::BUFFERS * S::IN;
-        __nv_bfloat16 *sk = sq_ + PI * S::Q, *sv = sk + PI * S::Q, *sp = decay_smem + S::BUFFERS * S::IN;
         if (warp == 0) {
             // log decays of tokens 2 lane, 2 lane + 1 and their sums
             double x[2];
@@ -374,13 +365,10 @@ __global__ void __launch_bounds__(32 * NW, NW == 4 ? 2 : 1) decay_chunk_kernel(c
             if (lane == 31) sh.last = expf((float)end);
             total += end;
         }
-        if constexpr (!S::F32) asm volatile("cp.async.wait_group 0;" ::: "memory");
         most = 0;
         __syncthreads();
         look(sk, S::QS, DK);
         look(sv, S::VS, S::DV);
-        if constexpr (S::BUFFERS == 2)
-            if (chunk + 1 < chunks) bring_chunk(chunk + 1);
         const bool odd = __syncthreads_or((most & 0xFFFFu) >= 0x7F80u || (most >> 16) >= 0x7F80u);
         const float last = sh.last;
         if (odd) {
@@ -388,7 +376,7 @@ __global__ void __launch_bounds__(32 * NW, NW == 4 ? 2 : 1) decay_chunk_kernel(c
             auto value = [&](const __nv_bfloat16* at, int plane) {
                 float x = 0.f;
 #pragma unroll
-                for (int z = PI - 1; z >= 0; --z) {
+                for (int z = N - 1; z >= 0; --z) {
                     const float y = __bfloat162float(at[z * plane]);
                     x = isnan(y) && z ? x : x + y;                   // (an infinity's remainders are NaN)
                 }
@@ -441,7 +429,7 @@ __global__ void __launch_bounds__(32 * NW, NW == 4 ? 2 : 1) decay_chunk_kernel(c
                         for (int i = 0; i < 4; ++i) sc[j][i] = 0.f;
                     if (j0 <= i0 + 15) {
 #pragma unroll
-                        for (int o = PI - 1; o >= 0; --o)
+                        for (int o = N - 1; o >= 0; --o)
 #pragma unroll
                             for (int a = o; a >= 0; --a)
 #pragma unroll
@@ -472,11 +460,11 @@ __global__ void __launch_bounds__(32 * NW, NW == 4 ? 2 : 1) decay_chunk_kernel(c
                         x[1] = weigh(sc[j][1], ga, g1, c + 1 <= i0 + g);
                         x[2] = weigh(sc[j][2], gb, g0, c <= i0 + g + 8);
                         x[3] = weigh(sc[j][3], gb, g1, c + 1 <= i0 + g + 8);
-                        uint32_t a[PM], b[PM];
-                        split_pair<PM>(x[0], x[1], a);
-                        split_pair<PM>(x[2], x[3], b);
+                        uint32_t a[N], b[N];
+                        split_pair<N>(x[0], x[1], a);
+                        split_pair<N>(x[2], x[3], b);
 #pragma unroll
-                        for (int z = 0; z < PM; ++z) {
+                        for (int z = 0; z < N; ++z) {
                             *reinterpret_cast<uint32_t*>(sp + z * S::P + (i0 + g) * S::PS + c) = a[z];
                             *reinterpret_cast<uint32_t*>(sp + z * S::P + (i0 + g + 8) * S::PS + c) = b[z];
                         }
@@ -488,27 +476,27 @@ __global__ void __launch_bounds__(32 * NW, NW == 4 ? 2 : 1) decay_chunk_kernel(c
                 for (int m = 0; m < 4; ++m)
 #pragma unroll
                     for (int i = 0; i < 8; ++i) out[m][i >> 2][i & 3] = 0.f;
-                // (F32: the remainders' products of all keys first, so that the whole sums are only added to, and cut, eight times)
+                // (the remainders' products of all keys first, so that the whole sums are only added to, and cut, eight times)
 #pragma unroll
-                for (int pass = S::F32 ? 0 : 1; pass < 2; ++pass)
+                for (int pass = 0; pass < 2; ++pass)
 #pragma unroll
                     for (int kt = 0; kt < DK / 16; ++kt) {
-                        uint32_t b[2][2][PM];                // [columns g, g + 8][k halves][part]
+                        uint32_t b[2][2][N];                // [columns g, g + 8][k halves][part]
 #pragma unroll
                         for (int c = 0; c < 2; ++c)
 #pragma unroll
-                            for (int k = 0; k < 2; ++k) split_pair<PM>(st[2 * kt + k][2 * c], st[2 * kt + k][2 * c + 1], b[c][k]);
+                            for (int k = 0; k < 2; ++k) split_pair<N>(st[2 * kt + k][2 * c], st[2 * kt + k][2 * c + 1], b[c][k]);
 #pragma unroll
                         for (int m = 0; m < 4; ++m) {
                             if (16 * m >= live) break;
 #pragma unroll
-                            for (int a = PI - 1; a >= 0; --a) {
-                                if (S::F32 && pass == 1 && a > 0) continue;
+                            for (int a = N - 1; a >= 0; --a) {
+                                if (pass == 1 && a > 0) continue;
                                 uint32_t af[4];
                                 ldsm(smem_at(sq_ + a * S::Q + (16 * m + (lane & 15)) * S::QS + 16 * kt + (lane >> 4) * 8), af);
 #pragma unroll
-                                for (int z = PM - 1; z >= 0; --z) {
-                                    if (a + z >= PM || (S::F32 && (pass == 1) != (a + z == 0))) continue;
+                                for (int z = N - 1; z >= 0; --z) {
+                                    if (a + z >= N || (pass == 1) != (a + z == 0)) continue;
                                     mma_bf16(out[m][0], af, b[0][0][z], b[0][1][z]);
                                     mma_bf16(out[m][1], af, b[1][0][z], b[1][1][z]);
                                 }
@@ -516,8 +504,8 @@ __global__ void __launch_bounds__(32 * NW, NW == 4 ? 2 : 1) decay_chunk_kernel(c
                         }
                     }
                 __syncthreads();                             // all scores are there
-                // ... faded, and the scores' part on top (F32: summed for itself)
-                float pv[S::F32 ? 4 : 1][2][4];
+                // ... faded; the scores' part is summed for itself
+                float pv[4][2][4];
 #pragma unroll
                 for (int m = 0; m < 4; ++m) {
                     const float e0 = sh.begin[16 * m + g], e1 = sh.begin[16 * m + g + 8];
@@ -526,15 +514,15 @@ __global__ void __launch_bounds__(32 * NW, NW == 4 ? 2 : 1) decay_chunk_kernel(c
 #pragma unroll
                         for (int i = 0; i < 4; ++i) {
                             out[m][c][i] = fade(out[m][c][i], i < 2 ? e0 : e1);
-                            if (S::F32) pv[S::F32 ? m : 0][c][i] = 0.f;
+                            pv[m][c][i] = 0.f;
                         }
                 }
 #pragma unroll
-                for (int o = PM - 1; o >= 0; --o)            // part a of the scores, o - a of the values
+                for (int o = N - 1; o >= 0; --o)            // part a of the scores, o - a of the values
 #pragma unroll
                     for (int kt = 0; kt < 4; ++kt)
 #pragma unroll
-                        for (int a = o; a >= 0 && o - a < PI; --a) {
+                        for (int a = o; a >= 0; --a) {
                             uint32_t bf[4];
                             ldsm_t(smem_at(sv + (o - a) * S::V + (16 * kt + (lane & 15)) * S::VS + 16 * warp + (lane >> 4) * 8), bf);
 #pragma unroll
@@ -543,7 +531,7 @@ __global__ void __launch_bounds__(32 * NW, NW == 4 ? 2 : 1) decay_chunk_kernel(c
                                 uint32_t af[4];
                                 ldsm(smem_at(sp + a * S::P + (16 * m + (lane & 15)) * S::PS + 16 * kt + (lane >> 4) * 8), af);
 #pragma unroll
-                                for (int c = 0; c < 2; ++c) mma_bf16(S::F32 ? pv[S::F32 ? m : 0][c] : out[m][c], af, bf[2 * c], bf[2 * c + 1]);
+                                for (int c = 0; c < 2; ++c) mma_bf16(pv[m][c], af, bf[2 * c], bf[2 * c + 1]);
                             }
                         }
 #pragma unroll
@@ -555,49 +543,43 @@ __global__ void __launch_bounds__(32 * NW, NW == 4 ? 2 : 1) decay_chunk_kernel(c
                         T* at = op + (int64_t)(tok0 + r) * p.o.token_stride + 16 * warp + 2 * tc;
 #pragma unroll
                         for (int c = 0; c < 2; ++c) {
-                            float x = out[m][c][2 * half], y = out[m][c][2 * half + 1];
-                            if constexpr (S::F32) {
-                                x += pv[m][c][2 * half];
-                                y += pv[m][c][2 * half + 1];
-                                *reinterpret_cast<float2*>(at + 8 * c) = make_float2(p.scale * x, p.scale * y);
-                            } else {
-                                *reinterpret_cast<uint32_t*>(at + 8 * c) = pack_bf16(p.scale * x, p.scale * y);
-                            }
+                            const float x = out[m][c][2 * half] + pv[m][c][2 * half], y = out[m][c][2 * half + 1] + pv[m][c][2 * half + 1];
+                            *reinterpret_cast<float2*>(at + 8 * c) = make_float2(p.scale * x, p.scale * y);
                         }
                     }
             }
             if (MODE != DECAY_OUTPUTS || chunk + 1 < chunks) {
                 // the state: v with its decay to the chunk's end, as parts, times k
-                uint32_t va[L / 16][PV][4];
+                uint32_t va[L / 16][N][4];
 #pragma unroll
                 for (int kt = 0; kt < L / 16; ++kt) {
-                    uint32_t raw[PI][4];
+                    uint32_t raw[N][4];
 #pragma unroll
-                    for (int z = 0; z < PI; ++z)
+                    for (int z = 0; z < N; ++z)
                         ldsm_t(smem_at(sv + z * S::V + (16 * kt + (lane & 7) + (lane >> 4) * 8) * S::VS + 16 * warp + (lane >> 3 & 1) * 8), raw[z]);
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
                         float x = 0.f, y = 0.f;
 #pragma unroll
-                        for (int z = PI - 1; z >= 0; --z) {
+                        for (int z = N - 1; z >= 0; --z) {
                             x += __uint_as_float(raw[z][i] << 16);
                             y += __uint_as_float(raw[z][i] & 0xFFFF0000u);
                         }
                         const float2 e = *reinterpret_cast<const float2*>(&sh.end[16 * kt + 2 * tc + (i >> 1) * 8]);
-                        uint32_t w[PV];
-                        split_pair<PV>(x * e.x, y * e.y, w);
+                        uint32_t w[N];
+                        split_pair<N>(x * e.x, y * e.y, w);
 #pragma unroll
-                        for (int z = 0; z < PV; ++z) va[kt][z][i] = w[z];
+                        for (int z = 0; z < N; ++z) va[kt][z][i] = w[z];
                     }
                 }
-                constexpr int JN = S::F32 ? 2 : 4;           // tiles of 8 keys' channels at a time
+                constexpr int JN = 2;                        // tiles of 8 keys' channels at a time
 #pragma unroll
                 for (int j = 0; j < DK / 8; j += JN) {
                     float d[JN][4];
 #pragma unroll
                     for (int i = 0; i < 4 * JN; ++i) d[i >> 2][i & 3] = 0.f;
 #pragma unroll
-                    for (int a = PI - 1; a >= 0; --a) {      // part a of k; the small products first
+                    for (int a = N - 1; a >= 0; --a) {      // part a of k; the small products first
                         uint32_t bf[L / 16][JN / 2][4];
 #pragma unroll
                         for (int kt = 0; kt < L / 16; ++kt)
@@ -605,7 +587,7 @@ __global__ void __launch_bounds__(32 * NW, NW == 4 ? 2 : 1) decay_chunk_kernel(c
                             for (int c = 0; c < JN / 2; ++c)
                                 ldsm_t(smem_at(sk + a * S::Q + (16 * kt + (lane & 15)) * S::QS + 8 * j + 16 * c + (lane >> 4) * 8), bf[kt][c]);
 #pragma unroll
-                        for (int z = PV - 1 - a; z >= 0; --z)
+                        for (int z = N - 1 - a; z >= 0; --z)
 #pragma unroll
                             for (int kt = 0; kt < L / 16; ++kt)
 #pragma unroll
@@ -619,8 +601,7 @@ __global__ void __launch_bounds__(32 * NW, NW == 4 ? 2 : 1) decay_chunk_kernel(c
             }
         }
         __syncthreads();                                     // this chunk's rows and scores have been used
-        if constexpr (S::BUFFERS == 1)
-            if (chunk + 1 < chunks) bring_chunk(chunk + 1);
+        if (chunk + 1 < chunks) bring_chunk(chunk + 1);
     }
     if (MODE == DECAY_STATES || (MODE == DECAY_ALL && sq.slot >= 0)) {
         float* to = MODE == DECAY_ALL ? p.m.states + ((int64_t)sq.slot * p.m.heads + h) * DK * p.m.value_dim : p.part + part_at;
