@@ -548,7 +548,8 @@ ccv3d_status ccv3d_gated_norm(const ccv3d_norm_desc* d, const void* x, const voi
  * Products, decaying states and group norms: a latent predictor with a memory of fixed size, a decoder with normed blocks
  * ------------------------------------------------------------------------------------------------
  * What goes on in the epilogue of a product or norm.  NONE: v; SILU: v / (1 + exp(-v)); GELU: v Phi(v) (by erf); GELU_TANH: its
- * tanh form, v / (1 + exp(-2 u)), u = sqrt(2 / pi) (v + 0.044715 v^3).
+ * tanh form, v / (1 + exp(-2 u)), u = sqrt(2 / pi) (v + 0.044715 v^3).  With BF16 outputs, SILU and GELU_TANH are good to 2^-20, and what is
+ * under 2^-53 may come out as zero.  Minus infinity becomes NaN, as in the formulas.
  */
 typedef enum { CCV3D_ACT_NONE = 0, CCV3D_ACT_SILU = 1, CCV3D_ACT_GELU = 2, CCV3D_ACT_GELU_TANH = 3 } ccv3d_activation;
 

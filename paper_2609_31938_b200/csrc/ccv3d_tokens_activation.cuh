@@ -25,9 +25,10 @@ __device__ __forceinline__ float activate(float x, int kind) {
     return x;
 }
 
-// The same for N values.  Without EXACT, quotients of two values share one reciprocal, 1 / a = b / (a b): the unit that makes 2^x and 1 / x
-// takes a sixteenth of a multiprocessor's lanes, and bounds epilogues that do little else.  (2^x is cut at 2^60, so that a b stays finite:
-// what is left of x below -41 is under 2^-53.)
+// The same for N neighbouring values.  Without EXACT, quotients of two values share one reciprocal, 1 / a = b / (a b): the unit that makes 2^x
+// and 1 / x takes a sixteenth of a multiprocessor's lanes, and bounds epilogues that do little else.  2^x is cut at 2^60, so that a b stays finite;
+// 2^-59 is taken off the quotient, below zero nothing is left, so that a value whose exponent was cut is multiplied by zero (minus infinity becomes
+// NaN, as in the formula).  That costs no instruction, and |x| 2^-59 with |x| < 42 where it is more than the value's rounding: less than 2^-53.
 template <bool EXACT, int KIND, int N>
 __device__ __forceinline__ void activate_all(float (&v)[N]) {
     if constexpr (EXACT || N % 2 || (KIND != CCV3D_ACT_SILU && KIND != CCV3D_ACT_GELU_TANH)) {
@@ -45,8 +46,8 @@ __device__ __forceinline__ void activate_all(float (&v)[N]) {
                 d[j] += 1.f;
             }
             asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(d[0] * d[1]));
-            v[i] *= r * d[1];
-            v[i + 1] *= r * d[0];
+            v[i] *= __saturatef(fmaf(r, d[1], -0x1p-59f));
+            v[i + 1] *= __saturatef(fmaf(r, d[0], -0x1p-59f));
         }
     }
 }
