@@ -569,7 +569,8 @@ typedef enum { CCV3D_ACT_NONE = 0, CCV3D_ACT_SILU = 1, CCV3D_ACT_GELU = 2, CCV3D
  *   ws      DEVICE scratch, 256-byte aligned, ccv3d_linear_workspace() bytes, of the call alone (NULL where that is 0)
  *   status  DEVICE word or NULL: receives CCV3D_TOKENS_TIMEOUT
  * Any other overlap of out or ws with another tensor is CCV3D_ERR_ALIAS.  Results do not depend on what else runs, the same call gives
- * the same bits; how rows are grouped in calls may change last bits.  Stream-ordered, no allocation, legal in a stream capture.
+ * the same bits; a row has the same whatever the other rows hold, how rows are grouped in calls may change last bits.  Stream-ordered, no
+ * allocation, legal in a stream capture.
  */
 typedef struct {
     int32_t rows, n_out, k;

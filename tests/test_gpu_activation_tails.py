@@ -58,3 +58,16 @@ def test_group_norms(off, pixels, kind, dtype):
     for shift in (None, bias.expand(2, -1).contiguous()):
         y = tk.group_norm(x, 2, weight, bias if shift is None else None, shift=shift, activation=kind)
         close(y.flatten(0, 1)[::997], bias, kind)
+
+
+@pytest.mark.parametrize("kind", ["silu", "gelu_tanh"])
+@pytest.mark.parametrize("gated", [False, True])
+def test_a_row_has_the_same_bits_beside_other_contents(gated, kind):
+    from paper_2609_31938_b200 import tokens as tk
+    g = torch.Generator(device="cuda").manual_seed(1)
+    r = lambda *s: torch.randn(s, generator=g, device="cuda").to(BF)  # noqa: E731
+    for rows in (16, 1000):
+        w, x = r(3000 * (1 + gated), 64) * 0.25, r(rows, 64)
+        y = tk.linear(x, w, activation=kind, gated=gated)
+        x[1::2] = r(rows // 2, 64)
+        assert torch.equal(tk.linear(x, w, activation=kind, gated=gated)[::2], y[::2])
