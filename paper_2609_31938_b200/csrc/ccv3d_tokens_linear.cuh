@@ -320,6 +320,9 @@ linear_tile_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_consta
             };
             if (p.res && w.slot < 0) {
                 if (p.res_boxes) {
+                    // all lanes have read the last tile's residual from the boxes, and its outputs have left them
+                    fence_async_smem();
+                    __syncwarp();
                     if (lane == 0) bulk_wait_read<0>();
                     ask(0, turn);
                     if (S::CW > S::CH) ask(S::CH, turn ^ 1);
