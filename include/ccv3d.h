@@ -567,7 +567,7 @@ typedef enum { CCV3D_ACT_NONE = 0, CCV3D_ACT_SILU = 1, CCV3D_ACT_GELU = 2, CCV3D
  * output is rounded once.  F32 operands go in as three BF16 numbers each (24 bits, exact), and products under 2^-24
  * of the whole are left out (few rows: FP32 arithmetic).  F32: an infinity may make its outputs NaN, and numbers under 2^-110 lose bits.
  *   ws      DEVICE scratch, 256-byte aligned, ccv3d_linear_workspace() bytes, of the call alone (NULL where that is 0)
- *   status  DEVICE word or NULL: receives CCV3D_TOKENS_TIMEOUT
+ *   status  DEVICE word or NULL: receives CCV3D_TOKENS_TIMEOUT; ccv3d_linear_status_word() has one to lend
  * Any other overlap of out or ws with another tensor is CCV3D_ERR_ALIAS.  Results do not depend on what else runs, the same call gives
  * the same bits; a row has the same whatever the other rows hold, how rows are grouped in calls may change last bits.  Stream-ordered, no
  * allocation, legal in a stream capture.
@@ -582,6 +582,11 @@ typedef struct {
 } ccv3d_linear_desc;
 ccv3d_status ccv3d_linear(const ccv3d_linear_desc* d, const void* x, const void* w, const void* bias, const void* residual,
                           void* out, void* ws, uint64_t ws_bytes, uint32_t* status, void* stream);
+/* A DEVICE word of the library for such reports, one for each device, zero at first, there as long as the process (address: HOST output).  May be
+ * asked for inside a stream capture. */
+ccv3d_status ccv3d_linear_status_word(uint32_t** word_host);
+/* Waits for the current device, reads a status word of it (HOST output) and clears it. */
+ccv3d_status ccv3d_take_status(uint32_t* status, uint32_t* bits_host);
 /* Bytes of scratch that such a call needs on the current device (HOST output). */
 ccv3d_status ccv3d_linear_workspace(const ccv3d_linear_desc* d, uint64_t* bytes_host);
 

@@ -127,7 +127,7 @@ EXPORTS = ("ccv3d_create", "ccv3d_forward", "ccv3d_forward_host", "ccv3d_workspa
            "ccv3d_forward_ring", "ccv3d_out_dims", "ccv3d_forward_ring_up", "ccv3d_rows_copy",
            "ccv3d_forward_host_stream", "ccv3d_set_workspace",
            "ccv3d_kv_append", "ccv3d_kv_attend", "ccv3d_kv_attend_workspace", "ccv3d_gated_norm",
-           "ccv3d_linear", "ccv3d_linear_workspace", "ccv3d_decay_attend", "ccv3d_decay_attend_workspace", "ccv3d_group_norm",
+           "ccv3d_linear", "ccv3d_linear_workspace", "ccv3d_linear_status_word", "ccv3d_take_status", "ccv3d_decay_attend", "ccv3d_decay_attend_workspace", "ccv3d_group_norm",
            "ccv3d_group_norm_workspace", "ccv3d_group_norm_ring", "ccv3d_group_norm_ring_workspace")
 
 
@@ -177,6 +177,8 @@ def _load() -> ctypes.CDLL:
     lp, dp, sp, gp = (ctypes.POINTER(c) for c in (LinearDesc, DecayMemoryC, StreamBatchC, GroupNormDesc))
     lib.ccv3d_linear.argtypes = [lp, vp, vp, vp, vp, vp, vp, u64, vp, vp]
     lib.ccv3d_linear_workspace.argtypes = [lp, u64p]
+    lib.ccv3d_linear_status_word.argtypes = [ctypes.POINTER(vp)]
+    lib.ccv3d_take_status.argtypes = [vp, ctypes.POINTER(ctypes.c_uint32)]
     lib.ccv3d_decay_attend.argtypes = [dp, sp, hp, hp, hp, vp, i64, i64, hp, i32, i32, f32, vp, u64, vp, vp]
     lib.ccv3d_decay_attend_workspace.argtypes = [dp, sp, i32, i32, u64p]
     lib.ccv3d_group_norm.argtypes = [gp, vp, vp, vp, vp, vp, vp, vp, u64, vp]
@@ -377,6 +379,20 @@ def ccv3d_linear_workspace(desc: LinearDesc):
     """(status, bytes of scratch a ccv3d_linear call of this shape needs)."""
     b = ctypes.c_uint64()
     s = lib.ccv3d_linear_workspace(desc, b)
+    return s, b.value
+
+
+def ccv3d_linear_status_word():
+    """(status, address of the current device's word for reports of products)."""
+    w = ctypes.c_void_p()
+    s = lib.ccv3d_linear_status_word(w)
+    return s, w.value
+
+
+def ccv3d_take_status(word):
+    """(status, bits): waits for the current device, reads one of its status words and clears it."""
+    b = ctypes.c_uint32()
+    s = lib.ccv3d_take_status(word, b)
     return s, b.value
 
 

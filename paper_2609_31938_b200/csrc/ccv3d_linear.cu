@@ -6,6 +6,8 @@ using namespace ccv3d;
 
 namespace {
 
+__device__ uint32_t linear_status_word;      // (lent to calls that have none of their own)
+
 // Tokens of a tile, and how its tiles fall to the pairs of SMs.
 struct LinearPlan {
     Device dev;
@@ -171,6 +173,33 @@ ccv3d_status launch_linear(bool gated, int BT, A&&... a) {
 }  // namespace
 
 extern "C" {
+
+ccv3d_status ccv3d_linear_status_word(uint32_t** word_host) {
+    if (!word_host) return CCV3D_ERR_INVALID_ARG;
+    Device dev;
+    const ccv3d_status s = current_device(&dev);
+    if (s != CCV3D_OK) return s;
+    // (the first asking may load the code, which a capture of this thread would not allow)
+    cudaStreamCaptureMode mode = cudaStreamCaptureModeRelaxed;
+    void* at = nullptr;
+    if (cudaThreadExchangeStreamCaptureMode(&mode) != cudaSuccess) { cudaGetLastError(); return CCV3D_ERR_CUDA; }
+    const bool found = cudaGetSymbolAddress(&at, linear_status_word) == cudaSuccess;
+    if (!found) cudaGetLastError();
+    if (cudaThreadExchangeStreamCaptureMode(&mode) != cudaSuccess || !found) { cudaGetLastError(); return CCV3D_ERR_CUDA; }
+    *word_host = (uint32_t*)at;
+    return CCV3D_OK;
+}
+
+ccv3d_status ccv3d_take_status(uint32_t* status, uint32_t* bits_host) {
+    if (!status || !bits_host) return CCV3D_ERR_INVALID_ARG;
+    if (misaligned(status, 4)) return CCV3D_ERR_ALIGNMENT;
+    uint32_t bits = 0;
+    bool ok = cudaDeviceSynchronize() == cudaSuccess && cudaMemcpy(&bits, status, 4, cudaMemcpyDeviceToHost) == cudaSuccess;
+    if (ok && bits) ok = cudaMemset(status, 0, 4) == cudaSuccess && cudaDeviceSynchronize() == cudaSuccess;
+    if (!ok) { cudaGetLastError(); return CCV3D_ERR_CUDA; }
+    *bits_host = bits;
+    return CCV3D_OK;
+}
 
 ccv3d_status ccv3d_linear_workspace(const ccv3d_linear_desc* d, uint64_t* bytes_host) {
     if (!bytes_host) return CCV3D_ERR_INVALID_ARG;

@@ -13,7 +13,7 @@ import torch
 
 from . import (ACTIVATIONS, BF16, F32, NORM_LAYER, NORM_NONE, NORM_RMS, OK, Ccv3dError, DecayMemoryC, GroupNormDesc, Heads, KvCache,
                LinearDesc, NormDesc, RotaryC, StreamBatchC, TokenBatchC, ccv3d_decay_attend_workspace, ccv3d_group_norm_ring_workspace,
-               ccv3d_group_norm_workspace, ccv3d_kv_attend_workspace, ccv3d_linear_workspace, lib)
+               ccv3d_group_norm_workspace, ccv3d_kv_attend_workspace, ccv3d_linear_status_word, ccv3d_linear_workspace, ccv3d_take_status, lib)
 
 _DTYPES = {torch.bfloat16: BF16, torch.float32: F32}
 _KINDS = {"none": NORM_NONE, "rms": NORM_RMS, "layer": NORM_LAYER}
@@ -450,28 +450,25 @@ def ring_group_norm(ring, slot, T, groups, weight, bias, scale, shift, eps, acti
         raise Ccv3dError(s, "ccv3d_group_norm_ring")
 
 
-_words = {}              # device -> word that products report in
+_words = {}              # device -> address of the library's word that products report in
 
 
 def _word(dev):
     w = _words.get(dev)
     if w is None:
-        # (there for every stream; a capture cannot make it, and its first call goes without)
-        if _capturing():
-            return None
-        w = _words[dev] = torch.zeros(1, dtype=torch.int32).to(f"cuda:{dev}")
-    return w.data_ptr()
+        s, w = ccv3d_linear_status_word()
+        if s != OK:
+            raise Ccv3dError(s, "ccv3d_linear_status_word")
+        _words[dev] = w
+    return w
 
 
 def status() -> int:
-    """TOKENS_* bits that products (``linear``) on the current device have reported, cleared by reading.  Waits for the device."""
-    dev = _device()
-    _synchronize(dev)
-    w = _words.get(dev)
-    bits = 0 if w is None else int(w.item())
-    if bits:
-        w.zero_()
-        _synchronize(dev)
+    """TOKENS_* bits that products (``linear``) on the current device have reported, replays of captured ones too, cleared by reading.
+    Waits for the device."""
+    s, bits = ccv3d_take_status(_word(_device()))
+    if s != OK:
+        raise Ccv3dError(s, "ccv3d_take_status")
     return bits
 
 
