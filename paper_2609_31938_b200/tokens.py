@@ -451,6 +451,7 @@ def ring_group_norm(ring, slot, T, groups, weight, bias, scale, shift, eps, acti
 
 
 _words = {}              # device -> address of the library's word that products report in
+_reports = threading.Lock()
 
 
 def _word(dev):
@@ -465,8 +466,9 @@ def _word(dev):
 
 def status() -> int:
     """TOKENS_* bits that products (``linear``) on the current device have reported, replays of captured ones too, cleared by reading.
-    Waits for the device."""
-    s, bits = ccv3d_take_status(_word(_device()))
+    Waits for the device, and holds back products of other threads meanwhile (not replays of their graphs)."""
+    with _reports:
+        s, bits = ccv3d_take_status(_word(_device()))
     if s != OK:
         raise Ccv3dError(s, "ccv3d_take_status")
     return bits
@@ -517,7 +519,8 @@ def linear(x, weight, bias=None, *, activation: str = "none", gated: bool = Fals
         return out
     d = LinearDesc(rows, n, k, bool(gated), _activation(activation), dt, od, xs, ws_, os_, rs)
     keep, ws, need = _scratch(("linear", dev, rows, n, k, bool(gated), dt), ccv3d_linear_workspace, "ccv3d_linear_workspace", d)
-    s = lib.ccv3d_linear(d, x.data_ptr(), weight.data_ptr(), b, _ptr(residual), out.data_ptr(), ws, need, _word(dev), _stream(dev))
+    with _reports:           # (see status)
+        s = lib.ccv3d_linear(d, x.data_ptr(), weight.data_ptr(), b, _ptr(residual), out.data_ptr(), ws, need, _word(dev), _stream(dev))
     if s != OK:
         raise Ccv3dError(s, "ccv3d_linear")
     return out
@@ -566,18 +569,21 @@ class DecayMemory:
         # there for every stream when this returns (in a capture, whose every replay zeroes it: for what follows there)
         self._status = torch.zeros(1, dtype=torch.int32, device=states.device if _capturing() else None).to(states.device)
         self._status_ptr = self._status.data_ptr()
+        self._lock = threading.Lock()
 
     @classmethod
     def empty(cls, slots, heads, key_dim, value_dim):
         return cls(torch.zeros((slots, heads, key_dim, value_dim), dtype=torch.float32, device="cuda"))
 
     def status(self) -> int:
-        """TOKENS_* bits that the calls so far have reported, cleared by reading.  Waits for the device."""
-        _synchronize(self.device)
-        bits = int(self._status.item())
-        if bits:
-            self._status.zero_()
+        """TOKENS_* bits that the calls so far have reported, cleared by reading.  Waits for the device, and holds back calls of other
+        threads meanwhile (not replays of their graphs)."""
+        with self._lock:
             _synchronize(self.device)
+            bits = int(self._status.item())
+            if bits:
+                self._status.zero_()
+                _synchronize(self.device)
         return bits
 
     def attend(self, q, k, v, log_decay, batch: StreamBatch, scale: float | None = None, out=None):
@@ -612,8 +618,9 @@ class DecayMemory:
         qk_heads = q.shape[1]
         keep, ws, need = _scratch(("decay", dev, c.batch, tokens, c.max_new, heads, self.key_dim, self.value_dim, dt),
                                   ccv3d_decay_attend_workspace, "ccv3d_decay_attend_workspace", self.c, c, qk_heads, dt)
-        s = lib.ccv3d_decay_attend(self.c, c, cq, ck, cv, log_decay.data_ptr(), log_decay.stride(0), log_decay.stride(1), co, qk_heads,
-                                   dt, self.key_dim ** -0.5 if scale is None else scale, ws, need, self._status_ptr, _stream(dev))
+        with self._lock:         # (see status)
+            s = lib.ccv3d_decay_attend(self.c, c, cq, ck, cv, log_decay.data_ptr(), log_decay.stride(0), log_decay.stride(1), co, qk_heads,
+                                       dt, self.key_dim ** -0.5 if scale is None else scale, ws, need, self._status_ptr, _stream(dev))
         if s != OK:
             raise Ccv3dError(s, "ccv3d_decay_attend")
         return out
