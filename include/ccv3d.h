@@ -593,8 +593,8 @@ ccv3d_status ccv3d_linear_workspace(const ccv3d_linear_desc* d, uint64_t* bytes_
 /*
  * Attention whose memory is one state of fixed size for each sequence and head, from which old tokens fade:
  *   S_t = exp(g_t) S_{t-1} + k_t v_t^T        out_t = scale * q_t S_t             S [key_dim, value_dim], FP32
- * over the new tokens of each sequence in order, g the token's and head's log decay (FP32; <= 0 in ordinary use, -infinity
- * forgets all that was before).  What kv_attend is to a cache that grows, this is to a stream of any length.
+ * over the new tokens of each sequence in order, g the token's and head's log decay (FP32; <= 0 in ordinary use, a state grows with positive
+ * ones, up to 88; what lies under -104, minus infinity too, forgets all that was before; NaN spoils it from there on until it is forgotten).  What kv_attend is to a cache that grows, this is to a stream of any length.
  * states [slots][heads][key_dim][value_dim], DEVICE FP32, 16-byte aligned: sequence b reads slot[b] and leaves its state after
  * its last token there; a sequence without new tokens leaves it as it was.  `fresh` (may be NULL): where fresh[b] is not 0, the
  * sequence starts from zeros whatever its slot holds.

@@ -14,7 +14,9 @@
 // Where sequences and heads are too few for the machine, sequences are cut into segments: their contributions to the state side by side,
 // then a scan over the segments (decay_scan_kernel), then the outputs.
 //
-// A chunk in which a key or value is not finite goes token by token (0 times infinity must not reach a token that does not see it).
+// A chunk in which a key or value is not finite goes token by token (0 times infinity must not reach a token that does not see it), and so does one
+// with a log decay of NaN, or whose positive log decays come to more than 16: products of sums would overflow, a state of zeros times infinity, where
+// the recurrence does not.
 #pragma once
 #include "ccv3d_tokens_common.cuh"
 
@@ -22,7 +24,8 @@ namespace ccv3d {
 
 constexpr int DECAY_CHUNK = 64;
 constexpr int DECAY_STEP_THREADS = 256;
-constexpr float DECAY_FORGET = -1e4f;      // a log decay below it is as good as minus infinity, and its sums stay finite
+constexpr float DECAY_GONE = -104.f, DECAY_FORGET = -1e4f;      // exp of what lies below the first is zero: it goes into sums as the second
+constexpr float DECAY_RISE = 16.f;
 
 struct DecayParams {
     ccv3d_decay_memory m;
@@ -35,7 +38,7 @@ struct DecayParams {
     uint32_t* status;
     int seg;                     // tokens of a segment (0: sequences are not cut)
     float* part;                 // [item][head][key][value]: contributions of the segments, then the states they start from
-    float* fade;                 // [item][head]: decay over a whole segment
+    float* fade;                 // [item][head]: log decay over a whole segment
     int items;                   // room in them
     long long wait_clk;
 };
@@ -83,6 +86,19 @@ __device__ __forceinline__ DecaySeq decay_seq(const DecayParams& p, int b, bool 
 // exp(g) S: what is forgotten wholly is zero whatever it was
 __device__ __forceinline__ float fade(float s, float f) { return f == 0.f ? 0.f : s * f; }
 __device__ __forceinline__ float fade_add(float s, float f, float x) { return f == 0.f ? x : fmaf(s, f, x); }
+// exp(t) s + x, where exp(t) may lie beyond FP32 and the product within
+__device__ __forceinline__ float grow_add(float s, float t, float x) {
+    if (t <= 64.f) return fade_add(s, expf(t), x);
+    const float f = expf(0.25f * t);
+    return s == 0.f ? x : fmaf(s * f * f * f, f, x);
+}
+
+// What a log decay adds to a chunk's rise (NaN stays), and whether all of them (two to a lane) leave the chunk to products.
+__device__ __forceinline__ float decay_rise(float g) { return g <= 0.f ? 0.f : g; }
+__device__ __forceinline__ bool decay_steep(float rise) {
+    if (!__any_sync(0xffffffffu, !(rise <= 0.f))) return false;
+    return !(warp_sum(rise) <= DECAY_RISE);
+}
 
 // ---------------------------------------------------------------------------------------------------- single tokens
 // Block (sequence, head, 64 value columns): thread t has columns 4 (t % 16) .. + 3 of rows R (t / 16) + i, whose keys and queries it reads four at
@@ -207,6 +223,7 @@ struct DecayShared {
     float end[DECAY_CHUNK];      // exp(G_end - G_j)
     float begin[DECAY_CHUNK];    // exp(G_i)
     float last;                  // exp(G_end)
+    int steep;
 };
 
 // Item (sequence, segment) of a cut call; false: there is none of this number.  All threads; word: 34 ints in shared memory.
@@ -324,7 +341,8 @@ __global__ void __launch_bounds__(32 * NW, NW == 4 ? 2 : 1) decay_chunk_kernel(c
     };
 
     const int chunks = (n + L - 1) / L;
-    double total = 0.0;                                // log decay of the chunks so far (warp 0)
+    double total = 0.0;                                // log decay of the chunks so far, and whether it is minus infinity (warp 0)
+    bool gone = false;
     bring_chunk(0);
     for (int chunk = 0; chunk < chunks; ++chunk) {
         const int tok0 = first + chunk * L, live = min(L, n - chunk * L);
@@ -341,12 +359,18 @@ __global__ void __launch_bounds__(32 * NW, NW == 4 ? 2 : 1) decay_chunk_kernel(c
         if (warp == 0) {
             // log decays of tokens 2 lane, 2 lane + 1 and their sums
             double x[2];
+            float rise = 0.f;
+            bool forget = false;
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
                 const int r = 2 * lane + i;
                 const float d = r < live ? __ldg(p.decay + (int64_t)(tok0 + r) * p.d_token + h * p.d_head) : 0.f;
-                x[i] = d < DECAY_FORGET ? (double)DECAY_FORGET : (double)d;
+                rise += decay_rise(d);
+                forget = forget || d < DECAY_GONE;
+                x[i] = d < DECAY_GONE ? (double)DECAY_FORGET : (double)d;
             }
+            const bool steep = decay_steep(rise);
+            gone = __any_sync(0xffffffffu, forget) || gone;
             double s = x[0] + x[1];
 #pragma unroll
             for (int o = 1; o < 32; o <<= 1) {
@@ -362,14 +386,14 @@ __global__ void __launch_bounds__(32 * NW, NW == 4 ? 2 : 1) decay_chunk_kernel(c
                 sh.begin[2 * lane + i] = expf((float)at);
                 sh.end[2 * lane + i] = expf((float)(end - at));
             }
-            if (lane == 31) sh.last = expf((float)end);
+            if (lane == 31) { sh.last = expf((float)end); sh.steep = steep; }
             total += end;
         }
         most = 0;
         __syncthreads();
         look(sk, S::QS, DK);
         look(sv, S::VS, S::DV);
-        const bool odd = __syncthreads_or((most & 0xFFFFu) >= 0x7F80u || (most >> 16) >= 0x7F80u);
+        const bool odd = __syncthreads_or((most & 0xFFFFu) >= 0x7F80u || (most >> 16) >= 0x7F80u || sh.steep);
         const float last = sh.last;
         if (odd) {
             // token by token; a lane's part of q S is summed over the four lanes of its rows
@@ -384,8 +408,7 @@ __global__ void __launch_bounds__(32 * NW, NW == 4 ? 2 : 1) decay_chunk_kernel(c
             };
 #pragma unroll 1
             for (int i = 0; i < live; ++i) {
-                const float prev = i ? sh.g[i - 1].x : 0.f, prev_lo = i ? sh.g[i - 1].y : 0.f;
-                const float f = expf((sh.g[i].x - prev) + (sh.g[i].y - prev_lo));
+                const float f = expf(__ldg(p.decay + (int64_t)(tok0 + i) * p.d_token + h * p.d_head));
                 const float v0 = value(sv + i * S::VS + 16 * warp + g, S::V), v1 = value(sv + i * S::VS + 16 * warp + g + 8, S::V);
                 float y0 = 0.f, y1 = 0.f;
 #pragma unroll
@@ -609,7 +632,7 @@ __global__ void __launch_bounds__(32 * NW, NW == 4 ? 2 : 1) decay_chunk_kernel(c
         for (int j = 0; j < DK / 8; ++j)
 #pragma unroll
             for (int i = 0; i < 4; ++i) *state_at(to, j, i) = st[j][i];
-        if (MODE == DECAY_STATES && t == 0 && slice == 0) p.fade[(int64_t)blockIdx.x * p.m.heads + h] = expf((float)total);
+        if (MODE == DECAY_STATES && t == 0 && slice == 0) p.fade[(int64_t)blockIdx.x * p.m.heads + h] = gone ? -INFINITY : (float)total;
     }
 }
 
@@ -657,10 +680,10 @@ __global__ void __launch_bounds__(DECAY_SCAN_THREADS) decay_scan_kernel(const __
         for (int j = 0; j < DECAY_SCAN_AHEAD; ++j)
             if (i + j < items) {
                 *reinterpret_cast<float4*>(at + (i + j) * per) = x;
-                x.x = fade_add(x.x, f[j], y[j].x);
-                x.y = fade_add(x.y, f[j], y[j].y);
-                x.z = fade_add(x.z, f[j], y[j].z);
-                x.w = fade_add(x.w, f[j], y[j].w);
+                x.x = grow_add(x.x, f[j], y[j].x);
+                x.y = grow_add(x.y, f[j], y[j].y);
+                x.z = grow_add(x.z, f[j], y[j].z);
+                x.w = grow_add(x.w, f[j], y[j].w);
             }
     }
     if (s.slot >= 0) *reinterpret_cast<float4*>(state) = x;

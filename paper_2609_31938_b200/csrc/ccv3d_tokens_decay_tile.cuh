@@ -35,11 +35,11 @@ template <int DK> struct DecayTileShape {
 struct DecayTileShared {
     // (a ring of five: the outputs of chunk c - 2 may still be made while the sums of chunk c + 2 are taken)
     float begin[DECAY_TILE_RING][DECAY_CHUNK];      // exp(G_i)
-    float last[DECAY_TILE_RING];
+    float last[DECAY_TILE_RING];                    // exp(G_end); -1: log decays that are not for products
     int odd[DECAY_TILE_RING];
     uint32_t tmem;
     int abort_flag;
-    float2 g[2][DECAY_CHUNK];
+    alignas(16) float2 g[2][DECAY_CHUNK];           // (read two at a time)
     float end[2][DECAY_CHUNK];
     uint64_t told[4], g_full[2], g_empty[2], v_ready, v_used, ready, used, s_full, out_full[2], out_empty[2], d3_full[2], d3_empty[2], meet_full, meet_empty, odd_done;
 };
@@ -309,7 +309,7 @@ __global__ void __launch_bounds__(DECAY_TILE_THREADS, 1) decay_tile_kernel(const
             // (the issuer tells of a chunk; it is never four ahead, while the front may be more than a phase of its barriers ahead of this)
             if (!(ok = decay_wait(&sh->told[chunk & 3], chunk >> 2 & 1, sh, p))) break;
             const bool last_one = chunk + 1 == chunks;
-            if (sh->odd[ring]) {
+            if (sh->odd[ring] || sh->last[ring] < 0.f) {
                 // token by token; the two halves' parts of q S meet in shared memory (the place of P)
                 const uint8_t* tok = base + (chunk & 1) * S::STAGE;
                 float* meet = reinterpret_cast<float*>(base + S::P_AT);
@@ -404,6 +404,7 @@ __global__ void __launch_bounds__(DECAY_TILE_THREADS, 1) decay_tile_kernel(const
         if (warp == 17) {
             // log decays of tokens 2 lane, 2 lane + 1 of a chunk and their sums, up to two chunks ahead
             double total = 0.0;
+            bool gone = false;
             float next[2];
             auto fetch = [&](int chunk) {
 #pragma unroll
@@ -417,7 +418,9 @@ __global__ void __launch_bounds__(DECAY_TILE_THREADS, 1) decay_tile_kernel(const
                 const int two = chunk & 1, ring = chunk % DECAY_TILE_RING;
                 double x[2];
 #pragma unroll
-                for (int i = 0; i < 2; ++i) x[i] = next[i] < DECAY_FORGET ? (double)DECAY_FORGET : (double)next[i];
+                for (int i = 0; i < 2; ++i) x[i] = next[i] < DECAY_GONE ? (double)DECAY_FORGET : (double)next[i];
+                const bool steep = decay_steep(decay_rise(next[0]) + decay_rise(next[1]));
+                gone = __any_sync(0xffffffffu, next[0] < DECAY_GONE || next[1] < DECAY_GONE) || gone;
                 if (chunk + 1 < chunks) fetch(chunk + 1);
                 double s = x[0] + x[1];
 #pragma unroll
@@ -435,12 +438,12 @@ __global__ void __launch_bounds__(DECAY_TILE_THREADS, 1) decay_tile_kernel(const
                     sh->begin[ring][2 * lane + i] = expf((float)at);
                     sh->end[two][2 * lane + i] = expf((float)(end - at));
                 }
-                if (lane == 31) sh->last[ring] = expf((float)end);
+                if (lane == 31) sh->last[ring] = steep ? -1.f : expf((float)end);
                 total += end;
                 __syncwarp();
                 if (lane == 0) mbar_arrive(smem_u32(&sh->g_full[two]));
             }
-            if (MODE == DECAY_STATES && ok && lane == 0 && slice == 0) p.fade[(int64_t)blockIdx.x * p.m.heads + h] = expf((float)total);
+            if (MODE == DECAY_STATES && ok && lane == 0 && slice == 0) p.fade[(int64_t)blockIdx.x * p.m.heads + h] = gone ? -INFINITY : (float)total;
         }
         // D = F32, A = B = BF16, M = 128; bits 15, 16: A, B lie with their rows, not K, side by side (tokens are K in D3 and for the values)
         constexpr uint32_t I = (1u << 4) | (1u << 7) | (1u << 10) | ((128u >> 4) << 24);
@@ -450,7 +453,7 @@ __global__ void __launch_bounds__(DECAY_TILE_THREADS, 1) decay_tile_kernel(const
         int turn = 0, s_turn = 0, odd_turn = 0;
         for (int chunk = 0; warp == 16 && ok && chunk < chunks; ++chunk) {
             if (!(ok = decay_wait(&sh->v_ready, chunk & 1, sh, p))) break;
-            const bool odd = sh->odd[chunk % DECAY_TILE_RING];
+            const bool odd = sh->odd[chunk % DECAY_TILE_RING] || sh->last[chunk % DECAY_TILE_RING] < 0.f;
             if (odd && OUT) {
                 // P and the state have been written, and go unused: before the state's warps hear of the chunk and go on
                 if (!(ok = decay_wait(&sh->ready, chunk & 1, sh, p))) break;
