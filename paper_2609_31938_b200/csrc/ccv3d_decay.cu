@@ -40,17 +40,25 @@ ccv3d_status plan_decay(const ccv3d_decay_memory* m, const ccv3d_stream_batch* b
     q->items = q->fade_at = 0;
     q->bytes = 0;
     if (q->step) return CCV3D_OK;
-    // Blocks of a chunk kernel for each item.  Where the sequences do not fill the machine, or one is far longer than the others, they are cut
-    // so that one turn of blocks does: a block's start and end cost as much as some chunks.
-    const int64_t wide = (int64_t)m->heads * ((m->value_dim + q->columns - 1) / q->columns), fit = q->dev.sm_count;
-    const int64_t longest = b->max_new < b->tokens ? b->max_new : b->tokens;
-    if (wide * b->batch >= fit && longest <= 8 * ((int64_t)b->tokens / b->batch + 64)) return CCV3D_OK;
-    const int64_t items = fit / wide > b->batch ? fit / wide : b->batch, chunks = (b->tokens + DECAY_CHUNK - 1) / DECAY_CHUNK;
-    int64_t per = (chunks + items - 1) / items;
+    // Where the sequences do not fill the machine they are cut so that one turn of blocks does: a block's start and end cost as much as some
+    // chunks.  Where one may be far longer than the others, segments are four times as long as their mean, so that not much else is cut
+    // (max_new is a bound, and may say so of sequences that are all alike).
+    const int64_t wide = (int64_t)m->heads * ((m->value_dim + q->columns - 1) / q->columns), fit = q->dev.sm_count, B = b->batch;
+    const int64_t longest = b->max_new < b->tokens ? b->max_new : b->tokens, mean = b->tokens / B + 64;
+    int64_t per;
+    if (wide * B < fit) {
+        const int64_t items = fit / wide > B ? fit / wide : B, chunks = (b->tokens + DECAY_CHUNK - 1) / DECAY_CHUNK;
+        per = (chunks + items - 1) / items;
+    } else {
+        if (longest <= 8 * mean) return CCV3D_OK;
+        per = 4 * mean / DECAY_CHUNK;
+    }
     if (per < 4) per = 4;
     if (per * DECAY_CHUNK >= longest) return CCV3D_OK;
+    // Items are segments of sequences of more than one: no more than tokens / seg, and one more for each such sequence.
     q->seg = (int)(per * DECAY_CHUNK);
-    q->items = b->tokens / q->seg + b->batch;
+    const int64_t cut = b->tokens / (q->seg + 1);
+    q->items = b->tokens / q->seg + (cut < B ? cut : B);
     q->fade_at = (q->items * m->heads * m->key_dim * m->value_dim * 4 + 255) / 256 * 256;
     q->bytes = (uint64_t)(q->fade_at + (q->items * m->heads * 4 + 255) / 256 * 256);
     return CCV3D_OK;
@@ -73,13 +81,13 @@ ccv3d_status launch_chunks(const DecayParams& p, const DecayPlan& q, int64_t ite
 
 template <typename T, int DK>
 ccv3d_status launch_prompt(const DecayParams& p, const DecayPlan& q, cudaStream_t st) {
-    if (!q.seg) return launch_chunks<T, DK, DECAY_ALL>(p, q, p.bt.batch, st);
+    if (!q.seg) return launch_chunks<T, DK, DECAY_OUTPUTS>(p, q, p.bt.batch, st);
     ccv3d_status s = launch_chunks<T, DK, DECAY_STATES>(p, q, q.items, st);
     if (s != CCV3D_OK) return s;
     const int64_t size = (int64_t)DK * p.m.value_dim;
     decay_scan_kernel<<<dim3(p.bt.batch, (unsigned)((size + 1023) / 1024), p.m.heads), DECAY_SCAN_THREADS, 0, st>>>(p);
     if ((s = launched()) != CCV3D_OK) return s;
-    return launch_chunks<T, DK, DECAY_OUTPUTS>(p, q, q.items, st);
+    return launch_chunks<T, DK, DECAY_OUTPUTS>(p, q, q.items + p.bt.batch, st);
 }
 
 template <typename T, int DK>

@@ -11,8 +11,8 @@
 // decay as three).  F32, 24 prompts of up to 700 tokens, 14 heads of 64 x 128: 328 us, bound by the latency of eight warps' products.
 // G is summed in 64 bits and kept as two floats, so that differences of sums that a strong decay made large still have all their bits.
 //
-// Where sequences and heads are too few for the machine, sequences are cut into segments: their contributions to the state side by side,
-// then a scan over the segments (decay_scan_kernel), then the outputs.
+// Where sequences and heads are too few for the machine, sequences of more than a segment are cut: their segments' contributions to the state side by
+// side, then a scan over the segments (decay_scan_kernel), then the outputs.  Other sequences of such a call go beside the outputs in one piece.
 //
 // A chunk in which a key or value is not finite goes token by token (0 times infinity must not reach a token that does not see it), and so does one
 // with a log decay of NaN, or whose positive log decays come to more than 16: products of sums would overflow, a state of zeros times infinity, where
@@ -37,9 +37,9 @@ struct DecayParams {
     float scale;
     uint32_t* status;
     int seg;                     // tokens of a segment (0: sequences are not cut)
-    float* part;                 // [item][head][key][value]: contributions of the segments, then the states they start from
+    float* part;                 // [item][head][key][value]: contributions of cut sequences' segments, then the states they start from
     float* fade;                 // [item][head]: log decay over a whole segment
-    int items;                   // room in them
+    int items;                   // room in them; the blocks behind them have the sequences that are not cut
     long long wait_clk;
 };
 
@@ -55,11 +55,12 @@ __device__ __forceinline__ void decay_span(const ccv3d_stream_batch& bt, int b, 
     first = s;
     n = e - s;
 }
-// All threads of the block.
-__device__ __forceinline__ DecaySeq decay_seq(const DecayParams& p, int b, bool tell) {
+// All threads of the block.  A sequence of more than `most` tokens (0: any number) is another block's: without tokens here.
+__device__ __forceinline__ DecaySeq decay_seq(const DecayParams& p, int b, bool tell, int most = 0) {
     DecaySeq s;
     bool bad;
     decay_span(p.bt, b, s.first, s.n, bad);
+    if (most && s.n > most) return {s.first, 0, -1, true};
     s.slot = __ldg(p.bt.slot + b);
     uint32_t word = bad ? CCV3D_TOKENS_BAD_LENGTH : 0u;
     int taken = 0;
@@ -226,7 +227,10 @@ struct DecayShared {
     int steep;
 };
 
-// Item (sequence, segment) of a cut call; false: there is none of this number.  All threads; word: 34 ints in shared memory.
+// Segments of a sequence of n tokens that is cut; 0: it is not.
+__device__ __forceinline__ int decay_segments(const DecayParams& p, int n) { return n > p.seg ? (n - 1) / p.seg + 1 : 0; }
+
+// Item (cut sequence, segment); false: there is none of this number.  All threads; word: 34 ints in shared memory.
 __device__ __forceinline__ bool decay_item(const DecayParams& p, int item, int& b, int& seg, int* word) {
     int* scan = word + 2;
     const int t = threadIdx.x, warps = blockDim.x >> 5;
@@ -237,7 +241,7 @@ __device__ __forceinline__ bool decay_item(const DecayParams& p, int item, int& 
         bool bad;
         if (base + t < p.bt.batch) {
             decay_span(p.bt, base + t, first, n, bad);
-            n = n / p.seg + (n % p.seg != 0);
+            n = decay_segments(p, n);
         }
         const int upto = warp_scan(n);
         if ((t & 31) == 31) scan[t >> 5] = upto;
@@ -258,7 +262,38 @@ __device__ __forceinline__ bool decay_item(const DecayParams& p, int item, int& 
     return b >= 0;
 }
 
-enum { DECAY_ALL, DECAY_STATES, DECAY_OUTPUTS };     // a whole sequence; a segment's contribution to the state; a segment's outputs
+// Passes over the chunks of a block: outputs of a sequence and its state, or of a cut one's segment; a segment's contribution to the state.
+enum { DECAY_OUTPUTS, DECAY_STATES };
+
+// A block's tokens, and where its state comes from and goes to.  All threads; word as above.
+struct DecayWork {
+    int first, n;
+    const float* from;           // nullptr: zeros
+    float* to;                   // nullptr: it is not kept
+    bool last;                   // the state is wanted behind the last chunk
+};
+template <int MODE>
+__device__ __forceinline__ bool decay_work(const DecayParams& p, int h, int dk, DecayWork& w, int* word) {
+    const int64_t size = (int64_t)dk * p.m.value_dim, block = blockIdx.x;
+    if (MODE == DECAY_STATES || block < p.items) {
+        int b, seg;
+        bool bad;
+        if (!decay_item(p, blockIdx.x, b, seg, word)) return false;
+        decay_span(p.bt, b, w.first, w.n, bad);
+        w.first += seg * p.seg;
+        w.n = min(p.seg, w.n - seg * p.seg);
+        float* part = p.part + (block * p.m.heads + h) * size;
+        w.last = MODE == DECAY_STATES;
+        w.from = w.last ? nullptr : part;
+        w.to = w.last ? part : nullptr;
+        return true;
+    }
+    const DecaySeq s = decay_seq(p, (int)block - p.items, blockIdx.y == 0, p.seg);
+    if (s.n == 0) return false;
+    float* state = s.slot < 0 ? nullptr : p.m.states + ((int64_t)s.slot * p.m.heads + h) * size;
+    w = {s.first, s.n, s.zero ? nullptr : state, state, state != nullptr};
+    return true;
+}
 
 template <int DK, int NW, int MODE>
 __global__ void __launch_bounds__(32 * NW, NW == 4 ? 2 : 1) decay_chunk_kernel(const __grid_constant__ DecayParams p) {
@@ -271,23 +306,9 @@ __global__ void __launch_bounds__(32 * NW, NW == 4 ? 2 : 1) decay_chunk_kernel(c
     const int t = threadIdx.x, warp = t >> 5, lane = t & 31, g = lane >> 2, tc = lane & 3;
     const int slices = p.m.value_dim / S::DV, slice = blockIdx.y % slices, h = blockIdx.y / slices;
     const int dv0 = slice * S::DV;
-    int first, n;
-    int64_t part_at = 0;                               // of the item's head in part
-    DecaySeq sq = {0, 0, -1, true};
-    if constexpr (MODE == DECAY_ALL) {
-        sq = decay_seq(p, blockIdx.x, blockIdx.y == 0);
-        first = sq.first;
-        n = sq.n;
-        if (n == 0) return;
-    } else {
-        int b, seg;
-        bool bad;
-        if (!decay_item(p, blockIdx.x, b, seg, word)) return;
-        decay_span(p.bt, b, first, n, bad);
-        first += seg * p.seg;
-        n = min(p.seg, n - seg * p.seg);
-        part_at = ((int64_t)blockIdx.x * p.m.heads + h) * DK * p.m.value_dim;
-    }
+    DecayWork work;
+    if (!decay_work<MODE>(p, h, DK, work, word)) return;
+    const int first = work.first, n = work.n;
     const T* kp = (const T*)p.k.data + h / p.group * p.k.head_stride;
     const T* qp = (const T*)p.q.data + h / p.group * p.q.head_stride;
     const T* vp = (const T*)p.v.data + h * p.v.head_stride + dv0;
@@ -295,15 +316,11 @@ __global__ void __launch_bounds__(32 * NW, NW == 4 ? 2 : 1) decay_chunk_kernel(c
 
     // S^T of this warp: rows dv = 16 warp + g (+ 8), columns dk = 8 j + 2 tc (+ 1)
     float st[DK / 8][4];
-    auto state_at = [&](float* base, int j, int i) { return base + (int64_t)(8 * j + 2 * tc + (i & 1)) * p.m.value_dim + dv0 + 16 * warp + g + (i >> 1) * 8; };
-    {
-        float* from = MODE == DECAY_ALL ? p.m.states + ((int64_t)max(sq.slot, 0) * p.m.heads + h) * DK * p.m.value_dim : p.part + part_at;
-        const bool zero = MODE == DECAY_STATES || (MODE == DECAY_ALL && sq.zero);
+    auto state_at = [&](auto* base, int j, int i) { return base + (int64_t)(8 * j + 2 * tc + (i & 1)) * p.m.value_dim + dv0 + 16 * warp + g + (i >> 1) * 8; };
 #pragma unroll
-        for (int j = 0; j < DK / 8; ++j)
+    for (int j = 0; j < DK / 8; ++j)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) st[j][i] = zero ? 0.f : *state_at(from, j, i);
-    }
+        for (int i = 0; i < 4; ++i) st[j][i] = MODE != DECAY_STATES && work.from ? *state_at(work.from, j, i) : 0.f;
 
     uint32_t most = 0;                                 // of keys and values: whether all are finite (this thread's)
     // rows of `dim` elements of tokens tok .. of a chunk of `live` into planes at `to`; what lies behind them is zero
@@ -571,7 +588,7 @@ __global__ void __launch_bounds__(32 * NW, NW == 4 ? 2 : 1) decay_chunk_kernel(c
                         }
                     }
             }
-            if (MODE != DECAY_OUTPUTS || chunk + 1 < chunks) {
+            if (work.last || chunk + 1 < chunks) {
                 // the state: v with its decay to the chunk's end, as parts, times k
                 uint32_t va[L / 16][N][4];
 #pragma unroll
@@ -626,12 +643,11 @@ __global__ void __launch_bounds__(32 * NW, NW == 4 ? 2 : 1) decay_chunk_kernel(c
         __syncthreads();                                     // this chunk's rows and scores have been used
         if (chunk + 1 < chunks) bring_chunk(chunk + 1);
     }
-    if (MODE == DECAY_STATES || (MODE == DECAY_ALL && sq.slot >= 0)) {
-        float* to = MODE == DECAY_ALL ? p.m.states + ((int64_t)sq.slot * p.m.heads + h) * DK * p.m.value_dim : p.part + part_at;
+    if (work.to) {
 #pragma unroll
         for (int j = 0; j < DK / 8; ++j)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) *state_at(to, j, i) = st[j][i];
+            for (int i = 0; i < 4; ++i) *state_at(work.to, j, i) = st[j][i];
         if (MODE == DECAY_STATES && t == 0 && slice == 0) p.fade[(int64_t)blockIdx.x * p.m.heads + h] = gone ? -INFINITY : (float)total;
     }
 }
@@ -642,15 +658,16 @@ constexpr int DECAY_SCAN_THREADS = 256, DECAY_SCAN_AHEAD = 4;
 __global__ void __launch_bounds__(DECAY_SCAN_THREADS) decay_scan_kernel(const __grid_constant__ DecayParams p) {
     const int64_t size = (int64_t)p.m.key_dim * p.m.value_dim, per = p.m.heads * size;
     const int b = blockIdx.x, h = blockIdx.z;
+    int first, n;
+    bool bad;
+    decay_span(p.bt, b, first, n, bad);
+    if (!decay_segments(p, n)) return;
     const DecaySeq s = decay_seq(p, b, blockIdx.y == 0 && h == 0);
-    if (s.n == 0) return;
     // items before this sequence's
     long long before = 0;
     for (int j = threadIdx.x; j < b; j += DECAY_SCAN_THREADS) {
-        int f, n;
-        bool bad;
-        decay_span(p.bt, j, f, n, bad);
-        before += n / p.seg + (n % p.seg != 0);
+        decay_span(p.bt, j, first, n, bad);
+        before += decay_segments(p, n);
     }
     __shared__ long long sums[DECAY_SCAN_THREADS / 32];
 #pragma unroll
@@ -662,7 +679,7 @@ __global__ void __launch_bounds__(DECAY_SCAN_THREADS) decay_scan_kernel(const __
     const int64_t e = (int64_t)blockIdx.y * (4 * DECAY_SCAN_THREADS) + 4 * threadIdx.x;
     if (e >= size) return;
     // (offsets that name tokens twice can give more items than there is room for)
-    const int items = (int)min((long long)(s.n / p.seg + (s.n % p.seg != 0)), max(0ll, p.items - before));
+    const int items = (int)min((long long)decay_segments(p, s.n), max(0ll, p.items - before));
     float* state = p.m.states + ((int64_t)max(s.slot, 0) * p.m.heads + h) * size + e;
     float4 x = s.zero ? make_float4(0.f, 0.f, 0.f, 0.f) : *reinterpret_cast<const float4*>(state);
     float* at = p.part + before * per + h * size + e;

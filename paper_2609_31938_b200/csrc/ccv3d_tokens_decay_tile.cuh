@@ -88,23 +88,9 @@ __global__ void __launch_bounds__(DECAY_TILE_THREADS, 1) decay_tile_kernel(const
     const int t = threadIdx.x, warp = __shfl_sync(0xffffffffu, t >> 5, 0), lane = t & 31;
     const int slices = (p.m.value_dim + DECAY_TILE_DV - 1) / DECAY_TILE_DV, slice = blockIdx.y % slices, h = blockIdx.y / slices;
     const int dv0 = slice * DECAY_TILE_DV, dvs = min(DECAY_TILE_DV, p.m.value_dim - dv0);
-    int first, n;
-    int64_t part_at = 0;
-    DecaySeq sq = {0, 0, -1, true};
-    if constexpr (MODE == DECAY_ALL) {
-        sq = decay_seq(p, blockIdx.x, blockIdx.y == 0);
-        first = sq.first;
-        n = sq.n;
-        if (n == 0) return;
-    } else {
-        int b, seg;
-        bool bad;
-        if (!decay_item(p, blockIdx.x, b, seg, (int*)sh->begin)) return;
-        decay_span(p.bt, b, first, n, bad);
-        first += seg * p.seg;
-        n = min(p.seg, n - seg * p.seg);
-        part_at = ((int64_t)blockIdx.x * p.m.heads + h) * DK * p.m.value_dim;
-    }
+    DecayWork work;
+    if (!decay_work<MODE>(p, h, DK, work, (int*)sh->begin)) return;
+    const int first = work.first, n = work.n;
     const int chunks = (n + L - 1) / L;
     if (at0 & 1023u) {                                         // (not so: nothing is touched)
         if (t == 0) report(p.status, CCV3D_TOKENS_TIMEOUT);
@@ -278,13 +264,9 @@ __global__ void __launch_bounds__(DECAY_TILE_THREADS, 1) decay_tile_kernel(const
         const uint32_t lanes = tmem + ((uint32_t)q << 21);
         const bool mine = dv < dvs;
         float st[KH];                                          // S^T[dv, half * KH ..]
-        auto state_at = [&](float* from, int j) { return from + (int64_t)(half * KH + j) * p.m.value_dim + dv0 + dv; };
-        {
-            float* from = MODE == DECAY_ALL ? p.m.states + ((int64_t)max(sq.slot, 0) * p.m.heads + h) * DK * p.m.value_dim : p.part + part_at;
-            const bool zero = MODE == DECAY_STATES || (MODE == DECAY_ALL && sq.zero) || !mine;
+        auto state_at = [&](auto* from, int j) { return from + (int64_t)(half * KH + j) * p.m.value_dim + dv0 + dv; };
 #pragma unroll
-            for (int j = 0; j < KH; ++j) st[j] = zero ? 0.f : *state_at(from, j);
-        }
+        for (int j = 0; j < KH; ++j) st[j] = MODE != DECAY_STATES && work.from && mine ? *state_at(work.from, j) : 0.f;
         auto put_state = [&]() {                              // its parts, for the next chunk's products
 #pragma unroll
             for (int j = 0; j < KH; j += 8) {
@@ -348,7 +330,7 @@ __global__ void __launch_bounds__(DECAY_TILE_THREADS, 1) decay_tile_kernel(const
             const uint32_t ph = turn >> 1 & 1;
             ++turn;
             if (OUT && !(ok = decay_wait(&sh->out_full[buf], ph, sh, p))) break;
-            if (MODE != DECAY_OUTPUTS || !last_one) {
+            if (work.last || !last_one) {
                 if (!(ok = decay_wait(&sh->d3_full[buf], ph, sh, p))) break;
                 tc_fence_after();
                 const float f = sh->last[ring];
@@ -393,10 +375,9 @@ __global__ void __launch_bounds__(DECAY_TILE_THREADS, 1) decay_tile_kernel(const
                 }
             }
         }
-        if (ok && mine && (MODE == DECAY_STATES || (MODE == DECAY_ALL && sq.slot >= 0))) {
-            float* to = MODE == DECAY_ALL ? p.m.states + ((int64_t)sq.slot * p.m.heads + h) * DK * p.m.value_dim : p.part + part_at;
+        if (ok && mine && work.to) {
 #pragma unroll
-            for (int j = 0; j < KH; ++j) *state_at(to, j) = st[j];
+            for (int j = 0; j < KH; ++j) *state_at(work.to, j) = st[j];
         }
     } else {
         // ------------------------------------------------------------------------------------------ MMAs
@@ -475,7 +456,7 @@ __global__ void __launch_bounds__(DECAY_TILE_THREADS, 1) decay_tile_kernel(const
             const int buf = turn & 1;
             const uint32_t ph = (turn >> 1 & 1) ^ 1u, st = (chunk & 1) * S::STAGE;
             ++turn;
-            if (MODE != DECAY_OUTPUTS || chunk + 1 < chunks) {
+            if (work.last || chunk + 1 < chunks) {
                 if (!(ok = decay_wait(&sh->d3_empty[buf], ph, sh, p))) break;
                 tc_fence_after();
                 if (elect_one()) {

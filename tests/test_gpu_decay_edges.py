@@ -67,3 +67,83 @@ def test_a_decay_of_nan_reaches_only_what_follows(at, n, dtype):
     want, w = c.run()
     torch.testing.assert_close(out[bad + 1:], want[bad + 1:], **tol)
     torch.testing.assert_close(m.states, w.states, rtol=2.0 ** -16, atol=1e-5)
+
+
+def attend(c, max_new):
+    from paper_2609_31938_b200 import tokens as tk
+    m = tk.DecayMemory(c.states.clone())
+    return m.attend(c.q, c.k, c.v, c.g, tk.StreamBatch(c.starts, c.slot, max_new, fresh=c.fresh)), m
+
+
+@pytest.mark.parametrize("dtype", [BF, F])
+@pytest.mark.parametrize("new,heads", [([1] * 200 + [3000] + [1] * 200, 4), ([2, 1500, 0, 30, 900, 257, 256, 1], 2), ([1] * 40 + [2100], 1)])
+def test_single_tokens_beside_long_prompts(new, heads, dtype):
+    c = Case(new, heads, 1, 64, 64, dtype, seed=31, rate=0.02)
+    g = torch.Generator(device="cuda").manual_seed(1)
+    c.fresh = (torch.rand(len(new), generator=g, device="cuda") < 0.3).int()
+    out, m = c.run()
+    c.check(out, m)
+    assert m.status() == 0
+    again, other = c.run()
+    assert torch.equal(out, again) and torch.equal(m.states, other.states)
+    # a bound that is far off: the same
+    out, m = attend(c, 100_000)
+    c.check(out, m)
+    assert m.status() == 0
+
+
+@pytest.mark.parametrize("dtype", [BF, F])
+@pytest.mark.parametrize("new,heads", [([200] * 40, 8), ([200], 2), ([150, 140], 1)])
+def test_a_loose_bound_does_not_change_a_bit(new, heads, dtype):
+    c = Case(new, heads, heads, 64, 128, dtype, seed=32)
+    out, m = attend(c, max(new))
+    loose, other = attend(c, 1 << 30)
+    assert torch.equal(out, loose) and torch.equal(m.states, other.states) and m.status() == other.status() == 0
+    c.check(out, m)
+
+
+@pytest.mark.parametrize("singles,prompt", [(256, 4000), (1024, 28000), (65000, 1000)])
+def test_scratch_goes_by_what_is_cut(singles, prompt):
+    """No more than the states of two segments for each 256 tokens, however many sequences there are."""
+    import paper_2609_31938_b200 as ccv
+    some = torch.zeros(16, device="cuda")
+    at = some.data_ptr()
+    for dtype in (ccv.BF16, ccv.F32):
+        memory = ccv.DecayMemoryC(at, singles + 1, 32, 128, 128)
+        tokens = singles + prompt
+        for bound in (prompt, 1 << 30):
+            s, n = ccv.ccv3d_decay_attend_workspace(memory, ccv.StreamBatchC(at, at, None, singles + 1, tokens, bound), 32, dtype)
+            assert s == ccv.OK and n <= 2 * (tokens / 256 + 1) * 32 * (128 * 128 + 1) * 4 + 512
+
+
+@pytest.mark.parametrize("dtype", [BF, F])
+@pytest.mark.parametrize("n", [4, 100, 1000])
+def test_bad_offsets_leave_other_sequences_and_states_alone(n, dtype):
+    from paper_2609_31938_b200 import TOKENS_BAD_LENGTH, TOKENS_BAD_SLOT
+    c = Case([n, 3, n, 2], 2, 2, 64, 64, dtype, seed=33)
+    want, w = c.run()
+    for starts, untouched in (([0, n, 10 * n, 2 * n + 3, 2 * n + 5], [0, 3]),      # one ends past the rows, the next begins there
+                              ([0, n, -7, 2 * n + 3, 2 * n + 5], [3])):            # ... or below the first, whose rows are then written twice
+        good = c.starts.clone()
+        c.starts[:] = torch.tensor(starts, device="cuda")
+        out, m = attend(c, max(c.new))
+        assert m.status() & TOKENS_BAD_LENGTH
+        c.starts = good
+        for b in (0, 3):
+            rows = slice(int(good[b]), int(good[b + 1]))
+            tol = dict(rtol=2.0 ** -6 if dtype == BF else 2.0 ** -16, atol=1e-3)
+            if b in untouched:
+                torch.testing.assert_close(out[rows], want[rows], **tol)
+            torch.testing.assert_close(m.states[c.slot[b]], w.states[c.slot[b]], rtol=2.0 ** -16, atol=1e-4)
+        free = torch.ones(len(c.states), dtype=torch.bool, device="cuda")
+        free[c.slot.long()] = False
+        assert torch.equal(m.states[free], c.states[free])
+    # a slot outside the pool: no state changes but those of the others
+    slot, c.slot = c.slot.clone(), c.slot.clone()
+    c.slot[0], c.slot[2] = -1, 1 << 30
+    out, m = attend(c, max(c.new))
+    assert m.status() == TOKENS_BAD_SLOT
+    lost = slot[[0, 2]].long()
+    assert torch.equal(m.states[lost], c.states[lost])
+    torch.testing.assert_close(m.states[slot[1]], w.states[slot[1]], rtol=2.0 ** -16, atol=1e-4)
+    torch.testing.assert_close(m.states[slot[3]], w.states[slot[3]], rtol=2.0 ** -16, atol=1e-4)
