@@ -563,7 +563,7 @@ typedef enum { CCV3D_ACT_NONE = 0, CCV3D_ACT_SILU = 1, CCV3D_ACT_GELU = 2, CCV3D
  *   k, n_out, rows: any number from 1 on (rows = 0: a call without work); k <= 65536, rows and n_out (gated: 2 n_out) below 2^31 - 2^16 - 256
  *   (F32: a third of that).
  * Products are exact, sums FP32: the tensor cores cut off what lies below a sum's last bit, 16 terms at a time, so that BF16 outputs lose up to
- * k 2^-28 of their terms' magnitude; F32 outputs are summed with rounding every 1024 terms (F32 operands: 128).  All behind the sums is FP32, the
+ * k 2^-28 of their terms' magnitude; F32 outputs are summed with rounding every 512 terms (F32 operands: 64), BF16 ones of up to some hundred rows every 1024.  All behind the sums is FP32, the
  * output is rounded once.  F32 operands go in as three BF16 numbers each (24 bits, exact), and products under 2^-24
  * of the whole are left out (few rows: FP32 arithmetic).  F32: an infinity may make its outputs NaN, and numbers under 2^-110 lose bits.
  *   ws      DEVICE scratch, 256-byte aligned, ccv3d_linear_workspace() bytes, of the call alone (NULL where that is 0)

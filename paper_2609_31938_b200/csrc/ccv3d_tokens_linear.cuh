@@ -18,8 +18,8 @@
 // (1.52), onto an F32 residual 414 us (1.28); 3520 x 1536 -> 6144 with GELU 52 us (4.5 turns of tiles take five); 64 rows on 180 MB of gated
 // weights 36 us (5 TB/s).  Tiles of 256 tokens want 92 GB/s of L2 for each SM, near what all of them get at once.
 //
-// F32 outputs: the tensor cores cut what they add to instead of rounding it, which shrinks long sums; so accumulators are handed over every
-// few K blocks and summed in registers with rounding.  F32 operands are split beforehand into three BF16 numbers each (8 + 8 + 8 bits,
+// F32 outputs, and few rows: the tensor cores cut what they add to instead of rounding it, which shrinks long sums; so accumulators are handed over
+// every few K blocks and summed in registers with rounding.  (BF16 outputs of many rows stay in them; 3520 x 1536 -> 6144 would take 6 % longer.)  F32 operands are split beforehand into three BF16 numbers each (8 + 8 + 8 bits,
 // exact); six of the nine products, smallest first, keep 2^-24.
 #pragma once
 #include "ccv3d_tc_ptx.cuh"
@@ -77,16 +77,18 @@ struct LinearWalk {
 
 template <int BT_, bool GATED_, int PARTS_, bool F32_OUT> struct LinearShape {
     static constexpr int BT = BT_, PARTS = PARTS_, SETS = GATED_ ? 2 : 1;
-    static constexpr bool GATED = GATED_, FOLD = F32_OUT;
+    static constexpr bool GATED = GATED_, F32 = F32_OUT, FOLD = F32_OUT || BT_ <= 64;
     static constexpr int COLS = SETS * BT;                                   // of an accumulator
     static constexpr int ROWB = PARTS == 3 ? 64 : 128, KB = ROWB / 2;        // bytes and elements of a row of a stage
     static constexpr uint32_t A_TILE = 128 * ROWB, B_TILE = BT / 2 * ROWB, A_BYTES = PARTS * SETS * A_TILE, STAGE = A_BYTES + PARTS * B_TILE;
     static constexpr int EPI_WARPS = FOLD && COLS == 256 ? 16 : 8, PARTS_OF_COLS = EPI_WARPS / 4, CW = BT / PARTS_OF_COLS;   // CW: tokens of a warp
-    static constexpr int LD = CW < 16 ? CW : 16, CH = FOLD || CW < 32 ? LD : 32;   // columns read at a time onto rounded sums; finished at a time
+    static constexpr int LD = CW < 16 ? CW : 16, CH = F32_OUT || CW < 32 ? LD : 32;   // columns read at a time onto rounded sums; finished at a time
     static constexpr int THREADS = 128 + 32 * EPI_WARPS;
     static constexpr uint32_t TMEM = 2 * COLS < 32 ? 32 : 2 * COLS;
-    // K blocks between hand-overs of a sum that is kept with rounding: 1024 terms of BF16, 128 of F32 (with their remainders)
-    static constexpr int HAND = FOLD ? (PARTS == 3 ? 4 : 16) : 1 << 30;
+    // K blocks between hand-overs of a sum that is kept with rounding: 64 terms of F32 (with their remainders), 512 of BF16 into F32 (errors half to all
+    // of those of FP32 arithmetic, which twice as many had more of: 4.5e-7 of the largest listed product against 3.6e-7, now 2.1e-7 at 3 % more
+    // time), 1024 into BF16 where rows are few and time goes by the weights' bytes
+    static constexpr int HAND = FOLD ? (PARTS == 3 ? 2 : F32_OUT ? 8 : 16) : 1 << 30;
     // outputs on their way: two boxes of 32 features and CH tokens for each warp
     static constexpr uint32_t BOX = 32 * CH * (F32_OUT ? 4 : 2), BOXES = 2 * EPI_WARPS * BOX;
     static constexpr int FIT = (int)((230400 - 1024 - BOXES) / STAGE), STAGES = FIT < LINEAR_MAX_STAGES ? FIT : LINEAR_MAX_STAGES;
@@ -385,61 +387,68 @@ linear_tile_kernel(const __grid_constant__ CUtensorMap tm_w, const __grid_consta
                     ask(c + 2 * S::CH, b);
                 }
             };
+            // (one accumulator's worth of a BF16 output: straight from tensor memory)
+            const bool whole = !S::FOLD || (!S::F32 && w.kb1 - w.kb0 <= S::HAND);
             if constexpr (S::FOLD) {
-                float sum[S::SETS][S::CW];
-#pragma unroll
-                for (int h = 0; h < S::SETS; ++h)
-#pragma unroll
-                    for (int j = 0; j < S::CW; ++j) sum[h][j] = 0.f;
-                for (int kb = w.kb0; kb < w.kb1; kb += S::HAND) {
-                    if (!(ok = linear_warp_wait(&sh->acc_full[acc], ph, sh, p))) break;
-                    tc_fence_after();
+                if (!whole) {
+                    float sum[S::SETS][S::CW];
 #pragma unroll
                     for (int h = 0; h < S::SETS; ++h)
 #pragma unroll
-                        for (int c = 0; c < S::CW; c += S::LD) {
-                            uint32_t v[32];
-                            tc_ld<S::LD>(mine + acc * S::COLS + h * S::BT + c, v);
-                            tc_wait_ld();
+                        for (int j = 0; j < S::CW; ++j) sum[h][j] = 0.f;
+                    for (int kb = w.kb0; kb < w.kb1; kb += S::HAND) {
+                        if (!(ok = linear_warp_wait(&sh->acc_full[acc], ph, sh, p))) break;
+                        tc_fence_after();
 #pragma unroll
-                            for (int j = 0; j < S::LD; ++j) sum[h][c + j] += __uint_as_float(v[j]);
-                        }
-                    tc_fence_before();
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive_leader(smem_u32(&sh->acc_empty[acc]));
-                    acc ^= 1;
-                    if (acc == 0) ph ^= 1;
-                }
-                if (ok) {
+                        for (int h = 0; h < S::SETS; ++h)
 #pragma unroll
-                    for (int c = 0; c < S::CW; c += S::CH) {
-                        float g[S::CH], u[S::CH];
+                            for (int c = 0; c < S::CW; c += S::LD) {
+                                uint32_t v[32];
+                                tc_ld<S::LD>(mine + acc * S::COLS + h * S::BT + c, v);
+                                tc_wait_ld();
 #pragma unroll
-                        for (int j = 0; j < S::CH; ++j) { g[j] = sum[0][c + j]; u[j] = sum[S::SETS - 1][c + j]; }
-                        leave(c, g, u);
-                    }
-                }
-            } else {
-                if (!(ok = linear_warp_wait(&sh->acc_full[acc], ph, sh, p))) break;
-                tc_fence_after();
-#pragma unroll 1
-                for (int c = 0; c < S::CW; c += S::CH) {
-                    uint32_t v[2][32];
-#pragma unroll
-                    for (int h = 0; h < S::SETS; ++h) tc_ld<S::CH>(mine + acc * S::COLS + h * S::BT + c, v[h]);
-                    tc_wait_ld();
-                    if (c + S::CH == S::CW) {
+                                for (int j = 0; j < S::LD; ++j) sum[h][c + j] += __uint_as_float(v[j]);
+                            }
                         tc_fence_before();
                         __syncwarp();
                         if (lane == 0) mbar_arrive_leader(smem_u32(&sh->acc_empty[acc]));
+                        acc ^= 1;
+                        if (acc == 0) ph ^= 1;
                     }
-                    float g[S::CH], u[S::CH];
+                    if (ok) {
 #pragma unroll
-                    for (int j = 0; j < S::CH; ++j) { g[j] = __uint_as_float(v[0][j]); u[j] = __uint_as_float(v[S::SETS - 1][j]); }
-                    leave(c, g, u);
+                        for (int c = 0; c < S::CW; c += S::CH) {
+                            float g[S::CH], u[S::CH];
+#pragma unroll
+                            for (int j = 0; j < S::CH; ++j) { g[j] = sum[0][c + j]; u[j] = sum[S::SETS - 1][c + j]; }
+                            leave(c, g, u);
+                        }
+                    }
                 }
-                acc ^= 1;
-                if (acc == 0) ph ^= 1;
+            }
+            if constexpr (!S::FOLD || !S::F32) {
+                if (whole) {
+                    if (!(ok = linear_warp_wait(&sh->acc_full[acc], ph, sh, p))) break;
+                    tc_fence_after();
+#pragma unroll 1
+                    for (int c = 0; c < S::CW; c += S::CH) {
+                        uint32_t v[2][32];
+#pragma unroll
+                        for (int h = 0; h < S::SETS; ++h) tc_ld<S::CH>(mine + acc * S::COLS + h * S::BT + c, v[h]);
+                        tc_wait_ld();
+                        if (c + S::CH == S::CW) {
+                            tc_fence_before();
+                            __syncwarp();
+                            if (lane == 0) mbar_arrive_leader(smem_u32(&sh->acc_empty[acc]));
+                        }
+                        float g[S::CH], u[S::CH];
+#pragma unroll
+                        for (int j = 0; j < S::CH; ++j) { g[j] = __uint_as_float(v[0][j]); u[j] = __uint_as_float(v[S::SETS - 1][j]); }
+                        leave(c, g, u);
+                    }
+                    acc ^= 1;
+                    if (acc == 0) ph ^= 1;
+                }
             }
         }
         if (lane == 0) bulk_wait_read<0>();          // (the boxes' places are this block's)
@@ -490,9 +499,9 @@ __global__ void __launch_bounds__(256) linear_join_kernel(const __grid_constant_
 
 // Few rows of F32: bound by the weights' bytes, which splitting them would double and double again; so in plain FP32 arithmetic.  A thread has
 // two features of a tile of 256 and BT tokens.  Weights come in by cp.async, K blocks of 32, in rows of 128 bytes whose 16-byte pieces are
-// swapped by row so that eight threads read eight banks' worth; tokens through registers, one block ahead.  Sums of 256 terms are added up
-// apart.
-constexpr int LINEAR_FEW_K = 32, LINEAR_FEW_FOLD = 8, LINEAR_FEW_THREADS = 128, LINEAR_FEW_STAGES = 3;
+// swapped by row so that eight threads read eight banks' worth; tokens through registers, one block ahead.  Sums of 64 terms are added up
+// apart (of 256, in the same time, errors were 1.3 to 1.8 times as large).
+constexpr int LINEAR_FEW_K = 32, LINEAR_FEW_FOLD = 2, LINEAR_FEW_THREADS = 128, LINEAR_FEW_STAGES = 3;
 template <bool GATED, int BT>
 __global__ void __launch_bounds__(LINEAR_FEW_THREADS) linear_few_kernel(const __grid_constant__ LinearParams p, const float* x, int64_t x_stride, const float* w,
                                                                         int64_t w_stride, int k) {
