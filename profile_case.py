@@ -5,7 +5,7 @@
     python profile_case.py --operator attend-step-b64
 
 Inputs are the seeded synthetic tensors of the benchmark (normal activations, fan-in-scaled weights).  --operator runs a
-case of perf/operators.py (a token operator) instead of a layer.
+case of perf/operators.py or perf/more_operators.py (a token operator) instead of a layer.
 """
 import argparse
 import os
@@ -18,14 +18,15 @@ sys.path.insert(0, os.path.dirname(os.path.abspath(__file__)))
 
 def run_operator(name, calls):
     import torch
-    from perf import operators
+    from perf import more_operators, operators
+    from paper_2609_31938_b200 import tokens
+    operators, case = next((m, c) for m in (operators, more_operators) for c in m.listed() if c["name"] == name)
     operators.own = True
-    case = next(c for c in operators.listed() if c["name"] == name)
     state = operators.prepare(case, 1)
     for _ in range(calls):
         operators.run(state)
     torch.cuda.synchronize()
-    assert "cache" not in state or state["cache"].status() == 0
+    assert tokens.status() == 0 and all(state[k].status() == 0 for k in ("cache", "memory") if k in state)
     print("ok", name)
 
 
@@ -47,7 +48,7 @@ def main():
     ap.add_argument("--f32", action="store_true", help="FP32 layer (tensor cores by 3xTF32 when the call is large enough)")
     ap.add_argument("--stride", type=int, nargs=3, default=[1, 1, 1], help="(s_t, s_h, s_w)")
     ap.add_argument("--dilation", type=int, nargs=3, default=[1, 1, 1], help="(d_t, d_h, d_w); size-preserving padding")
-    ap.add_argument("--operator", help="a case of perf/operators.py by its name")
+    ap.add_argument("--operator", help="a case of perf/operators.py or perf/more_operators.py by its name")
     a = ap.parse_args()
     if a.operator:
         return run_operator(a.operator, a.calls)
