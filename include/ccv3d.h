@@ -562,15 +562,16 @@ typedef enum { CCV3D_ACT_NONE = 0, CCV3D_ACT_SILU = 1, CCV3D_ACT_GELU = 2, CCV3D
  *   Rows of x and w are dense; their strides (in elements) and addresses are multiples of 16 bytes; out and residual go by elements.
  *   k, n_out, rows: any number from 1 on (rows = 0: a call without work); k <= 65536, rows and n_out (gated: 2 n_out) below 2^31 - 2^16 - 256
  *   (F32: a third of that).
- * Products are exact, sums FP32: the tensor cores cut off what lies below a sum's last bit, 16 terms at a time, so that BF16 outputs lose up to
- * k 2^-28 of their terms' magnitude; F32 outputs are summed with rounding every 512 terms (F32 operands: 64), BF16 ones of up to some hundred rows every 1024.  All behind the sums is FP32, the
- * output is rounded once.  F32 operands go in as three BF16 numbers each (24 bits, exact), and products under 2^-24
- * of the whole are left out (few rows: FP32 arithmetic).  F32: an infinity may make its outputs NaN, and numbers under 2^-110 lose bits.
+ * Products are exact, sums FP32: the tensor cores cut off what lies below a sum's last bit, 16 terms at a time, so that BF16 outputs lose
+ * up to k 2^-28 of their terms' magnitude; F32 outputs are summed with rounding every 512 terms (F32 operands: 64), BF16 ones of up to some
+ * hundred rows every 1024.  All behind the sums is FP32, the output is rounded once.  F32 operands go in as three BF16 numbers each (24
+ * bits, exact), and products under 2^-24 of the whole are left out (few rows: FP32 arithmetic).  F32: an infinity may make its outputs NaN,
+ * and numbers under 2^-110 lose bits.
  *   ws      DEVICE scratch, 256-byte aligned, ccv3d_linear_workspace() bytes, of the call alone (NULL where that is 0)
  *   status  DEVICE word or NULL: receives CCV3D_TOKENS_TIMEOUT; ccv3d_linear_status_word() has one to lend
- * Any other overlap of out or ws with another tensor is CCV3D_ERR_ALIAS.  Results do not depend on what else runs, the same call gives
- * the same bits; a row has the same whatever the other rows hold, how rows are grouped in calls may change last bits.  Stream-ordered, no
- * allocation, legal in a stream capture.
+ * Any other overlap of out or ws with another tensor is CCV3D_ERR_ALIAS (of their ranges of bytes: slices of one wider matrix are refused).
+ * Results do not depend on what else runs, the same call gives the same bits; a row has the same whatever the other rows hold, how rows are
+ * grouped in calls may change last bits.  Stream-ordered, no allocation, legal in a stream capture.
  */
 typedef struct {
     int32_t rows, n_out, k;
@@ -593,8 +594,9 @@ ccv3d_status ccv3d_linear_workspace(const ccv3d_linear_desc* d, uint64_t* bytes_
 /*
  * Attention whose memory is one state of fixed size for each sequence and head, from which old tokens fade:
  *   S_t = exp(g_t) S_{t-1} + k_t v_t^T        out_t = scale * q_t S_t             S [key_dim, value_dim], FP32
- * over the new tokens of each sequence in order, g the token's and head's log decay (FP32; <= 0 in ordinary use, a state grows with positive
- * ones, up to 88; what lies under -104, minus infinity too, forgets all that was before; NaN spoils it from there on until it is forgotten).  What kv_attend is to a cache that grows, this is to a stream of any length.
+ * over the new tokens of each sequence in order, g the token's and head's log decay (FP32; <= 0 in ordinary use, a state grows with
+ * positive ones, up to 88; what lies under -104, minus infinity too, forgets all that was before; NaN spoils it from there on until it is
+ * forgotten).  What kv_attend is to a cache that grows, this is to a stream of any length.
  * states [slots][heads][key_dim][value_dim], DEVICE FP32, 16-byte aligned: sequence b reads slot[b] and leaves its state after
  * its last token there; a sequence without new tokens leaves it as it was.  `fresh` (may be NULL): where fresh[b] is not 0, the
  * sequence starts from zeros whatever its slot holds.
@@ -604,10 +606,11 @@ ccv3d_status ccv3d_linear_workspace(const ccv3d_linear_desc* d, uint64_t* bytes_
  *   new_start [batch + 1], slot [batch], fresh [batch]: DEVICE int32, checked by the kernels: offsets out of range are cut, a slot outside the pool, or one that
  *          an earlier sequence of the call (with new tokens) has, is not touched (its sequence starts from zeros and its state is lost), both are reported.
  *          Rows of out that belong to no sequence are not written.
- * All sums and states are FP32; dtype F32: products to 2^-23; BF16 (from some 20 new tokens on): scores and the state are taken to 2^-16 for the outputs and to 2^-23 for the new state.  F32: numbers beyond
- * 3.38e38 may count as infinite, and those under 2^-110 lose bits.
+ * All sums and states are FP32; dtype F32: products to 2^-23; BF16 (from some 20 new tokens on): scores and the state are taken to 2^-16
+ * for the outputs and to 2^-23 for the new state.  F32: numbers beyond 3.38e38 may count as infinite, and those under 2^-110 lose bits.  A
+ * query that is not finite may make its outputs NaN where they were infinite.
  *   ws      DEVICE scratch, 256-byte aligned, ccv3d_decay_attend_workspace() bytes, of the call alone (NULL where that is 0)
- * An overlap of out, states or ws with another tensor is CCV3D_ERR_ALIAS.  Stream-ordered, no allocation, legal in a stream capture.
+ * An overlap of out, states or ws with another tensor (of their ranges of bytes) is CCV3D_ERR_ALIAS.  Stream-ordered, no allocation, legal in a stream capture.
  */
 typedef struct {
     float*  states;
@@ -635,7 +638,7 @@ ccv3d_status ccv3d_decay_attend_workspace(const ccv3d_decay_memory* memory, cons
  * x, y [samples, pixels, channels] in dtype with strides in elements, channels dense (any strides and alignment; fastest where rows start
  * on 16 bytes); weight, bias [channels] FP32 or NULL; scale, shift [samples, channels] FP32 (a stride between samples) or NULL.
  * Statistics and all arithmetic are FP32, the variance is taken around the mean; the output is rounded once.  A NaN or infinity makes
- * its sample and group NaN.  y may be x itself (same strides).  Any other overlap is CCV3D_ERR_ALIAS.
+ * its sample and group NaN.  y may be x itself (same strides).  Any other overlap (of ranges of bytes) is CCV3D_ERR_ALIAS.
  *   groups divides channels; channels <= 16384; samples and pixels from 0 (samples or pixels 0: a call without work)
  *   ws      DEVICE scratch, 256-byte aligned, ccv3d_group_norm_workspace() bytes, of the call alone (NULL where that is 0)
  * A sample gives the same bits whatever is normed beside it.  Stream-ordered, no allocation, legal in a stream capture.

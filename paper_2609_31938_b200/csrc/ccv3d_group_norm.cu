@@ -10,7 +10,7 @@ constexpr int GN_SMEM = 100 * 1024;
 constexpr int GN_PIECES = 8;             // most pieces of a thread in the one-pass form
 
 // How a call is cut up.  It goes by the sample's size and type alone, not by how many samples there are (but for how many go at once), so that
-// a stream of frames has the same bits however it is cut into calls.
+// a stream of frames has the same bits however it is cut into calls; nor by the device, whose 148 SMs and L2 stand here as numbers.
 struct GnPlan {
     bool vec, token, whole;
     int V, columns, lanes, chunks;       // chunks: of columns (token and three-kernel forms)

@@ -8,7 +8,7 @@
 // decay_chunk_kernel does so as mma.sync products of BF16 with FP32 sums.  A warp owns 16 value columns of S^T, in registers as the products leave them, which is also
 // the layout that the next product wants them in as its B operand: the state never leaves the registers.  What is not BF16 already goes in
 // as three BF16 numbers, 8 bits each, of whose nine products six are taken (BF16 inputs: scores with their decay and S as two, v with its
-// decay as three).  F32, 24 prompts of up to 700 tokens, 14 heads of 64 x 128: 328 us, bound by the latency of eight warps' products.
+// decay as three).  F32, 24 prompts of up to 700 tokens, 14 heads of 64 x 128: 330 us, bound by the latency of eight warps' products.
 // G is summed in 64 bits and kept as two floats, so that differences of sums that a strong decay made large still have all their bits.
 //
 // Where sequences and heads are too few for the machine, sequences of more than a segment are cut: their segments' contributions to the state side by
@@ -103,8 +103,7 @@ __device__ __forceinline__ bool decay_steep(float rise) {
 
 // ---------------------------------------------------------------------------------------------------- single tokens
 // Block (sequence, head, 64 value columns): thread t has columns 4 (t % 16) .. + 3 of rows R (t / 16) + i, whose keys and queries it reads four at
-// a time (one by one, the way to shared memory bounds prompts:   Up to eight tokens are brought in at
-// a time, and their outputs' parts summed together.
+// a time (one by one, the way to shared memory bounds prompts).  Up to eight tokens are brought in at a time, and their outputs' parts summed together.
 constexpr int DECAY_STEP_TOKENS = 8;
 template <typename T, int DK>
 __global__ void __launch_bounds__(DECAY_STEP_THREADS) decay_step_kernel(const __grid_constant__ DecayParams p) {

@@ -14,13 +14,16 @@
 // Tiles go round the pairs in turn; those of the last, unfilled turn are cut along K into equal shares of K blocks, whose sums
 // linear_join_kernel adds in order (no atomics: the same bits every run).
 //
-// Measured (BF16): 9472 x 4096 -> 4096 198 us = 1.61 PFLOP/s, 98 % of a plain library product's rate; 28160 x 6144 -> 1536 350 us
-// (1.52), onto an F32 residual 414 us (1.28); 3520 x 1536 -> 6144 with GELU 52 us (4.5 turns of tiles take five); 64 rows on 180 MB of gated
-// weights 36 us (5 TB/s).  Tiles of 256 tokens want 92 GB/s of L2 for each SM, near what all of them get at once.
+// Measured (BF16), in short bursts at up to 1965 MHz: 9472 x 4096 -> 4096 199 us = 1.60 PFLOP/s, 97 % of a plain library product's rate;
+// 28160 x 6144 -> 1536 341 us (1.56); 3520 x 1536 -> 6144 with GELU 52 us (1.28: 4.5 turns of tiles take five); gated, with SiLU, 103 us (1.29);
+// 64 rows on 180 MB of gated weights 35 us (5.2 TB/s).  Again and again, under the power cap: with GELU 58 us at 1590 MHz, 28160 x 6144 -> 1536 onto an
+// F32 residual 495 us (1.07) at 1350 MHz.  Tiles of 256 tokens want 92 GB/s of L2 for each SM, near what all of them get
+// at once.
 //
-// F32 outputs, and few rows: the tensor cores cut what they add to instead of rounding it, which shrinks long sums; so accumulators are handed over
-// every few K blocks and summed in registers with rounding.  (BF16 outputs of many rows stay in them; 3520 x 1536 -> 6144 would take 6 % longer.)  F32 operands are split beforehand into three BF16 numbers each (8 + 8 + 8 bits,
-// exact); six of the nine products, smallest first, keep 2^-24.
+// F32 outputs, and few rows: the tensor cores cut what they add to instead of rounding it, which shrinks long sums; so accumulators are
+// handed over every few K blocks and summed in registers with rounding.  (BF16 outputs of many rows stay in them; 3520 x 1536 -> 6144
+// would take 6 % longer.)  F32 operands are split beforehand into three BF16 numbers each (8 + 8 + 8 bits, exact); six of the nine
+// products, smallest first, keep 2^-24.
 #pragma once
 #include "ccv3d_tc_ptx.cuh"
 #include "ccv3d_tokens_activation.cuh"
